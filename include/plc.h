@@ -47,7 +47,7 @@ enum {
 };
 
 enum { PLC_PRED_TOPK = 0, PLC_PRED_DENSE = 1, PLC_PRED_LINEAR = 2 };
-enum { PLC_OUT_F32 = 0, PLC_OUT_F16 = 1 };
+enum { PLC_OUT_F32 = 0, PLC_OUT_F16 = 1, PLC_OUT_BF16 = 2 };   /* BF16: paged cache and beam search only */
 
 /* Codec parameters.  delta: quantiser step (>= 2^-12).  sigma_floor: added in quadrature to the
  * mixture's standard deviation before the scale class is taken (0 = none).  chunk_pos: positions
@@ -344,6 +344,117 @@ plc_status plc_append_sizes(const plc_ctx* ctx, int32_t B, uint64_t* open_sym_by
 plc_status plc_rans_encode_static(const int32_t* sym_dev, const int32_t* q_dev, int32_t n_streams, int32_t n_pos,
                                   int32_t head_dim, int32_t chunk_capacity, int32_t chunk_index,
                                   const plc_streams* out, uint32_t* status_dev, void* stream);
+
+/* ---- Paged cache: pages of positions that sessions share, attention over them, beam search. ----------------
+ * These calls need no plc_ctx and allocate nothing: whatever they work in is passed by the caller (16-byte
+ * aligned, at least the stated bytes, not used by another call that may run at the same time).  They can be
+ * captured into a graph.  Data-dependent problems are OR-ed into *status_dev, a device word of the caller's
+ * (zeroed by the caller; bits below), and nothing outside the stated extents is read or written:
+ *   1   too few free pages, or a row wider than max_pages (plc_pages_fork: see there)
+ *   8   a bounded wait inside a kernel ran out (the call's output is incomplete)
+ *   32  a page number, parent, path, length or row range out of range (per call: what then happens) */
+
+/* Pool of n_pages pages of page_pos positions each.  The view's session index is the page and its position index
+ * the slot in the page: element (layer, kv, page, head, slot, component) stands at
+ * layer*stride_layer + kv*stride_kv + page*stride_session + head*stride_head + slot*stride_pos + component.
+ * Heads first and slots first are both only strides; where stride_session = page_pos*stride_pos, a run of pages
+ * is a plain KV tensor that plc_decode can restore into.  dtype: PLC_OUT_F32, PLC_OUT_F16 or PLC_OUT_BF16.
+ * n_pages, page_pos >= 1; head_dim as in plc_config. */
+typedef struct {
+    plc_kv_view view;
+    int32_t n_layers, n_kv_heads, head_dim, n_pages, page_pos, dtype;
+} plc_page_pool;
+
+/* Who holds which page: table_dev [rows][max_pages] int32, the pages of each row in order, -1 behind them;
+ * len_dev [rows] committed positions; ref_dev [n_pages] how many table entries name the page (0 = free; a caller
+ * that holds on to a page itself adds one).  Calls read one book and write another: its arrays must not overlap
+ * the first one's, and the first stays valid until a page that only it names is taken by a later call. */
+typedef struct {
+    int32_t* table_dev;
+    int32_t* len_dev;
+    int32_t* ref_dev;
+    int32_t rows, max_pages;
+} plc_page_book;
+
+/* Row s of `out` continues row parent_dev[s] of `in` (-1: an empty row; a row that nobody continues is released).
+ * Its full pages are shared.  A partly filled last page goes to the first row s that continues it if no other holder
+ * is left (ref 1), and is copied (all layers, the used slots) to a fresh page for every other one, so that every row
+ * can write behind its length.  room_dev [out->rows] or NULL (0): every row gets fresh pages for that many positions
+ * more; pages that a row of `in` holds behind its length are not passed on.  Fresh pages are the lowest-numbered free ones of
+ * `in`, in order of s, a row's copied page first; pages that become free in this call can be taken by the next.
+ * out->max_pages = in->max_pages.  If the free pages do not suffice or a row would need more than max_pages pages,
+ * bit 1 is set, every row of `out` is empty, out's counts are in's and the pool is as before: `in` can still be used.
+ * A parent, length or room out of range makes that row empty (bit 32); page numbers out of range are dropped (bit 32).
+ * workspace: plc_pages_workspace bytes. */
+plc_status plc_pages_fork(const plc_page_pool* pool, const plc_page_book* in, const int32_t* parent_dev, const int32_t* room_dev,
+                          const plc_page_book* out, void* workspace_dev, uint64_t workspace_bytes, uint32_t* status_dev,
+                          void* stream);
+
+/* Verified drafts: path_dev [rows][path_stride], n_path_dev [rows].  Of the positions behind row s's length, those
+ * at len + path[s][0], len + path[s][1], ... (strictly rising, < the room) are kept and move, in every layer, to len, len + 1, ...;
+ * the length grows by n_path, pages behind it are released.  A path that does not rise, that leaves the row's pages
+ * or would write to a page with other holders, and n_path outside [0, path_stride], leave the row as it is (bit 32). */
+plc_status plc_pages_keep(const plc_page_pool* pool, const plc_page_book* in, const int32_t* path_dev, const int32_t* n_path_dev,
+                          int32_t path_stride, const plc_page_book* out, uint32_t* status_dev, void* stream);
+
+/* Moves the pages in use to the lowest numbers: with n of them, page n or higher moves to a free page below n, in rising
+ * order on both sides.  moved_dev [n_pages]: the new number of every page, -1 for free ones (for numbers that the
+ * caller keeps itself).  workspace: plc_pages_workspace bytes.  Page numbers out of range become -1 (bit 32). */
+plc_status plc_pages_compact(const plc_page_pool* pool, const plc_page_book* in, const plc_page_book* out, int32_t* moved_dev,
+                             void* workspace_dev, uint64_t workspace_bytes, uint32_t* status_dev, void* stream);
+/* Bytes of workspace for plc_pages_fork and plc_pages_compact on books of up to rows_in and rows_out rows. */
+plc_status plc_pages_workspace(int32_t n_pages, int32_t rows_in, int32_t rows_out, uint64_t* bytes);
+
+/* Drafted tokens that attend to their session's pages.  Session s (a row of the book) has the query rows
+ * begin_dev[s] .. begin_dev[s+1]-1 (begin_dev [rows+1], rising, <= n_rows; n_s of them); the keys and values of its
+ * drafted tokens already stand in its pages at positions len .. len + n_s - 1.  Query i sees every position below len
+ * and the drafted positions j whose bit is set in row i of mask_dev [n_rows][mask_words] (bit j of word j/32; bits that
+ * the words do not hold are 0); mask_dev NULL: j <= i, so that n_s = 1 is plain decoding and larger n_s a chain or a chunk of a
+ * prompt.  q_dev, out_dev: [n_rows][n_heads][head_dim] of the pool's type (f16 or bf16), strides in elements,
+ * 16-byte aligned vectors; query head h reads KV head h / (n_heads / n_kv_heads).  lse_dev [n_rows][n_heads] float or NULL. */
+typedef struct {
+    const void* q_dev;
+    int64_t q_stride_row, q_stride_head;
+    void* out_dev;
+    int64_t out_stride_row, out_stride_head;
+    float* lse_dev;
+    const int32_t* begin_dev;
+    const uint32_t* mask_dev;
+    int32_t n_rows, n_heads, mask_words;
+} plc_tree_queries;
+
+/* out = sum_t softmax_t(scale q.k_t) v_t over the positions that a query sees, lse = log sum_t exp(scale q.k_t); a
+ * query that sees none gets 0 and -inf.  What is not seen has no influence, infinities and NaN included.  Scores,
+ * maxima and sums are binary32; the weights are rounded to the pool's type for the product with v.  Rows of q outside every
+ * session's range are not written.  A row range, length or page number out of range (bit 32): ranges and lengths are cut
+ * to what there is, positions without a page are not seen.  workspace: plc_tree_attention_workspace bytes. */
+plc_status plc_tree_attention(const plc_page_pool* pool, int32_t layer, const plc_page_book* book, const plc_tree_queries* queries,
+                              float scale, void* workspace_dev, uint64_t workspace_bytes, uint32_t* status_dev, void* stream);
+plc_status plc_tree_attention_workspace(const plc_page_pool* pool, int32_t n_heads, uint64_t* bytes);
+
+/* One step of beam search for `sessions` sessions of `beams` beams: of the beams*vocab continuations with
+ *     score_dev[b][w] + logits[b][w][v] - log sum_v' exp logits[b][w][v']
+ * the n_out largest, in falling order, ties to the lowest (w, v); formed and compared in binary64 from the row's
+ * log-sum-exp.  logits_dev: [sessions*beams] rows of row_stride elements, dtype as plc_page_pool.  done_dev [sessions][beams]
+ * bytes or NULL: a beam that is done has one continuation, the token `eos`, at its own score.  A score that is not
+ * finite (a dead beam's -inf, a row with NaN or +inf) is none.  Outputs [sessions][n_out]: the score (binary32), the parent
+ * as a row b*beams + w (for plc_pages_fork and plc_beam_reorder) and the token; places without a continuation get
+ * -inf, -1, -1.  beams, n_out <= 128.  workspace: plc_beam_workspace bytes. */
+plc_status plc_beam_select(const void* logits_dev, int32_t dtype, int64_t row_stride, int32_t sessions, int32_t beams, int32_t vocab,
+                           const float* score_dev, const uint8_t* done_dev, int32_t eos, int32_t n_out, float* out_score_dev,
+                           int32_t* out_parent_dev, int32_t* out_token_dev, void* workspace_dev, uint64_t workspace_bytes, void* stream);
+plc_status plc_beam_workspace(int32_t sessions, int32_t beams, int32_t vocab, int32_t n_out, uint64_t* bytes);
+
+/* States that follow their beams: row r of each dst becomes row parent_dev[r] of its src (zeros for -1), all sets in one
+ * launch.  Strides and row_bytes in bytes, any alignment; a dst must not overlap any src.  n_sets <= 16.  A parent outside
+ * [-1, rows_in) counts as -1 (bit 32; status_dev may be NULL here). */
+typedef struct {
+    const void* src_dev;
+    void* dst_dev;
+    int64_t src_stride, dst_stride, row_bytes;
+} plc_row_set;
+plc_status plc_beam_reorder(const plc_row_set* sets, int32_t n_sets, const int32_t* parent_dev, int32_t rows_in, int32_t rows_out,
+                            uint32_t* status_dev, void* stream);
 
 /* Waits for the stream and returns the device status word's most severe code; clears it.
  * PLC_E_ALIGN here means that *total_bytes_dev was not a multiple of 16 when an encoder reserved a

@@ -12,11 +12,12 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _CSRC = os.path.join(_HERE, "csrc")
 _INC = os.path.join(os.path.dirname(_HERE), "include")
 _SO = os.path.join(_HERE, "libplc.so")
-_SOURCES = ["plc_api.cu", "plc_topk.cu", "plc_prefix.cu", "plc_codec.cu", "plc_coop.cu", "plc_dense.cu", "plc_static.cu", "plc_trie.cu"]
+_SOURCES = ["plc_api.cu", "plc_topk.cu", "plc_prefix.cu", "plc_codec.cu", "plc_coop.cu", "plc_dense.cu", "plc_static.cu", "plc_trie.cu",
+            "plc_pages.cu", "plc_attend.cu", "plc_beam.cu"]
 
 OK, E_INVALID, E_SHAPE, E_ALIGN, E_CAPACITY, E_CORRUPT, E_STATE, E_CUDA = range(8)
 PRED_TOPK, PRED_DENSE, PRED_LINEAR = 0, 1, 2
-OUT_F32, OUT_F16 = 0, 1
+OUT_F32, OUT_F16, OUT_BF16 = 0, 1, 2
 
 EXPORTS = ["plc_create", "plc_destroy", "plc_reserve", "plc_topk_softmax", "plc_prefix_dedup", "plc_encode",
            "plc_decode", "plc_append_step", "plc_append_flush", "plc_append_sizes", "plc_sync_status",
@@ -24,7 +25,9 @@ EXPORTS = ["plc_create", "plc_destroy", "plc_reserve", "plc_topk_softmax", "plc_
            "plc_launch_count", "plc_rans_encode_static", "plc_encode_adaptive", "plc_decode_adaptive",
            "plc_trie_create", "plc_trie_destroy", "plc_trie_insert", "plc_trie_best_match", "plc_trie_evict",
            "plc_trie_stats", "plc_create_linear", "plc_prefix_clusters", "plc_rotq_record_bytes", "plc_encode_rotq",
-           "plc_decode_rotq", "plc_poll_status", "plc_last_schedule", "plc_kernel_ms"]
+           "plc_decode_rotq", "plc_poll_status", "plc_last_schedule", "plc_kernel_ms", "plc_pages_workspace", "plc_pages_fork",
+           "plc_pages_keep", "plc_pages_compact", "plc_tree_attention", "plc_tree_attention_workspace", "plc_beam_workspace",
+           "plc_beam_select", "plc_beam_reorder"]
 
 
 def sources():
@@ -34,7 +37,7 @@ def sources():
 def build(force=False, verbose=False):
     """Compile libplc.so for sm_100a with nvcc (in-tree)."""
     srcs = sources()
-    deps = srcs + [os.path.join(_CSRC, h) for h in ("plc_common.cuh", "plc_coder.cuh", "plc_codec.cuh")] + [os.path.join(_INC, "plc.h")]
+    deps = srcs + [os.path.join(_CSRC, h) for h in ("plc_common.cuh", "plc_coder.cuh", "plc_codec.cuh", "plc_pages.cuh")] + [os.path.join(_INC, "plc.h")]
     if not force and os.path.exists(_SO) and all(os.path.getmtime(_SO) >= os.path.getmtime(d) for d in deps):
         return _SO
     cmd = ["nvcc", "-t", "0", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -428,3 +431,6 @@ def build_table(qp):
 
 def launch_count():
     return int(lib().plc_launch_count())
+
+
+from .serving import PageBook, PagePool, beam_reorder, beam_select  # noqa: E402,F401  (they use the names above)

@@ -21,7 +21,7 @@ constexpr int kSymLimit = 1 << 30;
 constexpr uint32_t kFull = 0xffffffffu;
 
 // Bits of the device status word.
-constexpr uint32_t kStCapacity = 1u, kStCorrupt = 2u, kStBadClass = 4u, kStTimeout = 8u, kStCursor = 16u;
+constexpr uint32_t kStCapacity = 1u, kStCorrupt = 2u, kStBadClass = 4u, kStTimeout = 8u, kStCursor = 16u, kStRange = 32u;
 
 // Device counters (plc_stats).
 struct Counters {

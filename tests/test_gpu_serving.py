@@ -1,0 +1,635 @@
+"""Paged cache, tree attention and beam search on the GPU against the oracle's literal definitions (binary64).
+
+Tolerances.  Books, counts, moved pages, parents and tokens: equal.  Copied page data: equal bit for bit, everything else in
+the pool untouched.  Attention, per output component, with u = half a step of the type (2^-11 f16, 2^-8 bf16, relative):
+  * scores are sums of d binary32 products: off by at most d 2^-23 of the sum of |q k| scale (the tensor cores' alignment
+    of addends loses at most one more bit than 2^-24 each), and the exponential of a binary32 argument x below
+    the maximum by 2^-23 |x| + 2^-22: a weight is off by a relative e = 2 (d 2^-23 B + 2^-22 + 2^-23 X), B the row's largest sum of
+    |q k| scale and X <= 2 B the span of its scores; twice, because the normaliser is off by as much;
+  * each weight is rounded to the type (u), the sum over positions is binary32 (n 2^-23), the result is rounded (u):
+    |out - exact| <= (u + e + n 2^-23) sum |p v| + u |exact| + half the smallest step of the type;
+  * |lse - exact| <= e + n 2^-23 + 2^-22 |exact|.
+Scores of beams: binary32 exponentials off by 2^-21 relative (argument up to 2^3 half steps where the terms count, 2 ulp of the
+function), the result rounded: |score - exact| <= 2^-20 + 2^-23 |exact|.  Orders: the inputs' scores are farther apart than 2^-18 or equal
+by construction, which is asserted on the oracle's.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_15356_b200 as plc
+from paper_2604_15356_b200 import synth
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    plc.build()
+    return torch.device("cuda:0")
+
+
+@pytest.fixture(scope="module")
+def ora():
+    from oracle import serving
+    return serving
+
+
+def i32(v, dev):
+    return torch.as_tensor(np.asarray(v), dtype=torch.int32).to(dev)
+
+
+def make_pool(rng, L, pages, H, page, d, dtype, dev, slots_first, fill=None):
+    """kv [L][2][P][H][page][d] with a margin of one layer behind it that no call may touch."""
+    shape = (L + 1, 2, pages, page, H, d) if slots_first else (L + 1, 2, pages, H, page, d)
+    base = torch.full(shape, float("nan"), dtype=TYPES[dtype]) if fill == "nan" else torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).to(TYPES[dtype])
+    base = base.to(dev)
+    kv = base.transpose(3, 4) if slots_first else base
+    return kv[:L], base
+
+
+def make_book(rng, held, cols, pages, dev):
+    order = rng.permutation(pages)
+    table = np.full((len(held), cols), -1, np.int32)
+    at = 0
+    for s, n in enumerate(held):
+        table[s, :n] = order[at:at + n]
+        at += n
+    ref = np.bincount(table[table >= 0], minlength=pages).astype(np.int32)
+    return table, ref
+
+
+def book_of(table, length, ref, dev):
+    return plc.PageBook(i32(table, dev), i32(length, dev), i32(ref, dev))
+
+
+def same_book(b, table, length, ref):
+    assert np.array_equal(b.table.cpu().numpy(), table)
+    assert np.array_equal(b.len.cpu().numpy(), length)
+    assert np.array_equal(b.ref.cpu().numpy(), ref)
+
+
+# ---------------------------------------------------------------------------------------------- attention
+
+def tree_mask(rng, begin, words, empty=()):
+    """Ancestors of random trees; the rows in `empty` see nothing drafted."""
+    N = begin[-1]
+    bits = np.zeros((N, words * 32), bool)
+    for s in range(len(begin) - 1):
+        for i in range(begin[s + 1] - begin[s]):
+            up = rng.integers(-1, i) if i else -1
+            if up >= 0:
+                bits[begin[s] + i] = bits[begin[s] + up]
+            if i < words * 32:
+                bits[begin[s] + i, i] = True
+    for r in empty:
+        bits[r] = False
+    w = np.packbits(bits, axis=1, bitorder="little").view(np.int32) if N else np.zeros((0, words), np.int32)
+    return bits, w
+
+
+def attention_case(dev, ora, seed, dtype, d, H, G, page, lens, n, tree=True, slots_first=False, words=None, layer=0, L=1, empty=(), scale=None,
+                   spread=1.0, behind=0, strided=False, bad_pages=(), nan_masked=False):
+    rng = np.random.default_rng(seed)
+    S = len(lens)
+    held = [-(-(a + b) // page) for a, b in zip(lens, n)]
+    pages = sum(held) + 2
+    kv, base = make_pool(rng, L, pages, H, page, d, dtype, dev, slots_first, fill="nan")
+    cols = max(max(held), 1) + 1
+    table, ref = make_book(rng, held, cols, pages, dev)
+    begin = np.cumsum([0] + list(n)).astype(np.int32)
+    N = int(begin[-1])
+    vals = torch.from_numpy(rng.standard_normal((2, S, max(a + b for a, b in zip(lens, n)) + 1, H, d)).astype(np.float32) * spread).to(TYPES[dtype])
+    for s in range(S):                                     # real values where positions are; NaN everywhere else
+        t = torch.arange(lens[s] + n[s])
+        if len(t):
+            at = torch.as_tensor(table[s].astype(np.int64))[t // page]
+            kv[layer][:, at.to(dev), :, (t % page).to(dev)] = vals[:, s, :len(t)].to(dev).transpose(0, 1)
+    q = torch.from_numpy(rng.standard_normal((N + behind, H * G, d)).astype(np.float32) * spread).to(TYPES[dtype])
+    words = words or max(1, -(-max(n) // 32))
+    bits, w = tree_mask(rng, begin, words, empty) if tree else (None, None)
+    if nan_masked:                                         # drafted positions of session 0 that only some rows see
+        for j in range(n[0]):
+            if not bits[begin[0]:begin[1], j][:2].any():
+                p = lens[0] + j
+                kv[layer, :, int(table[0, p // page]), :, p % page] = float("nan") if j % 2 else float("inf")
+                vals[:, 0, p] = float("nan")
+    for s, c in bad_pages:
+        table[s, c] = pages + 7
+    pool = plc.PagePool(kv)
+    book = book_of(table, lens, ref, dev)
+    qd = q.to(dev)
+    if strided:
+        wide = torch.full((N + behind, H * G + 3, d + 16), 9.0, dtype=TYPES[dtype], device=dev)
+        wide[:, 1:H * G + 1, 8:d + 8] = qd
+        qd = wide[:, 1:H * G + 1, 8:d + 8]
+    out = torch.full((N + behind, H * G, d), 77.0, dtype=TYPES[dtype], device=dev)
+    lse = torch.full((N + behind, H * G), 77.0, dtype=torch.float32, device=dev)
+    m = None
+    if tree:
+        m = torch.zeros(N + behind, words, dtype=torch.int32)
+        m[:N] = torch.from_numpy(w.copy()).view(N, words)
+        m = m.to(dev)
+    got, got_lse = pool.tree_attention(layer, book, qd, i32(begin, dev), mask=m, scale=scale, out=out, lse=lse)
+    torch.cuda.synchronize()
+    assert got.data_ptr() == out.data_ptr() and bool((out[N:] == 77).all()) and bool((lse[N:] == 77).all())
+
+    class Of:
+        heads = H
+
+        def __init__(self, j):
+            self.x = vals[j].float().numpy()
+
+        def __call__(self, s, g, t):
+            return None if (s, t // page) in bad_pages else self.x[s, t, g]
+
+    if nan_masked:                                         # only the rows that see no such position are compared
+        keep = [r for r in range(N) if r >= begin[1] or not any(bits[r, j] and bool(vals[0, 0, lens[0] + j].isnan().any()) for j in range(n[0]))]
+        assert len(keep) >= 2
+    else:
+        keep = list(range(N))
+    sc = 1 / math.sqrt(d) if scale is None else scale
+    ex, exl, mag, big = ora.attention(q[:N].double().numpy(), Of(0), Of(1), [int(x) for x in lens], [int(x) for x in begin], bits, sc)
+    got, got_lse = got[:N].double().cpu().numpy(), got_lse[:N].double().cpu().numpy()
+    u = torch.finfo(TYPES[dtype]).eps / 2
+    terms = max(a + b for a, b in zip(lens, n))
+    e = 2 * (d * 2.0 ** -23 * big + 2.0 ** -22 + 2.0 ** -23 * 2 * big)
+    tol = (u + e[..., None] + terms * 2.0 ** -23) * mag + u * np.abs(ex) + torch.finfo(TYPES[dtype]).smallest_normal * u
+    none = np.isinf(exl)
+    assert np.array_equal(got_lse[keep][none[keep]], exl[keep][none[keep]]) and not got[keep][none[keep]].any()
+    bad = np.abs(got - ex)[keep] > tol[keep]
+    assert not bad.any() and not np.isnan(got[keep]).any(), (np.argwhere(bad)[:5], np.abs(got - ex)[keep].max())
+    fine = ~none[keep]
+    off = np.abs(got_lse - np.where(none, 0, exl))[keep][fine]
+    assert (off <= (e + terms * 2.0 ** -23 + 2.0 ** -22 * np.abs(np.where(none, 0, exl)))[keep][fine]).all(), off.max()
+    return pool
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d, H, G, page, slots_first", [(32, 3, 1, 16, False), (64, 1, 5, 1, True), (128, 2, 8, 24, False), (128, 8, 1, 64, True),
+                                                        (256, 1, 3, 100, False), (256, 2, 16, 32, True)])
+def test_attention_of_ragged_trees(dev, ora, dtype, d, H, G, page, slots_first):
+    """Lengths of zero and one, around tile and page ends; sessions without queries; trees of one to 40 nodes."""
+    pool = attention_case(dev, ora, d + H, dtype, d, H, G, page, lens=[0, 1, 127, 128, 129, 300, 0, 63], n=[3, 1, 40, 0, 17, 2, 0, 1], slots_first=slots_first,
+                          behind=2)
+    pool.check()
+
+
+@pytest.mark.parametrize("dtype, d, H, G, n", [("f16", 64, 1, 1, 1), ("bf16", 128, 2, 4, 1), ("f16", 128, 1, 8, 100), ("bf16", 64, 2, 7, 33), ("f16", 256, 1, 2, 150),
+                                               ("bf16", 32, 1, 1, 260)])
+def test_attention_of_chains(dev, ora, dtype, d, H, G, n):
+    """No mask: single-token decoding, a drafted chain, a chunk of a prompt (several row tiles a session)."""
+    attention_case(dev, ora, n, dtype, d, H, G, 16, lens=[200, 0, 37, 511], n=[n, n, 1, n], tree=False, behind=1).check()
+
+
+def test_attention_over_longer_contexts(dev, ora):
+    """One session whose positions are split over the whole GPU, and a ragged batch whose parts begin inside sessions."""
+    attention_case(dev, ora, 1, "bf16", 128, 1, 2, 64, lens=[9001], n=[5]).check()
+    attention_case(dev, ora, 2, "f16", 64, 2, 1, 48, lens=[4000, 10, 0, 2500, 700, 1], n=[1, 9, 4, 1, 0, 2]).check()
+    attention_case(dev, ora, 3, "f16", 128, 1, 8, 256, lens=[3000, 5], n=[40, 37]).check()
+
+
+def test_attention_masks(dev, ora):
+    """Rows that see nothing drafted, rows that see nothing at all, masks of fewer and of more words than drafts."""
+    attention_case(dev, ora, 4, "f16", 64, 1, 2, 16, lens=[0, 20, 0], n=[5, 6, 33], empty=(0, 3, 6, 12, 40)).check()
+    attention_case(dev, ora, 5, "bf16", 128, 1, 1, 16, lens=[50, 0], n=[70, 40], words=1).check()
+    attention_case(dev, ora, 6, "f16", 128, 2, 2, 16, lens=[50, 129], n=[7, 3], words=4).check()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_attention_does_not_look_at_what_is_masked(dev, ora, dtype):
+    """Infinities and NaN at drafted positions that a row does not see leave it as it is, keys and values alike."""
+    attention_case(dev, ora, 7, dtype, 128, 2, 2, 16, lens=[60, 10], n=[30, 4], nan_masked=True)
+    attention_case(dev, ora, 8, dtype, 64, 1, 1, 8, lens=[0, 10], n=[12, 4], nan_masked=True)
+    attention_case(dev, ora, 8, dtype, 256, 1, 1, 8, lens=[125, 10], n=[12, 4], nan_masked=True)
+
+
+def test_attention_scales_and_strides(dev, ora):
+    """Large scores (the running maximum rises late and by much), a small scale, strided queries, another layer."""
+    attention_case(dev, ora, 9, "bf16", 128, 2, 2, 16, lens=[700, 33], n=[3, 1], spread=3.0, scale=1.0)
+    attention_case(dev, ora, 10, "f16", 64, 2, 2, 16, lens=[300, 33], n=[3, 1], scale=0.001)
+    attention_case(dev, ora, 11, "f16", 128, 2, 3, 32, lens=[300, 33], n=[9, 1], strided=True, L=3, layer=2, slots_first=True)
+
+
+def test_attention_reports_pages_out_of_range(dev, ora):
+    pool = attention_case(dev, ora, 12, "f16", 64, 1, 2, 16, lens=[100, 40], n=[4, 2], bad_pages=((0, 2), (1, 0)))
+    with pytest.raises(plc.PlcError) as e:
+        pool.check()
+    assert e.value.code == plc.E_INVALID
+    pool.check()                                           # the word has been cleared
+
+
+def test_attention_cuts_ranges_and_lengths_to_what_there_is(dev):
+    kv = torch.zeros(1, 2, 4, 1, 16, 64, dtype=torch.float16, device=dev)
+    pool = plc.PagePool(kv)
+    for length, begin in (([40], [0, 9]), ([-3], [0, 2]), ([30], [0, 4]), ([10], [2, 1]), ([10], [-2, 3]), ([1 << 30], [0, 4])):
+        book = book_of(np.array([[0, 1]]), length, np.array([1, 1, 0, 0]), dev)
+        out, lse = pool.tree_attention(0, book, torch.ones(4, 2, 64, dtype=torch.float16, device=dev), i32(begin, dev), out=torch.zeros(4, 2, 64, dtype=torch.float16, device=dev))
+        assert not out.any()
+        with pytest.raises(plc.PlcError) as e:
+            pool.check()
+        assert e.value.code == plc.E_INVALID
+
+
+def test_attention_offsets_pass_32_bits(dev, ora):
+    """Pages that lie farther apart than 2^31 elements and 2^32 bytes."""
+    far = (1 << 31) + 64
+    store = torch.empty(2 * far + 4 * 8 * 64, dtype=torch.float16, device=dev)
+    kv = store.as_strided((1, 2, 3, 1, 8, 64), (0, 8 * 64, far, 8 * 64, 64, 1))
+    rng = np.random.default_rng(3)
+    x = torch.from_numpy(rng.standard_normal((2, 3, 1, 8, 64)).astype(np.float32)).half()
+    kv[0] = x.to(dev)
+    q = torch.from_numpy(rng.standard_normal((1, 1, 64)).astype(np.float32)).half()
+    out, _ = plc.PagePool(kv).tree_attention(0, book_of(np.array([[2, 0]]), [14], np.array([1, 0, 1]), dev), q.to(dev), i32([0, 1], dev))
+    K = torch.cat([x[0, 2, 0], x[0, 0, 0]])[:15].double()
+    V = torch.cat([x[1, 2, 0], x[1, 0, 0]])[:15].double()
+    want = torch.softmax(K @ q[0, 0].double() / 8, 0) @ V
+    assert float((out.cpu().double()[0, 0] - want).abs().max()) < 2.0 ** -9
+
+
+def test_attention_on_another_stream_and_in_graphs(dev):
+    """Two captured graphs and an eager call, each with its own results: a replay reads the lengths that stand there then."""
+    rng = np.random.default_rng(5)
+    kv, _ = make_pool(rng, 1, 40, 2, 16, 128, "bf16", dev, False)
+    pool, q = plc.PagePool(kv), torch.randn(6, 8, 128, device=dev).bfloat16()
+    begin = i32([0, 1, 6], dev)
+    table = rng.permutation(40)[:36].reshape(2, 18)
+    book = book_of(table, [200, 100], np.ones(40), dev)
+    want = [t.clone() for t in pool.tree_attention(0, book, q, begin)]
+    side = torch.cuda.Stream(dev)
+    side.wait_stream(torch.cuda.current_stream(dev))
+    with torch.cuda.stream(side):
+        here = pool.tree_attention(0, book, q, begin)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(here, want))
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            res = pool.tree_attention(0, book, q, begin)
+        graphs.append((g, res))
+    for g, res in graphs:
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(res, want))
+    book.len.copy_(i32([17, 283], dev))
+    want2 = [t.clone() for t in pool.tree_attention(0, book, q, begin)]
+    for g, res in reversed(graphs):
+        g.replay()
+    torch.cuda.synchronize()
+    for g, res in graphs:
+        assert all(torch.equal(a, b) for a, b in zip(res, want2))
+    assert not torch.equal(want[0], want2[0])
+
+
+# ---------------------------------------------------------------------------------------------- pages
+
+def forked(rng, S, W, page, pages, cols):
+    """A book as beams leave it: rows of a session share their first pages."""
+    table, length, at = np.full((S * W, cols), -1, np.int32), np.zeros(S * W, np.int32), 0
+    order = rng.permutation(pages)
+    for s in range(S):
+        n = int(rng.integers(0, (cols - 1) * page)) if s else (cols - 2) * page   # the first session ends on a page's end
+        full, part, shared = n // page, n % page > 0, n // page // 2
+        first = order[at:at + shared]
+        at += shared
+        for w in range(W):
+            mine = full - shared + part + (s % 3 == 1)     # some rows hold a page of room
+            table[s * W + w, :shared + mine] = np.concatenate([first, order[at:at + mine]])
+            at += mine
+            length[s * W + w] = n
+    ref = np.bincount(table[table >= 0], minlength=pages).astype(np.int32)
+    return table, length, ref
+
+
+@pytest.mark.parametrize("dtype, L, H, d, page, slots_first, S, W", [
+    ("f16", 2, 2, 64, 16, False, 5, 3), ("bf16", 1, 3, 128, 5, True, 9, 4), ("f32", 3, 1, 32, 8, False, 4, 2), ("f32", 1, 2, 256, 100, True, 2, 5),
+    ("f16", 1, 1, 128, 1, False, 6, 2), ("f16", 1, 1, 32, 4, True, 700, 2)])
+def test_fork_copies_and_counts(dev, ora, dtype, L, H, d, page, slots_first, S, W):
+    rng = np.random.default_rng(S * W + page)
+    cols = 7
+    pages = S * W * (cols + 3)
+    table, length, ref = forked(rng, S, W, page, pages, cols)
+    table[0, 6], ref[pages - 1] = -1, ref[pages - 1] + 2    # the caller holds on to a page itself
+    kv, base = make_pool(rng, L, pages, H, page, d, dtype, dev, slots_first)
+    before = base.clone()
+    out_rows = S * W + 3                                     # more rows than before: a session gets more beams
+    parent = rng.integers(-1, S * W, out_rows)
+    parent[:S * W // 2] = np.arange(S * W // 2)              # these go on as they are
+    room = np.minimum(rng.integers(0, 2 * page, out_rows), cols * page - np.where(parent < 0, 0, length[parent]))
+    pool = plc.PagePool(kv)
+    for r in (room, None):
+        base.copy_(before)
+        new = pool.fork(book_of(table, length, ref, dev), i32(parent, dev), None if r is None else i32(r, dev))
+        t, n, f, copies, bits = ora.fork(table, length, ref, parent, r, page)
+        assert bits == 0 and (page == 1 or len(copies) >= 1)
+        same_book(new, t, n, f)
+        want = before.transpose(3, 4).clone() if slots_first else before.clone()
+        for src, dst, used in copies:
+            want[:L, :, dst, :, :used] = want[:L, :, src, :, :used]
+        assert torch.equal(base, want.transpose(3, 4) if slots_first else want)
+    pool.check()
+
+
+def test_fork_without_enough_pages_changes_nothing(dev, ora):
+    rng = np.random.default_rng(8)
+    table, ref = make_book(rng, [3, 2], 4, 7, dev)           # two pages are free
+    length = np.array([33, 20], np.int32)
+    kv, base = make_pool(rng, 1, 7, 1, 16, 64, "f16", dev, False)
+    before, pool = base.clone(), plc.PagePool(kv)
+    for parent, room, enough in (([0, 0, 0], None, True), ([0, 0, 0, 0], None, False), ([0, 1], [16, 16], True), ([0, 1, 1], [16, 16, 0], False),
+                                 ([0], [32], False)):        # the last one needs a fifth column
+        base.copy_(before)
+        new = pool.fork(book_of(table, length, ref, dev), i32(parent, dev), None if room is None else i32(room, dev))
+        t, n, f, copies, bits = ora.fork(table, length, ref, parent, room, 16)
+        assert bits == (0 if enough else ora.CAPACITY)
+        same_book(new, t, n, f)
+        if enough:
+            pool.check()
+        else:
+            assert torch.equal(base, before)
+            with pytest.raises(plc.PlcError) as e:
+                pool.check()
+            assert e.value.code == plc.E_CAPACITY
+
+
+def test_fork_refuses_what_is_out_of_range(dev, ora):
+    rng = np.random.default_rng(9)
+    table, ref = make_book(rng, [3, 2, 1], 4, 20, dev)
+    kv, _ = make_pool(rng, 1, 20, 1, 16, 64, "f16", dev, False)
+    pool = plc.PagePool(kv)
+    wrong = table.copy()
+    wrong[0, 1], wrong[2, 0] = 20, -5
+    for t0, length, parent, room in ((table, [33, 20, 3], [0, 3, -2, 1], [0, 0, 0, 0]), (table, [33, -1, 65], [0, 1, 2, 0], [0, 0, 0, 0]),
+                                     (table, [33, 20, 3], [0, 1, 2, 0], [0, -1, 1 << 30, 0]), (wrong, [33, 20, 3], [0, 0, 1, 2], [0, 0, 0, 0])):
+        new = pool.fork(book_of(t0, length, ref, dev), i32(parent, dev), i32(room, dev))
+        t, n, f, _, bits = ora.fork(t0, np.array(length, np.int32), ref, parent, room, 16)
+        same_book(new, t, n, f)
+        word = int(pool.status)
+        pool.status.zero_()
+        assert word == bits != 0
+
+
+@pytest.mark.parametrize("dtype, L, H, d, page, slots_first, S, m", [
+    ("f16", 2, 2, 64, 16, False, 5, 9), ("bf16", 1, 3, 128, 5, True, 9, 40), ("f32", 3, 1, 32, 8, False, 4, 2), ("f32", 1, 2, 256, 100, True, 1, 150),
+    ("f16", 1, 40, 128, 1, False, 3, 70)])
+def test_keep_moves_the_accepted_path(dev, ora, dtype, L, H, d, page, slots_first, S, m):
+    rng = np.random.default_rng(S + m)
+    length = rng.integers(0, 4 * page, S).astype(np.int32)
+    held = [-(-(int(n) + m) // page) + (s % 2) for s, n in enumerate(length)]
+    pages, cols = sum(held) + 2, max(held) + 1
+    table, ref = make_book(rng, held, cols, pages, dev)
+    kv, base = make_pool(rng, L, pages, H, page, d, dtype, dev, slots_first)
+    before = base.clone()
+    n_path = rng.integers(0, m + 1, S)
+    n_path[0] = m                                            # everything is kept
+    path = np.full((S, m), -9, np.int32)
+    for s in range(S):
+        path[s, :n_path[s]] = np.sort(rng.choice(m, n_path[s], replace=False))
+    pool = plc.PagePool(kv)
+    new = pool.keep(book_of(table, length, ref, dev), i32(path, dev), i32(n_path, dev))
+    t, n, f, moves, bits = ora.keep(table, length, ref, path, n_path, page)
+    assert bits == 0
+    same_book(new, t, n, f)
+    old = before.transpose(3, 4) if slots_first else before
+    want = old.clone()
+    for s, a, b in moves:
+        want[:L, :, int(table[s, b // page]), :, b % page] = old[:L, :, int(table[s, a // page]), :, a % page]
+    assert torch.equal(base, want.transpose(3, 4) if slots_first else want)
+    pool.check()
+
+
+def test_keep_leaves_rows_with_bad_paths_as_they_are(dev, ora):
+    rng = np.random.default_rng(11)
+    table, ref = make_book(rng, [3] * 9, 4, 40, dev)
+    table[8, 1] = table[7, 1]                                # two rows hold the page that one of them would write to
+    ref = np.bincount(table[table >= 0], minlength=40).astype(np.int32)
+    length = np.array([20, 20, 20, 20, 20, -1, 65, 14, 14], np.int32)
+    path = np.array([[0, 2, 5], [0, 0, 1], [3, 2, 5], [-1, 2, 5], [0, 2, 28], [0, 1, 2], [0, 1, 2], [1, 2, 5], [0, 1, 2]], np.int32)
+    n_path = np.array([3, 3, 3, 3, 3, 1, 1, 3, 4], np.int32)
+    kv, base = make_pool(rng, 1, 40, 2, 16, 64, "f16", dev, False)
+    before, pool = base.clone(), plc.PagePool(kv)
+    new = pool.keep(book_of(table, length, ref, dev), i32(path, dev), i32(n_path, dev))
+    t, n, f, moves, bits = ora.keep(table, length, ref, path, n_path, 16)
+    assert bits == ora.RANGE and {m[0] for m in moves} == {0}
+    same_book(new, t, n, f)
+    want = before.clone()
+    for s, a, b in moves:
+        want[:1, :, int(table[s, b // 16]), :, b % 16] = before[:1, :, int(table[s, a // 16]), :, a % 16]
+    assert torch.equal(base, want)
+    assert int(pool.status) == ora.RANGE
+
+
+@pytest.mark.parametrize("dtype, L, H, d, page, slots_first, S, pages", [
+    ("f16", 2, 2, 64, 16, False, 5, 60), ("bf16", 1, 3, 128, 5, True, 9, 100), ("f32", 1, 2, 256, 100, True, 2, 12), ("f16", 1, 1, 32, 2, False, 900, 5000),
+    ("f16", 1, 1, 64, 16, False, 1, 1), ("f16", 1, 1, 64, 16, False, 3, 40)])
+def test_compact_moves_pages_down(dev, ora, dtype, L, H, d, page, slots_first, S, pages):
+    rng = np.random.default_rng(pages)
+    held = [min(5, pages // S) if pages != 40 else 0 for s in range(S)]   # the last case: a pool without pages in use
+    table, ref = make_book(rng, held, 6, pages, dev)
+    if S > 1 and pages != 40:
+        table[1, 0] = table[0, 0]                            # a shared page; row 1's own is still held by the caller
+        ref[table[0, 0]] += 1
+    length = rng.integers(0, 2 * page, S).astype(np.int32)
+    kv, base = make_pool(rng, L, pages, H, page, d, dtype, dev, slots_first)
+    before, pool = base.clone(), plc.PagePool(kv)
+    new, moved = pool.compact(book_of(table, length, ref, dev))
+    t, f, where = ora.compact(table, ref)
+    same_book(new, t, length, f)
+    assert np.array_equal(moved.cpu().numpy(), where)
+    old = before.transpose(3, 4) if slots_first else before
+    want = old.clone()
+    for p in range(pages):
+        if where[p] >= 0:
+            want[:L, :, where[p]] = old[:L, :, p]
+    assert torch.equal(base, want.transpose(3, 4) if slots_first else want)
+    pool.check()
+
+
+# ---------------------------------------------------------------------------------------------- beams
+
+def check_beams(ora, x, cum, n_out, done=None, eos=-1, gap=2.0 ** -18):
+    S, W, V = x.shape
+    es, ep, et = ora.beam_select(x.double().cpu().numpy(), cum.cpu().numpy(), n_out, None if done is None else done.cpu().numpy(), eos)
+    # neighbours in the order are equal logits of one row, equal rows, or farther apart than the kernel's error
+    more = ora.beam_select(x.double().cpu().numpy(), cum.cpu().numpy(), min(n_out + 1, W * V), None if done is None else done.cpu().numpy(), eos)[0]
+    with np.errstate(invalid="ignore"):
+        step = more[:, :-1] - more[:, 1:]
+    assert (np.isnan(step) | (step == 0) | (step > gap)).all(), "the case's scores are too near each other to say anything"
+    s, p, t = plc.beam_select(x, cum, n_out, done=done, eos=eos)
+    s, p, t = s.double().cpu().numpy(), p.cpu().numpy(), t.cpu().numpy()
+    assert np.array_equal(p, ep) and np.array_equal(t, et)
+    fine = ~np.isinf(es)
+    assert np.array_equal(fine, ~np.isinf(s)) and (np.abs(s - es)[fine] <= 2.0 ** -20 + 2.0 ** -23 * np.abs(es[fine])).all()
+
+
+def spaced(rng, S, W, V, dtype, dev, peak=None):
+    """Logits whose large values are far apart across the rows of a session (multiples of 1/8 in a row; rows differ by the score)."""
+    x = np.round(rng.standard_normal((S, W, V)) * 16) / 8
+    return torch.from_numpy(x.astype(np.float32)).to(TYPES[dtype]).to(dev)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("S, W, V, n_out", [(1, 1, 1, 1), (2, 3, 7, 5), (1, 4, 257, 8), (5, 2, 1000, 3), (3, 8, 4099, 16), (1, 5, 20001, 64), (2, 16, 513, 32),
+                                            (1, 3, 9000, 128), (1, 128, 300, 128)])
+def test_beam_selection(dev, ora, dtype, S, W, V, n_out):
+    """Odd vocabularies (rows off 16-byte boundaries), many equal logits (ties by column), several parts a row, n_out above the vocabulary."""
+    rng = np.random.default_rng(V + n_out)
+    x = spaced(rng, S, W, V, dtype, dev)
+    for attempt in range(40):                                # scores of the beams that keep the rows' values apart
+        cum = torch.from_numpy(rng.uniform(-9, -1, (S, W)).astype(np.float32)).to(dev)
+        es = ora.beam_select(x.double().cpu().numpy(), cum.cpu().numpy(), min(n_out + 1, W * V))[0]
+        with np.errstate(invalid="ignore"):
+            step = es[:, :-1] - es[:, 1:]
+        if (np.isnan(step) | (step == 0) | (step > 2.0 ** -17)).all():
+            break
+    check_beams(ora, x, cum, min(n_out, W * V))
+
+
+def test_beam_selection_of_first_steps_and_ended_beams(dev, ora):
+    rng = np.random.default_rng(2)
+    x = spaced(rng, 4, 4, 500, "f16", dev)
+    cum = torch.tensor([[-1.0, -math.inf, -math.inf, -math.inf], [-3.0, -2.03, -4.31, -1.77], [-math.inf] * 4, [-5.0, -5.13, -0.4, math.inf]], device=dev)
+    done = torch.tensor([[False] * 4, [False, True, False, True], [False, True, False, False], [True, True, True, True]], device=dev)
+    check_beams(ora, x, cum, 6, done=done, eos=3)
+    s, p, t = plc.beam_select(x, cum, 6, done=done, eos=3)
+    assert p[2].tolist() == [-1] * 6 and t[2].tolist() == [-1] * 6
+    assert p[3].tolist() == [14, 12, 13, -1, -1, -1] and t[3].tolist() == [3, 3, 3, -1, -1, -1]
+
+
+def test_equal_beams_tie_to_the_lower_one(dev):
+    """Equal rows have equal sums wherever they start: their continuations alternate, the lower row first."""
+    for V, dtype in ((1001, "f16"), (5003, "bf16"), (333, "f32"), (40001, "f16")):
+        rng = np.random.default_rng(V)
+        row = torch.from_numpy(rng.permutation(V).astype(np.float32) / 64).to(TYPES[dtype])
+        x = row.expand(3, 4, V).contiguous().to(dev)
+        order = torch.argsort(row.float(), descending=True, stable=True)
+        s, p, t = plc.beam_select(x, torch.full((3, 4), -2.5, device=dev), 8)
+        top = row.float()[order[:40]].tolist()
+        want = sorted([(-v, w, int(c)) for w in range(4) for v, c in zip(top, order[:40].tolist())])[:8]
+        for b in range(3):
+            assert p[b].tolist() == [4 * b + w for _, w, _ in want] and t[b].tolist() == [c for _, _, c in want]
+
+
+def test_beam_selection_with_infinities_and_nan(dev, ora):
+    rng = np.random.default_rng(4)
+    x = spaced(rng, 3, 4, 900, "f32", dev)
+    x[0, :, 10:] = -math.inf                                 # all but ten tokens are banned
+    x[1, 0, 5], x[1, 1, 7], x[1, 2] = math.nan, math.inf, -math.inf
+    x[2, 1, :899] = -math.inf                                # one token left
+    x[2, 0, 3], x[2, 0, 4] = -0.0, 0.0
+    cum = torch.tensor([[-1.0, -2.1, -3.3, -4.7], [-1.0, -1.0, -1.0, -1.1], [-30.0, -1.2, math.nan, -50.0]], device=dev)
+    check_beams(ora, x, cum, 50)
+    s, p, t = plc.beam_select(x, cum, 50)
+    assert (p[0] >= 0).sum() == 40 and (p[1][p[1] >= 0] == 7).all()
+
+
+def test_beam_selection_where_everything_ties(dev, ora):
+    """All logits equal: the lowest columns of the lowest rows."""
+    for dtype in ("f16", "f32"):
+        x = torch.full((2, 3, 6001), 1.5, dtype=TYPES[dtype], device=dev)
+        s, p, t = plc.beam_select(x, torch.full((2, 3), -1.0, device=dev), 128)
+        for b in range(2):
+            assert p[b].tolist() == [3 * b] * 128 and t[b].tolist() == list(range(128))
+        x = torch.arange(70000, device=dev).float().div(70000).to(TYPES[dtype]).expand(1, 1, -1).contiguous()   # rising: every step beats the last
+        order = torch.argsort(x[0, 0].float(), descending=True, stable=True)[:100]
+        s, p, t = plc.beam_select(x, torch.zeros(1, 1, device=dev), 100)
+        assert torch.equal(t[0].long(), order)
+
+
+def test_reordering_of_states(dev):
+    rng = np.random.default_rng(6)
+    R = 37
+    states = [torch.randint(0, 9, (R, 5), dtype=torch.int32, device=dev), torch.randn(R, 3, 7, device=dev).half(), torch.randint(0, 255, (R, 33), dtype=torch.uint8, device=dev),
+              torch.randn(R, 40000, device=dev), torch.randn(R, 64, device=dev)[:, :48], torch.randn(R, device=dev), torch.randn(R, 0, device=dev)] * 3
+    for rows in (1, 37, 64):
+        parent = i32(rng.integers(-1, R, rows), dev)
+        got = plc.beam_reorder(parent, states)
+        at = parent.long()
+        for g, t in zip(got, states):
+            want = t[at.clamp(min=0)].clone()
+            want[at < 0] = 0
+            assert g.shape == want.shape and torch.equal(g, want)
+    word = torch.zeros(1, dtype=torch.int32, device=dev)
+    got = plc.beam_reorder(i32([R, 0, -2], dev), states[:1], status=word)
+    assert int(word) == 32 and not got[0][0].any() and not got[0][2].any() and torch.equal(got[0][1], states[0][0])
+
+
+# ---------------------------------------------------------------------------------------------- together
+
+def test_beams_over_a_restored_cache(dev, ora):
+    """A coded cache is decoded into pages, beams fork it, attend, are selected, and drafted paths are kept: every row's keys and
+    values stay those of its own history, which is kept beside it in plain tensors."""
+    S, W, n, L, H, d, V, K, page = 2, 3, 40, 2, 2, 64, 400, 32, 16
+    table = synth.markov_table(V, 8.0, 5, max_states=64)
+    tokens = synth.sample_tokens(table, S, n, 6)
+    logits = synth.position_logits(table, tokens).to(dev)
+    T = synth.make_tables(L, H, V, d, 7)
+    src = synth.make_kv(T, tokens, 0.05, 8).to(dev)
+    ctx = plc.Context(T.to(dev), K, 0.02, chunk_pos=32, out_dtype=plc.OUT_F16)
+    st = plc.StreamSet(S * ctx.W, ctx.max_chunks(n), 3 * S * n * ctx.W * d + 8192, dev)
+    ctx.encode(src, logits, st)
+    pages, each = 60, -(-n // page)
+    kv = torch.zeros(L, 2, pages, page, H, d, dtype=torch.float16, device=dev).transpose(3, 4)
+    pool = plc.PagePool(kv)
+    ctx.decode(st, logits, pool.sessions_view(4, S, n))
+    plain = torch.zeros(L, 2, S, H, n, d, dtype=torch.float16, device=dev)
+    ctx.decode(st, logits, plain)
+    assert ctx.sync_status() == plc.OK
+    first = np.full((S, 8), -1, np.int32)
+    for s in range(S):
+        first[s, :each] = 4 + s * each + np.arange(each)
+    book = book_of(first, [n] * S, np.bincount(first[first >= 0], minlength=pages), dev)
+    history = [plain[:, :, s].float().cpu() for s in range(S)]                    # [L][2][H][positions][d]
+    book = pool.fork(book, i32(np.repeat(np.arange(S), W), dev), torch.full((S * W,), 4, dtype=torch.int32, device=dev))
+    history = [history[s].clone() for s in range(S) for _ in range(W)]
+    score = torch.full((S, W), -math.inf, device=dev)
+    score[:, 0] = 0
+    toks = torch.zeros(S * W, 8, dtype=torch.int32, device=dev)
+    gen = torch.Generator(device="cpu").manual_seed(3)
+    proj = torch.randn(H * 2 * d, V, generator=gen).to(dev) * 0.3
+    for step in range(3):
+        R, m = S * W, 4                                                           # a tree of four drafts: 0 -> 1, 0 -> 2, 3
+        new = torch.randn(L, 2, R, H, m, d, generator=gen).half()
+        pos = book.len.long()[:, None] + torch.arange(m, device=dev)
+        at = book.table.long().gather(1, pos // page)
+        kv.permute(2, 4, 0, 1, 3, 5)[at, pos % page] = new.to(dev).permute(2, 4, 0, 1, 3, 5)
+        q = torch.randn(R * m, 2 * H, d, generator=gen).half()
+        mask = torch.tensor([0b0001, 0b0011, 0b0101, 0b1000], dtype=torch.int32).repeat(R)[:, None].to(dev)
+        out, lse = pool.tree_attention(1, book, q.to(dev), torch.arange(0, R * m + 1, m, dtype=torch.int32, device=dev), mask=mask)
+        bits = np.array([[1, 0, 0, 0], [1, 1, 0, 0], [1, 0, 1, 0], [0, 0, 0, 1]], bool)
+        for r in range(R):
+            k, v = (torch.cat([history[r][1, j], new[1, j, r].float()], 1).double() for j in (0, 1))   # [H][n + m][d]
+            for i in range(m):
+                sees = torch.cat([torch.ones(history[r].shape[3], dtype=torch.bool), torch.from_numpy(bits[i])])
+                for h in range(2 * H):
+                    w = torch.softmax(k[h // 2][sees] @ q[r * m + i, h].double() / math.sqrt(d), 0)
+                    want = w @ v[h // 2][sees]
+                    assert float((out[r * m + i, h].cpu().double() - want).abs().max()) < 2.0 ** -8
+        # the path 0 -> 2 is accepted everywhere, then the beams go on from what was seen last
+        book = pool.keep(book, i32([[0, 2]] * R, dev), i32([2] * R, dev))
+        history = [torch.cat([history[r], new[:, :, r].float()[:, :, :, [0, 2]]], 3) for r in range(R)]
+        x = (out.view(R, m, -1)[:, 2].float() @ proj).view(S, W, V)
+        score, parent, token = plc.beam_select(x, score, W)
+        assert bool((parent >= 0).all())
+        toks, = plc.beam_reorder(parent, [toks])
+        toks[:, step] = token.flatten()
+        par = parent.flatten().tolist()
+        book = pool.fork(book, parent.flatten(), torch.full((R,), 4, dtype=torch.int32, device=dev))
+        history = [history[p].clone() for p in par]
+        if step == 1:
+            book, moved = pool.compact(book)
+            live = int((book.ref > 0).sum())
+            assert not book.ref[live:].any() and int(book.table.max()) == live - 1
+        for r in range(R):                                                        # every row's pages hold its own history
+            t = torch.arange(history[r].shape[3], device=dev)
+            mine = kv[:, :, book.table[r].long()[t // page], :, t % page]
+            assert torch.equal(mine.permute(1, 2, 3, 0, 4).float().cpu(), history[r])
+        assert int(book.len[0]) == history[0].shape[3]
+    pool.check()
