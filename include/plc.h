@@ -430,7 +430,7 @@ typedef struct {
  * to what there is, positions without a page are not seen.  workspace: plc_tree_attention_workspace bytes. */
 plc_status plc_tree_attention(const plc_page_pool* pool, int32_t layer, const plc_page_book* book, const plc_tree_queries* queries,
                               float scale, void* workspace_dev, uint64_t workspace_bytes, uint32_t* status_dev, void* stream);
-plc_status plc_tree_attention_workspace(const plc_page_pool* pool, int32_t n_heads, uint64_t* bytes);
+plc_status plc_tree_attention_workspace(const plc_page_pool* pool, int32_t sessions, int32_t n_heads, int32_t n_rows, uint64_t* bytes);
 
 /* One step of beam search for `sessions` sessions of `beams` beams: of the beams*vocab continuations with
  *     score_dev[b][w] + logits[b][w][v] - log sum_v' exp logits[b][w][v']

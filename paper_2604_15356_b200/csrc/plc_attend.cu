@@ -1,10 +1,34 @@
 // Attention of drafted tokens over their session's pages (plc_tree_attention).
+//
+// For a session's KV head the rows are its drafted tokens times the query heads of the group.  Per tile of TN positions:
+//   S = Q K^T        [128 x TN]  tcgen05.mma, both operands in shared memory, S in TMEM
+//   P = exp2(c S - m)            a thread a row: running maximum m and sum l in binary32, P rounded to the pool's type
+//   O = O + P V      [128 x d]   tcgen05.mma, P read from TMEM (over S's columns), V as it lies in the page (d contiguous)
+// and out = O / l at the end.  K and V are read once per 128 (or 256) rows: for the few rows of single tokens and small
+// trees that is the floor, and HBM bounds the kernel; from about 128 rows on the products and the exponentials do.
+//
+// Work.  All (session, head, row tile, position tile) form one sequence, cut into equal ranges, one a CTA: lengths that
+// differ, and one long context, fill the GPU alike.  A CTA's first and last piece may be parts of an item (session, head,
+// row tile); those leave O, m and l in the workspace and a second, small launch joins them in a fixed order.
+//
+// Roles in a CTA: warps that each own 32 rows (softmax, epilogue), three warps that copy (cp.async, 16 bytes a lane, each position's
+// address from the page table, since a page may be any size and lie anywhere), one thread that issues the products.  Two layouts: NT = 1 (128
+// rows; two CTAs an SM, whose phases overlap) and NT = 2 (two row tiles that share each K and V tile; one CTA an SM).
+//
+// The weights are rounded to the type of V because the product takes both operands in one type; l sums them unrounded.  For f16
+// they are formed as 2^12 times themselves, so that weights down to 2^-26 of the largest keep all their bits.  A
+// row's maximum is raised only when it would grow by more than 2^3 (a weight is at most 2^15 then), which spares most passes over O.
 #include <cuda_bf16.h>
 
 #include "plc_pages.cuh"
 
 namespace plc {
 namespace {
+
+constexpr uint32_t kSpin = 1u << 22;
+constexpr int kLoaders = 96;                      // threads that copy: three warps, so that a CTA has a whole number of warps a scheduler
+constexpr float kRaise = 3.f, kShiftF16 = 12.f;
+constexpr int kWordRing = 4;                      // tiles whose validity words are kept: more than the loader can be ahead of the softmax
 
 struct AttendArgs {
     const void* q; int64_t qs_row, qs_head;       // elements
@@ -13,107 +37,712 @@ struct AttendArgs {
     const int32_t* begin; const uint32_t* mask;
     int rows, heads, group, mask_words, layer;
     float scale;
+    float* part_o;                                // [2 * grid][part_rows][d]
+    float2* part_ml;                              // [2 * grid][part_rows]: maximum (scaled, base 2), sum
+    int4* first;                                  // [grid]: session, head, row tile, first position tile of each CTA's range (-1: none)
+    int part_rows;
 };
 
-template <class T> __device__ __forceinline__ float widen(T v);
-template <> __device__ __forceinline__ float widen(__half v) { return __half2float(v); }
-template <> __device__ __forceinline__ float widen(__nv_bfloat16 v) { return __bfloat162float(v); }
-template <class T> __device__ __forceinline__ T narrow(float v);
-template <> __device__ __forceinline__ __half narrow(float v) { return __float2half_rn(v); }
-template <> __device__ __forceinline__ __nv_bfloat16 narrow(float v) { return __float2bfloat16_rn(v); }
-
-// The plain form: a warp a (query row, head), 32 positions at a time with a running maximum and sum.
-template <class T, int D>
-__global__ void __launch_bounds__(128) attend_kernel(PoolDev p, BookDev b, AttendArgs a, uint32_t* status) {
-    __shared__ float qs[4][D];
-    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    const int row = blockIdx.x, head = blockIdx.y * 4 + wid;
-    if (head >= a.heads) return;
-    if (row == 0 && head == 0) {
-        bool bad = false;
-        for (int i = lane; i < b.rows; i += 32) bad |= a.begin[i] < 0 || a.begin[i + 1] < a.begin[i] || a.begin[i + 1] > a.rows;
-        if (bad) atomicOr(status, kStRange);
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(n) : "memory"); }
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// Arrives when the thread's copies issued so far have landed.
+__device__ __forceinline__ void mbar_arrive_copies(uint32_t bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+// Bounded wait: false where another role has given up, or (error bit set) the phase did not complete within the limit.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* failed, uint32_t* status) {
+    for (uint32_t i = 0; i < kSpin; ++i) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (ok) return true;
+        if ((i & 15) == 15 && *failed) return false;
     }
-    int s = 0;
-    {
-        int lo = 0, hi = b.rows;                  // the last session that begins at or before the row
-        while (hi - lo > 1) { const int m = (lo + hi) / 2; if (a.begin[m] <= row) lo = m; else hi = m; }
-        s = lo;
-    }
-    const int first = max(a.begin[s], 0), end = a.begin[s + 1];
-    if (row < first || row >= end) return;
-    const int most = most_positions(b, p);
-    int len = b.len[s], n = min(end, a.rows) - first;
-    if (len < 0 || len > most || n > most - len) {
-        if (lane == 0) atomicOr(status, kStRange);
-        len = min(max(len, 0), most);
-        n = min(n, most - len);
-    }
-    const int i = row - first, kh = head / a.group;
-    const T* q = static_cast<const T*>(a.q) + row * a.qs_row + head * a.qs_head;
-    for (int c = lane; c < D; c += 32) qs[wid][c] = widen(q[c]);
-    __syncwarp();
-    const uint8_t* kb = p.base + a.layer * p.sl + kh * p.sh;
-    float m = -INFINITY, sum = 0.f, o[D / 32];
-#pragma unroll
-    for (int c = 0; c < D / 32; ++c) o[c] = 0.f;
-    for (int t0 = 0; t0 < len + n; t0 += 32) {
-        const int t = t0 + lane, j = t - len;
-        bool sees = t < len + n && (j < 0 || (a.mask ? j < a.mask_words * 32 && (a.mask[(int64_t)row * a.mask_words + j / 32] >> (j & 31) & 1) : j <= i));
-        int64_t at = 0;
-        if (sees) {
-            const int page = b.table[(int64_t)s * b.max_pages + t / p.page_pos];
-            at = (int64_t)page * p.spage + (int64_t)(t % p.page_pos) * p.sp;
-            if (page < 0 || page >= p.n_pages) { atomicOr(status, kStRange); sees = false; at = 0; }
-        }
-        float x = -INFINITY;
-        if (sees) {
-            const T* k = reinterpret_cast<const T*>(kb + at);
-            x = 0.f;
-            for (int c = 0; c < D; c += 8) {
-                const uint4 r = *reinterpret_cast<const uint4*>(k + c);
-                const T* h = reinterpret_cast<const T*>(&r);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x = fmaf(qs[wid][c + e], widen(h[e]), x);
-            }
-            x *= a.scale;
-        }
-        float top = x;
-#pragma unroll
-        for (int w = 16; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, w));
-        top = fmaxf(top, m);
-        if (top == -INFINITY) continue;
-        const float w = sees ? __expf(x - top) : 0.f, old = __expf(m - top);
-        m = top;
-        sum = sum * old + warp_sum(w);
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) o[c] *= old;
-        const uint32_t who = __ballot_sync(kFull, sees);
-        for (int e = 0; e < 32; ++e) {
-            if (!(who >> e & 1)) continue;
-            const int64_t from = __shfl_sync(kFull, at, e);
-            const float we = __shfl_sync(kFull, w, e);
-            const T* v = reinterpret_cast<const T*>(kb + p.skv + from);
-#pragma unroll
-            for (int c = 0; c < D / 32; ++c) o[c] = fmaf(we, widen(v[c * 32 + lane]), o[c]);
-        }
-    }
-    T* out = static_cast<T*>(a.out) + row * a.os_row + head * a.os_head;
-#pragma unroll
-    for (int c = 0; c < D / 32; ++c) out[c * 32 + lane] = narrow<T>(sum == 0.f ? 0.f : o[c] / sum);
-    if (a.lse && lane == 0) a.lse[(int64_t)row * a.heads + head] = sum == 0.f ? -INFINITY : m + logf(sum);
+    *failed = 1u;
+    atomicOr(status, kStTimeout);
+    return false;
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool take) {   // zeros where not `take`
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
+}
+// 128-byte swizzled rows.  K-major (Q, K): 1024 bytes from eight rows to the next eight.  MN-major (V): the same step along
+// the positions, `block` bytes from 64 components to the next 64.
+__device__ __forceinline__ uint64_t desc_k(uint32_t addr) { return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61); }
+__device__ __forceinline__ uint64_t desc_mn(uint32_t addr, uint32_t block) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(block >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(0u) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc), "r"(0u) : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+          "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+        "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
+        "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr), "r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]),
+        "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
 }
 
-template <class T>
-cudaError_t launch_attend(const PoolDev& p, const BookDev& b, const AttendArgs& a, uint32_t* status, cudaStream_t st) {
-    const dim3 grid(a.rows, (a.heads + 3) / 4);
-    switch (p.d) {
-        case 32: attend_kernel<T, 32><<<grid, 128, 0, st>>>(p, b, a, status); break;
-        case 64: attend_kernel<T, 64><<<grid, 128, 0, st>>>(p, b, a, status); break;
-        case 128: attend_kernel<T, 128><<<grid, 128, 0, st>>>(p, b, a, status); break;
-        default: attend_kernel<T, 256><<<grid, 128, 0, st>>>(p, b, a, status); break;
+template <class T> struct Kind;
+template <> struct Kind<__half> {
+    static constexpr uint32_t format = 0;
+    static constexpr float shift = kShiftF16;
+    static constexpr uint32_t exponent = 0x7c00u;
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
     }
-    return cudaGetLastError();
+    static __device__ __forceinline__ float widen(uint16_t v) { return __half2float(__ushort_as_half(v)); }
+};
+template <> struct Kind<__nv_bfloat16> {
+    static constexpr uint32_t format = 1;
+    static constexpr float shift = 0.f;
+    static constexpr uint32_t exponent = 0x7f80u;
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    static __device__ __forceinline__ float widen(uint16_t v) { return __bfloat162float(__ushort_as_bfloat16(v)); }
+};
+
+template <int D, int NT> struct Shape {
+    static constexpr int TN = D == 256 ? 64 : 128;                     // positions a tile: S and O of a CTA's row tiles fit in TMEM, K and V in shared memory
+    static constexpr int blocks = (D + 63) / 64;                       // 128-byte wide column blocks (32 components: half of one)
+    static constexpr int DV = blocks * 64;                             // columns of O
+    static constexpr int stages = D == 128 ? NT : NT == 2 ? 3 : 2;
+    static constexpr int q_bytes = blocks * 128 * 128, kv_bytes = blocks * TN * 128;
+    static constexpr int tmem = NT * (TN + DV) > 256 ? 512 : 256;
+    static constexpr int rows = NT * 128, threads = NT * 128 + kLoaders + 32;
+    static constexpr int per_sm = NT == 1 && D != 256 ? 2 : 1;
+    static constexpr size_t smem = (size_t)NT * q_bytes + 2 * stages * kv_bytes + 2 * TN * 8 + 1024 + 512;
+};
+
+// A session as the call gives it, cut to what there is.
+struct Session { int first, n, len, kv; };
+__device__ __forceinline__ Session session_of(const PoolDev& p, const BookDev& b, const AttendArgs& a, int s, bool* bad) {
+    const int b0 = a.begin[s], b1 = a.begin[s + 1], len = b.len[s], most = most_positions(b, p);
+    Session x;
+    x.first = min(max(b0, 0), a.rows);
+    x.n = min(max(b1, x.first), a.rows) - x.first;
+    x.len = min(max(len, 0), most);
+    x.kv = x.n > 0 ? (int)min((long long)x.len + x.n, (long long)most) : 0;
+    *bad = b0 < 0 || b1 < b0 || b1 > a.rows || len < 0 || len > most || (long long)x.len + x.n > most;
+    return x;
+}
+
+// Where a range of position tiles stands: item (session, head, row tile) and tile in it.
+template <int TN, int ROWS> struct Walk {
+    int s, h, rt, tile, tiles, row_tiles;
+    Session x;
+    __device__ __forceinline__ void enter(const PoolDev& p, const BookDev& b, const AttendArgs& a) {
+        bool bad;
+        x = session_of(p, b, a, s, &bad);
+        tiles = (x.kv + TN - 1) / TN;
+        row_tiles = (int)(((long long)x.n * a.group + ROWS - 1) / ROWS);
+    }
+    __device__ __forceinline__ void start(const PoolDev& p, const BookDev& b, const AttendArgs& a, int session, long long rest) {
+        s = session;
+        enter(p, b, a);
+        const int item = (int)(rest / tiles);
+        tile = (int)(rest - (long long)item * tiles);
+        h = item / row_tiles;
+        rt = item - h * row_tiles;
+    }
+    __device__ __forceinline__ void next_item(const PoolDev& p, const BookDev& b, const AttendArgs& a) {
+        tile = 0;
+        if (++rt < row_tiles) return;
+        rt = 0;
+        if (++h < p.H) return;
+        h = 0;
+        do {
+            if (++s >= b.rows) return;
+            enter(p, b, a);
+        } while (x.n == 0);
+    }
+    __device__ __forceinline__ int rows(const AttendArgs& a) const { return min(ROWS, x.n * a.group - rt * ROWS); }
+};
+
+// 32 bits: which of the positions t .. t+31 row i (the i-th drafted token) sees, as far as the mask says.
+__device__ __forceinline__ uint32_t seen_bits(const AttendArgs& a, const Session& x, int i, int t) {
+    const int j = t - x.len;                      // drafted index of the first one
+    if (j <= -32) return ~0u;
+    auto word = [&](int w) -> uint32_t {          // drafted positions 32 w ...
+        if (w < 0) return ~0u;                    // committed ones
+        if (a.mask) return w < a.mask_words ? a.mask[(int64_t)(x.first + i) * a.mask_words + w] : 0u;
+        const int up = i - 32 * w;                // bits 0 .. up
+        return up < 0 ? 0u : up >= 31 ? ~0u : (2u << up) - 1u;
+    };
+    const int w = j >> 5;
+    return __funnelshift_r(word(w), word(w + 1), j & 31);
+}
+
+template <class T, int D, int NT>
+__global__ void __launch_bounds__(Shape<D, NT>::threads, Shape<D, NT>::per_sm)
+attend_kernel(PoolDev p, BookDev b, const __grid_constant__ AttendArgs a, uint32_t* status) {
+    using Sh = Shape<D, NT>;
+    using Wk = Walk<Sh::TN, Sh::rows>;
+    constexpr int TN = Sh::TN, stages = Sh::stages, n_warps = Sh::threads / 32;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint8_t* ks = smem + NT * Sh::q_bytes;
+    uint8_t* vs = ks + stages * Sh::kv_bytes;
+    int64_t* offs = reinterpret_cast<int64_t*>(vs + stages * Sh::kv_bytes);             // [2][TN]
+    uint64_t* bars = reinterpret_cast<uint64_t*>(offs + 2 * TN);
+    uint32_t* words = reinterpret_cast<uint32_t*>(bars + 4 * stages + 3 + 3 * NT);      // [kWordRing][4]
+    uint32_t* tmem_slot = words + kWordRing * 4;
+    volatile uint32_t* failed = tmem_slot + 1;
+    // [2]: piece number + 1 of the last pieces whose V holds infinities or NaN at drafted positions, by its parity (no row tile is a whole piece behind)
+    volatile uint32_t* dirty = tmem_slot + 2;
+    __shared__ long long sums[n_warps];
+    __shared__ long long range_at[2];             // the range's first session, and the tiles of it that lie before the range
+    const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
+    const uint32_t kfull = smem_u32(bars), vfull = kfull + 8 * stages, kempty = vfull + 8 * stages, vempty = kempty + 8 * stages;
+    const uint32_t qfull = vempty + 8 * stages, qempty = qfull + 8, drain = qempty + 8, sfull = drain + 8, pfull = sfull + 8 * NT, ofull = pfull + 8 * NT;
+    chain_next();
+
+    constexpr int mma_warp = n_warps - 1;
+    if (tid == 0) {
+        for (int i = 0; i < stages; ++i) {
+            mbar_init(kfull + 8 * i, kLoaders + kLoaders / 32);
+            mbar_init(vfull + 8 * i, kLoaders);
+            mbar_init(kempty + 8 * i, 1);
+            mbar_init(vempty + 8 * i, 1);
+        }
+        mbar_init(qfull, kLoaders);
+        mbar_init(qempty, 1);
+        mbar_init(drain, 1);
+        for (int i = 0; i < NT; ++i) {
+            mbar_init(sfull + 8 * i, 1);
+            mbar_init(pfull + 8 * i, 4);
+            mbar_init(ofull + 8 * i, 1);
+        }
+        *failed = dirty[0] = dirty[1] = 0u;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (wid == mma_warp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"((uint32_t)Sh::tmem) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    fence_before();
+
+    // this CTA's range of the sequence of tiles: a thread sums a run of sessions, the threads' sums are scanned
+    const int run = (b.rows + Sh::threads - 1) / Sh::threads, s0 = min(b.rows, tid * run), s1 = min(b.rows, s0 + run);
+    auto tiles_of = [&](int s, bool* bad) -> long long {
+        const Session x = session_of(p, b, a, s, bad);
+        return (long long)((x.kv + TN - 1) / TN) * (((long long)x.n * a.group + Sh::rows - 1) / Sh::rows) * p.H;
+    };
+    long long mine = 0;
+    bool any_bad = false;
+    for (int s = s0; s < s1; ++s) {
+        bool bad;
+        mine += tiles_of(s, &bad);
+        any_bad |= bad;
+    }
+    if (any_bad && blockIdx.x == 0) atomicOr(status, kStRange);
+    long long upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(kFull, upto, o);
+        if (lane >= o) upto += v;
+    }
+    if (lane == 31) sums[wid] = upto;
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *tmem_slot;
+    long long total = 0, ahead = upto - mine;
+    for (int w = 0; w < n_warps; ++w) {
+        if (w < wid) ahead += sums[w];
+        total += sums[w];
+    }
+    const int workers = (int)min((long long)gridDim.x, total), me = blockIdx.x;
+    const long long t0 = me < workers ? total * me / workers : total, t1 = me < workers ? total * (me + 1) / workers : total;
+    if (t0 < t1 && t0 >= ahead && t0 < ahead + mine) {
+        long long at = ahead;
+        bool bad;
+        int s = s0;
+        for (; s < s1; ++s) {
+            const long long f = tiles_of(s, &bad);
+            if (t0 < at + f) break;
+            at += f;
+        }
+        range_at[0] = s;
+        range_at[1] = t0 - at;
+    }
+    __syncthreads();
+    Wk w{};
+    long long left = t1 - t0;
+    if (left > 0) w.start(p, b, a, (int)range_at[0], range_at[1]);
+    if (tid == 0) a.first[me] = left > 0 ? make_int4(w.s, w.h, w.rt, w.tile) : make_int4(-1, 0, 0, 0);
+
+    if (wid >= NT * 4 && wid < mma_warp) {
+        // ---- copies.  A tile's addresses are found by one thread a position and passed on in shared memory.
+        const int lt = tid - NT * 128;
+        constexpr int pieces = D * 2 / 16;
+        const uint32_t q_s = smem_u32(smem), k_s = smem_u32(ks), v_s = smem_u32(vs);
+        int done = 0, item = 0;
+        bool ok = true, go = true;                    // this thread's waits; all loaders' (they leave together: they share a barrier)
+        while (left > 0 && go) {
+            const int m = (int)min(left, (long long)(w.tiles - w.tile)), rows = w.rows(a), row0 = w.rt * Sh::rows;
+            const int32_t* row = b.table + (int64_t)w.s * b.max_pages;
+            const uint8_t* kb = p.base + (int64_t)a.layer * p.sl + (int64_t)w.h * p.sh;
+            ok = ok && mbar_wait(qempty, (uint32_t)(item & 1) ^ 1u, failed, status);
+            if (ok)
+                for (int u = lt; u < Sh::rows * pieces; u += kLoaders) {
+                    const int r = u / pieces, c = u - r * pieces, rr = row0 + r, i = rr / a.group, g = rr - i * a.group;
+                    const uint8_t* src = static_cast<const uint8_t*>(a.q);
+                    if (r < rows) src += 2 * ((int64_t)(w.x.first + i) * a.qs_row + (int64_t)(w.h * a.group + g) * a.qs_head) + c * 16;
+                    copy16(q_s + (r >> 7) * Sh::q_bytes + (c >> 3) * 16384 + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4), src, r < rows);
+                }
+            mbar_arrive_copies(qfull);
+            for (int j = 0; j < m; ++j, ++done) {
+                const int st = done % stages;
+                const uint32_t ph = (uint32_t)(done / stages) & 1u;
+                int64_t* off = offs + (done & 1) * TN;
+                uint32_t valid[2] = {0, 0};
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int word = (lt >> 5) + e * (kLoaders / 32);
+                    if (word >= TN / 32) break;
+                    const int t = (w.tile + j) * TN + word * 32 + lane;
+                    bool have = t < w.x.kv;
+                    int64_t at = 0;
+                    if (have) {
+                        const int pg = t / p.page_pos, page = row[pg];
+                        if (page >= 0 && page < p.n_pages) at = (int64_t)page * p.spage + (int64_t)(t - pg * p.page_pos) * p.sp;
+                        else { have = false; atomicOr(status, kStRange); }
+                    }
+                    off[word * 32 + lane] = have ? at : INT64_MIN;
+                    valid[e] = __ballot_sync(kFull, have);
+                }
+                ok = ok && mbar_wait(kempty + 8 * st, ph ^ 1u, failed, status);
+                uint32_t all;
+                asm volatile(
+                    "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\t"
+                    "barrier.cta.red.and.pred q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                    : "=r"(all) : "r"((uint32_t)ok), "n"(kLoaders) : "memory");
+                go = all != 0;
+                if (!go) break;
+                if (lane == 0) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        if ((lt >> 5) + e * (kLoaders / 32) < TN / 32) words[(done % kWordRing) * 4 + (lt >> 5) + e * (kLoaders / 32)] = valid[e];
+                }
+#pragma unroll 8
+                for (int u = lt; u < TN * pieces; u += kLoaders) {
+                    const int r = u / pieces, c = u % pieces;
+                    const int64_t o = off[r];
+                    copy16(k_s + st * Sh::kv_bytes + (c >> 3) * (TN * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4), o == INT64_MIN ? kb : kb + o + c * 16, o != INT64_MIN);
+                }
+                mbar_arrive_copies(kfull + 8 * st);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(kfull + 8 * st);            // the validity words, too, are there
+                ok = mbar_wait(vempty + 8 * st, ph ^ 1u, failed, status);
+                if (ok) {
+#pragma unroll 8
+                    for (int u = lt; u < TN * pieces; u += kLoaders) {
+                        const int r = u / pieces, c = u % pieces;
+                        const int64_t o = off[r];
+                        copy16(v_s + st * Sh::kv_bytes + (c >> 3) * (TN * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4),
+                               o == INT64_MIN ? kb : kb + p.skv + o + c * 16, o != INT64_MIN);
+                    }
+                    mbar_arrive_copies(vfull + 8 * st);
+                }
+            }
+            left -= m;
+            ++item;
+            if (left > 0) w.next_item(p, b, a);
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    } else if (wid == mma_warp) {
+        if (lane == 0) {
+            // ---- products, in the order QK(0), then for every tile PV(j), QK(j+1), the row tiles in turn.  They run in the order in which they are
+            // issued, so that S of the next tile may take the columns of P of this one.
+            constexpr uint32_t common = (1u << 4) | (Kind<T>::format << 7) | (Kind<T>::format << 10) | (8u << 24);
+            constexpr uint32_t id_qk = common | ((uint32_t)(TN >> 3) << 17), id_pv = common | (1u << 16) | ((uint32_t)(Sh::DV >> 3) << 17);
+            const uint32_t q_s = smem_u32(smem), k_s = smem_u32(ks), v_s = smem_u32(vs);
+            int kd = 0, vd = 0, item = 0;
+            uint32_t pph[NT];
+            for (int i = 0; i < NT; ++i) pph[i] = 0;
+            bool ok = true;
+            auto qk = [&](int n, bool last) {          // every row tile in use against the next K tile is two calls: see below
+                const int st = kd % stages;
+                const uint32_t kaddr = k_s + st * Sh::kv_bytes, s_at = tmem + n * TN;
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k)
+                    mma_ss(s_at, desc_k(q_s + n * Sh::q_bytes + (k >> 2) * 16384) + 2 * (k & 3), desc_k(kaddr + (k >> 2) * (TN * 128)) + 2 * (k & 3), id_qk, k ? 1u : 0u);
+                mma_commit(sfull + 8 * n);
+                if (last) { mma_commit(kempty + 8 * st); ++kd; }
+            };
+            auto wait_k = [&]() {
+                ok = ok && mbar_wait(kfull + 8 * (kd % stages), (uint32_t)(kd / stages) & 1u, failed, status);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                fence_after();
+            };
+            while (left > 0 && ok) {
+                const int m = (int)min(left, (long long)(w.tiles - w.tile)), nt = NT == 2 && w.rows(a) > 128 ? 2 : 1;
+                ok = mbar_wait(qfull, (uint32_t)(item & 1), failed, status);
+                wait_k();
+                if (!ok) break;
+                for (int n = 0; n < nt; ++n) qk(n, n == nt - 1);
+                if (m == 1) mma_commit(qempty);
+                for (int j = 0; j < m && ok; ++j, ++vd) {
+                    const int st = vd % stages;
+                    for (int n = 0; n < nt && ok; ++n) {
+                        ok = mbar_wait(pfull + 8 * n, pph[n], failed, status);
+                        pph[n] ^= 1u;
+                        if (n == 0) ok = ok && mbar_wait(vfull + 8 * st, (uint32_t)(vd / stages) & 1u, failed, status);
+                        if (!ok) break;
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        fence_after();
+                        const uint32_t vaddr = v_s + st * Sh::kv_bytes, o_at = tmem + NT * TN + n * Sh::DV, p_at = tmem + n * TN;
+#pragma unroll
+                        for (int k = 0; k < TN / 16; ++k) mma_ts(o_at, p_at + 8 * k, desc_mn(vaddr + k * 2048, TN * 128), id_pv, j | k ? 1u : 0u);
+                        mma_commit(ofull + 8 * n);
+                        if (n == nt - 1) mma_commit(vempty + 8 * st);
+                        if (j + 1 < m) {
+                            if (n == 0) wait_k();
+                            if (!ok) break;
+                            qk(n, n == nt - 1);
+                            if (j + 2 == m && n == nt - 1) mma_commit(qempty);
+                        }
+                    }
+                }
+                left -= m;
+                ++item;
+                if (left > 0) w.next_item(p, b, a);
+            }
+            mma_commit(drain);                        // nothing issued runs when the CTA frees its TMEM
+            for (uint32_t i = 0; i < kSpin; ++i) {
+                uint32_t done;
+                asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], 0;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(drain) : "memory");
+                if (done) break;
+            }
+        }
+    } else {
+        // ---- softmax and epilogue: a thread a row
+        const int nt = wid >> 2, r_tile = (wid & 3) * 32 + lane, r_item = nt * 128 + r_tile;
+        const uint32_t lanes = (uint32_t)((wid & 3) * 32) << 16, s_at = tmem + nt * TN + lanes, o_at = tmem + NT * TN + nt * Sh::DV + lanes;
+        const float c = a.scale * 1.44269504088896f;
+        int done = 0, tiles_done = 0, part = 0;       // tiles of this row tile, of the CTA
+        bool ok = true;
+        while (left > 0 && ok) {
+            const int m = (int)min(left, (long long)(w.tiles - w.tile)), rows = w.rows(a);
+            const bool in_use = nt == 0 || rows > 128, works = r_tile - lane + nt * 128 < rows;   // the row tile; this warp
+            const int rr = w.rt * Sh::rows + r_item, i = rr / a.group;
+            float top = -INFINITY, sum = 0.f;         // top: what the weights are relative to, scaled, base 2
+            const bool may_hide = a.mask != nullptr || w.x.n > 1;
+            for (int j = 0; j < m && in_use; ++j, ++done) {
+                const int t = (w.tile + j) * TN;
+                ok = mbar_wait(sfull + 8 * nt, (uint32_t)done & 1u, failed, status);
+                ok = __all_sync(kFull, ok);
+                if (!ok) break;
+                fence_after();
+                const uint32_t* valid = words + ((tiles_done + j) % kWordRing) * 4;
+                bool masked = t + TN > w.x.len;
+#pragma unroll
+                for (int e = 0; e < TN / 32; ++e) masked |= valid[e] != ~0u;
+                if (works) {
+                    uint32_t vis[TN / 32];
+                    if (masked) {
+#pragma unroll
+                        for (int e = 0; e < TN / 32; ++e) vis[e] = valid[e] & (r_item < rows ? seen_bits(a, w.x, i, t + 32 * e) : 0u);
+                    }
+                    float x_top = -INFINITY;
+#pragma unroll
+                    for (int e = 0; e < TN / 32; ++e) {
+                        uint32_t x[32];
+                        tmem_ld32(s_at + 32 * e, x);
+                        wait_ld();
+                        if (masked) {
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) x[k] = vis[e] >> k & 1u ? x[k] : 0xff800000u;
+                        }
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) x_top = fmaxf(x_top, __uint_as_float(x[k]));
+                    }
+                    const float now = x_top * c;
+                    const bool raise = now > top + kRaise;            // also the first finite score
+                    if (__any_sync(kFull, raise)) {
+                        const float f = raise && top > -INFINITY ? exp2_approx(top - now) : raise ? 0.f : 1.f;
+                        if (raise) top = now;
+                        sum *= f;
+                        if (j > 0) {
+                            ok = mbar_wait(ofull + 8 * nt, (uint32_t)(done - 1) & 1u, failed, status);
+                            ok = __all_sync(kFull, ok);
+                            if (!ok) break;
+                            fence_after();
+#pragma unroll 1
+                            for (int e = 0; e < Sh::DV / 32; ++e) {
+                                uint32_t o[32];
+                                tmem_ld32(o_at + 32 * e, o);
+                                wait_ld();
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(f == 0.f ? 0.f : __uint_as_float(o[k]) * f);
+                                tmem_st32(o_at + 32 * e, o);
+                            }
+                        }
+                    }
+                    const float base = top == -INFINITY ? 0.f : top - Kind<T>::shift;
+                    float part_sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int e = 0; e < TN / 32; ++e) {
+                        uint32_t x[32], y[16];
+                        tmem_ld32(s_at + 32 * e, x);
+                        wait_ld();
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) {
+                            float v = exp2_approx(fmaf(__uint_as_float(x[k]), c, -base));
+                            if (masked) v = vis[e] >> k & 1u ? v : 0.f;
+                            x[k] = __float_as_uint(v);
+                            part_sum[k & 3] += v;
+                        }
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) y[k] = Kind<T>::pack(__uint_as_float(x[2 * k]), __uint_as_float(x[2 * k + 1]));
+                        tmem_st16(s_at + 16 * e, y);
+                    }
+                    sum += (part_sum[0] + part_sum[1]) + (part_sum[2] + part_sum[3]);
+                    wait_st();
+                }
+                if (may_hide && t + TN > w.x.len) {
+                    // Weights of 0 do not hide infinities and NaN from the product: at drafted positions they are taken out of V, and added
+                    // to the rows that see them at the end.
+                    const int st = (tiles_done + j) % stages;
+                    ok = mbar_wait(vfull + 8 * st, (uint32_t)((tiles_done + j) / stages) & 1u, failed, status);
+                    ok = __all_sync(kFull, ok);
+                    if (!ok) break;
+                    bool found = false;
+                    for (int u = (wid & 3) * 32 + lane; u < TN * Sh::blocks * 8; u += 128) {
+                        const int r = (u >> 3) % TN;
+                        if (t + r < w.x.len || (D == 32 && (((u & 7) ^ (r & 7)) >= 4))) continue;
+                        uint4* at = reinterpret_cast<uint4*>(vs + st * Sh::kv_bytes + u * 16);
+                        uint4 v = *at;
+                        uint32_t* h = reinterpret_cast<uint32_t*>(&v);
+                        bool hit = false;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            if ((h[k] & Kind<T>::exponent) == Kind<T>::exponent) { h[k] &= 0xffff0000u; hit = true; }
+                            if ((h[k] >> 16 & Kind<T>::exponent) == Kind<T>::exponent) { h[k] &= 0xffffu; hit = true; }
+                        }
+                        if (hit) {
+                            dirty[part & 1] = (uint32_t)part + 1u;
+                            __threadfence_block();            // who finds the zeros finds the flag
+                            *at = v;
+                            found = true;
+                        }
+                    }
+                    if (found) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(pfull + 8 * nt);
+            }
+            tiles_done += m;
+            if (ok && in_use) {
+                ok = mbar_wait(ofull + 8 * nt, (uint32_t)(done - 1) & 1u, failed, status);
+                ok = __all_sync(kFull, ok);
+            }
+            if (!ok) break;
+            if (in_use && works) {
+                fence_after();
+                const bool whole = w.tile == 0 && m == w.tiles, live = r_item < rows;
+                const int64_t n_row = w.x.first + i, head = (int64_t)w.h * a.group + (rr - i * a.group), slot = ((int64_t)2 * me + (part > 0)) * a.part_rows + r_item;
+                const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;   // NaN stays NaN
+                const bool special = may_hide && dirty[part & 1] == (uint32_t)part + 1u;
+#pragma unroll 1
+                for (int e = 0; e < (D + 31) / 32; ++e) {
+                    uint32_t o[32];
+                    tmem_ld32(o_at + 32 * e, o);
+                    wait_ld();
+                    if (!live) continue;
+                    if (sum == 0.f) {
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) o[k] = 0u;        // nothing was seen: whatever the product made of it
+                    }
+                    if (special) {
+                        for (int t = max(w.tile * TN, w.x.len); t < min((w.tile + m) * TN, w.x.kv); ++t) {
+                            if (!(seen_bits(a, w.x, i, t) & 1u)) continue;
+                            const int page = b.table[(int64_t)w.s * b.max_pages + t / p.page_pos];
+                            if (page < 0 || page >= p.n_pages) continue;
+                            const uint16_t* v = reinterpret_cast<const uint16_t*>(p.base + (int64_t)a.layer * p.sl + (int64_t)w.h * p.sh + p.skv +
+                                                                                  (int64_t)page * p.spage + (int64_t)(t % p.page_pos) * p.sp) + 32 * e;
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                if ((v[k] & Kind<T>::exponent) == Kind<T>::exponent) o[k] = __float_as_uint(__uint_as_float(o[k]) + Kind<T>::widen(v[k]));
+                        }
+                    }
+                    if (whole) {
+                        uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + n_row * a.os_row + head * a.os_head + 32 * e);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            uint32_t y[4];
+#pragma unroll
+                            for (int l = 0; l < 4; ++l) y[l] = Kind<T>::pack(__uint_as_float(o[8 * k + 2 * l]) * inv, __uint_as_float(o[8 * k + 2 * l + 1]) * inv);
+                            dst[k] = make_uint4(y[0], y[1], y[2], y[3]);
+                        }
+                    } else {
+                        uint4* dst = reinterpret_cast<uint4*>(a.part_o + slot * D + 32 * e);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) dst[k] = make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+                    }
+                }
+                if (live) {
+                    if (!whole) a.part_ml[slot] = make_float2(top, sum);
+                    else if (a.lse) a.lse[n_row * a.heads + head] = sum == 0.f ? -INFINITY : (top - Kind<T>::shift + log2f(sum)) * 0.693147180559945f;
+                }
+                fence_before();
+            }
+            left -= m;
+            ++part;
+            if (left > 0) w.next_item(p, b, a);
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (wid == mma_warp) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)Sh::tmem) : "memory");
+    }
+}
+
+// Joins the pieces of items that more than one CTA had: block c looks at the boundary between CTAs c - 1 and c, and takes the item if that is the
+// first boundary inside it.  A warp a row at a time.
+constexpr int kJoinThreads = 128, kJoinRows = 16;
+template <class T, int D, int ROWS>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(PoolDev p, BookDev b, const __grid_constant__ AttendArgs a, int workers) {
+    chain_wait();
+    const int c = blockIdx.x + 1, lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const int4 f = a.first[c], prev = a.first[c - 1];
+    if (f.x < 0 || f.w == 0) return;
+    auto same = [&](const int4& o) { return o.x == f.x && o.y == f.y && o.z == f.z; };
+    if (same(prev) && prev.w > 0) return;
+    const int64_t lead = (int64_t)2 * (c - 1) + (same(prev) ? 0 : 1);      // the piece that the item begins with
+    int last = c;
+    while (last + 1 < workers) {
+        const int4 o = a.first[last + 1];
+        if (!same(o) || o.w == 0) break;
+        ++last;
+    }
+    bool bad;
+    const Session x = session_of(p, b, a, f.x, &bad);
+    const int rows = min(ROWS, x.n * a.group - f.z * ROWS);
+    const int end = min(rows, ((int)blockIdx.y + 1) * kJoinRows);
+    for (int r = blockIdx.y * kJoinRows + wid; r < end; r += kJoinThreads / 32) {
+        auto at = [&](int k) -> int64_t { return (k < c ? lead : (int64_t)2 * k) * a.part_rows + r; };
+        float top = -INFINITY;
+        for (int k = c - 1; k <= last; ++k) top = fmaxf(top, a.part_ml[at(k)].x);
+        float sum = 0.f, o[D / 32];
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
+        for (int k = c - 1; k <= last; ++k) {
+            const float2 ml = a.part_ml[at(k)];
+            if (ml.y == 0.f) continue;                                     // nothing was seen there
+            const float w = exp2f(ml.x - top);
+            sum = fmaf(ml.y, w, sum);
+            const float* from = a.part_o + at(k) * D + lane;
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) o[e] = fmaf(from[32 * e], w, o[e]);
+        }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const int rr = f.z * ROWS + r, i = rr / a.group;
+        const int64_t n_row = x.first + i, head = (int64_t)f.y * a.group + (rr - i * a.group);
+        uint16_t* out = static_cast<uint16_t*>(a.out) + n_row * a.os_row + head * a.os_head + lane;
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) out[32 * e] = (uint16_t)(Kind<T>::pack(o[e] * inv, 0.f) & 0xffffu);
+        if (a.lse && lane == 0) a.lse[n_row * a.heads + head] = sum == 0.f ? -INFINITY : (top - Kind<T>::shift + log2f(sum)) * 0.693147180559945f;
+    }
+}
+
+// Which layout a call takes, and what it needs.
+struct Plan { int nt, grid, part_rows; uint64_t bytes; };
+template <int D, int NT> Plan plan_of(long long rows) {
+    using Sh = Shape<D, NT>;
+    Plan x;
+    x.nt = NT;
+    x.grid = Sh::per_sm * sm_count();
+    x.part_rows = (int)(rows < Sh::rows ? rows : Sh::rows);
+    x.bytes = (uint64_t)x.grid * 16 + 2ull * x.grid * x.part_rows * (8 + 4 * D);
+    return x;
+}
+// Two row tiles share K and V where a session has more rows than one holds.
+Plan plan(const PoolDev& p, int heads, int sessions, int n_rows) {
+    const long long rows = (long long)n_rows * (heads / p.H);
+    const bool two = rows > 128LL * sessions;
+    switch (p.d) {
+        case 32: return two ? plan_of<32, 2>(rows) : plan_of<32, 1>(rows);
+        case 64: return two ? plan_of<64, 2>(rows) : plan_of<64, 1>(rows);
+        case 128: return two ? plan_of<128, 2>(rows) : plan_of<128, 1>(rows);
+        default: return plan_of<256, 1>(rows);
+    }
+}
+
+template <class T, int D, int NT>
+cudaError_t launch_attend(const PoolDev& p, const BookDev& b, const AttendArgs& a, const Plan& x, uint32_t* status, cudaStream_t st) {
+    using Sh = Shape<D, NT>;
+    cudaError_t e = cudaFuncSetAttribute(attend_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Sh::smem);
+    if (e != cudaSuccess) return e;
+    e = launch_kernel(attend_kernel<T, D, NT>, x.grid, Sh::threads, Sh::smem, st, false, 1, p, b, a, status);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(x.grid - 1, (x.part_rows + kJoinRows - 1) / kJoinRows);
+    cfg.blockDim = dim3(kJoinThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, join_kernel<T, D, Sh::rows>, p, b, a, x.grid);
+}
+template <class T>
+cudaError_t launch_type(const PoolDev& p, const BookDev& b, const AttendArgs& a, const Plan& x, uint32_t* status, cudaStream_t st) {
+    switch (p.d) {
+        case 32: return x.nt == 2 ? launch_attend<T, 32, 2>(p, b, a, x, status, st) : launch_attend<T, 32, 1>(p, b, a, x, status, st);
+        case 64: return x.nt == 2 ? launch_attend<T, 64, 2>(p, b, a, x, status, st) : launch_attend<T, 64, 1>(p, b, a, x, status, st);
+        case 128: return x.nt == 2 ? launch_attend<T, 128, 2>(p, b, a, x, status, st) : launch_attend<T, 128, 1>(p, b, a, x, status, st);
+        default: return launch_attend<T, 256, 1>(p, b, a, x, status, st);
+    }
 }
 
 plc_status check_heads(const PoolDev& p, int32_t n_heads) {
@@ -128,12 +757,12 @@ using namespace plc;
 
 extern "C" {
 
-plc_status plc_tree_attention_workspace(const plc_page_pool* pool, int32_t n_heads, uint64_t* bytes) {
+plc_status plc_tree_attention_workspace(const plc_page_pool* pool, int32_t sessions, int32_t n_heads, int32_t n_rows, uint64_t* bytes) {
     PoolDev p;
     plc_status rc = check_pool(pool, &p);
     if (rc || (rc = check_heads(p, n_heads))) return rc;
-    if (!bytes) return PLC_E_INVALID;
-    *bytes = 16;
+    if (!bytes || sessions < 1 || n_rows < 0) return PLC_E_INVALID;
+    *bytes = plan(p, n_heads, sessions, n_rows).bytes;
     return PLC_OK;
 }
 
@@ -146,19 +775,24 @@ plc_status plc_tree_attention(const plc_page_pool* pool, int32_t layer, const pl
     if (!t || !t->q_dev || !t->out_dev || !t->begin_dev || t->n_rows < 0 || !status_dev || !workspace_dev) return PLC_E_INVALID;
     if (layer < 0 || layer >= p.L || pool->dtype == PLC_OUT_F32 || (t->mask_dev && t->mask_words < 1) || !(scale > 0.f) || isinf(scale)) return PLC_E_INVALID;
     if ((rc = check_heads(p, t->n_heads))) return rc;
+    const int group = t->n_heads / p.H;
+    if ((long long)t->n_rows * group > (1 << 30)) return PLC_E_SHAPE;
     if (!plc_aligned16(t->q_dev) || !plc_aligned16(t->out_dev) || !plc_aligned16(workspace_dev) || t->q_stride_row % 8 || t->q_stride_head % 8 ||
         t->out_stride_row % 8 || t->out_stride_head % 8)
         return PLC_E_ALIGN;
-    uint64_t need = 0;
-    plc_tree_attention_workspace(pool, t->n_heads, &need);
-    if (workspace_bytes < need) return PLC_E_CAPACITY;
+    const Plan x = plan(p, t->n_heads, b.rows, t->n_rows);
+    if (workspace_bytes < x.bytes) return PLC_E_CAPACITY;
     if (t->n_rows == 0) return PLC_OK;
-    const AttendArgs a{t->q_dev, t->q_stride_row, t->q_stride_head, t->out_dev, t->out_stride_row, t->out_stride_head, t->lse_dev, t->begin_dev,
-                       t->mask_dev, t->n_rows, t->n_heads, t->n_heads / p.H, t->mask_dev ? t->mask_words : 0, layer, scale};
+    AttendArgs a{t->q_dev, t->q_stride_row, t->q_stride_head, t->out_dev, t->out_stride_row, t->out_stride_head, t->lse_dev, t->begin_dev,
+                 t->mask_dev, t->n_rows, t->n_heads, group, t->mask_dev ? t->mask_words : 0, layer, scale, nullptr, nullptr, nullptr, x.part_rows};
+    a.first = static_cast<int4*>(workspace_dev);
+    a.part_o = reinterpret_cast<float*>(a.first + x.grid);
+    a.part_ml = reinterpret_cast<float2*>(a.part_o + 2ll * x.grid * x.part_rows * p.d);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = pool->dtype == PLC_OUT_F16 ? launch_attend<__half>(p, b, a, status_dev, st) : launch_attend<__nv_bfloat16>(p, b, a, status_dev, st);
+    const cudaError_t e =
+        pool->dtype == PLC_OUT_F16 ? launch_type<__half>(p, b, a, x, status_dev, st) : launch_type<__nv_bfloat16>(p, b, a, x, status_dev, st);
     if (e != cudaSuccess) return PLC_E_CUDA;
-    count_launch();
+    count_launch(2);
     return PLC_OK;
 }
 

@@ -200,7 +200,7 @@ class PagePool:
             if N == 0:
                 return out, lse
             b = C.c_uint64()
-            _check(lib().plc_tree_attention_workspace(C.byref(self._c), heads, C.byref(b)), "plc_tree_attention_workspace")
+            _check(lib().plc_tree_attention_workspace(C.byref(self._c), book.table.shape[0], heads, N, C.byref(b)), "plc_tree_attention_workspace")
             ws = torch.empty(b.value, dtype=torch.uint8, device=dev)
             t = TreeQueries(q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr(),
                             begin.data_ptr(), None if mask is None else mask.data_ptr(), N, heads, words)

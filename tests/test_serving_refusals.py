@@ -43,7 +43,7 @@ def test_pools_that_are_refused(lib, change, code):
     assert lib.plc_pages_keep(C.byref(p), C.byref(i), C.c_void_p(A), C.c_void_p(A), 4, C.byref(o), C.c_void_p(A), None) == code
     assert lib.plc_pages_compact(C.byref(p), C.byref(i), C.byref(o), C.c_void_p(A), C.c_void_p(WS), C.c_uint64(1 << 20), C.c_void_p(A), None) == code
     b = C.c_uint64()
-    assert lib.plc_tree_attention_workspace(C.byref(p), 4, C.byref(b)) == code
+    assert lib.plc_tree_attention_workspace(C.byref(p), 3, 4, 7, C.byref(b)) == code
 
 
 def test_books_and_workspaces_that_are_refused(lib):
@@ -77,7 +77,7 @@ def queries(**change):
     (dict(q_stride_row=516), plc.E_ALIGN), (dict(out_stride_head=68), plc.E_ALIGN)])
 def test_queries_that_are_refused(lib, change, code):
     p, b, t, n = pool(), book(), queries(**change), C.c_uint64()
-    assert lib.plc_tree_attention_workspace(C.byref(p), 8, C.byref(n)) == plc.OK
+    assert lib.plc_tree_attention_workspace(C.byref(p), 3, 8, 7, C.byref(n)) == plc.OK
     call = lambda layer, scale, p, bytes_: lib.plc_tree_attention(C.byref(p), layer, C.byref(b), C.byref(t), C.c_float(scale), C.c_void_p(WS),  # noqa: E731
                                                                   C.c_uint64(bytes_), C.c_void_p(A), None)
     assert call(0, 0.125, p, n.value) == code
