@@ -18,134 +18,13 @@
 // The weights are rounded to the type of V because the product takes both operands in one type; l sums them unrounded.  For f16
 // they are formed as 2^12 times themselves, so that weights down to 2^-26 of the largest keep all their bits.  A
 // row's maximum is raised only when it would grow by more than 2^3 (a weight is at most 2^15 then), which spares most passes over O.
-#include <cuda_bf16.h>
-
-#include "plc_pages.cuh"
+#include "plc_attend.cuh"
 
 namespace plc {
 namespace {
 
-constexpr uint32_t kSpin = 1u << 22;
 constexpr int kLoaders = 96;                      // threads that copy: three warps, so that a CTA has a whole number of warps a scheduler
-constexpr float kRaise = 3.f, kShiftF16 = 12.f;
 constexpr int kWordRing = 4;                      // tiles whose validity words are kept: more than the loader can be ahead of the softmax
-
-struct AttendArgs {
-    const void* q; int64_t qs_row, qs_head;       // elements
-    void* out; int64_t os_row, os_head;
-    float* lse;
-    const int32_t* begin; const uint32_t* mask;
-    int rows, heads, group, mask_words, layer;
-    float scale;
-    float* part_o;                                // [2 * grid][part_rows][d]
-    float2* part_ml;                              // [2 * grid][part_rows]: maximum (scaled, base 2), sum
-    int4* first;                                  // [grid]: session, head, row tile, first position tile of each CTA's range (-1: none)
-    int part_rows;
-};
-
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(n) : "memory"); }
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
-// Arrives when the thread's copies issued so far have landed.
-__device__ __forceinline__ void mbar_arrive_copies(uint32_t bar) {
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
-}
-// Bounded wait: false where another role has given up, or (error bit set) the phase did not complete within the limit.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* failed, uint32_t* status) {
-    for (uint32_t i = 0; i < kSpin; ++i) {
-        uint32_t ok;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-        if (ok) return true;
-        if ((i & 15) == 15 && *failed) return false;
-    }
-    *failed = 1u;
-    atomicOr(status, kStTimeout);
-    return false;
-}
-__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool take) {   // zeros where not `take`
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
-}
-// 128-byte swizzled rows.  K-major (Q, K): 1024 bytes from eight rows to the next eight.  MN-major (V): the same step along
-// the positions, `block` bytes from 64 components to the next 64.
-__device__ __forceinline__ uint64_t desc_k(uint32_t addr) { return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61); }
-__device__ __forceinline__ uint64_t desc_mn(uint32_t addr, uint32_t block) {
-    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(block >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
-}
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(0u) : "memory");
-}
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc), "r"(0u) : "memory");
-}
-__device__ __forceinline__ void mma_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t* r) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
-          "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(addr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
-        "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
-        "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-        : "memory");
-}
-__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr), "r"(r[0]),
-        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]),
-        "r"(r[14]), "r"(r[15])
-        : "memory");
-}
-__device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ float exp2_approx(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-
-template <class T> struct Kind;
-template <> struct Kind<__half> {
-    static constexpr uint32_t format = 0;
-    static constexpr float shift = kShiftF16;
-    static constexpr uint32_t exponent = 0x7c00u;
-    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
-        const __half2 h = __floats2half2_rn(lo, hi);
-        return *reinterpret_cast<const uint32_t*>(&h);
-    }
-    static __device__ __forceinline__ float widen(uint16_t v) { return __half2float(__ushort_as_half(v)); }
-};
-template <> struct Kind<__nv_bfloat16> {
-    static constexpr uint32_t format = 1;
-    static constexpr float shift = 0.f;
-    static constexpr uint32_t exponent = 0x7f80u;
-    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
-        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-        return *reinterpret_cast<const uint32_t*>(&h);
-    }
-    static __device__ __forceinline__ float widen(uint16_t v) { return __bfloat162float(__ushort_as_bfloat16(v)); }
-};
 
 template <int D, int NT> struct Shape {
     static constexpr int TN = D == 256 ? 64 : 128;                     // positions a tile: S and O of a CTA's row tiles fit in TMEM, K and V in shared memory
@@ -158,65 +37,6 @@ template <int D, int NT> struct Shape {
     static constexpr int per_sm = NT == 1 && D != 256 ? 2 : 1;
     static constexpr size_t smem = (size_t)NT * q_bytes + 2 * stages * kv_bytes + 2 * TN * 8 + 1024 + 512;
 };
-
-// A session as the call gives it, cut to what there is.
-struct Session { int first, n, len, kv; };
-__device__ __forceinline__ Session session_of(const PoolDev& p, const BookDev& b, const AttendArgs& a, int s, bool* bad) {
-    const int b0 = a.begin[s], b1 = a.begin[s + 1], len = b.len[s], most = most_positions(b, p);
-    Session x;
-    x.first = min(max(b0, 0), a.rows);
-    x.n = min(max(b1, x.first), a.rows) - x.first;
-    x.len = min(max(len, 0), most);
-    x.kv = x.n > 0 ? (int)min((long long)x.len + x.n, (long long)most) : 0;
-    *bad = b0 < 0 || b1 < b0 || b1 > a.rows || len < 0 || len > most || (long long)x.len + x.n > most;
-    return x;
-}
-
-// Where a range of position tiles stands: item (session, head, row tile) and tile in it.
-template <int TN, int ROWS> struct Walk {
-    int s, h, rt, tile, tiles, row_tiles;
-    Session x;
-    __device__ __forceinline__ void enter(const PoolDev& p, const BookDev& b, const AttendArgs& a) {
-        bool bad;
-        x = session_of(p, b, a, s, &bad);
-        tiles = (x.kv + TN - 1) / TN;
-        row_tiles = (int)(((long long)x.n * a.group + ROWS - 1) / ROWS);
-    }
-    __device__ __forceinline__ void start(const PoolDev& p, const BookDev& b, const AttendArgs& a, int session, long long rest) {
-        s = session;
-        enter(p, b, a);
-        const int item = (int)(rest / tiles);
-        tile = (int)(rest - (long long)item * tiles);
-        h = item / row_tiles;
-        rt = item - h * row_tiles;
-    }
-    __device__ __forceinline__ void next_item(const PoolDev& p, const BookDev& b, const AttendArgs& a) {
-        tile = 0;
-        if (++rt < row_tiles) return;
-        rt = 0;
-        if (++h < p.H) return;
-        h = 0;
-        do {
-            if (++s >= b.rows) return;
-            enter(p, b, a);
-        } while (x.n == 0);
-    }
-    __device__ __forceinline__ int rows(const AttendArgs& a) const { return min(ROWS, x.n * a.group - rt * ROWS); }
-};
-
-// 32 bits: which of the positions t .. t+31 row i (the i-th drafted token) sees, as far as the mask says.
-__device__ __forceinline__ uint32_t seen_bits(const AttendArgs& a, const Session& x, int i, int t) {
-    const int j = t - x.len;                      // drafted index of the first one
-    if (j <= -32) return ~0u;
-    auto word = [&](int w) -> uint32_t {          // drafted positions 32 w ...
-        if (w < 0) return ~0u;                    // committed ones
-        if (a.mask) return w < a.mask_words ? a.mask[(int64_t)(x.first + i) * a.mask_words + w] : 0u;
-        const int up = i - 32 * w;                // bits 0 .. up
-        return up < 0 ? 0u : up >= 31 ? ~0u : (2u << up) - 1u;
-    };
-    const int w = j >> 5;
-    return __funnelshift_r(word(w), word(w + 1), j & 31);
-}
 
 template <class T, int D, int NT>
 __global__ void __launch_bounds__(Shape<D, NT>::threads, Shape<D, NT>::per_sm)
@@ -235,8 +55,6 @@ attend_kernel(PoolDev p, BookDev b, const __grid_constant__ AttendArgs a, uint32
     volatile uint32_t* failed = tmem_slot + 1;
     // [2]: piece number + 1 of the last pieces whose V holds infinities or NaN at drafted positions, by its parity (no row tile is a whole piece behind)
     volatile uint32_t* dirty = tmem_slot + 2;
-    __shared__ long long sums[n_warps];
-    __shared__ long long range_at[2];             // the range's first session, and the tiles of it that lie before the range
     const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
     const uint32_t kfull = smem_u32(bars), vfull = kfull + 8 * stages, kempty = vfull + 8 * stages, vempty = kempty + 8 * stages;
     const uint32_t qfull = vempty + 8 * stages, qempty = qfull + 8, drain = qempty + 8, sfull = drain + 8, pfull = sfull + 8 * NT, ofull = pfull + 8 * NT;
@@ -267,54 +85,11 @@ attend_kernel(PoolDev p, BookDev b, const __grid_constant__ AttendArgs a, uint32
     }
     fence_before();
 
-    // this CTA's range of the sequence of tiles: a thread sums a run of sessions, the threads' sums are scanned
-    const int run = (b.rows + Sh::threads - 1) / Sh::threads, s0 = min(b.rows, tid * run), s1 = min(b.rows, s0 + run);
-    auto tiles_of = [&](int s, bool* bad) -> long long {
-        const Session x = session_of(p, b, a, s, bad);
-        return (long long)((x.kv + TN - 1) / TN) * (((long long)x.n * a.group + Sh::rows - 1) / Sh::rows) * p.H;
-    };
-    long long mine = 0;
-    bool any_bad = false;
-    for (int s = s0; s < s1; ++s) {
-        bool bad;
-        mine += tiles_of(s, &bad);
-        any_bad |= bad;
-    }
-    if (any_bad && blockIdx.x == 0) atomicOr(status, kStRange);
-    long long upto = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(kFull, upto, o);
-        if (lane >= o) upto += v;
-    }
-    if (lane == 31) sums[wid] = upto;
-    __syncthreads();
+    Wk w{};
+    long long left = find_range<TN, Sh::rows, Sh::threads>(p, b, a, status, w);
     fence_after();
     const uint32_t tmem = *tmem_slot;
-    long long total = 0, ahead = upto - mine;
-    for (int w = 0; w < n_warps; ++w) {
-        if (w < wid) ahead += sums[w];
-        total += sums[w];
-    }
-    const int workers = (int)min((long long)gridDim.x, total), me = blockIdx.x;
-    const long long t0 = me < workers ? total * me / workers : total, t1 = me < workers ? total * (me + 1) / workers : total;
-    if (t0 < t1 && t0 >= ahead && t0 < ahead + mine) {
-        long long at = ahead;
-        bool bad;
-        int s = s0;
-        for (; s < s1; ++s) {
-            const long long f = tiles_of(s, &bad);
-            if (t0 < at + f) break;
-            at += f;
-        }
-        range_at[0] = s;
-        range_at[1] = t0 - at;
-    }
-    __syncthreads();
-    Wk w{};
-    long long left = t1 - t0;
-    if (left > 0) w.start(p, b, a, (int)range_at[0], range_at[1]);
-    if (tid == 0) a.first[me] = left > 0 ? make_int4(w.s, w.h, w.rt, w.tile) : make_int4(-1, 0, 0, 0);
+    const int me = blockIdx.x;
 
     if (wid >= NT * 4 && wid < mma_warp) {
         // ---- copies.  A tile's addresses are found by one thread a position and passed on in shared memory.
@@ -494,7 +269,7 @@ attend_kernel(PoolDev p, BookDev b, const __grid_constant__ AttendArgs a, uint32
                     for (int e = 0; e < TN / 32; ++e) {
                         uint32_t x[32];
                         tmem_ld32(s_at + 32 * e, x);
-                        wait_ld();
+                        wait_ld(x);
                         if (masked) {
 #pragma unroll
                             for (int k = 0; k < 32; ++k) x[k] = vis[e] >> k & 1u ? x[k] : 0xff800000u;
@@ -517,7 +292,7 @@ attend_kernel(PoolDev p, BookDev b, const __grid_constant__ AttendArgs a, uint32
                             for (int e = 0; e < Sh::DV / 32; ++e) {
                                 uint32_t o[32];
                                 tmem_ld32(o_at + 32 * e, o);
-                                wait_ld();
+                                wait_ld(o);
 #pragma unroll
                                 for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(f == 0.f ? 0.f : __uint_as_float(o[k]) * f);
                                 tmem_st32(o_at + 32 * e, o);
@@ -530,7 +305,7 @@ attend_kernel(PoolDev p, BookDev b, const __grid_constant__ AttendArgs a, uint32
                     for (int e = 0; e < TN / 32; ++e) {
                         uint32_t x[32], y[16];
                         tmem_ld32(s_at + 32 * e, x);
-                        wait_ld();
+                        wait_ld(x);
 #pragma unroll
                         for (int k = 0; k < 32; ++k) {
                             float v = exp2_approx(fmaf(__uint_as_float(x[k]), c, -base));
@@ -594,7 +369,7 @@ attend_kernel(PoolDev p, BookDev b, const __grid_constant__ AttendArgs a, uint32
                 for (int e = 0; e < (D + 31) / 32; ++e) {
                     uint32_t o[32];
                     tmem_ld32(o_at + 32 * e, o);
-                    wait_ld();
+                    wait_ld(o);
                     if (!live) continue;
                     if (sum == 0.f) {
 #pragma unroll
@@ -646,68 +421,29 @@ attend_kernel(PoolDev p, BookDev b, const __grid_constant__ AttendArgs a, uint32
     }
 }
 
-// Joins the pieces of items that more than one CTA had: block c looks at the boundary between CTAs c - 1 and c, and takes the item if that is the
-// first boundary inside it.  A warp a row at a time.
-constexpr int kJoinThreads = 128, kJoinRows = 16;
-template <class T, int D, int ROWS>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(PoolDev p, BookDev b, const __grid_constant__ AttendArgs a, int workers) {
-    chain_wait();
-    const int c = blockIdx.x + 1, lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    const int4 f = a.first[c], prev = a.first[c - 1];
-    if (f.x < 0 || f.w == 0) return;
-    auto same = [&](const int4& o) { return o.x == f.x && o.y == f.y && o.z == f.z; };
-    if (same(prev) && prev.w > 0) return;
-    const int64_t lead = (int64_t)2 * (c - 1) + (same(prev) ? 0 : 1);      // the piece that the item begins with
-    int last = c;
-    while (last + 1 < workers) {
-        const int4 o = a.first[last + 1];
-        if (!same(o) || o.w == 0) break;
-        ++last;
-    }
-    bool bad;
-    const Session x = session_of(p, b, a, f.x, &bad);
-    const int rows = min(ROWS, x.n * a.group - f.z * ROWS);
-    const int end = min(rows, ((int)blockIdx.y + 1) * kJoinRows);
-    for (int r = blockIdx.y * kJoinRows + wid; r < end; r += kJoinThreads / 32) {
-        auto at = [&](int k) -> int64_t { return (k < c ? lead : (int64_t)2 * k) * a.part_rows + r; };
-        float top = -INFINITY;
-        for (int k = c - 1; k <= last; ++k) top = fmaxf(top, a.part_ml[at(k)].x);
-        float sum = 0.f, o[D / 32];
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
-        for (int k = c - 1; k <= last; ++k) {
-            const float2 ml = a.part_ml[at(k)];
-            if (ml.y == 0.f) continue;                                     // nothing was seen there
-            const float w = exp2f(ml.x - top);
-            sum = fmaf(ml.y, w, sum);
-            const float* from = a.part_o + at(k) * D + lane;
-#pragma unroll
-            for (int e = 0; e < D / 32; ++e) o[e] = fmaf(from[32 * e], w, o[e]);
-        }
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        const int rr = f.z * ROWS + r, i = rr / a.group;
-        const int64_t n_row = x.first + i, head = (int64_t)f.y * a.group + (rr - i * a.group);
-        uint16_t* out = static_cast<uint16_t*>(a.out) + n_row * a.os_row + head * a.os_head + lane;
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e) out[32 * e] = (uint16_t)(Kind<T>::pack(o[e] * inv, 0.f) & 0xffffu);
-        if (a.lse && lane == 0) a.lse[n_row * a.heads + head] = sum == 0.f ? -INFINITY : (top - Kind<T>::shift + log2f(sum)) * 0.693147180559945f;
-    }
-}
-
-// Which layout a call takes, and what it needs.
-struct Plan { int nt, grid, part_rows; uint64_t bytes; };
-template <int D, int NT> Plan plan_of(long long rows) {
+template <int D, int NT> AttendPlan plan_of(long long rows) {
     using Sh = Shape<D, NT>;
-    Plan x;
-    x.nt = NT;
+    AttendPlan x;
+    x.row_tile = Sh::rows;
     x.grid = Sh::per_sm * sm_count();
     x.part_rows = (int)(rows < Sh::rows ? rows : Sh::rows);
     x.bytes = (uint64_t)x.grid * 16 + 2ull * x.grid * x.part_rows * (8 + 4 * D);
     return x;
 }
-// Two row tiles share K and V where a session has more rows than one holds.
-Plan plan(const PoolDev& p, int heads, int sessions, int n_rows) {
+// Up to kFewRows rows a session and KV head (32 of 256 components) take the layout for few rows; beyond, two row tiles share K and V where a
+// session has more rows than one holds.
+constexpr int kFewRows = 64;
+AttendPlan plan(const PoolDev& p, int heads, int sessions, int n_rows) {
     const long long rows = (long long)n_rows * (heads / p.H);
+    const int few = p.d == 256 ? kFewRows / 2 : kFewRows;
+    if (rows <= (long long)few * sessions) {
+        AttendPlan x;
+        x.row_tile = few;
+        x.grid = sm_count();
+        x.part_rows = (int)(rows < few ? rows : few);
+        x.bytes = (uint64_t)x.grid * 16 + 2ull * x.grid * x.part_rows * (8 + 4 * p.d);
+        return x;
+    }
     const bool two = rows > 128LL * sessions;
     switch (p.d) {
         case 32: return two ? plan_of<32, 2>(rows) : plan_of<32, 1>(rows);
@@ -718,29 +454,19 @@ Plan plan(const PoolDev& p, int heads, int sessions, int n_rows) {
 }
 
 template <class T, int D, int NT>
-cudaError_t launch_attend(const PoolDev& p, const BookDev& b, const AttendArgs& a, const Plan& x, uint32_t* status, cudaStream_t st) {
+cudaError_t launch_attend(const PoolDev& p, const BookDev& b, const AttendArgs& a, const AttendPlan& x, uint32_t* status, cudaStream_t st) {
     using Sh = Shape<D, NT>;
     cudaError_t e = cudaFuncSetAttribute(attend_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Sh::smem);
     if (e != cudaSuccess) return e;
     e = launch_kernel(attend_kernel<T, D, NT>, x.grid, Sh::threads, Sh::smem, st, false, 1, p, b, a, status);
-    if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(x.grid - 1, (x.part_rows + kJoinRows - 1) / kJoinRows);
-    cfg.blockDim = dim3(kJoinThreads);
-    cfg.stream = st;
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &at;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, join_kernel<T, D, Sh::rows>, p, b, a, x.grid);
+    return e != cudaSuccess ? e : launch_join<T, D, Sh::rows>(p, b, a, x, st);
 }
 template <class T>
-cudaError_t launch_type(const PoolDev& p, const BookDev& b, const AttendArgs& a, const Plan& x, uint32_t* status, cudaStream_t st) {
+cudaError_t launch_type(const PoolDev& p, const BookDev& b, const AttendArgs& a, const AttendPlan& x, uint32_t* status, cudaStream_t st) {
     switch (p.d) {
-        case 32: return x.nt == 2 ? launch_attend<T, 32, 2>(p, b, a, x, status, st) : launch_attend<T, 32, 1>(p, b, a, x, status, st);
-        case 64: return x.nt == 2 ? launch_attend<T, 64, 2>(p, b, a, x, status, st) : launch_attend<T, 64, 1>(p, b, a, x, status, st);
-        case 128: return x.nt == 2 ? launch_attend<T, 128, 2>(p, b, a, x, status, st) : launch_attend<T, 128, 1>(p, b, a, x, status, st);
+        case 32: return x.row_tile == 256 ? launch_attend<T, 32, 2>(p, b, a, x, status, st) : launch_attend<T, 32, 1>(p, b, a, x, status, st);
+        case 64: return x.row_tile == 256 ? launch_attend<T, 64, 2>(p, b, a, x, status, st) : launch_attend<T, 64, 1>(p, b, a, x, status, st);
+        case 128: return x.row_tile == 256 ? launch_attend<T, 128, 2>(p, b, a, x, status, st) : launch_attend<T, 128, 1>(p, b, a, x, status, st);
         default: return launch_attend<T, 256, 1>(p, b, a, x, status, st);
     }
 }
@@ -780,7 +506,7 @@ plc_status plc_tree_attention(const plc_page_pool* pool, int32_t layer, const pl
     if (!plc_aligned16(t->q_dev) || !plc_aligned16(t->out_dev) || !plc_aligned16(workspace_dev) || t->q_stride_row % 8 || t->q_stride_head % 8 ||
         t->out_stride_row % 8 || t->out_stride_head % 8)
         return PLC_E_ALIGN;
-    const Plan x = plan(p, t->n_heads, b.rows, t->n_rows);
+    const AttendPlan x = plan(p, t->n_heads, b.rows, t->n_rows);
     if (workspace_bytes < x.bytes) return PLC_E_CAPACITY;
     if (t->n_rows == 0) return PLC_OK;
     AttendArgs a{t->q_dev, t->q_stride_row, t->q_stride_head, t->out_dev, t->out_stride_row, t->out_stride_head, t->lse_dev, t->begin_dev,
@@ -789,8 +515,8 @@ plc_status plc_tree_attention(const plc_page_pool* pool, int32_t layer, const pl
     a.part_o = reinterpret_cast<float*>(a.first + x.grid);
     a.part_ml = reinterpret_cast<float2*>(a.part_o + 2ll * x.grid * x.part_rows * p.d);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const cudaError_t e =
-        pool->dtype == PLC_OUT_F16 ? launch_type<__half>(p, b, a, x, status_dev, st) : launch_type<__nv_bfloat16>(p, b, a, x, status_dev, st);
+    const cudaError_t e = x.row_tile <= kFewRows ? launch_attend_few(p, b, a, x, pool->dtype == PLC_OUT_BF16, status_dev, st)
+        : pool->dtype == PLC_OUT_F16 ? launch_type<__half>(p, b, a, x, status_dev, st) : launch_type<__nv_bfloat16>(p, b, a, x, status_dev, st);
     if (e != cudaSuccess) return PLC_E_CUDA;
     count_launch(2);
     return PLC_OK;

@@ -1,0 +1,343 @@
+// Tree attention: what its kernels share (the sequence of position tiles and a CTA's range of it, masks, the tensor core's instructions).
+#pragma once
+#include <cuda_bf16.h>
+
+#include "plc_pages.cuh"
+
+namespace plc {
+
+constexpr uint32_t kSpin = 1u << 22;
+constexpr float kRaise = 3.f, kShiftF16 = 12.f;
+
+struct AttendArgs {
+    const void* q; int64_t qs_row, qs_head;       // elements
+    void* out; int64_t os_row, os_head;
+    float* lse;
+    const int32_t* begin; const uint32_t* mask;
+    int rows, heads, group, mask_words, layer;
+    float scale;
+    float* part_o;                                // [2 * grid][part_rows][d]
+    float2* part_ml;                              // [2 * grid][part_rows]: maximum (scaled, base 2), sum
+    int4* first;                                  // [grid]: session, head, row tile, first position tile of each CTA's range (-1: none)
+    int part_rows;
+};
+
+// Which kernel a call takes, and what it needs.
+struct AttendPlan { int row_tile, grid, part_rows; uint64_t bytes; };
+
+cudaError_t launch_attend_few(const PoolDev& p, const BookDev& b, const AttendArgs& a, const AttendPlan& x, bool bf16, uint32_t* status, cudaStream_t st);
+
+#ifdef __CUDACC__
+namespace {
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t n) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(n) : "memory"); }
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// Arrives when the thread's copies issued so far have landed.
+__device__ __forceinline__ void mbar_arrive_copies(uint32_t bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+// Bounded wait: false where another role has given up, or (error bit set) the phase did not complete within the limit.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* failed, uint32_t* status) {
+    for (uint32_t i = 0; i < kSpin; ++i) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (ok) return true;
+        if ((i & 15) == 15 && *failed) return false;
+    }
+    *failed = 1u;
+    atomicOr(status, kStTimeout);
+    return false;
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool take) {   // zeros where not `take`
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
+}
+// 128-byte swizzled rows.  K-major (Q, K): 1024 bytes from eight rows to the next eight.  MN-major (V): the same step along
+// the positions, `block` bytes from 64 components to the next 64.
+__device__ __forceinline__ uint64_t desc_k(uint32_t addr) { return (uint64_t)((addr & 0x3FFFFu) >> 4) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61); }
+__device__ __forceinline__ uint64_t desc_mn(uint32_t addr, uint32_t block) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(block >> 4) << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(0u) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc), "r"(0u) : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+          "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+        "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
+        "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr), "r"(r[0]),
+        "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]),
+        "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+// The loads into r have arrived; what is computed from r stays behind this.
+template <int N> __device__ __forceinline__ void wait_ld(uint32_t (&r)[N]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
+}
+__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+template <class T> struct Kind;
+template <> struct Kind<__half> {
+    static constexpr uint32_t format = 0;
+    static constexpr float shift = kShiftF16;
+    static constexpr uint32_t exponent = 0x7c00u;
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    static __device__ __forceinline__ float widen(uint16_t v) { return __half2float(__ushort_as_half(v)); }
+};
+template <> struct Kind<__nv_bfloat16> {
+    static constexpr uint32_t format = 1;
+    static constexpr float shift = 0.f;
+    static constexpr uint32_t exponent = 0x7f80u;
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    static __device__ __forceinline__ float widen(uint16_t v) { return __bfloat162float(__ushort_as_bfloat16(v)); }
+};
+
+// A session as the call gives it, cut to what there is.
+struct Session { int first, n, len, kv; };
+__device__ __forceinline__ Session session_of(const PoolDev& p, const BookDev& b, const AttendArgs& a, int s, bool* bad) {
+    const int b0 = a.begin[s], b1 = a.begin[s + 1], len = b.len[s], most = most_positions(b, p);
+    Session x;
+    x.first = min(max(b0, 0), a.rows);
+    x.n = min(max(b1, x.first), a.rows) - x.first;
+    x.len = min(max(len, 0), most);
+    x.kv = x.n > 0 ? (int)min((long long)x.len + x.n, (long long)most) : 0;
+    *bad = b0 < 0 || b1 < b0 || b1 > a.rows || len < 0 || len > most || (long long)x.len + x.n > most;
+    return x;
+}
+
+// Where a range of position tiles stands: item (session, head, row tile) and tile in it.
+template <int TN, int ROWS> struct Walk {
+    int s, h, rt, tile, tiles, row_tiles;
+    Session x;
+    __device__ __forceinline__ void enter(const PoolDev& p, const BookDev& b, const AttendArgs& a) {
+        bool bad;
+        x = session_of(p, b, a, s, &bad);
+        tiles = (x.kv + TN - 1) / TN;
+        row_tiles = (int)(((long long)x.n * a.group + ROWS - 1) / ROWS);
+    }
+    __device__ __forceinline__ void start(const PoolDev& p, const BookDev& b, const AttendArgs& a, int session, long long rest) {
+        s = session;
+        enter(p, b, a);
+        const int item = (int)(rest / tiles);
+        tile = (int)(rest - (long long)item * tiles);
+        h = item / row_tiles;
+        rt = item - h * row_tiles;
+    }
+    __device__ __forceinline__ void next_item(const PoolDev& p, const BookDev& b, const AttendArgs& a) {
+        tile = 0;
+        if (++rt < row_tiles) return;
+        rt = 0;
+        if (++h < p.H) return;
+        h = 0;
+        do {
+            if (++s >= b.rows) return;
+            enter(p, b, a);
+        } while (x.n == 0);
+    }
+    __device__ __forceinline__ int rows(const AttendArgs& a) const { return min(ROWS, x.n * a.group - rt * ROWS); }
+};
+
+// 32 bits: which of the positions t .. t+31 row i (the i-th drafted token) sees, as far as the mask says.
+__device__ __forceinline__ uint32_t seen_bits(const AttendArgs& a, const Session& x, int i, int t) {
+    const int j = t - x.len;                      // drafted index of the first one
+    if (j <= -32) return ~0u;
+    auto word = [&](int w) -> uint32_t {          // drafted positions 32 w ...
+        if (w < 0) return ~0u;                    // committed ones
+        if (a.mask) return w < a.mask_words ? a.mask[(int64_t)(x.first + i) * a.mask_words + w] : 0u;
+        const int up = i - 32 * w;                // bits 0 .. up
+        return up < 0 ? 0u : up >= 31 ? ~0u : (2u << up) - 1u;
+    };
+    const int w = j >> 5;
+    return __funnelshift_r(word(w), word(w + 1), j & 31);
+}
+
+// A CTA's range [0, left) of the sequence of tiles, from w on.  Every thread of the CTA calls it; two barriers.
+template <int TN, int ROWS, int THREADS>
+__device__ __forceinline__ long long find_range(const PoolDev& p, const BookDev& b, const AttendArgs& a, uint32_t* status, Walk<TN, ROWS>& w) {
+    __shared__ long long sums[THREADS / 32];
+    __shared__ long long range_at[2];             // the range's first session, and the tiles of it that lie before the range
+    const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
+    // a thread sums a run of sessions, the threads' sums are scanned
+    const int run = (b.rows + THREADS - 1) / THREADS, s0 = min(b.rows, tid * run), s1 = min(b.rows, s0 + run);
+    auto tiles_of = [&](int s, bool* bad) -> long long {
+        const Session x = session_of(p, b, a, s, bad);
+        return (long long)((x.kv + TN - 1) / TN) * (((long long)x.n * a.group + ROWS - 1) / ROWS) * p.H;
+    };
+    long long mine = 0;
+    bool any_bad = false;
+    for (int s = s0; s < s1; ++s) {
+        bool bad;
+        mine += tiles_of(s, &bad);
+        any_bad |= bad;
+    }
+    if (any_bad && blockIdx.x == 0) atomicOr(status, kStRange);
+    long long upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(kFull, upto, o);
+        if (lane >= o) upto += v;
+    }
+    if (lane == 31) sums[wid] = upto;
+    __syncthreads();
+    long long total = 0, ahead = upto - mine;
+    for (int v = 0; v < THREADS / 32; ++v) {
+        if (v < wid) ahead += sums[v];
+        total += sums[v];
+    }
+    const int workers = (int)min((long long)gridDim.x, total), me = blockIdx.x;
+    const long long t0 = me < workers ? total * me / workers : total, t1 = me < workers ? total * (me + 1) / workers : total;
+    if (t0 < t1 && t0 >= ahead && t0 < ahead + mine) {
+        long long at = ahead;
+        bool bad;
+        int s = s0;
+        for (; s < s1; ++s) {
+            const long long f = tiles_of(s, &bad);
+            if (t0 < at + f) break;
+            at += f;
+        }
+        range_at[0] = s;
+        range_at[1] = t0 - at;
+    }
+    __syncthreads();
+    if (t1 > t0) w.start(p, b, a, (int)range_at[0], range_at[1]);
+    if (tid == 0) a.first[me] = t1 > t0 ? make_int4(w.s, w.h, w.rt, w.tile) : make_int4(-1, 0, 0, 0);
+    return t1 - t0;
+}
+
+// The tiles of a range one after the other; a piece is what the range holds of one item.
+template <int TN, int ROWS> struct Tiles {
+    Walk<TN, ROWS> w;
+    long long left;                               // from this piece on
+    int j, m, piece;                              // tile of the piece, tiles in it, number of the piece
+    __device__ __forceinline__ void start(const Walk<TN, ROWS>& from, long long n) {
+        w = from;
+        left = n;
+        j = piece = 0;
+        m = n > 0 ? (int)min(n, (long long)(w.tiles - w.tile)) : 0;
+    }
+    __device__ __forceinline__ bool more() const { return left > 0; }
+    __device__ __forceinline__ bool last() const { return j == m - 1; }
+    __device__ __forceinline__ void next(const PoolDev& p, const BookDev& b, const AttendArgs& a) {
+        if (++j < m) return;
+        left -= m;
+        if (left <= 0) return;
+        w.next_item(p, b, a);
+        j = 0;
+        ++piece;
+        m = (int)min(left, (long long)(w.tiles - w.tile));
+    }
+};
+
+// Joins the pieces of items that more than one CTA had: block c looks at the boundary between CTAs c - 1 and c, and takes the item if that is the
+// first boundary inside it.  A warp a row at a time.
+constexpr int kJoinThreads = 128, kJoinRows = 16;
+template <class T, int D, int ROWS>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(PoolDev p, BookDev b, const __grid_constant__ AttendArgs a, int workers) {
+    chain_wait();
+    const int c = blockIdx.x + 1, lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const int4 f = a.first[c], prev = a.first[c - 1];
+    if (f.x < 0 || f.w == 0) return;
+    auto same = [&](const int4& o) { return o.x == f.x && o.y == f.y && o.z == f.z; };
+    if (same(prev) && prev.w > 0) return;
+    const int64_t lead = (int64_t)2 * (c - 1) + (same(prev) ? 0 : 1);      // the piece that the item begins with
+    int last = c;
+    while (last + 1 < workers) {
+        const int4 o = a.first[last + 1];
+        if (!same(o) || o.w == 0) break;
+        ++last;
+    }
+    bool bad;
+    const Session x = session_of(p, b, a, f.x, &bad);
+    const int rows = min(ROWS, x.n * a.group - f.z * ROWS);
+    const int end = min(rows, ((int)blockIdx.y + 1) * kJoinRows);
+    for (int r = blockIdx.y * kJoinRows + wid; r < end; r += kJoinThreads / 32) {
+        auto at = [&](int k) -> int64_t { return (k < c ? lead : (int64_t)2 * k) * a.part_rows + r; };
+        float top = -INFINITY;
+        for (int k = c - 1; k <= last; ++k) top = fmaxf(top, a.part_ml[at(k)].x);
+        float sum = 0.f, o[D / 32];
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
+        for (int k = c - 1; k <= last; ++k) {
+            const float2 ml = a.part_ml[at(k)];
+            if (ml.y == 0.f) continue;                                     // nothing was seen there
+            const float w = exp2f(ml.x - top);
+            sum = fmaf(ml.y, w, sum);
+            const float* from = a.part_o + at(k) * D + lane;
+#pragma unroll
+            for (int e = 0; e < D / 32; ++e) o[e] = fmaf(from[32 * e], w, o[e]);
+        }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const int rr = f.z * ROWS + r, i = rr / a.group;
+        const int64_t n_row = x.first + i, head = (int64_t)f.y * a.group + (rr - i * a.group);
+        uint16_t* out = static_cast<uint16_t*>(a.out) + n_row * a.os_row + head * a.os_head + lane;
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) out[32 * e] = (uint16_t)(Kind<T>::pack(o[e] * inv, 0.f) & 0xffffu);
+        if (a.lse && lane == 0) a.lse[n_row * a.heads + head] = sum == 0.f ? -INFINITY : (top - Kind<T>::shift + log2f(sum)) * 0.693147180559945f;
+    }
+}
+
+template <class T, int D, int ROWS>
+cudaError_t launch_join(const PoolDev& p, const BookDev& b, const AttendArgs& a, const AttendPlan& x, cudaStream_t st) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(x.grid - 1, (x.part_rows + kJoinRows - 1) / kJoinRows);
+    cfg.blockDim = dim3(kJoinThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, join_kernel<T, D, ROWS>, p, b, a, x.grid);
+}
+
+}  // namespace
+#endif
+
+}  // namespace plc
