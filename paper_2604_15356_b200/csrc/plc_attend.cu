@@ -438,9 +438,9 @@ AttendPlan plan(const PoolDev& p, int heads, int sessions, int n_rows) {
     const int few = p.d == 256 ? kFewRows / 2 : kFewRows;
     if (rows <= (long long)few * sessions) {
         AttendPlan x;
-        x.row_tile = few;
+        x.row_tile = rows <= 16LL * sessions ? 16 : rows <= 32LL * sessions ? 32 : few;
         x.grid = sm_count();
-        x.part_rows = (int)(rows < few ? rows : few);
+        x.part_rows = (int)(rows < x.row_tile ? rows : x.row_tile);
         x.bytes = (uint64_t)x.grid * 16 + 2ull * x.grid * x.part_rows * (8 + 4 * p.d);
         return x;
     }

@@ -53,8 +53,10 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     atomicOr(status, kStTimeout);
     return false;
 }
+// Not ordered with the compiler's own accesses: what is copied to is read behind a barrier only.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src)); }
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool take) {   // zeros where not `take`
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0));
 }
 // 128-byte swizzled rows.  K-major (Q, K): 1024 bytes from eight rows to the next eight.  MN-major (V): the same step along
 // the positions, `block` bytes from 64 components to the next 64.

@@ -15,28 +15,30 @@
 namespace plc {
 namespace {
 
-constexpr int kTN = 128, kSoft = 128, kCopy = 128, kFewThreads = kSoft + kCopy + 32;
+constexpr int kTN = 128, kCopy = 128;
 constexpr int kWords = 16;                        // tiles whose validity words are kept: more than the ring holds
 
-template <int D> struct Few {
-    static constexpr int N = D == 256 ? 32 : 64;                       // most rows
+// N: most rows of an item, and the columns of its products.
+template <int D, int N> struct Few {
     static constexpr int blocks = (D + 63) / 64;                       // 128-byte wide column blocks (32 components: half of one)
-    static constexpr int slot = blocks * kTN * 128, slots = D == 256 ? 3 : D == 128 ? 4 : 8;
+    static constexpr int slot = blocks * kTN * 128, slots = D == 256 ? 3 : (D == 128 ? 1 : 2) * (N == 16 ? 6 : N == 32 ? 5 : 4);
     static constexpr int q_bytes = blocks * N * 128, q_bufs = D == 256 ? 1 : 2;
     static constexpr int p_bytes = N * kTN * 2, p_bufs = D == 256 ? 1 : 2;
     static constexpr int o_blocks = D == 256 ? 2 : 1;
-    static constexpr int tmem = 256;                                   // S twice, O
-    static constexpr size_t smem = (size_t)q_bufs * q_bytes + p_bufs * p_bytes + slots * slot + 3 * kTN * 8 + 4096 + 1024;
+    // softmax: groups of four warps, which share the rows; N / groups of them a thread
+    static constexpr int groups = N == 16 ? 1 : 2, C = N / groups, soft = 128 * groups, threads = soft + kCopy + 64;
+    static constexpr int tmem = N == 64 || o_blocks * N == 64 ? 256 : 128;   // S twice, O twice
+    static constexpr size_t smem = (size_t)q_bufs * q_bytes + p_bufs * p_bytes + slots * slot + 3 * kTN * 8 + N * (8 + 4 * 13) + 768 + 1024;
 };
 
-__device__ __forceinline__ bool vote(uint32_t mine, bool all) {        // of the four softmax warps
+// Of N threads at a barrier of their own: whether any, or all, say so.
+template <int ID, int N> __device__ __forceinline__ bool vote_any(bool mine) {
     uint32_t r;
-    if (all)
-        asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(mine) : "memory");
-    else
-        asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(r) : "r"(mine) : "memory");
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)mine), "n"(ID), "n"(N) : "memory");
     return r != 0;
 }
+template <int ID, int N> __device__ __forceinline__ bool vote_all(bool mine) { return !vote_any<ID, N>(!mine); }
 __device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t* r) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
@@ -49,30 +51,101 @@ __device__ __forceinline__ float warp_max(float x) {
     asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
     return y;
 }
+// Sixteen values over the warp at once: lane l returns the sum of value l / 2 (lanes 2 r and 2 r + 1 the same).
+__device__ __forceinline__ float warp_sums(const float* x, int lane) {
+    float y[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[i] = x[i];
+#pragma unroll
+    for (int o = 16, n = 8; n > 0; o >>= 1, n >>= 1) {
+        const bool high = lane & o;                  // keeps the upper half of what is left
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float give = high ? y[i] : y[n + i], keep = high ? y[n + i] : y[i];
+            y[i] = keep + __shfl_xor_sync(kFull, give, o);
+        }
+    }
+    return y[0] + __shfl_xor_sync(kFull, y[0], 1);
+}
 // P: blocks of 8 rows, in each 16 bytes a position (MN-major without swizzle: 128 bytes from eight positions to the next eight,
 // 2048 from eight rows to the next eight).
 __device__ __forceinline__ uint64_t desc_p(uint32_t addr) { return (uint64_t)((addr & 0x3FFFFu) >> 4) | (8ull << 16) | (128ull << 32) | (1ull << 46); }
 
+// What rows row0 .. row0 + n - 1 (n <= 32) see of a warp's 32 positions t .. t+31, turned round: bit r says whether row row0 + r sees this lane's.
+__device__ __noinline__ uint32_t seen_rows(const AttendArgs& a, const Session x, int row0, int n, int t, uint32_t valid) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t see = lane < n ? valid & seen_bits(a, x, (row0 + lane) / a.group, t) : 0u;
+    uint32_t mine = 0;
+    for (int k = 0; k < 32; ++k) {
+        const uint32_t who = __ballot_sync(kFull, see >> k & 1u);
+        if (k == lane) mine = who;
+    }
+    return mine;
+}
+
+// Weights of 0 do not hide infinities and NaN from the product: at drafted positions they are taken out of V (this thread's vector of it), and put_back
+// adds them to the rows that see them.  Returns whether there were any.
 template <class T, int D>
-__global__ void __launch_bounds__(kFewThreads, 1) few_kernel(PoolDev p, BookDev b, const __grid_constant__ AttendArgs a, uint32_t* status) {
-    using F = Few<D>;
-    using Tl = Tiles<kTN, F::N>;
-    constexpr int N = F::N, chunks = N / 16, slots = F::slots;
+__device__ __noinline__ bool take_out(uint8_t* tile, int pos) {
+    bool any = false;
+    for (int e = 0; e < D / 8; ++e) {
+        uint4* at = reinterpret_cast<uint4*>(tile + (e >> 3) * (kTN * 128) + pos * 128 + (((e & 7) ^ (pos & 7)) << 4));
+        uint4 v = *at;
+        uint32_t* h = reinterpret_cast<uint32_t*>(&v);
+        bool hit = false;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if ((h[k] & Kind<T>::exponent) == Kind<T>::exponent) { h[k] &= 0xffff0000u; hit = true; }
+            if ((h[k] >> 16 & Kind<T>::exponent) == Kind<T>::exponent) { h[k] &= 0xffffu; hit = true; }
+        }
+        if (hit) *at = v;
+        any |= hit;
+    }
+    return any;
+}
+template <class T>
+__device__ __noinline__ void put_back(const PoolDev& p, const BookDev& b, const AttendArgs& a, const Session x, int s, int h, int t0, int t1, int row0, int rows, int d,
+                                      const int64_t* row_at, float* part) {
+    for (int t = max(t0, x.len); t < min(t1, x.kv); ++t) {
+        const int page = b.table[(int64_t)s * b.max_pages + t / p.page_pos];
+        if (page < 0 || page >= p.n_pages) continue;
+        const uint16_t v = reinterpret_cast<const uint16_t*>(p.base + (int64_t)a.layer * p.sl + (int64_t)h * p.sh + p.skv + (int64_t)page * p.spage +
+                                                             (int64_t)(t % p.page_pos) * p.sp)[d];
+        if ((v & Kind<T>::exponent) != Kind<T>::exponent) continue;
+        for (int r = 0; r < rows; ++r) {
+            if (!(seen_bits(a, x, (row0 + r) / a.group, t) & 1u)) continue;
+            if (part) { part[(int64_t)r * p.d] += Kind<T>::widen(v); continue; }
+            uint16_t* o = static_cast<uint16_t*>(a.out) + row_at[r] + d;
+            *o = (uint16_t)(Kind<T>::pack(Kind<T>::widen(*o) + Kind<T>::widen(v), 0.f) & 0xffffu);
+        }
+    }
+}
+
+template <class T, int D, int N>
+__global__ void __launch_bounds__(Few<D, N>::threads, 1) few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b, const __grid_constant__ AttendArgs a,
+                                                             uint32_t* status) {
+    using F = Few<D, N>;
+    using Tl = Tiles<kTN, N>;
+    constexpr int slots = F::slots, C = F::C, soft_warps = F::soft / 32, qk_warp = F::threads / 32 - 2, pv_warp = qk_warp + 1;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* qs = ring + slots * F::slot;
     uint8_t* ps = qs + F::q_bufs * F::q_bytes;
-    int64_t* offs = reinterpret_cast<int64_t*>(ps + F::p_bufs * F::p_bytes);            // [3][kTN]
-    int64_t* row_at = offs + 3 * kTN;                                                   // [N] where a row of the result goes
-    uint64_t* bars = reinterpret_cast<uint64_t*>(row_at + N);
-    float* base_s = reinterpret_cast<float*>(bars + 2 * slots + 12);                    // [N] what the weights' exponents are relative to
+    uint64_t* from = reinterpret_cast<uint64_t*>(ps + F::p_bufs * F::p_bytes);          // [3][kTN] where a position's key stands
+    int64_t* row_at = reinterpret_cast<int64_t*>(from + 3 * kTN);                       // [N] where a row of the result goes
+    float* base_s = reinterpret_cast<float*>(row_at + N);                               // [N] what the weights' exponents are relative to
     float* top_s = base_s + N;                                                          // [N] maximum (scaled, base 2)
     float* factor_s = top_s + N;                                                        // [N]
     float* warp_s = factor_s + N;                                                       // [4][N]
-    uint32_t* words = reinterpret_cast<uint32_t*>(warp_s + 4 * N);                      // [kWords][4] positions that exist
-    uint32_t* tmem_slot = words + kWords * 4;
+    float* sum_s = warp_s + 4 * N;                                                      // [4][N] the last finished piece's: sums, maxima, 1 / sum
+    float* last_top_s = sum_s + 4 * N;                                                  // [N]
+    float* inv_s = last_top_s + N;                                                      // [N]
+    uint32_t* words = reinterpret_cast<uint32_t*>(inv_s + N);                           // [kWords][4] positions that exist
+    Tl* done = reinterpret_cast<Tl*>(words + kWords * 4);                               // the softmax's last finished piece
+    uint64_t* bars = reinterpret_cast<uint64_t*>(done + 1);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * slots + 12);
     volatile uint32_t* failed = tmem_slot + 1;
-    volatile uint32_t* dirty = tmem_slot + 2;     // number + 1 of the last piece whose V holds infinities or NaN at drafted positions
+    volatile uint32_t* dirty = tmem_slot + 2;     // [2] by a piece's parity: number + 1 of the last one whose V holds infinities or NaN at drafted positions
     const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
     const uint32_t full = smem_u32(bars), empty = full + 8 * slots, qfull = empty + 8 * slots, qempty = qfull + 16, sfull = qempty + 16, pfull = sfull + 16,
                    ofull = pfull + 16, drain = ofull + 16;
@@ -83,60 +156,82 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(PoolDev p, BookDev 
             mbar_init(qfull + 8 * i, kCopy);
             mbar_init(qempty + 8 * i, 1);
             mbar_init(sfull + 8 * i, 1);
-            mbar_init(pfull + 8 * i, kSoft / 32);
+            mbar_init(pfull + 8 * i, soft_warps);
             mbar_init(ofull + 8 * i, 1);
+            mbar_init(drain + 8 * i, 1);
         }
-        mbar_init(drain, 1);
-        *failed = *dirty = 0u;
+        *failed = dirty[0] = dirty[1] = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    constexpr int mma_warp = kFewThreads / 32 - 1;
-    if (wid == mma_warp) {
+    if (wid == qk_warp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"((uint32_t)F::tmem) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     fence_before();
     Walk<kTN, N> w0{};
-    const long long total = find_range<kTN, N, kFewThreads>(p, b, a, status, w0);
+    const long long total = find_range<kTN, N, F::threads>(p, b, a, status, w0);
     fence_after();
     const uint32_t tmem = *tmem_slot, ring_s = smem_u32(ring), q_s = smem_u32(qs), p_s = smem_u32(ps);
 
-    if (wid >= 4 && wid < mma_warp) {
+    if (wid >= soft_warps && wid < qk_warp) {
         // ---- copies
-        const int lt = tid - kSoft;
-        constexpr int pieces = D / 8, step = kCopy / pieces;                // 16-byte pieces of a vector; vectors a round
+        const int lt = tid - F::soft;
+        constexpr int pieces = D / 8, step = kCopy / pieces, rounds = kTN / step;   // 16-byte pieces of a vector; vectors a round
         const int c = lt % pieces, r0 = lt / pieces;
+        const uint32_t to = (c >> 3) * (kTN * 128) + r0 * 128;
         Tl kx, vx;
         kx.start(w0, total);
         vx.start(w0, total);
         int kt = 0, vt = 0, sl = 0;
         bool ok = true;
-        auto fill = [&](const uint8_t* src, const int64_t* off) {            // a tile into the next slot of the ring
+        auto fill = [&](int tile, int64_t delta) {           // a tile's keys, or values (delta further on), into the next slot of the ring
             const int s = sl % slots;
             ok = __all_sync(kFull, ok && mbar_wait(empty + 8 * s, ((uint32_t)(sl / slots) & 1u) ^ 1u, failed, status));
             ++sl;
             if (!ok) return;
-            const uint32_t dst = ring_s + s * F::slot + (c >> 3) * (kTN * 128);
-            const uint8_t* mine = src + c * 16;
+            const uint32_t dst = ring_s + s * F::slot + to;
+            const uint64_t* src = from + tile % 3 * kTN + r0;
+            const uint32_t* valid = words + tile % kWords * 4;
+            delta += c * 16;
+            const bool all = (valid[0] & valid[1] & valid[2] & valid[3]) == ~0u;
 #pragma unroll
-            for (int k = 0; k < kTN / step; ++k) {
-                const int r = r0 + k * step;
-                const int64_t o = off[r];
-                copy16(dst + r * 128 + (((c & 7) ^ (r & 7)) << 4), o == INT64_MIN ? src : mine + o, o != INT64_MIN);
+            for (int k0 = 0; k0 < rounds; k0 += 8) {
+                uint64_t at[8];
+#pragma unroll
+                for (int k = 0; k < 8 && k0 + k < rounds; ++k) at[k] = src[(k0 + k) * step];
+                if (all) {
+#pragma unroll
+                    for (int k = 0; k < 8 && k0 + k < rounds; ++k)
+                        copy16(dst + (k0 + k) * step * 128 + (((c & 7) ^ ((r0 + (k0 + k) * step) & 7)) << 4), reinterpret_cast<const uint8_t*>(at[k] + delta));
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8 && k0 + k < rounds; ++k) {
+                        const int r = r0 + (k0 + k) * step;
+                        copy16(dst + (k0 + k) * step * 128 + (((c & 7) ^ (r & 7)) << 4), reinterpret_cast<const uint8_t*>(at[k] + delta), valid[r >> 5] >> (r & 31) & 1u);
+                    }
+                }
             }
             mbar_arrive_copies(full + 8 * s);
             __syncwarp();
             if (lane == 0) mbar_arrive(full + 8 * s);                        // the validity words, too, are there
         };
+        int slot_in = 0, page = -1;                  // this thread's position of K's next tile: slot in its page, the page
+        auto look_up = [&]() {                       // issued a tile ahead of its use
+            const int t = (kx.w.tile + kx.j) * kTN + lt, pg = t / p.page_pos;
+            const bool have = t < kx.w.x.kv;
+            slot_in = have ? t - pg * p.page_pos : -1;
+            page = have ? b.table[(int64_t)kx.w.s * b.max_pages + pg] : 0;
+        };
+        if (kx.more()) look_up();
         for (;;) {
             const bool more = kx.more();
             if (!more && !vx.more()) break;
             if (more) {
                 if (kx.j == 0) {
-                    const int q = kx.piece % F::q_bufs, rows = kx.w.rows(a), up = (rows + 15) & ~15;
+                    const int q = kx.piece % F::q_bufs, rows = kx.w.rows(a);
                     ok = ok && mbar_wait(qempty + 8 * q, ((uint32_t)(kx.piece / F::q_bufs) & 1u) ^ 1u, failed, status);
                     if (ok) {
-                        for (int r = r0; r < up; r += step) {
+                        for (int r = r0; r < N; r += step) {
                             const int rr = kx.w.rt * N + r, i = rr / a.group, g = rr - i * a.group;
                             const uint8_t* src = static_cast<const uint8_t*>(a.q);
                             if (r < rows) src += 2 * ((int64_t)(kx.w.x.first + i) * a.qs_row + (int64_t)(kx.w.h * a.group + g) * a.qs_head) + c * 16;
@@ -145,309 +240,288 @@ __global__ void __launch_bounds__(kFewThreads, 1) few_kernel(PoolDev p, BookDev 
                         mbar_arrive_copies(qfull + 8 * q);
                     }
                 }
-                const int t = (kx.w.tile + kx.j) * kTN + lt;
-                bool have = t < kx.w.x.kv;
-                int64_t at = 0;
-                if (have) {
-                    const int pg = t / p.page_pos, page = b.table[(int64_t)kx.w.s * b.max_pages + pg];
-                    if (page >= 0 && page < p.n_pages) at = (int64_t)page * p.spage + (int64_t)(t - pg * p.page_pos) * p.sp;
-                    else { have = false; atomicOr(status, kStRange); }
-                }
-                offs[kt % 3 * kTN + lt] = have ? at : INT64_MIN;
+                const bool there = page >= 0 && page < p.n_pages, have = slot_in >= 0 && there;
+                if (!there) atomicOr(status, kStRange);
+                // (a position that does not exist: anywhere in the pool, nothing is read)
+                from[kt % 3 * kTN + lt] = reinterpret_cast<uint64_t>(p.base) +
+                                          (have ? (int64_t)a.layer * p.sl + (int64_t)kx.w.h * p.sh + (int64_t)page * p.spage + (int64_t)slot_in * p.sp : 0);
                 const uint32_t valid = __ballot_sync(kFull, have);
                 if (lane == 0) words[kt % kWords * 4 + (lt >> 5)] = valid;
             }
-            uint32_t all;
-            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                         : "=r"(all) : "r"((uint32_t)ok) : "memory");
-            if (!all) break;
+            if (!vote_all<1, kCopy>(ok)) break;
             if (more) {
-                fill(p.base + (int64_t)a.layer * p.sl + (int64_t)kx.w.h * p.sh, offs + kt % 3 * kTN);
+                fill(kt, 0);
                 ++kt;
                 kx.next(p, b, a);
+                if (kx.more()) look_up();
             }
             if (kt > 1 || !more) {                                           // V of a tile after K of the next
-                fill(p.base + (int64_t)a.layer * p.sl + (int64_t)vx.w.h * p.sh + p.skv, offs + vt % 3 * kTN);
+                fill(vt, p.skv);
                 ++vt;
                 vx.next(p, b, a);
             }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
-    } else if (wid == mma_warp) {
-        if (lane == 0 && total > 0) {
-            // ---- products
-            constexpr uint32_t common = (1u << 4) | (Kind<T>::format << 7) | (Kind<T>::format << 10) | (8u << 24);
-            Tl qx, vx;
-            qx.start(w0, total);
-            vx.start(w0, total);
-            int sl = 0;
+    } else if (wid >= qk_warp) {
+        if (lane == 0) {
+            // ---- products, a thread for each of the two.  The ring holds K(0), then K(x + 1), V(x) for every tile x.
+            constexpr uint32_t id_qk = (1u << 4) | (Kind<T>::format << 7) | (Kind<T>::format << 10) | (8u << 24) | ((uint32_t)(N >> 3) << 17), id_pv = id_qk | (3u << 15);
+            Tl tl;
+            tl.start(w0, total);
             bool ok = true;
-            auto ready = [&]() {                      // the next slot of the ring
-                ok = ok && mbar_wait(full + 8 * (sl % slots), (uint32_t)(sl / slots) & 1u, failed, status);
+            auto ready = [&](int i) {
+                ok = ok && mbar_wait(full + 8 * (i % slots), (uint32_t)(i / slots) & 1u, failed, status);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 fence_after();
             };
-            auto columns = [&](const Tl& x) { return (uint32_t)((x.w.rows(a) + 15) & ~15); };
-            auto qk = [&](int x) {
-                const int q = qx.piece % F::q_bufs;
-                if (qx.j == 0) ok = ok && mbar_wait(qfull + 8 * q, (uint32_t)(qx.piece / F::q_bufs) & 1u, failed, status);
-                ready();
-                if (!ok) return;
-                const uint32_t k_at = ring_s + sl % slots * F::slot, q_at = q_s + q * F::q_bytes, id = common | (columns(qx) >> 3 << 17);
+            if (wid == qk_warp) {
+                for (int x = 0; tl.more(); ++x, tl.next(p, b, a)) {
+                    const int q = tl.piece % F::q_bufs, i = x ? 2 * x - 1 : 0;
+                    if (tl.j == 0) ok = ok && mbar_wait(qfull + 8 * q, (uint32_t)(tl.piece / F::q_bufs) & 1u, failed, status);
+                    if (x >= 2) ok = ok && mbar_wait(pfull + 8 * (x & 1), (uint32_t)((x - 2) >> 1) & 1u, failed, status);   // S has been read
+                    ready(i);
+                    if (!ok) break;
+                    const uint64_t k_at = desc_k(ring_s + i % slots * F::slot), q_at = desc_k(q_s + q * F::q_bytes);
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k)
-                    mma_ss(tmem + (x & 1) * N, desc_k(k_at + (k >> 2) * (kTN * 128)) + 2 * (k & 3), desc_k(q_at + (k >> 2) * (N * 128)) + 2 * (k & 3), id, k ? 1u : 0u);
-                mma_commit(sfull + 8 * (x & 1));
-                mma_commit(empty + 8 * (sl % slots));
-                if (qx.last()) mma_commit(qempty + 8 * q);
-                ++sl;
-                qx.next(p, b, a);
-            };
-            qk(0);
-            for (int x = 0; vx.more() && ok; ++x) {
-                if (qx.more()) qk(x + 1);
-                ok = ok && mbar_wait(pfull + 8 * (x & 1), (uint32_t)(x >> 1) & 1u, failed, status);
-                ready();
-                if (!ok) break;
-                const uint32_t v_at = ring_s + sl % slots * F::slot, p_at = p_s + x % F::p_bufs * F::p_bytes, id = common | (3u << 15) | (columns(vx) >> 3 << 17);
+                    for (int k = 0; k < D / 16; ++k)
+                        mma_ss(tmem + (x & 1) * N, k_at + (k >> 2) * (kTN * 128 / 16) + 2 * (k & 3), q_at + (k >> 2) * (N * 128 / 16) + 2 * (k & 3), id_qk, k ? 1u : 0u);
+                    mma_commit(sfull + 8 * (x & 1));
+                    mma_commit(empty + 8 * (i % slots));
+                    if (tl.last()) mma_commit(qempty + 8 * q);
+                }
+            } else {
+                for (int x = 0; tl.more(); ++x, tl.next(p, b, a)) {
+                    const int i = x + 1 < total ? 2 * x + 2 : 2 * x + 1;
+                    ok = ok && mbar_wait(pfull + 8 * (x & 1), (uint32_t)(x >> 1) & 1u, failed, status);
+                    ready(i);
+                    if (!ok) break;
+                    // lanes past the components of a vector take the first block again
+                    const uint64_t v_at = desc_mn(ring_s + i % slots * F::slot, D >= 128 ? kTN * 128 : 0), p_at = desc_p(p_s + x % F::p_bufs * F::p_bytes);
+                    const uint32_t o_to = tmem + 2 * N + (tl.piece & 1) * F::o_blocks * N;
 #pragma unroll
-                for (int o = 0; o < F::o_blocks; ++o)
+                    for (int o = 0; o < F::o_blocks; ++o)
 #pragma unroll
-                    for (int k = 0; k < kTN / 16; ++k)               // lanes past the components of a vector take the first block again
-                        mma_ss(tmem + 2 * N + o * N, desc_mn(v_at + o * 2 * kTN * 128 + k * 2048, D >= 128 ? kTN * 128 : 0), desc_p(p_at + k * 256), id, vx.j | k ? 1u : 0u);
-                mma_commit(ofull + 8 * (x & 1));
-                mma_commit(empty + 8 * (sl % slots));
-                ++sl;
-                vx.next(p, b, a);
+                        for (int k = 0; k < kTN / 16; ++k)
+                            mma_ss(o_to + o * N, v_at + (o * 2 * kTN * 128 + k * 2048) / 16, p_at + k * 16, id_pv, tl.j | k ? 1u : 0u);
+                    mma_commit(ofull + 8 * (x & 1));
+                    mma_commit(empty + 8 * (i % slots));
+                }
             }
-            mma_commit(drain);                        // nothing issued runs when the CTA frees its tensor memory
+            const uint32_t mine = drain + 8 * (wid - qk_warp);
+            mma_commit(mine);                         // nothing issued runs when the CTA frees its tensor memory
             for (uint32_t i = 0; i < kSpin; ++i) {
                 uint32_t done;
-                asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], 0;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(drain) : "memory");
+                asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], 0;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(done) : "r"(mine) : "memory");
                 if (done) break;
             }
         }
     } else {
         // ---- softmax and results: a thread a position, then a component
-        const uint32_t lanes = (uint32_t)(wid * 32) << 16;
-        const float c = a.scale * 1.44269504088896f;
+        const int quarter = wid & 3, col0 = (wid >> 2) * C, pos = tid & 127;                 // the warp's positions (components), its group's rows
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16, o_at = tmem + 2 * N + col0 + lanes;
+        const unsigned long long c2 = pack2(a.scale * 1.44269504088896f, a.scale * 1.44269504088896f);
         Tl sx;
         sx.start(w0, total);
-        float sum[N];
+        unsigned long long sum[C / 2];                // of this thread's weights, pairs of rows
         bool ok = true;
+        auto results = [&](int last) -> bool {        // of the piece that *done tells of; a thread a component
+            ok = ok && mbar_wait(ofull + 8 * (last & 1), (uint32_t)(last >> 1) & 1u, failed, status);
+            if (!vote_all<2, F::soft>(ok)) return false;
+            const Tl f = *done;
+            const int rows = f.w.rows(a), row0 = f.w.rt * N;
+            const bool whole = f.w.tile == 0 && f.m == f.w.tiles;
+            const int64_t slot = ((int64_t)2 * blockIdx.x + (f.piece > 0)) * a.part_rows;
+            if (tid < rows) {
+                const float l = (sum_s[tid] + sum_s[N + tid]) + (sum_s[2 * N + tid] + sum_s[3 * N + tid]), top = last_top_s[tid];
+                const int rr = row0 + tid, i = rr / a.group;
+                const int64_t n_row = f.w.x.first + i, head = (int64_t)f.w.h * a.group + (rr - i * a.group);
+                row_at[tid] = n_row * a.os_row + head * a.os_head;
+                inv_s[tid] = l == 0.f ? 0.f : whole ? 1.f / l : 1.f;             // 0: nothing was seen
+                if (!whole) a.part_ml[slot + tid] = make_float2(top, l);
+                else if (a.lse) a.lse[n_row * a.heads + head] = l == 0.f ? -INFINITY : (top - Kind<T>::shift + log2f(l)) * 0.693147180559945f;
+            }
+            vote_all<2, F::soft>(true);
+            fence_after();
+#pragma unroll 1
+            for (int ch = 0; ch < F::o_blocks * C / 16; ++ch) {
+                const int r0 = 16 * ch % C + col0, d = 16 * ch / C * 128 + pos;
+                if (r0 >= rows) continue;
+                uint32_t y[16];
+                tmem_ld16(o_at + ((f.piece & 1) * F::o_blocks + 16 * ch / C) * N + 16 * ch % C, y);
+                wait_ld(y);
+                if (d >= D) continue;
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (r0 + r < rows) {
+                        const float g = inv_s[r0 + r], v = g == 0.f ? 0.f : __uint_as_float(y[r]) * g;
+                        if (whole) static_cast<uint16_t*>(a.out)[row_at[r0 + r] + d] = (uint16_t)(Kind<T>::pack(v, 0.f) & 0xffffu);
+                        else a.part_o[(slot + r0 + r) * D + d] = v;
+                    }
+            }
+            if (dirty[f.piece & 1] == (uint32_t)f.piece + 1u && vote_all<2, F::soft>(true))       // every group's rows are written
+                for (int d = tid; d < D; d += F::soft)
+                    put_back<T>(p, b, a, f.w.x, f.w.s, f.w.h, f.w.tile * kTN, (f.w.tile + f.m) * kTN, row0, rows, d, row_at, whole ? nullptr : a.part_o + slot * D + d);
+            fence_before();
+            return true;
+        };
         for (int x = 0; sx.more(); ++x, sx.next(p, b, a)) {
-            const Session& ses = sx.w.x;
-            const int rows = sx.w.rows(a), n_ch = (rows + 15) >> 4, t0 = (sx.w.tile + sx.j) * kTN, t = t0 + tid, row0 = sx.w.rt * N;
-            const bool first = sx.j == 0, may_hide = a.mask != nullptr || ses.n > 1;
+            const int t0 = (sx.w.tile + sx.j) * kTN;
+            const bool first = sx.j == 0, drafted = t0 + kTN > sx.w.x.len;
             ok = ok && mbar_wait(sfull + 8 * (x & 1), (uint32_t)(x >> 1) & 1u, failed, status);
             if (x >= F::p_bufs) ok = ok && mbar_wait(ofull + 8 * ((x - F::p_bufs) & 1), (uint32_t)((x - F::p_bufs) >> 1) & 1u, failed, status);
             ok = __all_sync(kFull, ok);
             fence_after();
-            uint32_t s[N];
-#pragma unroll
-            for (int ch = 0; ch < chunks; ++ch)
-                if (ch < n_ch) tmem_ld16(tmem + (x & 1) * N + lanes + 16 * ch, s + 16 * ch);
-            wait_ld(s);
-            const uint32_t* valid = words + x % kWords * 4;
-            const bool masked = t0 + kTN > ses.len || (valid[0] & valid[1] & valid[2] & valid[3]) != ~0u;
-            uint32_t vis[(N + 31) / 32];
-            if (masked) {                             // a lane finds what a row sees of the warp's 32 positions; a ballot a position turns that round
-#pragma unroll
-                for (int e = 0; e < (N + 31) / 32; ++e) {
-                    const int r = 32 * e + lane;
-                    uint32_t see = 0;
-                    if (r < rows) see = valid[wid] & seen_bits(a, ses, (row0 + r) / a.group, t0 + 32 * wid);
-                    vis[e] = 0;
-                    for (int k = 0; k < 32; ++k) {
-                        const uint32_t who = __ballot_sync(kFull, see >> k & 1u);
-                        if (k == lane) vis[e] = who;
-                    }
-                }
-#pragma unroll
-                for (int r = 0; r < N; ++r) s[r] = vis[r >> 5] >> (r & 31) & 1u ? s[r] : 0xff800000u;
+            const uint32_t s_at = tmem + (x & 1) * N + col0 + lanes;
+            const uint4 valid = *reinterpret_cast<const uint4*>(words + x % kWords * 4);
+            const bool may_hide = a.mask != nullptr || sx.w.x.n > 1, hide = may_hide && drafted;
+            const bool masked = hide || (valid.x & valid.y & valid.z & valid.w) != ~0u;
+            uint32_t vis = 0;                         // the group's rows that see this thread's position
+            if (masked) {
+                const uint32_t mine = words[x % kWords * 4 + quarter];
+                vis = hide ? seen_rows(a, sx.w.x, sx.w.rt * N + col0, sx.w.rows(a) - col0, t0 + 32 * quarter, mine) : mine >> lane & 1u ? ~0u : 0u;
             }
-            bool need = first || !ok;
+            uint32_t s[16];                           // 16 rows' scores at a time; more of them stay in tensor memory meanwhile
+            auto scores = [&](int ch) {
+                tmem_ld16(s_at + 16 * ch, s);
+                wait_ld(s);
+                if (masked) {
+                    const uint32_t mine = vis >> (16 * ch);
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] = mine >> r & 1u ? s[r] : 0xff800000u;
+                }
+            };
+            // exponents relative to base, four rows from r on
+            auto exponents = [&](int r, float* e) {
+                const ulonglong2 base = *reinterpret_cast<const ulonglong2*>(base_s + col0 + r);
+                const int k = r & 15;
+                unpack2(fma2(pack2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, base.x), e[0], e[1]);
+                unpack2(fma2(pack2(__uint_as_float(s[k + 2]), __uint_as_float(s[k + 3])), c2, base.y), e[2], e[3]);
+            };
+            if (C == 16) scores(0);
+            float high = -INFINITY;                   // one above the border asks for a new maximum (rows without one have a base far below)
             if (!first) {
 #pragma unroll
-                for (int ch = 0; ch < chunks; ++ch)
-                    if (ch < n_ch) {
-#pragma unroll
-                        for (int r = 16 * ch; r < 16 * ch + 16; ++r) need |= __uint_as_float(s[r]) * c > top_s[r] + kRaise;
-                    }
+                for (int r = 0; r < C; r += 4) {
+                    if (C > 16 && (r & 15) == 0) scores(r >> 4);
+                    float e[4];
+                    exponents(r, e);
+                    high = fmaxf(high, fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3])));
+                }
             }
-            if (vote(need, false)) {
+            if (vote_any<2, F::soft>(first || !ok || high > kRaise + Kind<T>::shift)) {
                 // some row's maximum rises: all warps' maxima, the factors, and what has been summed so far
 #pragma unroll
-                for (int ch = 0; ch < chunks; ++ch)
-                    if (ch < n_ch) {
-#pragma unroll
-                        for (int r = 16 * ch; r < 16 * ch + 16; ++r) {
-                            const float m = warp_max(__uint_as_float(s[r]));
-                            if (lane == (r & 31)) warp_s[wid * N + r] = m;
-                        }
-                    }
+                for (int r = 0; r < C; ++r) {
+                    if (C > 16 && (r & 15) == 0) scores(r >> 4);
+                    const float m = warp_max(__uint_as_float(s[r & 15]));
+                    if (lane == r) warp_s[quarter * N + col0 + r] = m;
+                }
                 if (!first) ok = ok && mbar_wait(ofull + 8 * ((x - 1) & 1), (uint32_t)((x - 1) >> 1) & 1u, failed, status);
-                if (!vote(ok, true)) { ok = false; break; }
+                if (!vote_all<2, F::soft>(ok)) { ok = false; break; }
                 if (tid < N) {
-                    const float now = fmaxf(fmaxf(warp_s[tid], warp_s[N + tid]), fmaxf(warp_s[2 * N + tid], warp_s[3 * N + tid])) * c;
+                    const float now = fmaxf(fmaxf(warp_s[tid], warp_s[N + tid]), fmaxf(warp_s[2 * N + tid], warp_s[3 * N + tid])) * (a.scale * 1.44269504088896f);
                     const float old = first ? -INFINITY : top_s[tid];
                     const float top = now > old + kRaise ? now : old;
                     top_s[tid] = top;
-                    base_s[tid] = top == -INFINITY ? 0.f : top - Kind<T>::shift;
+                    base_s[tid] = top == -INFINITY ? 1e30f : Kind<T>::shift - top;
                     factor_s[tid] = top == old ? 1.f : old == -INFINITY ? 0.f : exp2_approx(old - top);
                 }
-                vote(1u, true);
+                vote_all<2, F::soft>(true);
                 if (first) {
 #pragma unroll
-                    for (int r = 0; r < N; ++r) sum[r] = 0.f;
+                    for (int r = 0; r < C / 2; ++r) sum[r] = 0ull;
                 } else {
                     fence_after();
 #pragma unroll
-                    for (int ch = 0; ch < chunks; ++ch)
-                        if (ch < n_ch) {
+                    for (int r = 0; r < C; r += 2) {
+                        float lo, hi;
+                        unpack2(sum[r / 2], lo, hi);
+                        sum[r / 2] = pack2(lo * factor_s[col0 + r], hi * factor_s[col0 + r + 1]);
+                    }
+#pragma unroll 1
+                    for (int ch = 0; ch < F::o_blocks * C / 16; ++ch) {
+                        uint32_t y[16];
+                        const uint32_t at = o_at + ((sx.piece & 1) * F::o_blocks + 16 * ch / C) * N + 16 * ch % C;
+                        tmem_ld16(at, y);
+                        wait_ld(y);
 #pragma unroll
-                            for (int r = 16 * ch; r < 16 * ch + 16; ++r) sum[r] *= factor_s[r];
-                            for (int o = 0; o < F::o_blocks; ++o) {
-                                uint32_t y[16];
-                                const uint32_t at = tmem + 2 * N + o * N + lanes + 16 * ch;
-                                tmem_ld16(at, y);
-                                wait_ld(y);
-#pragma unroll
-                                for (int r = 0; r < 16; ++r) {
-                                    const float f = factor_s[16 * ch + r];
-                                    y[r] = __float_as_uint(f == 0.f ? 0.f : __uint_as_float(y[r]) * f);
-                                }
-                                tmem_st16(at, y);
-                            }
+                        for (int r = 0; r < 16; ++r) {
+                            const float f = factor_s[col0 + (16 * ch + r) % C];
+                            y[r] = __float_as_uint(f == 0.f ? 0.f : __uint_as_float(y[r]) * f);
                         }
+                        tmem_st16(at, y);
+                    }
                     wait_st();
                 }
             }
-            uint8_t* pp = ps + x % F::p_bufs * F::p_bytes + tid * 16;
+            uint8_t* pp = ps + x % F::p_bufs * F::p_bytes + col0 / 8 * 2048 + pos * 16;
 #pragma unroll
-            for (int ch = 0; ch < chunks; ++ch)
-                if (ch < n_ch) {
-                    uint32_t y[8];
+            for (int r = 0; r < C; r += 8) {
+                if (C > 16 && (r & 15) == 0) scores(r >> 4);
+                uint32_t y[4];
 #pragma unroll
-                    for (int r = 16 * ch; r < 16 * ch + 16; ++r) {
-                        float v = exp2_approx(fmaf(__uint_as_float(s[r]), c, -base_s[r]));
-                        if (masked) v = vis[r >> 5] >> (r & 31) & 1u ? v : 0.f;
-                        sum[r] += v;
-                        s[r] = __float_as_uint(v);
-                    }
+                for (int k = 0; k < 8; k += 4) {
+                    float e[4];
+                    exponents(r + k, e);
 #pragma unroll
-                    for (int r = 0; r < 8; ++r) y[r] = Kind<T>::pack(__uint_as_float(s[16 * ch + 2 * r]), __uint_as_float(s[16 * ch + 2 * r + 1]));
-                    *reinterpret_cast<uint4*>(pp + (2 * ch) * 2048) = make_uint4(y[0], y[1], y[2], y[3]);
-                    *reinterpret_cast<uint4*>(pp + (2 * ch + 1) * 2048) = make_uint4(y[4], y[5], y[6], y[7]);
+                    for (int i = 0; i < 4; ++i) e[i] = exp2_approx(e[i]);                 // a score of -inf has the weight 0
+                    sum[(r + k) / 2] = add2(sum[(r + k) / 2], pack2(e[0], e[1]));
+                    sum[(r + k) / 2 + 1] = add2(sum[(r + k) / 2 + 1], pack2(e[2], e[3]));
+                    y[k / 2] = Kind<T>::pack(e[0], e[1]);
+                    y[k / 2 + 1] = Kind<T>::pack(e[2], e[3]);
                 }
-            if (may_hide && t0 + kTN > ses.len) {
-                // Weights of 0 do not hide infinities and NaN from the product: at drafted positions they are taken out of V, and added to the rows
-                // that see them at the end.
+                *reinterpret_cast<uint4*>(pp + (r / 8) * 2048) = make_uint4(y[0], y[1], y[2], y[3]);
+            }
+            if (hide && wid < 4) {
                 const int sl = x + 1 < total ? 2 * x + 2 : 2 * x + 1;       // V's place in the order of the ring
                 ok = ok && mbar_wait(full + 8 * (sl % slots), (uint32_t)(sl / slots) & 1u, failed, status);
-                if (ok && t >= ses.len && t < ses.kv)
-#pragma unroll 4
-                    for (int e = 0; e < D / 8; ++e) {
-                        uint4* at = reinterpret_cast<uint4*>(ring + sl % slots * F::slot + (e >> 3) * (kTN * 128) + tid * 128 + (((e & 7) ^ (tid & 7)) << 4));
-                        uint4 v = *at;
-                        uint32_t* h = reinterpret_cast<uint32_t*>(&v);
-                        bool hit = false;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            if ((h[k] & Kind<T>::exponent) == Kind<T>::exponent) { h[k] &= 0xffff0000u; hit = true; }
-                            if ((h[k] >> 16 & Kind<T>::exponent) == Kind<T>::exponent) { h[k] &= 0xffffu; hit = true; }
-                        }
-                        if (hit) { *dirty = (uint32_t)sx.piece + 1u; *at = v; }
-                    }
+                if (ok && t0 + tid >= sx.w.x.len && t0 + tid < sx.w.x.kv && take_out<T, D>(ring + sl % slots * F::slot, tid)) dirty[sx.piece & 1] = (uint32_t)sx.piece + 1u;
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // P (and V) as the product reads them
             fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(pfull + 8 * (x & 1));
+            // the results of the piece before, whose last product has had this tile's time to finish
+            if (first && x > 0 && !(ok = results(x - 1))) break;
             if (!sx.last()) continue;
-
-            // ---- the piece is done: sums over the positions, then a thread a component
+            // the piece is done: its sums over the positions
+            if (tid == 0) *done = sx;
 #pragma unroll
-            for (int ch = 0; ch < chunks; ++ch)
-                if (ch < n_ch) {
+            for (int ch = 0; ch < C / 16; ++ch) {
+                float l[16];
 #pragma unroll
-                    for (int r = 16 * ch; r < 16 * ch + 16; ++r) {
-                        const float v = warp_sum(sum[r]);
-                        if (lane == (r & 31)) warp_s[wid * N + r] = v;
-                    }
-                }
-            ok = ok && mbar_wait(ofull + 8 * (x & 1), (uint32_t)(x >> 1) & 1u, failed, status);
-            if (!vote(ok, true)) { ok = false; break; }
-            const bool whole = sx.w.tile == 0 && sx.m == sx.w.tiles;
-            const int64_t slot = ((int64_t)2 * blockIdx.x + (sx.piece > 0)) * a.part_rows;
-            if (tid < rows) {
-                const float l = (warp_s[tid] + warp_s[N + tid]) + (warp_s[2 * N + tid] + warp_s[3 * N + tid]), top = top_s[tid];
-                const int rr = row0 + tid, i = rr / a.group;
-                const int64_t n_row = ses.first + i, head = (int64_t)sx.w.h * a.group + (rr - i * a.group);
-                row_at[tid] = n_row * a.os_row + head * a.os_head;
-                factor_s[tid] = l == 0.f ? 0.f : whole ? 1.f / l : 1.f;          // 0: nothing was seen
-                if (!whole) a.part_ml[slot + tid] = make_float2(top, l);
-                else if (a.lse) a.lse[n_row * a.heads + head] = l == 0.f ? -INFINITY : (top - Kind<T>::shift + log2f(l)) * 0.693147180559945f;
+                for (int r = 0; r < 16; r += 2) unpack2(sum[8 * ch + r / 2], l[r], l[r + 1]);
+                const float v = warp_sums(l, lane);
+                if (!(lane & 1)) sum_s[quarter * N + col0 + 16 * ch + lane / 2] = v;
             }
-            vote(1u, true);
-            fence_after();
-            const bool special = may_hide && *dirty == (uint32_t)sx.piece + 1u;
-            for (int o = 0; o < F::o_blocks; ++o) {
-                const int d = o * 128 + tid;
-                for (int ch = 0; ch < n_ch; ++ch) {
-                    uint32_t y[16];
-                    tmem_ld16(tmem + 2 * N + o * N + lanes + 16 * ch, y);
-                    wait_ld(y);
-                    if (d >= D) continue;
-                    if (special) {
-                        for (int u = max(sx.w.tile * kTN, ses.len); u < min((sx.w.tile + sx.m) * kTN, ses.kv); ++u) {
-                            const int page = b.table[(int64_t)sx.w.s * b.max_pages + u / p.page_pos];
-                            if (page < 0 || page >= p.n_pages) continue;
-                            const uint16_t v = reinterpret_cast<const uint16_t*>(p.base + (int64_t)a.layer * p.sl + (int64_t)sx.w.h * p.sh + p.skv +
-                                                                                 (int64_t)page * p.spage + (int64_t)(u % p.page_pos) * p.sp)[d];
-                            if ((v & Kind<T>::exponent) != Kind<T>::exponent) continue;
-#pragma unroll
-                            for (int r = 0; r < 16; ++r)
-                                if (16 * ch + r < rows && (seen_bits(a, ses, (row0 + 16 * ch + r) / a.group, u) & 1u))
-                                    y[r] = __float_as_uint(__uint_as_float(y[r]) + Kind<T>::widen(v));
-                        }
-                    }
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int q = 16 * ch + r;
-                        if (q >= rows) break;
-                        const float f = factor_s[q], v = f == 0.f ? 0.f : __uint_as_float(y[r]) * f;
-                        if (whole) static_cast<uint16_t*>(a.out)[row_at[q] + d] = (uint16_t)(Kind<T>::pack(v, 0.f) & 0xffffu);
-                        else a.part_o[(slot + q) * D + d] = v;
-                    }
-                }
-            }
-            fence_before();
+            if (tid < N) last_top_s[tid] = top_s[tid];
+            if (x + 1 == total) results(x);
         }
     }
     fence_before();
     __syncthreads();
-    if (wid == mma_warp) {
+    if (wid == qk_warp) {
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)F::tmem) : "memory");
     }
 }
 
-template <class T, int D>
+template <class T, int D, int N>
 cudaError_t launch(const PoolDev& p, const BookDev& b, const AttendArgs& a, const AttendPlan& x, uint32_t* status, cudaStream_t st) {
-    using F = Few<D>;
-    cudaError_t e = cudaFuncSetAttribute(few_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::smem);
+    using F = Few<D, N>;
+    cudaError_t e = cudaFuncSetAttribute(few_kernel<T, D, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::smem);
     if (e != cudaSuccess) return e;
-    e = launch_kernel(few_kernel<T, D>, x.grid, kFewThreads, F::smem, st, false, 1, p, b, a, status);
-    return e != cudaSuccess ? e : launch_join<T, D, F::N>(p, b, a, x, st);
+    e = launch_kernel(few_kernel<T, D, N>, x.grid, F::threads, F::smem, st, false, 1, p, b, a, status);
+    return e != cudaSuccess ? e : launch_join<T, D, N>(p, b, a, x, st);
 }
 template <class T>
 cudaError_t launch_type(const PoolDev& p, const BookDev& b, const AttendArgs& a, const AttendPlan& x, uint32_t* status, cudaStream_t st) {
+    const bool least = x.row_tile == 16, mid = x.row_tile == 32;
     switch (p.d) {
-        case 32: return launch<T, 32>(p, b, a, x, status, st);
-        case 64: return launch<T, 64>(p, b, a, x, status, st);
-        case 128: return launch<T, 128>(p, b, a, x, status, st);
-        default: return launch<T, 256>(p, b, a, x, status, st);
+        case 32: return least ? launch<T, 32, 16>(p, b, a, x, status, st) : mid ? launch<T, 32, 32>(p, b, a, x, status, st) : launch<T, 32, 64>(p, b, a, x, status, st);
+        case 64: return least ? launch<T, 64, 16>(p, b, a, x, status, st) : mid ? launch<T, 64, 32>(p, b, a, x, status, st) : launch<T, 64, 64>(p, b, a, x, status, st);
+        case 128: return least ? launch<T, 128, 16>(p, b, a, x, status, st) : mid ? launch<T, 128, 32>(p, b, a, x, status, st) : launch<T, 128, 64>(p, b, a, x, status, st);
+        default: return least ? launch<T, 256, 16>(p, b, a, x, status, st) : launch<T, 256, 32>(p, b, a, x, status, st);
     }
 }
 
