@@ -42,7 +42,7 @@ template <class T, int D, int NT>
 __global__ void __launch_bounds__(Shape<D, NT>::threads, Shape<D, NT>::per_sm)
 attend_kernel(PoolDev p, BookDev b, const __grid_constant__ AttendArgs a, uint32_t* status) {
     using Sh = Shape<D, NT>;
-    using Wk = Walk<Sh::TN, Sh::rows>;
+    using Wk = Walk<Sh::rows>;
     constexpr int TN = Sh::TN, stages = Sh::stages, n_warps = Sh::threads / 32;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -86,7 +86,7 @@ attend_kernel(PoolDev p, BookDev b, const __grid_constant__ AttendArgs a, uint32
     fence_before();
 
     Wk w{};
-    long long left = find_range<TN, Sh::rows, Sh::threads>(p, b, a, status, w);
+    long long left = find_range<Sh::rows, Sh::threads>(p, b, a, status, w);
     fence_after();
     const uint32_t tmem = *tmem_slot;
     const int me = blockIdx.x;
@@ -510,12 +510,13 @@ plc_status plc_tree_attention(const plc_page_pool* pool, int32_t layer, const pl
     if (workspace_bytes < x.bytes) return PLC_E_CAPACITY;
     if (t->n_rows == 0) return PLC_OK;
     AttendArgs a{t->q_dev, t->q_stride_row, t->q_stride_head, t->out_dev, t->out_stride_row, t->out_stride_head, t->lse_dev, t->begin_dev,
-                 t->mask_dev, t->n_rows, t->n_heads, group, t->mask_dev ? t->mask_words : 0, layer, scale, nullptr, nullptr, nullptr, x.part_rows};
+                 t->mask_dev, t->n_rows, t->n_heads, group, t->mask_dev ? t->mask_words : 0, layer, scale, nullptr, nullptr, nullptr, x.part_rows, p.d == 256 ? 64 : 128, 0, 0, {}};
     a.first = static_cast<int4*>(workspace_dev);
     a.part_o = reinterpret_cast<float*>(a.first + x.grid);
     a.part_ml = reinterpret_cast<float2*>(a.part_o + 2ll * x.grid * x.part_rows * p.d);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = x.row_tile <= kFewRows ? launch_attend_few(p, b, a, x, pool->dtype == PLC_OUT_BF16, status_dev, st)
+    const cudaError_t e = x.row_tile <= kFewRows
+        ? (pool->dtype == PLC_OUT_F16 ? launch_attend_few_f16(p, b, a, x, status_dev, st) : launch_attend_few_bf16(p, b, a, x, status_dev, st))
         : pool->dtype == PLC_OUT_F16 ? launch_type<__half>(p, b, a, x, status_dev, st) : launch_type<__nv_bfloat16>(p, b, a, x, status_dev, st);
     if (e != cudaSuccess) return PLC_E_CUDA;
     count_launch(2);

@@ -20,12 +20,16 @@ struct AttendArgs {
     float2* part_ml;                              // [2 * grid][part_rows]: maximum (scaled, base 2), sum
     int4* first;                                  // [grid]: session, head, row tile, first position tile of each CTA's range (-1: none)
     int part_rows;
+    int tile_pos;                                 // positions a tile (whole pages, or whole parts of a page, where the copies are boxes)
+    int box_pos, boxes;                           // positions a box, boxes a tile; 0: no boxes
+    int box_dim[4];                               // what dimensions 1 .. 4 of the boxes' map are: 0 slot, 1 head, 2 page, 3 key or value
 };
 
 // Which kernel a call takes, and what it needs.
 struct AttendPlan { int row_tile, grid, part_rows; uint64_t bytes; };
 
-cudaError_t launch_attend_few(const PoolDev& p, const BookDev& b, const AttendArgs& a, const AttendPlan& x, bool bf16, uint32_t* status, cudaStream_t st);
+cudaError_t launch_attend_few_f16(const PoolDev& p, const BookDev& b, const AttendArgs& a, const AttendPlan& x, uint32_t* status, cudaStream_t st);
+cudaError_t launch_attend_few_bf16(const PoolDev& p, const BookDev& b, const AttendArgs& a, const AttendPlan& x, uint32_t* status, cudaStream_t st);
 
 #ifdef __CUDACC__
 namespace {
@@ -155,13 +159,13 @@ __device__ __forceinline__ Session session_of(const PoolDev& p, const BookDev& b
 }
 
 // Where a range of position tiles stands: item (session, head, row tile) and tile in it.
-template <int TN, int ROWS> struct Walk {
+template <int ROWS> struct Walk {
     int s, h, rt, tile, tiles, row_tiles;
     Session x;
     __device__ __forceinline__ void enter(const PoolDev& p, const BookDev& b, const AttendArgs& a) {
         bool bad;
         x = session_of(p, b, a, s, &bad);
-        tiles = (x.kv + TN - 1) / TN;
+        tiles = (x.kv + a.tile_pos - 1) / a.tile_pos;
         row_tiles = (int)(((long long)x.n * a.group + ROWS - 1) / ROWS);
     }
     __device__ __forceinline__ void start(const PoolDev& p, const BookDev& b, const AttendArgs& a, int session, long long rest) {
@@ -201,8 +205,8 @@ __device__ __forceinline__ uint32_t seen_bits(const AttendArgs& a, const Session
 }
 
 // A CTA's range [0, left) of the sequence of tiles, from w on.  Every thread of the CTA calls it; two barriers.
-template <int TN, int ROWS, int THREADS>
-__device__ __forceinline__ long long find_range(const PoolDev& p, const BookDev& b, const AttendArgs& a, uint32_t* status, Walk<TN, ROWS>& w) {
+template <int ROWS, int THREADS>
+__device__ __forceinline__ long long find_range(const PoolDev& p, const BookDev& b, const AttendArgs& a, uint32_t* status, Walk<ROWS>& w) {
     __shared__ long long sums[THREADS / 32];
     __shared__ long long range_at[2];             // the range's first session, and the tiles of it that lie before the range
     const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
@@ -210,7 +214,7 @@ __device__ __forceinline__ long long find_range(const PoolDev& p, const BookDev&
     const int run = (b.rows + THREADS - 1) / THREADS, s0 = min(b.rows, tid * run), s1 = min(b.rows, s0 + run);
     auto tiles_of = [&](int s, bool* bad) -> long long {
         const Session x = session_of(p, b, a, s, bad);
-        return (long long)((x.kv + TN - 1) / TN) * (((long long)x.n * a.group + ROWS - 1) / ROWS) * p.H;
+        return (long long)((x.kv + a.tile_pos - 1) / a.tile_pos) * (((long long)x.n * a.group + ROWS - 1) / ROWS) * p.H;
     };
     long long mine = 0;
     bool any_bad = false;
@@ -254,11 +258,11 @@ __device__ __forceinline__ long long find_range(const PoolDev& p, const BookDev&
 }
 
 // The tiles of a range one after the other; a piece is what the range holds of one item.
-template <int TN, int ROWS> struct Tiles {
-    Walk<TN, ROWS> w;
+template <int ROWS> struct Tiles {
+    Walk<ROWS> w;
     long long left;                               // from this piece on
     int j, m, piece;                              // tile of the piece, tiles in it, number of the piece
-    __device__ __forceinline__ void start(const Walk<TN, ROWS>& from, long long n) {
+    __device__ __forceinline__ void start(const Walk<ROWS>& from, long long n) {
         w = from;
         left = n;
         j = piece = 0;

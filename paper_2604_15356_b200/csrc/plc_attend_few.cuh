@@ -10,25 +10,29 @@
 // scores of a tile are formed while the one before is in the softmax.
 // A row's maximum is common to the CTA and raised only where some score passes it by 2^3 (a vote of the four warps a tile); each thread sums the
 // weights of its positions, and the sums are joined at the end of an item.
+#pragma once
+#include <cuda.h>
+
 #include "plc_attend.cuh"
 
 namespace plc {
 namespace {
 
-constexpr int kTN = 128, kCopy = 128;
+constexpr int kTN = 128;
 constexpr int kWords = 16;                        // tiles whose validity words are kept: more than the ring holds
 
 // N: most rows of an item, and the columns of its products.
-template <int D, int N> struct Few {
+template <int D, int N, bool BOX> struct Few {
     static constexpr int blocks = (D + 63) / 64;                       // 128-byte wide column blocks (32 components: half of one)
     static constexpr int slot = blocks * kTN * 128, slots = D == 256 ? 3 : (D == 128 ? 1 : 2) * (N == 16 ? 6 : N == 32 ? 5 : 4);
     static constexpr int q_bytes = blocks * N * 128, q_bufs = D == 256 ? 1 : 2;
     static constexpr int p_bytes = N * kTN * 2, p_bufs = D == 256 ? 1 : 2;
     static constexpr int o_blocks = D == 256 ? 2 : 1;
     // softmax: groups of four warps, which share the rows; N / groups of them a thread
-    static constexpr int groups = N == 16 ? 1 : 2, C = N / groups, soft = 128 * groups, threads = soft + kCopy + 64;
+    static constexpr int groups = N == 16 ? 1 : 2, C = N / groups, soft = 128 * groups;
+    static constexpr int copy = BOX ? 32 : 128, threads = soft + copy + 64;
     static constexpr int tmem = N == 64 || o_blocks * N == 64 ? 256 : 128;   // S twice, O twice
-    static constexpr size_t smem = (size_t)q_bufs * q_bytes + p_bufs * p_bytes + slots * slot + 3 * kTN * 8 + N * (8 + 4 * 13) + 768 + 1024;
+    static constexpr size_t smem = (size_t)q_bufs * q_bytes + p_bufs * p_bytes + slots * slot + (BOX ? 0 : 3 * kTN * 8) + N * (8 + 4 * 13) + 768 + 1024;
 };
 
 // Of N threads at a barrier of their own: whether any, or all, say so.
@@ -121,18 +125,19 @@ __device__ __noinline__ void put_back(const PoolDev& p, const BookDev& b, const 
     }
 }
 
-template <class T, int D, int N>
-__global__ void __launch_bounds__(Few<D, N>::threads, 1) few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b, const __grid_constant__ AttendArgs a,
-                                                             uint32_t* status) {
-    using F = Few<D, N>;
-    using Tl = Tiles<kTN, N>;
+template <class T, int D, int N, bool BOX>
+__global__ void __launch_bounds__(Few<D, N, BOX>::threads, 1)
+few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b, const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map,
+           uint32_t* status) {
+    using F = Few<D, N, BOX>;
+    using Tl = Tiles<N>;
     constexpr int slots = F::slots, C = F::C, soft_warps = F::soft / 32, qk_warp = F::threads / 32 - 2, pv_warp = qk_warp + 1;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* qs = ring + slots * F::slot;
     uint8_t* ps = qs + F::q_bufs * F::q_bytes;
-    uint64_t* from = reinterpret_cast<uint64_t*>(ps + F::p_bufs * F::p_bytes);          // [3][kTN] where a position's key stands
-    int64_t* row_at = reinterpret_cast<int64_t*>(from + 3 * kTN);                       // [N] where a row of the result goes
+    uint64_t* from = reinterpret_cast<uint64_t*>(ps + F::p_bufs * F::p_bytes);                               // [3][kTN] where a position's key stands (without boxes)
+    int64_t* row_at = reinterpret_cast<int64_t*>(from + (BOX ? 0 : 3 * kTN));                       // [N] where a row of the result goes
     float* base_s = reinterpret_cast<float*>(row_at + N);                               // [N] what the weights' exponents are relative to
     float* top_s = base_s + N;                                                          // [N] maximum (scaled, base 2)
     float* factor_s = top_s + N;                                                        // [N]
@@ -151,9 +156,9 @@ __global__ void __launch_bounds__(Few<D, N>::threads, 1) few_kernel(const __grid
                    ofull = pfull + 16, drain = ofull + 16;
     chain_next();
     if (tid == 0) {
-        for (int i = 0; i < slots; ++i) { mbar_init(full + 8 * i, kCopy + kCopy / 32); mbar_init(empty + 8 * i, 1); }
+        for (int i = 0; i < slots; ++i) { mbar_init(full + 8 * i, BOX ? 1 : F::copy + F::copy / 32); mbar_init(empty + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(qfull + 8 * i, kCopy);
+            mbar_init(qfull + 8 * i, F::copy);
             mbar_init(qempty + 8 * i, 1);
             mbar_init(sfull + 8 * i, 1);
             mbar_init(pfull + 8 * i, soft_warps);
@@ -167,101 +172,177 @@ __global__ void __launch_bounds__(Few<D, N>::threads, 1) few_kernel(const __grid
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"((uint32_t)F::tmem) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    const int tile_pos = BOX ? a.tile_pos : kTN;
+    if (BOX && tile_pos < kTN) {                  // positions of a tile that no box fills: zeros once and for all
+        constexpr int row_pieces = F::blocks * 8;
+        for (int i = tid; i < slots * (kTN - tile_pos) * row_pieces; i += F::threads) {
+            const int s = i / ((kTN - tile_pos) * row_pieces), k = i % ((kTN - tile_pos) * row_pieces), r = tile_pos + k / row_pieces, c = k % row_pieces;
+            *reinterpret_cast<uint4*>(ring + s * F::slot + (c >> 3) * (kTN * 128) + r * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
     fence_before();
-    Walk<kTN, N> w0{};
-    const long long total = find_range<kTN, N, F::threads>(p, b, a, status, w0);
+    Walk<N> w0{};
+    const long long total = find_range<N, F::threads>(p, b, a, status, w0);
     fence_after();
     const uint32_t tmem = *tmem_slot, ring_s = smem_u32(ring), q_s = smem_u32(qs), p_s = smem_u32(ps);
 
     if (wid >= soft_warps && wid < qk_warp) {
-        // ---- copies
         const int lt = tid - F::soft;
-        constexpr int pieces = D / 8, step = kCopy / pieces, rounds = kTN / step;   // 16-byte pieces of a vector; vectors a round
-        const int c = lt % pieces, r0 = lt / pieces;
-        const uint32_t to = (c >> 3) * (kTN * 128) + r0 * 128;
-        Tl kx, vx;
-        kx.start(w0, total);
-        vx.start(w0, total);
-        int kt = 0, vt = 0, sl = 0;
-        bool ok = true;
-        auto fill = [&](int tile, int64_t delta) {           // a tile's keys, or values (delta further on), into the next slot of the ring
-            const int s = sl % slots;
-            ok = __all_sync(kFull, ok && mbar_wait(empty + 8 * s, ((uint32_t)(sl / slots) & 1u) ^ 1u, failed, status));
-            ++sl;
-            if (!ok) return;
-            const uint32_t dst = ring_s + s * F::slot + to;
-            const uint64_t* src = from + tile % 3 * kTN + r0;
-            const uint32_t* valid = words + tile % kWords * 4;
-            delta += c * 16;
-            const bool all = (valid[0] & valid[1] & valid[2] & valid[3]) == ~0u;
-#pragma unroll
-            for (int k0 = 0; k0 < rounds; k0 += 8) {
-                uint64_t at[8];
-#pragma unroll
-                for (int k = 0; k < 8 && k0 + k < rounds; ++k) at[k] = src[(k0 + k) * step];
-                if (all) {
-#pragma unroll
-                    for (int k = 0; k < 8 && k0 + k < rounds; ++k)
-                        copy16(dst + (k0 + k) * step * 128 + (((c & 7) ^ ((r0 + (k0 + k) * step) & 7)) << 4), reinterpret_cast<const uint8_t*>(at[k] + delta));
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 8 && k0 + k < rounds; ++k) {
-                        const int r = r0 + (k0 + k) * step;
-                        copy16(dst + (k0 + k) * step * 128 + (((c & 7) ^ (r & 7)) << 4), reinterpret_cast<const uint8_t*>(at[k] + delta), valid[r >> 5] >> (r & 31) & 1u);
-                    }
-                }
+        constexpr int pieces = D / 8;                // 16-byte pieces of a vector
+        auto load_q = [&](const Tl& x, bool ok) -> bool {    // a piece's rows of Q
+            const int q = x.piece % F::q_bufs, rows = x.w.rows(a);
+            ok = ok && mbar_wait(qempty + 8 * q, ((uint32_t)(x.piece / F::q_bufs) & 1u) ^ 1u, failed, status);
+            if (!ok) return false;
+            for (int u = lt; u < N * pieces; u += F::copy) {
+                const int r = u / pieces, c = u % pieces, rr = x.w.rt * N + r, i = rr / a.group, g = rr - i * a.group;
+                const uint8_t* src = static_cast<const uint8_t*>(a.q);
+                if (r < rows) src += 2 * ((int64_t)(x.w.x.first + i) * a.qs_row + (int64_t)(x.w.h * a.group + g) * a.qs_head) + c * 16;
+                copy16(q_s + q * F::q_bytes + (c >> 3) * (N * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4), src, r < rows);
             }
-            mbar_arrive_copies(full + 8 * s);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(full + 8 * s);                        // the validity words, too, are there
+            mbar_arrive_copies(qfull + 8 * q);
+            return true;
         };
-        int slot_in = 0, page = -1;                  // this thread's position of K's next tile: slot in its page, the page
-        auto look_up = [&]() {                       // issued a tile ahead of its use
-            const int t = (kx.w.tile + kx.j) * kTN + lt, pg = t / p.page_pos;
-            const bool have = t < kx.w.x.kv;
-            slot_in = have ? t - pg * p.page_pos : -1;
-            page = have ? b.table[(int64_t)kx.w.s * b.max_pages + pg] : 0;
-        };
-        if (kx.more()) look_up();
-        for (;;) {
-            const bool more = kx.more();
-            if (!more && !vx.more()) break;
-            if (more) {
-                if (kx.j == 0) {
-                    const int q = kx.piece % F::q_bufs, rows = kx.w.rows(a);
-                    ok = ok && mbar_wait(qempty + 8 * q, ((uint32_t)(kx.piece / F::q_bufs) & 1u) ^ 1u, failed, status);
-                    if (ok) {
-                        for (int r = r0; r < N; r += step) {
-                            const int rr = kx.w.rt * N + r, i = rr / a.group, g = rr - i * a.group;
-                            const uint8_t* src = static_cast<const uint8_t*>(a.q);
-                            if (r < rows) src += 2 * ((int64_t)(kx.w.x.first + i) * a.qs_row + (int64_t)(kx.w.h * a.group + g) * a.qs_head) + c * 16;
-                            copy16(q_s + q * F::q_bytes + (c >> 3) * (N * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4), src, r < rows);
+        if constexpr (BOX) {
+            // ---- copies, one warp: a lane a box of the tile (box_pos positions of one page, 64 components wide)
+            Tl kx;
+            kx.start(w0, total);
+            int sl = 0, page = -1, slot = 0, head = 0, last_page = -1, last_slot = 0, last_head = 0;   // the lane's box of K's tile, and of the tile before
+            bool ok = true;
+            const int my_box = 4 * lane / a.box_pos; // of the four positions whose validity the lane tells
+            auto look_up = [&]() {                   // issued a tile ahead of its use; -1: behind the last position
+                const int t = (kx.w.tile + kx.j) * tile_pos + lane * a.box_pos, pg = t / p.page_pos;
+                slot = t - pg * p.page_pos;
+                page = lane < a.boxes && t < kx.w.x.kv ? b.table[(int64_t)kx.w.s * b.max_pages + pg] : -1;
+                if (page == -1 && lane < a.boxes && t < kx.w.x.kv) page = -2;
+            };
+            auto fill = [&](int pg, int at, int h, int kv) {
+                const int s = sl % slots;
+                ok = __all_sync(kFull, ok && mbar_wait(empty + 8 * s, ((uint32_t)(sl / slots) & 1u) ^ 1u, failed, status));
+                ++sl;
+                if (!ok) return;
+                const bool have = pg >= 0 && pg < p.n_pages;
+                const int n = __popc(__ballot_sync(kFull, have));
+                if (lane == 0)
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(full + 8 * s), "r"(n * a.box_pos * F::blocks * 128) : "memory");
+                __syncwarp();
+                if (!have) return;
+                int at_dim[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) at_dim[i] = a.box_dim[i] == 0 ? at : a.box_dim[i] == 1 ? h : a.box_dim[i] == 2 ? pg : kv;
+#pragma unroll
+                for (int k = 0; k < F::blocks; ++k)
+                    asm volatile(
+                        "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(
+                            ring_s + s * F::slot + k * (kTN * 128) + lane * a.box_pos * 128),
+                        "l"(&map), "r"(k * 64), "r"(at_dim[0]), "r"(at_dim[1]), "r"(at_dim[2]), "r"(at_dim[3]), "r"(full + 8 * s)
+                        : "memory");
+            };
+            if (total > 0) look_up();
+            for (long long x = 0; x <= total && ok; ++x) {
+                if (x < total) {
+                    if (kx.j == 0) ok = __all_sync(kFull, load_q(kx, ok));
+                    if (page < -1 || page >= p.n_pages) atomicOr(status, kStRange);
+                    const int box = __shfl_sync(kFull, page, my_box & 31), t = (kx.w.tile + kx.j) * tile_pos + 4 * lane;
+                    const bool there = box >= 0 && box < p.n_pages && 4 * lane < tile_pos;
+                    const int n = there ? min(max(kx.w.x.kv - t, 0), 4) : 0;
+                    const uint32_t word = __reduce_or_sync(0xffu << (lane & 24), ((1u << n) - 1u) << (4 * (lane & 7)));
+                    if ((lane & 7) == 0) words[x % kWords * 4 + (lane >> 3)] = word;
+                    head = kx.w.h;
+                    __syncwarp();
+                    fill(page, slot, head, 0);
+                }
+                const int p1 = page, s1 = slot, h1 = head;
+                if (x + 1 < total) { kx.next(p, b, a); look_up(); }
+                if (x > 0) fill(last_page, last_slot, last_head, 1);         // V of a tile after K of the next
+                last_page = p1; last_slot = s1; last_head = h1;
+            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            if (!ok)                                 // boxes still in flight (none after a complete run) land before the CTA ends
+                for (int i = sl > slots ? sl - slots : 0; i < sl; ++i)
+                    for (uint32_t k = 0; k < kSpin; ++k) {
+                        uint32_t done;
+                        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                                     : "=r"(done) : "r"(full + 8 * (i % slots)), "r"((uint32_t)(i / slots) & 1u) : "memory");
+                        if (done) break;
+                    }
+        } else {
+            // ---- copies, four warps, position by position (pages of any size)
+            constexpr int step = F::copy / pieces, rounds = kTN / step;   // vectors a round
+            const int c = lt % pieces, r0 = lt / pieces;
+            const uint32_t to = (c >> 3) * (kTN * 128) + r0 * 128;
+            Tl kx, vx;
+            kx.start(w0, total);
+            vx.start(w0, total);
+            int kt = 0, vt = 0, sl = 0;
+            bool ok = true;
+            auto fill = [&](int tile, int64_t delta) {           // a tile's keys, or values (delta further on), into the next slot of the ring
+                const int s = sl % slots;
+                ok = __all_sync(kFull, ok && mbar_wait(empty + 8 * s, ((uint32_t)(sl / slots) & 1u) ^ 1u, failed, status));
+                ++sl;
+                if (!ok) return;
+                const uint32_t dst = ring_s + s * F::slot + to;
+                const uint64_t* src = from + tile % 3 * kTN + r0;
+                const uint32_t* valid = words + tile % kWords * 4;
+                delta += c * 16;
+                const bool all = (valid[0] & valid[1] & valid[2] & valid[3]) == ~0u;
+#pragma unroll
+                for (int k0 = 0; k0 < rounds; k0 += 8) {
+                    uint64_t at[8];
+#pragma unroll
+                    for (int k = 0; k < 8 && k0 + k < rounds; ++k) at[k] = src[(k0 + k) * step];
+                    if (all) {
+#pragma unroll
+                        for (int k = 0; k < 8 && k0 + k < rounds; ++k)
+                            copy16(dst + (k0 + k) * step * 128 + (((c & 7) ^ ((r0 + (k0 + k) * step) & 7)) << 4), reinterpret_cast<const uint8_t*>(at[k] + delta));
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 8 && k0 + k < rounds; ++k) {
+                            const int r = r0 + (k0 + k) * step;
+                            copy16(dst + (k0 + k) * step * 128 + (((c & 7) ^ (r & 7)) << 4), reinterpret_cast<const uint8_t*>(at[k] + delta), valid[r >> 5] >> (r & 31) & 1u);
                         }
-                        mbar_arrive_copies(qfull + 8 * q);
                     }
                 }
-                const bool there = page >= 0 && page < p.n_pages, have = slot_in >= 0 && there;
-                if (!there) atomicOr(status, kStRange);
-                // (a position that does not exist: anywhere in the pool, nothing is read)
-                from[kt % 3 * kTN + lt] = reinterpret_cast<uint64_t>(p.base) +
-                                          (have ? (int64_t)a.layer * p.sl + (int64_t)kx.w.h * p.sh + (int64_t)page * p.spage + (int64_t)slot_in * p.sp : 0);
-                const uint32_t valid = __ballot_sync(kFull, have);
-                if (lane == 0) words[kt % kWords * 4 + (lt >> 5)] = valid;
+                mbar_arrive_copies(full + 8 * s);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(full + 8 * s);                        // the validity words, too, are there
+            };
+            int slot_in = 0, page = -1;                  // this thread's position of K's next tile: slot in its page, the page
+            auto look_up = [&]() {                       // issued a tile ahead of its use
+                const int t = (kx.w.tile + kx.j) * kTN + lt, pg = t / p.page_pos;
+                const bool have = t < kx.w.x.kv;
+                slot_in = have ? t - pg * p.page_pos : -1;
+                page = have ? b.table[(int64_t)kx.w.s * b.max_pages + pg] : 0;
+            };
+            if (kx.more()) look_up();
+            for (;;) {
+                const bool more = kx.more();
+                if (!more && !vx.more()) break;
+                if (more) {
+                    if (kx.j == 0) ok = load_q(kx, ok);
+                    const bool there = page >= 0 && page < p.n_pages, have = slot_in >= 0 && there;
+                    if (!there) atomicOr(status, kStRange);
+                    // (a position that does not exist: anywhere in the pool, nothing is read)
+                    from[kt % 3 * kTN + lt] = reinterpret_cast<uint64_t>(p.base) +
+                                              (have ? (int64_t)a.layer * p.sl + (int64_t)kx.w.h * p.sh + (int64_t)page * p.spage + (int64_t)slot_in * p.sp : 0);
+                    const uint32_t valid = __ballot_sync(kFull, have);
+                    if (lane == 0) words[kt % kWords * 4 + (lt >> 5)] = valid;
+                }
+                if (!vote_all<1, F::copy>(ok)) break;
+                if (more) {
+                    fill(kt, 0);
+                    ++kt;
+                    kx.next(p, b, a);
+                    if (kx.more()) look_up();
+                }
+                if (kt > 1 || !more) {                                           // V of a tile after K of the next
+                    fill(vt, p.skv);
+                    ++vt;
+                    vx.next(p, b, a);
+                }
             }
-            if (!vote_all<1, kCopy>(ok)) break;
-            if (more) {
-                fill(kt, 0);
-                ++kt;
-                kx.next(p, b, a);
-                if (kx.more()) look_up();
-            }
-            if (kt > 1 || !more) {                                           // V of a tile after K of the next
-                fill(vt, p.skv);
-                ++vt;
-                vx.next(p, b, a);
-            }
+            asm volatile("cp.async.wait_all;" ::: "memory");
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
     } else if (wid >= qk_warp) {
         if (lane == 0) {
             // ---- products, a thread for each of the two.  The ring holds K(0), then K(x + 1), V(x) for every tile x.
@@ -360,13 +441,13 @@ __global__ void __launch_bounds__(Few<D, N>::threads, 1) few_kernel(const __grid
             }
             if (dirty[f.piece & 1] == (uint32_t)f.piece + 1u && vote_all<2, F::soft>(true))       // every group's rows are written
                 for (int d = tid; d < D; d += F::soft)
-                    put_back<T>(p, b, a, f.w.x, f.w.s, f.w.h, f.w.tile * kTN, (f.w.tile + f.m) * kTN, row0, rows, d, row_at, whole ? nullptr : a.part_o + slot * D + d);
+                    put_back<T>(p, b, a, f.w.x, f.w.s, f.w.h, f.w.tile * tile_pos, (f.w.tile + f.m) * tile_pos, row0, rows, d, row_at, whole ? nullptr : a.part_o + slot * D + d);
             fence_before();
             return true;
         };
         for (int x = 0; sx.more(); ++x, sx.next(p, b, a)) {
-            const int t0 = (sx.w.tile + sx.j) * kTN;
-            const bool first = sx.j == 0, drafted = t0 + kTN > sx.w.x.len;
+            const int t0 = (sx.w.tile + sx.j) * tile_pos;
+            const bool first = sx.j == 0, drafted = t0 + tile_pos > sx.w.x.len;
             ok = ok && mbar_wait(sfull + 8 * (x & 1), (uint32_t)(x >> 1) & 1u, failed, status);
             if (x >= F::p_bufs) ok = ok && mbar_wait(ofull + 8 * ((x - F::p_bufs) & 1), (uint32_t)((x - F::p_bufs) >> 1) & 1u, failed, status);
             ok = __all_sync(kFull, ok);
@@ -472,10 +553,17 @@ __global__ void __launch_bounds__(Few<D, N>::threads, 1) few_kernel(const __grid
                 }
                 *reinterpret_cast<uint4*>(pp + (r / 8) * 2048) = make_uint4(y[0], y[1], y[2], y[3]);
             }
-            if (hide && wid < 4) {
+            // V of positions that do not exist is whatever the boxes brought or left: zeros instead, since weights of 0 do not hide it
+            const bool blank = BOX && masked && pos < tile_pos && !(words[x % kWords * 4 + quarter] >> lane & 1u);
+            if ((hide || (BOX && masked)) && wid < 4) {
                 const int sl = x + 1 < total ? 2 * x + 2 : 2 * x + 1;       // V's place in the order of the ring
                 ok = ok && mbar_wait(full + 8 * (sl % slots), (uint32_t)(sl / slots) & 1u, failed, status);
-                if (ok && t0 + tid >= sx.w.x.len && t0 + tid < sx.w.x.kv && take_out<T, D>(ring + sl % slots * F::slot, tid)) dirty[sx.piece & 1] = (uint32_t)sx.piece + 1u;
+                uint8_t* tile = ring + sl % slots * F::slot;
+                if (ok && blank)
+                    for (int e = 0; e < F::blocks * 8; ++e)
+                        *reinterpret_cast<uint4*>(tile + (e >> 3) * (kTN * 128) + pos * 128 + (((e & 7) ^ (pos & 7)) << 4)) = make_uint4(0, 0, 0, 0);
+                else if (ok && hide && pos < tile_pos && t0 + pos >= sx.w.x.len && t0 + pos < sx.w.x.kv && take_out<T, D>(tile, pos))
+                    dirty[sx.piece & 1] = (uint32_t)sx.piece + 1u;
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // P (and V) as the product reads them
             fence_before();
@@ -506,29 +594,78 @@ __global__ void __launch_bounds__(Few<D, N>::threads, 1) few_kernel(const __grid
     }
 }
 
-template <class T, int D, int N>
-cudaError_t launch(const PoolDev& p, const BookDev& b, const AttendArgs& a, const AttendPlan& x, uint32_t* status, cudaStream_t st) {
-    using F = Few<D, N>;
-    cudaError_t e = cudaFuncSetAttribute(few_kernel<T, D, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::smem);
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled_fn() {
+    static const EncodeTiledFn fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess
+                   ? reinterpret_cast<EncodeTiledFn>(f) : nullptr;
+    }();
+    return fn;
+}
+
+// The layer's keys and values in boxes of 64 components by as many positions as a page has whole boxes of (a multiple of the eight
+// rows that the swizzle repeats after, at most 128).  False where the pool has no such boxes: pages of other sizes, vectors of 32
+// components (a box row would be half a shared memory row), strides that are not positive or not multiples of each other.
+bool make_boxes(const PoolDev& p, AttendArgs& a, bool bf16, CUtensorMap* map) {
+    if (p.d < 64 || p.page_pos % 8) return false;
+    int box = 8;
+    for (int k = 16; k <= 128; k += 8)
+        if (p.page_pos % k == 0) box = k;
+    const int64_t stride[4] = {p.sp, p.sh, p.spage, p.skv};
+    const cuuint64_t extent[4] = {(cuuint64_t)p.page_pos, (cuuint64_t)p.H, (cuuint64_t)p.n_pages, 2};
+    int order[4] = {0, 1, 2, 3};
+    for (int i = 0; i < 4; ++i) {
+        if (stride[i] <= 0 || stride[i] >= (1ll << 40)) return false;
+        for (int j = i; j > 0 && stride[order[j]] < stride[order[j - 1]]; --j) { const int t = order[j]; order[j] = order[j - 1]; order[j - 1] = t; }
+    }
+    cuuint64_t dims[5] = {(cuuint64_t)p.d}, strides[4];
+    cuuint32_t boxes[5] = {64}, ones[5] = {1, 1, 1, 1, 1};
+    for (int i = 0; i < 4; ++i) {
+        dims[i + 1] = extent[order[i]];
+        strides[i] = (cuuint64_t)stride[order[i]];
+        boxes[i + 1] = order[i] == 0 ? (cuuint32_t)box : 1;
+        if (i > 0 && strides[i] % strides[i - 1]) return false;
+        a.box_dim[i] = order[i];
+    }
+    const EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn || fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, p.base + (int64_t)a.layer * p.sl, dims, strides, boxes, ones,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return false;
+    a.box_pos = box;
+    a.boxes = 128 / box;
+    a.tile_pos = box * a.boxes;
+    return true;
+}
+
+template <class T, int D, int N, bool BOX>
+cudaError_t launch(const PoolDev& p, const BookDev& b, const AttendArgs& a, const CUtensorMap& map, const AttendPlan& x, uint32_t* status, cudaStream_t st) {
+    using F = Few<D, N, BOX>;
+    cudaError_t e = cudaFuncSetAttribute(few_kernel<T, D, N, BOX>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::smem);
     if (e != cudaSuccess) return e;
-    e = launch_kernel(few_kernel<T, D, N>, x.grid, F::threads, F::smem, st, false, 1, p, b, a, status);
+    e = launch_kernel(few_kernel<T, D, N, BOX>, x.grid, F::threads, F::smem, st, false, 1, p, b, a, map, status);
     return e != cudaSuccess ? e : launch_join<T, D, N>(p, b, a, x, st);
 }
 template <class T>
-cudaError_t launch_type(const PoolDev& p, const BookDev& b, const AttendArgs& a, const AttendPlan& x, uint32_t* status, cudaStream_t st) {
-    const bool least = x.row_tile == 16, mid = x.row_tile == 32;
+cudaError_t launch_few(const PoolDev& p, const BookDev& b, const AttendArgs& args, const AttendPlan& x, bool bf16, uint32_t* status, cudaStream_t st) {
+    AttendArgs a = args;
+    a.tile_pos = kTN;
+    CUtensorMap map{};
+    const bool boxes = make_boxes(p, a, bf16, &map), least = x.row_tile == 16, mid = x.row_tile == 32;
+    if (boxes) switch (p.d) {
+            case 64: return least ? launch<T, 64, 16, true>(p, b, a, map, x, status, st) : mid ? launch<T, 64, 32, true>(p, b, a, map, x, status, st) : launch<T, 64, 64, true>(p, b, a, map, x, status, st);
+            case 128: return least ? launch<T, 128, 16, true>(p, b, a, map, x, status, st) : mid ? launch<T, 128, 32, true>(p, b, a, map, x, status, st) : launch<T, 128, 64, true>(p, b, a, map, x, status, st);
+            default: return least ? launch<T, 256, 16, true>(p, b, a, map, x, status, st) : launch<T, 256, 32, true>(p, b, a, map, x, status, st);
+        }
     switch (p.d) {
-        case 32: return least ? launch<T, 32, 16>(p, b, a, x, status, st) : mid ? launch<T, 32, 32>(p, b, a, x, status, st) : launch<T, 32, 64>(p, b, a, x, status, st);
-        case 64: return least ? launch<T, 64, 16>(p, b, a, x, status, st) : mid ? launch<T, 64, 32>(p, b, a, x, status, st) : launch<T, 64, 64>(p, b, a, x, status, st);
-        case 128: return least ? launch<T, 128, 16>(p, b, a, x, status, st) : mid ? launch<T, 128, 32>(p, b, a, x, status, st) : launch<T, 128, 64>(p, b, a, x, status, st);
-        default: return least ? launch<T, 256, 16>(p, b, a, x, status, st) : launch<T, 256, 32>(p, b, a, x, status, st);
+        case 32: return least ? launch<T, 32, 16, false>(p, b, a, map, x, status, st) : mid ? launch<T, 32, 32, false>(p, b, a, map, x, status, st) : launch<T, 32, 64, false>(p, b, a, map, x, status, st);
+        case 64: return least ? launch<T, 64, 16, false>(p, b, a, map, x, status, st) : mid ? launch<T, 64, 32, false>(p, b, a, map, x, status, st) : launch<T, 64, 64, false>(p, b, a, map, x, status, st);
+        case 128: return least ? launch<T, 128, 16, false>(p, b, a, map, x, status, st) : mid ? launch<T, 128, 32, false>(p, b, a, map, x, status, st) : launch<T, 128, 64, false>(p, b, a, map, x, status, st);
+        default: return least ? launch<T, 256, 16, false>(p, b, a, map, x, status, st) : launch<T, 256, 32, false>(p, b, a, map, x, status, st);
     }
 }
 
 }  // namespace
-
-cudaError_t launch_attend_few(const PoolDev& p, const BookDev& b, const AttendArgs& a, const AttendPlan& x, bool bf16, uint32_t* status, cudaStream_t st) {
-    return bf16 ? launch_type<__nv_bfloat16>(p, b, a, x, status, st) : launch_type<__half>(p, b, a, x, status, st);
-}
-
 }  // namespace plc
