@@ -24,13 +24,16 @@ constexpr int kWords = 16;                        // tiles whose validity words 
 // N: most rows of an item, and the columns of its products.
 template <int D, int N, bool BOX> struct Few {
     static constexpr int blocks = (D + 63) / 64;                       // 128-byte wide column blocks (32 components: half of one)
-    static constexpr int slot = blocks * kTN * 128, slots = D == 256 ? 3 : (D == 128 ? 1 : 2) * (N == 16 ? 6 : N == 32 ? 5 : 4);
+    static constexpr int slot = blocks * kTN * 128;
+    // rings of K and of V: each slot has one producer, in order, so that no wait can be a phase early
+    static constexpr int k_slots = D == 256 ? 1 : (D == 128 ? 1 : 2) * (N == 16 ? 3 : 2), v_slots = D == 256 ? 2 : (D == 128 ? 1 : 2) * (N == 64 ? 2 : 3);
+    static constexpr int slots = k_slots + v_slots;
     static constexpr int q_bytes = blocks * N * 128, q_bufs = D == 256 ? 1 : 2;
     static constexpr int p_bytes = N * kTN * 2, p_bufs = D == 256 ? 1 : 2;
     static constexpr int o_blocks = D == 256 ? 2 : 1;
     // softmax: groups of four warps, which share the rows; N / groups of them a thread
     static constexpr int groups = N == 16 ? 1 : 2, C = N / groups, soft = 128 * groups;
-    static constexpr int copy = BOX ? 32 : 128, threads = soft + copy + 64;
+    static constexpr int copy = 128, q_copy = BOX ? 64 : 128, threads = soft + copy + 64;
     static constexpr int tmem = N == 64 || o_blocks * N == 64 ? 256 : 128;   // S twice, O twice
     static constexpr size_t smem = (size_t)q_bufs * q_bytes + p_bufs * p_bytes + slots * slot + (BOX ? 0 : 3 * kTN * 8) + N * (8 + 4 * 13) + 768 + 1024;
 };
@@ -109,7 +112,7 @@ __device__ __noinline__ bool take_out(uint8_t* tile, int pos) {
 }
 template <class T>
 __device__ __noinline__ void put_back(const PoolDev& p, const BookDev& b, const AttendArgs& a, const Session x, int s, int h, int t0, int t1, int row0, int rows, int d,
-                                      const int64_t* row_at, float* part) {
+                                      const int64_t* row_at, bool whole) {
     for (int t = max(t0, x.len); t < min(t1, x.kv); ++t) {
         const int page = b.table[(int64_t)s * b.max_pages + t / p.page_pos];
         if (page < 0 || page >= p.n_pages) continue;
@@ -118,8 +121,8 @@ __device__ __noinline__ void put_back(const PoolDev& p, const BookDev& b, const 
         if ((v & Kind<T>::exponent) != Kind<T>::exponent) continue;
         for (int r = 0; r < rows; ++r) {
             if (!(seen_bits(a, x, (row0 + r) / a.group, t) & 1u)) continue;
-            if (part) { part[(int64_t)r * p.d] += Kind<T>::widen(v); continue; }
-            uint16_t* o = static_cast<uint16_t*>(a.out) + row_at[r] + d;
+            if (!whole) { reinterpret_cast<float*>(row_at[r])[d] += Kind<T>::widen(v); continue; }
+            uint16_t* o = reinterpret_cast<uint16_t*>(row_at[r]) + d;
             *o = (uint16_t)(Kind<T>::pack(Kind<T>::widen(*o) + Kind<T>::widen(v), 0.f) & 0xffffu);
         }
     }
@@ -131,13 +134,13 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
            uint32_t* status) {
     using F = Few<D, N, BOX>;
     using Tl = Tiles<N>;
-    constexpr int slots = F::slots, C = F::C, soft_warps = F::soft / 32, qk_warp = F::threads / 32 - 2, pv_warp = qk_warp + 1;
+    constexpr int slots = F::slots, k_slots = F::k_slots, v_slots = F::v_slots, C = F::C, soft_warps = F::soft / 32, qk_warp = F::threads / 32 - 2;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* qs = ring + slots * F::slot;
     uint8_t* ps = qs + F::q_bufs * F::q_bytes;
     uint64_t* from = reinterpret_cast<uint64_t*>(ps + F::p_bufs * F::p_bytes);                               // [3][kTN] where a position's key stands (without boxes)
-    int64_t* row_at = reinterpret_cast<int64_t*>(from + (BOX ? 0 : 3 * kTN));                       // [N] where a row of the result goes
+    int64_t* row_at = reinterpret_cast<int64_t*>(from + (BOX ? 0 : 3 * kTN));                       // [N] the address that a row of the result goes to
     float* base_s = reinterpret_cast<float*>(row_at + N);                               // [N] what the weights' exponents are relative to
     float* top_s = base_s + N;                                                          // [N] maximum (scaled, base 2)
     float* factor_s = top_s + N;                                                        // [N]
@@ -152,13 +155,13 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
     volatile uint32_t* failed = tmem_slot + 1;
     volatile uint32_t* dirty = tmem_slot + 2;     // [2] by a piece's parity: number + 1 of the last one whose V holds infinities or NaN at drafted positions
     const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
-    const uint32_t full = smem_u32(bars), empty = full + 8 * slots, qfull = empty + 8 * slots, qempty = qfull + 16, sfull = qempty + 16, pfull = sfull + 16,
+    const uint32_t full = smem_u32(bars), empty = full + 8 * slots, v_full = full + 8 * k_slots, v_empty = empty + 8 * k_slots, qfull = empty + 8 * slots, qempty = qfull + 16, sfull = qempty + 16, pfull = sfull + 16,
                    ofull = pfull + 16, drain = ofull + 16;
     chain_next();
     if (tid == 0) {
-        for (int i = 0; i < slots; ++i) { mbar_init(full + 8 * i, BOX ? 1 : F::copy + F::copy / 32); mbar_init(empty + 8 * i, 1); }
+        for (int i = 0; i < slots; ++i) { mbar_init(full + 8 * i, BOX ? 2 : F::copy + F::copy / 32); mbar_init(empty + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(qfull + 8 * i, F::copy);
+            mbar_init(qfull + 8 * i, F::q_copy);
             mbar_init(qempty + 8 * i, 1);
             mbar_init(sfull + 8 * i, 1);
             mbar_init(pfull + 8 * i, soft_warps);
@@ -174,96 +177,100 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
     }
     const int tile_pos = BOX ? a.tile_pos : kTN;
     if (BOX && tile_pos < kTN) {                  // positions of a tile that no box fills: zeros once and for all
-        constexpr int row_pieces = F::blocks * 8;
-        for (int i = tid; i < slots * (kTN - tile_pos) * row_pieces; i += F::threads) {
-            const int s = i / ((kTN - tile_pos) * row_pieces), k = i % ((kTN - tile_pos) * row_pieces), r = tile_pos + k / row_pieces, c = k % row_pieces;
-            *reinterpret_cast<uint4*>(ring + s * F::slot + (c >> 3) * (kTN * 128) + r * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
-        }
+        for (int i = tid; i < slots * F::blocks * kTN * 8; i += F::threads)          // pieces of 16 bytes as they lie there, eight a position
+            if ((i >> 3) % kTN >= tile_pos) *reinterpret_cast<uint4*>(ring + i * 16) = make_uint4(0, 0, 0, 0);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     fence_before();
     Walk<N> w0{};
     const long long total = find_range<N, F::threads>(p, b, a, status, w0);
     fence_after();
-    const uint32_t tmem = *tmem_slot, ring_s = smem_u32(ring), q_s = smem_u32(qs), p_s = smem_u32(ps);
+    const uint32_t tmem = *tmem_slot, ring_s = smem_u32(ring), v_ring_s = ring_s + k_slots * F::slot, q_s = smem_u32(qs), p_s = smem_u32(ps);
 
     if (wid >= soft_warps && wid < qk_warp) {
         const int lt = tid - F::soft;
         constexpr int pieces = D / 8;                // 16-byte pieces of a vector
-        auto load_q = [&](const Tl& x, bool ok) -> bool {    // a piece's rows of Q
+        auto load_q = [&](const Tl& x, bool ok) -> bool {    // a piece's rows of Q; whole warps
             const int q = x.piece % F::q_bufs, rows = x.w.rows(a);
-            ok = ok && mbar_wait(qempty + 8 * q, ((uint32_t)(x.piece / F::q_bufs) & 1u) ^ 1u, failed, status);
+            ok = __all_sync(kFull, ok && mbar_wait(qempty + 8 * q, ((uint32_t)(x.piece / F::q_bufs) & 1u) ^ 1u, failed, status));
             if (!ok) return false;
-            for (int u = lt; u < N * pieces; u += F::copy) {
-                const int r = u / pieces, c = u % pieces, rr = x.w.rt * N + r, i = rr / a.group, g = rr - i * a.group;
-                const uint8_t* src = static_cast<const uint8_t*>(a.q);
-                if (r < rows) src += 2 * ((int64_t)(x.w.x.first + i) * a.qs_row + (int64_t)(x.w.h * a.group + g) * a.qs_head) + c * 16;
-                copy16(q_s + q * F::q_bytes + (c >> 3) * (N * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4), src, r < rows);
+            constexpr int halves = (N + 31) / 32;
+            unsigned long long row[halves];          // where a row stands, found by one lane
+#pragma unroll
+            for (int e = 0; e < halves; ++e) {
+                const int r = 32 * e + lane, rr = x.w.rt * N + r, i = rr / a.group;
+                row[e] = r < rows ? (unsigned long long)a.q + 2 * ((int64_t)(x.w.x.first + i) * a.qs_row + (int64_t)(x.w.h * a.group + rr - i * a.group) * a.qs_head) : 0ull;
+            }
+#pragma unroll 4
+            for (int u = lt; u < N * pieces; u += F::q_copy) {
+                const int r = u / pieces, c = u % pieces;
+                unsigned long long src = __shfl_sync(kFull, row[0], r & 31);
+                if (halves > 1) { const unsigned long long up = __shfl_sync(kFull, row[halves - 1], r & 31); src = r < 32 ? src : up; }
+                copy16(q_s + q * F::q_bytes + (c >> 3) * (N * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4), reinterpret_cast<const uint8_t*>(src ? src + c * 16 : (unsigned long long)a.q), src != 0);
             }
             mbar_arrive_copies(qfull + 8 * q);
             return true;
         };
         if constexpr (BOX) {
-            // ---- copies, one warp: a lane a box of the tile (box_pos positions of one page, 64 components wide)
-            Tl kx;
-            kx.start(w0, total);
-            int sl = 0, page = -1, slot = 0, head = 0, last_page = -1, last_slot = 0, last_head = 0;   // the lane's box of K's tile, and of the tile before
+            // ---- copies: two warps for the keys, two for the values; of the two each issues every other box of a tile (box_pos positions of one page,
+            // 64 components wide).  A lane looks a box's page up, a tile ahead.
+            const int half = (lt >> 5) & 1, kv = lt >> 6;
+            Tl x;
+            x.start(w0, total);
+            int page = -1, slot = 0, issued = 0;
             bool ok = true;
             const int my_box = 4 * lane / a.box_pos; // of the four positions whose validity the lane tells
-            auto look_up = [&]() {                   // issued a tile ahead of its use; -1: behind the last position
-                const int t = (kx.w.tile + kx.j) * tile_pos + lane * a.box_pos, pg = t / p.page_pos;
+            auto look_up = [&]() {                   // -1: behind the last position
+                const int t = (x.w.tile + x.j) * tile_pos + lane * a.box_pos, pg = t / p.page_pos;
                 slot = t - pg * p.page_pos;
-                page = lane < a.boxes && t < kx.w.x.kv ? b.table[(int64_t)kx.w.s * b.max_pages + pg] : -1;
-                if (page == -1 && lane < a.boxes && t < kx.w.x.kv) page = -2;
+                page = lane < a.boxes && t < x.w.x.kv ? b.table[(int64_t)x.w.s * b.max_pages + pg] : -1;
+                if (page == -1 && lane < a.boxes && t < x.w.x.kv) page = -2;
             };
-            auto fill = [&](int pg, int at, int h, int kv) {
-                const int s = sl % slots;
-                ok = __all_sync(kFull, ok && mbar_wait(empty + 8 * s, ((uint32_t)(sl / slots) & 1u) ^ 1u, failed, status));
-                ++sl;
-                if (!ok) return;
-                const bool have = pg >= 0 && pg < p.n_pages;
-                const int n = __popc(__ballot_sync(kFull, have));
-                if (lane == 0)
-                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(full + 8 * s), "r"(n * a.box_pos * F::blocks * 128) : "memory");
-                __syncwarp();
-                if (!have) return;
-                int at_dim[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) at_dim[i] = a.box_dim[i] == 0 ? at : a.box_dim[i] == 1 ? h : a.box_dim[i] == 2 ? pg : kv;
-#pragma unroll
-                for (int k = 0; k < F::blocks; ++k)
-                    asm volatile(
-                        "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(
-                            ring_s + s * F::slot + k * (kTN * 128) + lane * a.box_pos * 128),
-                        "l"(&map), "r"(k * 64), "r"(at_dim[0]), "r"(at_dim[1]), "r"(at_dim[2]), "r"(at_dim[3]), "r"(full + 8 * s)
-                        : "memory");
-            };
+            const int ring_slots = kv ? v_slots : k_slots;
+            const uint32_t my_full = kv ? v_full : full, my_empty = kv ? v_empty : empty, my_ring = kv ? v_ring_s : ring_s;
             if (total > 0) look_up();
-            for (long long x = 0; x <= total && ok; ++x) {
-                if (x < total) {
-                    if (kx.j == 0) ok = __all_sync(kFull, load_q(kx, ok));
+            for (int n = 0; x.more(); ++n) {
+                if (kv == 0 && x.j == 0) ok = load_q(x, ok);
+                const bool have = page >= 0 && page < p.n_pages;
+                const uint32_t boxes = __ballot_sync(kFull, have);
+                const int here = page, at = slot, h = x.w.h;
+                if (kv == 0 && half == 0) {
                     if (page < -1 || page >= p.n_pages) atomicOr(status, kStRange);
-                    const int box = __shfl_sync(kFull, page, my_box & 31), t = (kx.w.tile + kx.j) * tile_pos + 4 * lane;
-                    const bool there = box >= 0 && box < p.n_pages && 4 * lane < tile_pos;
-                    const int n = there ? min(max(kx.w.x.kv - t, 0), 4) : 0;
-                    const uint32_t word = __reduce_or_sync(0xffu << (lane & 24), ((1u << n) - 1u) << (4 * (lane & 7)));
-                    if ((lane & 7) == 0) words[x % kWords * 4 + (lane >> 3)] = word;
-                    head = kx.w.h;
-                    __syncwarp();
-                    fill(page, slot, head, 0);
+                    const int t = (x.w.tile + x.j) * tile_pos + 4 * lane;
+                    const int valid = boxes >> (my_box & 31) & 1u && 4 * lane < tile_pos ? min(max(x.w.x.kv - t, 0), 4) : 0;
+                    const uint32_t word = __reduce_or_sync(0xffu << (lane & 24), ((1u << valid) - 1u) << (4 * (lane & 7)));
+                    if ((lane & 7) == 0) words[n % kWords * 4 + (lane >> 3)] = word;
                 }
-                const int p1 = page, s1 = slot, h1 = head;
-                if (x + 1 < total) { kx.next(p, b, a); look_up(); }
-                if (x > 0) fill(last_page, last_slot, last_head, 1);         // V of a tile after K of the next
-                last_page = p1; last_slot = s1; last_head = h1;
+                x.next(p, b, a);
+                if (x.more()) look_up();
+                const int s = n % ring_slots;
+                ok = __all_sync(kFull, ok && mbar_wait(my_empty + 8 * s, ((uint32_t)(n / ring_slots) & 1u) ^ 1u, failed, status));
+                if (!ok) break;
+                const uint32_t mine = boxes & (half ? 0xaaaaaaaau : 0x55555555u), bar = my_full + 8 * s;
+                if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(__popc(mine) * a.box_pos * F::blocks * 128) : "memory");
+                for (int e = half; e < a.boxes; e += 2) {
+                    const int pg = __shfl_sync(kFull, here, e), sl = __shfl_sync(kFull, at, e);
+                    if (!(mine >> e & 1u) || lane != 0) continue;
+                    int c[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) c[k] = a.box_dim[k] == 0 ? sl : a.box_dim[k] == 1 ? h : a.box_dim[k] == 2 ? pg : kv;
+#pragma unroll
+                    for (int k = 0; k < F::blocks; ++k)
+                        asm volatile(
+                            "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(
+                                my_ring + s * F::slot + k * (kTN * 128) + e * a.box_pos * 128),
+                            "l"(&map), "r"(k * 64), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]), "r"(bar)
+                            : "memory");
+                }
+                issued = n + 1;
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
             if (!ok)                                 // boxes still in flight (none after a complete run) land before the CTA ends
-                for (int i = sl > slots ? sl - slots : 0; i < sl; ++i)
+                for (int n = issued > ring_slots ? issued - ring_slots : 0; n < issued; ++n)
                     for (uint32_t k = 0; k < kSpin; ++k) {
                         uint32_t done;
                         asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                                     : "=r"(done) : "r"(full + 8 * (i % slots)), "r"((uint32_t)(i / slots) & 1u) : "memory");
+                                     : "=r"(done) : "r"(my_full + 8 * (n % ring_slots)), "r"((uint32_t)(n / ring_slots) & 1u) : "memory");
                         if (done) break;
                     }
         } else {
@@ -274,17 +281,17 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
             Tl kx, vx;
             kx.start(w0, total);
             vx.start(w0, total);
-            int kt = 0, vt = 0, sl = 0;
+            int kt = 0, vt = 0;
             bool ok = true;
-            auto fill = [&](int tile, int64_t delta) {           // a tile's keys, or values (delta further on), into the next slot of the ring
-                const int s = sl % slots;
-                ok = __all_sync(kFull, ok && mbar_wait(empty + 8 * s, ((uint32_t)(sl / slots) & 1u) ^ 1u, failed, status));
-                ++sl;
+            auto fill = [&](int tile, bool values) {           // a tile's keys or values into the next slot of their ring
+                const int s = tile % (values ? v_slots : k_slots);
+                const uint32_t ph = (uint32_t)(tile / (values ? v_slots : k_slots)) & 1u, bar = (values ? v_full : full) + 8 * s;
+                ok = __all_sync(kFull, ok && mbar_wait((values ? v_empty : empty) + 8 * s, ph ^ 1u, failed, status));
                 if (!ok) return;
-                const uint32_t dst = ring_s + s * F::slot + to;
+                const uint32_t dst = (values ? v_ring_s : ring_s) + s * F::slot + to;
+                const int64_t delta = (values ? p.skv : 0) + c * 16;
                 const uint64_t* src = from + tile % 3 * kTN + r0;
                 const uint32_t* valid = words + tile % kWords * 4;
-                delta += c * 16;
                 const bool all = (valid[0] & valid[1] & valid[2] & valid[3]) == ~0u;
 #pragma unroll
                 for (int k0 = 0; k0 < rounds; k0 += 8) {
@@ -303,9 +310,9 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
                         }
                     }
                 }
-                mbar_arrive_copies(full + 8 * s);
+                mbar_arrive_copies(bar);
                 __syncwarp();
-                if (lane == 0) mbar_arrive(full + 8 * s);                        // the validity words, too, are there
+                if (lane == 0) mbar_arrive(bar);                        // the validity words, too, are there
             };
             int slot_in = 0, page = -1;                  // this thread's position of K's next tile: slot in its page, the page
             auto look_up = [&]() {                       // issued a tile ahead of its use
@@ -330,13 +337,13 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
                 }
                 if (!vote_all<1, F::copy>(ok)) break;
                 if (more) {
-                    fill(kt, 0);
+                    fill(kt, false);
                     ++kt;
                     kx.next(p, b, a);
                     if (kx.more()) look_up();
                 }
                 if (kt > 1 || !more) {                                           // V of a tile after K of the next
-                    fill(vt, p.skv);
+                    fill(vt, true);
                     ++vt;
                     vx.next(p, b, a);
                 }
@@ -345,39 +352,39 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
         }
     } else if (wid >= qk_warp) {
         if (lane == 0) {
-            // ---- products, a thread for each of the two.  The ring holds K(0), then K(x + 1), V(x) for every tile x.
+            // ---- products, a thread for each of the two
             constexpr uint32_t id_qk = (1u << 4) | (Kind<T>::format << 7) | (Kind<T>::format << 10) | (8u << 24) | ((uint32_t)(N >> 3) << 17), id_pv = id_qk | (3u << 15);
             Tl tl;
             tl.start(w0, total);
             bool ok = true;
-            auto ready = [&](int i) {
-                ok = ok && mbar_wait(full + 8 * (i % slots), (uint32_t)(i / slots) & 1u, failed, status);
+            auto ready = [&](uint32_t bar, uint32_t phase) {
+                ok = ok && mbar_wait(bar, phase & 1u, failed, status);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 fence_after();
             };
             if (wid == qk_warp) {
                 for (int x = 0; tl.more(); ++x, tl.next(p, b, a)) {
-                    const int q = tl.piece % F::q_bufs, i = x ? 2 * x - 1 : 0;
+                    const int q = tl.piece % F::q_bufs, i = x % k_slots;
                     if (tl.j == 0) ok = ok && mbar_wait(qfull + 8 * q, (uint32_t)(tl.piece / F::q_bufs) & 1u, failed, status);
                     if (x >= 2) ok = ok && mbar_wait(pfull + 8 * (x & 1), (uint32_t)((x - 2) >> 1) & 1u, failed, status);   // S has been read
-                    ready(i);
+                    ready(full + 8 * i, (uint32_t)(x / k_slots));
                     if (!ok) break;
-                    const uint64_t k_at = desc_k(ring_s + i % slots * F::slot), q_at = desc_k(q_s + q * F::q_bytes);
+                    const uint64_t k_at = desc_k(ring_s + i * F::slot), q_at = desc_k(q_s + q * F::q_bytes);
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k)
                         mma_ss(tmem + (x & 1) * N, k_at + (k >> 2) * (kTN * 128 / 16) + 2 * (k & 3), q_at + (k >> 2) * (N * 128 / 16) + 2 * (k & 3), id_qk, k ? 1u : 0u);
                     mma_commit(sfull + 8 * (x & 1));
-                    mma_commit(empty + 8 * (i % slots));
+                    mma_commit(empty + 8 * i);
                     if (tl.last()) mma_commit(qempty + 8 * q);
                 }
             } else {
                 for (int x = 0; tl.more(); ++x, tl.next(p, b, a)) {
-                    const int i = x + 1 < total ? 2 * x + 2 : 2 * x + 1;
+                    const int i = x % v_slots;
                     ok = ok && mbar_wait(pfull + 8 * (x & 1), (uint32_t)(x >> 1) & 1u, failed, status);
-                    ready(i);
+                    ready(v_full + 8 * i, (uint32_t)(x / v_slots));
                     if (!ok) break;
                     // lanes past the components of a vector take the first block again
-                    const uint64_t v_at = desc_mn(ring_s + i % slots * F::slot, D >= 128 ? kTN * 128 : 0), p_at = desc_p(p_s + x % F::p_bufs * F::p_bytes);
+                    const uint64_t v_at = desc_mn(v_ring_s + i * F::slot, D >= 128 ? kTN * 128 : 0), p_at = desc_p(p_s + x % F::p_bufs * F::p_bytes);
                     const uint32_t o_to = tmem + 2 * N + (tl.piece & 1) * F::o_blocks * N;
 #pragma unroll
                     for (int o = 0; o < F::o_blocks; ++o)
@@ -385,7 +392,7 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
                         for (int k = 0; k < kTN / 16; ++k)
                             mma_ss(o_to + o * N, v_at + (o * 2 * kTN * 128 + k * 2048) / 16, p_at + k * 16, id_pv, tl.j | k ? 1u : 0u);
                     mma_commit(ofull + 8 * (x & 1));
-                    mma_commit(empty + 8 * (i % slots));
+                    mma_commit(v_empty + 8 * i);
                 }
             }
             const uint32_t mine = drain + 8 * (wid - qk_warp);
@@ -416,7 +423,7 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
                 const float l = (sum_s[tid] + sum_s[N + tid]) + (sum_s[2 * N + tid] + sum_s[3 * N + tid]), top = last_top_s[tid];
                 const int rr = row0 + tid, i = rr / a.group;
                 const int64_t n_row = f.w.x.first + i, head = (int64_t)f.w.h * a.group + (rr - i * a.group);
-                row_at[tid] = n_row * a.os_row + head * a.os_head;
+                row_at[tid] = whole ? reinterpret_cast<int64_t>(a.out) + 2 * (n_row * a.os_row + head * a.os_head) : reinterpret_cast<int64_t>(a.part_o + (slot + tid) * D);
                 inv_s[tid] = l == 0.f ? 0.f : whole ? 1.f / l : 1.f;             // 0: nothing was seen
                 if (!whole) a.part_ml[slot + tid] = make_float2(top, l);
                 else if (a.lse) a.lse[n_row * a.heads + head] = l == 0.f ? -INFINITY : (top - Kind<T>::shift + log2f(l)) * 0.693147180559945f;
@@ -435,18 +442,20 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
                 for (int r = 0; r < 16; ++r)
                     if (r0 + r < rows) {
                         const float g = inv_s[r0 + r], v = g == 0.f ? 0.f : __uint_as_float(y[r]) * g;
-                        if (whole) static_cast<uint16_t*>(a.out)[row_at[r0 + r] + d] = (uint16_t)(Kind<T>::pack(v, 0.f) & 0xffffu);
-                        else a.part_o[(slot + r0 + r) * D + d] = v;
+                        const int64_t to = row_at[r0 + r];
+                        if (whole) reinterpret_cast<uint16_t*>(to)[d] = (uint16_t)(Kind<T>::pack(v, 0.f) & 0xffffu);
+                        else reinterpret_cast<float*>(to)[d] = v;
                     }
             }
             if (dirty[f.piece & 1] == (uint32_t)f.piece + 1u && vote_all<2, F::soft>(true))       // every group's rows are written
                 for (int d = tid; d < D; d += F::soft)
-                    put_back<T>(p, b, a, f.w.x, f.w.s, f.w.h, f.w.tile * tile_pos, (f.w.tile + f.m) * tile_pos, row0, rows, d, row_at, whole ? nullptr : a.part_o + slot * D + d);
+                    put_back<T>(p, b, a, f.w.x, f.w.s, f.w.h, f.w.tile * tile_pos, (f.w.tile + f.m) * tile_pos, row0, rows, d, row_at, whole);
             fence_before();
             return true;
         };
         for (int x = 0; sx.more(); ++x, sx.next(p, b, a)) {
             const int t0 = (sx.w.tile + sx.j) * tile_pos;
+            const int in_use = (sx.w.rows(a) - col0 + 3) & ~3;   // of the group's rows, in fours; the others' weights may be anything
             const bool first = sx.j == 0, drafted = t0 + tile_pos > sx.w.x.len;
             ok = ok && mbar_wait(sfull + 8 * (x & 1), (uint32_t)(x >> 1) & 1u, failed, status);
             if (x >= F::p_bufs) ok = ok && mbar_wait(ofull + 8 * ((x - F::p_bufs) & 1), (uint32_t)((x - F::p_bufs) >> 1) & 1u, failed, status);
@@ -483,6 +492,7 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
             if (!first) {
 #pragma unroll
                 for (int r = 0; r < C; r += 4) {
+                    if (r >= in_use) break;
                     if (C > 16 && (r & 15) == 0) scores(r >> 4);
                     float e[4];
                     exponents(r, e);
@@ -493,6 +503,7 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
                 // some row's maximum rises: all warps' maxima, the factors, and what has been summed so far
 #pragma unroll
                 for (int r = 0; r < C; ++r) {
+                    if (r >= in_use) break;
                     if (C > 16 && (r & 15) == 0) scores(r >> 4);
                     const float m = warp_max(__uint_as_float(s[r & 15]));
                     if (lane == r) warp_s[quarter * N + col0 + r] = m;
@@ -538,10 +549,12 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
             uint8_t* pp = ps + x % F::p_bufs * F::p_bytes + col0 / 8 * 2048 + pos * 16;
 #pragma unroll
             for (int r = 0; r < C; r += 8) {
+                if (r >= in_use) break;
                 if (C > 16 && (r & 15) == 0) scores(r >> 4);
-                uint32_t y[4];
+                uint32_t y[4] = {0, 0, 0, 0};
 #pragma unroll
                 for (int k = 0; k < 8; k += 4) {
+                    if (r + k >= in_use) break;
                     float e[4];
                     exponents(r + k, e);
 #pragma unroll
@@ -556,9 +569,8 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
             // V of positions that do not exist is whatever the boxes brought or left: zeros instead, since weights of 0 do not hide it
             const bool blank = BOX && masked && pos < tile_pos && !(words[x % kWords * 4 + quarter] >> lane & 1u);
             if ((hide || (BOX && masked)) && wid < 4) {
-                const int sl = x + 1 < total ? 2 * x + 2 : 2 * x + 1;       // V's place in the order of the ring
-                ok = ok && mbar_wait(full + 8 * (sl % slots), (uint32_t)(sl / slots) & 1u, failed, status);
-                uint8_t* tile = ring + sl % slots * F::slot;
+                ok = ok && mbar_wait(v_full + 8 * (x % v_slots), (uint32_t)(x / v_slots) & 1u, failed, status);
+                uint8_t* tile = ring + (k_slots + x % v_slots) * F::slot;
                 if (ok && blank)
                     for (int e = 0; e < F::blocks * 8; ++e)
                         *reinterpret_cast<uint4*>(tile + (e >> 3) * (kTN * 128) + pos * 128 + (((e & 7) ^ (pos & 7)) << 4)) = make_uint4(0, 0, 0, 0);
