@@ -6,9 +6,8 @@ of the tensors' device.  Results and workspaces are allocated by torch on that s
 and captured graphs do not share any.
 """
 import ctypes as C
-import math
 
-from . import E_ALIGN, E_CAPACITY, E_CUDA, E_INVALID, E_SHAPE, OUT_BF16, OUT_F16, OUT_F32, KVView, PlcError, _check, _ptr, lib
+from . import E_ALIGN, E_CAPACITY, E_CUDA, E_INVALID, E_SHAPE, OUT_BF16, OUT_F16, OUT_F32, KVView, PlcError, _check, lib
 
 
 class PagePoolC(C.Structure):
@@ -35,38 +34,70 @@ def _need(ok, code, where):
         raise PlcError(code, where)
 
 
-def _dtype(t, where, wide=True):
-    import torch
-    kinds = {torch.float16: OUT_F16, torch.bfloat16: OUT_BF16}
-    if wide:
-        kinds[torch.float32] = OUT_F32
-    _need(t.dtype in kinds, E_INVALID, where)
-    return kinds[t.dtype]
+_api = None
 
 
-def _i32(t, shape, device, where):
-    """t as what the library reads: int32, contiguous, on the device, of the shape (None: any extent)."""
+def _lib():
+    """The library with the argument types of this module's calls set, so that plain integers can be passed."""
+    global _api
+    if _api is None:
+        api, P, I, L, F = lib(), C.c_void_p, C.c_int32, C.c_int64, C.c_float
+        U = C.c_uint64
+        for name, types in (("plc_pages_fork", [P, P, P, P, P, P, U, P, P]), ("plc_pages_keep", [P, P, P, P, I, P, P, P]),
+                            ("plc_pages_compact", [P, P, P, P, P, U, P, P]), ("plc_pages_workspace", [I, I, I, P]),
+                            ("plc_tree_attention", [P, I, P, P, F, P, U, P, P]), ("plc_tree_attention_workspace", [P, I, I, I, P]),
+                            ("plc_beam_select", [P, I, L, I, I, I, P, P, I, I, P, P, P, P, U, P]), ("plc_beam_workspace", [I, I, I, I, P]),
+                            ("plc_beam_reorder", [P, I, P, I, I, P, P])):
+            getattr(api, name).argtypes = types
+        _api = api
+    return _api
+
+
+_KINDS = {}
+
+
+def _kind(dtype, where, wide=True):
     import torch
-    _need(t.dtype == torch.int32 and t.device == device and t.is_contiguous(), E_INVALID, where)
-    _need(t.dim() == len(shape) and all(w is None or n == w for n, w in zip(t.shape, shape)), E_SHAPE, where)
+    if not _KINDS:
+        _KINDS.update({torch.float16: OUT_F16, torch.bfloat16: OUT_BF16, torch.float32: OUT_F32})
+    kind = _KINDS.get(dtype)
+    _need(kind is not None and (wide or kind != OUT_F32), E_INVALID, where)
+    return kind
+
+
+def _i32(t, device, where):
+    """t as what the library reads: int32, contiguous, on the device."""
+    import torch
+    if t.dtype != torch.int32 or t.device != device or not t.is_contiguous():
+        raise PlcError(E_INVALID, where)
     return t
 
 
-class _On:
-    """The device of a call: made current for it, with its current stream."""
+def _run(device, call, *args):
+    """The call on the current stream of the tensors' device, with that device current."""
+    import torch
+    if torch.cuda.current_device() == device.index:
+        return call(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    with torch.cuda.device(device):
+        return call(*args, torch._C._cuda_getCurrentRawStream(device.index))
 
-    def __init__(self, device):
-        import torch
-        self.guard = torch.cuda.device(device)
-        self.device = device
 
-    def __enter__(self):
-        import torch
-        self.guard.__enter__()
-        return C.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
+_sizes = {}
 
-    def __exit__(self, *e):
-        return self.guard.__exit__(*e)
+
+def _bytes(device, call, *args):
+    """A workspace size, asked for once a device (it may go by the device's size)."""
+    import torch
+    key = (device.index, call.__name__) + args
+    n = _sizes.get(key)
+    if n is None:
+        b = C.c_uint64()
+        with torch.cuda.device(device):
+            _check(call(*args, C.byref(b)), call.__name__)
+        if len(_sizes) >= 4096:
+            _sizes.clear()
+        n = _sizes[key] = b.value
+    return n
 
 
 class PageBook:
@@ -75,13 +106,49 @@ class PageBook:
 
     def __init__(self, table, len, ref):
         dev = table.device
-        _i32(table, (None, None), dev, "PageBook.table")
-        _i32(len, (table.shape[0],), dev, "PageBook.len")
-        _i32(ref, (None,), dev, "PageBook.ref")
-        self.table, self.len, self.ref = table, len, ref
+        for t, n, dim in ((table, "table", 2), (len, "len", 1), (ref, "ref", 1)):
+            _i32(t, dev, "PageBook." + n)
+            _need(t.dim() == dim, E_SHAPE, "PageBook." + n)
+        _need(len.shape[0] == table.shape[0], E_SHAPE, "PageBook.len")
+        self._parts = (table, len, ref)
+        self.rows, self.max_pages = table.shape
+        self.n_pages, self.device = ref.shape[0], dev
+        self._c = PageBookC(table.data_ptr(), len.data_ptr(), ref.data_ptr(), self.rows, self.max_pages)
+        self._by = C.byref(self._c)
 
-    def c(self):
-        return PageBookC(self.table.data_ptr(), self.len.data_ptr(), self.ref.data_ptr(), self.table.shape[0], self.table.shape[1])
+    @classmethod
+    def _new(cls, rows, max_pages, n_pages, device, extra=0):
+        """A book that a call fills, in one allocation; (book, address of `extra` bytes behind it)."""
+        import torch
+        self = cls.__new__(cls)
+        n = rows * max_pages
+        words = (n + rows + n_pages + 3) & ~3
+        self._store = torch.empty(words + (extra + 3) // 4, dtype=torch.int32, device=device)
+        at = self._store.data_ptr()
+        self._parts = None
+        self.rows, self.max_pages, self.n_pages, self.device = rows, max_pages, n_pages, device
+        self._c = PageBookC(at, at + 4 * n, at + 4 * (n + rows), rows, max_pages)
+        self._by = C.byref(self._c)
+        return self, at + 4 * words
+
+    def _views(self):
+        if self._parts is None:
+            n, s = self.rows * self.max_pages, self._store
+            self._parts = (s.as_strided((self.rows, self.max_pages), (self.max_pages, 1), 0), s.as_strided((self.rows,), (1,), n),
+                           s.as_strided((self.n_pages,), (1,), n + self.rows))
+        return self._parts
+
+    @property
+    def table(self):
+        return self._views()[0]
+
+    @property
+    def len(self):
+        return self._views()[1]
+
+    @property
+    def ref(self):
+        return self._views()[2]
 
 
 class PagePool:
@@ -92,18 +159,21 @@ class PagePool:
         import torch
         _need(kv.dim() == 6 and kv.shape[1] == 2 and kv.stride(5) == 1, E_SHAPE, "PagePool")
         _need(kv.is_cuda, E_INVALID, "PagePool")
-        self.kv = kv
+        self.kv, self.device, self.n_pages = kv, kv.device, kv.shape[2]
         s = kv.stride()
         L, _, P, H, page, d = kv.shape
-        self._c = PagePoolC(KVView(kv.data_ptr(), s[0], s[1], s[2], s[3], s[4]), L, H, d, P, page, _dtype(kv, "PagePool"))
+        self._c = PagePoolC(KVView(kv.data_ptr(), s[0], s[1], s[2], s[3], s[4]), L, H, d, P, page, _kind(kv.dtype, "PagePool"))
+        self._by = C.byref(self._c)
         self.status = torch.zeros(1, dtype=torch.int32, device=kv.device)
+        self._word = self.status.data_ptr()
+        self._need_bytes = {}
 
     def new_book(self, rows, max_pages):
         """A book of empty rows over a pool whose pages are all free."""
         import torch
-        dev = self.kv.device
+        dev = self.device
         return PageBook(torch.full((rows, max_pages), -1, dtype=torch.int32, device=dev), torch.zeros(rows, dtype=torch.int32, device=dev),
-                        torch.zeros(self.kv.shape[2], dtype=torch.int32, device=dev))
+                        torch.zeros(self.n_pages, dtype=torch.int32, device=dev))
 
     def sessions_view(self, first_page, sessions, n):
         """KVView of consecutive pages as plain sessions of n positions, for Context.encode / Context.decode: session i
@@ -117,62 +187,43 @@ class PagePool:
                       each * v.stride_session, v.stride_head, v.stride_pos)
 
     def _book(self, book, where):
-        _need(book.table.device == self.kv.device, E_INVALID, where)
-        _need(book.ref.shape[0] == self.kv.shape[2], E_SHAPE, where)
-        return book.c()
-
-    def _new(self, book, rows):
-        import torch
-        return PageBook(torch.empty(rows, book.table.shape[1], dtype=torch.int32, device=self.kv.device),
-                        torch.empty(rows, dtype=torch.int32, device=self.kv.device), torch.empty_like(book.ref))
-
-    def _workspace(self, book, rows):
-        import torch
-        b = C.c_uint64()
-        _check(lib().plc_pages_workspace(self.kv.shape[2], book.table.shape[0], rows, C.byref(b)), "plc_pages_workspace")
-        return torch.empty(b.value, dtype=torch.uint8, device=self.kv.device)
+        _need(book.device == self.device, E_INVALID, where)
+        _need(book.n_pages == self.n_pages, E_SHAPE, where)
+        return book._by
 
     def fork(self, book, parent, room=None):
         """New book whose row s continues row parent[s] (-1: empty), with pages for room[s] positions more."""
-        import torch
-        where, dev = "plc_pages_fork", self.kv.device
+        where, dev, api = "plc_pages_fork", self.device, _lib()
         a = self._book(book, where)
-        rows = _i32(parent.reshape(-1), (None,), dev, where).shape[0]
+        rows = _i32(parent, dev, where).numel()
         _need(rows >= 1, E_INVALID, where)
         if room is not None:
-            _i32(room, (rows,), dev, where)
-        with _On(dev) as st:
-            new = self._new(book, rows)
-            ws, b = self._workspace(book, rows), new.c()
-            _check(lib().plc_pages_fork(C.byref(self._c), C.byref(a), _ptr(parent), _ptr(room), C.byref(b), _ptr(ws),
-                                        C.c_uint64(ws.numel()), _ptr(self.status), st), where)
+            _need(_i32(room, dev, where).numel() == rows, E_SHAPE, where)
+        need = _bytes(dev, api.plc_pages_workspace, self.n_pages, book.rows, rows)
+        new, ws = PageBook._new(rows, book.max_pages, self.n_pages, dev, need)
+        _check(_run(dev, api.plc_pages_fork, self._by, a, parent.data_ptr(), None if room is None else room.data_ptr(), new._by, ws, need, self._word), where)
         return new
 
     def keep(self, book, path, n_path):
         """New book after the drafted positions path[s][:n_path[s]] of every row have been accepted."""
-        where, dev = "plc_pages_keep", self.kv.device
+        where, dev, api = "plc_pages_keep", self.device, _lib()
         a = self._book(book, where)
-        rows = book.table.shape[0]
-        _i32(path, (rows, None), dev, where)
-        _i32(n_path, (rows,), dev, where)
-        with _On(dev) as st:
-            new = self._new(book, rows)
-            b = new.c()
-            _check(lib().plc_pages_keep(C.byref(self._c), C.byref(a), _ptr(path), _ptr(n_path), path.shape[1], C.byref(b),
-                                        _ptr(self.status), st), where)
+        _i32(path, dev, where)
+        _i32(n_path, dev, where)
+        _need(path.dim() == 2 and path.shape[0] == book.rows == n_path.numel(), E_SHAPE, where)
+        new, _ = PageBook._new(book.rows, book.max_pages, self.n_pages, dev)
+        _check(_run(dev, api.plc_pages_keep, self._by, a, path.data_ptr(), n_path.data_ptr(), path.shape[1], new._by, self._word), where)
         return new
 
     def compact(self, book):
         """(new book, moved): the pages in use have the lowest numbers; moved[p] is page p's new number (-1: free)."""
         import torch
-        where = "plc_pages_compact"
+        where, dev, api = "plc_pages_compact", self.device, _lib()
         a = self._book(book, where)
-        with _On(self.kv.device) as st:
-            new = self._new(book, book.table.shape[0])
-            moved = torch.empty_like(book.ref)
-            ws, b = self._workspace(book, book.table.shape[0]), new.c()
-            _check(lib().plc_pages_compact(C.byref(self._c), C.byref(a), C.byref(b), _ptr(moved), _ptr(ws), C.c_uint64(ws.numel()),
-                                           _ptr(self.status), st), where)
+        need = _bytes(dev, api.plc_pages_workspace, self.n_pages, book.rows, book.rows)
+        new, ws = PageBook._new(book.rows, book.max_pages, self.n_pages, dev, need)
+        moved = torch.empty(self.n_pages, dtype=torch.int32, device=dev)
+        _check(_run(dev, api.plc_pages_compact, self._by, a, new._by, moved.data_ptr(), ws, need, self._word), where)
         return new, moved
 
     def tree_attention(self, layer, book, q, begin, mask=None, scale=None, out=None, lse=None):
@@ -180,32 +231,42 @@ class PagePool:
         values stand behind its length.  mask [N][words] int32: bit j of row i = drafted position j is seen (None: j <= i).
         scale: 1 / sqrt(d) if not given.  out, lse: written where given."""
         import torch
-        where, dev = "plc_tree_attention", self.kv.device
+        where, dev, api = "plc_tree_attention", self.device, _lib()
         a = self._book(book, where)
-        _need(q.dim() == 3 and q.shape[2] == self.kv.shape[5], E_SHAPE, where)
-        _need(q.device == dev and q.dtype == self.kv.dtype and q.stride(2) == 1, E_INVALID, where)
-        _dtype(q, where, wide=False)
-        N, heads, d = q.shape
-        _i32(begin, (book.table.shape[0] + 1,), dev, where)
-        words = 0
+        _need(q.dim() == 3, E_SHAPE, where)
+        (N, heads, d), (row, head, one) = q.shape, q.stride()
+        _need(d == self._c.head_dim, E_SHAPE, where)
+        _need(q.device == dev and q.dtype == self.kv.dtype and one == 1, E_INVALID, where)
+        _kind(q.dtype, where, wide=False)
+        _need(_i32(begin, dev, where).numel() == book.rows + 1, E_SHAPE, where)
+        words, bits = 0, None
         if mask is not None:
-            words = _i32(mask, (N, None), dev, where).shape[1]
-        with _On(dev) as st:
-            if out is None:
-                out = torch.empty(N, heads, d, dtype=q.dtype, device=dev)
+            _i32(mask, dev, where)
+            _need(mask.dim() == 2 and mask.shape[0] == N, E_SHAPE, where)
+            words, bits = mask.shape[1], mask.data_ptr()
+        if out is None:
+            out = torch.empty((N, heads, d), dtype=q.dtype, device=dev)
+            out_row, out_head = heads * d, d
+        else:
             _need(out.shape == q.shape and out.dtype == q.dtype and out.device == dev and out.stride(2) == 1, E_INVALID, where)
-            if lse is None:
-                lse = torch.empty(N, heads, dtype=torch.float32, device=dev)
+            out_row, out_head, _ = out.stride()
+        if lse is None:
+            lse = torch.empty((N, heads), dtype=torch.float32, device=dev)
+        else:
             _need(lse.shape == (N, heads) and lse.dtype == torch.float32 and lse.device == dev and lse.is_contiguous(), E_INVALID, where)
-            if N == 0:
-                return out, lse
+        if N == 0:
+            return out, lse
+        need = self._need_bytes.get((book.rows, heads, N))
+        if need is None:
             b = C.c_uint64()
-            _check(lib().plc_tree_attention_workspace(C.byref(self._c), book.table.shape[0], heads, N, C.byref(b)), "plc_tree_attention_workspace")
-            ws = torch.empty(b.value, dtype=torch.uint8, device=dev)
-            t = TreeQueries(q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr(),
-                            begin.data_ptr(), None if mask is None else mask.data_ptr(), N, heads, words)
-            _check(lib().plc_tree_attention(C.byref(self._c), int(layer), C.byref(a), C.byref(t), C.c_float(1 / math.sqrt(d) if scale is None else scale),
-                                            _ptr(ws), C.c_uint64(ws.numel()), _ptr(self.status), st), where)
+            with torch.cuda.device(dev):
+                _check(api.plc_tree_attention_workspace(self._by, book.rows, heads, N, C.byref(b)), "plc_tree_attention_workspace")
+            if len(self._need_bytes) >= 4096:
+                self._need_bytes.clear()
+            need = self._need_bytes[(book.rows, heads, N)] = b.value
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        t = TreeQueries(q.data_ptr(), row, head, out.data_ptr(), out_row, out_head, lse.data_ptr(), begin.data_ptr(), bits, N, heads, words)
+        _check(_run(dev, api.plc_tree_attention, self._by, layer, a, C.byref(t), d ** -0.5 if scale is None else scale, ws.data_ptr(), need, self._word), where)
         return out, lse
 
     def check(self):
@@ -221,22 +282,23 @@ def beam_select(logits, score, n_out, done=None, eos=-1):
     [sessions][beams][vocab], score [sessions][beams] float32, done [sessions][beams] bool.  parent counts the rows of all
     sessions (-1, with token -1 and score -inf: no continuation)."""
     import torch
-    where, dev = "plc_beam_select", logits.device
-    _need(logits.is_cuda and logits.dim() == 3 and logits.stride(2) == 1, E_INVALID, where)
-    S, W, V = logits.shape
-    _need(S < 2 or logits.stride(0) == W * logits.stride(1), E_SHAPE, where)
+    where, dev, api = "plc_beam_select", logits.device, _lib()
+    _need(logits.is_cuda and logits.dim() == 3, E_INVALID, where)
+    (S, W, V), (session, row, one) = logits.shape, logits.stride()
+    _need(one == 1, E_INVALID, where)
+    _need(S < 2 or W < 2 or session == W * row, E_SHAPE, where)
+    if W < 2:
+        row = session
     _need(score.dtype == torch.float32 and score.device == dev and score.is_contiguous() and score.shape == (S, W), E_INVALID, where)
     if done is not None:
         _need(done.dtype == torch.bool and done.device == dev and done.is_contiguous() and done.shape == (S, W), E_INVALID, where)
-    kind = _dtype(logits, where)
-    b = C.c_uint64()
-    _check(lib().plc_beam_workspace(S, W, V, int(n_out), C.byref(b)), "plc_beam_workspace")
-    with _On(dev) as st:
-        ws = torch.empty(b.value, dtype=torch.uint8, device=dev)
-        out = torch.empty(S, n_out, dtype=torch.float32, device=dev)
-        parent, token = (torch.empty(S, n_out, dtype=torch.int32, device=dev) for _ in range(2))
-        _check(lib().plc_beam_select(_ptr(logits), kind, C.c_int64(logits.stride(1) if S * W > 1 else V), S, W, V, _ptr(score), _ptr(done), int(eos), int(n_out),
-                                     _ptr(out), _ptr(parent), _ptr(token), _ptr(ws), C.c_uint64(ws.numel()), st), where)
+    kind = _kind(logits.dtype, where)
+    need = _bytes(dev, api.plc_beam_workspace, S, W, V, n_out)
+    ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    out = torch.empty((S, n_out), dtype=torch.float32, device=dev)
+    parent, token = torch.empty((2, S, n_out), dtype=torch.int32, device=dev).unbind(0)
+    _check(_run(dev, api.plc_beam_select, logits.data_ptr(), kind, row, S, W, V, score.data_ptr(), None if done is None else done.data_ptr(), eos, n_out,
+                out.data_ptr(), parent.data_ptr(), token.data_ptr(), ws.data_ptr(), need), where)
     return out, parent, token
 
 
@@ -244,20 +306,21 @@ def beam_reorder(parent, states, status=None):
     """New tensors whose row r is row parent[r] of each of `states` (zeros for -1): state tensors that follow their beams,
     indexed by the row first, the rest of a row contiguous.  status: int32 word that receives 32 for a parent out of range."""
     import torch
-    where, dev = "plc_beam_reorder", parent.device
-    _need(parent.is_cuda and parent.dtype == torch.int32 and parent.is_contiguous() and parent.numel() > 0, E_INVALID, where)
-    rows = parent.numel()
-    _need(len(states) > 0, E_INVALID, where)
+    where, dev, api = "plc_beam_reorder", parent.device, _lib()
+    _need(parent.is_cuda and len(states) > 0, E_INVALID, where)
+    rows, rows_in = _i32(parent, dev, where).numel(), states[0].shape[0] if states[0].dim() else 0
+    _need(rows > 0 and rows_in > 0, E_INVALID, where)
+    word = None if status is None else _i32(status, dev, where).data_ptr()
+    out, sets = [], []
     for t in states:
-        _need(t.device == dev and t.dim() >= 1 and t.shape[0] == states[0].shape[0] and (t.shape[0] == 0 or t[0].is_contiguous()), E_INVALID, where)
-    with _On(dev) as st:
-        out = [torch.empty((rows,) + tuple(t.shape[1:]), dtype=t.dtype, device=dev) for t in states]
-        todo = [(t, o) for t, o in zip(states, out) if o.numel()]
-        if status is not None:
-            _i32(status, (1,), dev, where)
-        for i in range(0, len(todo), 16):
-            some = todo[i:i + 16]
-            sets = (RowSet * len(some))(*[RowSet(t.data_ptr(), o.data_ptr(), t.stride(0) * t.element_size(), o.stride(0) * o.element_size(),
-                                                 o[0].numel() * o.element_size()) for t, o in some])
-            _check(lib().plc_beam_reorder(sets, len(some), _ptr(parent), states[0].shape[0], rows, _ptr(status), st), where)
+        _need(t.device == dev and t.dim() >= 1 and t.shape[0] == rows_in and (t.is_contiguous() or t[0].is_contiguous()), E_INVALID, where)
+        o = torch.empty((rows,) + t.shape[1:], dtype=t.dtype, device=dev)
+        out.append(o)
+        size = t.element_size()
+        row = t.numel() // rows_in * size
+        if row:
+            sets.append(RowSet(t.data_ptr(), o.data_ptr(), t.stride(0) * size, row, row))
+    for i in range(0, len(sets), 16):
+        some = sets[i:i + 16]
+        _check(_run(dev, api.plc_beam_reorder, (RowSet * len(some))(*some), len(some), parent.data_ptr(), rows_in, rows, word), where)
     return out
