@@ -6,7 +6,7 @@
 // sorted lists by score.  HBM bound: each logit is read once.
 //
 // Exactness: continuations of different rows are compared by score + x - lse in binary64.  Exponentials are binary32 (x - maximum
-// is subtracted before it is scaled, so that the largest terms, which carry the sum, have the smallest errors); groups of eight are added in
+// is subtracted before it is scaled, so that the largest terms, which carry the sum, have the smallest errors); 32 of them are added in
 // binary32 and the groups in binary64, in an order that depends on the column alone and not on the row's alignment:
 // equal rows have equal sums, so that their ties go to the lower row.
 #include <cuda_bf16.h>
@@ -19,7 +19,8 @@ namespace {
 
 constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
 constexpr int kMostOut = 128;                     // n_out, beams
-constexpr int kBuffer = 512;                      // a warp's candidates: cut to n_out when a step of 256 more might not fit
+constexpr int kBuffer = 512;                     // a warp's candidates where lists are long: cut to n_out when a step of 256 more might not fit
+constexpr int kPending = 31 + 256;                // and where they have at most 32 entries: those not yet merged into the list
 constexpr int kMostListed = 16384;                // entries of a session's lists (the merge holds them in shared memory)
 
 struct SelectArgs {
@@ -39,122 +40,291 @@ __device__ __forceinline__ uint32_t order_bits(float x) {
 }
 __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o); }
 
-template <class T> struct Octet;                  // eight logits
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float kLog2e = 1.44269504088896f;
+
+// Eight logits as they stand in memory; -inf behind the n-th.
+template <class T> struct Octet;
 template <> struct Octet<float> {
-    static __device__ __forceinline__ void load(const float* p, bool vec, int n, float* x) {
-        if (vec && n >= 8) {
-            const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-            x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = i < n ? p[i] : -INFINITY;
+    uint4 a, b;
+    __device__ __forceinline__ void load(const float* p, bool vec, int n) {
+        if (n >= 8) {
+            if (vec) { a = reinterpret_cast<const uint4*>(p)[0]; b = reinterpret_cast<const uint4*>(p)[1]; return; }
+            const uint32_t* q = reinterpret_cast<const uint32_t*>(p);
+            a = make_uint4(q[0], q[1], q[2], q[3]);
+            b = make_uint4(q[4], q[5], q[6], q[7]);
+            return;
         }
+        uint32_t* w = reinterpret_cast<uint32_t*>(this);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = i < n ? __float_as_uint(p[i]) : 0xff800000u;
+    }
+    __device__ __forceinline__ void widen(float* x) const {
+        x[0] = __uint_as_float(a.x); x[1] = __uint_as_float(a.y); x[2] = __uint_as_float(a.z); x[3] = __uint_as_float(a.w);
+        x[4] = __uint_as_float(b.x); x[5] = __uint_as_float(b.y); x[6] = __uint_as_float(b.z); x[7] = __uint_as_float(b.w);
     }
 };
-template <class H> __device__ __forceinline__ float widen(H v);
-template <> __device__ __forceinline__ float widen(__half v) { return __half2float(v); }
-template <> __device__ __forceinline__ float widen(__nv_bfloat16 v) { return __bfloat162float(v); }
-template <class H> struct Octet {
-    static __device__ __forceinline__ void load(const H* p, bool vec, int n, float* x) {
-        if (vec && n >= 8) {
-            const uint4 r = *reinterpret_cast<const uint4*>(p);
-            const H* h = reinterpret_cast<const H*>(&r);
+template <class H> struct Half8 {
+    uint4 a;
+    __device__ __forceinline__ void load(const H* p, bool vec, int n, uint32_t none) {
+        if (n >= 8) {
+            if (vec) { a = *reinterpret_cast<const uint4*>(p); return; }
+            // rows that start off 16-byte boundaries: the aligned words that hold the eight, put together
+            const bool odd = reinterpret_cast<uintptr_t>(p) & 2;
+            const uint32_t* q = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)3);
+            uint32_t w[5];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = widen(h[i]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = i < n ? widen(p[i]) : -INFINITY;
+            for (int i = 0; i < 4; ++i) w[i] = q[i];
+            w[4] = odd ? q[4] : 0u;
+            a = odd ? make_uint4(__funnelshift_r(w[0], w[1], 16), __funnelshift_r(w[1], w[2], 16), __funnelshift_r(w[2], w[3], 16), __funnelshift_r(w[3], w[4], 16))
+                    : make_uint4(w[0], w[1], w[2], w[3]);
+            return;
         }
+        const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
+        uint32_t w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = i < n ? q[i] : none;
+        a = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+    }
+};
+template <> struct Octet<__half> : Half8<__half> {
+    __device__ __forceinline__ void load(const __half* p, bool vec, int n) { Half8<__half>::load(p, vec, n, 0xfc00u); }
+    __device__ __forceinline__ void widen(float* x) const {
+        const __half2* h = reinterpret_cast<const __half2*>(&a);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const float2 f = __half22float2(h[i]); x[2 * i] = f.x; x[2 * i + 1] = f.y; }
+    }
+};
+template <> struct Octet<__nv_bfloat16> : Half8<__nv_bfloat16> {
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, bool vec, int n) { Half8<__nv_bfloat16>::load(p, vec, n, 0xff80u); }
+    __device__ __forceinline__ void widen(float* x) const {
+        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
     }
 };
 
-// Cuts a warp's buffer of n keys (n <= kBuffer) to its k largest, in no particular order; returns the k-th largest's value bits.
-// Bisection over the value bits, then ties by column: few calls, so it is kept small.
-__device__ __forceinline__ uint32_t cut(unsigned long long* buf, int n, int k, int lane) {
-    unsigned long long key[kBuffer / 32];
-#pragma unroll
-    for (int i = 0; i < kBuffer / 32; ++i) key[i] = i * 32 + lane < n ? buf[i * 32 + lane] : 0ull;
-    unsigned long long lo = 0;                    // the largest t with at least k keys >= t
-    for (int bit = 63; bit >= 0; --bit) {
-        const unsigned long long t = lo | (1ull << bit);
+// The largest t such that at least k of the warp's values (keys of which `n` lanes' slots hold one each, invalid ones 0) are >= t.
+template <int M> __device__ __forceinline__ uint32_t kth_largest(const uint32_t* v, int k) {
+    uint32_t lo = 0;
+#pragma unroll 1
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t t = lo | (1u << bit);
         int c = 0;
 #pragma unroll
-        for (int i = 0; i < kBuffer / 32; ++i) c += key[i] >= t;
+        for (int i = 0; i < M; ++i) c += v[i] >= t;
         if (__reduce_add_sync(kFull, c) >= k) lo = t;
+    }
+    return lo;
+}
+
+// Cuts a warp's buffer of n > k keys to its k largest, in no particular order; returns the smallest of their value bits.  Bisection over the
+// values, then over the columns of those that equal the last one.
+__device__ __noinline__ uint32_t cut(unsigned long long* buf, int n, int k, int lane) {
+    constexpr int M = kBuffer / 32;
+    unsigned long long key[M];
+    uint32_t v[M];
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+        key[i] = i * 32 + lane < n ? buf[i * 32 + lane] : 0ull;
+        v[i] = (uint32_t)(key[i] >> 32);
+    }
+    const uint32_t least = kth_largest<M>(v, k);
+    int above = 0, equal = 0;
+#pragma unroll
+    for (int i = 0; i < M; ++i) { above += v[i] > least; equal += key[i] != 0 && v[i] == least; }
+    above = __reduce_add_sync(kFull, above);
+    equal = __reduce_add_sync(kFull, equal);
+    uint32_t column = 0;                          // lowest complement of a column that is taken at the border
+    if (above + equal > k) {
+#pragma unroll
+        for (int i = 0; i < M; ++i) v[i] = key[i] != 0 && v[i] == least ? (uint32_t)key[i] : 0u;
+        column = kth_largest<M>(v, k - above);
     }
     __syncwarp();
     int at = 0;
     const uint32_t lt = lanemask_lt();
 #pragma unroll
-    for (int i = 0; i < kBuffer / 32; ++i) {
-        const bool take = key[i] >= lo && key[i] != 0;
+    for (int i = 0; i < M; ++i) {
+        const uint32_t hi = (uint32_t)(key[i] >> 32);
+        const bool take = key[i] != 0 && (hi > least || (hi == least && (uint32_t)key[i] >= column));
         const uint32_t m = __ballot_sync(kFull, take);
         if (take) buf[at + __popc(m & lt)] = key[i];
         at += __popc(m);
     }
     __syncwarp();
-    return (uint32_t)(lo >> 32);
+    return least;
 }
 
-template <class T>
-__global__ void __launch_bounds__(kRowThreads) beam_rows_kernel(SelectArgs a) {
-    __shared__ unsigned long long buf[kRowWarps][kBuffer];
+// A warp's 32 keys in falling order, a lane each (bitonic), and the 32 largest of two such lists.
+__device__ __forceinline__ unsigned long long exchange(unsigned long long x, int stride, bool larger) {
+    const unsigned long long y = __shfl_xor_sync(kFull, x, stride);
+    return (y > x) == larger ? y : x;
+}
+__device__ __forceinline__ unsigned long long sort32(unsigned long long x, int lane) {
+#pragma unroll
+    for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+        for (int stride = size >> 1; stride > 0; stride >>= 1) x = exchange(x, stride, ((lane & stride) == 0) == ((lane & size) == 0 || size == 32));
+    return x;
+}
+__device__ __forceinline__ unsigned long long merge32(unsigned long long x, unsigned long long y, int lane) {
+    const unsigned long long r = __shfl_sync(kFull, y, 31 - lane);
+    x = r > x ? r : x;
+#pragma unroll
+    for (int stride = 16; stride > 0; stride >>= 1) x = exchange(x, stride, (lane & stride) == 0);
+    return x;
+}
+
+// A warp takes 1024 logits a step, 32 a lane (four groups of eight), so that 64 bytes a lane are on their way.  What a candidate has to reach is known
+// to all warps of the block: a warp's k-th best so far is a lower bound of the part's.  SHORT (k <= 32): a warp keeps its list sorted, a lane an
+// entry, and merges 32 candidates at a time into it; else it cuts a buffer of them now and then.
+constexpr int kGroups = 4, kStep = 32 * 8 * kGroups;
+template <class T, bool SHORT>
+__global__ void __launch_bounds__(kRowThreads, 3) beam_rows_kernel(SelectArgs a) {
+    constexpr int room = SHORT ? kPending + 1 : kBuffer;
+    __shared__ unsigned long long buf[kRowWarps][room];
     __shared__ int held[kRowWarps];
     __shared__ float wtop[kRowWarps];
     __shared__ double wsum[kRowWarps];
+    __shared__ unsigned int border;
     chain_next();
     const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
     if (a.done && a.done[row]) return;            // one continuation, at the beam's own score: the logits are not needed
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    if (tid == 0) border = 0u;
+    __syncthreads();
     const T* x0 = static_cast<const T*>(a.logits) + (int64_t)row * a.row_stride;
     const bool vec = (reinterpret_cast<uintptr_t>(x0) & 15) == 0;
     const int c0 = part * a.part_len, c1 = min(a.V, c0 + a.part_len);
     float m = -FLT_MAX;                           // not -inf: exp(-inf - m) stays 0
     double s = 0.0;
-    int n = 0;
-    uint32_t least = 0;                           // value bits that a candidate has to reach
+    int n = 0;                                    // candidates in the buffer
+    unsigned long long list = 0ull;               // SHORT: the lane's entry of the warp's list
     unsigned long long* mine = buf[wid];
+    volatile unsigned int* least = &border;       // value bits that a candidate has to reach
     const uint32_t lt = lanemask_lt();
-    for (int base = c0 + wid * 256; base < c1; base += kRowThreads * 8) {
-        const int c = base + lane * 8, left = c1 - c;
-        float x[8];
-        Octet<T>::load(x0 + c, vec, left, x);
-        float t = x[0];
+    auto raise = [&](uint32_t v) { if (lane == 0 && v > *least) atomicMax(&border, v); };
+    auto merge = [&]() {                          // SHORT: the buffer's last (at most 32) candidates into the list
+        __syncwarp();
+        const int take = min(n, 32), at = n - take + lane;
+        list = merge32(list, sort32(lane < take ? mine[at] : 0ull, lane), lane);
+        n -= take;
+        raise((uint32_t)(__shfl_sync(kFull, list, a.k - 1) >> 32));
+        __syncwarp();
+    };
+    Octet<T> o[kGroups];
+    auto fetch = [&](int base) {
 #pragma unroll
-        for (int i = 1; i < 8; ++i) t = fmaxf(t, x[i]);
-        if (t > m) { s *= (double)__expf(m - t); m = t; }
-        float e[8];
+        for (int g = 0; g < kGroups; ++g) { const int c = base + g * 256 + lane * 8; o[g].load(x0 + c, vec, c1 - c); }
+    };
+    int base = c0 + wid * kStep;
+    if (base < c1) fetch(base);
+    for (; base < c1; base += kRowWarps * kStep) {
+        Octet<T> now[kGroups];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = exp2f((x[i] - m) * 1.44269504088896f);
-        s += (double)(((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7])));
-        if (__any_sync(kFull, left > 0 && order_bits(t) >= least)) {
+        for (int g = 0; g < kGroups; ++g) now[g] = o[g];
+        if (base + kRowWarps * kStep < c1) fetch(base + kRowWarps * kStep);
+        float top[kGroups], t = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            float x[8];
+            now[g].widen(x);
+            top[g] = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+            t = fmaxf(t, top[g]);
+        }
+        if (t > m) { s *= (double)exp2_approx((m - t) * kLog2e); m = t; }
+        float part_sum = 0.f;
+        const unsigned long long neg = pack2(-m, -m), scale = pack2(kLog2e, kLog2e);
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            float x[8];
+            now[g].widen(x);
+            unsigned long long e[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float lo, hi;
+                unpack2(fma2(add2(pack2(x[2 * i], x[2 * i + 1]), neg), scale, 0ull), lo, hi);
+                e[i] = pack2(exp2_approx(lo), exp2_approx(hi));
+            }
+            float lo, hi;
+            unpack2(add2(add2(e[0], e[1]), add2(e[2], e[3])), lo, hi);
+            part_sum += lo + hi;
+        }
+        s += (double)part_sum;
+        uint32_t need = *least;
+        if (SHORT && need == 0) {                  // at the start: the k-th best of the lanes' maxima
+            const unsigned long long v = sort32((unsigned long long)order_bits(t) << 32, lane);
+            need = (uint32_t)(__shfl_sync(kFull, v, a.k - 1) >> 32);
+            raise(need);
+        }
+        if (!__any_sync(kFull, order_bits(t) >= need)) continue;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            if (!__any_sync(kFull, order_bits(top[g]) >= need)) continue;
+            const int c = base + g * 256 + lane * 8;
+            float x[8];
+            now[g].widen(x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const uint32_t o = order_bits(x[i]);
-                const bool take = i < left && o >= least;
+                const uint32_t v = order_bits(x[i]);
+                const bool take = c + i < c1 && v >= need;
                 const uint32_t b = __ballot_sync(kFull, take);
-                if (take) mine[n + __popc(b & lt)] = ((unsigned long long)o << 32) | (uint32_t)~(c + i);
+                if (take) mine[n + __popc(b & lt)] = ((unsigned long long)v << 32) | (uint32_t)~(c + i);
                 n += __popc(b);
             }
-            __syncwarp();
-            if (n > kBuffer - 256) { least = cut(mine, n, a.k, lane); n = min(n, a.k); }
+            if (SHORT) {
+                while (n >= 32) { merge(); need = max(need, *least); }
+            } else if (n > kBuffer - 256) {
+                need = max(need, cut(mine, n, a.k, lane));
+                n = a.k;
+                raise(need);
+            }
         }
     }
-    if (n > a.k) { cut(mine, n, a.k, lane); n = a.k; }
+    if (SHORT) {
+        if (n > 0) merge();
+        mine[lane] = list;
+        n = 32;
+    } else if (n > a.k) {
+        raise(cut(mine, n, a.k, lane));
+        n = a.k;
+    }
     float top = m;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
-    s *= (double)exp2f((m - top) * 1.44269504088896f);
+    for (int w = 16; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, w));
+    s *= (double)exp2_approx((m - top) * kLog2e);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(kFull, s, o);
-    if (lane == 0) { held[wid] = n; wtop[wid] = top; wsum[wid] = s; }
+    for (int w = 16; w > 0; w >>= 1) s += __shfl_xor_sync(kFull, s, w);
+    if (lane == 0) { wtop[wid] = top; wsum[wid] = s; }
+    __syncthreads();
+    // what the other warps have found leaves out most of this one's candidates
+    {
+        const uint32_t need = border;
+        int kept = 0;
+        for (int i = 0; i < n; i += 32) {
+            const unsigned long long key = i + lane < n ? mine[i + lane] : 0ull;
+            const bool take = key != 0 && (uint32_t)(key >> 32) >= need;
+            const uint32_t b = __ballot_sync(kFull, take);
+            if (take) mine[kept + __popc(b & lt)] = key;
+            kept += __popc(b);
+            __syncwarp();
+        }
+        n = kept;
+        if (lane == 0) held[wid] = n;
+    }
     __syncthreads();
     const long long slot = (long long)row * a.parts + part;
     if (tid == 0) {
         float all = wtop[0];
         for (int w = 1; w < kRowWarps; ++w) all = fmaxf(all, wtop[w]);
         double sum = 0.0;
-        for (int w = 0; w < kRowWarps; ++w) sum += wsum[w] * (double)exp2f((wtop[w] - all) * 1.44269504088896f);
+        for (int w = 0; w < kRowWarps; ++w) sum += wsum[w] * (double)exp2_approx((wtop[w] - all) * kLog2e);
         a.sum[slot] = sum;
         a.top[slot] = all;
     }
@@ -172,94 +342,108 @@ __global__ void __launch_bounds__(kRowThreads) beam_rows_kernel(SelectArgs a) {
     }
 }
 
-// Better of two continuations: the larger score, then the lower place (row in the session, column).
-struct Best { double score; unsigned long long place; int list; };
-__device__ __forceinline__ bool better(double s, unsigned long long p, const Best& b) { return s > b.score || (s == b.score && p < b.place); }
-__device__ __forceinline__ Best warp_best(Best b) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        const double s = __shfl_xor_sync(kFull, b.score, o);
-        const unsigned long long p = __shfl_xor_sync(kFull, b.place, o);
-        const int l = __shfl_xor_sync(kFull, b.list, o);
-        if (better(s, p, b)) { b.score = s; b.place = p; b.list = l; }
-    }
-    return b;
+// A continuation: its score's order-preserving bits (0: none), and its place (row in the session, column) as one number.
+struct Cont { unsigned long long score; uint32_t place; };
+__device__ __forceinline__ bool better(const Cont& a, const Cont& b) { return a.score > b.score || (a.score == b.score && a.place < b.place); }
+__device__ __forceinline__ Cont shuffle(const Cont& c, int lane) { return Cont{__shfl_sync(kFull, c.score, lane), __shfl_sync(kFull, c.place, lane)}; }
+__device__ __forceinline__ Cont exchange(const Cont& x, int lane, int stride, bool larger) {
+    const Cont y = shuffle(x, lane ^ stride);
+    return better(y, x) == larger ? y : x;
+}
+__device__ __forceinline__ Cont sort32(Cont x, int lane) {
+#pragma unroll 1
+    for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll 1
+        for (int stride = size >> 1; stride > 0; stride >>= 1) x = exchange(x, lane, stride, ((lane & stride) == 0) == ((lane & size) == 0 || size == 32));
+    return x;
+}
+__device__ __forceinline__ Cont merge32(Cont x, const Cont& y, int lane) {
+    const Cont r = shuffle(y, 31 - lane);
+    if (better(r, x)) x = r;
+#pragma unroll 1
+    for (int stride = 16; stride > 0; stride >>= 1) x = exchange(x, lane, stride, (lane & stride) == 0);
+    return x;
+}
+__device__ __forceinline__ unsigned long long order_bits(double x) {
+    const unsigned long long b = (unsigned long long)__double_as_longlong(x);
+    return b ^ ((unsigned long long)((long long)b >> 63) | (1ull << 63));
+}
+__device__ __forceinline__ double double_of(unsigned long long o) {
+    return __longlong_as_double((long long)(o >> 63 ? o ^ (1ull << 63) : ~o));
 }
 
-// A block a session: its lists are merged by taking the best head n_out times; the lists of a warp first, then the warps'.
+// A block a session: the 32 best of its lists' entries, then the 32 behind those, and so on.  The lists' first entries come first, so that
+// soon only few of the others pass the 32nd best so far; 32 at a time are sorted and merged into the warp's 32, and the warps' in the end.
 constexpr int kMergeThreads = 256, kMergeWarps = kMergeThreads / 32;
 __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(SelectArgs a) {
     extern __shared__ unsigned long long keys[];             // [beams][parts][k]
-    __shared__ double offset[kMostOut];                      // score - lse
-    __shared__ int done[kMostOut];
-    __shared__ Best won[kMergeWarps][kMostOut];
-    __shared__ int n_won[kMergeWarps];
+    __shared__ double offset[kMostOut];                      // score - lse; -inf: no continuation
+    __shared__ Cont best[kMergeWarps][32];
+    __shared__ Cont border;
     chain_wait();
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, lists = a.beams * a.parts;
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, lists = a.beams * a.parts, entries = lists * a.k;
+    const unsigned long long* from = a.list + (long long)b * entries;
+    for (int i = tid; i < entries; i += kMergeThreads) keys[i] = from[i];
     for (int w = tid; w < a.beams; w += kMergeThreads) {
         const long long row = (long long)b * a.beams + w;
         const double own = (double)a.score[row];
-        done[w] = a.done && a.done[row];
         double o = own;
-        if (!done[w]) {
+        if (a.done && a.done[row]) {                         // its one continuation stands first in its first list
+            o = 0.0;
+            if (!isfinite(own)) o = -INFINITY;
+        } else {
             float top = -FLT_MAX;
             for (int p = 0; p < a.parts; ++p) top = fmaxf(top, a.top[row * a.parts + p]);
             double sum = 0.0;
-            for (int p = 0; p < a.parts; ++p) sum += a.sum[row * a.parts + p] * (double)exp2f((a.top[row * a.parts + p] - top) * 1.44269504088896f);
+            for (int p = 0; p < a.parts; ++p) sum += a.sum[row * a.parts + p] * (double)exp2_approx((a.top[row * a.parts + p] - top) * kLog2e);
             o = own - ((double)top + log(sum));
         }
         offset[w] = isfinite(own) && isfinite(o) ? o : -INFINITY;
     }
-    const unsigned long long* from = a.list + (long long)b * lists * a.k;
-    for (int i = tid; i < lists * a.k; i += kMergeThreads) keys[i] = from[i];
     __syncthreads();
-    // a list's head as a continuation; `at` entries of it have been taken
-    auto head = [&](int l, int at) -> Best {
-        const int w = l / a.parts;
-        const Best none{-INFINITY, ~0ull, -1};
-        if (offset[w] == -INFINITY) return none;
-        if (done[w]) return l % a.parts == 0 && at == 0 ? Best{offset[w], (unsigned long long)w * a.V + a.eos, l} : none;
-        if (at >= a.k) return none;
-        const unsigned long long key = keys[l * a.k + at];
-        if (key == 0) return none;
-        const double s = (double)value_of((uint32_t)(key >> 32)) + offset[w];
-        return s > -INFINITY ? Best{s, (unsigned long long)w * a.V + (uint32_t)~(uint32_t)key, l} : none;
-    };
-    // a warp has the lists wid, wid + 8, ...; a lane every 32nd of those: at most beams*parts / 256, whose heads it keeps
-    constexpr int kMine = 8;
-    int at[kMine];
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) at[i] = 0;
-    int n = 0;
-    for (; n < a.n_out; ++n) {
-        Best m{-INFINITY, ~0ull, -1};
-#pragma unroll
-        for (int i = 0; i < kMine; ++i) {
-            const int l = (i * 32 + lane) * kMergeWarps + wid;
-            if (l < lists) { const Best h = head(l, at[i]); if (better(h.score, h.place, m)) m = h; }
+    for (int done = 0; done < a.n_out; done += 32) {
+        const int want = min(32, a.n_out - done);
+        Cont mine{0ull, ~0u};
+        const Cont above = done ? border : Cont{~0ull, 0u};  // the last one taken
+        int l = tid % lists, j = tid / lists;
+        const int dl = kMergeThreads % lists, dj = kMergeThreads / lists;
+        for (int i0 = wid * 32; i0 < entries; i0 += kMergeThreads) {
+            Cont c{0ull, ~0u};
+            if (i0 + lane < entries) {
+                const int w = l / a.parts;
+                const double o = offset[w];
+                if (a.done && a.done[(long long)b * a.beams + w]) {
+                    if (l % a.parts == 0 && j == 0 && o > -INFINITY)
+                        c = Cont{order_bits((double)a.score[(long long)b * a.beams + w]), (uint32_t)w * (uint32_t)a.V + (uint32_t)a.eos};
+                } else {
+                    const unsigned long long key = keys[l * a.k + j];
+                    const double s = (double)value_of((uint32_t)(key >> 32)) + o;
+                    if (key != 0 && s > -INFINITY) c = Cont{order_bits(s), (uint32_t)w * (uint32_t)a.V + ~(uint32_t)key};
+                }
+            }
+            l += dl;
+            j += dj;
+            if (l >= lists) { l -= lists; ++j; }
+            const Cont last = shuffle(mine, want - 1);
+            const bool take = c.score != 0 && better(c, last) && better(above, c);
+            if (!__any_sync(kFull, take)) continue;
+            if (!take) c = Cont{0ull, ~0u};
+            mine = merge32(mine, sort32(c, lane), lane);
         }
-        m = warp_best(m);
-        if (m.list < 0) break;
-#pragma unroll
-        for (int i = 0; i < kMine; ++i)
-            if ((i * 32 + lane) * kMergeWarps + wid == m.list) ++at[i];
-        if (lane == 0) won[wid][n] = m;
-    }
-    if (lane == 0) n_won[wid] = n;
-    __syncthreads();
-    if (wid) return;
-    int pos = 0;
-    for (n = 0; n < a.n_out; ++n) {
-        Best m{-INFINITY, ~0ull, -1};
-        if (lane < kMergeWarps && pos < n_won[lane]) { m = won[lane][pos]; m.list = lane; }
-        m = warp_best(m);
-        if (lane == m.list) ++pos;
-        if (lane == 0) {
-            const long long o = (long long)b * a.n_out + n;
-            a.out_score[o] = (float)m.score;
-            a.out_parent[o] = m.list < 0 ? -1 : (int)(b * a.beams + m.place / a.V);
-            a.out_token[o] = m.list < 0 ? -1 : (int)(m.place % a.V);
+        best[wid][lane] = mine;
+        __syncthreads();
+        if (wid == 0) {
+            for (int w = 1; w < kMergeWarps && w * 32 < entries; ++w) mine = merge32(mine, best[w][lane], lane);
+            if (lane == 31) border = mine;
+            if (lane < want) {
+                const long long o = (long long)b * a.n_out + done + lane;
+                const bool some = mine.score != 0;
+                a.out_score[o] = some ? (float)double_of(mine.score) : -INFINITY;
+                a.out_parent[o] = some ? (int)(b * a.beams + mine.place / (uint32_t)a.V) : -1;
+                a.out_token[o] = some ? (int)(mine.place % (uint32_t)a.V) : -1;
+            }
         }
+        __syncthreads();
     }
 }
 
@@ -310,10 +494,8 @@ __global__ void __launch_bounds__(kCopyThreads) beam_reorder_kernel(const __grid
 // Parts of a row: enough for the GPU where rows are few, as long as a part has 4096 logits and the session's lists fit the merge.
 int row_parts(long long rows, int beams, int V, int k) {
     const long long most = (V + 4095) / 4096, fill = (8LL * sm_count() + rows - 1) / rows, fit = kMostListed / ((long long)beams * k);
-    const long long lists = 2048 / beams;         // a merging lane keeps at most 8 heads
     long long p = fill < most ? fill : most;
     p = p < fit ? p : fit;
-    p = p < lists ? p : lists;
     return (int)(p < 1 ? 1 : p);
 }
 uint64_t beam_bytes(long long rows, int beams, int V, int n_out, int* parts, int* k) {
@@ -323,7 +505,8 @@ uint64_t beam_bytes(long long rows, int beams, int V, int n_out, int* parts, int
 }
 plc_status check_beams(int32_t sessions, int32_t beams, int32_t vocab, int32_t n_out) {
     if (sessions < 1 || beams < 1 || vocab < 1 || n_out < 1) return PLC_E_INVALID;
-    if (beams > kMostOut || n_out > kMostOut || sessions > (1 << 20) || (long long)sessions * beams > (1 << 24)) return PLC_E_SHAPE;
+    if (beams > kMostOut || n_out > kMostOut || sessions > (1 << 20) || (long long)sessions * beams > (1 << 24) || (long long)beams * vocab >= (1ll << 32))
+        return PLC_E_SHAPE;
     return PLC_OK;
 }
 
@@ -365,7 +548,10 @@ plc_status plc_beam_select(const void* logits_dev, int32_t dtype, int64_t row_st
     a.top = reinterpret_cast<float*>(a.sum + rows * a.parts);
     a.out_score = out_score_dev; a.out_parent = out_parent_dev; a.out_token = out_token_dev;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    auto kern = dtype == PLC_OUT_F32 ? beam_rows_kernel<float> : dtype == PLC_OUT_F16 ? beam_rows_kernel<__half> : beam_rows_kernel<__nv_bfloat16>;
+    const bool brief = a.k <= 32;
+    auto kern = dtype == PLC_OUT_F32 ? (brief ? beam_rows_kernel<float, true> : beam_rows_kernel<float, false>)
+              : dtype == PLC_OUT_F16 ? (brief ? beam_rows_kernel<__half, true> : beam_rows_kernel<__half, false>)
+                                     : (brief ? beam_rows_kernel<__nv_bfloat16, true> : beam_rows_kernel<__nv_bfloat16, false>);
     if (launch_kernel(kern, (unsigned)(rows * a.parts), kRowThreads, 0, st, false, 1, a) != cudaSuccess) return PLC_E_CUDA;
     const size_t smem = (size_t)beams * a.parts * a.k * 8;
     if (cudaFuncSetAttribute(beam_merge_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostListed * 8) != cudaSuccess) return PLC_E_CUDA;
