@@ -17,7 +17,7 @@
 namespace plc {
 namespace {
 
-constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
+constexpr int kRowThreads = 128, kRowWarps = kRowThreads / 32;
 constexpr int kMostOut = 128;                     // n_out, beams
 constexpr int kBuffer = 512;                     // a warp's candidates where lists are long: cut to n_out when a step of 256 more might not fit
 constexpr int kPending = 31 + 256;                // and where they have at most 32 entries: those not yet merged into the list
@@ -63,6 +63,11 @@ template <> struct Octet<float> {
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = i < n ? __float_as_uint(p[i]) : 0xff800000u;
     }
+    __device__ __forceinline__ float top() const {
+        float x[8];
+        widen(x);
+        return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
+    }
     __device__ __forceinline__ void widen(float* x) const {
         x[0] = __uint_as_float(a.x); x[1] = __uint_as_float(a.y); x[2] = __uint_as_float(a.z); x[3] = __uint_as_float(a.w);
         x[4] = __uint_as_float(b.x); x[5] = __uint_as_float(b.y); x[6] = __uint_as_float(b.z); x[7] = __uint_as_float(b.w);
@@ -93,6 +98,11 @@ template <class H> struct Half8 {
 };
 template <> struct Octet<__half> : Half8<__half> {
     __device__ __forceinline__ void load(const __half* p, bool vec, int n) { Half8<__half>::load(p, vec, n, 0xfc00u); }
+    __device__ __forceinline__ float top() const {
+        const __half2* h = reinterpret_cast<const __half2*>(&a);
+        const float2 f = __half22float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
+        return fmaxf(f.x, f.y);
+    }
     __device__ __forceinline__ void widen(float* x) const {
         const __half2* h = reinterpret_cast<const __half2*>(&a);
 #pragma unroll
@@ -101,6 +111,11 @@ template <> struct Octet<__half> : Half8<__half> {
 };
 template <> struct Octet<__nv_bfloat16> : Half8<__nv_bfloat16> {
     __device__ __forceinline__ void load(const __nv_bfloat16* p, bool vec, int n) { Half8<__nv_bfloat16>::load(p, vec, n, 0xff80u); }
+    __device__ __forceinline__ float top() const {
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&a);
+        const float2 f = __bfloat1622float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
+        return fmaxf(f.x, f.y);
+    }
     __device__ __forceinline__ void widen(float* x) const {
         const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
@@ -186,10 +201,10 @@ __device__ __forceinline__ unsigned long long merge32(unsigned long long x, unsi
 // entry, and merges 32 candidates at a time into it; else it cuts a buffer of them now and then.
 constexpr int kGroups = 4, kStep = 32 * 8 * kGroups;
 template <class T, bool SHORT>
-__global__ void __launch_bounds__(kRowThreads, 3) beam_rows_kernel(SelectArgs a) {
+__global__ void __launch_bounds__(kRowThreads, 6) beam_rows_kernel(SelectArgs a) {
     constexpr int room = SHORT ? kPending + 1 : kBuffer;
     __shared__ unsigned long long buf[kRowWarps][room];
-    __shared__ int held[kRowWarps];
+    __shared__ int held[kRowWarps];               // candidates in the buffers
     __shared__ float wtop[kRowWarps];
     __shared__ double wsum[kRowWarps];
     __shared__ unsigned int border;
@@ -198,6 +213,7 @@ __global__ void __launch_bounds__(kRowThreads, 3) beam_rows_kernel(SelectArgs a)
     if (a.done && a.done[row]) return;            // one continuation, at the beam's own score: the logits are not needed
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     if (tid == 0) border = 0u;
+    if (lane == 0) held[wid] = 0;
     __syncthreads();
     const T* x0 = static_cast<const T*>(a.logits) + (int64_t)row * a.row_stride;
     const bool vec = (reinterpret_cast<uintptr_t>(x0) & 15) == 0;
@@ -232,12 +248,7 @@ __global__ void __launch_bounds__(kRowThreads, 3) beam_rows_kernel(SelectArgs a)
         if (base + kRowWarps * kStep < c1) fetch(base + kRowWarps * kStep);
         float top[kGroups], t = -INFINITY;
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-            float x[8];
-            now[g].widen(x);
-            top[g] = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-            t = fmaxf(t, top[g]);
-        }
+        for (int g = 0; g < kGroups; ++g) { top[g] = now[g].top(); t = fmaxf(t, top[g]); }
         if (t > m) { s *= (double)exp2_approx((m - t) * kLog2e); m = t; }
         float part_sum = 0.f;
         const unsigned long long neg = pack2(-m, -m), scale = pack2(kLog2e, kLog2e);
@@ -263,27 +274,31 @@ __global__ void __launch_bounds__(kRowThreads, 3) beam_rows_kernel(SelectArgs a)
             need = (uint32_t)(__shfl_sync(kFull, v, a.k - 1) >> 32);
             raise(need);
         }
-        if (!__any_sync(kFull, order_bits(t) >= need)) continue;
+        float limit = need ? value_of(need) : -INFINITY;
+        if (!__any_sync(kFull, t >= limit)) continue;
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
-            if (!__any_sync(kFull, order_bits(top[g]) >= need)) continue;
-            const int c = base + g * 256 + lane * 8;
-            float x[8];
-            now[g].widen(x);
+            if (!__any_sync(kFull, top[g] >= limit)) continue;
+            if (top[g] >= limit) {                 // few lanes: each puts its own into the buffer
+                const int c = base + g * 256 + lane * 8;
+                float x[8];
+                now[g].widen(x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t v = order_bits(x[i]);
-                const bool take = c + i < c1 && v >= need;
-                const uint32_t b = __ballot_sync(kFull, take);
-                if (take) mine[n + __popc(b & lt)] = ((unsigned long long)v << 32) | (uint32_t)~(c + i);
-                n += __popc(b);
+                for (int i = 0; i < 8; ++i)
+                    if (x[i] >= limit && c + i < c1) mine[atomicAdd(&held[wid], 1)] = ((unsigned long long)order_bits(x[i]) << 32) | (uint32_t)~(c + i);
             }
-            if (SHORT) {
-                while (n >= 32) { merge(); need = max(need, *least); }
-            } else if (n > kBuffer - 256) {
-                need = max(need, cut(mine, n, a.k, lane));
-                n = a.k;
-                raise(need);
+            __syncwarp();
+            n = *reinterpret_cast<volatile int*>(&held[wid]);
+            if (SHORT ? n >= 32 : n > kBuffer - 256) {
+                if (SHORT) while (n >= 32) merge();
+                else {
+                    raise(cut(mine, n, a.k, lane));
+                    n = a.k;
+                }
+                if (lane == 0) held[wid] = n;
+                __syncwarp();
+                need = max(need, *least);
+                limit = value_of(need);
             }
         }
     }
@@ -491,12 +506,17 @@ __global__ void __launch_bounds__(kCopyThreads) beam_reorder_kernel(const __grid
     }
 }
 
-// Parts of a row: enough for the GPU where rows are few, as long as a part has 4096 logits and the session's lists fit the merge.
+// Parts of a row: of those that leave a part 4096 logits and fit the merge, the one with the least rounds of blocks times (a warp's logits plus kSetUp, what
+// its first candidates and the joining of the warps cost, in logits).
+constexpr int kSetUp = 3000, kResident = 6;       // blocks an SM
 int row_parts(long long rows, int beams, int V, int k) {
-    const long long most = (V + 4095) / 4096, fill = (8LL * sm_count() + rows - 1) / rows, fit = kMostListed / ((long long)beams * k);
-    long long p = fill < most ? fill : most;
-    p = p < fit ? p : fit;
-    return (int)(p < 1 ? 1 : p);
+    const long long most = (V + 4095) / 4096, fit = kMostListed / ((long long)beams * k), slots = (long long)kResident * sm_count();
+    long long best = 1, least = 0;
+    for (long long p = 1; p <= most && p <= fit && p <= 64; ++p) {
+        const long long cost = (rows * p + slots - 1) / slots * ((V + p - 1) / p / kRowWarps + kSetUp);
+        if (p == 1 || cost < least) { best = p; least = cost; }
+    }
+    return (int)best;
 }
 uint64_t beam_bytes(long long rows, int beams, int V, int n_out, int* parts, int* k) {
     *k = n_out < V ? n_out : V;
