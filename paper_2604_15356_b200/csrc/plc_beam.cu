@@ -17,10 +17,11 @@
 namespace plc {
 namespace {
 
-constexpr int kRowThreads = 128, kRowWarps = kRowThreads / 32;
+constexpr int kRowThreads = 128, kRowWarps = kRowThreads / 32, kResident = 7;   // blocks an SM
 constexpr int kMostOut = 128;                     // n_out, beams
-constexpr int kBuffer = 512;                     // a warp's candidates where lists are long: cut to n_out when a step of 256 more might not fit
-constexpr int kPending = 31 + 256;                // and where they have at most 32 entries: those not yet merged into the list
+constexpr int kChunks = 32;                       // pieces of a lane's logits whose maxima are kept
+constexpr int kRoom = 1024;                       // candidates of a part that are ranked as they are
+constexpr int kBuffer = 512;                      // and, where there are more (equal logits), at a time
 constexpr int kMostListed = 16384;                // entries of a session's lists (the merge holds them in shared memory)
 
 struct SelectArgs {
@@ -49,6 +50,9 @@ constexpr float kLog2e = 1.44269504088896f;
 
 // Eight logits as they stand in memory; -inf behind the n-th.
 template <class T> struct Octet;
+__device__ __forceinline__ float widen(float v) { return v; }
+__device__ __forceinline__ float widen(__half v) { return __half2float(v); }
+__device__ __forceinline__ float widen(__nv_bfloat16 v) { return __bfloat162float(v); }
 template <> struct Octet<float> {
     uint4 a, b;
     __device__ __forceinline__ void load(const float* p, bool vec, int n) {
@@ -176,183 +180,182 @@ __device__ __noinline__ uint32_t cut(unsigned long long* buf, int n, int k, int 
     return least;
 }
 
-// A warp's 32 keys in falling order, a lane each (bitonic), and the 32 largest of two such lists.
-__device__ __forceinline__ unsigned long long exchange(unsigned long long x, int stride, bool larger) {
-    const unsigned long long y = __shfl_xor_sync(kFull, x, stride);
-    return (y > x) == larger ? y : x;
-}
-__device__ __forceinline__ unsigned long long sort32(unsigned long long x, int lane) {
-#pragma unroll
-    for (int size = 2; size <= 32; size <<= 1)
-#pragma unroll
-        for (int stride = size >> 1; stride > 0; stride >>= 1) x = exchange(x, stride, ((lane & stride) == 0) == ((lane & size) == 0 || size == 32));
-    return x;
-}
-__device__ __forceinline__ unsigned long long merge32(unsigned long long x, unsigned long long y, int lane) {
-    const unsigned long long r = __shfl_sync(kFull, y, 31 - lane);
-    x = r > x ? r : x;
-#pragma unroll
-    for (int stride = 16; stride > 0; stride >>= 1) x = exchange(x, stride, (lane & stride) == 0);
-    return x;
-}
-
-// A warp takes 1024 logits a step, 32 a lane (four groups of eight), so that 64 bytes a lane are on their way.  What a candidate has to reach is known
-// to all warps of the block: a warp's k-th best so far is a lower bound of the part's.  SHORT (k <= 32): a warp keeps its list sorted, a lane an
-// entry, and merges 32 candidates at a time into it; else it cuts a buffer of them now and then.
-constexpr int kGroups = 4, kStep = 32 * 8 * kGroups;
-template <class T, bool SHORT>
-__global__ void __launch_bounds__(kRowThreads, 6) beam_rows_kernel(SelectArgs a) {
-    constexpr int room = SHORT ? kPending + 1 : kBuffer;
-    __shared__ unsigned long long buf[kRowWarps][room];
-    __shared__ int held[kRowWarps];               // candidates in the buffers
+// A block takes a part of a row in two passes.  The first streams: a warp takes 32 lanes times kGroups times eight logits a step, the next step's loads on
+// their way, forms the sum and keeps the maximum of each lane's chunks of steps.  The k-th largest of the lanes' maxima is a bound that k logits reach and
+// few others do, so the second pass looks at the chunks that reach it alone: about k of them, from L2.
+template <class T> struct Step { static constexpr int groups = 4; };                  // 64 bytes a lane
+template <> struct Step<float> { static constexpr int groups = 2; };
+template <class T>
+__global__ void __launch_bounds__(kRowThreads, kResident) beam_rows_kernel(SelectArgs a) {
+    constexpr int groups = Step<T>::groups, step = 256 * groups;
+    __shared__ float tops[kChunks][kRowThreads];
+    __shared__ unsigned long long found[kRoom];
     __shared__ float wtop[kRowWarps];
     __shared__ double wsum[kRowWarps];
-    __shared__ unsigned int border;
+    __shared__ __align__(16) uint32_t order[kRowThreads];
+    __shared__ float bound;
+    __shared__ int count;
     chain_next();
     const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
     if (a.done && a.done[row]) return;            // one continuation, at the beam's own score: the logits are not needed
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-    if (tid == 0) border = 0u;
-    if (lane == 0) held[wid] = 0;
-    __syncthreads();
     const T* x0 = static_cast<const T*>(a.logits) + (int64_t)row * a.row_stride;
     const bool vec = (reinterpret_cast<uintptr_t>(x0) & 15) == 0;
     const int c0 = part * a.part_len, c1 = min(a.V, c0 + a.part_len);
+    const int steps = (c1 - c0 + kRowWarps * step - 1) / (kRowWarps * step), per_chunk = (steps + kChunks - 1) / kChunks;
+    // the i-th step of this warp begins at column
+    auto column = [&](int w, int i) { return c0 + (i * kRowWarps + w) * step; };
     float m = -FLT_MAX;                           // not -inf: exp(-inf - m) stays 0
+    float top = -INFINITY, chunk_top = -INFINITY;
     double s = 0.0;
-    int n = 0;                                    // candidates in the buffer
-    unsigned long long list = 0ull;               // SHORT: the lane's entry of the warp's list
-    unsigned long long* mine = buf[wid];
-    volatile unsigned int* least = &border;       // value bits that a candidate has to reach
-    const uint32_t lt = lanemask_lt();
-    auto raise = [&](uint32_t v) { if (lane == 0 && v > *least) atomicMax(&border, v); };
-    auto merge = [&]() {                          // SHORT: the buffer's last (at most 32) candidates into the list
-        __syncwarp();
-        const int take = min(n, 32), at = n - take + lane;
-        list = merge32(list, sort32(lane < take ? mine[at] : 0ull, lane), lane);
-        n -= take;
-        raise((uint32_t)(__shfl_sync(kFull, list, a.k - 1) >> 32));
-        __syncwarp();
-    };
-    Octet<T> o[kGroups];
+    Octet<T> o[groups];
     auto fetch = [&](int base) {
+        const T* x = x0 + base + lane * 8;
+        if (vec && base + step <= c1) {
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) { const int c = base + g * 256 + lane * 8; o[g].load(x0 + c, vec, c1 - c); }
+            for (int g = 0; g < groups; ++g) o[g].load(x + g * 256, true, 8);
+        } else {
+#pragma unroll
+            for (int g = 0; g < groups; ++g) o[g].load(x + g * 256, vec, c1 - (base + g * 256 + lane * 8));
+        }
     };
-    int base = c0 + wid * kStep;
-    if (base < c1) fetch(base);
-    for (; base < c1; base += kRowWarps * kStep) {
-        Octet<T> now[kGroups];
+    fetch(column(wid, 0));
+    int left = per_chunk, chunk = 0;
+    for (int i = 0; i < steps; ++i) {
+        Octet<T> now[groups];
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) now[g] = o[g];
-        if (base + kRowWarps * kStep < c1) fetch(base + kRowWarps * kStep);
-        float top[kGroups], t = -INFINITY;
+        for (int g = 0; g < groups; ++g) now[g] = o[g];
+        if (i + 1 < steps) fetch(column(wid, i + 1));
+        float t = now[0].top();
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) { top[g] = now[g].top(); t = fmaxf(t, top[g]); }
+        for (int g = 1; g < groups; ++g) t = fmaxf(t, now[g].top());
+        chunk_top = fmaxf(chunk_top, t);
         if (t > m) { s *= (double)exp2_approx((m - t) * kLog2e); m = t; }
         float part_sum = 0.f;
         const unsigned long long neg = pack2(-m, -m), scale = pack2(kLog2e, kLog2e);
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
+        for (int g = 0; g < groups; ++g) {
             float x[8];
             now[g].widen(x);
             unsigned long long e[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int k = 0; k < 4; ++k) {
                 float lo, hi;
-                unpack2(fma2(add2(pack2(x[2 * i], x[2 * i + 1]), neg), scale, 0ull), lo, hi);
-                e[i] = pack2(exp2_approx(lo), exp2_approx(hi));
+                unpack2(fma2(add2(pack2(x[2 * k], x[2 * k + 1]), neg), scale, 0ull), lo, hi);
+                e[k] = pack2(exp2_approx(lo), exp2_approx(hi));
             }
             float lo, hi;
             unpack2(add2(add2(e[0], e[1]), add2(e[2], e[3])), lo, hi);
             part_sum += lo + hi;
         }
         s += (double)part_sum;
-        uint32_t need = *least;
-        if (SHORT && need == 0) {                  // at the start: the k-th best of the lanes' maxima
-            const unsigned long long v = sort32((unsigned long long)order_bits(t) << 32, lane);
-            need = (uint32_t)(__shfl_sync(kFull, v, a.k - 1) >> 32);
-            raise(need);
-        }
-        float limit = need ? value_of(need) : -INFINITY;
-        if (!__any_sync(kFull, t >= limit)) continue;
-#pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-            if (!__any_sync(kFull, top[g] >= limit)) continue;
-            if (top[g] >= limit) {                 // few lanes: each puts its own into the buffer
-                const int c = base + g * 256 + lane * 8;
-                float x[8];
-                now[g].widen(x);
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (x[i] >= limit && c + i < c1) mine[atomicAdd(&held[wid], 1)] = ((unsigned long long)order_bits(x[i]) << 32) | (uint32_t)~(c + i);
-            }
-            __syncwarp();
-            n = *reinterpret_cast<volatile int*>(&held[wid]);
-            if (SHORT ? n >= 32 : n > kBuffer - 256) {
-                if (SHORT) while (n >= 32) merge();
-                else {
-                    raise(cut(mine, n, a.k, lane));
-                    n = a.k;
-                }
-                if (lane == 0) held[wid] = n;
-                __syncwarp();
-                need = max(need, *least);
-                limit = value_of(need);
-            }
+        if (--left == 0 || i + 1 == steps) {
+            tops[chunk++][tid] = chunk_top;
+            top = fmaxf(top, chunk_top);
+            chunk_top = -INFINITY;
+            left = per_chunk;
         }
     }
-    if (SHORT) {
-        if (n > 0) merge();
-        mine[lane] = list;
-        n = 32;
-    } else if (n > a.k) {
-        raise(cut(mine, n, a.k, lane));
-        n = a.k;
-    }
-    float top = m;
+    order[tid] = order_bits(top);
+    if (tid == 0) count = 0;
+    float warp_top = m;
 #pragma unroll
-    for (int w = 16; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, w));
-    s *= (double)exp2_approx((m - top) * kLog2e);
+    for (int w = 16; w > 0; w >>= 1) warp_top = fmaxf(warp_top, __shfl_xor_sync(kFull, warp_top, w));
+    s *= (double)exp2_approx((m - warp_top) * kLog2e);
 #pragma unroll
     for (int w = 16; w > 0; w >>= 1) s += __shfl_xor_sync(kFull, s, w);
-    if (lane == 0) { wtop[wid] = top; wsum[wid] = s; }
-    __syncthreads();
-    // what the other warps have found leaves out most of this one's candidates
-    {
-        const uint32_t need = border;
-        int kept = 0;
-        for (int i = 0; i < n; i += 32) {
-            const unsigned long long key = i + lane < n ? mine[i + lane] : 0ull;
-            const bool take = key != 0 && (uint32_t)(key >> 32) >= need;
-            const uint32_t b = __ballot_sync(kFull, take);
-            if (take) mine[kept + __popc(b & lt)] = key;
-            kept += __popc(b);
-            __syncwarp();
-        }
-        n = kept;
-        if (lane == 0) held[wid] = n;
-    }
+    if (lane == 0) { wtop[wid] = warp_top; wsum[wid] = s; }
     __syncthreads();
     const long long slot = (long long)row * a.parts + part;
-    if (tid == 0) {
-        float all = wtop[0];
-        for (int w = 1; w < kRowWarps; ++w) all = fmaxf(all, wtop[w]);
-        double sum = 0.0;
-        for (int w = 0; w < kRowWarps; ++w) sum += wsum[w] * (double)exp2_approx((wtop[w] - all) * kLog2e);
-        a.sum[slot] = sum;
-        a.top[slot] = all;
+    {
+        int rank = 0;                             // of the lane's maximum among all
+        const uint32_t mine = order[tid];
+#pragma unroll 4
+        for (int i = 0; i < kRowThreads; i += 4) {
+            const uint4 v = *reinterpret_cast<const uint4*>(order + i);
+            rank += (v.x > mine || (v.x == mine && i < tid)) + (v.y > mine || (v.y == mine && i + 1 < tid)) + (v.z > mine || (v.z == mine && i + 2 < tid)) +
+                    (v.w > mine || (v.w == mine && i + 3 < tid));
+        }
+        if (rank == a.k - 1) bound = top;
+        if (tid == 0) {
+            float all = wtop[0];
+            for (int w = 1; w < kRowWarps; ++w) all = fmaxf(all, wtop[w]);
+            double sum = 0.0;
+            for (int w = 0; w < kRowWarps; ++w) sum += wsum[w] * (double)exp2_approx((wtop[w] - all) * kLog2e);
+            a.sum[slot] = sum;
+            a.top[slot] = all;
+        }
     }
-    // each key's place is the number of larger ones
+    __syncthreads();
+    const uint32_t lt = lanemask_lt();
+    // what lane l of warp w took in its i-th step, a logit a lane (0: none)
+    auto look = [&](int w, int l, int i) -> unsigned long long {
+        const int at = column(w, i) + (lane >> 3) * 256 + l * 8 + (lane & 7);
+        return lane < 8 * groups && at < c1 ? ((unsigned long long)order_bits(widen(x0[at])) << 32) | (uint32_t)~at : 0ull;
+    };
+    {
+        const float limit = bound;
+        const uint32_t least = order_bits(limit);
+        for (int c = 0; c < chunk; ++c) {
+            uint32_t who = __ballot_sync(kFull, tops[c][tid] >= limit);
+            while (who) {
+                const int l = __ffs(who) - 1;
+                who &= who - 1;
+                for (int i = c * per_chunk; i < min(steps, (c + 1) * per_chunk); ++i) {
+                    const unsigned long long key = look(wid, l, i);
+                    const bool take = (uint32_t)(key >> 32) >= least && key != 0;
+                    const uint32_t b = __ballot_sync(kFull, take);
+                    if (!b) continue;
+                    int at = 0;
+                    if (lane == 0) at = atomicAdd(&count, __popc(b));
+                    at = __shfl_sync(kFull, at, 0) + __popc(b & lt);
+                    if (take && at < kRoom) found[at] = key;
+                }
+            }
+        }
+    }
+    __syncthreads();
+    int n = count;
+    if (n > kRoom) {                              // many equal logits: one warp looks through them, in no more than kBuffer places
+        __syncthreads();
+        if (wid == 0) {
+            n = 0;
+            unsigned long long worst = 0ull;      // what a candidate has to pass, once k have been found
+            for (int w = 0; w < kRowWarps; ++w)
+                for (int c = 0; c < chunk; ++c) {
+                    uint32_t who = __ballot_sync(kFull, order_bits(tops[c][w * 32 + lane]) >= max((uint32_t)(worst >> 32), order_bits(bound)));
+                    while (who) {
+                        const int l = __ffs(who) - 1;
+                        who &= who - 1;
+                        for (int i = c * per_chunk; i < min(steps, (c + 1) * per_chunk); ++i) {
+                            const unsigned long long key = look(w, l, i);
+                            const bool take = key > worst;
+                            const uint32_t b = __ballot_sync(kFull, take);
+                            if (take) found[n + __popc(b & lt)] = key;
+                            n += __popc(b);
+                            if (n <= kBuffer - 32) continue;
+                            cut(found, n, a.k, lane);
+                            n = a.k;
+                            worst = ~0ull;
+                            for (int k = lane; k < n; k += 32) worst = min(worst, found[k]);
+#pragma unroll
+                            for (int k = 16; k > 0; k >>= 1) worst = min(worst, __shfl_xor_sync(kFull, worst, k));
+                        }
+                    }
+                }
+            __syncwarp();
+            if (lane == 0) count = n;
+        }
+        __syncthreads();
+        n = count;
+    }
+    // each candidate's place is the number of better ones
     unsigned long long* out = a.list + slot * a.k;
-    int total = 0;
-    for (int w = 0; w < kRowWarps; ++w) total += held[w];
-    for (int i = total + tid; i < a.k; i += kRowThreads) out[i] = 0ull;
-    for (int i = lane; i < n; i += 32) {
-        const unsigned long long key = mine[i];
+    for (int i = n + tid; i < a.k; i += kRowThreads) out[i] = 0ull;
+    for (int i = tid; i < n; i += kRowThreads) {
+        const unsigned long long key = found[i];
         int place = 0;
-        for (int w = 0; w < kRowWarps; ++w)
-            for (int j = 0; j < held[w]; ++j) place += buf[w][j] > key;
+        for (int j = 0; j < n; ++j) place += found[j] > key;
         if (place < a.k) out[place] = key;
     }
 }
@@ -508,7 +511,7 @@ __global__ void __launch_bounds__(kCopyThreads) beam_reorder_kernel(const __grid
 
 // Parts of a row: of those that leave a part 4096 logits and fit the merge, the one with the least rounds of blocks times (a warp's logits plus kSetUp, what
 // its first candidates and the joining of the warps cost, in logits).
-constexpr int kSetUp = 3000, kResident = 6;       // blocks an SM
+constexpr int kSetUp = 1500;
 int row_parts(long long rows, int beams, int V, int k) {
     const long long most = (V + 4095) / 4096, fit = kMostListed / ((long long)beams * k), slots = (long long)kResident * sm_count();
     long long best = 1, least = 0;
@@ -568,10 +571,7 @@ plc_status plc_beam_select(const void* logits_dev, int32_t dtype, int64_t row_st
     a.top = reinterpret_cast<float*>(a.sum + rows * a.parts);
     a.out_score = out_score_dev; a.out_parent = out_parent_dev; a.out_token = out_token_dev;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const bool brief = a.k <= 32;
-    auto kern = dtype == PLC_OUT_F32 ? (brief ? beam_rows_kernel<float, true> : beam_rows_kernel<float, false>)
-              : dtype == PLC_OUT_F16 ? (brief ? beam_rows_kernel<__half, true> : beam_rows_kernel<__half, false>)
-                                     : (brief ? beam_rows_kernel<__nv_bfloat16, true> : beam_rows_kernel<__nv_bfloat16, false>);
+    auto kern = dtype == PLC_OUT_F32 ? beam_rows_kernel<float> : dtype == PLC_OUT_F16 ? beam_rows_kernel<__half> : beam_rows_kernel<__nv_bfloat16>;
     if (launch_kernel(kern, (unsigned)(rows * a.parts), kRowThreads, 0, st, false, 1, a) != cudaSuccess) return PLC_E_CUDA;
     const size_t smem = (size_t)beams * a.parts * a.k * 8;
     if (cudaFuncSetAttribute(beam_merge_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostListed * 8) != cudaSuccess) return PLC_E_CUDA;
