@@ -26,14 +26,18 @@ template <int D, int N, bool BOX> struct Few {
     static constexpr int blocks = (D + 63) / 64;                       // 128-byte wide column blocks (32 components: half of one)
     static constexpr int slot = blocks * kTN * 128;
     // rings of K and of V: each slot has one producer, in order, so that no wait can be a phase early
-    static constexpr int k_slots = D == 256 ? 1 : (D == 128 ? 1 : 2) * (N == 16 ? 3 : 2), v_slots = D == 256 ? 2 : (D == 128 ? 1 : 2) * (N == 64 ? 2 : 3);
+    // Two CTAs an SM where the rows are fewest (their chains of small steps hide each other's latencies), else one with all of the shared memory.
+    static constexpr int per_sm = BOX && N == 16 && D != 256 ? 2 : 1;
+    static constexpr int wide = D == 128 ? 1 : 2;                      // slots in the room of one of 128 components
+    static constexpr int k_slots = D == 256 ? 1 : wide * (per_sm == 2 ? 2 : N == 16 ? 3 : 2), v_slots = D == 256 ? 2 : wide * (per_sm == 2 ? 1 : N == 64 ? 2 : 3);
     static constexpr int slots = k_slots + v_slots;
     static constexpr int q_bytes = blocks * N * 128, q_bufs = D == 256 ? 1 : 2;
-    static constexpr int p_bytes = N * kTN * 2, p_bufs = D == 256 ? 1 : 2;
+    static constexpr int p_bytes = N * kTN * 2, p_bufs = D == 256 || per_sm == 2 ? 1 : 2;
     static constexpr int o_blocks = D == 256 ? 2 : 1;
     // softmax: groups of four warps, which share the rows; N / groups of them a thread
     static constexpr int groups = N == 16 ? 1 : 2, C = N / groups, soft = 128 * groups;
-    static constexpr int copy = 128, q_copy = BOX ? 64 : 128, threads = soft + copy + 64;
+    static constexpr int pair = per_sm == 2 ? 1 : 2;                   // warps that copy keys in boxes, and as many for values
+    static constexpr int copy = BOX ? 64 * pair : 128, q_copy = BOX ? 32 * pair : 128, threads = soft + copy + 64;
     static constexpr int tmem = N == 64 || o_blocks * N == 64 ? 256 : 128;   // S twice, O twice
     static constexpr size_t smem = (size_t)q_bufs * q_bytes + p_bufs * p_bytes + slots * slot + (BOX ? 0 : 3 * kTN * 8) + N * (8 + 4 * 13) + 768 + 1024;
 };
@@ -129,7 +133,7 @@ __device__ __noinline__ void put_back(const PoolDev& p, const BookDev& b, const 
 }
 
 template <class T, int D, int N, bool BOX>
-__global__ void __launch_bounds__(Few<D, N, BOX>::threads, 1)
+__global__ void __launch_bounds__(Few<D, N, BOX>::threads, Few<D, N, BOX>::per_sm)
 few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b, const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map,
            uint32_t* status) {
     using F = Few<D, N, BOX>;
@@ -159,7 +163,7 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
                    ofull = pfull + 16, drain = ofull + 16;
     chain_next();
     if (tid == 0) {
-        for (int i = 0; i < slots; ++i) { mbar_init(full + 8 * i, BOX ? 2 : F::copy + F::copy / 32); mbar_init(empty + 8 * i, 1); }
+        for (int i = 0; i < slots; ++i) { mbar_init(full + 8 * i, BOX ? F::pair : F::copy + F::copy / 32); mbar_init(empty + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) {
             mbar_init(qfull + 8 * i, F::q_copy);
             mbar_init(qempty + 8 * i, 1);
@@ -212,9 +216,9 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
             return true;
         };
         if constexpr (BOX) {
-            // ---- copies: two warps for the keys, two for the values; of the two each issues every other box of a tile (box_pos positions of one page,
-            // 64 components wide).  A lane looks a box's page up, a tile ahead.
-            const int half = (lt >> 5) & 1, kv = lt >> 6;
+            // ---- copies: a warp or two for the keys, as many for the values; of two each issues every other box of a tile (box_pos positions of one
+            // page, 64 components wide).  A lane looks a box's page up, a tile ahead.
+            const int half = (lt >> 5) % F::pair, kv = lt / F::q_copy;
             Tl x;
             x.start(w0, total);
             int page = -1, slot = 0, issued = 0;
@@ -246,9 +250,9 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
                 const int s = n % ring_slots;
                 ok = __all_sync(kFull, ok && mbar_wait(my_empty + 8 * s, ((uint32_t)(n / ring_slots) & 1u) ^ 1u, failed, status));
                 if (!ok) break;
-                const uint32_t mine = boxes & (half ? 0xaaaaaaaau : 0x55555555u), bar = my_full + 8 * s;
+                const uint32_t mine = F::pair == 1 ? boxes : boxes & (half ? 0xaaaaaaaau : 0x55555555u), bar = my_full + 8 * s;
                 if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(__popc(mine) * a.box_pos * F::blocks * 128) : "memory");
-                for (int e = half; e < a.boxes; e += 2) {
+                for (int e = half; e < a.boxes; e += F::pair) {
                     const int pg = __shfl_sync(kFull, here, e), sl = __shfl_sync(kFull, at, e);
                     if (!(mine >> e & 1u) || lane != 0) continue;
                     int c[4];
@@ -657,8 +661,10 @@ cudaError_t launch(const PoolDev& p, const BookDev& b, const AttendArgs& a, cons
     using F = Few<D, N, BOX>;
     cudaError_t e = cudaFuncSetAttribute(few_kernel<T, D, N, BOX>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)F::smem);
     if (e != cudaSuccess) return e;
-    e = launch_kernel(few_kernel<T, D, N, BOX>, x.grid, F::threads, F::smem, st, false, 1, p, b, a, map, status);
-    return e != cudaSuccess ? e : launch_join<T, D, N>(p, b, a, x, st);
+    AttendPlan y = x;
+    y.grid = F::per_sm * sm_count();
+    e = launch_kernel(few_kernel<T, D, N, BOX>, y.grid, F::threads, F::smem, st, false, 1, p, b, a, map, status);
+    return e != cudaSuccess ? e : launch_join<T, D, N>(p, b, a, y, st);
 }
 template <class T>
 cudaError_t launch_few(const PoolDev& p, const BookDev& b, const AttendArgs& args, const AttendPlan& x, bool bf16, uint32_t* status, cudaStream_t st) {
