@@ -439,7 +439,7 @@ AttendPlan plan(const PoolDev& p, int heads, int sessions, int n_rows) {
     if (rows <= (long long)few * sessions) {
         AttendPlan x;
         x.row_tile = rows <= 16LL * sessions ? 16 : rows <= 32LL * sessions ? 32 : few;
-        x.grid = (x.row_tile == 16 && p.d != 256 ? 2 : 1) * sm_count();      // at most: see Few::per_sm
+        x.grid = (x.row_tile <= 32 && p.d != 256 ? 2 : 1) * sm_count();      // at most: see Few::per_sm
         x.part_rows = (int)(rows < x.row_tile ? rows : x.row_tile);
         x.bytes = (uint64_t)x.grid * 16 + 2ull * x.grid * x.part_rows * (8 + 4 * p.d);
         return x;

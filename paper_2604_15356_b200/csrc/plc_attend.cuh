@@ -282,49 +282,81 @@ template <int ROWS> struct Tiles {
 };
 
 // Joins the pieces of items that more than one CTA had: block c looks at the boundary between CTAs c - 1 and c, and takes the item if that is the
-// first boundary inside it.  A warp a row at a time.
-constexpr int kJoinThreads = 128, kJoinRows = 16;
+// first boundary inside it.  A warp a row; a lane a piece for the weights, then a lane its components with the pieces' loads eight at a time
+// (a piece after the other, 37 pieces took 84 us).
+constexpr int kJoinThreads = 128;
+template <int ROWS> struct Join { static constexpr int rows = ROWS < 128 ? 4 : 8; };          // a block's
 template <class T, int D, int ROWS>
-__global__ void __launch_bounds__(kJoinThreads) join_kernel(PoolDev p, BookDev b, const __grid_constant__ AttendArgs a, int workers) {
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b, const __grid_constant__ AttendArgs a, int workers) {
+    constexpr int VEC = D / 32;                   // a lane's components
     chain_wait();
     const int c = blockIdx.x + 1, lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     const int4 f = a.first[c], prev = a.first[c - 1];
     if (f.x < 0 || f.w == 0) return;
     auto same = [&](const int4& o) { return o.x == f.x && o.y == f.y && o.z == f.z; };
     if (same(prev) && prev.w > 0) return;
-    const int64_t lead = (int64_t)2 * (c - 1) + (same(prev) ? 0 : 1);      // the piece that the item begins with
-    int last = c;
-    while (last + 1 < workers) {
-        const int4 o = a.first[last + 1];
-        if (!same(o) || o.w == 0) break;
-        ++last;
-    }
+    const int r0 = blockIdx.y * Join<ROWS>::rows;
     bool bad;
     const Session x = session_of(p, b, a, f.x, &bad);
     const int rows = min(ROWS, x.n * a.group - f.z * ROWS);
-    const int end = min(rows, ((int)blockIdx.y + 1) * kJoinRows);
-    for (int r = blockIdx.y * kJoinRows + wid; r < end; r += kJoinThreads / 32) {
-        auto at = [&](int k) -> int64_t { return (k < c ? lead : (int64_t)2 * k) * a.part_rows + r; };
+    if (r0 >= rows) return;
+    int pieces = 2;                               // CTA c - 1 had the first one, c, c + 1, ... the others
+    for (int k = c + 1; k < workers; k += 32) {
+        int4 o = make_int4(-1, 0, 0, 0);
+        if (k + lane < workers) o = a.first[k + lane];
+        const uint32_t in = __ballot_sync(kFull, same(o) && o.w > 0);
+        const int run = __ffs(~in) - 1;           // 32 ones: -1
+        pieces += run < 0 ? 32 : run;
+        if (run >= 0) break;
+    }
+    const int64_t lead = (int64_t)2 * (c - 1) + (same(prev) ? 0 : 1);      // the piece that the item begins with
+    for (int r = r0 + wid; r < min(rows, r0 + Join<ROWS>::rows); r += kJoinThreads / 32) {
+        auto at = [&](int k) -> int64_t { return (k == 0 ? lead : (int64_t)2 * (c - 1 + k)) * a.part_rows + r; };
         float top = -INFINITY;
-        for (int k = c - 1; k <= last; ++k) top = fmaxf(top, a.part_ml[at(k)].x);
-        float sum = 0.f, o[D / 32];
+        for (int k = lane; k < pieces; k += 32) top = fmaxf(top, a.part_ml[at(k)].x);
 #pragma unroll
-        for (int e = 0; e < D / 32; ++e) o[e] = 0.f;
-        for (int k = c - 1; k <= last; ++k) {
-            const float2 ml = a.part_ml[at(k)];
-            if (ml.y == 0.f) continue;                                     // nothing was seen there
-            const float w = exp2f(ml.x - top);
-            sum = fmaf(ml.y, w, sum);
-            const float* from = a.part_o + at(k) * D + lane;
+        for (int w = 16; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, w));
+        float sum = 0.f, o[VEC];
 #pragma unroll
-            for (int e = 0; e < D / 32; ++e) o[e] = fmaf(from[32 * e], w, o[e]);
+        for (int e = 0; e < VEC; ++e) o[e] = 0.f;
+        for (int k0 = 0; k0 < pieces; k0 += 32) {
+            float weight = 0.f;
+            if (k0 + lane < pieces) {
+                const float2 ml = a.part_ml[at(k0 + lane)];
+                if (ml.y != 0.f) { weight = exp2f(ml.x - top); sum = fmaf(ml.y, weight, sum); }   // 0: nothing was seen there
+            }
+            const int n = min(32, pieces - k0);
+            for (int j0 = 0; j0 < n; j0 += 8) {
+                float y[8][VEC];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float* from = a.part_o + at(k0 + min(j0 + j, n - 1)) * D + lane * VEC;
+#pragma unroll
+                    for (int e = 0; e < VEC; e += 4) {
+                        if (VEC >= 4) *reinterpret_cast<float4*>(&y[j][e]) = *reinterpret_cast<const float4*>(from + e);
+                        else if (VEC == 2) *reinterpret_cast<float2*>(&y[j][0]) = *reinterpret_cast<const float2*>(from);
+                        else y[j][0] = *from;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float w = __shfl_sync(kFull, weight, (j0 + j) & 31);
+                    if (j0 + j < n && w != 0.f) {
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) o[e] = fmaf(y[j][e], w, o[e]);
+                    }
+                }
+            }
         }
+        sum = warp_sum(sum);
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         const int rr = f.z * ROWS + r, i = rr / a.group;
         const int64_t n_row = x.first + i, head = (int64_t)f.y * a.group + (rr - i * a.group);
-        uint16_t* out = static_cast<uint16_t*>(a.out) + n_row * a.os_row + head * a.os_head + lane;
+        uint16_t* out = static_cast<uint16_t*>(a.out) + n_row * a.os_row + head * a.os_head + lane * VEC;
+        if constexpr (VEC == 1) *out = (uint16_t)(Kind<T>::pack(o[0] * inv, 0.f) & 0xffffu);
+        else
 #pragma unroll
-        for (int e = 0; e < D / 32; ++e) out[32 * e] = (uint16_t)(Kind<T>::pack(o[e] * inv, 0.f) & 0xffffu);
+            for (int e = 0; e < VEC; e += 2) reinterpret_cast<uint32_t*>(out)[e / 2] = Kind<T>::pack(o[e] * inv, o[e + 1] * inv);
         if (a.lse && lane == 0) a.lse[n_row * a.heads + head] = sum == 0.f ? -INFINITY : (top - Kind<T>::shift + log2f(sum)) * 0.693147180559945f;
     }
 }
@@ -332,7 +364,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(PoolDev p, BookDev b
 template <class T, int D, int ROWS>
 cudaError_t launch_join(const PoolDev& p, const BookDev& b, const AttendArgs& a, const AttendPlan& x, cudaStream_t st) {
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(x.grid - 1, (x.part_rows + kJoinRows - 1) / kJoinRows);
+    cfg.gridDim = dim3(x.grid - 1, (x.part_rows + Join<ROWS>::rows - 1) / Join<ROWS>::rows);
     cfg.blockDim = dim3(kJoinThreads);
     cfg.stream = st;
     cudaLaunchAttribute at{};

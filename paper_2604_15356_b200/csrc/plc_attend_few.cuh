@@ -27,15 +27,15 @@ template <int D, int N, bool BOX> struct Few {
     static constexpr int slot = blocks * kTN * 128;
     // rings of K and of V: each slot has one producer, in order, so that no wait can be a phase early
     // Two CTAs an SM where the rows are fewest (their chains of small steps hide each other's latencies), else one with all of the shared memory.
-    static constexpr int per_sm = BOX && N == 16 && D != 256 ? 2 : 1;
+    static constexpr int per_sm = BOX && N <= 32 && D != 256 ? 2 : 1;
     static constexpr int wide = D == 128 ? 1 : 2;                      // slots in the room of one of 128 components
-    static constexpr int k_slots = D == 256 ? 1 : wide * (per_sm == 2 ? 2 : N == 16 ? 3 : 2), v_slots = D == 256 ? 2 : wide * (per_sm == 2 ? 1 : N == 64 ? 2 : 3);
+    static constexpr int k_slots = D == 256 ? 1 : wide * (per_sm == 2 ? (N == 16 ? 2 : 1) : N == 16 ? 3 : 2), v_slots = D == 256 ? 2 : wide * (per_sm == 2 ? 1 : N == 64 ? 2 : 3);
     static constexpr int slots = k_slots + v_slots;
     static constexpr int q_bytes = blocks * N * 128, q_bufs = D == 256 ? 1 : 2;
     static constexpr int p_bytes = N * kTN * 2, p_bufs = D == 256 || per_sm == 2 ? 1 : 2;
     static constexpr int o_blocks = D == 256 ? 2 : 1;
     // softmax: groups of four warps, which share the rows; N / groups of them a thread
-    static constexpr int groups = N == 16 ? 1 : 2, C = N / groups, soft = 128 * groups;
+    static constexpr int groups = N == 16 || per_sm == 2 ? 1 : 2, C = N / groups, soft = 128 * groups;
     static constexpr int pair = per_sm == 2 ? 1 : 2;                   // warps that copy keys in boxes, and as many for values
     static constexpr int copy = BOX ? 64 * pair : 128, q_copy = BOX ? 32 * pair : 128, threads = soft + copy + 64;
     static constexpr int tmem = N == 64 || o_blocks * N == 64 ? 256 : 128;   // S twice, O twice
