@@ -29,10 +29,10 @@ template <int D, int N, bool BOX> struct Few {
     // Two CTAs an SM where the rows are fewest (their chains of small steps hide each other's latencies), else one with all of the shared memory.
     static constexpr int per_sm = BOX && N <= 32 && D != 256 ? 2 : 1;
     static constexpr int wide = D == 128 ? 1 : 2;                      // slots in the room of one of 128 components
-    static constexpr int k_slots = D == 256 ? 1 : wide * (per_sm == 2 ? (N == 16 ? 2 : 1) : N == 16 ? 3 : 2), v_slots = D == 256 ? 2 : wide * (per_sm == 2 ? 1 : N == 64 ? 2 : 3);
+    static constexpr int k_slots = D == 256 ? 1 : wide * (per_sm == 2 ? 1 : N == 16 ? 3 : 2), v_slots = D == 256 ? 2 : wide * (per_sm == 2 ? 1 : N == 64 ? 2 : 3);
     static constexpr int slots = k_slots + v_slots;
     static constexpr int q_bytes = blocks * N * 128, q_bufs = D == 256 ? 1 : 2;
-    static constexpr int p_bytes = N * kTN * 2, p_bufs = D == 256 || per_sm == 2 ? 1 : 2;
+    static constexpr int p_bytes = N * kTN * 2, p_bufs = D == 256 ? 1 : 2;
     static constexpr int o_blocks = D == 256 ? 2 : 1;
     // softmax: groups of four warps, which share the rows; N / groups of them a thread
     static constexpr int groups = N == 16 || per_sm == 2 ? 1 : 2, C = N / groups, soft = 128 * groups;
@@ -85,17 +85,30 @@ __device__ __forceinline__ uint64_t desc_p(uint32_t addr) { return (uint64_t)((a
 // What rows row0 .. row0 + n - 1 (n <= 32) see of a warp's 32 positions t .. t+31, turned round: bit r says whether row row0 + r sees this lane's.
 __device__ __noinline__ uint32_t seen_rows(const AttendArgs& a, const Session x, int row0, int n, int t, uint32_t valid) {
     const int lane = threadIdx.x & 31;
-    const uint32_t see = lane < n ? valid & seen_bits(a, x, (row0 + lane) / a.group, t) : 0u;
-    uint32_t mine = 0;
-    for (int k = 0; k < 32; ++k) {
-        const uint32_t who = __ballot_sync(kFull, see >> k & 1u);
-        if (k == lane) mine = who;
+    uint32_t v = lane < n ? valid & seen_bits(a, x, (row0 + lane) / a.group, t) : 0u;
+    uint32_t low = 0x0000ffffu;                   // a 32 x 32 transposition: blocks of 16, 8, ... 1 bits change places with the lane that far away
+#pragma unroll
+    for (int j = 16; j > 0; j >>= 1) {
+        const uint32_t other = __shfl_xor_sync(kFull, v, j);
+        v = lane & j ? (v & ~low) | (other >> j & low) : (v & low) | (other & low) << j;
+        low ^= low << (j >> 1);
     }
-    return mine;
+    return v;
 }
 
 // Weights of 0 do not hide infinities and NaN from the product: at drafted positions they are taken out of V (this thread's vector of it), and put_back
 // adds them to the rows that see them.  Returns whether there were any.
+template <class T, int D>
+__device__ __forceinline__ bool special(const uint8_t* tile, int pos) {
+    constexpr uint32_t all = Kind<T>::exponent * 0x10001u, one = (0x8000u - Kind<T>::exponent) * 0x10001u;
+    uint32_t hit = 0;                             // an exponent of ones carries into the sign
+#pragma unroll 4
+    for (int e = 0; e < D / 8; ++e) {
+        const uint4 v = *reinterpret_cast<const uint4*>(tile + (e >> 3) * (kTN * 128) + pos * 128 + (((e & 7) ^ (pos & 7)) << 4));
+        hit |= ((v.x & all) + one) | ((v.y & all) + one) | ((v.z & all) + one) | ((v.w & all) + one);
+    }
+    return hit & 0x80008000u;
+}
 template <class T, int D>
 __device__ __noinline__ bool take_out(uint8_t* tile, int pos) {
     bool any = false;
@@ -457,149 +470,153 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
             fence_before();
             return true;
         };
-        for (int x = 0; sx.more(); ++x, sx.next(p, b, a)) {
-            const int t0 = (sx.w.tile + sx.j) * tile_pos;
-            const int in_use = (sx.w.rows(a) - col0 + 3) & ~3;   // of the group's rows, in fours; the others' weights may be anything
-            const bool first = sx.j == 0, drafted = t0 + tile_pos > sx.w.x.len;
-            ok = ok && mbar_wait(sfull + 8 * (x & 1), (uint32_t)(x >> 1) & 1u, failed, status);
-            if (x >= F::p_bufs) ok = ok && mbar_wait(ofull + 8 * ((x - F::p_bufs) & 1), (uint32_t)((x - F::p_bufs) >> 1) & 1u, failed, status);
-            ok = __all_sync(kFull, ok);
-            fence_after();
-            const uint32_t s_at = tmem + (x & 1) * N + col0 + lanes;
-            const uint4 valid = *reinterpret_cast<const uint4*>(words + x % kWords * 4);
-            const bool may_hide = a.mask != nullptr || sx.w.x.n > 1, hide = may_hide && drafted;
-            const bool masked = hide || (valid.x & valid.y & valid.z & valid.w) != ~0u;
-            uint32_t vis = 0;                         // the group's rows that see this thread's position
-            if (masked) {
-                const uint32_t mine = words[x % kWords * 4 + quarter];
-                vis = hide ? seen_rows(a, sx.w.x, sx.w.rt * N + col0, sx.w.rows(a) - col0, t0 + 32 * quarter, mine) : mine >> lane & 1u ? ~0u : 0u;
-            }
-            uint32_t s[16];                           // 16 rows' scores at a time; more of them stay in tensor memory meanwhile
-            auto scores = [&](int ch) {
-                tmem_ld16(s_at + 16 * ch, s);
-                wait_ld(s);
+        for (int x = 0;; ++x) {
+            const bool more = x < total, first = more && sx.j == 0;
+            if (more) {
+                const int t0 = (sx.w.tile + sx.j) * tile_pos;
+                const int in_use = (sx.w.rows(a) - col0 + 3) & ~3;   // of the group's rows, in fours; the others' weights may be anything
+                const bool drafted = t0 + tile_pos > sx.w.x.len;
+                ok = ok && mbar_wait(sfull + 8 * (x & 1), (uint32_t)(x >> 1) & 1u, failed, status);
+                if (x >= F::p_bufs) ok = ok && mbar_wait(ofull + 8 * ((x - F::p_bufs) & 1), (uint32_t)((x - F::p_bufs) >> 1) & 1u, failed, status);
+                ok = __all_sync(kFull, ok);
+                fence_after();
+                const uint32_t s_at = tmem + (x & 1) * N + col0 + lanes;
+                const uint4 valid = *reinterpret_cast<const uint4*>(words + x % kWords * 4);
+                const bool may_hide = a.mask != nullptr || sx.w.x.n > 1, hide = may_hide && drafted;
+                const bool masked = hide || (valid.x & valid.y & valid.z & valid.w) != ~0u;
+                uint32_t vis = 0;                         // the group's rows that see this thread's position
                 if (masked) {
-                    const uint32_t mine = vis >> (16 * ch);
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = mine >> r & 1u ? s[r] : 0xff800000u;
+                    const uint32_t mine = words[x % kWords * 4 + quarter];
+                    vis = hide ? seen_rows(a, sx.w.x, sx.w.rt * N + col0, sx.w.rows(a) - col0, t0 + 32 * quarter, mine) : mine >> lane & 1u ? ~0u : 0u;
                 }
-            };
-            // exponents relative to base, four rows from r on
-            auto exponents = [&](int r, float* e) {
-                const ulonglong2 base = *reinterpret_cast<const ulonglong2*>(base_s + col0 + r);
-                const int k = r & 15;
-                unpack2(fma2(pack2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, base.x), e[0], e[1]);
-                unpack2(fma2(pack2(__uint_as_float(s[k + 2]), __uint_as_float(s[k + 3])), c2, base.y), e[2], e[3]);
-            };
-            if (C == 16) scores(0);
-            float high = -INFINITY;                   // one above the border asks for a new maximum (rows without one have a base far below)
-            if (!first) {
+                uint32_t s[16];                           // 16 rows' scores at a time; more of them stay in tensor memory meanwhile
+                auto scores = [&](int ch) {
+                    tmem_ld16(s_at + 16 * ch, s);
+                    wait_ld(s);
+                    if (masked) {
+                        const uint32_t mine = vis >> (16 * ch);
 #pragma unroll
-                for (int r = 0; r < C; r += 4) {
-                    if (r >= in_use) break;
-                    if (C > 16 && (r & 15) == 0) scores(r >> 4);
-                    float e[4];
-                    exponents(r, e);
-                    high = fmaxf(high, fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3])));
-                }
-            }
-            if (vote_any<2, F::soft>(first || !ok || high > kRaise + Kind<T>::shift)) {
-                // some row's maximum rises: all warps' maxima, the factors, and what has been summed so far
-#pragma unroll
-                for (int r = 0; r < C; ++r) {
-                    if (r >= in_use) break;
-                    if (C > 16 && (r & 15) == 0) scores(r >> 4);
-                    const float m = warp_max(__uint_as_float(s[r & 15]));
-                    if (lane == r) warp_s[quarter * N + col0 + r] = m;
-                }
-                if (!first) ok = ok && mbar_wait(ofull + 8 * ((x - 1) & 1), (uint32_t)((x - 1) >> 1) & 1u, failed, status);
-                if (!vote_all<2, F::soft>(ok)) { ok = false; break; }
-                if (tid < N) {
-                    const float now = fmaxf(fmaxf(warp_s[tid], warp_s[N + tid]), fmaxf(warp_s[2 * N + tid], warp_s[3 * N + tid])) * (a.scale * 1.44269504088896f);
-                    const float old = first ? -INFINITY : top_s[tid];
-                    const float top = now > old + kRaise ? now : old;
-                    top_s[tid] = top;
-                    base_s[tid] = top == -INFINITY ? 1e30f : Kind<T>::shift - top;
-                    factor_s[tid] = top == old ? 1.f : old == -INFINITY ? 0.f : exp2_approx(old - top);
-                }
-                vote_all<2, F::soft>(true);
-                if (first) {
-#pragma unroll
-                    for (int r = 0; r < C / 2; ++r) sum[r] = 0ull;
-                } else {
-                    fence_after();
-#pragma unroll
-                    for (int r = 0; r < C; r += 2) {
-                        float lo, hi;
-                        unpack2(sum[r / 2], lo, hi);
-                        sum[r / 2] = pack2(lo * factor_s[col0 + r], hi * factor_s[col0 + r + 1]);
+                        for (int r = 0; r < 16; ++r) s[r] = mine >> r & 1u ? s[r] : 0xff800000u;
                     }
-#pragma unroll 1
-                    for (int ch = 0; ch < F::o_blocks * C / 16; ++ch) {
-                        uint32_t y[16];
-                        const uint32_t at = o_at + ((sx.piece & 1) * F::o_blocks + 16 * ch / C) * N + 16 * ch % C;
-                        tmem_ld16(at, y);
-                        wait_ld(y);
+                };
+                // exponents relative to base, four rows from r on
+                auto exponents = [&](int r, float* e) {
+                    const ulonglong2 base = *reinterpret_cast<const ulonglong2*>(base_s + col0 + r);
+                    const int k = r & 15;
+                    unpack2(fma2(pack2(__uint_as_float(s[k]), __uint_as_float(s[k + 1])), c2, base.x), e[0], e[1]);
+                    unpack2(fma2(pack2(__uint_as_float(s[k + 2]), __uint_as_float(s[k + 3])), c2, base.y), e[2], e[3]);
+                };
+                if (C == 16) scores(0);
+                float high = -INFINITY;                   // one above the border asks for a new maximum (rows without one have a base far below)
+                if (!first) {
 #pragma unroll
-                        for (int r = 0; r < 16; ++r) {
-                            const float f = factor_s[col0 + (16 * ch + r) % C];
-                            y[r] = __float_as_uint(f == 0.f ? 0.f : __uint_as_float(y[r]) * f);
+                    for (int r = 0; r < C; r += 4) {
+                        if (r >= in_use) break;
+                        if (C > 16 && (r & 15) == 0) scores(r >> 4);
+                        float e[4];
+                        exponents(r, e);
+                        high = fmaxf(high, fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3])));
+                    }
+                }
+                if (vote_any<2, F::soft>(first || !ok || high > kRaise + Kind<T>::shift)) {
+                    // some row's maximum rises: all warps' maxima, the factors, and what has been summed so far
+#pragma unroll
+                    for (int r = 0; r < C; ++r) {
+                        if (r >= in_use) break;
+                        if (C > 16 && (r & 15) == 0) scores(r >> 4);
+                        const float m = warp_max(__uint_as_float(s[r & 15]));
+                        if (lane == r) warp_s[quarter * N + col0 + r] = m;
+                    }
+                    if (!first) ok = ok && mbar_wait(ofull + 8 * ((x - 1) & 1), (uint32_t)((x - 1) >> 1) & 1u, failed, status);
+                    if (!vote_all<2, F::soft>(ok)) { ok = false; break; }
+                    if (tid < N) {
+                        const float now = fmaxf(fmaxf(warp_s[tid], warp_s[N + tid]), fmaxf(warp_s[2 * N + tid], warp_s[3 * N + tid])) * (a.scale * 1.44269504088896f);
+                        const float old = first ? -INFINITY : top_s[tid];
+                        const float top = now > old + kRaise ? now : old;
+                        top_s[tid] = top;
+                        base_s[tid] = top == -INFINITY ? 1e30f : Kind<T>::shift - top;
+                        factor_s[tid] = top == old ? 1.f : old == -INFINITY ? 0.f : exp2_approx(old - top);
+                    }
+                    vote_all<2, F::soft>(true);
+                    if (first) {
+#pragma unroll
+                        for (int r = 0; r < C / 2; ++r) sum[r] = 0ull;
+                    } else {
+                        fence_after();
+#pragma unroll
+                        for (int r = 0; r < C; r += 2) {
+                            float lo, hi;
+                            unpack2(sum[r / 2], lo, hi);
+                            sum[r / 2] = pack2(lo * factor_s[col0 + r], hi * factor_s[col0 + r + 1]);
                         }
-                        tmem_st16(at, y);
+#pragma unroll 1
+                        for (int ch = 0; ch < F::o_blocks * C / 16; ++ch) {
+                            uint32_t y[16];
+                            const uint32_t at = o_at + ((sx.piece & 1) * F::o_blocks + 16 * ch / C) * N + 16 * ch % C;
+                            tmem_ld16(at, y);
+                            wait_ld(y);
+#pragma unroll
+                            for (int r = 0; r < 16; ++r) {
+                                const float f = factor_s[col0 + (16 * ch + r) % C];
+                                y[r] = __float_as_uint(f == 0.f ? 0.f : __uint_as_float(y[r]) * f);
+                            }
+                            tmem_st16(at, y);
+                        }
+                        wait_st();
                     }
-                    wait_st();
                 }
-            }
-            uint8_t* pp = ps + x % F::p_bufs * F::p_bytes + col0 / 8 * 2048 + pos * 16;
+                uint8_t* pp = ps + x % F::p_bufs * F::p_bytes + col0 / 8 * 2048 + pos * 16;
 #pragma unroll
-            for (int r = 0; r < C; r += 8) {
-                if (r >= in_use) break;
-                if (C > 16 && (r & 15) == 0) scores(r >> 4);
-                uint32_t y[4] = {0, 0, 0, 0};
+                for (int r = 0; r < C; r += 8) {
+                    if (r >= in_use) break;
+                    if (C > 16 && (r & 15) == 0) scores(r >> 4);
+                    uint32_t y[4] = {0, 0, 0, 0};
 #pragma unroll
-                for (int k = 0; k < 8; k += 4) {
-                    if (r + k >= in_use) break;
-                    float e[4];
-                    exponents(r + k, e);
+                    for (int k = 0; k < 8; k += 4) {
+                        if (r + k >= in_use) break;
+                        float e[4];
+                        exponents(r + k, e);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) e[i] = exp2_approx(e[i]);                 // a score of -inf has the weight 0
-                    sum[(r + k) / 2] = add2(sum[(r + k) / 2], pack2(e[0], e[1]));
-                    sum[(r + k) / 2 + 1] = add2(sum[(r + k) / 2 + 1], pack2(e[2], e[3]));
-                    y[k / 2] = Kind<T>::pack(e[0], e[1]);
-                    y[k / 2 + 1] = Kind<T>::pack(e[2], e[3]);
+                        for (int i = 0; i < 4; ++i) e[i] = exp2_approx(e[i]);                 // a score of -inf has the weight 0
+                        sum[(r + k) / 2] = add2(sum[(r + k) / 2], pack2(e[0], e[1]));
+                        sum[(r + k) / 2 + 1] = add2(sum[(r + k) / 2 + 1], pack2(e[2], e[3]));
+                        y[k / 2] = Kind<T>::pack(e[0], e[1]);
+                        y[k / 2 + 1] = Kind<T>::pack(e[2], e[3]);
+                    }
+                    *reinterpret_cast<uint4*>(pp + (r / 8) * 2048) = make_uint4(y[0], y[1], y[2], y[3]);
                 }
-                *reinterpret_cast<uint4*>(pp + (r / 8) * 2048) = make_uint4(y[0], y[1], y[2], y[3]);
+                // V of positions that do not exist is whatever the boxes brought or left: zeros instead, since weights of 0 do not hide it
+                const bool blank = BOX && masked && pos < tile_pos && !(words[x % kWords * 4 + quarter] >> lane & 1u);
+                if ((hide || (BOX && masked)) && wid < 4) {
+                    ok = ok && mbar_wait(v_full + 8 * (x % v_slots), (uint32_t)(x / v_slots) & 1u, failed, status);
+                    uint8_t* tile = ring + (k_slots + x % v_slots) * F::slot;
+                    if (ok && blank)
+                        for (int e = 0; e < F::blocks * 8; ++e)
+                            *reinterpret_cast<uint4*>(tile + (e >> 3) * (kTN * 128) + pos * 128 + (((e & 7) ^ (pos & 7)) << 4)) = make_uint4(0, 0, 0, 0);
+                    else if (ok && hide && pos < tile_pos && t0 + pos >= sx.w.x.len && t0 + pos < sx.w.x.kv && special<T, D>(tile, pos) && take_out<T, D>(tile, pos))
+                        dirty[sx.piece & 1] = (uint32_t)sx.piece + 1u;
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // P (and V) as the product reads them
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(pfull + 8 * (x & 1));
             }
-            // V of positions that do not exist is whatever the boxes brought or left: zeros instead, since weights of 0 do not hide it
-            const bool blank = BOX && masked && pos < tile_pos && !(words[x % kWords * 4 + quarter] >> lane & 1u);
-            if ((hide || (BOX && masked)) && wid < 4) {
-                ok = ok && mbar_wait(v_full + 8 * (x % v_slots), (uint32_t)(x / v_slots) & 1u, failed, status);
-                uint8_t* tile = ring + (k_slots + x % v_slots) * F::slot;
-                if (ok && blank)
-                    for (int e = 0; e < F::blocks * 8; ++e)
-                        *reinterpret_cast<uint4*>(tile + (e >> 3) * (kTN * 128) + pos * 128 + (((e & 7) ^ (pos & 7)) << 4)) = make_uint4(0, 0, 0, 0);
-                else if (ok && hide && pos < tile_pos && t0 + pos >= sx.w.x.len && t0 + pos < sx.w.x.kv && take_out<T, D>(tile, pos))
-                    dirty[sx.piece & 1] = (uint32_t)sx.piece + 1u;
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // P (and V) as the product reads them
-            fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(pfull + 8 * (x & 1));
             // the results of the piece before, whose last product has had this tile's time to finish
-            if (first && x > 0 && !(ok = results(x - 1))) break;
-            if (!sx.last()) continue;
-            // the piece is done: its sums over the positions
-            if (tid == 0) *done = sx;
+            if (x > 0 && (first || !more) && !(ok = results(x - 1))) break;
+            if (!more) break;
+            if (sx.last()) {                          // the piece is done: its sums over the positions
+                if (tid == 0) *done = sx;
 #pragma unroll
-            for (int ch = 0; ch < C / 16; ++ch) {
-                float l[16];
+                for (int ch = 0; ch < C / 16; ++ch) {
+                    float l[16];
 #pragma unroll
-                for (int r = 0; r < 16; r += 2) unpack2(sum[8 * ch + r / 2], l[r], l[r + 1]);
-                const float v = warp_sums(l, lane);
-                if (!(lane & 1)) sum_s[quarter * N + col0 + 16 * ch + lane / 2] = v;
+                    for (int r = 0; r < 16; r += 2) unpack2(sum[8 * ch + r / 2], l[r], l[r + 1]);
+                    const float v = warp_sums(l, lane);
+                    if (!(lane & 1)) sum_s[quarter * N + col0 + 16 * ch + lane / 2] = v;
+                }
+                if (tid < N) last_top_s[tid] = top_s[tid];
             }
-            if (tid < N) last_top_s[tid] = top_s[tid];
-            if (x + 1 == total) results(x);
+            sx.next(p, b, a);
         }
     }
     fence_before();
