@@ -1,5 +1,6 @@
 // Tree attention: what its kernels share (the sequence of position tiles and a CTA's range of it, masks, the tensor core's instructions).
 #pragma once
+#include <cuda.h>
 #include <cuda_bf16.h>
 
 #include "plc_pages.cuh"
@@ -30,6 +31,8 @@ struct AttendPlan { int row_tile, grid, part_rows; uint64_t bytes; };
 
 cudaError_t launch_attend_few_f16(const PoolDev& p, const BookDev& b, const AttendArgs& a, const AttendPlan& x, uint32_t* status, cudaStream_t st);
 cudaError_t launch_attend_few_bf16(const PoolDev& p, const BookDev& b, const AttendArgs& a, const AttendPlan& x, uint32_t* status, cudaStream_t st);
+cudaError_t launch_attend_many_f16(const PoolDev& p, const BookDev& b, const AttendArgs& a, const AttendPlan& x, uint32_t* status, cudaStream_t st);
+cudaError_t launch_attend_many_bf16(const PoolDev& p, const BookDev& b, const AttendArgs& a, const AttendPlan& x, uint32_t* status, cudaStream_t st);
 
 #ifdef __CUDACC__
 namespace {
@@ -117,6 +120,12 @@ template <int N> __device__ __forceinline__ void wait_ld(uint32_t (&r)[N]) {
     for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
 }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// The larger of three (sm_100 has it as one instruction); NaN only if all are.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -281,6 +290,104 @@ template <int ROWS> struct Tiles {
     }
 };
 
+// Weights of 0 do not hide infinities and NaN from the product: at drafted positions they are taken out of V (one position's vector in a tile of TN),
+// and added to the rows that see them at the end.  Returns whether there were any.
+template <class T, int D, int TN>
+__device__ __forceinline__ bool special(const uint8_t* tile, int pos) {
+    constexpr uint32_t all = Kind<T>::exponent * 0x10001u, one = (0x8000u - Kind<T>::exponent) * 0x10001u;
+    uint32_t hit = 0;                             // an exponent of ones carries into the sign
+#pragma unroll 4
+    for (int e = 0; e < D / 8; ++e) {
+        const uint4 v = *reinterpret_cast<const uint4*>(tile + (e >> 3) * (TN * 128) + pos * 128 + (((e & 7) ^ (pos & 7)) << 4));
+        hit |= ((v.x & all) + one) | ((v.y & all) + one) | ((v.z & all) + one) | ((v.w & all) + one);
+    }
+    return hit & 0x80008000u;
+}
+template <class T, int D, int TN>
+__device__ __noinline__ bool take_out(uint8_t* tile, int pos) {
+    bool any = false;
+    for (int e = 0; e < D / 8; ++e) {
+        uint4* at = reinterpret_cast<uint4*>(tile + (e >> 3) * (TN * 128) + pos * 128 + (((e & 7) ^ (pos & 7)) << 4));
+        uint4 v = *at;
+        uint32_t* h = reinterpret_cast<uint32_t*>(&v);
+        bool hit = false;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if ((h[k] & Kind<T>::exponent) == Kind<T>::exponent) { h[k] &= 0xffff0000u; hit = true; }
+            if ((h[k] >> 16 & Kind<T>::exponent) == Kind<T>::exponent) { h[k] &= 0xffffu; hit = true; }
+        }
+        if (hit) *at = v;
+        any |= hit;
+    }
+    return any;
+}
+
+// Copies of the keys (kv = 0) or values (1) of a CTA's range into their ring, by `pair` warps of which each issues every pair-th box of a tile (box_pos positions
+// of one page, 64 components wide).  A lane looks a box's page up, a tile ahead.  The first warp of the keys also writes which positions of a
+// tile exist (a bit each); load_q(tile, ok) is called at the start of each piece for the keys.
+template <int ROWS, int BLOCKS, int TN, class Q>
+__device__ __forceinline__ void copy_boxes(const PoolDev& p, const BookDev& b, const AttendArgs& a, const CUtensorMap& map, const Walk<ROWS>& from, long long total, int kv, int half,
+                                           int pair, uint32_t ring, int slot_bytes, int slots, uint32_t full, uint32_t empty, uint32_t* words, int word_ring,
+                                           volatile uint32_t* failed, uint32_t* status, Q&& load_q) {
+    const int lane = threadIdx.x & 31;
+    Tiles<ROWS> x;
+    x.start(from, total);
+    int page = -1, slot = 0, issued = 0;
+    bool ok = true;
+    const int my_box = 4 * lane / a.box_pos;         // of the four positions whose validity the lane tells
+    auto look_up = [&]() {                           // -1: behind the last position
+        const int t = (x.w.tile + x.j) * a.tile_pos + lane * a.box_pos, pg = t / p.page_pos;
+        slot = t - pg * p.page_pos;
+        page = lane < a.boxes && t < x.w.x.kv ? b.table[(int64_t)x.w.s * b.max_pages + pg] : -1;
+        if (page == -1 && lane < a.boxes && t < x.w.x.kv) page = -2;
+    };
+    if (total > 0) look_up();
+    for (int n = 0; x.more(); ++n) {
+        if (kv == 0 && x.j == 0) ok = load_q(x, ok);
+        const bool have = page >= 0 && page < p.n_pages;
+        const uint32_t boxes = __ballot_sync(kFull, have);
+        const int here = page, at = slot, h = x.w.h;
+        if (kv == 0 && half == 0) {
+            if (page < -1 || page >= p.n_pages) atomicOr(status, kStRange);
+            const int t = (x.w.tile + x.j) * a.tile_pos + 4 * lane;
+            const int valid = boxes >> (my_box & 31) & 1u && 4 * lane < a.tile_pos ? min(max(x.w.x.kv - t, 0), 4) : 0;
+            const uint32_t word = __reduce_or_sync(0xffu << (lane & 24), ((1u << valid) - 1u) << (4 * (lane & 7)));
+            if ((lane & 7) == 0) words[n % word_ring * 4 + (lane >> 3)] = word;
+        }
+        x.next(p, b, a);
+        if (x.more()) look_up();
+        const int s = n % slots;
+        ok = __all_sync(kFull, ok && mbar_wait(empty + 8 * s, ((uint32_t)(n / slots) & 1u) ^ 1u, failed, status));
+        if (!ok) break;
+        const uint32_t mine = pair == 1 ? boxes : boxes & (half ? 0xaaaaaaaau : 0x55555555u), bar = full + 8 * s;
+        if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(__popc(mine) * a.box_pos * BLOCKS * 128) : "memory");
+        for (int e = half; e < a.boxes; e += pair) {
+            const int pg = __shfl_sync(kFull, here, e), sl = __shfl_sync(kFull, at, e);
+            if (!(mine >> e & 1u) || lane != 0) continue;
+            int c[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) c[k] = a.box_dim[k] == 0 ? sl : a.box_dim[k] == 1 ? h : a.box_dim[k] == 2 ? pg : kv;
+#pragma unroll
+            for (int k = 0; k < BLOCKS; ++k)
+                asm volatile(
+                    "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(
+                        ring + s * slot_bytes + k * (TN * 128) + e * a.box_pos * 128),
+                    "l"(&map), "r"(k * 64), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]), "r"(bar)
+                    : "memory");
+        }
+        issued = n + 1;
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (!ok)                                         // boxes still in flight (none after a complete run) land before the CTA ends
+        for (int n = issued > slots ? issued - slots : 0; n < issued; ++n)
+            for (uint32_t k = 0; k < kSpin; ++k) {
+                uint32_t done;
+                asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                             : "=r"(done) : "r"(full + 8 * (n % slots)), "r"((uint32_t)(n / slots) & 1u) : "memory");
+                if (done) break;
+            }
+}
+
 // Joins the pieces of items that more than one CTA had: block c looks at the boundary between CTAs c - 1 and c, and takes the item if that is the
 // first boundary inside it.  A warp a row; a lane a piece for the weights, then a lane its components with the pieces' loads eight at a time
 // (a piece after the other, 37 pieces took 84 us).
@@ -359,6 +466,52 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
             for (int e = 0; e < VEC; e += 2) reinterpret_cast<uint32_t*>(out)[e / 2] = Kind<T>::pack(o[e] * inv, o[e + 1] * inv);
         if (a.lse && lane == 0) a.lse[n_row * a.heads + head] = sum == 0.f ? -INFINITY : (top - Kind<T>::shift + log2f(sum)) * 0.693147180559945f;
     }
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled_fn() {
+    static const EncodeTiledFn fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess
+                   ? reinterpret_cast<EncodeTiledFn>(f) : nullptr;
+    }();
+    return fn;
+}
+
+// The layer's keys and values in boxes of 64 components by as many positions as a page has whole boxes of (a multiple of the eight
+// rows that the swizzle repeats after, at most `most`).  False where the pool has no such boxes: pages of other sizes, vectors of 32
+// components (a box row would be half a shared memory row), strides that are not positive or not multiples of each other.
+bool make_boxes(const PoolDev& p, AttendArgs& a, bool bf16, int most, CUtensorMap* map) {
+    if (p.d < 64 || p.page_pos % 8) return false;
+    int box = 8;
+    for (int k = 16; k <= most; k += 8)
+        if (p.page_pos % k == 0) box = k;
+    const int64_t stride[4] = {p.sp, p.sh, p.spage, p.skv};
+    const cuuint64_t extent[4] = {(cuuint64_t)p.page_pos, (cuuint64_t)p.H, (cuuint64_t)p.n_pages, 2};
+    int order[4] = {0, 1, 2, 3};
+    for (int i = 0; i < 4; ++i) {
+        if (stride[i] <= 0 || stride[i] >= (1ll << 40)) return false;
+        for (int j = i; j > 0 && stride[order[j]] < stride[order[j - 1]]; --j) { const int t = order[j]; order[j] = order[j - 1]; order[j - 1] = t; }
+    }
+    cuuint64_t dims[5] = {(cuuint64_t)p.d}, strides[4];
+    cuuint32_t boxes[5] = {64}, ones[5] = {1, 1, 1, 1, 1};
+    for (int i = 0; i < 4; ++i) {
+        dims[i + 1] = extent[order[i]];
+        strides[i] = (cuuint64_t)stride[order[i]];
+        boxes[i + 1] = order[i] == 0 ? (cuuint32_t)box : 1;
+        if (i > 0 && strides[i] % strides[i - 1]) return false;
+        a.box_dim[i] = order[i];
+    }
+    const EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn || fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, p.base + (int64_t)a.layer * p.sl, dims, strides, boxes, ones,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return false;
+    a.box_pos = box;
+    a.boxes = most / box;
+    a.tile_pos = box * a.boxes;
+    return true;
 }
 
 template <class T, int D, int ROWS>

@@ -11,8 +11,6 @@
 // A row's maximum is common to the CTA and raised only where some score passes it by 2^3 (a vote of the four warps a tile); each thread sums the
 // weights of its positions, and the sums are joined at the end of an item.
 #pragma once
-#include <cuda.h>
-
 #include "plc_attend.cuh"
 
 namespace plc {
@@ -96,37 +94,6 @@ __device__ __noinline__ uint32_t seen_rows(const AttendArgs& a, const Session x,
     return v;
 }
 
-// Weights of 0 do not hide infinities and NaN from the product: at drafted positions they are taken out of V (this thread's vector of it), and put_back
-// adds them to the rows that see them.  Returns whether there were any.
-template <class T, int D>
-__device__ __forceinline__ bool special(const uint8_t* tile, int pos) {
-    constexpr uint32_t all = Kind<T>::exponent * 0x10001u, one = (0x8000u - Kind<T>::exponent) * 0x10001u;
-    uint32_t hit = 0;                             // an exponent of ones carries into the sign
-#pragma unroll 4
-    for (int e = 0; e < D / 8; ++e) {
-        const uint4 v = *reinterpret_cast<const uint4*>(tile + (e >> 3) * (kTN * 128) + pos * 128 + (((e & 7) ^ (pos & 7)) << 4));
-        hit |= ((v.x & all) + one) | ((v.y & all) + one) | ((v.z & all) + one) | ((v.w & all) + one);
-    }
-    return hit & 0x80008000u;
-}
-template <class T, int D>
-__device__ __noinline__ bool take_out(uint8_t* tile, int pos) {
-    bool any = false;
-    for (int e = 0; e < D / 8; ++e) {
-        uint4* at = reinterpret_cast<uint4*>(tile + (e >> 3) * (kTN * 128) + pos * 128 + (((e & 7) ^ (pos & 7)) << 4));
-        uint4 v = *at;
-        uint32_t* h = reinterpret_cast<uint32_t*>(&v);
-        bool hit = false;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if ((h[k] & Kind<T>::exponent) == Kind<T>::exponent) { h[k] &= 0xffff0000u; hit = true; }
-            if ((h[k] >> 16 & Kind<T>::exponent) == Kind<T>::exponent) { h[k] &= 0xffffu; hit = true; }
-        }
-        if (hit) *at = v;
-        any |= hit;
-    }
-    return any;
-}
 template <class T>
 __device__ __noinline__ void put_back(const PoolDev& p, const BookDev& b, const AttendArgs& a, const Session x, int s, int h, int t0, int t1, int row0, int rows, int d,
                                       const int64_t* row_at, bool whole) {
@@ -229,67 +196,10 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
             return true;
         };
         if constexpr (BOX) {
-            // ---- copies: a warp or two for the keys, as many for the values; of two each issues every other box of a tile (box_pos positions of one
-            // page, 64 components wide).  A lane looks a box's page up, a tile ahead.
-            const int half = (lt >> 5) % F::pair, kv = lt / F::q_copy;
-            Tl x;
-            x.start(w0, total);
-            int page = -1, slot = 0, issued = 0;
-            bool ok = true;
-            const int my_box = 4 * lane / a.box_pos; // of the four positions whose validity the lane tells
-            auto look_up = [&]() {                   // -1: behind the last position
-                const int t = (x.w.tile + x.j) * tile_pos + lane * a.box_pos, pg = t / p.page_pos;
-                slot = t - pg * p.page_pos;
-                page = lane < a.boxes && t < x.w.x.kv ? b.table[(int64_t)x.w.s * b.max_pages + pg] : -1;
-                if (page == -1 && lane < a.boxes && t < x.w.x.kv) page = -2;
-            };
-            const int ring_slots = kv ? v_slots : k_slots;
-            const uint32_t my_full = kv ? v_full : full, my_empty = kv ? v_empty : empty, my_ring = kv ? v_ring_s : ring_s;
-            if (total > 0) look_up();
-            for (int n = 0; x.more(); ++n) {
-                if (kv == 0 && x.j == 0) ok = load_q(x, ok);
-                const bool have = page >= 0 && page < p.n_pages;
-                const uint32_t boxes = __ballot_sync(kFull, have);
-                const int here = page, at = slot, h = x.w.h;
-                if (kv == 0 && half == 0) {
-                    if (page < -1 || page >= p.n_pages) atomicOr(status, kStRange);
-                    const int t = (x.w.tile + x.j) * tile_pos + 4 * lane;
-                    const int valid = boxes >> (my_box & 31) & 1u && 4 * lane < tile_pos ? min(max(x.w.x.kv - t, 0), 4) : 0;
-                    const uint32_t word = __reduce_or_sync(0xffu << (lane & 24), ((1u << valid) - 1u) << (4 * (lane & 7)));
-                    if ((lane & 7) == 0) words[n % kWords * 4 + (lane >> 3)] = word;
-                }
-                x.next(p, b, a);
-                if (x.more()) look_up();
-                const int s = n % ring_slots;
-                ok = __all_sync(kFull, ok && mbar_wait(my_empty + 8 * s, ((uint32_t)(n / ring_slots) & 1u) ^ 1u, failed, status));
-                if (!ok) break;
-                const uint32_t mine = F::pair == 1 ? boxes : boxes & (half ? 0xaaaaaaaau : 0x55555555u), bar = my_full + 8 * s;
-                if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(__popc(mine) * a.box_pos * F::blocks * 128) : "memory");
-                for (int e = half; e < a.boxes; e += F::pair) {
-                    const int pg = __shfl_sync(kFull, here, e), sl = __shfl_sync(kFull, at, e);
-                    if (!(mine >> e & 1u) || lane != 0) continue;
-                    int c[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) c[k] = a.box_dim[k] == 0 ? sl : a.box_dim[k] == 1 ? h : a.box_dim[k] == 2 ? pg : kv;
-#pragma unroll
-                    for (int k = 0; k < F::blocks; ++k)
-                        asm volatile(
-                            "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(
-                                my_ring + s * F::slot + k * (kTN * 128) + e * a.box_pos * 128),
-                            "l"(&map), "r"(k * 64), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]), "r"(bar)
-                            : "memory");
-                }
-                issued = n + 1;
-            }
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            if (!ok)                                 // boxes still in flight (none after a complete run) land before the CTA ends
-                for (int n = issued > ring_slots ? issued - ring_slots : 0; n < issued; ++n)
-                    for (uint32_t k = 0; k < kSpin; ++k) {
-                        uint32_t done;
-                        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                                     : "=r"(done) : "r"(my_full + 8 * (n % ring_slots)), "r"((uint32_t)(n / ring_slots) & 1u) : "memory");
-                        if (done) break;
-                    }
+            // ---- copies: a warp or two for the keys, as many for the values
+            const int kv = lt / F::q_copy;
+            copy_boxes<N, F::blocks, kTN>(p, b, a, map, w0, total, kv, (lt >> 5) % F::pair, F::pair, kv ? v_ring_s : ring_s, F::slot, kv ? v_slots : k_slots,
+                                          kv ? v_full : full, kv ? v_empty : empty, words, kWords, failed, status, load_q);
         } else {
             // ---- copies, four warps, position by position (pages of any size)
             constexpr int step = F::copy / pieces, rounds = kTN / step;   // vectors a round
@@ -593,7 +503,7 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
                     if (ok && blank)
                         for (int e = 0; e < F::blocks * 8; ++e)
                             *reinterpret_cast<uint4*>(tile + (e >> 3) * (kTN * 128) + pos * 128 + (((e & 7) ^ (pos & 7)) << 4)) = make_uint4(0, 0, 0, 0);
-                    else if (ok && hide && pos < tile_pos && t0 + pos >= sx.w.x.len && t0 + pos < sx.w.x.kv && special<T, D>(tile, pos) && take_out<T, D>(tile, pos))
+                    else if (ok && hide && pos < tile_pos && t0 + pos >= sx.w.x.len && t0 + pos < sx.w.x.kv && special<T, D, kTN>(tile, pos) && take_out<T, D, kTN>(tile, pos))
                         dirty[sx.piece & 1] = (uint32_t)sx.piece + 1u;
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // P (and V) as the product reads them
@@ -627,52 +537,6 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
     }
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeTiledFn encode_tiled_fn() {
-    static const EncodeTiledFn fn = [] {
-        void* f = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess
-                   ? reinterpret_cast<EncodeTiledFn>(f) : nullptr;
-    }();
-    return fn;
-}
-
-// The layer's keys and values in boxes of 64 components by as many positions as a page has whole boxes of (a multiple of the eight
-// rows that the swizzle repeats after, at most 128).  False where the pool has no such boxes: pages of other sizes, vectors of 32
-// components (a box row would be half a shared memory row), strides that are not positive or not multiples of each other.
-bool make_boxes(const PoolDev& p, AttendArgs& a, bool bf16, CUtensorMap* map) {
-    if (p.d < 64 || p.page_pos % 8) return false;
-    int box = 8;
-    for (int k = 16; k <= 128; k += 8)
-        if (p.page_pos % k == 0) box = k;
-    const int64_t stride[4] = {p.sp, p.sh, p.spage, p.skv};
-    const cuuint64_t extent[4] = {(cuuint64_t)p.page_pos, (cuuint64_t)p.H, (cuuint64_t)p.n_pages, 2};
-    int order[4] = {0, 1, 2, 3};
-    for (int i = 0; i < 4; ++i) {
-        if (stride[i] <= 0 || stride[i] >= (1ll << 40)) return false;
-        for (int j = i; j > 0 && stride[order[j]] < stride[order[j - 1]]; --j) { const int t = order[j]; order[j] = order[j - 1]; order[j - 1] = t; }
-    }
-    cuuint64_t dims[5] = {(cuuint64_t)p.d}, strides[4];
-    cuuint32_t boxes[5] = {64}, ones[5] = {1, 1, 1, 1, 1};
-    for (int i = 0; i < 4; ++i) {
-        dims[i + 1] = extent[order[i]];
-        strides[i] = (cuuint64_t)stride[order[i]];
-        boxes[i + 1] = order[i] == 0 ? (cuuint32_t)box : 1;
-        if (i > 0 && strides[i] % strides[i - 1]) return false;
-        a.box_dim[i] = order[i];
-    }
-    const EncodeTiledFn fn = encode_tiled_fn();
-    if (!fn || fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 5, p.base + (int64_t)a.layer * p.sl, dims, strides, boxes, ones,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-        return false;
-    a.box_pos = box;
-    a.boxes = 128 / box;
-    a.tile_pos = box * a.boxes;
-    return true;
-}
-
 template <class T, int D, int N, bool BOX>
 cudaError_t launch(const PoolDev& p, const BookDev& b, const AttendArgs& a, const CUtensorMap& map, const AttendPlan& x, uint32_t* status, cudaStream_t st) {
     using F = Few<D, N, BOX>;
@@ -688,7 +552,7 @@ cudaError_t launch_few(const PoolDev& p, const BookDev& b, const AttendArgs& arg
     AttendArgs a = args;
     a.tile_pos = kTN;
     CUtensorMap map{};
-    const bool boxes = make_boxes(p, a, bf16, &map), least = x.row_tile == 16, mid = x.row_tile == 32;
+    const bool boxes = make_boxes(p, a, bf16, kTN, &map), least = x.row_tile == 16, mid = x.row_tile == 32;
     if (boxes) switch (p.d) {
             case 64: return least ? launch<T, 64, 16, true>(p, b, a, map, x, status, st) : mid ? launch<T, 64, 32, true>(p, b, a, map, x, status, st) : launch<T, 64, 64, true>(p, b, a, map, x, status, st);
             case 128: return least ? launch<T, 128, 16, true>(p, b, a, map, x, status, st) : mid ? launch<T, 128, 32, true>(p, b, a, map, x, status, st) : launch<T, 128, 64, true>(p, b, a, map, x, status, st);
