@@ -15,16 +15,17 @@ namespace {
 
 constexpr int kWordRing = 8;                      // tiles whose validity words are kept: more than the copies can be ahead of the softmax
 
-template <int D, int NT> struct Shape {
+template <int D, int NT, bool BOX> struct Shape {
     static constexpr int TN = D == 256 ? 64 : 128;                     // positions a tile: S and O of a CTA's row tiles fit in tensor memory
     static constexpr int blocks = (D + 63) / 64;                       // 128-byte wide column blocks (32 components: half of one)
     static constexpr int DV = blocks * 64;                             // columns of O
-    static constexpr int stages = D == 128 ? NT : NT == 2 ? 3 : 2;
+    // tiles kept of K and of V: as many as fit, of K one more (its next tile is waited for first)
+    static constexpr int vstages = D == 128 ? NT : NT == 1 ? 2 : BOX ? 4 : 3, kstages = BOX && (D != 128 || NT == 2) ? vstages + 1 : vstages;
     static constexpr int q_bytes = blocks * 128 * 128, kv_bytes = blocks * TN * 128;
     static constexpr int tmem = NT * (TN + DV) > 256 ? 512 : 256;
     static constexpr int rows = NT * 128, soft = NT * 128, threads = soft + 128;
     static constexpr int per_sm = NT == 1 && D != 256 ? 2 : 1;
-    static constexpr size_t smem = (size_t)NT * q_bytes + 2 * stages * kv_bytes + 2 * TN * 8 + 1024 + 512;
+    static constexpr size_t smem = (size_t)NT * q_bytes + (kstages + vstages) * kv_bytes + (BOX ? 0 : 2 * TN * 8) + 1024 + 512;
 };
 
 // Scores of positions that the row does not see become -inf, in place.
@@ -63,31 +64,33 @@ __device__ __noinline__ void put_back_row(const PoolDev& p, const BookDev& b, co
 }
 
 template <class T, int D, int NT, bool BOX>
-__global__ void __launch_bounds__(Shape<D, NT>::threads, Shape<D, NT>::per_sm)
+__global__ void __launch_bounds__(Shape<D, NT, BOX>::threads, Shape<D, NT, BOX>::per_sm)
 many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b, const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map, uint32_t* status) {
-    using Sh = Shape<D, NT>;
+    using Sh = Shape<D, NT, BOX>;
     using Wk = Walk<Sh::rows>;
-    constexpr int TN = Sh::TN, stages = Sh::stages, soft_warps = Sh::soft / 32, mma_warp = soft_warps + 3, loaders = BOX ? 64 : 96;
+    constexpr int TN = Sh::TN, kst = Sh::kstages, vst = Sh::vstages, soft_warps = Sh::soft / 32, mma_warp = soft_warps + 3, loaders = BOX ? 64 : 96;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* ks = smem + NT * Sh::q_bytes;
-    uint8_t* vs = ks + stages * Sh::kv_bytes;
-    int64_t* offs = reinterpret_cast<int64_t*>(vs + stages * Sh::kv_bytes);             // [2][TN]
-    uint32_t* words = reinterpret_cast<uint32_t*>(offs + 2 * TN);                       // [kWordRing][4]
+    uint8_t* vs = ks + kst * Sh::kv_bytes;
+    int64_t* offs = reinterpret_cast<int64_t*>(vs + vst * Sh::kv_bytes);             // [2][TN], without boxes
+    uint32_t* words = reinterpret_cast<uint32_t*>(offs + (BOX ? 0 : 2 * TN));                       // [kWordRing][4]
     uint64_t* bars = reinterpret_cast<uint64_t*>(words + kWordRing * 4);
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 4 * stages + 3 + 3 * NT);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * (kst + vst) + 3 + 3 * NT);
     volatile uint32_t* failed = tmem_slot + 1;
     // [2]: piece number + 1 of the last pieces whose V holds infinities or NaN at drafted positions, by its parity (no row tile is a whole piece behind)
     volatile uint32_t* dirty = tmem_slot + 2;
     const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
-    const uint32_t kfull = smem_u32(bars), vfull = kfull + 8 * stages, kempty = vfull + 8 * stages, vempty = kempty + 8 * stages;
-    const uint32_t qfull = vempty + 8 * stages, qempty = qfull + 8, drain = qempty + 8, sfull = drain + 8, pfull = sfull + 8 * NT, ofull = pfull + 8 * NT;
+    const uint32_t kfull = smem_u32(bars), vfull = kfull + 8 * kst, kempty = vfull + 8 * vst, vempty = kempty + 8 * kst;
+    const uint32_t qfull = vempty + 8 * vst, qempty = qfull + 8, drain = qempty + 8, sfull = drain + 8, pfull = sfull + 8 * NT, ofull = pfull + 8 * NT;
     chain_next();
     if (tid == 0) {
-        for (int i = 0; i < stages; ++i) {
+        for (int i = 0; i < kst; ++i) {
             mbar_init(kfull + 8 * i, BOX ? 1 : loaders + loaders / 32);
-            mbar_init(vfull + 8 * i, BOX ? 1 : loaders);
             mbar_init(kempty + 8 * i, 1);
+        }
+        for (int i = 0; i < vst; ++i) {
+            mbar_init(vfull + 8 * i, BOX ? 1 : loaders);
             mbar_init(vempty + 8 * i, 1);
         }
         mbar_init(qfull, BOX ? 32 : loaders);
@@ -107,7 +110,7 @@ many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b
     }
     const int tile_pos = BOX ? a.tile_pos : TN;
     if (BOX && tile_pos < TN) {                   // positions of a tile that no box fills: zeros once and for all
-        for (int i = tid; i < 2 * stages * Sh::blocks * TN * 8; i += Sh::threads)      // pieces of 16 bytes as they lie there, eight a position
+        for (int i = tid; i < (kst + vst) * Sh::blocks * TN * 8; i += Sh::threads)      // pieces of 16 bytes as they lie there, eight a position
             if ((i >> 3) % TN >= tile_pos) *reinterpret_cast<uint4*>(ks + i * 16) = make_uint4(0, 0, 0, 0);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -123,27 +126,42 @@ many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b
     if (wid >= soft_warps && wid < mma_warp) {
         const int lt = tid - Sh::soft;
         int item = 0;
-        // a piece's rows of Q, by `threads` threads
-        auto load_q = [&](const Wk& x, int threads, bool ok) -> bool {
-            const int rows = x.rows(a), row0 = x.rt * Sh::rows;
+        // a piece's rows of Q, by `threads` threads, the first of them `lt0`: a thread has one piece of 16 bytes in every step-th row
+        auto load_q = [&](const Wk& x, int threads, int lt0, bool ok) -> bool {
             ok = ok && mbar_wait(qempty, (uint32_t)(item & 1) ^ 1u, failed, status);
             ++item;
             if (!ok) return false;
-            for (int u = lt; u < Sh::rows * pieces; u += threads) {
-                const int r = u / pieces, c = u - r * pieces, rr = row0 + r, i = rr / a.group, g = rr - i * a.group;
-                const uint8_t* src = static_cast<const uint8_t*>(a.q);
-                if (r < rows) src += 2 * ((int64_t)(x.x.first + i) * a.qs_row + (int64_t)(x.h * a.group + g) * a.qs_head) + c * 16;
-                copy16(q_s + (r >> 7) * Sh::q_bytes + (c >> 3) * 16384 + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4), src, r < rows);
+            const int step = threads / pieces, r0 = (lt - lt0) / pieces, c = (lt - lt0) - r0 * pieces;
+            const int rows = x.rows(a), i0 = (x.rt * Sh::rows + r0) / a.group, di = step / a.group, dg = step - di * a.group;
+            int g = x.rt * Sh::rows + r0 - i0 * a.group;
+            const int64_t wrap = 2 * (a.qs_row - (int64_t)a.group * a.qs_head), ahead = 2 * (di * a.qs_row + dg * a.qs_head);
+            const uint8_t* src = static_cast<const uint8_t*>(a.q) + 2 * ((int64_t)(x.x.first + i0) * a.qs_row + (int64_t)(x.h * a.group + g) * a.qs_head) + c * 16;
+            const uint32_t dst = q_s + (c >> 3) * 16384;
+#pragma unroll 4
+            for (int r = r0; r < Sh::rows; r += step) {
+                copy16(dst + (r >> 7) * Sh::q_bytes + (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4), r < rows ? src : static_cast<const uint8_t*>(a.q), r < rows);
+                src += ahead;
+                g += dg;
+                if (g >= a.group) { g -= a.group; src += wrap; }
             }
             mbar_arrive_copies(qfull);
             return true;
         };
         if constexpr (BOX) {
-            // ---- copies in boxes: a warp for the keys and the queries, one for the values
+            // ---- copies in boxes: a warp for the keys, one for the values, one for the queries, so that the next piece's tiles are on their way while
+            // its queries wait for the last products of this one
             if (lt < 64) {
                 const int kv = lt >> 5;
-                copy_boxes<Sh::rows, Sh::blocks, TN>(p, b, a, map, w, left, kv, 0, 1, kv ? v_s : k_s, Sh::kv_bytes, stages, kv ? vfull : kfull, kv ? vempty : kempty, words, kWordRing,
-                                                     failed, status, [&](const Tiles<Sh::rows>& x, bool ok) -> bool { return __all_sync(kFull, load_q(x.w, 32, ok)); });
+                copy_boxes<Sh::rows, Sh::blocks, TN>(p, b, a, map, w, left, kv, 0, 1, kv ? v_s : k_s, Sh::kv_bytes, kv ? vst : kst, kv ? vfull : kfull, kv ? vempty : kempty, words, kWordRing,
+                                                     failed, status, [](const Tiles<Sh::rows>&, bool ok) -> bool { return ok; });
+            } else {
+                bool ok = true;
+                while (left > 0 && ok) {
+                    ok = __all_sync(kFull, load_q(w, 32, 64, ok));
+                    left -= min(left, (long long)(w.tiles - w.tile));
+                    if (left > 0) w.next_item(p, b, a);
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");
             }
         } else {
             // ---- copies, three warps, position by position (pages of any size).  A tile's addresses are found by one thread a position and
@@ -154,10 +172,10 @@ many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b
                 const int m = (int)min(left, (long long)(w.tiles - w.tile));
                 const int32_t* row = b.table + (int64_t)w.s * b.max_pages;
                 const uint8_t* kb = p.base + (int64_t)a.layer * p.sl + (int64_t)w.h * p.sh;
-                ok = load_q(w, loaders, ok);
+                ok = load_q(w, loaders, 0, ok);
                 for (int j = 0; j < m; ++j, ++done) {
-                    const int st = done % stages;
-                    const uint32_t ph = (uint32_t)(done / stages) & 1u;
+                    const int st = done % kst;                   // without boxes the rings are alike
+                    const uint32_t ph = (uint32_t)(done / kst) & 1u;
                     int64_t* off = offs + (done & 1) * TN;
                     uint32_t valid[2] = {0, 0};
 #pragma unroll
@@ -225,43 +243,47 @@ many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b
             for (int i = 0; i < NT; ++i) pph[i] = 0;
             bool ok = true;
             auto qk = [&](int n, bool last) {          // every row tile in use against the next K tile is two calls: see below
-                const int st = kd % stages;
-                const uint32_t kaddr = k_s + st * Sh::kv_bytes, s_at = tmem + n * TN;
+                const int st = kd % kst;
+                const uint32_t s_at = tmem + n * TN;
+                const uint64_t q_at = desc_k(q_s + n * Sh::q_bytes), k_at = desc_k(k_s + st * Sh::kv_bytes);
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k)
-                    mma_ss(s_at, desc_k(q_s + n * Sh::q_bytes + (k >> 2) * 16384) + 2 * (k & 3), desc_k(kaddr + (k >> 2) * (TN * 128)) + 2 * (k & 3), id_qk, k ? 1u : 0u);
+                    mma_ss(s_at, q_at + (k >> 2) * (16384 >> 4) + 2 * (k & 3), k_at + (k >> 2) * (TN * 128 >> 4) + 2 * (k & 3), id_qk, k ? 1u : 0u);
                 mma_commit(sfull + 8 * n);
                 if (last) { mma_commit(kempty + 8 * st); ++kd; }
             };
             auto wait_k = [&]() {
-                ok = ok && mbar_wait(kfull + 8 * (kd % stages), (uint32_t)(kd / stages) & 1u, failed, status);
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                fence_after();
+                ok = ok && mbar_wait(kfull + 8 * (kd % kst), (uint32_t)(kd / kst) & 1u, failed, status);
+                // boxes and products are of one proxy; what threads wrote to V is fenced by those who wrote it
+                if (!BOX) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             };
             while (left > 0 && ok) {
                 const int m = (int)min(left, (long long)(w.tiles - w.tile)), nt = NT == 2 && w.rows(a) > 128 ? 2 : 1;
                 ok = mbar_wait(qfull, (uint32_t)(item & 1), failed, status);
+                if (BOX) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 wait_k();
                 if (!ok) break;
+                fence_after();
                 for (int n = 0; n < nt; ++n) qk(n, n == nt - 1);
                 if (m == 1) mma_commit(qempty);
                 for (int j = 0; j < m && ok; ++j, ++vd) {
-                    const int st = vd % stages;
+                    const int st = vd % vst;
+                    // the tiles first: they are there long before the weights, and the time from the weights to the next scores counts
+                    ok = mbar_wait(vfull + 8 * st, (uint32_t)(vd / vst) & 1u, failed, status);
+                    if (j + 1 < m) wait_k();
+                    if (!BOX) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    const uint64_t v_at = desc_mn(v_s + st * Sh::kv_bytes, TN * 128);
                     for (int n = 0; n < nt && ok; ++n) {
                         ok = mbar_wait(pfull + 8 * n, pph[n], failed, status);
                         pph[n] ^= 1u;
-                        if (n == 0) ok = ok && mbar_wait(vfull + 8 * st, (uint32_t)(vd / stages) & 1u, failed, status);
                         if (!ok) break;
-                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         fence_after();
-                        const uint32_t vaddr = v_s + st * Sh::kv_bytes, o_at = tmem + NT * TN + n * Sh::DV, p_at = tmem + n * TN;
+                        const uint32_t o_at = tmem + NT * TN + n * Sh::DV, p_at = tmem + n * TN;
 #pragma unroll
-                        for (int k = 0; k < TN / 16; ++k) mma_ts(o_at, p_at + 8 * k, desc_mn(vaddr + k * 2048, TN * 128), id_pv, j | k ? 1u : 0u);
+                        for (int k = 0; k < TN / 16; ++k) mma_ts(o_at, p_at + 8 * k, v_at + k * (2048 >> 4), id_pv, j | k ? 1u : 0u);
                         mma_commit(ofull + 8 * n);
                         if (n == nt - 1) mma_commit(vempty + 8 * st);
                         if (j + 1 < m) {
-                            if (n == 0) wait_k();
-                            if (!ok) break;
                             qk(n, n == nt - 1);
                             if (j + 2 == m && n == nt - 1) mma_commit(qempty);
                         }
@@ -373,8 +395,8 @@ many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b
                 if (hide || (BOX && masked)) {
                     // V of positions that do not exist is whatever the boxes brought or left: zeros instead, since weights of 0 do not hide it; and
                     // what drafted positions have of infinities and NaN is taken out.  Both row tiles do the same to it.
-                    const int st = (tiles_done + j) % stages, pos = r_tile;
-                    ok = __all_sync(kFull, mbar_wait(vfull + 8 * st, (uint32_t)((tiles_done + j) / stages) & 1u, failed, status));
+                    const int st = (tiles_done + j) % vst, pos = r_tile;
+                    ok = __all_sync(kFull, mbar_wait(vfull + 8 * st, (uint32_t)((tiles_done + j) / vst) & 1u, failed, status));
                     if (!ok) break;
                     uint8_t* tile = vs + st * Sh::kv_bytes;
                     if (pos < min(TN, tile_pos)) {
@@ -452,7 +474,7 @@ many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b
 
 template <class T, int D, int NT, bool BOX>
 cudaError_t launch_many_as(const PoolDev& p, const BookDev& b, const AttendArgs& a, const CUtensorMap& map, const AttendPlan& x, uint32_t* status, cudaStream_t st) {
-    using Sh = Shape<D, NT>;
+    using Sh = Shape<D, NT, BOX>;
     cudaError_t e = cudaFuncSetAttribute(many_kernel<T, D, NT, BOX>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Sh::smem);
     if (e != cudaSuccess) return e;
     e = launch_kernel(many_kernel<T, D, NT, BOX>, x.grid, Sh::threads, Sh::smem, st, false, 1, p, b, a, map, status);
