@@ -22,7 +22,8 @@ template <int D, int NT, bool BOX> struct Shape {
     // tiles kept of K and of V: as many as fit, of K one more (its next tile is waited for first)
     static constexpr int vstages = D == 128 ? NT : NT == 1 ? 2 : BOX ? 4 : 3, kstages = BOX && (D != 128 || NT == 2) ? vstages + 1 : vstages;
     static constexpr int q_bytes = blocks * 128 * 128, kv_bytes = blocks * TN * 128;
-    static constexpr int tmem = NT * (TN + DV) > 256 ? 512 : 256;
+    static constexpr int bufs = D == 256 ? 2 : 1;                      // of scores, a row tile: as many as fit
+    static constexpr int tmem = NT * (bufs * TN + DV) > 256 ? 512 : 256;
     static constexpr int rows = NT * 128, soft = NT * 128, threads = soft + 128;
     static constexpr int per_sm = NT == 1 && D != 256 ? 2 : 1;
     static constexpr size_t smem = (size_t)NT * q_bytes + (kstages + vstages) * kv_bytes + (BOX ? 0 : 2 * TN * 8) + 1024 + 512;
@@ -68,7 +69,7 @@ __global__ void __launch_bounds__(Shape<D, NT, BOX>::threads, Shape<D, NT, BOX>:
 many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b, const __grid_constant__ AttendArgs a, const __grid_constant__ CUtensorMap map, uint32_t* status) {
     using Sh = Shape<D, NT, BOX>;
     using Wk = Walk<Sh::rows>;
-    constexpr int TN = Sh::TN, kst = Sh::kstages, vst = Sh::vstages, soft_warps = Sh::soft / 32, mma_warp = soft_warps + 3, loaders = BOX ? 64 : 96;
+    constexpr int TN = Sh::TN, bufs = Sh::bufs, kst = Sh::kstages, vst = Sh::vstages, soft_warps = Sh::soft / 32, mma_warp = soft_warps + 3, loaders = BOX ? 64 : 96;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     uint8_t* ks = smem + NT * Sh::q_bytes;
@@ -76,13 +77,14 @@ many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b
     int64_t* offs = reinterpret_cast<int64_t*>(vs + vst * Sh::kv_bytes);             // [2][TN], without boxes
     uint32_t* words = reinterpret_cast<uint32_t*>(offs + (BOX ? 0 : 2 * TN));                       // [kWordRing][4]
     uint64_t* bars = reinterpret_cast<uint64_t*>(words + kWordRing * 4);
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * (kst + vst) + 3 + 3 * NT);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * (kst + vst) + 3 + 3 * bufs * NT);
     volatile uint32_t* failed = tmem_slot + 1;
-    // [2]: piece number + 1 of the last pieces whose V holds infinities or NaN at drafted positions, by its parity (no row tile is a whole piece behind)
-    volatile uint32_t* dirty = tmem_slot + 2;
+    // V that held infinities or NaN at drafted positions: [row tile][2] piece number + 1, by its parity (no warp is two pieces behind the others of its row
+    // tile, but a row tile may be many behind the other); [kWordRing] tile number + 1, by which a row tile knows of what the other has taken out before it
+    volatile uint32_t *dirty = tmem_slot + 2, *taken = dirty + 2 * NT;
     const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
     const uint32_t kfull = smem_u32(bars), vfull = kfull + 8 * kst, kempty = vfull + 8 * vst, vempty = kempty + 8 * kst;
-    const uint32_t qfull = vempty + 8 * vst, qempty = qfull + 8, drain = qempty + 8, sfull = drain + 8, pfull = sfull + 8 * NT, ofull = pfull + 8 * NT;
+    const uint32_t qfull = vempty + 8 * vst, qempty = qfull + 8, drain = qempty + 8, sfull = drain + 8, pfull = sfull + 8 * bufs * NT, ofull = pfull + 8 * bufs * NT;
     chain_next();
     if (tid == 0) {
         for (int i = 0; i < kst; ++i) {
@@ -96,12 +98,12 @@ many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b
         mbar_init(qfull, BOX ? 32 : loaders);
         mbar_init(qempty, 1);
         mbar_init(drain, 1);
-        for (int i = 0; i < NT; ++i) {
+        for (int i = 0; i < bufs * NT; ++i) {
             mbar_init(sfull + 8 * i, 1);
             mbar_init(pfull + 8 * i, 4);
             mbar_init(ofull + 8 * i, 1);
         }
-        *failed = dirty[0] = dirty[1] = 0u;
+        for (int i = 1; i < 2 + 2 * NT + kWordRing; ++i) tmem_slot[i] = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (wid == mma_warp) {
@@ -234,22 +236,26 @@ many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b
         }
     } else if (wid == mma_warp) {
         if (lane == 0) {
-            // ---- products, in the order QK(0), then for every tile PV(j), QK(j+1), the row tiles in turn.  They run in the order in which they are
-            // issued, so that S of the next tile may take the columns of P of this one.
+            // ---- products: the scores of the first tiles, as many as there are buffers for; then for every tile P V and the scores of the tile that takes
+            // the columns of that P, the row tiles in turn.  They run in the order in which they are issued.
             constexpr uint32_t common = (1u << 4) | (Kind<T>::format << 7) | (Kind<T>::format << 10) | (8u << 24);
             constexpr uint32_t id_qk = common | ((uint32_t)(TN >> 3) << 17), id_pv = common | (1u << 16) | ((uint32_t)(Sh::DV >> 3) << 17);
             int kd = 0, vd = 0, item = 0;
-            uint32_t pph[NT];
-            for (int i = 0; i < NT; ++i) pph[i] = 0;
+            uint32_t cs = 0, cp = 0;                   // scores and products P V, modulo 4, a byte a row tile
+            auto next = [](uint32_t& c, int n) -> uint32_t {
+                const uint32_t v = c >> (8 * n) & 3u;
+                c = (c & ~(3u << (8 * n))) | ((v + 1u) & 3u) << (8 * n);
+                return v;
+            };
             bool ok = true;
-            auto qk = [&](int n, bool last) {          // every row tile in use against the next K tile is two calls: see below
-                const int st = kd % kst;
-                const uint32_t s_at = tmem + n * TN;
+            auto qk = [&](int n, bool last) {
+                const int st = kd % kst, at = n * bufs + (int)(next(cs, n) % bufs);
+                const uint32_t s_at = tmem + at * TN;
                 const uint64_t q_at = desc_k(q_s + n * Sh::q_bytes), k_at = desc_k(k_s + st * Sh::kv_bytes);
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k)
                     mma_ss(s_at, q_at + (k >> 2) * (16384 >> 4) + 2 * (k & 3), k_at + (k >> 2) * (TN * 128 >> 4) + 2 * (k & 3), id_qk, k ? 1u : 0u);
-                mma_commit(sfull + 8 * n);
+                mma_commit(sfull + 8 * at);
                 if (last) { mma_commit(kempty + 8 * st); ++kd; }
             };
             auto wait_k = [&]() {
@@ -261,31 +267,35 @@ many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b
                 const int m = (int)min(left, (long long)(w.tiles - w.tile)), nt = NT == 2 && w.rows(a) > 128 ? 2 : 1;
                 ok = mbar_wait(qfull, (uint32_t)(item & 1), failed, status);
                 if (BOX) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                wait_k();
-                if (!ok) break;
-                fence_after();
-                for (int n = 0; n < nt; ++n) qk(n, n == nt - 1);
-                if (m == 1) mma_commit(qempty);
+                for (int j = 0; j < bufs && j < m && ok; ++j) {
+                    wait_k();
+                    if (!ok) break;
+                    fence_after();
+                    for (int n = 0; n < nt; ++n) qk(n, n == nt - 1);
+                }
+                if (m <= bufs) mma_commit(qempty);
                 for (int j = 0; j < m && ok; ++j, ++vd) {
                     const int st = vd % vst;
+                    const bool more = j + bufs < m;
                     // the tiles first: they are there long before the weights, and the time from the weights to the next scores counts
                     ok = mbar_wait(vfull + 8 * st, (uint32_t)(vd / vst) & 1u, failed, status);
-                    if (j + 1 < m) wait_k();
+                    if (more) wait_k();
                     if (!BOX) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     const uint64_t v_at = desc_mn(v_s + st * Sh::kv_bytes, TN * 128);
                     for (int n = 0; n < nt && ok; ++n) {
-                        ok = mbar_wait(pfull + 8 * n, pph[n], failed, status);
-                        pph[n] ^= 1u;
+                        const uint32_t turn = next(cp, n);
+                        const int at = n * bufs + (int)(turn % bufs);
+                        ok = mbar_wait(pfull + 8 * at, turn / bufs & 1u, failed, status);
                         if (!ok) break;
                         fence_after();
-                        const uint32_t o_at = tmem + NT * TN + n * Sh::DV, p_at = tmem + n * TN;
+                        const uint32_t o_at = tmem + NT * bufs * TN + n * Sh::DV, p_at = tmem + at * TN;
 #pragma unroll
                         for (int k = 0; k < TN / 16; ++k) mma_ts(o_at, p_at + 8 * k, v_at + k * (2048 >> 4), id_pv, j | k ? 1u : 0u);
-                        mma_commit(ofull + 8 * n);
+                        mma_commit(ofull + 8 * at);
                         if (n == nt - 1) mma_commit(vempty + 8 * st);
-                        if (j + 1 < m) {
+                        if (more) {
                             qk(n, n == nt - 1);
-                            if (j + 2 == m && n == nt - 1) mma_commit(qempty);
+                            if (j + bufs + 1 == m && n == nt - 1) mma_commit(qempty);
                         }
                     }
                 }
@@ -303,11 +313,15 @@ many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b
     } else if (wid < soft_warps) {
         // ---- softmax and results: a thread a row
         const int nt = wid >> 2, r_tile = (wid & 3) * 32 + lane, r_item = nt * 128 + r_tile;
-        const uint32_t lanes = (uint32_t)((wid & 3) * 32) << 16, s_at = tmem + nt * TN + lanes, o_at = tmem + NT * TN + nt * Sh::DV + lanes;
+        const uint32_t lanes = (uint32_t)((wid & 3) * 32) << 16, s_0 = tmem + nt * bufs * TN + lanes, o_at = tmem + NT * bufs * TN + nt * Sh::DV + lanes;
         const float c = a.scale * 1.44269504088896f;
         const unsigned long long c2 = pack2(c, c);
         int done = 0, tiles_done = 0, part = 0;       // tiles of this row tile, of the CTA
         bool ok = true;
+        // the last product of the row tile, and so all before it.  Two buffers have a barrier each: of two products on their way one parity would not tell.
+        auto wait_o = [&]() -> bool {
+            return __all_sync(kFull, mbar_wait(ofull + 8 * (nt * bufs + (done - 1) % bufs), (uint32_t)((done - 1) / bufs) & 1u, failed, status));
+        };
         while (left > 0 && ok) {
             const int m = (int)min(left, (long long)(w.tiles - w.tile)), rows = w.rows(a);
             const bool in_use = nt == 0 || rows > 128, works = r_tile - lane + nt * 128 < rows;   // the row tile; this warp
@@ -315,8 +329,9 @@ many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b
             float top = -INFINITY, sum = 0.f;         // top: what the weights are relative to, scaled, base 2
             const bool may_hide = a.mask != nullptr || w.x.n > 1;
             for (int j = 0; j < m && in_use; ++j, ++done) {
-                const int t = (w.tile + j) * tile_pos;
-                ok = __all_sync(kFull, mbar_wait(sfull + 8 * nt, (uint32_t)done & 1u, failed, status));
+                const int t = (w.tile + j) * tile_pos, buf = done % bufs;
+                const uint32_t s_at = s_0 + buf * TN;
+                ok = __all_sync(kFull, mbar_wait(sfull + 8 * (nt * bufs + buf), (uint32_t)(done / bufs) & 1u, failed, status));
                 if (!ok) break;
                 fence_after();
                 const uint32_t* valid = words + ((tiles_done + j) % kWordRing) * 4;
@@ -352,7 +367,7 @@ many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b
                         if (raise) top = now;
                         sum *= f;
                         if (j > 0) {
-                            ok = __all_sync(kFull, mbar_wait(ofull + 8 * nt, (uint32_t)(done - 1) & 1u, failed, status));
+                            ok = wait_o();
                             if (!ok) break;
                             fence_after();
 #pragma unroll 1
@@ -404,20 +419,26 @@ many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b
                         if (BOX && !there)
                             for (int e = 0; e < Sh::blocks * 8; ++e)
                                 *reinterpret_cast<uint4*>(tile + (e >> 3) * (TN * 128) + pos * 128 + (((e & 7) ^ (pos & 7)) << 4)) = make_uint4(0, 0, 0, 0);
-                        else if (hide && t + pos >= w.x.len && t + pos < w.x.kv && special<T, D, TN>(tile, pos)) {
-                            dirty[part & 1] = (uint32_t)part + 1u;
+                        else if (hide && t + pos >= w.x.len && t + pos < w.x.kv) {
+                            const bool found = special<T, D, TN>(tile, pos);
                             __threadfence_block();            // who finds the zeros finds the word
-                            take_out<T, D, TN>(tile, pos);
+                            volatile uint32_t& word = taken[(tiles_done + j) % kWordRing];
+                            if (found || word == (uint32_t)(tiles_done + j) + 1u) dirty[2 * nt + (part & 1)] = (uint32_t)part + 1u;
+                            if (found) {
+                                word = (uint32_t)(tiles_done + j) + 1u;
+                                __threadfence_block();
+                                take_out<T, D, TN>(tile, pos);
+                            }
                         }
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
                 fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(pfull + 8 * nt);
+                if (lane == 0) mbar_arrive(pfull + 8 * (nt * bufs + buf));
             }
             tiles_done += m;
-            if (ok && in_use) ok = __all_sync(kFull, mbar_wait(ofull + 8 * nt, (uint32_t)(done - 1) & 1u, failed, status));
+            if (ok && in_use) ok = wait_o();
             if (!ok) break;
             if (in_use && works) {
                 fence_after();
@@ -452,7 +473,7 @@ many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b
                     }
                 }
                 if (live) {
-                    if (may_hide && dirty[part & 1] == (uint32_t)part + 1u)
+                    if (may_hide && dirty[2 * nt + (part & 1)] == (uint32_t)part + 1u)
                         put_back_row<T>(p, b, a, w.x, w.s, w.h, w.tile * tile_pos, (w.tile + m) * tile_pos, i, whole ? static_cast<void*>(out) : mid, whole);
                     if (!whole) a.part_ml[slot] = make_float2(top, sum);
                     else if (a.lse) a.lse[n_row * a.heads + head] = sum == 0.f ? -INFINITY : (top - Kind<T>::shift + log2f(sum)) * 0.693147180559945f;
