@@ -498,6 +498,8 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
                 // V of positions that do not exist is whatever the boxes brought or left: zeros instead, since weights of 0 do not hide it
                 const bool blank = BOX && masked && pos < tile_pos && !(words[x % kWords * 4 + quarter] >> lane & 1u);
                 if ((hide || (BOX && masked)) && wid < 4) {
+                    // with one slot the tile before may still be awaited, and a parity tells only one tile from the next: its product first
+                    if (v_slots == 1 && x > 0) ok = ok && mbar_wait(ofull + 8 * ((x - 1) & 1), (uint32_t)((x - 1) >> 1) & 1u, failed, status);
                     ok = ok && mbar_wait(v_full + 8 * (x % v_slots), (uint32_t)(x / v_slots) & 1u, failed, status);
                     uint8_t* tile = ring + (k_slots + x % v_slots) * F::slot;
                     if (ok && blank)

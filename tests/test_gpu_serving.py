@@ -633,3 +633,64 @@ def test_beams_over_a_restored_cache(dev, ora):
             assert torch.equal(mine.permute(1, 2, 3, 0, 4).float().cpu(), history[r])
         assert int(book.len[0]) == history[0].shape[3]
     pool.check()
+
+
+def attention_in_64_bits(kv, layer, table, lens, q, begin, bits, scale):
+    """The formula over one layer's pages, session by session; sums of magnitudes for the tolerance beside it."""
+    H, page, d = kv.shape[3], kv.shape[4], kv.shape[5]
+    G = q.shape[1] // H
+    out, mag = (torch.zeros(q.shape, dtype=torch.float64, device=q.device) for _ in range(2))
+    big = torch.zeros(q.shape[:2], dtype=torch.float64, device=q.device)
+    for s, at in enumerate(lens):
+        lo, hi = int(begin[s]), int(begin[s + 1])
+        n, T = hi - lo, at + hi - lo
+        if n == 0:
+            continue
+        pages = torch.as_tensor(table[s, :-(-T // page)].astype(np.int64), device=q.device)
+        k, v = (kv[layer, j, pages].double().transpose(1, 2).reshape(-1, H, d)[:T].transpose(0, 1) for j in range(2))
+        x = q[lo:hi].double().reshape(n, H, G, d).permute(1, 2, 0, 3)
+        score = torch.einsum("hgnd,htd->hgnt", x, k) * scale
+        most = torch.einsum("hgnd,htd->hgnt", x.abs(), k.abs()).amax(-1) * scale
+        sees = torch.ones(n, T, dtype=torch.bool, device=q.device)
+        sees[:, at:] = torch.ones(n, n, dtype=torch.bool, device=q.device).tril() if bits is None else torch.as_tensor(bits[lo:hi, :n], device=q.device).bool()
+        w = score.masked_fill(~sees, -math.inf).softmax(-1)
+        out[lo:hi] = torch.einsum("hgnt,htd->hgnd", w, v).permute(2, 0, 1, 3).reshape(n, H * G, d)
+        mag[lo:hi] = torch.einsum("hgnt,htd->hgnd", w, v.abs()).permute(2, 0, 1, 3).reshape(n, H * G, d)
+        big[lo:hi] = most.permute(2, 0, 1).reshape(n, H * G)
+    return out, mag, big
+
+
+@pytest.mark.parametrize("dtype, d, G, page, n", [("bf16", 128, 4, 32, 1), ("f16", 128, 3, 24, 9), ("f16", 64, 4, 16, 5), ("bf16", 64, 8, 64, 7), ("bf16", 256, 2, 32, 8),
+                                                  ("f16", 32, 4, 32, 4), ("f16", 128, 4, 20, 3), ("bf16", 128, 8, 32, 14), ("f16", 128, 8, 64, 30), ("bf16", 64, 8, 32, 33),
+                                                  ("f16", 256, 8, 32, 14), ("f16", 128, 8, 36, 31)])
+def test_attention_of_batches_with_many_pieces_an_sm(dev, dtype, d, G, page, n):
+    """Ragged batches that give every SM many pieces one after the other, most of which end inside a tile; the same call again and again."""
+    rng = np.random.default_rng(d + n)
+    H, S = 8, 160
+    lens = [int(x) for x in rng.integers(0, 420, S)]
+    drafts = [n if i % 5 else int(rng.integers(0, n + 1)) for i in range(S)]
+    held = [-(-(a + b) // page) for a, b in zip(lens, drafts)]
+    pages = sum(held) + 2
+    table, ref = make_book(rng, held, max(held) + 1, pages, dev)
+    gen = torch.Generator(device=dev).manual_seed(n)
+    kv = torch.randn(1, 2, pages, H, page, d, device=dev, generator=gen).to(TYPES[dtype])
+    begin = np.cumsum([0] + drafts).astype(np.int32)
+    N = int(begin[-1])
+    q = torch.randn(N, H * G, d, device=dev, generator=gen).to(TYPES[dtype])
+    bits, w = tree_mask(rng, begin, -(-n // 32), ())
+    mask = torch.from_numpy(w.copy()).view(N, -1).to(dev) if n > 1 else None
+    ex, mag, big = attention_in_64_bits(kv, 0, table, lens, q, begin, bits if n > 1 else None, 1 / math.sqrt(d))
+    for s in range(S):                                     # what stands behind a session's last position is not to be seen
+        t = torch.arange(lens[s] + drafts[s], held[s] * page)
+        kv[0, :, torch.as_tensor(table[s].astype(np.int64))[t // page].to(dev), :, (t % page).to(dev)] = float("nan")
+    pool, book = plc.PagePool(kv), book_of(table, lens, ref, dev)
+    u = torch.finfo(TYPES[dtype]).eps / 2
+    terms = max(a + b for a, b in zip(lens, drafts))
+    e = 2 * (d * 2.0 ** -23 * big + 2.0 ** -22 + 2.0 ** -23 * 2 * big)
+    tol = (u + e[..., None] + terms * 2.0 ** -23) * mag + u * ex.abs() + torch.finfo(TYPES[dtype]).smallest_normal * u
+    for _ in range(25):
+        got = pool.tree_attention(0, book, q, i32(begin, dev), mask=mask)
+        got = got[0] if isinstance(got, tuple) else got
+        bad = ~((got.double() - ex).abs() <= tol)
+        assert not bad.any(), (int(bad.any(-1).sum()), float((got.double() - ex).abs().max()))
+    pool.check()
