@@ -366,7 +366,7 @@ typedef struct {
 } plc_page_pool;
 
 /* Who holds which page: table_dev [rows][max_pages] int32, the pages of each row in order, -1 behind them;
- * len_dev [rows] committed positions; ref_dev [n_pages] how many table entries name the page (0 = free; a caller
+ * len_dev [rows] committed positions, at most 2^31 - 2^16; ref_dev [n_pages] how many table entries name the page (0 = free; a caller
  * that holds on to a page itself adds one).  Calls read one book and write another: its arrays must not overlap
  * the first one's, and the first stays valid until a page that only it names is taken by a later call. */
 typedef struct {

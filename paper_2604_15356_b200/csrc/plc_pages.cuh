@@ -4,6 +4,8 @@
 
 namespace plc {
 
+constexpr int kMostPositions = 0x7fff0000;        // of a row
+
 // A pool as the kernels see it: strides in bytes.
 struct PoolDev {
     uint8_t* base;
@@ -40,9 +42,9 @@ inline plc_status check_book(const plc_page_book* b, BookDev* out) {
 }
 
 #ifdef __CUDACC__
-// Positions that `max_pages` pages hold, as far as a length can count them.
+// Positions that `max_pages` pages hold, as far as an int counts them with a tile's positions to spare.
 __device__ __forceinline__ int most_positions(const BookDev& b, const PoolDev& p) {
-    return (int)min((long long)b.max_pages * p.page_pos, (long long)0x7fffffff);
+    return (int)min((long long)b.max_pages * p.page_pos, (long long)kMostPositions);
 }
 #endif
 

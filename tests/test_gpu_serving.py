@@ -694,3 +694,158 @@ def test_attention_of_batches_with_many_pieces_an_sm(dev, dtype, d, G, page, n):
         bad = ~((got.double() - ex).abs() <= tol)
         assert not bad.any(), (int(bad.any(-1).sum()), float((got.double() - ex).abs().max()))
     pool.check()
+
+
+@pytest.mark.parametrize("dtype, d, G, page, n", [("f16", 128, 8, 16, 20), ("bf16", 128, 8, 24, 40), ("bf16", 128, 8, 20, 40), ("f16", 64, 8, 136, 20), ("bf16", 64, 8, 8, 40),
+                                                  ("f16", 256, 8, 16, 20), ("bf16", 256, 4, 12, 40), ("f16", 32, 8, 32, 40)])
+def test_attention_of_many_rows_does_not_look_at_what_is_masked(dev, ora, dtype, d, G, page, n):
+    """Infinities and NaN at masked drafted positions, for row tiles of 128 and 256, with pages that boxes copy and others."""
+    attention_case(dev, ora, n + d, dtype, d, 1, G, page, lens=[125, 300], n=[n, n // 4], nan_masked=True).check()
+    attention_case(dev, ora, n + d, dtype, d, 2, G, page, lens=[0, 10, 7], n=[n, 2, n], empty=(1, n + 1, n + 3)).check()
+
+
+@pytest.mark.parametrize("d, G, page, n", [(128, 8, 16, 20), (128, 8, 16, 40), (64, 8, 8, 40), (256, 8, 16, 20), (128, 8, 12, 40)])
+def test_attention_of_many_rows_reports_pages_out_of_range(dev, ora, d, G, page, n):
+    pool = attention_case(dev, ora, d, "bf16", d, 1, G, page, lens=[100, 40], n=[n, n], bad_pages=((0, 2), (1, 0)))
+    with pytest.raises(plc.PlcError) as e:
+        pool.check()
+    assert e.value.code == plc.E_INVALID
+
+
+def test_attention_of_wide_sessions_among_narrow_ones(dev):
+    """Row tiles that are in use now and then only, infinities in what they have drafted: a row sees its own, and no row another's."""
+    rng = np.random.default_rng(0)
+    H, G, d, page, S = 4, 8, 128, 32, 80
+    drafts = [60 if s % 8 == 0 else 3 for s in range(S)]
+    lens = [int(x) for x in rng.integers(0, 300, S)]
+    held = [-(-(a + b) // page) for a, b in zip(lens, drafts)]
+    table, ref = make_book(rng, held, max(held), sum(held), dev)
+    kv = torch.randn(1, 2, sum(held), H, page, d, device=dev, generator=torch.Generator(device=dev).manual_seed(0)).bfloat16()
+    begin = np.cumsum([0] + drafts).astype(np.int32)
+    q = torch.randn(int(begin[-1]), H * G, d, device=dev, generator=torch.Generator(device=dev).manual_seed(1)).bfloat16()
+    pool, book = plc.PagePool(kv), book_of(table, lens, ref, dev)
+    plain = pool.tree_attention(0, book, q, i32(begin, dev))[0].clone()
+    hit = torch.zeros(q.shape[0], dtype=torch.bool, device=dev)
+    for s in range(0, S, 8):                               # the last drafted position's value: only the last row sees it
+        t = lens[s] + drafts[s] - 1
+        kv[0, 1, int(table[s, t // page]), :, t % page, 5] = math.inf
+        hit[int(begin[s + 1]) - 1] = True
+    for _ in range(10):
+        got = pool.tree_attention(0, book, q, i32(begin, dev))[0]
+        assert bool(torch.isinf(got[hit][..., 5]).all()) and bool((got[~hit] == plain[~hit]).all())
+        got[hit, :, 5] = 0
+        assert bool(torch.isfinite(got).all())
+    pool.check()
+
+
+def test_page_calls_in_graphs_and_on_streams(dev):
+    """Fork, draft, attend, keep, compact as one captured graph, replayed over new contents; a second graph on another stream beside it."""
+    rng = np.random.default_rng(3)
+    S, H, d, page, P = 6, 2, 64, 16, 90
+
+    def state(seed):
+        gen = torch.Generator(device=dev).manual_seed(seed)
+        kv = torch.randn(2, 2, P, H, page, d, device=dev, generator=gen).half()
+        table, ref = make_book(np.random.default_rng(seed), [3] * S, 6, P, dev)
+        return kv, table, ref, [20 + 4 * i for i in range(S)]
+
+    parent, room = i32([0, 0, 2, 3, 3, 5], dev), i32([5] * S, dev)
+    begin, q = i32([0] + [5 * (i + 1) for i in range(S)], dev), torch.randn(5 * S, 2 * H, d, device=dev).half()
+    path, n_path = i32(rng.permutation(5)[:2].repeat(S).reshape(2, S).T.copy(), dev).sort(1).values.contiguous(), i32([2, 1, 0, 2, 2, 1], dev)
+
+    def steps(pool, book):
+        new = pool.fork(book, parent, room)
+        out = pool.tree_attention(1, new, q, begin)
+        kept = pool.keep(new, path, n_path)
+        small, moved = pool.compact(kept)
+        return out + (kept.table, kept.len, kept.ref, small.table, small.len, small.ref, moved)
+
+    def eager(seed):
+        kv, table, ref, lens = state(seed)
+        pool = plc.PagePool(kv)
+        res = [t.clone() for t in steps(pool, book_of(table, lens, ref, dev))]
+        pool.check()
+        return res + [kv]
+
+    want = {seed: eager(seed) for seed in range(3)}
+    held = []
+    for seed in range(2):
+        kv, table, ref, lens = state(seed)
+        pool, book, g = plc.PagePool(kv), book_of(table, lens, ref, dev), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            res = steps(pool, book)
+        held.append((g, pool, book, res, kv))
+    sides = [torch.cuda.Stream(dev), torch.cuda.Stream(dev)]
+    torch.cuda.synchronize()
+    for (g, *_), side in zip(held, sides):                 # both at once
+        with torch.cuda.stream(side):
+            g.replay()
+    torch.cuda.synchronize()
+    for seed, (g, pool, book, res, kv) in enumerate(held):
+        assert all(torch.equal(a, b) for a, b in zip(list(res) + [kv], want[seed]))
+    for g, pool, book, res, kv in held:                    # other contents in the same places
+        kv2, table, ref, lens = state(2)
+        kv.copy_(kv2)
+        book.table.copy_(i32(table, dev)), book.ref.copy_(i32(ref, dev)), book.len.copy_(i32(lens, dev))
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(list(res) + [kv], want[2]))
+        pool.check()
+
+
+def test_beam_calls_in_graphs_and_on_streams(dev):
+    gen = torch.Generator(device=dev).manual_seed(4)
+    sets = [(torch.randn(3, 8, 5003, device=dev, generator=gen).half(), torch.randn(3, 8, device=dev, generator=gen), torch.randn(24, 7, device=dev, generator=gen)) for _ in range(3)]
+
+    def steps(logits, score, tokens):
+        s, parent, token = plc.beam_select(logits, score, 8)
+        return [s, parent, token] + plc.beam_reorder(parent.view(-1), [tokens])
+
+    want = [[t.clone() for t in steps(*x)] for x in sets]
+    held = []
+    for i in range(2):
+        x = [t.clone() for t in sets[i]]
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            res = steps(*x)
+        held.append((g, x, res))
+    torch.cuda.synchronize()
+    for g, _, _ in held:
+        with torch.cuda.stream(torch.cuda.Stream(dev)):
+            g.replay()
+    torch.cuda.synchronize()
+    for i, (g, x, res) in enumerate(held):
+        assert all(torch.equal(a, b) for a, b in zip(res, want[i]))
+        for a, b in zip(x, sets[2]):
+            a.copy_(b)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(res, want[2]))
+
+
+def test_reordering_of_many_states_and_odd_rows(dev):
+    """More tensors than one launch takes, rows of one to 4099 bytes, rows without anything, expanded rows, one parent for all."""
+    gen = torch.Generator(device=dev).manual_seed(6)
+    states = [torch.randint(0, 255, (5, n), device=dev, generator=gen, dtype=torch.uint8) for n in (1, 2, 3, 5, 7, 15, 16, 17, 31, 33, 64, 127, 255, 1025, 4096, 4099, 12, 9, 0)]
+    states += [torch.randn(5, 3, 2, device=dev, generator=gen)[:, 1], torch.randn(1, 9, device=dev, generator=gen).expand(5, 9), torch.arange(5, device=dev)]
+    for parent in ([4, 4, 4], [0, -1, 2, 3, 4, 1, 0], [-1]):
+        rows = torch.tensor(parent, device=dev)
+        for a, b in zip(plc.beam_reorder(i32(parent, dev), states), states):
+            want = b[rows.clamp(min=0)].clone()
+            want[rows < 0] = 0
+            assert torch.equal(a, want)
+
+
+def test_lengths_near_two_to_the_31(dev):
+    """One page named by 2^17 entries of a row: lengths that an int holds, but not with a tile's positions added, are refused."""
+    page, cols = 1 << 14, (1 << 17) + 2
+    pool = plc.PagePool(torch.zeros(1, 2, 2, 1, page, 32, dtype=torch.float16, device=dev))
+    table = torch.zeros(1, cols, dtype=torch.int32, device=dev)
+    q, begin = torch.zeros(1, 1, 32, dtype=torch.float16, device=dev), i32([0, 0], dev)
+    for length in (0x7fffffff, 0x7fff0001):
+        book = plc.PageBook(table, i32([length], dev), i32([cols, 0], dev))
+        for call in (lambda: pool.fork(book, i32([0], dev)), lambda: pool.keep(book, i32([[1]], dev), i32([1], dev)), lambda: pool.tree_attention(0, book, q, begin)):
+            call()
+            with pytest.raises(plc.PlcError) as e:
+                pool.check()
+            assert e.value.code == plc.E_INVALID
