@@ -4,13 +4,15 @@
 // Each call is two launches: a small one that decides (one block walks the rows and the pages' counts in order, since
 // a fresh page's number depends on every row and page before it) and one that moves pages and writes the new
 // book with the whole GPU.  Bound by HBM where pages move (every byte read once and written once, 16 bytes a thread and
-// access), else by the two launches; the second is chained to the first.
+// access), else by the two launches; the second is chained to the first.  A call that has little to do is one launch instead, a cluster of eight blocks
+// with the cluster's barrier between the two parts.
 #include "plc_pages.cuh"
 
 namespace plc {
 namespace {
 
 constexpr int kPlanThreads = 1024, kMoveThreads = 256;
+constexpr int kFewBlocks = 8, kFewThreads = kPlanThreads;
 constexpr int kPartBytes = 32768;                 // of a page's plane (one layer's keys or values): a block's share at a time
 
 struct Workspace {
@@ -65,6 +67,11 @@ __device__ __forceinline__ unsigned long long block_scan(unsigned long long v, u
     return ahead + x - v;
 }
 
+// All of a cluster's blocks have come here, and see what the others have written.
+__device__ __forceinline__ void cluster_meet() {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+
 // What row s of the new book continues.
 struct ForkRow {
     int from;             // row of the old book, -1: none
@@ -98,9 +105,8 @@ __device__ __forceinline__ bool fork_copies(const PoolDev& p, const BookDev& in,
 }
 
 // Block 0 plans; the others copy the counts, which the second launch then changes.
-__global__ void __launch_bounds__(kPlanThreads)
-fork_plan_kernel(PoolDev p, BookDev in, BookDev out, const int32_t* parent, const int32_t* room, Workspace w, uint32_t* status) {
-    chain_next();
+__device__ __forceinline__ void fork_plan(const PoolDev& p, const BookDev& in, const BookDev& out, const int32_t* parent, const int32_t* room, const Workspace& w,
+                                          uint32_t* status) {
     const int tid = threadIdx.x;
     if (blockIdx.x > 0) {
         for (long long i = (long long)(blockIdx.x - 1) * kPlanThreads + tid; i < p.n_pages; i += (long long)(gridDim.x - 1) * kPlanThreads)
@@ -156,22 +162,28 @@ fork_plan_kernel(PoolDev p, BookDev in, BookDev out, const int32_t* parent, cons
     if (bits) atomicOr(status, bits);
     if (tid == 0) { w.head[0] = short_of ? 0 : (int)(need >> 40); w.head[1] = short_of; }
 }
+__global__ void __launch_bounds__(kPlanThreads)
+fork_plan_kernel(PoolDev p, BookDev in, BookDev out, const int32_t* parent, const int32_t* room, Workspace w, uint32_t* status) {
+    chain_next();
+    fork_plan(p, in, out, parent, room, w, status);
+}
 
 // Copies `used` slots of one plane of a page, the vectors [v0, v0 + n) of them in the plane's own order.
 struct Mover {
     int lanes_log2;       // 16-byte pieces of a vector
     bool slots_inner;     // neighbouring slots are nearer than neighbouring heads
 };
+template <int THREADS>
 __device__ __forceinline__ void move_vectors(const PoolDev& p, const Mover& m, const uint8_t* src, uint8_t* dst, int used, int v0, int n) {
     const int inner = m.slots_inner ? used : p.H;
     const int64_t si = m.slots_inner ? p.sp : p.sh, so = m.slots_inner ? p.sh : p.sp;
     const int units = n << m.lanes_log2;
-    for (int u0 = threadIdx.x; u0 < units; u0 += 4 * kMoveThreads) {
+    for (int u0 = threadIdx.x; u0 < units; u0 += 4 * THREADS) {
         uint4 x[4];
         int64_t off[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int u = u0 + k * kMoveThreads;
+            const int u = u0 + k * THREADS;
             if (u < units) {
                 const int v = v0 + (u >> m.lanes_log2), o = v / inner, i = v - o * inner;
                 off[k] = o * so + i * si + (int64_t)(u & ((1 << m.lanes_log2) - 1)) * 16;
@@ -180,12 +192,13 @@ __device__ __forceinline__ void move_vectors(const PoolDev& p, const Mover& m, c
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-            if (u0 + k * kMoveThreads < units) *reinterpret_cast<uint4*>(dst + off[k]) = x[k];
+            if (u0 + k * THREADS < units) *reinterpret_cast<uint4*>(dst + off[k]) = x[k];
     }
 }
 __device__ __forceinline__ int64_t plane_offset(const PoolDev& p, int plane) { return (int64_t)(plane >> 1) * p.sl + (int64_t)(plane & 1) * p.skv; }
 
 // Every page move of the list, one (move, plane, part) a block at a time; `used` null: whole pages.
+template <int THREADS>
 __device__ __forceinline__ void move_pages(const PoolDev& p, const Mover& m, int moves, const int32_t* src, const int32_t* at, const int32_t* used,
                                            const int32_t* list) {
     const int per_part = max(1, kPartBytes >> (m.lanes_log2 + 4));
@@ -196,15 +209,15 @@ __device__ __forceinline__ void move_pages(const PoolDev& p, const Mover& m, int
         const int u = used ? used[c] : p.page_pos, v0 = part * per_part, n = min(per_part, u * p.H - v0);
         if (n <= 0) continue;
         uint8_t* base = p.base + plane_offset(p, plane);
-        move_vectors(p, m, base + (int64_t)src[c] * p.spage, base + (int64_t)list[at ? at[c] : c] * p.spage, u, v0, n);
+        move_vectors<THREADS>(p, m, base + (int64_t)src[c] * p.spage, base + (int64_t)list[at ? at[c] : c] * p.spage, u, v0, n);
     }
 }
 
-__global__ void __launch_bounds__(kMoveThreads)
-fork_move_kernel(PoolDev p, Mover m, BookDev in, BookDev out, const int32_t* parent, const int32_t* room, Workspace w, uint32_t* status) {
-    chain_wait();
+template <int THREADS>
+__device__ __forceinline__ void fork_move(const PoolDev& p, const Mover& m, const BookDev& in, const BookDev& out, const int32_t* parent, const int32_t* room,
+                                          const Workspace& w, uint32_t* status) {
     const bool short_of = w.head[1] != 0;
-    const long long step = (long long)gridDim.x * kMoveThreads, t0 = (long long)blockIdx.x * kMoveThreads + threadIdx.x;
+    const long long step = (long long)gridDim.x * THREADS, t0 = (long long)blockIdx.x * THREADS + threadIdx.x;
     const int cols = out.max_pages;
     uint32_t bits = 0;
     for (long long i = t0; i < (long long)out.rows * cols; i += step) {
@@ -241,7 +254,18 @@ fork_move_kernel(PoolDev p, Mover m, BookDev in, BookDev out, const int32_t* par
             if (held != 1) atomicAdd(&out.ref[page], held - 1);
         }
     if (bits) atomicOr(status, bits);
-    move_pages(p, m, w.head[0], w.src, w.at, w.used, w.list);
+    move_pages<THREADS>(p, m, w.head[0], w.src, w.at, w.used, w.list);
+}
+__global__ void __launch_bounds__(kMoveThreads)
+fork_move_kernel(PoolDev p, Mover m, BookDev in, BookDev out, const int32_t* parent, const int32_t* room, Workspace w, uint32_t* status) {
+    chain_wait();
+    fork_move<kMoveThreads>(p, m, in, out, parent, room, w, status);
+}
+__global__ void __launch_bounds__(kFewThreads)
+fork_few_kernel(PoolDev p, Mover m, BookDev in, BookDev out, const int32_t* parent, const int32_t* room, Workspace w, uint32_t* status) {
+    fork_plan(p, in, out, parent, room, w, status);
+    cluster_meet();
+    fork_move<kFewThreads>(p, m, in, out, parent, room, w, status);
 }
 
 // Whether row s's path can be kept as it is asked for; every thread of the block calls it.
@@ -265,29 +289,31 @@ __device__ __forceinline__ bool path_ok(const PoolDev& p, const BookDev& in, con
 // Slot len + path[i] -> len + i, i rising: a thread has one 16-byte column of a plane to itself and path[i] >= i, so no
 // slot is written before it has been read.  Eight positions' loads are in flight a thread.  Also copies the counts.
 constexpr int kKeepThreads = 128, kKeepBatch = 64;
-__global__ void __launch_bounds__(kKeepThreads)
-keep_move_kernel(PoolDev p, int lanes_log2, BookDev in, BookDev out, const int32_t* paths, const int32_t* n_path, int stride) {
+template <int THREADS>
+__device__ __forceinline__ void copy_counts(const PoolDev& p, const BookDev& in, const BookDev& out, unsigned block, unsigned blocks) {
+    for (long long i = (long long)block * THREADS + threadIdx.x; i < p.n_pages; i += (long long)blocks * THREADS) out.ref[i] = in.ref[i];
+}
+// `share` of `shares` blocks that move row s.
+template <int THREADS>
+__device__ __forceinline__ void keep_move(const PoolDev& p, int lanes_log2, const BookDev& in, const int32_t* paths, const int32_t* n_path, int stride, int s, int share,
+                                          int shares) {
     __shared__ int64_t from[kKeepBatch], to[kKeepBatch];
-    chain_next();
-    for (long long i = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * kKeepThreads + threadIdx.x; i < p.n_pages;
-         i += (long long)gridDim.x * gridDim.y * kKeepThreads)
-        out.ref[i] = in.ref[i];
-    const int s = blockIdx.x, n = n_path[s], len = in.len[s];
+    const int n = n_path[s], len = in.len[s];
     const int32_t* path = paths + (long long)s * stride;
     const int32_t* row = in.table + (long long)s * in.max_pages;
     if (n == 0 || !path_ok(p, in, path, n, stride, s, len)) return;
-    const int columns = p.H << lanes_log2, blocks = (columns + kKeepThreads - 1) / kKeepThreads, items = 2 * p.L * blocks;
+    const int columns = p.H << lanes_log2, blocks = (columns + THREADS - 1) / THREADS, items = 2 * p.L * blocks;
     for (int i0 = 0; i0 < n; i0 += kKeepBatch) {
         const int m = min(kKeepBatch, n - i0);
         __syncthreads();
-        for (int i = threadIdx.x; i < m; i += kKeepThreads) {
+        for (int i = threadIdx.x; i < m; i += THREADS) {
             const int a = len + path[i0 + i], b = len + i0 + i;
             from[i] = a == b ? -1 : (int64_t)row[a / p.page_pos] * p.spage + (int64_t)(a % p.page_pos) * p.sp;
             to[i] = (int64_t)row[b / p.page_pos] * p.spage + (int64_t)(b % p.page_pos) * p.sp;
         }
         __syncthreads();
-        for (int item = blockIdx.y; item < items; item += gridDim.y) {
-            const int plane = item / blocks, column = (item - plane * blocks) * kKeepThreads + threadIdx.x;
+        for (int item = share; item < items; item += shares) {
+            const int plane = item / blocks, column = (item - plane * blocks) * THREADS + threadIdx.x;
             if (column >= columns) continue;
             uint8_t* base = p.base + plane_offset(p, plane) + (int64_t)(column >> lanes_log2) * p.sh + (int64_t)(column & ((1 << lanes_log2) - 1)) * 16;
             for (int i = 0; i < m; i += 8) {
@@ -302,17 +328,23 @@ keep_move_kernel(PoolDev p, int lanes_log2, BookDev in, BookDev out, const int32
         }
     }
 }
+__global__ void __launch_bounds__(kKeepThreads)
+keep_move_kernel(PoolDev p, int lanes_log2, BookDev in, BookDev out, const int32_t* paths, const int32_t* n_path, int stride) {
+    chain_next();
+    copy_counts<kKeepThreads>(p, in, out, blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y);
+    keep_move<kKeepThreads>(p, lanes_log2, in, paths, n_path, stride, blockIdx.x, blockIdx.y, gridDim.y);
+}
 
 // The new book: a block a row.
-__global__ void __launch_bounds__(kKeepThreads)
-keep_book_kernel(PoolDev p, BookDev in, BookDev out, const int32_t* paths, const int32_t* n_path, int stride, uint32_t* status) {
-    chain_wait();
-    const int s = blockIdx.x, n = n_path[s], len = in.len[s];
+template <int THREADS>
+__device__ __forceinline__ void keep_book(const PoolDev& p, const BookDev& in, const BookDev& out, const int32_t* paths, const int32_t* n_path, int stride, int s,
+                                          uint32_t* status) {
+    const int n = n_path[s], len = in.len[s];
     const bool ok = path_ok(p, in, paths + (long long)s * stride, n, stride, s, len);
     // a row that stays as it is keeps what it holds behind its length, too
     const long long now = (long long)len + n, keep = ok ? (now + p.page_pos - 1) / p.page_pos : in.max_pages;
     uint32_t bits = ok ? 0u : kStRange;
-    for (int j = threadIdx.x; j < in.max_pages; j += kKeepThreads) {
+    for (int j = threadIdx.x; j < in.max_pages; j += THREADS) {
         const long long i = (long long)s * in.max_pages + j;
         const int page = in.table[i];
         if (page != -1 && !page_ok(p, page)) bits |= kStRange;
@@ -322,10 +354,22 @@ keep_book_kernel(PoolDev p, BookDev in, BookDev out, const int32_t* paths, const
     if (threadIdx.x == 0) out.len[s] = ok ? (int)now : len;
     if (bits) atomicOr(status, bits);
 }
+__global__ void __launch_bounds__(kKeepThreads)
+keep_book_kernel(PoolDev p, BookDev in, BookDev out, const int32_t* paths, const int32_t* n_path, int stride, uint32_t* status) {
+    chain_wait();
+    keep_book<kKeepThreads>(p, in, out, paths, n_path, stride, blockIdx.x, status);
+}
+// One row.
+constexpr int kKeepFewThreads = 512;
+__global__ void __launch_bounds__(kKeepFewThreads)
+keep_few_kernel(PoolDev p, int lanes_log2, BookDev in, BookDev out, const int32_t* paths, const int32_t* n_path, int stride, uint32_t* status) {
+    copy_counts<kKeepFewThreads>(p, in, out, blockIdx.x, gridDim.x);
+    keep_move<kKeepFewThreads>(p, lanes_log2, in, paths, n_path, stride, 0, blockIdx.x, gridDim.x);
+    cluster_meet();
+    if (blockIdx.x == 0) keep_book<kKeepFewThreads>(p, in, out, paths, n_path, stride, 0, status);
+}
 
-__global__ void __launch_bounds__(kPlanThreads)
-compact_plan_kernel(PoolDev p, BookDev in, BookDev out, int32_t* moved, Workspace w) {
-    chain_next();
+__device__ __forceinline__ void compact_plan(const PoolDev& p, const BookDev& in, const BookDev& out, int32_t* moved, const Workspace& w) {
     const int tid = threadIdx.x;
     unsigned long long live = 0, total;
     for (long long i = tid; i < p.n_pages; i += kPlanThreads) live += in.ref[i] > 0;
@@ -352,11 +396,16 @@ compact_plan_kernel(PoolDev p, BookDev in, BookDev out, int32_t* moved, Workspac
     }
     if (tid == 0) w.head[0] = moves;
 }
+__global__ void __launch_bounds__(kPlanThreads)
+compact_plan_kernel(PoolDev p, BookDev in, BookDev out, int32_t* moved, Workspace w) {
+    chain_next();
+    compact_plan(p, in, out, moved, w);
+}
 
-__global__ void __launch_bounds__(kMoveThreads)
-compact_move_kernel(PoolDev p, Mover m, BookDev in, BookDev out, const int32_t* moved, Workspace w, uint32_t* status) {
-    chain_wait();
-    const long long step = (long long)gridDim.x * kMoveThreads, t0 = (long long)blockIdx.x * kMoveThreads + threadIdx.x;
+template <int THREADS>
+__device__ __forceinline__ void compact_move(const PoolDev& p, const Mover& m, const BookDev& in, const BookDev& out, const int32_t* moved, const Workspace& w,
+                                             uint32_t* status) {
+    const long long step = (long long)gridDim.x * THREADS, t0 = (long long)blockIdx.x * THREADS + threadIdx.x;
     uint32_t bits = 0;
     for (long long i = t0; i < (long long)in.rows * in.max_pages; i += step) {
         const int page = in.table[i];
@@ -365,7 +414,18 @@ compact_move_kernel(PoolDev p, Mover m, BookDev in, BookDev out, const int32_t* 
     }
     for (long long i = t0; i < in.rows; i += step) out.len[i] = in.len[i];
     if (bits) atomicOr(status, bits);
-    move_pages(p, m, w.head[0], w.src, nullptr, nullptr, w.list);
+    move_pages<THREADS>(p, m, w.head[0], w.src, nullptr, nullptr, w.list);
+}
+__global__ void __launch_bounds__(kMoveThreads)
+compact_move_kernel(PoolDev p, Mover m, BookDev in, BookDev out, const int32_t* moved, Workspace w, uint32_t* status) {
+    chain_wait();
+    compact_move<kMoveThreads>(p, m, in, out, moved, w, status);
+}
+__global__ void __launch_bounds__(kFewThreads)
+compact_few_kernel(PoolDev p, Mover m, BookDev in, BookDev out, int32_t* moved, Workspace w, uint32_t* status) {
+    if (blockIdx.x == 0) compact_plan(p, in, out, moved, w);
+    cluster_meet();
+    compact_move<kFewThreads>(p, m, in, out, moved, w, status);
 }
 
 Mover mover_of(const PoolDev& p) {
@@ -385,6 +445,12 @@ unsigned move_blocks(const PoolDev& p, long long moves, long long words) {
     const long long want = parts > tables ? parts : tables, most = 8LL * sm_count();
     return (unsigned)(want < 1 ? 1 : want > most ? most : want);
 }
+
+// Whether one cluster does a call, by the bytes that it may move at most and the words that it goes through.  A launch less saves the caller 1.7 us (fork of
+// four beams, 16 KB: 15.3 -> 13.6 us a call; a path of 13 positions, 400 KB: 15.4 -> 13.7 us); eight SMs move whole pages slowly (compaction
+// of 400 KB: 7.1 -> 14.8 us), paths, whose loads are all in flight at once, as fast as more.
+constexpr long long kFewPageBytes = 1 << 17, kFewPathBytes = 1 << 20, kFewWords = 1 << 14;
+long long plane_bytes(const PoolDev& p, long long positions) { return positions * p.H * p.d * p.esz * 2 * p.L; }
 
 bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
@@ -429,11 +495,17 @@ plc_status plc_pages_fork(const plc_page_pool* pool, const plc_page_book* in, co
     if ((rc = check_workspace(p, i.rows, o.rows, workspace_dev, workspace_bytes))) return rc;
     const Workspace w = workspace_at(workspace_dev, p.n_pages, i.rows, o.rows);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const long long words = (long long)(i.rows > o.rows ? i.rows : o.rows) * i.max_pages;
+    if (plane_bytes(p, (long long)o.rows * p.page_pos) <= kFewPageBytes && words + p.n_pages <= kFewWords) {
+        if (launch_kernel(fork_few_kernel, kFewBlocks, kFewThreads, 0, st, false, kFewBlocks, p, mover_of(p), i, o, parent_dev, room_dev, w, status_dev) != cudaSuccess)
+            return PLC_E_CUDA;
+        count_launch(1);
+        return PLC_OK;
+    }
     const unsigned counters = (unsigned)((p.n_pages + 4 * kPlanThreads - 1) / (4 * kPlanThreads));
     if (launch_kernel(fork_plan_kernel, 1 + (counters > 64 ? 64 : counters), kPlanThreads, 0, st, false, 1, p, i, o, parent_dev, room_dev, w, status_dev) !=
         cudaSuccess)
         return PLC_E_CUDA;
-    const long long words = (long long)(i.rows > o.rows ? i.rows : o.rows) * i.max_pages;
     if (launch_kernel(fork_move_kernel, move_blocks(p, o.rows, words), kMoveThreads, 0, st, true, 1, p, mover_of(p), i, o, parent_dev, room_dev, w,
                       status_dev) != cudaSuccess)
         return PLC_E_CUDA;
@@ -450,6 +522,13 @@ plc_status plc_pages_keep(const plc_page_pool* pool, const plc_page_book* in, co
     if (!path_dev || !n_path_dev || !status_dev || path_stride < 1) return PLC_E_INVALID;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const Mover m = mover_of(p);
+    if (i.rows == 1 && plane_bytes(p, path_stride) <= kFewPathBytes && (long long)i.max_pages + p.n_pages <= kFewWords) {
+        if (launch_kernel(keep_few_kernel, kFewBlocks, kKeepFewThreads, 0, st, false, kFewBlocks, p, m.lanes_log2, i, o, path_dev, n_path_dev, (int)path_stride,
+                          status_dev) != cudaSuccess)
+            return PLC_E_CUDA;
+        count_launch(1);
+        return PLC_OK;
+    }
     const long long items = 2LL * p.L * (((p.H << m.lanes_log2) + kKeepThreads - 1) / kKeepThreads);
     long long split = (16LL * sm_count() + i.rows - 1) / i.rows;
     split = split > items ? items : split;
@@ -475,6 +554,12 @@ plc_status plc_pages_compact(const plc_page_pool* pool, const plc_page_book* in,
     if ((rc = check_workspace(p, i.rows, o.rows, workspace_dev, workspace_bytes))) return rc;
     const Workspace w = workspace_at(workspace_dev, p.n_pages, i.rows, o.rows);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (plane_bytes(p, (long long)p.n_pages / 2 * p.page_pos) <= kFewPageBytes && (long long)i.rows * i.max_pages + p.n_pages <= kFewWords) {
+        if (launch_kernel(compact_few_kernel, kFewBlocks, kFewThreads, 0, st, false, kFewBlocks, p, mover_of(p), i, o, moved_dev, w, status_dev) != cudaSuccess)
+            return PLC_E_CUDA;
+        count_launch(1);
+        return PLC_OK;
+    }
     if (launch_kernel(compact_plan_kernel, 1, kPlanThreads, 0, st, false, 1, p, i, o, moved_dev, w) != cudaSuccess) return PLC_E_CUDA;
     if (launch_kernel(compact_move_kernel, move_blocks(p, p.n_pages, (long long)i.rows * i.max_pages), kMoveThreads, 0, st, true, 1, p, mover_of(p), i, o,
                       static_cast<const int32_t*>(moved_dev), w, status_dev) != cudaSuccess)

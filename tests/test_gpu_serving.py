@@ -849,3 +849,36 @@ def test_lengths_near_two_to_the_31(dev):
             with pytest.raises(plc.PlcError) as e:
                 pool.check()
             assert e.value.code == plc.E_INVALID
+
+
+@pytest.mark.parametrize("pages, page, L", [(40, 4, 1), (40, 64, 2), (17000, 4, 1)])
+def test_small_and_large_page_calls_alike(dev, ora, pages, page, L):
+    """Calls that one cluster does, and the same ones that more blocks do because of a page's bytes or the pages' number."""
+    rng = np.random.default_rng(pages + page)
+    kv, _ = make_pool(rng, L, pages, 2, page, 32, "f16", dev, False)
+    lens = [page * 2 + 1]
+    table, ref = np.full((1, 8), -1, np.int32), np.zeros(pages, np.int32)
+    held = pages - 1 - np.arange(4)
+    table[0, :4] = held
+    ref[held] = 1
+    pool = plc.PagePool(kv)
+    book = book_of(table, lens, ref, dev)
+    was = kv[:, :, torch.as_tensor(held.astype(np.int64)).to(dev)].clone()
+    two = pool.fork(book, i32([0, 0], dev), i32([page, 1], dev))
+    t, n, r = (x.cpu().numpy() for x in (two.table, two.len, two.ref))
+    assert n.tolist() == [page * 2 + 1] * 2 and (t[:, :2] == held[:2]).all() and r[held[:2]].tolist() == [2, 2] and r.sum() == (t >= 0).sum()
+    assert t[0, 2] == held[2] and t[1, 2] != held[2] and len(set(t[t >= 0])) == len(t[t >= 0]) - 2
+    assert torch.equal(kv[:, :, int(t[1, 2]), :, :1], was[:, :, 2, :, :1])
+    got = pool.keep(book, i32([[1, 2]], dev), i32([2], dev))
+    x = was.permute(0, 1, 3, 2, 4, 5).reshape(L, 2, 2, 4 * page, 32)[:, :, :, page * 2 + 2:page * 2 + 4]
+    at = [page * 2 + 1, page * 2 + 2]
+    for i, p in enumerate(at):
+        assert torch.equal(kv[:, :, int(held[p // page]), :, p % page], x[:, :, :, i])
+    assert got.len.tolist() == [page * 2 + 3] and got.table.cpu().numpy()[0].tolist() == [*held[:3], -1, -1, -1, -1, -1] and int(got.ref.sum()) == 3
+    low, moved = pool.compact(got)
+    assert sorted(low.table.cpu().numpy()[0, :3].tolist()) == [0, 1, 2] and low.ref[:3].tolist() == [1, 1, 1] and int(low.ref.sum()) == 3
+    m = moved.cpu().numpy()
+    assert (m[held[:3]] == low.table.cpu().numpy()[0, :3]).all()
+    for i in range(2):
+        assert torch.equal(kv[:, :, int(m[held[i]])], was[:, :, i])
+    pool.check()
