@@ -24,6 +24,7 @@ struct AttendArgs {
     int tile_pos;                                 // positions a tile (whole pages, or whole parts of a page, where the copies are boxes)
     int box_pos, boxes;                           // positions a box, boxes a tile; 0: no boxes
     int box_dim[4];                               // what dimensions 1 .. 4 of the boxes' map are: 0 slot, 1 head, 2 page, 3 key or value
+    int whole;                                    // not 0: a CTA an item (at most so many), nothing to join
 };
 
 // Which kernel a call takes, and what it needs.
@@ -180,8 +181,8 @@ template <int ROWS> struct Walk {
     __device__ __forceinline__ void start(const PoolDev& p, const BookDev& b, const AttendArgs& a, int session, long long rest) {
         s = session;
         enter(p, b, a);
-        const int item = (int)(rest / tiles);
-        tile = (int)(rest - (long long)item * tiles);
+        const int item = (int)(a.whole ? rest : rest / tiles);
+        tile = a.whole ? 0 : (int)(rest - (long long)item * tiles);
         h = item / row_tiles;
         rt = item - h * row_tiles;
     }
@@ -213,7 +214,7 @@ __device__ __forceinline__ uint32_t seen_bits(const AttendArgs& a, const Session
     return __funnelshift_r(word(w), word(w + 1), j & 31);
 }
 
-// A CTA's range [0, left) of the sequence of tiles, from w on.  Every thread of the CTA calls it; two barriers.
+// A CTA's range [0, left) of the sequence of tiles, from w on (a.whole: of the sequence of items, one of them).  Every thread of the CTA calls it; two barriers.
 template <int ROWS, int THREADS>
 __device__ __forceinline__ long long find_range(const PoolDev& p, const BookDev& b, const AttendArgs& a, uint32_t* status, Walk<ROWS>& w) {
     __shared__ long long sums[THREADS / 32];
@@ -223,7 +224,7 @@ __device__ __forceinline__ long long find_range(const PoolDev& p, const BookDev&
     const int run = (b.rows + THREADS - 1) / THREADS, s0 = min(b.rows, tid * run), s1 = min(b.rows, s0 + run);
     auto tiles_of = [&](int s, bool* bad) -> long long {
         const Session x = session_of(p, b, a, s, bad);
-        return (long long)((x.kv + a.tile_pos - 1) / a.tile_pos) * (((long long)x.n * a.group + ROWS - 1) / ROWS) * p.H;
+        return (long long)(a.whole ? min(x.kv, 1) : (x.kv + a.tile_pos - 1) / a.tile_pos) * (((long long)x.n * a.group + ROWS - 1) / ROWS) * p.H;
     };
     long long mine = 0;
     bool any_bad = false;
@@ -263,7 +264,7 @@ __device__ __forceinline__ long long find_range(const PoolDev& p, const BookDev&
     __syncthreads();
     if (t1 > t0) w.start(p, b, a, (int)range_at[0], range_at[1]);
     if (tid == 0) a.first[me] = t1 > t0 ? make_int4(w.s, w.h, w.rt, w.tile) : make_int4(-1, 0, 0, 0);
-    return t1 - t0;
+    return a.whole ? (t1 > t0 ? w.tiles : 0) : t1 - t0;
 }
 
 // The tiles of a range one after the other; a piece is what the range holds of one item.

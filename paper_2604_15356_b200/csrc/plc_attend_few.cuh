@@ -546,8 +546,9 @@ cudaError_t launch(const PoolDev& p, const BookDev& b, const AttendArgs& a, cons
     if (e != cudaSuccess) return e;
     AttendPlan y = x;
     y.grid = F::per_sm * sm_count();
+    if (a.whole && a.whole < y.grid) y.grid = a.whole;
     e = launch_kernel(few_kernel<T, D, N, BOX>, y.grid, F::threads, F::smem, st, false, 1, p, b, a, map, status);
-    return e != cudaSuccess ? e : launch_join<T, D, N>(p, b, a, y, st);
+    return e != cudaSuccess || a.whole ? e : launch_join<T, D, N>(p, b, a, y, st);
 }
 template <class T>
 cudaError_t launch_few(const PoolDev& p, const BookDev& b, const AttendArgs& args, const AttendPlan& x, bool bf16, uint32_t* status, cudaStream_t st) {

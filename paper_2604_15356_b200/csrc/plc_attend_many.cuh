@@ -498,8 +498,8 @@ cudaError_t launch_many_as(const PoolDev& p, const BookDev& b, const AttendArgs&
     using Sh = Shape<D, NT, BOX>;
     cudaError_t e = cudaFuncSetAttribute(many_kernel<T, D, NT, BOX>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Sh::smem);
     if (e != cudaSuccess) return e;
-    e = launch_kernel(many_kernel<T, D, NT, BOX>, x.grid, Sh::threads, Sh::smem, st, false, 1, p, b, a, map, status);
-    return e != cudaSuccess ? e : launch_join<T, D, Sh::rows>(p, b, a, x, st);
+    e = launch_kernel(many_kernel<T, D, NT, BOX>, a.whole && a.whole < x.grid ? a.whole : x.grid, Sh::threads, Sh::smem, st, false, 1, p, b, a, map, status);
+    return e != cudaSuccess || a.whole ? e : launch_join<T, D, Sh::rows>(p, b, a, x, st);
 }
 template <class T>
 cudaError_t launch_many(const PoolDev& p, const BookDev& b, const AttendArgs& args, const AttendPlan& x, bool bf16, uint32_t* status, cudaStream_t st) {

@@ -882,3 +882,28 @@ def test_small_and_large_page_calls_alike(dev, ora, pages, page, L):
     for i in range(2):
         assert torch.equal(kv[:, :, int(m[held[i]])], was[:, :, i])
     pool.check()
+
+
+@pytest.mark.parametrize("dtype, d, H, G, page, cols, n", [("f16", 64, 1, 1, 16, 24, [1]), ("bf16", 128, 8, 4, 32, 12, [1, 0, 3]), ("f16", 128, 4, 8, 12, 32, [9, 1]),
+                                                           ("bf16", 128, 4, 8, 128, 3, [30, 2]), ("f16", 256, 2, 8, 64, 6, [40, 0, 0, 1]), ("bf16", 32, 8, 2, 8, 48, [1] * 18)])
+def test_attention_of_few_short_items(dev, dtype, d, H, G, page, cols, n):
+    """Calls whose rows of pages are so short that no item is split, beside the same contents in a longer book, where they are."""
+    rng = np.random.default_rng(cols)
+    S = len(n)
+    lens = [int(rng.integers(0, page * cols - max(n) + 1)) for _ in range(S)]
+    lens[0] = page * cols - n[0]
+    held = [-(-(a + b) // page) for a, b in zip(lens, n)]
+    table, ref = make_book(rng, held, cols, sum(held) + 1, dev)
+    gen = torch.Generator(device=dev).manual_seed(0)
+    kv = torch.randn(1, 2, sum(held) + 1, H, page, d, device=dev, generator=gen).to(TYPES[dtype])
+    begin = np.cumsum([0] + n).astype(np.int32)
+    q = torch.randn(int(begin[-1]), H * G, d, device=dev, generator=gen).to(TYPES[dtype])
+    ex, mag, big = attention_in_64_bits(kv, 0, table, lens, q, begin, None, 1 / math.sqrt(d))
+    u = torch.finfo(TYPES[dtype]).eps / 2
+    e = 2 * (d * 2.0 ** -23 * big + 2.0 ** -22 + 2.0 ** -23 * 2 * big)
+    tol = (u + e[..., None] + page * cols * 2.0 ** -23) * mag + u * ex.abs() + torch.finfo(TYPES[dtype]).smallest_normal * u
+    pool = plc.PagePool(kv)
+    for t in (table, np.concatenate([table, np.full((S, 1000), -1, np.int32)], 1)):
+        got = pool.tree_attention(0, book_of(t, lens, ref, dev), q, i32(begin, dev))[0]
+        assert bool(((got.double() - ex).abs() <= tol).all())
+    pool.check()
