@@ -294,12 +294,14 @@ def beam_select(logits, score, n_out, done=None, eos=-1):
         _need(done.dtype == torch.bool and done.device == dev and done.is_contiguous() and done.shape == (S, W), E_INVALID, where)
     kind = _kind(logits.dtype, where)
     need = _bytes(dev, api.plc_beam_workspace, S, W, V, n_out)
+    n = S * n_out
     ws = torch.empty(need, dtype=torch.uint8, device=dev)
     out = torch.empty((S, n_out), dtype=torch.float32, device=dev)
-    parent, token = torch.empty((2, S, n_out), dtype=torch.int32, device=dev).unbind(0)
+    store = torch.empty(2 * n, dtype=torch.int32, device=dev)
+    at = store.data_ptr()
     _check(_run(dev, api.plc_beam_select, logits.data_ptr(), kind, row, S, W, V, score.data_ptr(), None if done is None else done.data_ptr(), eos, n_out,
-                out.data_ptr(), parent.data_ptr(), token.data_ptr(), ws.data_ptr(), need), where)
-    return out, parent, token
+                out.data_ptr(), at, at + 4 * n, ws.data_ptr(), need), where)
+    return out, store.as_strided((S, n_out), (n_out, 1), 0), store.as_strided((S, n_out), (n_out, 1), n)
 
 
 def beam_reorder(parent, states, status=None):
@@ -319,8 +321,8 @@ def beam_reorder(parent, states, status=None):
         size = t.element_size()
         row = t.numel() // rows_in * size
         if row:
-            sets.append(RowSet(t.data_ptr(), o.data_ptr(), t.stride(0) * size, row, row))
-    for i in range(0, len(sets), 16):
-        some = sets[i:i + 16]
-        _check(_run(dev, api.plc_beam_reorder, (RowSet * len(some))(*some), len(some), parent.data_ptr(), rows_in, rows, word), where)
+            sets += (t.data_ptr(), o.data_ptr(), t.stride(0) * size, row, row)
+    for i in range(0, len(sets), 80):                        # sixteen plc_row_set of five 64-bit words
+        some = sets[i:i + 80]
+        _check(_run(dev, api.plc_beam_reorder, (C.c_int64 * len(some))(*some), len(some) // 5, parent.data_ptr(), rows_in, rows, word), where)
     return out
