@@ -45,21 +45,28 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarri
 __device__ __forceinline__ void mbar_arrive_copies(uint32_t bar) {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
+__device__ __forceinline__ bool mbar_done(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok;
+}
 // Bounded wait: false where another role has given up, or (error bit set) the phase did not complete within the limit.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* failed, uint32_t* status) {
+__device__ __noinline__ bool mbar_wait_on(uint32_t bar, uint32_t parity, volatile uint32_t* failed, uint32_t* status) {
+#pragma unroll 1
     for (uint32_t i = 0; i < kSpin; ++i) {
-        uint32_t ok;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-        if (ok) return true;
+        if (mbar_done(bar, parity)) return true;
         if ((i & 15) == 15 && *failed) return false;
     }
     *failed = 1u;
     atomicOr(status, kStTimeout);
     return false;
+}
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* failed, uint32_t* status) {
+    return mbar_done(bar, parity) || mbar_wait_on(bar, parity, failed, status);
 }
 // Not ordered with the compiler's own accesses: what is copied to is read behind a barrier only.
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src)); }
@@ -228,6 +235,7 @@ __device__ __forceinline__ long long find_range(const PoolDev& p, const BookDev&
     };
     long long mine = 0;
     bool any_bad = false;
+#pragma unroll 1
     for (int s = s0; s < s1; ++s) {
         bool bad;
         mine += tiles_of(s, &bad);
@@ -243,6 +251,7 @@ __device__ __forceinline__ long long find_range(const PoolDev& p, const BookDev&
     if (lane == 31) sums[wid] = upto;
     __syncthreads();
     long long total = 0, ahead = upto - mine;
+#pragma unroll 1
     for (int v = 0; v < THREADS / 32; ++v) {
         if (v < wid) ahead += sums[v];
         total += sums[v];
@@ -253,6 +262,7 @@ __device__ __forceinline__ long long find_range(const PoolDev& p, const BookDev&
         long long at = ahead;
         bool bad;
         int s = s0;
+#pragma unroll 1
         for (; s < s1; ++s) {
             const long long f = tiles_of(s, &bad);
             if (t0 < at + f) break;

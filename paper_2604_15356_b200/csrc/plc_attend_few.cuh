@@ -55,6 +55,9 @@ __device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t* r) {
           "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(addr) : "memory");
 }
+__device__ __forceinline__ void tmem_ld4(uint32_t addr, uint32_t* r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
 __device__ __forceinline__ float warp_max(float x) {
     float y;
     asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
@@ -185,7 +188,7 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
                 const int r = 32 * e + lane, rr = x.w.rt * N + r, i = rr / a.group;
                 row[e] = r < rows ? (unsigned long long)a.q + 2 * ((int64_t)(x.w.x.first + i) * a.qs_row + (int64_t)(x.w.h * a.group + rr - i * a.group) * a.qs_head) : 0ull;
             }
-#pragma unroll 4
+#pragma unroll 2
             for (int u = lt; u < N * pieces; u += F::q_copy) {
                 const int r = u / pieces, c = u % pieces;
                 unsigned long long src = __shfl_sync(kFull, row[0], r & 31);
@@ -348,7 +351,7 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
             const int64_t slot = ((int64_t)2 * blockIdx.x + (f.piece > 0)) * a.part_rows;
             if (tid < rows) {
                 const float l = (sum_s[tid] + sum_s[N + tid]) + (sum_s[2 * N + tid] + sum_s[3 * N + tid]), top = last_top_s[tid];
-                const int rr = row0 + tid, i = rr / a.group;
+                const int rr = row0 + tid, i = (int)((uint32_t)rr / (uint32_t)a.group);
                 const int64_t n_row = f.w.x.first + i, head = (int64_t)f.w.h * a.group + (rr - i * a.group);
                 row_at[tid] = whole ? reinterpret_cast<int64_t>(a.out) + 2 * (n_row * a.os_row + head * a.os_head) : reinterpret_cast<int64_t>(a.part_o + (slot + tid) * D);
                 inv_s[tid] = l == 0.f ? 0.f : whole ? 1.f / l : 1.f;             // 0: nothing was seen
@@ -357,22 +360,25 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
             }
             vote_all<2, F::soft>(true);
             fence_after();
+            // four rows at a time: this code is fetched anew for most pieces, and short code costs less than more loads at a time give
 #pragma unroll 1
-            for (int ch = 0; ch < F::o_blocks * C / 16; ++ch) {
-                const int r0 = 16 * ch % C + col0, d = 16 * ch / C * 128 + pos;
-                if (r0 >= rows) continue;
-                uint32_t y[16];
-                tmem_ld16(o_at + ((f.piece & 1) * F::o_blocks + 16 * ch / C) * N + 16 * ch % C, y);
-                wait_ld(y);
-                if (d >= D) continue;
+            for (int o = 0; o < F::o_blocks; ++o) {
+                const int d = o * 128 + pos;
+#pragma unroll 1
+                for (int r0 = col0; r0 < min(rows, col0 + C); r0 += 4) {
+                    uint32_t y[4];
+                    tmem_ld4(o_at - col0 + ((f.piece & 1) * F::o_blocks + o) * N + r0, y);
+                    wait_ld(y);
+                    if (d >= D) continue;
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (r0 + r < rows) {
-                        const float g = inv_s[r0 + r], v = g == 0.f ? 0.f : __uint_as_float(y[r]) * g;
-                        const int64_t to = row_at[r0 + r];
-                        if (whole) reinterpret_cast<uint16_t*>(to)[d] = (uint16_t)(Kind<T>::pack(v, 0.f) & 0xffffu);
-                        else reinterpret_cast<float*>(to)[d] = v;
-                    }
+                    for (int r = 0; r < 4; ++r)
+                        if (r0 + r < rows) {
+                            const float g = inv_s[r0 + r], v = g == 0.f ? 0.f : __uint_as_float(y[r]) * g;
+                            const int64_t to = row_at[r0 + r];
+                            if (whole) reinterpret_cast<uint16_t*>(to)[d] = (uint16_t)(Kind<T>::pack(v, 0.f) & 0xffffu);
+                            else reinterpret_cast<float*>(to)[d] = v;
+                        }
+                }
             }
             if (dirty[f.piece & 1] == (uint32_t)f.piece + 1u && vote_all<2, F::soft>(true))       // every group's rows are written
                 for (int d = tid; d < D; d += F::soft)
@@ -503,6 +509,7 @@ few_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
                     ok = ok && mbar_wait(v_full + 8 * (x % v_slots), (uint32_t)(x / v_slots) & 1u, failed, status);
                     uint8_t* tile = ring + (k_slots + x % v_slots) * F::slot;
                     if (ok && blank)
+#pragma unroll 2
                         for (int e = 0; e < F::blocks * 8; ++e)
                             *reinterpret_cast<uint4*>(tile + (e >> 3) * (kTN * 128) + pos * 128 + (((e & 7) ^ (pos & 7)) << 4)) = make_uint4(0, 0, 0, 0);
                     else if (ok && hide && pos < tile_pos && t0 + pos >= sx.w.x.len && t0 + pos < sx.w.x.kv && special<T, D, kTN>(tile, pos) && take_out<T, D, kTN>(tile, pos))
