@@ -907,3 +907,25 @@ def test_attention_of_few_short_items(dev, dtype, d, H, G, page, cols, n):
         got = pool.tree_attention(0, book_of(t, lens, ref, dev), q, i32(begin, dev))[0]
         assert bool(((got.double() - ex).abs() <= tol).all())
     pool.check()
+
+
+@pytest.mark.parametrize("n, lens", [([2, 1], [300, 40]), ([40, 3], [1000, 7]), ([5, 60], [0, 2000])])
+def test_attention_into_strided_results_and_from_expanded_queries(dev, n, lens):
+    """Results as a view of a wider tensor whose other elements stay as they are; one query row for all."""
+    rng = np.random.default_rng(1)
+    H, G, d, page = 2, 8, 128, 32
+    held = [-(-(a + b) // page) for a, b in zip(lens, n)]
+    table, ref = make_book(rng, held, max(held), sum(held), dev)
+    gen = torch.Generator(device=dev).manual_seed(2)
+    kv = torch.randn(1, 2, sum(held), H, page, d, device=dev, generator=gen).half()
+    begin = np.cumsum([0] + n).astype(np.int32)
+    N = int(begin[-1])
+    pool, book = plc.PagePool(kv), book_of(table, lens, ref, dev)
+    q = torch.randn(1, H * G, d, device=dev, generator=gen).half().expand(N, H * G, d)
+    want, lse = pool.tree_attention(0, book, q.contiguous(), i32(begin, dev))
+    wide = torch.full((N, H * G + 2, d + 24), 5.0, dtype=torch.float16, device=dev)
+    got, lse2 = pool.tree_attention(0, book, q, i32(begin, dev), out=wide[:, 1:-1, 16:-8])
+    assert torch.equal(got, want) and torch.equal(lse, lse2)
+    wide[:, 1:-1, 16:-8] = 5.0
+    assert bool((wide == 5).all())
+    pool.check()
