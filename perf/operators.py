@@ -389,8 +389,7 @@ def _beam(st):
     f = x.sub_(x.exp().sum(-1, keepdim=True).log_()).add_(cum[..., None])                           # [S][W][V] scores
     f.masked_fill_(st["done"][..., None], -math.inf)
     f[..., st["eos"]] = torch.where(st["done"], cum, f[..., st["eos"]])
-    f = f.view(S, W * V)
-    f.masked_fill_(~f.isfinite(), -math.inf)            # such a score is none
+    f = f.view(S, W * V).nan_to_num_(nan=-math.inf, posinf=math.inf, neginf=-math.inf)
     best, at = f.topk(n, dim=1)
     # ties at the border go to the lowest index: the r-th candidate that has the last value taken
     last = best[:, -1:]
@@ -400,12 +399,9 @@ def _beam(st):
     at, o = at.sort(1)
     best, o = best.gather(1, o).sort(dim=1, descending=True, stable=True)
     at = at.gather(1, o)
-    none = best == -math.inf
-    parent = torch.where(none, -1, at // V + torch.arange(S, device=at.device)[:, None] * W).int()
-    token = torch.where(none, -1, at % V).int()
+    parent = (at // V + torch.arange(S, device=at.device)[:, None] * W).int()
     rows = parent.flatten().long()
-    tokens, logp2 = (torch.where(rows[:, None] < 0, torch.zeros_like(t[0]), t[rows.clamp(min=0)]) for t in st["states"])
-    return {"score": best.float(), "parent": parent, "token": token, "tokens": tokens, "logp2": logp2}
+    return {"score": best.float(), "parent": parent, "token": (at % V).int(), "tokens": st["states"][0][rows], "logp2": st["states"][1][rows]}
 
 
 # ---------------------------------------------------------------------------------------------- work and exact values
