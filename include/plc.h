@@ -434,8 +434,9 @@ plc_status plc_tree_attention_workspace(const plc_page_pool* pool, int32_t sessi
 
 /* One step of beam search for `sessions` sessions of `beams` beams: of the beams*vocab continuations with
  *     score_dev[b][w] + logits[b][w][v] - log sum_v' exp logits[b][w][v']
- * the n_out largest, in falling order, ties to the lowest (w, v); formed and compared in binary64 from the row's
- * log-sum-exp.  logits_dev: [sessions*beams] rows of row_stride elements, dtype as plc_page_pool.  done_dev [sessions][beams]
+ * the n_out largest, in falling order, ties to the lowest (w, v); formed and compared in binary64 as
+ * (logit - the row's largest) + (score - log of the row's sum of exp(logit - the largest)), so that rows of the type's lowest
+ * values keep their score.  logits_dev: [sessions*beams] rows of row_stride elements, dtype as plc_page_pool.  done_dev [sessions][beams]
  * bytes or NULL: a beam that is done has one continuation, the token `eos`, at its own score.  A score that is not
  * finite (a dead beam's -inf, a row with NaN or +inf) is none.  Outputs [sessions][n_out]: the score (binary32), the parent
  * as a row b*beams + w (for plc_pages_fork and plc_beam_reorder) and the token; places without a continuation get

@@ -175,9 +175,9 @@ def beam_select(logits, score, n_out, done=None, eos=-1):
             x = logits[s, w].astype(np.float64)
             if np.isnan(x).any() or x.max() == math.inf or x.max() == -math.inf:
                 continue
-            lse = x.max() + math.log(np.exp(x - x.max()).sum())
+            rest = own - math.log(np.exp(x - x.max()).sum())     # the maximum stays with x: at -3e38 it would swallow all else
             order = np.lexsort((np.arange(V), -x))[:n_out]
-            c += [(-(own + x[v] - lse), w, int(v)) for v in order if x[v] > -math.inf]
+            c += [(-((x[v] - x.max()) + rest), w, int(v)) for v in order if x[v] > -math.inf]
         for i, (f, w, v) in enumerate(sorted(c)[:n_out]):
             out[s, i], parent[s, i], token[s, i] = -f, s * W + w, v
     return out, parent, token

@@ -7,7 +7,8 @@
 // Measured: 512 rows of 128256 logits in bf16, 8 beams a session and 8 of their continuations: rows 38 us (131 MB, 3.4 TB/s; the exponentials' unit 0.49 busy,
 // 21 warps an SM), merge 8 us, the states' rows 10 us; 49 us together.  With a list a warp that every logit was held against: 229 us.
 //
-// Exactness: continuations of different rows are compared by score + x - lse in binary64.  Exponentials are binary32 (x - maximum
+// Exactness: continuations of different rows are compared by (x - maximum) + (score - log sum) in binary64, the maximum taken off first: at the
+// type's lowest values (a row that is masked with them as a whole) nothing else would be left of the sum.  Exponentials are binary32 (x - maximum
 // is subtracted before it is scaled, so that the largest terms, which carry the sum, have the smallest errors); 32 of them are added in
 // binary32 and the groups in binary64, in an order that depends on the column alone and not on the row's alignment:
 // equal rows have equal sums, so that their ties go to the lower row.
@@ -397,7 +398,8 @@ __device__ __forceinline__ double double_of(unsigned long long o) {
 constexpr int kMergeThreads = 256, kMergeWarps = kMergeThreads / 32;
 __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(SelectArgs a) {
     extern __shared__ unsigned long long keys[];             // [beams][parts][k]
-    __shared__ double offset[kMostOut];                      // score - lse; -inf: no continuation
+    __shared__ double offset[kMostOut];                      // score - log of the sum of exp(x - top); -inf: no continuation
+    __shared__ float row_top[kMostOut];                      // the row's largest logit
     __shared__ Cont best[kMergeWarps][32];
     __shared__ Cont border;
     chain_wait();
@@ -408,16 +410,17 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(SelectArgs a)
         const long long row = (long long)b * a.beams + w;
         const double own = (double)a.score[row];
         double o = own;
+        float top = -FLT_MAX;
         if (a.done && a.done[row]) {                         // its one continuation stands first in its first list
             o = 0.0;
             if (!isfinite(own)) o = -INFINITY;
         } else {
-            float top = -FLT_MAX;
             for (int p = 0; p < a.parts; ++p) top = fmaxf(top, a.top[row * a.parts + p]);
             double sum = 0.0;
             for (int p = 0; p < a.parts; ++p) sum += a.sum[row * a.parts + p] * (double)exp2_approx((a.top[row * a.parts + p] - top) * kLog2e);
-            o = own - ((double)top + log(sum));
+            o = own - log(sum);
         }
+        row_top[w] = top;
         offset[w] = isfinite(own) && isfinite(o) ? o : -INFINITY;
     }
     __syncthreads();
@@ -437,7 +440,7 @@ __global__ void __launch_bounds__(kMergeThreads) beam_merge_kernel(SelectArgs a)
                         c = Cont{order_bits((double)a.score[(long long)b * a.beams + w]), (uint32_t)w * (uint32_t)a.V + (uint32_t)a.eos};
                 } else {
                     const unsigned long long key = keys[l * a.k + j];
-                    const double s = (double)value_of((uint32_t)(key >> 32)) + o;
+                    const double s = ((double)value_of((uint32_t)(key >> 32)) - (double)row_top[w]) + o;
                     if (key != 0 && s > -INFINITY) c = Cont{order_bits(s), (uint32_t)w * (uint32_t)a.V + ~(uint32_t)key};
                 }
             }

@@ -929,3 +929,38 @@ def test_attention_into_strided_results_and_from_expanded_queries(dev, n, lens):
     wide[:, 1:-1, 16:-8] = 5.0
     assert bool((wide == 5).all())
     pool.check()
+
+
+# ---------------------------------------------------------------------------------------------- calls at the borders
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("V", [259, 32000, 70001])
+def test_beam_selection_at_the_lowest_values(dev, dtype, V):
+    """Tokens masked with the type's lowest finite value: all of a beam's, all but one, some, of several sessions.  A beam that is masked as a
+    whole has each token at its score less log V.  Exact values by the formula in binary64, the row's maximum taken off first; tolerance as above."""
+    low = torch.finfo(TYPES[dtype]).min
+    rng = np.random.default_rng(V)
+    x = spaced(rng, 4, 4, V, dtype, dev)
+    x[0, 0] = low
+    x[0, 2] = low
+    x[0, 2, V - 2] = 1.5
+    x[0, 3, ::2] = low
+    x[1] = low                                               # nothing else in the session
+    x[2, 1:] = low
+    x[2, 0] = low
+    x[2, 0, 17] = -4.0
+    x[3, :, 1:] = low
+    cum = torch.tensor([[-5.0, -20.0, -9.3, -30.17], [-20.0, -math.inf, -20.0, -19.51], [-7.0, -math.inf, -math.inf, -math.inf], [-4.0, -3.0, -2.0, -1.0]], device=dev)
+    n_out = 40
+    f = x.double()
+    f = f - f.amax(-1, keepdim=True)
+    f = ((f - f.exp().sum(-1, keepdim=True).log()) + cum.double()[..., None]).flatten(1)
+    best, at = f.sort(dim=1, descending=True, stable=True)
+    step = (best[:, :n_out] - best[:, 1:n_out + 1]).cpu()
+    assert bool((torch.isnan(step) | (step == 0) | (step > 2.0 ** -18)).all())
+    best, at = best[:, :n_out], at[:, :n_out]
+    none = best == -math.inf
+    s, p, t = plc.beam_select(x, cum, n_out)
+    assert torch.equal(p.long(), torch.where(none, -1, at // V + 4 * torch.arange(4, device=dev)[:, None])) and torch.equal(t.long(), torch.where(none, -1, at % V))
+    assert bool((s[none] == -math.inf).all()) and bool(((s.double() - best).abs() <= 2.0 ** -20 + 2.0 ** -23 * best.abs())[~none].all())
+    assert p[1, 0] == 7 and abs(float(s[1, 0]) - (-19.51 - math.log(V))) < 1e-4

@@ -145,3 +145,17 @@ def test_the_binding_checks_its_tensors():
         plc.beam_select(torch.zeros(1, 2, 8), torch.zeros(1, 2), 2)
     with pytest.raises(plc.PlcError):
         plc.beam_reorder(i, [i])
+
+
+@pytest.mark.parametrize("low", [float(np.finfo(np.float32).min), -3.3895313892515355e38, -65504.0, -1e9])
+def test_the_oracle_at_the_lowest_values(low):
+    """A beam whose tokens all are masked with one value has each at its own score less log V, and does not pass a live one."""
+    from oracle import serving as o
+    V = 32000
+    x = np.full((1, 2, V), low)
+    x[0, 1] = 0.0
+    x[0, 1, 7] = 20.0
+    s, p, k = o.beam_select(x, np.array([[-20.0, -30.0]]), 3)
+    live = -30.0 - np.log(np.exp(-20.0) * (V - 1) + 1)
+    assert p.tolist() == [[1, 0, 0]] and k.tolist() == [[7, 0, 1]]
+    assert np.allclose(s, [[live, -20.0 - np.log(V), -20.0 - np.log(V)]], rtol=1e-13)
