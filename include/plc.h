@@ -358,7 +358,8 @@ plc_status plc_rans_encode_static(const int32_t* sym_dev, const int32_t* q_dev, 
  * the slot in the page: element (layer, kv, page, head, slot, component) stands at
  * layer*stride_layer + kv*stride_kv + page*stride_session + head*stride_head + slot*stride_pos + component.
  * Heads first and slots first are both only strides; where stride_session = page_pos*stride_pos, a run of pages
- * is a plain KV tensor that plc_decode can restore into.  dtype: PLC_OUT_F32, PLC_OUT_F16 or PLC_OUT_BF16.
+ * is a plain KV tensor that plc_decode can restore into (the pool's dtype has to be the context's out_dtype, which nothing
+ * here can see) or plc_encode read (f16).  dtype: PLC_OUT_F32, PLC_OUT_F16 or PLC_OUT_BF16.
  * n_pages, page_pos >= 1; head_dim as in plc_config. */
 typedef struct {
     plc_kv_view view;

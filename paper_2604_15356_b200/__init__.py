@@ -62,6 +62,11 @@ class KVView(C.Structure):
                 ("stride_session", C.c_int64), ("stride_head", C.c_int64), ("stride_pos", C.c_int64)]
 
 
+class PoolView(KVView):
+    """A view that knows what it stands for (PagePool.sessions_view): dtype (OUT_*), and extents = (layers, heads, head_dim, sessions,
+    positions) that lie behind it."""
+
+
 class Streams(C.Structure):
     _fields_ = [("payload_dev", C.c_void_p), ("payload_capacity", C.c_uint64), ("chunk_offset_dev", C.c_void_p),
                 ("chunk_bytes_dev", C.c_void_p), ("total_bytes_dev", C.c_void_p), ("max_chunks", C.c_int32)]
@@ -258,17 +263,30 @@ class Context:
         _check(lib().plc_rotq_record_bytes(self._h, int(bits), C.byref(b)), "plc_rotq_record_bytes")
         return b.value
 
+    def _view(self, kv, S, n, dtype, where):
+        """kv as a KVView.  One that knows its type and extents has to be of the type that the call reads or writes, and to hold what it
+        reads or writes."""
+        if not isinstance(kv, KVView):
+            return kv_view(kv)
+        if isinstance(kv, PoolView):
+            L, H, d, sessions, positions = kv.extents
+            if kv.dtype != dtype:
+                raise PlcError(E_INVALID, where)
+            if self.cfg.n_layers > L or self.cfg.n_kv_heads > H or self.cfg.head_dim != d or S > sessions or n > positions:
+                raise PlcError(E_SHAPE, where)
+        return kv
+
     def encode_rotq(self, kv, logits, params, records, pos_begin=None, pos_end=None):
         """Rotated fixed-rate quantiser (Prop. 3 step 3): records uint8 [S*W*n*record_bytes] on the device."""
         S, n = logits.shape[0], logits.shape[1]
-        view = kv if isinstance(kv, KVView) else kv_view(kv)
+        view = self._view(kv, S, n, OUT_F16, "plc_encode_rotq")
         _check(lib().plc_encode_rotq(self._h, C.byref(view), _ptr(logits), S, n, _ptr(pos_begin), _ptr(pos_end),
                                      C.byref(params), _ptr(records), C.c_uint64(records.numel() * records.element_size()),
                                      _stream()), "plc_encode_rotq")
 
     def decode_rotq(self, records, logits, params, kv_out, pos_begin=None, pos_end=None):
         S, n = logits.shape[0], logits.shape[1]
-        view = kv_out if isinstance(kv_out, KVView) else kv_view(kv_out)
+        view = self._view(kv_out, S, n, self.cfg.out_dtype, "plc_decode_rotq")
         _check(lib().plc_decode_rotq(self._h, _ptr(records), C.c_uint64(records.numel() * records.element_size()),
                                      _ptr(logits), S, n, _ptr(pos_begin), _ptr(pos_end), C.byref(params), C.byref(view),
                                      _stream()), "plc_decode_rotq")
@@ -284,7 +302,7 @@ class Context:
 
     def encode(self, kv, logits, streams, pos_begin=None, pos_end=None, debug=None, tokens=None):
         S, n = logits.shape[0], logits.shape[1]
-        view = kv if isinstance(kv, KVView) else kv_view(kv)
+        view = self._view(kv, S, n, OUT_F16, "plc_encode")
         st = streams.c()
         if tokens is not None:
             _check(lib().plc_encode_adaptive(self._h, C.byref(view), _ptr(logits), _ptr(tokens), S, n, _ptr(pos_begin),
@@ -296,7 +314,7 @@ class Context:
 
     def decode(self, streams, logits, kv_out, pos_begin=None, pos_end=None, debug=None, tokens=None):
         S, n = logits.shape[0], logits.shape[1]
-        view = kv_out if isinstance(kv_out, KVView) else kv_view(kv_out)
+        view = self._view(kv_out, S, n, self.cfg.out_dtype, "plc_decode")
         st = streams.c()
         if tokens is not None:
             _check(lib().plc_decode_adaptive(self._h, C.byref(st), _ptr(logits), _ptr(tokens), S, n, _ptr(pos_begin),

@@ -7,7 +7,7 @@ and captured graphs do not share any.
 """
 import ctypes as C
 
-from . import E_ALIGN, E_CAPACITY, E_CUDA, E_INVALID, E_SHAPE, OUT_BF16, OUT_F16, OUT_F32, KVView, PlcError, _check, lib
+from . import E_ALIGN, E_CAPACITY, E_CUDA, E_INVALID, E_SHAPE, OUT_BF16, OUT_F16, OUT_F32, KVView, PlcError, PoolView, _check, lib
 
 
 class PagePoolC(C.Structure):
@@ -177,14 +177,18 @@ class PagePool:
 
     def sessions_view(self, first_page, sessions, n):
         """KVView of consecutive pages as plain sessions of n positions, for Context.encode / Context.decode: session i
-        has the pages first_page + i * ceil(n / page) ....  Needs slots before heads, so that a page follows the other."""
+        has the pages first_page + i * ceil(n / page) ....  Needs slots before heads, so that a page follows the other.
+        The pool's type has to be what the call works in: float16 for encoding, the context's out_dtype for decoding (a
+        pool that attention reads: out_dtype=OUT_F16; bfloat16 pools have no such calls)."""
         c, page = self._c, self.kv.shape[4]
         each = -(-n // page)
         _need(c.view.stride_session == page * c.view.stride_pos, E_SHAPE, "sessions_view")
         _need(first_page >= 0 and sessions >= 1 and n >= 1 and first_page + sessions * each <= c.n_pages, E_INVALID, "sessions_view")
         v = c.view
-        return KVView(self.kv.data_ptr() + first_page * v.stride_session * self.kv.element_size(), v.stride_layer, v.stride_kv,
-                      each * v.stride_session, v.stride_head, v.stride_pos)
+        view = PoolView(self.kv.data_ptr() + first_page * v.stride_session * self.kv.element_size(), v.stride_layer, v.stride_kv,
+                        each * v.stride_session, v.stride_head, v.stride_pos)
+        view.dtype, view.extents = c.dtype, (c.n_layers, c.n_kv_heads, c.head_dim, sessions, each * page)
+        return view
 
     def _book(self, book, where):
         _need(book.device == self.device, E_INVALID, where)

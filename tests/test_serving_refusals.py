@@ -159,3 +159,76 @@ def test_the_oracle_at_the_lowest_values(low):
     live = -30.0 - np.log(np.exp(-20.0) * (V - 1) + 1)
     assert p.tolist() == [[1, 0, 0]] and k.tolist() == [[7, 0, 1]]
     assert np.allclose(s, [[live, -20.0 - np.log(V), -20.0 - np.log(V)]], rtol=1e-13)
+
+
+class _Reached:
+    """Stands in for the library: notes which calls come through, and does nothing."""
+
+    def __init__(self):
+        self.calls = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.calls.append(name)
+            return plc.OK
+        return call
+
+
+def _session_pages(kind, L=2, H=4, d=64, pages=12, page=16):
+    import torch
+    p = plc.PagePool.__new__(plc.PagePool)
+    p.kv = torch.zeros(L, 2, pages, page, H, d, dtype={plc.OUT_F16: torch.float16, plc.OUT_BF16: torch.bfloat16, plc.OUT_F32: torch.float32}[kind]).transpose(3, 4)
+    p._c = serving.PagePoolC(plc.kv_view(p.kv), L, H, d, pages, page, kind)
+    return p
+
+
+def _codec_calls(monkeypatch, out_dtype, L=2, H=4, d=64, V=8):
+    """Context without a library behind it -> the calls that take a view, by name: (what it needs, the call)."""
+    import torch
+    ctx = plc.Context.__new__(plc.Context)
+    ctx.cfg, ctx.T, ctx._h = plc.Config(L, H, d, V, 4, 0.02, 0.0, 32, 0, out_dtype), None, C.c_void_p()
+    lib = _Reached()
+    monkeypatch.setattr(plc, "lib", lambda: lib)
+    monkeypatch.setattr(plc, "_stream", lambda: None)
+
+    class St:
+        c = staticmethod(plc.Streams)
+    x = lambda S, n: torch.zeros(S, n, V, dtype=torch.float16)  # noqa: E731
+    rec, par, tok = torch.zeros(16, dtype=torch.uint8), plc.RotqParams(), torch.zeros(4, dtype=torch.int32)
+    return lib, {"plc_encode": (plc.OUT_F16, lambda v, S, n: ctx.encode(v, x(S, n), St)), "plc_decode": (out_dtype, lambda v, S, n: ctx.decode(St, x(S, n), v)),
+                 "plc_encode_adaptive": (plc.OUT_F16, lambda v, S, n: ctx.encode(v, x(S, n), St, tokens=tok)),
+                 "plc_decode_adaptive": (out_dtype, lambda v, S, n: ctx.decode(St, x(S, n), v, tokens=tok)),
+                 "plc_encode_rotq": (plc.OUT_F16, lambda v, S, n: ctx.encode_rotq(v, x(S, n), par, rec)),
+                 "plc_decode_rotq": (out_dtype, lambda v, S, n: ctx.decode_rotq(rec, x(S, n), par, v))}
+
+
+@pytest.mark.parametrize("out_dtype", [plc.OUT_F16, plc.OUT_F32])
+@pytest.mark.parametrize("kind", [plc.OUT_F16, plc.OUT_BF16, plc.OUT_F32])
+def test_pages_of_another_type_are_not_coded(monkeypatch, kind, out_dtype):
+    """A run of pages is taken by the codec's calls in the pool's own type alone, and as far as it reaches."""
+    view = _session_pages(kind).sessions_view(1, 3, 40)
+    lib, calls = _codec_calls(monkeypatch, out_dtype)
+    for name, (needs, call) in calls.items():
+        del lib.calls[:]
+        if needs != kind:
+            with pytest.raises(plc.PlcError) as e:
+                call(view, 3, 40)
+            assert e.value.code == plc.E_INVALID and lib.calls == [], name
+            continue
+        call(view, 3, 40)
+        call(view, 1, 48)                                                  # a session has three pages
+        assert lib.calls == [name, name]
+        for S, n in ((4, 40), (3, 49)):
+            with pytest.raises(plc.PlcError) as e:
+                call(view, S, n)
+            assert e.value.code == plc.E_SHAPE and lib.calls == [name, name], name
+
+
+@pytest.mark.parametrize("change", [dict(L=3), dict(H=5), dict(d=128), dict(d=32)])
+def test_pages_of_another_shape_are_not_coded(monkeypatch, change):
+    view = _session_pages(plc.OUT_F16).sessions_view(0, 2, 20)
+    lib, calls = _codec_calls(monkeypatch, plc.OUT_F16, **change)
+    for name, (_, call) in calls.items():
+        with pytest.raises(plc.PlcError) as e:
+            call(view, 2, 20)
+        assert e.value.code == plc.E_SHAPE and lib.calls == [], name
