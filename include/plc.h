@@ -354,6 +354,10 @@ plc_status plc_rans_encode_static(const int32_t* sym_dev, const int32_t* q_dev, 
  *   8   a bounded wait inside a kernel ran out (the call's output is incomplete)
  *   32  a page number, parent, path, length or row range out of range (per call: what then happens) */
 
+/* Moves the bits of a status word to *bits_dev and zeroes the word, in one step: bits that calls on other streams set
+ * meanwhile are in *bits_dev or still in the word. */
+plc_status plc_take_status(uint32_t* status_dev, uint32_t* bits_dev, void* stream);
+
 /* Pool of n_pages pages of page_pos positions each.  The view's session index is the page and its position index
  * the slot in the page: element (layer, kv, page, head, slot, component) stands at
  * layer*stride_layer + kv*stride_kv + page*stride_session + head*stride_head + slot*stride_pos + component.

@@ -26,7 +26,7 @@ EXPORTS = ["plc_create", "plc_destroy", "plc_reserve", "plc_topk_softmax", "plc_
            "plc_launch_count", "plc_rans_encode_static", "plc_encode_adaptive", "plc_decode_adaptive",
            "plc_trie_create", "plc_trie_destroy", "plc_trie_insert", "plc_trie_best_match", "plc_trie_evict",
            "plc_trie_stats", "plc_create_linear", "plc_prefix_clusters", "plc_rotq_record_bytes", "plc_encode_rotq",
-           "plc_decode_rotq", "plc_poll_status", "plc_last_schedule", "plc_kernel_ms", "plc_pages_workspace", "plc_pages_fork",
+           "plc_decode_rotq", "plc_poll_status", "plc_last_schedule", "plc_kernel_ms", "plc_take_status", "plc_pages_workspace", "plc_pages_fork",
            "plc_pages_keep", "plc_pages_compact", "plc_tree_attention", "plc_tree_attention_workspace", "plc_beam_workspace",
            "plc_beam_select", "plc_beam_reorder"]
 

@@ -428,6 +428,9 @@ compact_few_kernel(PoolDev p, Mover m, BookDev in, BookDev out, int32_t* moved, 
     compact_move<kFewThreads>(p, m, in, out, moved, w, status);
 }
 
+// One step, so that no bit that a call on another stream sets meanwhile is lost.
+__global__ void take_status_kernel(uint32_t* status, uint32_t* bits) { *bits = atomicExch(status, 0u); }
+
 Mover mover_of(const PoolDev& p) {
     Mover m;
     const int pieces = p.d * p.esz / 16;
@@ -478,6 +481,14 @@ plc_status check_workspace(const PoolDev& p, int rows_in, int rows_out, void* ws
 using namespace plc;
 
 extern "C" {
+
+plc_status plc_take_status(uint32_t* status_dev, uint32_t* bits_dev, void* stream) {
+    if (!status_dev || !bits_dev || status_dev == bits_dev) return PLC_E_INVALID;
+    if ((reinterpret_cast<uintptr_t>(status_dev) | reinterpret_cast<uintptr_t>(bits_dev)) & 3) return PLC_E_ALIGN;
+    if (launch_kernel(take_status_kernel, 1, 1, 0, static_cast<cudaStream_t>(stream), false, 1, status_dev, bits_dev) != cudaSuccess) return PLC_E_CUDA;
+    count_launch(1);
+    return PLC_OK;
+}
 
 plc_status plc_pages_workspace(int32_t n_pages, int32_t rows_in, int32_t rows_out, uint64_t* bytes) {
     if (n_pages < 1 || rows_in < 1 || rows_out < 1 || !bytes) return PLC_E_INVALID;

@@ -44,7 +44,7 @@ def _lib():
         api, P, I, L, F = lib(), C.c_void_p, C.c_int32, C.c_int64, C.c_float
         U = C.c_uint64
         for name, types in (("plc_pages_fork", [P, P, P, P, P, P, U, P, P]), ("plc_pages_keep", [P, P, P, P, I, P, P, P]),
-                            ("plc_pages_compact", [P, P, P, P, P, U, P, P]), ("plc_pages_workspace", [I, I, I, P]),
+                            ("plc_pages_compact", [P, P, P, P, P, U, P, P]), ("plc_pages_workspace", [I, I, I, P]), ("plc_take_status", [P, P, P]),
                             ("plc_tree_attention", [P, I, P, P, F, P, U, P, P]), ("plc_tree_attention_workspace", [P, I, I, I, P]),
                             ("plc_beam_select", [P, I, L, I, I, I, P, P, I, I, P, P, P, P, U, P]), ("plc_beam_workspace", [I, I, I, I, P]),
                             ("plc_beam_reorder", [P, I, P, I, I, P, P])):
@@ -274,9 +274,12 @@ class PagePool:
         return out, lse
 
     def check(self):
-        """Waits for the work and raises where a call has found something wrong on the device; clears the word."""
-        bits = int(self.status.item())
-        self.status.zero_()
+        """Waits for the current stream's work and raises where a call has found something wrong on the device; clears the word.
+        What a call that still runs on another stream finds stays there for the next check."""
+        import torch
+        taken = torch.empty(1, dtype=torch.int32, device=self.device)
+        _check(_run(self.device, _lib().plc_take_status, self._word, taken.data_ptr()), "plc_take_status")
+        bits = int(taken.item())
         for bit, code in ((8, E_CUDA), (1, E_CAPACITY), (32, E_INVALID)):
             _need(not bits & bit, code, f"status word {bits}")
 

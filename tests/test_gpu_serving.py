@@ -964,3 +964,34 @@ def test_beam_selection_at_the_lowest_values(dev, dtype, V):
     assert torch.equal(p.long(), torch.where(none, -1, at // V + 4 * torch.arange(4, device=dev)[:, None])) and torch.equal(t.long(), torch.where(none, -1, at % V))
     assert bool((s[none] == -math.inf).all()) and bool(((s.double() - best).abs() <= 2.0 ** -20 + 2.0 ** -23 * best.abs())[~none].all())
     assert p[1, 0] == 7 and abs(float(s[1, 0]) - (-19.51 - math.log(V))) < 1e-4
+
+
+def test_no_status_is_lost_while_it_is_read(dev, monkeypatch):
+    """A call that finds something wrong between the reading of the word and the end of check() is told of by the next check()."""
+    pool = plc.PagePool(torch.zeros(1, 2, 8, 1, 4, 32, dtype=torch.float16, device=dev))
+    book, side, real, late = pool.new_book(2, 3), torch.cuda.Stream(dev), torch.Tensor.item, [True]
+    torch.cuda.synchronize()
+
+    def wrong():                                           # a parent that there is not
+        with torch.cuda.stream(side):
+            pool.fork(book, i32([5, 0], dev))
+        side.synchronize()
+
+    def item(self):
+        value = real(self)
+        if late:
+            late.clear()
+            wrong()
+        return value
+
+    with monkeypatch.context() as m:
+        m.setattr(torch.Tensor, "item", item)
+        pool.check()                                       # nothing was wrong when the word was read
+    for _ in range(2):
+        with pytest.raises(plc.PlcError) as e:
+            pool.check()
+        assert e.value.code == plc.E_INVALID
+        pool.check()
+        wrong()
+    with pytest.raises(plc.PlcError):
+        pool.check()

@@ -232,3 +232,9 @@ def test_pages_of_another_shape_are_not_coded(monkeypatch, change):
         with pytest.raises(plc.PlcError) as e:
             call(view, 2, 20)
         assert e.value.code == plc.E_SHAPE and lib.calls == [], name
+
+
+def test_status_words_that_are_refused(lib):
+    take = lambda a, b: lib.plc_take_status(C.c_void_p(a), C.c_void_p(b), None)  # noqa: E731
+    assert take(0, B) == plc.E_INVALID and take(A, 0) == plc.E_INVALID and take(A, A) == plc.E_INVALID
+    assert take(A + 2, B) == plc.E_ALIGN and take(A, B + 1) == plc.E_ALIGN
