@@ -445,7 +445,8 @@ plc_status plc_tree_attention_workspace(const plc_page_pool* pool, int32_t sessi
  * bytes or NULL: a beam that is done has one continuation, the token `eos`, at its own score.  A score that is not
  * finite (a dead beam's -inf, a row with NaN or +inf) is none.  Outputs [sessions][n_out]: the score (binary32), the parent
  * as a row b*beams + w (for plc_pages_fork and plc_beam_reorder) and the token; places without a continuation get
- * -inf, -1, -1.  beams, n_out <= 128, beams*vocab < 2^32.  workspace: plc_beam_workspace bytes. */
+ * -inf, -1, -1.  beams, n_out <= 128, vocab <= 2^31 - 2^16, beams*vocab < 2^32, sessions <= 2^20,
+ * sessions*beams <= 2^24.  workspace: plc_beam_workspace bytes. */
 plc_status plc_beam_select(const void* logits_dev, int32_t dtype, int64_t row_stride, int32_t sessions, int32_t beams, int32_t vocab,
                            const float* score_dev, const uint8_t* done_dev, int32_t eos, int32_t n_out, float* out_score_dev,
                            int32_t* out_parent_dev, int32_t* out_token_dev, void* workspace_dev, uint64_t workspace_bytes, void* stream);

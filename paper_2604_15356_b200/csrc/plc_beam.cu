@@ -25,6 +25,7 @@ constexpr int kMostOut = 128;                     // n_out, beams
 constexpr int kChunks = 32;                       // pieces of a lane's logits whose maxima are kept
 constexpr int kRoom = 1024;                       // candidates of a part that are ranked as they are
 constexpr int kBuffer = 512;                      // and, where there are more (equal logits), at a time
+constexpr int kMostVocab = 0x7fff0000;             // a column is an int, with up to 5000 more where a block's last step begins
 constexpr int kMostListed = 16384;                // entries of a session's lists (the merge holds them in shared memory)
 
 struct SelectArgs {
@@ -533,7 +534,7 @@ uint64_t beam_bytes(long long rows, int beams, int V, int n_out, int* parts, int
 }
 plc_status check_beams(int32_t sessions, int32_t beams, int32_t vocab, int32_t n_out) {
     if (sessions < 1 || beams < 1 || vocab < 1 || n_out < 1) return PLC_E_INVALID;
-    if (beams > kMostOut || n_out > kMostOut || sessions > (1 << 20) || (long long)sessions * beams > (1 << 24) || (long long)beams * vocab >= (1ll << 32))
+    if (beams > kMostOut || n_out > kMostOut || vocab > kMostVocab || sessions > (1 << 20) || (long long)sessions * beams > (1 << 24) || (long long)beams * vocab >= (1ll << 32))
         return PLC_E_SHAPE;
     return PLC_OK;
 }

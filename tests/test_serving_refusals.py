@@ -238,3 +238,13 @@ def test_status_words_that_are_refused(lib):
     take = lambda a, b: lib.plc_take_status(C.c_void_p(a), C.c_void_p(b), None)  # noqa: E731
     assert take(0, B) == plc.E_INVALID and take(A, 0) == plc.E_INVALID and take(A, A) == plc.E_INVALID
     assert take(A + 2, B) == plc.E_ALIGN and take(A, B + 1) == plc.E_ALIGN
+
+
+@pytest.mark.parametrize("V", [2 ** 31 - 1, 2 ** 31 - 64, 2 ** 31 - 4096, 2 ** 31 - 2 ** 16 + 1])
+def test_vocabularies_near_two_to_the_31_are_refused(lib, V):
+    """A column with a block's logits added has to be an int."""
+    b = C.c_uint64()
+    assert lib.plc_beam_workspace(1, 1, V, 4, C.byref(b)) == plc.E_SHAPE
+    assert lib.plc_beam_select(C.c_void_p(A), plc.OUT_F16, C.c_int64(V), 1, 1, V, C.c_void_p(A), None, -1, 4, C.c_void_p(A), C.c_void_p(A), C.c_void_p(A),
+                               C.c_void_p(WS), C.c_uint64(1 << 20), None) == plc.E_SHAPE
+    assert lib.plc_beam_workspace(1, 1, 2 ** 31 - 2 ** 16, 4, C.byref(b)) == plc.OK and 0 < b.value <= 64 * (8 * 4 + 12)
