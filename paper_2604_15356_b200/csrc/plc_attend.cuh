@@ -364,6 +364,7 @@ __device__ __forceinline__ void copy_boxes(const PoolDev& p, const BookDev& b, c
             const int valid = boxes >> (my_box & 31) & 1u && 4 * lane < a.tile_pos ? min(max(x.w.x.kv - t, 0), 4) : 0;
             const uint32_t word = __reduce_or_sync(0xffu << (lane & 24), ((1u << valid) - 1u) << (4 * (lane & 7)));
             if ((lane & 7) == 0) words[n % word_ring * 4 + (lane >> 3)] = word;
+            __syncwarp();                                // four lanes' words, which lane 0's arrival tells of
         }
         x.next(p, b, a);
         if (x.more()) look_up();
