@@ -34,6 +34,13 @@ def _need(ok, code, where):
         raise PlcError(code, where)
 
 
+def _int32(code, where, *values):
+    """What the library takes as int32: ctypes would cut larger numbers to their low bits."""
+    for v in values:
+        if not -0x80000000 <= v <= 0x7fffffff:
+            raise PlcError(code, where)
+
+
 _api = None
 
 
@@ -110,6 +117,7 @@ class PageBook:
             _i32(t, dev, "PageBook." + n)
             _need(t.dim() == dim, E_SHAPE, "PageBook." + n)
         _need(len.shape[0] == table.shape[0], E_SHAPE, "PageBook.len")
+        _int32(E_SHAPE, "PageBook", *table.shape, *ref.shape)
         self._parts = (table, len, ref)
         self.rows, self.max_pages = table.shape
         self.n_pages, self.device = ref.shape[0], dev
@@ -162,6 +170,7 @@ class PagePool:
         self.kv, self.device, self.n_pages = kv, kv.device, kv.shape[2]
         s = kv.stride()
         L, _, P, H, page, d = kv.shape
+        _int32(E_SHAPE, "PagePool", L, P, H, page, d)
         self._c = PagePoolC(KVView(kv.data_ptr(), s[0], s[1], s[2], s[3], s[4]), L, H, d, P, page, _kind(kv.dtype, "PagePool"))
         self._by = C.byref(self._c)
         self.status = torch.zeros(1, dtype=torch.int32, device=kv.device)
@@ -201,6 +210,7 @@ class PagePool:
         a = self._book(book, where)
         rows = _i32(parent, dev, where).numel()
         _need(rows >= 1, E_INVALID, where)
+        _int32(E_SHAPE, where, rows)
         if room is not None:
             _need(_i32(room, dev, where).numel() == rows, E_SHAPE, where)
         need = _bytes(dev, api.plc_pages_workspace, self.n_pages, book.rows, rows)
@@ -215,6 +225,7 @@ class PagePool:
         _i32(path, dev, where)
         _i32(n_path, dev, where)
         _need(path.dim() == 2 and path.shape[0] == book.rows == n_path.numel(), E_SHAPE, where)
+        _int32(E_SHAPE, where, path.shape[1])
         new, _ = PageBook._new(book.rows, book.max_pages, self.n_pages, dev)
         _check(_run(dev, api.plc_pages_keep, self._by, a, path.data_ptr(), n_path.data_ptr(), path.shape[1], new._by, self._word), where)
         return new
@@ -240,6 +251,8 @@ class PagePool:
         _need(q.dim() == 3, E_SHAPE, where)
         (N, heads, d), (row, head, one) = q.shape, q.stride()
         _need(d == self._c.head_dim, E_SHAPE, where)
+        _int32(E_INVALID, where, layer)
+        _int32(E_SHAPE, where, N, heads)
         _need(q.device == dev and q.dtype == self.kv.dtype and one == 1, E_INVALID, where)
         _kind(q.dtype, where, wide=False)
         _need(_i32(begin, dev, where).numel() == book.rows + 1, E_SHAPE, where)
@@ -248,6 +261,7 @@ class PagePool:
             _i32(mask, dev, where)
             _need(mask.dim() == 2 and mask.shape[0] == N, E_SHAPE, where)
             words, bits = mask.shape[1], mask.data_ptr()
+            _int32(E_SHAPE, where, words)
         if out is None:
             out = torch.empty((N, heads, d), dtype=q.dtype, device=dev)
             out_row, out_head = heads * d, d
@@ -293,6 +307,8 @@ def beam_select(logits, score, n_out, done=None, eos=-1):
     _need(logits.is_cuda and logits.dim() == 3, E_INVALID, where)
     (S, W, V), (session, row, one) = logits.shape, logits.stride()
     _need(one == 1, E_INVALID, where)
+    _int32(E_SHAPE, where, S, W, V, n_out)
+    _int32(E_INVALID, where, eos)
     _need(S < 2 or W < 2 or session == W * row, E_SHAPE, where)
     if W < 2:
         row = session
@@ -319,6 +335,7 @@ def beam_reorder(parent, states, status=None):
     _need(parent.is_cuda and len(states) > 0, E_INVALID, where)
     rows, rows_in = _i32(parent, dev, where).numel(), states[0].shape[0] if states[0].dim() else 0
     _need(rows > 0 and rows_in > 0, E_INVALID, where)
+    _int32(E_SHAPE, where, rows, rows_in)
     word = None if status is None else _i32(status, dev, where).data_ptr()
     out, sets = [], []
     for t in states:

@@ -995,3 +995,18 @@ def test_no_status_is_lost_while_it_is_read(dev, monkeypatch):
         wrong()
     with pytest.raises(plc.PlcError):
         pool.check()
+
+
+def test_numbers_that_are_no_int32_are_refused(dev):
+    """Layers, end tokens and counts that hold the number of a valid one in their low 32 bits."""
+    kv = torch.zeros(2, 2, 4, 1, 16, 64, dtype=torch.float16, device=dev)
+    pool, q, begin = plc.PagePool(kv), torch.zeros(1, 1, 64, dtype=torch.float16, device=dev), i32([0, 1], dev)
+    book = pool.fork(pool.new_book(1, 2), i32([0], dev), i32([4], dev))
+    x, score, done = torch.zeros(1, 2, 8, device=dev), torch.zeros(1, 2, device=dev), torch.tensor([[True, False]], device=dev)
+    for wide in (1 << 32, -(1 << 32), 1 << 63):
+        for code, call in ((plc.E_INVALID, lambda: pool.tree_attention(wide + 1, book, q, begin)), (plc.E_INVALID, lambda: plc.beam_select(x, score, 2, done=done, eos=wide + 3)),
+                           (plc.E_SHAPE, lambda: plc.beam_select(x, score, wide + 2))):
+            with pytest.raises(plc.PlcError) as e:
+                call()
+            assert e.value.code == code
+    pool.check()
