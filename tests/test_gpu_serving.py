@@ -1010,3 +1010,75 @@ def test_numbers_that_are_no_int32_are_refused(dev):
                 call()
             assert e.value.code == code
     pool.check()
+
+
+@pytest.mark.parametrize("cols", [2, 40])
+@pytest.mark.parametrize("dtype, d, H, G, page", [("f16", 64, 1, 2, 16), ("bf16", 128, 2, 8, 16), ("bf16", 128, 2, 24, 16), ("f16", 128, 1, 40, 16), ("bf16", 256, 1, 16, 16),
+                                                  ("f16", 32, 1, 2, 12), ("bf16", 64, 1, 40, 12)])
+def test_attention_answers_for_what_is_left_of_ranges_and_lengths(dev, dtype, d, H, G, page, cols):
+    """Row ranges, lengths and pages out of range: the rows that are left get the formula's value over the positions that are left (tolerance as above), the
+    others stay as they were, and each call is told of.  Items taken whole and split, few rows and many, boxes and single positions."""
+    rng = np.random.default_rng(d + G + cols)
+    most, P, N = cols * page, 4, 5
+    kv = torch.from_numpy(rng.standard_normal((1, 2, P, H, page, d)).astype(np.float32)).to(TYPES[dtype]).to(dev)
+    q = torch.from_numpy(rng.standard_normal((N, H * G, d)).astype(np.float32)).to(TYPES[dtype]).to(dev)
+    pool, scale = plc.PagePool(kv), 1 / math.sqrt(d)
+    for lens, begin, missing in (([most + 8], [0, 9], ()), ([-3], [0, 2], ()), ([most - 2], [1, 5], ()), ([10], [2, 1], ()), ([10], [-2, 3], ()), ([1 << 30], [0, 4], ()),
+                                 ([3, most], [0, 3, 2], ()), ([most - 1, 7], [1, 3, 77], ()), ([page + 3], [0, 2], ((0, 1),)), ([-7, -7], [-5, -4, 2], ())):
+        S = len(lens)
+        table = rng.integers(0, P, (S, cols)).astype(np.int32)
+        for s, c in missing:
+            table[s, c] = P + 3
+        out, lse = torch.full((N, H * G, d), 5.0, dtype=TYPES[dtype], device=dev), torch.full((N, H * G), 7.0, device=dev)
+        pool.tree_attention(0, book_of(table, lens, np.ones(P), dev), q, i32(begin, dev), out=out, lse=lse)
+        with pytest.raises(plc.PlcError) as e:
+            pool.check()
+        assert e.value.code == plc.E_INVALID
+        rest = torch.ones(N, dtype=torch.bool, device=dev)
+        for s in range(S):
+            lo = min(max(begin[s], 0), N)
+            hi = min(max(begin[s + 1], lo), N)
+            at = min(max(lens[s], 0), most)
+            t = np.arange(min(at + hi - lo, most))
+            t = t[table[s, t // page] < P]
+            pages, slots = torch.as_tensor(table[s, t // page].astype(np.int64), device=dev), torch.as_tensor(t % page, device=dev)
+            k, v = (kv[0, j, pages, :, slots].double().transpose(0, 1) for j in range(2))       # [H][positions][d]
+            for row in range(lo, hi):
+                rest[row] = False
+                sees = torch.as_tensor(t <= at + row - lo, device=dev)
+                x = q[row].double().view(H, G, d)
+                z = (torch.einsum("hgd,htd->hgt", x, k) * scale).masked_fill(~sees, -math.inf)
+                big = (torch.einsum("hgd,htd->hgt", x.abs(), k.abs()) * scale).amax(-1).flatten()
+                want, mag = (torch.einsum("hgt,htd->hgd", z.softmax(-1), y).reshape(H * G, d) for y in (v, v.abs()))
+                u, err = torch.finfo(TYPES[dtype]).eps / 2, 2 * (d * 2.0 ** -23 * big + 2.0 ** -22 + 2.0 ** -23 * 2 * big) + len(t) * 2.0 ** -23
+                tol = (u + err[:, None]) * mag + u * want.abs() + torch.finfo(TYPES[dtype]).smallest_normal * u
+                assert bool(((out[row].double() - want).abs() <= tol).all()), (lens, begin, row)
+                exl = z.logsumexp(-1).flatten()
+                assert bool(((lse[row].double() - exl).abs() <= err + 2.0 ** -22 * exl.abs()).all()), (lens, begin, row)
+        assert bool((out[rest] == 5).all()) and bool((lse[rest] == 7).all()), (lens, begin)
+
+
+def test_attention_over_two_to_the_31_positions(dev):
+    """The longest row that is taken, its entries naming four pages over and over: the softmax over the four, each as often as it stands there.  The
+    sums: a CTA (148 or more) has at most 2^24 / 148 tiles, whose sums a thread adds in binary32 and whose eight products each are added to the
+    result at a step of 2^-23 at most."""
+    page, d, cols = 1 << 14, 64, 131068                    # 131068 * 2^14 = 2^31 - 2^16
+    gen = torch.Generator(device=dev).manual_seed(8)
+    kv = torch.randn(1, 2, 4, 1, page, d, device=dev, generator=gen).half()
+    kv[0, 1] += torch.arange(4, device=dev)[:, None, None, None]
+    table = torch.randint(0, 4, (1, cols), dtype=torch.int32, device=dev, generator=gen)
+    q = torch.randn(1, 2, d, device=dev, generator=gen).half()
+    pool = plc.PagePool(kv)
+    times = torch.bincount(table[0], minlength=4)
+    out, lse = pool.tree_attention(0, plc.PageBook(table, i32([cols * page - 1], dev), times.int()), q, i32([0, 1], dev))
+    pool.check()
+    k, v = (kv[0, j, :, 0].double() for j in range(2))
+    z = torch.einsum("hd,ptd->hpt", q[0].double(), k) / 8
+    big = (torch.einsum("hd,ptd->hpt", q[0].double().abs(), k.abs()) / 8).amax((1, 2))
+    z = (z + times.double().log()[:, None]).flatten(1)
+    p, tiles = z.softmax(-1), -(-(1 << 24) // 148)
+    want, mag = p @ v.reshape(-1, d), p @ v.reshape(-1, d).abs()
+    e = 2 * (d * 2.0 ** -23 * big + 2.0 ** -22 + 2.0 ** -23 * 2 * big)
+    assert bool(((lse[0].double() - z.logsumexp(-1)).abs() <= e + tiles * 2.0 ** -24 + 2.0 ** -22 * 32).all())
+    tol = (2.0 ** -11 + e[:, None] + tiles * 2.0 ** -24 + 8 * tiles * 2.0 ** -23) * mag + 2.0 ** -11 * want.abs()
+    assert bool(((out[0].double() - want).abs() <= tol).all())
