@@ -28,7 +28,9 @@ AttendPlan plan_of(int row_tile, int per_sm, long long rows, int d) {
     return x;
 }
 // Up to kFewRows rows a session and KV head (32 of 256 components) take the layout for few rows; beyond, two row tiles share K and V where a
-// session has more rows than one holds.
+// session has more rows than one holds.  By the mean, since a session's rows are known on the device only; where sessions are alike or have about the
+// mean that is right, where they are not it costs: a chunk of 2048 among 255 single tokens (8 x 4 heads of 128, 512 positions) 626 us, in calls
+// of their own 198 + 120; four trees of 26 rows among 60 sessions without any 91 us, by themselves 75.
 constexpr int kFewRows = 64;
 AttendPlan plan(const PoolDev& p, int heads, int sessions, int n_rows) {
     const long long rows = (long long)n_rows * (heads / p.H);
@@ -42,8 +44,13 @@ AttendPlan plan(const PoolDev& p, int heads, int sessions, int n_rows) {
 }
 
 // How many items a call has at most, if they are no more than SMs and short: then a CTA takes one whole, and there is no second launch to join them.  A tile
-// after the other costs 1.6 us each, the second launch 2.4 us on the device and 2 us of the caller's time: one token of 32 heads of 128, a call by
-// itself 18.1 -> 16.0 us at 512 positions; replayed in a graph 10.8 -> 9.4 us at 128 positions, 12.7 -> 12.0 at 256, 12.6 -> 14.2 at 512.
+// after the other costs 1.6 us each, the second launch 2.4 us on the device and 2 us of the caller's time.  One token of 32 heads of 128, split and whole:
+//   positions   calls in a row (the caller's time)   each waited for   in a graph
+//      128            18.9   16.7                     32.3   31.0      10.8    9.5
+//      256            19.0   16.7                     34.9   33.5      12.8   12.1
+//      384            18.9   16.7                     34.7   36.1      12.8   14.4
+// Beyond 256 the call costs its caller less and the device more; the border stands where a fourth tile begins.  It goes by what a row of the book can hold, which
+// is what the host knows.
 constexpr int kWholePositions = 384;
 int whole_items(const PoolDev& p, const BookDev& b, long long rows, int n_rows, int row_tile) {
     const long long items = p.H * (rows / row_tile + (n_rows < b.rows ? n_rows : b.rows));

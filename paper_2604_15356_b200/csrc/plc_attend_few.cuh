@@ -11,8 +11,10 @@
 // A row's maximum is common to the CTA and raised only where some score passes it by 2^3 (a vote of the four warps a tile); each thread sums the
 // weights of its positions, and the sums are joined at the end of an item.
 //
-// Measured, components in 16 bits: one token of 4 heads a KV head, 37 sessions x 8192 positions x 8 KV heads x 128 components 182 us (6.8 TB/s; d = 64
-// 6.0, d = 256 6.4 TB/s; position by position, at d = 32, 1.7); 256 sessions of up to 512 positions 74 us (353 MB, 4.8 TB/s): items end inside
+// Measured, components in 16 bits: one token of 4 heads a KV head, 37 sessions x 8192 positions x 8 KV heads x 128 components 182 us (6.8 TB/s at 1965 MHz; as
+// many bytes at d = 64 6.7, d = 256 6.8 TB/s; caches flushed before each call 6.2).  Position by position, caches flushed: pages of 100 positions 6.1 TB/s, of 20 5.8, of one 5.0; of 100 at
+// d = 64 4.4, d = 32 2.4: copies of 16 bytes each, and a vector has few of them.  Boxes that do not fill a tile: pages of 24 (120 of 128 positions) 5.3, of 72
+// (72) 5.0, since every tile then has positions to hide.  256 sessions of up to 512 positions 74 us (353 MB, 4.8 TB/s): items end inside
 // tiles there and each has a maximum, sums and results of its own, chains of votes that the copies wait for.  Code that is run once an item is
 // fetched anew by then, so it is kept short: with its loops unrolled that call took 107 us, 0.34 of the warps' time without an instruction.
 // Slower or the same: two slots of K or of V an SM's CTA in place of the second Q (74 -> 75 and 77 us), more CTAs than fit at once (7 to 40 %).

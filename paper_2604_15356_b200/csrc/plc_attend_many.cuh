@@ -6,10 +6,14 @@
 //   O = O + P V      [128 rows x d]       tcgen05.mma, P from tensor memory, V as it lies in the page (d contiguous)
 //
 // NT = 1: 128 rows, two CTAs an SM.  NT = 2: two row tiles that share each K and V tile, one CTA an SM: while the weights of one tile are
-// formed, the products of the other run.  Masks are written into S first, so that the loops over the scores have none: a masked tile is rare.
+// formed, the products of the other run.  Masks are written into S first, so that the loops over the scores have none: a masked tile is rare where boxes
+// fill a tile (pages that divide it); elsewhere every tile is one.
 //
-// Measured, bf16, 8 KV heads of 128 components: 131072 positions, 512 rows a KV head 310 us (885 TFLOP/s; 0.53 of the measured rate of a product by
-// itself), 37 sessions x 8192 x 256 rows 350 us, x 128 rows 222 us (5.6 TB/s); 8 sessions x 8192 x 256 rows of 256 components 215 us.
+// Measured, bf16, 8 KV heads of 128 components.  131072 positions, 512 rows a KV head: the kernel by itself 310 us (885 TFLOP/s, 0.53 of the measured rate of a
+// product by itself), call after call 341 to 351 us (under the power cap, 1650 MHz), each waited for 348 (1717 MHz), caches flushed between
+// them 323 to 336 (1750 MHz).  37 sessions x 8192 x 256 rows 331 us at first, 397 call after call (1600 MHz); x 128 rows 234 and 250; 8 sessions x 8192 x 256 rows of 256
+// components 221 and 234.  Without a mask every row tile goes through all of its session's positions: a chunk of 2048 behind nothing 179 us, behind 8192 positions
+// 433.  Pages whose boxes do not fill a tile, 37 x 8192 x 256 rows: of 24 positions 478 us, of 72 761; position by position, of 100, 452.
 // With NT = 2 a pair of tiles takes 4400 clocks, of which the tensor pipe is busy for 2050 and the exponentials' unit for 2050: a row tile's
 // weights (2200 clocks in the softmax's four warps) and its products (1050) follow each other, with four signals between them, and tensor memory
 // has no room for a second S beside two O.  What did not help: S in halves of 64 positions, each with its own turn (products of 64 and 128 columns in turn run at a third of

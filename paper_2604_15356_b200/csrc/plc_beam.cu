@@ -5,7 +5,9 @@
 // the n_out largest logits; a second, small launch joins the parts: the row's log-sum-exp, and a merge of the
 // sorted lists by score.  HBM bound: each logit is read once.
 // Measured: 512 rows of 128256 logits in bf16, 8 beams a session and 8 of their continuations: rows 38 us (131 MB, 3.4 TB/s; the exponentials' unit 0.49 busy,
-// 21 warps an SM), merge 8 us, the states' rows 10 us; 49 us together.  With a list a warp that every logit was held against: 229 us.
+// 21 warps an SM), merge 8 us, the states' rows 10 us; 49 us together.  With a list a warp that every logit was held against: 229 us.  Where fewer lanes than
+// n_out hold a logit above the lowest of the row (ten tokens of 128256 that are not masked) the bound is that lowest one, all logits reach it, and one warp looks
+// through them: 865 us instead of 48.
 //
 // Exactness: continuations of different rows are compared by (x - maximum) + (score - log sum) in binary64, the maximum taken off first: at the
 // type's lowest values (a row that is masked with them as a whole) nothing else would be left of the sum.  Exponentials are binary32 (x - maximum

@@ -451,7 +451,8 @@ unsigned move_blocks(const PoolDev& p, long long moves, long long words) {
 
 // Whether one cluster does a call, by the bytes that it may move at most and the words that it goes through.  A launch less saves the caller 1.7 us (fork of
 // four beams, 16 KB: 15.3 -> 13.6 us a call; a path of 13 positions, 400 KB: 15.4 -> 13.7 us); eight SMs move whole pages slowly (compaction
-// of 400 KB: 7.1 -> 14.8 us), paths, whose loads are all in flight at once, as fast as more.
+// of 400 KB: 7.1 -> 14.8 us), paths, whose loads are all in flight at once, as fast as more.  Paths in this form are of one row: its blocks share a path's
+// planes, and one of them writes the row's book.
 constexpr long long kFewPageBytes = 1 << 17, kFewPathBytes = 1 << 20, kFewWords = 1 << 14;
 long long plane_bytes(const PoolDev& p, long long positions) { return positions * p.H * p.d * p.esz * 2 * p.L; }
 

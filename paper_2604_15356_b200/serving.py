@@ -109,7 +109,8 @@ def _bytes(device, call, *args):
 
 class PageBook:
     """Who holds which page: table [rows][max_pages], len [rows], ref [pages] (int32 on the device).  Calls return new
-    books; an old one stays valid until a page that only it names is taken by a later call."""
+    books; an old one stays valid until a page that only it names is taken by a later call.  A book that a call has made is
+    one allocation, with that call's workspace (about 16 bytes a page) behind it for as long as the book lives."""
 
     def __init__(self, table, len, ref):
         dev = table.device
@@ -219,7 +220,7 @@ class PagePool:
         return new
 
     def keep(self, book, path, n_path):
-        """New book after the drafted positions path[s][:n_path[s]] of every row have been accepted."""
+        """New book after the drafted positions path[s][:n_path[s]] of every row have been accepted (path: one column or more)."""
         where, dev, api = "plc_pages_keep", self.device, _lib()
         a = self._book(book, where)
         _i32(path, dev, where)
@@ -244,7 +245,8 @@ class PagePool:
     def tree_attention(self, layer, book, q, begin, mask=None, scale=None, out=None, lse=None):
         """(out, lse) of the query rows q [N][heads][d]; session s has the rows begin[s] .. begin[s+1]-1, whose keys and
         values stand behind its length.  mask [N][words] int32: bit j of row i = drafted position j is seen (None: j <= i).
-        scale: 1 / sqrt(d) if not given.  out, lse: written where given."""
+        scale: positive, 1 / sqrt(d) if not given.  out, lse: written where given.  Chunks of prompts go into a call of
+        their own: one call's work is cut by the mean number of rows."""
         import torch
         where, dev, api = "plc_tree_attention", self.device, _lib()
         a = self._book(book, where)
