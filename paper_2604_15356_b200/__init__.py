@@ -264,9 +264,11 @@ class Context:
         return b.value
 
     def _view(self, kv, S, n, dtype, where):
-        """kv as a KVView.  One that knows its type and extents has to be of the type that the call reads or writes, and to hold what it
-        reads or writes."""
+        """kv as a KVView.  A tensor has to have elements of the size that the call reads or writes; a view that knows its type and
+        extents has to be of that type and to hold what the call reads or writes."""
         if not isinstance(kv, KVView):
+            if kv.element_size() != (4 if dtype == OUT_F32 else 2):
+                raise PlcError(E_INVALID, where)
             return kv_view(kv)
         if isinstance(kv, PoolView):
             L, H, d, sessions, positions = kv.extents

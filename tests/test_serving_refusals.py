@@ -248,3 +248,21 @@ def test_vocabularies_near_two_to_the_31_are_refused(lib, V):
     assert lib.plc_beam_select(C.c_void_p(A), plc.OUT_F16, C.c_int64(V), 1, 1, V, C.c_void_p(A), None, -1, 4, C.c_void_p(A), C.c_void_p(A), C.c_void_p(A),
                                C.c_void_p(WS), C.c_uint64(1 << 20), None) == plc.E_SHAPE
     assert lib.plc_beam_workspace(1, 1, 2 ** 31 - 2 ** 16, 4, C.byref(b)) == plc.OK and 0 < b.value <= 64 * (8 * 4 + 12)
+
+
+@pytest.mark.parametrize("out_dtype", [plc.OUT_F16, plc.OUT_F32])
+def test_tensors_of_another_width_are_not_coded(monkeypatch, out_dtype):
+    """Elements of half the size would be written past the tensor's end."""
+    import torch
+    lib, calls = _codec_calls(monkeypatch, out_dtype)
+    for name, (needs, call) in calls.items():
+        for dtype in (torch.float16, torch.bfloat16, torch.float32, torch.uint8):
+            kv = torch.zeros(2, 2, 3, 4, 40, 64, dtype=dtype)
+            del lib.calls[:]
+            if dtype.itemsize == (4 if needs == plc.OUT_F32 else 2):
+                call(kv, 3, 40)
+                assert lib.calls == [name]
+                continue
+            with pytest.raises(plc.PlcError) as e:
+                call(kv, 3, 40)
+            assert e.value.code == plc.E_INVALID and lib.calls == [], (name, dtype)
