@@ -468,6 +468,115 @@ typedef struct {
 plc_status plc_beam_reorder(const plc_row_set* sets, int32_t n_sets, const int32_t* parent_dev, int32_t rows_in, int32_t rows_out,
                             uint32_t* status_dev, void* stream);
 
+/* ---- The decoding loop around the paged cache: rotary positions, new tokens into the pages, eviction, log probabilities. ---- */
+
+/* Rotary positions.  dim (even, at most head_dim) components of a head turn, the rest stay; pair i is (i, i + dim/2), or (2i, 2i + 1)
+ * where interleaved is set.  turns_dev [dim/2] (8-byte aligned): turns a position in units of 2^-64 (plc_rotary_turns).  At position pos
+ *     y_a = scale (x_a cos t - x_b sin t),  y_b = scale (x_b cos t + x_a sin t),  t = 2 pi pos turns_i 2^-64,
+ * any int32 position, the negative ones turning back. */
+typedef struct {
+    const uint64_t* turns_dev;
+    int32_t dim, interleaved;
+    float scale;
+} plc_rotary;
+
+/* turns[i] = radians[i] / (2 pi) 2^64 modulo 2^64, rounded to nearest (exact arithmetic; host side, no GPU work); 0 <= radians <= 65536. */
+plc_status plc_rotary_turns(const double* radians, int32_t n, uint64_t* turns);
+
+/* x, out [n_rows][heads][head_dim], strides in elements; out is x itself with x's strides, or does not overlap it. */
+typedef struct {
+    const void* x_dev;
+    void* out_dev;
+    int64_t x_stride_row, x_stride_head, out_stride_row, out_stride_head;
+    int32_t heads;
+} plc_rotary_set;
+
+/* Turns the rows of up to four sets (queries and keys, say) at positions pos_dev [n_rows]; back: by the opposite angles, which is the gradient
+ * of the turn.  dtype as plc_page_pool; head_dim <= 1024, all sets together at most 4096 heads.  Arithmetic is binary32, the angle is exact to
+ * 2^-33 turns and its sine and cosine are binary32, the result is rounded once.  16 bytes at a time where strides, addresses and dim allow
+ * it, else component by component. */
+plc_status plc_rotary_apply(const plc_rotary* rotary, const plc_rotary_set* sets, int32_t n_sets, const int32_t* pos_dev, int32_t n_rows,
+                            int32_t head_dim, int32_t dtype, int32_t back, void* stream);
+
+/* New tokens: session s (a row of the book) has the rows begin_dev[s] .. begin_dev[s+1]-1, as in plc_tree_queries.  q_dev, out_dev
+ * [n_rows][n_heads][head_dim] (n_heads 0: no queries; out may be q itself), k_dev, v_dev [n_rows][n_kv_heads][head_dim], all of the pool's type, strides in
+ * elements.  pos_dev [n_rows]: the positions that they turn by, or NULL: where they stand, len + i. */
+typedef struct {
+    const void* q_dev;
+    int64_t q_stride_row, q_stride_head;
+    void* out_dev;
+    int64_t out_stride_row, out_stride_head;
+    const void* k_dev;
+    int64_t k_stride_row, k_stride_head;
+    const void* v_dev;
+    int64_t v_stride_row, v_stride_head;
+    const int32_t* begin_dev;
+    const int32_t* pos_dev;
+    int32_t n_rows, n_heads;
+} plc_new_tokens;
+
+/* Writes the keys (turned; rotary NULL: as they are) and values of session s's i-th new token at position len + i of its pages, and the turned
+ * queries to out.  The book stays as it is: the positions count once plc_pages_keep has taken them.  A position behind the row's pages, on a page
+ * that does not exist or that has other holders is not written (bit 32; its queries are turned all the same); rows outside every range are left
+ * out; ranges that do not rise: bit 32, of rows in several ranges some may be left out. */
+plc_status plc_pages_append(const plc_page_pool* pool, int32_t layer, const plc_page_book* book, const plc_rotary* rotary,
+                            const plc_new_tokens* tokens, uint32_t* status_dev, void* stream);
+
+/* Weights by which positions are evicted: element (row of the book, layer, KV head, position < n_pos) stands at
+ * row*stride_row + layer*stride_layer + head*stride_head + position.  They follow beams through plc_beam_reorder. */
+typedef struct {
+    float* base_dev;
+    int64_t stride_row, stride_layer, stride_head;
+    int32_t n_pos;
+} plc_weights;
+
+/* The newest tokens of the sessions, after plc_pages_keep: entry e of the list is row rows_dev[e] of q and lse (rows_dev NULL: row e; -1: no row),
+ * session s has the entries begin_dev[s] .. begin_dev[s+1]-1, and they stand at its last positions, in order.  q_dev [n_rows][n_heads][head_dim] of
+ * the pool's type (f16 or bf16) as the attention had it, 16-byte aligned vectors, lse_dev [n_rows][n_heads] what it left. */
+typedef struct {
+    const void* q_dev;
+    int64_t q_stride_row, q_stride_head;
+    const float* lse_dev;
+    const int32_t* rows_dev;
+    const int32_t* begin_dev;
+    int32_t n_rows, n_list, n_heads;
+} plc_weigh_queries;
+
+/* weights[s][layer][h][t] = decay weights[s][layer][h][t] + sum of exp(scale q.k_t - lse) over the entries of session s that stand at t or behind it and the query
+ * heads of KV head h, for t < len; the positions of the entries themselves begin at 0 instead of their old weight, and so does all where decay is 0 (nothing is
+ * read).  Sessions without entries are left as they are.  Entries whose lse is infinite (they saw nothing) count for nothing.
+ * scale: positive and finite, as for the attention; decay: finite, not negative.  Scores and sums are binary32, sums in an order
+ * that does not change from call to call.  Positions from n_pos on are left out (bit 1).  Ranges, lengths, rows and page numbers out of range, and more entries
+ * than positions (bit 32): ranges and lengths are cut to what there is, a row counts for nothing, positions without a page receive nothing. */
+plc_status plc_pages_weigh(const plc_page_pool* pool, int32_t layer, const plc_page_book* book, const plc_weigh_queries* queries, float scale,
+                           float decay, const plc_weights* weights, uint32_t* status_dev, void* stream);
+
+/* Rows with more than their budget (budget_dev [rows], negative: the row stays; or NULL: `budget` for all) keep that many positions: in every layer and head by
+ * itself the last min(recent, budget) ones, and of the others those with the largest weights, ties to the lower position, NaN last.  What is kept moves together in
+ * order, in the pages and in out_weights_dev [rows][n_layers][n_kv_heads][n_pos] (contiguous; must not overlap weights; 0 from the new length on).
+ * The new length is the budget, pages behind it are released; of the pages that the row still has, those with other holders are replaced by fresh ones, the
+ * lowest-numbered free ones of `in`, in order.  Other rows stay as they are, what they hold behind their length too, and their weights are copied.
+ * Keys that were turned stay turned: later tokens are given their positions by plc_new_tokens.pos_dev, since len + i no longer counts what was evicted.
+ * If the free pages do not suffice, bit 1 is set and out is what in was, weights and pool as before.  A length out of range or above n_pos, and a page number
+ * out of range, leave the row as it is (bit 32).  n_layers*n_kv_heads*rows < 2^30.  workspace: plc_pages_evict_workspace bytes. */
+plc_status plc_pages_evict(const plc_page_pool* pool, const plc_page_book* in, const plc_weights* weights, const int32_t* budget_dev, int32_t budget,
+                           int32_t recent, const plc_page_book* out, float* out_weights_dev, void* workspace_dev, uint64_t workspace_bytes,
+                           uint32_t* status_dev, void* stream);
+plc_status plc_pages_evict_workspace(const plc_page_pool* pool, int32_t rows, int32_t n_pos, uint64_t* bytes);
+
+/* Rows of logits [rows][vocab] (row_stride elements apart, dtype as plc_page_pool), with p the softmax of a row:
+ *   logp_dev [rows][n_tokens] = log p of tokens_dev [rows][n_tokens] (-1: 0; any other token outside [0, vocab): 0, and bit 32 of *status_dev, which may be NULL)
+ *   entropy_dev [rows] (or NULL) = - sum p log p, in nats
+ *   top_logp_dev, top_token_dev [rows][n_top]: the n_top likeliest tokens in falling order, ties to the lower one; those of probability 0 and places
+ *   behind the vocabulary get -inf and -1
+ * A row with NaN, +inf or nothing but -inf has log probabilities (of tokens in range) and entropy NaN, alternatives -inf and -1.
+ * Exponentials are binary32, in groups of 32, the groups' sums binary64.  n_tokens <= 2^20, n_top <= 128, vocab as for plc_beam_select, rows <= 2^24.
+ * workspace: plc_token_logprobs_workspace bytes. */
+plc_status plc_token_logprobs(const void* logits_dev, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab, const int32_t* tokens_dev,
+                              int32_t n_tokens, int32_t n_top, float* logp_dev, float* entropy_dev, float* top_logp_dev, int32_t* top_token_dev,
+                              void* workspace_dev, uint64_t workspace_bytes, uint32_t* status_dev, void* stream);
+plc_status plc_token_logprobs_workspace(int32_t rows, int32_t vocab, int32_t n_top, uint64_t* bytes);
+
 /* Waits for the stream and returns the device status word's most severe code; clears it.
  * PLC_E_ALIGN here means that *total_bytes_dev was not a multiple of 16 when an encoder reserved a
  * chunk's place (the chunk is then not written). */

@@ -181,3 +181,140 @@ def beam_select(logits, score, n_out, done=None, eos=-1):
         for i, (f, w, v) in enumerate(sorted(c)[:n_out]):
             out[s, i], parent[s, i], token[s, i] = -f, s * W + w, v
     return out, parent, token
+
+
+def rotary(x, pos, freq, interleaved=False, scale=1.0, back=False):
+    """x [N][heads][d] with its first 2 len(freq) components turned at pos [N], pair by pair."""
+    y = np.asarray(x, np.float64).copy()
+    n = len(freq)
+    for r in range(y.shape[0]):
+        for i, f in enumerate(freq):
+            t = math.remainder(int(pos[r]) * float(f), 2 * math.pi) * (-1 if back else 1)
+            a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + n)
+            xa, xb = y[r, :, a].copy(), y[r, :, b].copy()
+            y[r, :, a] = scale * (xa * math.cos(t) - xb * math.sin(t))
+            y[r, :, b] = scale * (xb * math.cos(t) + xa * math.sin(t))
+    return y
+
+
+def append_places(table, length, ref, begin, page_pos, n_rows):
+    """-> for every row (page, slot, position it stands at) or None where it is written nowhere, whether it is in a range, status bits."""
+    places, within, bits = [None] * n_rows, [None] * n_rows, 0
+    for s in range(table.shape[0]):
+        for i in range(begin[s], begin[s + 1]):
+            t = int(length[s]) + i - begin[s]
+            within[i] = t
+            j = t // page_pos
+            page = int(table[s, j]) if length[s] >= 0 and j < table.shape[1] else -1
+            if 0 <= page < len(ref) and ref[page] == 1:
+                places[i] = (page, t % page_pos)
+            else:
+                bits |= RANGE
+    return places, within, bits
+
+
+def weigh(q, lse, k_of, length, begin, rows, scale, decay, weight):
+    """weight [S][H][T] after the sessions' newest entries; k_of(s, h, t) -> the key or None.  Also the bound's parts: the sum of the
+    terms, each times how far its exponent's pieces reach."""
+    S, H, T = weight.shape
+    G = q.shape[1] // H
+    out, reach = np.asarray(weight, np.float64).copy(), np.zeros(weight.shape)
+    for s in range(S):
+        entries = range(begin[s], begin[s + 1])
+        if not len(entries):
+            continue
+        start = int(length[s]) - len(entries)
+        for h in range(H):
+            for t in range(min(int(length[s]), T)):
+                total = far = 0.0
+                key = k_of(s, h, t)
+                for j, e in enumerate(entries):
+                    r = e if rows is None else int(rows[e])
+                    if not 0 <= r < q.shape[0] or t > start + j or key is None:
+                        continue
+                    for g in range(h * G, (h + 1) * G):
+                        if math.isinf(lse[r, g]):
+                            continue
+                        w = math.exp(scale * float(q[r, g] @ key) - float(lse[r, g]))
+                        total += w
+                        far += w * (scale * float(np.abs(q[r, g]) @ np.abs(key)) * (len(key) + 2) + 2 * abs(float(lse[r, g])))
+                old = decay * float(out[s, h, t]) if t < start and decay else 0.0
+                out[s, h, t] = old + total
+                reach[s, h, t] = far
+    return out, reach
+
+
+def evict(table, length, ref, weight, budget, recent, page_pos):
+    """-> table, length, ref, weight of the new book, moves [(row, layer, head, from (page, slot), to (page, slot))], status bits."""
+    rows, cols = table.shape
+    n_pages, T = len(ref), weight.shape[3]
+    goes, bits = [], 0
+    for s in range(rows):
+        b, n = int(budget[s]), int(length[s])
+        ok = 0 <= n <= cols * page_pos
+        if b >= 0 and n > b and ok:
+            ok = n <= T and all(0 <= table[s, j] < n_pages for j in range(_pages(n, page_pos)))
+            if ok:
+                goes.append(s)
+        if not ok:
+            bits |= RANGE
+    free = [p for p in range(n_pages) if ref[p] == 0]
+    new, new_len, new_ref = table.copy(), length.copy(), ref.astype(np.int64).copy()
+    new_w = np.zeros_like(weight)
+    for s in range(rows):
+        n = max(0, min(int(length[s]), T))
+        new_w[s, :, :, :n] = weight[s, :, :, :n]
+    kept_w, moves = new_w.copy(), []
+    for s in goes:
+        b, n = int(budget[s]), int(length[s])
+        for j in range(cols):
+            p = int(table[s, j])
+            if not 0 <= p < n_pages:
+                new[s, j] = -1
+            elif j >= _pages(b, page_pos):
+                new_ref[p] -= 1
+                new[s, j] = -1
+            elif ref[p] != 1:
+                if not free:
+                    return table.copy(), length.copy(), ref.copy(), new_w, [], bits | CAPACITY
+                new_ref[p] -= 1
+                new[s, j] = free.pop(0)
+                new_ref[new[s, j]] = 1
+        new_len[s] = b
+        last = min(recent, b)
+        for l in range(weight.shape[1]):
+            for h in range(weight.shape[2]):
+                w = weight[s, l, h]
+                order = sorted(range(n - last), key=lambda t: (-w[t] if w[t] == w[t] else math.inf, w[t] != w[t], t))
+                kept = sorted(order[:b - last]) + list(range(n - last, n))
+                kept_w[s, l, h] = 0
+                for i, t in enumerate(kept):
+                    kept_w[s, l, h, i] = w[t]
+                    moves.append((s, l, h, (int(table[s, t // page_pos]), t % page_pos), (int(new[s, i // page_pos]), i % page_pos)))
+    return new, new_len, new_ref.astype(np.int32), kept_w, moves, bits
+
+
+def token_logprobs(x, tokens, n_top):
+    """x [N][V], tokens [N][m] -> logp, entropy, top_logp, top_token, and the first two moments of the distance to the largest logit."""
+    N, V = x.shape
+    logp, entropy = np.zeros(tokens.shape), np.zeros(N)
+    top_logp, top_token, moments = np.full((N, n_top), -np.inf), np.full((N, n_top), -1, np.int32), np.zeros((N, 2))
+    for r in range(N):
+        row = np.asarray(x[r], np.float64)
+        if np.isnan(row).any() or not np.isfinite(row.max()):
+            logp[r], entropy[r] = np.where((tokens[r] >= 0) & (tokens[r] < V), np.nan, 0), np.nan
+            continue
+        y = row - row.max()
+        e = np.exp(y)
+        p, far = e / e.sum(), np.where(e > 0, -y, 0.0)
+        l = math.log(e.sum())
+        entropy[r] = l + float(p @ far)
+        moments[r] = p @ far, p @ far ** 2
+        for i, v in enumerate(tokens[r]):
+            if 0 <= v < V:
+                logp[r, i] = y[v] - l
+        order = np.lexsort((np.arange(V), -row))[:n_top]
+        for i, v in enumerate(order):
+            if y[v] > -np.inf:
+                top_logp[r, i], top_token[r, i] = y[v] - l, v
+    return logp, entropy, top_logp, top_token, moments

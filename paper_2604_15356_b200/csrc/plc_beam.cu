@@ -14,357 +14,18 @@
 // is subtracted before it is scaled, so that the largest terms, which carry the sum, have the smallest errors); 32 of them are added in
 // binary32 and the groups in binary64, in an order that depends on the column alone and not on the row's alignment:
 // equal rows have equal sums, so that their ties go to the lower row.
-#include <cuda_bf16.h>
-#include <float.h>
-
-#include "plc_common.cuh"
+#include "plc_logits.cuh"
 
 namespace plc {
 namespace {
 
-constexpr int kRowThreads = 128, kRowWarps = kRowThreads / 32, kResident = 7;   // blocks an SM
 constexpr int kMostOut = 128;                     // n_out, beams
-constexpr int kChunks = 32;                       // pieces of a lane's logits whose maxima are kept
-constexpr int kRoom = 1024;                       // candidates of a part that are ranked as they are
-constexpr int kBuffer = 512;                      // and, where there are more (equal logits), at a time
-constexpr int kMostVocab = 0x7fff0000;             // a column is an int, with up to 5000 more where a block's last step begins
 constexpr int kMostListed = 16384;                // entries of a session's lists (the merge holds them in shared memory)
 
-struct SelectArgs {
-    const void* logits; int64_t row_stride;
-    int rows, V, k, parts, part_len;              // k: entries of a list, min(n_out, V); part_len: a multiple of 8
-    const float* score; const uint8_t* done; int beams, eos, n_out;
-    unsigned long long* list;                     // [rows][parts][k] keys, best first
-    double* sum;                                  // [rows][parts] sum of exp(x - maximum)
-    float* top;                                   // [rows][parts] maximum
+struct SelectArgs : RowArgs {
+    const float* score; int beams, eos, n_out;
     float* out_score; int32_t* out_parent; int32_t* out_token;
 };
-
-// A key orders by (value, lower column first): the value's order-preserving bits above the complement of the column.
-__device__ __forceinline__ uint32_t order_bits(float x) {
-    const uint32_t b = __float_as_uint(x + 0.0f);                       // -0 becomes +0
-    return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
-}
-__device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o); }
-
-__device__ __forceinline__ float exp2_approx(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-constexpr float kLog2e = 1.44269504088896f;
-
-// Eight logits as they stand in memory; -inf behind the n-th.
-template <class T> struct Octet;
-__device__ __forceinline__ float widen(float v) { return v; }
-__device__ __forceinline__ float widen(__half v) { return __half2float(v); }
-__device__ __forceinline__ float widen(__nv_bfloat16 v) { return __bfloat162float(v); }
-template <> struct Octet<float> {
-    uint4 a, b;
-    __device__ __forceinline__ void load(const float* p, bool vec, int n) {
-        if (n >= 8) {
-            if (vec) { a = reinterpret_cast<const uint4*>(p)[0]; b = reinterpret_cast<const uint4*>(p)[1]; return; }
-            const uint32_t* q = reinterpret_cast<const uint32_t*>(p);
-            a = make_uint4(q[0], q[1], q[2], q[3]);
-            b = make_uint4(q[4], q[5], q[6], q[7]);
-            return;
-        }
-        uint32_t* w = reinterpret_cast<uint32_t*>(this);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = i < n ? __float_as_uint(p[i]) : 0xff800000u;
-    }
-    __device__ __forceinline__ float top() const {
-        float x[8];
-        widen(x);
-        return fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-    }
-    __device__ __forceinline__ void widen(float* x) const {
-        x[0] = __uint_as_float(a.x); x[1] = __uint_as_float(a.y); x[2] = __uint_as_float(a.z); x[3] = __uint_as_float(a.w);
-        x[4] = __uint_as_float(b.x); x[5] = __uint_as_float(b.y); x[6] = __uint_as_float(b.z); x[7] = __uint_as_float(b.w);
-    }
-};
-template <class H> struct Half8 {
-    uint4 a;
-    __device__ __forceinline__ void load(const H* p, bool vec, int n, uint32_t none) {
-        if (n >= 8) {
-            if (vec) { a = *reinterpret_cast<const uint4*>(p); return; }
-            // rows that start off 16-byte boundaries: the aligned words that hold the eight, put together
-            const bool odd = reinterpret_cast<uintptr_t>(p) & 2;
-            const uint32_t* q = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)3);
-            uint32_t w[5];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = q[i];
-            w[4] = odd ? q[4] : 0u;
-            a = odd ? make_uint4(__funnelshift_r(w[0], w[1], 16), __funnelshift_r(w[1], w[2], 16), __funnelshift_r(w[2], w[3], 16), __funnelshift_r(w[3], w[4], 16))
-                    : make_uint4(w[0], w[1], w[2], w[3]);
-            return;
-        }
-        const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
-        uint32_t w[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = i < n ? q[i] : none;
-        a = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
-    }
-};
-template <> struct Octet<__half> : Half8<__half> {
-    __device__ __forceinline__ void load(const __half* p, bool vec, int n) { Half8<__half>::load(p, vec, n, 0xfc00u); }
-    __device__ __forceinline__ float top() const {
-        const __half2* h = reinterpret_cast<const __half2*>(&a);
-        const float2 f = __half22float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
-        return fmaxf(f.x, f.y);
-    }
-    __device__ __forceinline__ void widen(float* x) const {
-        const __half2* h = reinterpret_cast<const __half2*>(&a);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { const float2 f = __half22float2(h[i]); x[2 * i] = f.x; x[2 * i + 1] = f.y; }
-    }
-};
-template <> struct Octet<__nv_bfloat16> : Half8<__nv_bfloat16> {
-    __device__ __forceinline__ void load(const __nv_bfloat16* p, bool vec, int n) { Half8<__nv_bfloat16>::load(p, vec, n, 0xff80u); }
-    __device__ __forceinline__ float top() const {
-        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&a);
-        const float2 f = __bfloat1622float2(__hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3])));
-        return fmaxf(f.x, f.y);
-    }
-    __device__ __forceinline__ void widen(float* x) const {
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-    }
-};
-
-// The largest t such that at least k of the warp's values (keys of which `n` lanes' slots hold one each, invalid ones 0) are >= t.
-template <int M> __device__ __forceinline__ uint32_t kth_largest(const uint32_t* v, int k) {
-    uint32_t lo = 0;
-#pragma unroll 1
-    for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t t = lo | (1u << bit);
-        int c = 0;
-#pragma unroll
-        for (int i = 0; i < M; ++i) c += v[i] >= t;
-        if (__reduce_add_sync(kFull, c) >= k) lo = t;
-    }
-    return lo;
-}
-
-// Cuts a warp's buffer of n > k keys to its k largest, in no particular order; returns the smallest of their value bits.  Bisection over the
-// values, then over the columns of those that equal the last one.
-__device__ __noinline__ uint32_t cut(unsigned long long* buf, int n, int k, int lane) {
-    constexpr int M = kBuffer / 32;
-    unsigned long long key[M];
-    uint32_t v[M];
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < M; ++i) {
-        key[i] = i * 32 + lane < n ? buf[i * 32 + lane] : 0ull;
-        v[i] = (uint32_t)(key[i] >> 32);
-    }
-    const uint32_t least = kth_largest<M>(v, k);
-    int above = 0, equal = 0;
-#pragma unroll
-    for (int i = 0; i < M; ++i) { above += v[i] > least; equal += key[i] != 0 && v[i] == least; }
-    above = __reduce_add_sync(kFull, above);
-    equal = __reduce_add_sync(kFull, equal);
-    uint32_t column = 0;                          // lowest complement of a column that is taken at the border
-    if (above + equal > k) {
-#pragma unroll
-        for (int i = 0; i < M; ++i) v[i] = key[i] != 0 && v[i] == least ? (uint32_t)key[i] : 0u;
-        column = kth_largest<M>(v, k - above);
-    }
-    __syncwarp();
-    int at = 0;
-    const uint32_t lt = lanemask_lt();
-#pragma unroll
-    for (int i = 0; i < M; ++i) {
-        const uint32_t hi = (uint32_t)(key[i] >> 32);
-        const bool take = key[i] != 0 && (hi > least || (hi == least && (uint32_t)key[i] >= column));
-        const uint32_t m = __ballot_sync(kFull, take);
-        if (take) buf[at + __popc(m & lt)] = key[i];
-        at += __popc(m);
-    }
-    __syncwarp();
-    return least;
-}
-
-// A block takes a part of a row in two passes.  The first streams: a warp takes 32 lanes times kGroups times eight logits a step, the next step's loads on
-// their way, forms the sum and keeps the maximum of each lane's chunks of steps.  The k-th largest of the lanes' maxima is a bound that k logits reach and
-// few others do, so the second pass looks at the chunks that reach it alone: about k of them, from L2.
-template <class T> struct Step { static constexpr int groups = 4; };                  // 64 bytes a lane
-template <> struct Step<float> { static constexpr int groups = 2; };
-template <class T>
-__global__ void __launch_bounds__(kRowThreads, kResident) beam_rows_kernel(SelectArgs a) {
-    constexpr int groups = Step<T>::groups, step = 256 * groups;
-    __shared__ float tops[kChunks][kRowThreads];
-    __shared__ unsigned long long found[kRoom];
-    __shared__ float wtop[kRowWarps];
-    __shared__ double wsum[kRowWarps];
-    __shared__ __align__(16) uint32_t order[kRowThreads];
-    __shared__ float bound;
-    __shared__ int count;
-    chain_next();
-    const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
-    if (a.done && a.done[row]) return;            // one continuation, at the beam's own score: the logits are not needed
-    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-    const T* x0 = static_cast<const T*>(a.logits) + (int64_t)row * a.row_stride;
-    const bool vec = (reinterpret_cast<uintptr_t>(x0) & 15) == 0;
-    const int c0 = part * a.part_len, c1 = min(a.V, c0 + a.part_len);
-    const int steps = (c1 - c0 + kRowWarps * step - 1) / (kRowWarps * step), per_chunk = (steps + kChunks - 1) / kChunks;
-    // the i-th step of this warp begins at column
-    auto column = [&](int w, int i) { return c0 + (i * kRowWarps + w) * step; };
-    float m = -FLT_MAX;                           // not -inf: exp(-inf - m) stays 0
-    float top = -INFINITY, chunk_top = -INFINITY;
-    double s = 0.0;
-    Octet<T> o[groups];
-    auto fetch = [&](int base) {
-        const T* x = x0 + base + lane * 8;
-        if (vec && base + step <= c1) {
-#pragma unroll
-            for (int g = 0; g < groups; ++g) o[g].load(x + g * 256, true, 8);
-        } else {
-#pragma unroll
-            for (int g = 0; g < groups; ++g) o[g].load(x + g * 256, vec, c1 - (base + g * 256 + lane * 8));
-        }
-    };
-    fetch(column(wid, 0));
-    int left = per_chunk, chunk = 0;
-    for (int i = 0; i < steps; ++i) {
-        Octet<T> now[groups];
-#pragma unroll
-        for (int g = 0; g < groups; ++g) now[g] = o[g];
-        if (i + 1 < steps) fetch(column(wid, i + 1));
-        float t = now[0].top();
-#pragma unroll
-        for (int g = 1; g < groups; ++g) t = fmaxf(t, now[g].top());
-        chunk_top = fmaxf(chunk_top, t);
-        if (t > m) { s *= (double)exp2_approx((m - t) * kLog2e); m = t; }
-        float part_sum = 0.f;
-        const unsigned long long neg = pack2(-m, -m), scale = pack2(kLog2e, kLog2e);
-#pragma unroll
-        for (int g = 0; g < groups; ++g) {
-            float x[8];
-            now[g].widen(x);
-            unsigned long long e[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float lo, hi;
-                unpack2(fma2(add2(pack2(x[2 * k], x[2 * k + 1]), neg), scale, 0ull), lo, hi);
-                e[k] = pack2(exp2_approx(lo), exp2_approx(hi));
-            }
-            float lo, hi;
-            unpack2(add2(add2(e[0], e[1]), add2(e[2], e[3])), lo, hi);
-            part_sum += lo + hi;
-        }
-        s += (double)part_sum;
-        if (--left == 0 || i + 1 == steps) {
-            tops[chunk++][tid] = chunk_top;
-            top = fmaxf(top, chunk_top);
-            chunk_top = -INFINITY;
-            left = per_chunk;
-        }
-    }
-    order[tid] = order_bits(top);
-    if (tid == 0) count = 0;
-    float warp_top = m;
-#pragma unroll
-    for (int w = 16; w > 0; w >>= 1) warp_top = fmaxf(warp_top, __shfl_xor_sync(kFull, warp_top, w));
-    s *= (double)exp2_approx((m - warp_top) * kLog2e);
-#pragma unroll
-    for (int w = 16; w > 0; w >>= 1) s += __shfl_xor_sync(kFull, s, w);
-    if (lane == 0) { wtop[wid] = warp_top; wsum[wid] = s; }
-    __syncthreads();
-    const long long slot = (long long)row * a.parts + part;
-    {
-        int rank = 0;                             // of the lane's maximum among all
-        const uint32_t mine = order[tid];
-#pragma unroll 4
-        for (int i = 0; i < kRowThreads; i += 4) {
-            const uint4 v = *reinterpret_cast<const uint4*>(order + i);
-            rank += (v.x > mine || (v.x == mine && i < tid)) + (v.y > mine || (v.y == mine && i + 1 < tid)) + (v.z > mine || (v.z == mine && i + 2 < tid)) +
-                    (v.w > mine || (v.w == mine && i + 3 < tid));
-        }
-        if (rank == a.k - 1) bound = top;
-        if (tid == 0) {
-            float all = wtop[0];
-            for (int w = 1; w < kRowWarps; ++w) all = fmaxf(all, wtop[w]);
-            double sum = 0.0;
-            for (int w = 0; w < kRowWarps; ++w) sum += wsum[w] * (double)exp2_approx((wtop[w] - all) * kLog2e);
-            a.sum[slot] = sum;
-            a.top[slot] = all;
-        }
-    }
-    __syncthreads();
-    const uint32_t lt = lanemask_lt();
-    // what lane l of warp w took in its i-th step, a logit a lane (0: none)
-    auto look = [&](int w, int l, int i) -> unsigned long long {
-        const int at = column(w, i) + (lane >> 3) * 256 + l * 8 + (lane & 7);
-        return lane < 8 * groups && at < c1 ? ((unsigned long long)order_bits(widen(x0[at])) << 32) | (uint32_t)~at : 0ull;
-    };
-    {
-        const float limit = bound;
-        const uint32_t least = order_bits(limit);
-        for (int c = 0; c < chunk; ++c) {
-            uint32_t who = __ballot_sync(kFull, tops[c][tid] >= limit);
-            while (who) {
-                const int l = __ffs(who) - 1;
-                who &= who - 1;
-                for (int i = c * per_chunk; i < min(steps, (c + 1) * per_chunk); ++i) {
-                    const unsigned long long key = look(wid, l, i);
-                    const bool take = (uint32_t)(key >> 32) >= least && key != 0;
-                    const uint32_t b = __ballot_sync(kFull, take);
-                    if (!b) continue;
-                    int at = 0;
-                    if (lane == 0) at = atomicAdd(&count, __popc(b));
-                    at = __shfl_sync(kFull, at, 0) + __popc(b & lt);
-                    if (take && at < kRoom) found[at] = key;
-                }
-            }
-        }
-    }
-    __syncthreads();
-    int n = count;
-    if (n > kRoom) {                              // many equal logits: one warp looks through them, in no more than kBuffer places
-        __syncthreads();
-        if (wid == 0) {
-            n = 0;
-            unsigned long long worst = 0ull;      // what a candidate has to pass, once k have been found
-            for (int w = 0; w < kRowWarps; ++w)
-                for (int c = 0; c < chunk; ++c) {
-                    uint32_t who = __ballot_sync(kFull, order_bits(tops[c][w * 32 + lane]) >= max((uint32_t)(worst >> 32), order_bits(bound)));
-                    while (who) {
-                        const int l = __ffs(who) - 1;
-                        who &= who - 1;
-                        for (int i = c * per_chunk; i < min(steps, (c + 1) * per_chunk); ++i) {
-                            const unsigned long long key = look(w, l, i);
-                            const bool take = key > worst;
-                            const uint32_t b = __ballot_sync(kFull, take);
-                            if (take) found[n + __popc(b & lt)] = key;
-                            n += __popc(b);
-                            if (n <= kBuffer - 32) continue;
-                            cut(found, n, a.k, lane);
-                            n = a.k;
-                            worst = ~0ull;
-                            for (int k = lane; k < n; k += 32) worst = min(worst, found[k]);
-#pragma unroll
-                            for (int k = 16; k > 0; k >>= 1) worst = min(worst, __shfl_xor_sync(kFull, worst, k));
-                        }
-                    }
-                }
-            __syncwarp();
-            if (lane == 0) count = n;
-        }
-        __syncthreads();
-        n = count;
-    }
-    // each candidate's place is the number of better ones
-    unsigned long long* out = a.list + slot * a.k;
-    for (int i = n + tid; i < a.k; i += kRowThreads) out[i] = 0ull;
-    for (int i = tid; i < n; i += kRowThreads) {
-        const unsigned long long key = found[i];
-        int place = 0;
-        for (int j = 0; j < n; ++j) place += found[j] > key;
-        if (place < a.k) out[place] = key;
-    }
-}
 
 // A continuation: its score's order-preserving bits (0: none), and its place (row in the session, column) as one number.
 struct Cont { unsigned long long score; uint32_t place; };
@@ -579,8 +240,8 @@ plc_status plc_beam_select(const void* logits_dev, int32_t dtype, int64_t row_st
     a.top = reinterpret_cast<float*>(a.sum + rows * a.parts);
     a.out_score = out_score_dev; a.out_parent = out_parent_dev; a.out_token = out_token_dev;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    auto kern = dtype == PLC_OUT_F32 ? beam_rows_kernel<float> : dtype == PLC_OUT_F16 ? beam_rows_kernel<__half> : beam_rows_kernel<__nv_bfloat16>;
-    if (launch_kernel(kern, (unsigned)(rows * a.parts), kRowThreads, 0, st, false, 1, a) != cudaSuccess) return PLC_E_CUDA;
+    auto kern = dtype == PLC_OUT_F32 ? rows_kernel<float, false> : dtype == PLC_OUT_F16 ? rows_kernel<__half, false> : rows_kernel<__nv_bfloat16, false>;
+    if (launch_kernel(kern, (unsigned)(rows * a.parts), kRowThreads, 0, st, false, 1, static_cast<RowArgs>(a)) != cudaSuccess) return PLC_E_CUDA;
     const size_t smem = (size_t)beams * a.parts * a.k * 8;
     if (cudaFuncSetAttribute(beam_merge_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostListed * 8) != cudaSuccess) return PLC_E_CUDA;
     if (launch_kernel(beam_merge_kernel, (unsigned)sessions, kMergeThreads, smem, st, true, 1, a) != cudaSuccess) return PLC_E_CUDA;

@@ -1,0 +1,169 @@
+// Log probabilities of given tokens, the entropy of their rows and the likeliest alternatives (plc_token_logprobs).
+//
+// With y = x - max x and Z = sum exp y:  log p_v = y_v - ln Z,  H = ln Z + (sum exp(y) (-y)) / Z.  One pass over the logits (the rows of beam selection, with the
+// second sum beside the first) leaves maximum, sums and the n largest of each part of a row; a second, small launch joins the parts and
+// looks the given tokens up.  HBM bound: each logit is read once.
+//
+// Exponentials and the sums of 32 of them are binary32, what is added up beyond binary64.  The largest term of Z is exactly 1 and -y >= 0, so that neither a
+// log probability near 0 nor a small entropy is the difference of larger numbers (terms below 2^-24 of their group are rounded to it).
+#include "plc_logits.cuh"
+
+namespace plc {
+namespace {
+
+constexpr int kMostTop = 128, kMostTokens = 1 << 20;
+constexpr int kMostListed = 1024;                 // entries of a row's lists
+constexpr int kJoinThreads = 128;
+
+struct LogprobArgs : RowArgs {
+    const int32_t* tokens; int n_tokens, n_top, esz_log2, bf16;
+    float* logp; float* entropy; float* top_logp; int32_t* top_token;
+    uint32_t* status;
+};
+
+// A block a row.
+__global__ void __launch_bounds__(kJoinThreads) logprob_join_kernel(LogprobArgs a) {
+    __shared__ unsigned long long keys[kMostListed];
+    __shared__ double log_sum;
+    __shared__ float row_top;
+    chain_wait();
+    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
+    const long long slot = (long long)row * a.parts;
+    const int entries = a.parts * a.k;
+    for (int i = tid; i < entries; i += kJoinThreads) keys[i] = a.list[slot * a.k + i];
+    if (tid < 32) {                               // at most 64 parts, two a lane
+        float top = -FLT_MAX;
+        for (int q = lane; q < a.parts; q += 32) top = fmaxf(top, a.top[slot + q]);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
+        double sum = 0.0, spread = 0.0;
+        for (int q = lane; q < a.parts; q += 32) {
+            const float t = a.top[slot + q];
+            const double f = (double)exp2_approx((t - top) * kLog2e), s = a.sum[slot + q];
+            sum += f * s;
+            if (s != 0.0) spread += f * (a.spread[slot + q] + s * ((double)top - (double)t));
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            sum += __shfl_xor_sync(kFull, sum, o);
+            spread += __shfl_xor_sync(kFull, spread, o);
+        }
+        if (lane == 0) {
+            const bool some = sum > 0.0;          // NaN, and nothing but -inf: not a distribution
+            const double l = some ? log(sum) : (double)NAN;
+            log_sum = l;
+            row_top = top;
+            if (a.entropy) a.entropy[row] = (float)(l + spread / sum);
+        }
+    }
+    __syncthreads();
+    const double l = log_sum;
+    const float top = row_top;
+    for (int i = tid; i < a.n_tokens; i += kJoinThreads) {
+        const long long at = (long long)row * a.n_tokens + i;
+        const int v = a.tokens[at];
+        float y = 0.f;
+        if (v >= 0 && v < a.V) {
+            const uint8_t* x = static_cast<const uint8_t*>(a.logits) + (((int64_t)row * a.row_stride + v) << a.esz_log2);
+            const float z = a.esz_log2 == 2 ? *reinterpret_cast<const float*>(x)
+                            : a.bf16 ? widen(*reinterpret_cast<const __nv_bfloat16*>(x)) : widen(*reinterpret_cast<const __half*>(x));
+            y = (float)(((double)z - (double)top) - l);
+        } else if (v != -1 && a.status) atomicOr(a.status, kStRange);
+        a.logp[at] = y;
+    }
+    // an entry's place is the number of better ones: those before it in its own list, and in each other list as many as a bisection finds
+    for (int i = tid; i < entries; i += kJoinThreads) {
+        const unsigned long long key = keys[i];
+        const int mine = i / a.k;
+        int place = i - mine * a.k;
+        for (int q = 0; q < a.parts && place < a.n_top; ++q) {
+            if (q == mine) continue;
+            int lo = 0, hi = a.k;                 // keys[lo - 1] > key >= keys[hi]
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (keys[q * a.k + mid] > key) lo = mid + 1;
+                else hi = mid;
+            }
+            place += lo;
+        }
+        if (key != 0 && place < a.n_top) {
+            const float z = value_of((uint32_t)(key >> 32));
+            const double y = ((double)z - (double)top) - l;
+            const bool some = isfinite(y);
+            a.top_logp[(long long)row * a.n_top + place] = some ? (float)y : -INFINITY;
+            a.top_token[(long long)row * a.n_top + place] = some ? (int)~(uint32_t)key : -1;
+        }
+    }
+    for (int i = min(a.n_top, a.V) + tid; i < a.n_top; i += kJoinThreads) {
+        a.top_logp[(long long)row * a.n_top + i] = -INFINITY;
+        a.top_token[(long long)row * a.n_top + i] = -1;
+    }
+}
+
+// Parts of a row, as for beams: the least rounds of blocks times (a warp's logits plus what is done once).
+constexpr int kSetUp = 1500;
+int row_parts(long long rows, int V, int k) {
+    const long long most = (V + 4095) / 4096, fit = k ? kMostListed / k : 64, slots = (long long)kResident * sm_count();
+    long long best = 1, least = 0;
+    for (long long q = 1; q <= most && q <= fit && q <= 64; ++q) {
+        const long long cost = (rows * q + slots - 1) / slots * ((V + q - 1) / q / kRowWarps + kSetUp);
+        if (q == 1 || cost < least) { best = q; least = cost; }
+    }
+    return (int)best;
+}
+uint64_t logprob_bytes(long long rows, int V, int n_top, int* parts, int* k) {
+    *k = n_top < V ? n_top : V;
+    *parts = row_parts(rows, V, *k);
+    return (uint64_t)rows * *parts * (8ull * *k + 20);
+}
+plc_status check_rows(int32_t rows, int32_t vocab, int32_t n_tokens, int32_t n_top) {
+    if (rows < 1 || vocab < 1 || n_tokens < 0 || n_top < 0) return PLC_E_INVALID;
+    return rows > (1 << 24) || vocab > kMostVocab || n_tokens > kMostTokens || n_top > kMostTop ? PLC_E_SHAPE : PLC_OK;
+}
+
+}  // namespace
+}  // namespace plc
+
+using namespace plc;
+
+extern "C" {
+
+plc_status plc_token_logprobs_workspace(int32_t rows, int32_t vocab, int32_t n_top, uint64_t* bytes) {
+    const plc_status rc = check_rows(rows, vocab, 0, n_top);
+    if (rc) return rc;
+    if (!bytes) return PLC_E_INVALID;
+    int parts, k;
+    *bytes = logprob_bytes(rows, vocab, n_top, &parts, &k);
+    return PLC_OK;
+}
+
+plc_status plc_token_logprobs(const void* logits_dev, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab, const int32_t* tokens_dev, int32_t n_tokens,
+                              int32_t n_top, float* logp_dev, float* entropy_dev, float* top_logp_dev, int32_t* top_token_dev, void* workspace_dev,
+                              uint64_t workspace_bytes, uint32_t* status_dev, void* stream) {
+    const plc_status rc = check_rows(rows, vocab, n_tokens, n_top);
+    if (rc) return rc;
+    if (!logits_dev || !workspace_dev || (n_tokens > 0 && (!tokens_dev || !logp_dev)) || (n_top > 0 && (!top_logp_dev || !top_token_dev))) return PLC_E_INVALID;
+    if (dtype != PLC_OUT_F32 && dtype != PLC_OUT_F16 && dtype != PLC_OUT_BF16) return PLC_E_INVALID;
+    const int esz = dtype == PLC_OUT_F32 ? 4 : 2;
+    if ((reinterpret_cast<uintptr_t>(logits_dev) & (esz - 1)) || (reinterpret_cast<uintptr_t>(workspace_dev) & 15)) return PLC_E_ALIGN;
+    LogprobArgs a{};
+    const uint64_t need = logprob_bytes(rows, vocab, n_top, &a.parts, &a.k);
+    if (workspace_bytes < need) return PLC_E_CAPACITY;
+    if ((long long)rows * a.parts > 0x7fffffffll) return PLC_E_SHAPE;
+    a.logits = logits_dev; a.row_stride = row_stride; a.rows = rows; a.V = vocab;
+    a.part_len = ((vocab + a.parts - 1) / a.parts + 7) & ~7;
+    a.list = static_cast<unsigned long long*>(workspace_dev);
+    a.sum = reinterpret_cast<double*>(a.list + (int64_t)rows * a.parts * a.k);
+    a.spread = a.sum + (int64_t)rows * a.parts;
+    a.top = reinterpret_cast<float*>(a.spread + (int64_t)rows * a.parts);
+    a.tokens = tokens_dev; a.n_tokens = n_tokens; a.n_top = n_top; a.esz_log2 = esz == 4 ? 2 : 1; a.bf16 = dtype == PLC_OUT_BF16;
+    a.logp = logp_dev; a.entropy = entropy_dev; a.top_logp = top_logp_dev; a.top_token = top_token_dev; a.status = status_dev;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    auto kern = dtype == PLC_OUT_F32 ? rows_kernel<float, true> : dtype == PLC_OUT_F16 ? rows_kernel<__half, true> : rows_kernel<__nv_bfloat16, true>;
+    if (launch_kernel(kern, (unsigned)(rows * a.parts), kRowThreads, 0, st, false, 1, static_cast<RowArgs>(a)) != cudaSuccess) return PLC_E_CUDA;
+    if (launch_kernel(logprob_join_kernel, (unsigned)rows, kJoinThreads, 0, st, true, 1, a) != cudaSuccess) return PLC_E_CUDA;
+    count_launch(2);
+    return PLC_OK;
+}
+
+}  // extern "C"

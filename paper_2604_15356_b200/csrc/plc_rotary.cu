@@ -1,0 +1,333 @@
+// Rotary positions: tensors of queries and keys are turned (plc_rotary_apply), and new tokens' keys are turned on their way into the pages, values
+// beside them (plc_pages_append).
+//
+// A pair (x_a, x_b) of components at position pos becomes s (x_a cos t - x_b sin t, x_b cos t + x_a sin t), t = pos f_i.  The frequency is held in turns a
+// position as a fraction of 64 bits, so that the product with the position, cut to its low 64 bits, is the angle modulo a turn to 2^-33 turns at any
+// position that an int holds: no product in 64-bit floating point and no reduction.  Its sine and cosine are formed once a row and pair, in shared memory, for all
+// heads.
+//
+// Bound by HBM where rows are many (each component read and written once, 16 bytes a thread and access), by the launch where they are few.  A block takes a few
+// rows with all their heads.
+#include <cuda_bf16.h>
+#include <math.h>
+
+#include "plc_pages.cuh"
+
+namespace plc {
+namespace {
+
+constexpr int kTurnThreads = 256, kMostRows = 8;  // of a block
+constexpr int kMostSets = 4, kMostDim = 1024;
+
+struct TurnSet {
+    const uint8_t* x; uint8_t* out;
+    int64_t xs_row, xs_head, os_row, os_head;     // bytes
+    int heads, dim;                               // dim: components that turn
+    int per_head, per_head_magic;                 // units of a head; 2^32 over it, rounded up
+    int first;                                    // unit of a row that the set begins with
+};
+struct TurnArgs {
+    TurnSet set[kMostSets];
+    int sets, units, units_magic;                 // units of a row
+    const uint64_t* turns; int pairs; float scale; bool back;
+    const int32_t* pos; int rows, d, rows_block;
+    const int32_t* begin; int layer;              // pages: ranges of the sessions' rows
+};
+
+template <class T> struct Wide;
+template <> struct Wide<float> {
+    static __device__ __forceinline__ float get(float v) { return v; }
+    static __device__ __forceinline__ float put(float v) { return v; }
+};
+template <> struct Wide<__half> {
+    static __device__ __forceinline__ float get(__half v) { return __half2float(v); }
+    static __device__ __forceinline__ __half put(float v) { return __float2half_rn(v); }
+};
+template <> struct Wide<__nv_bfloat16> {
+    static __device__ __forceinline__ float get(__nv_bfloat16 v) { return __bfloat162float(v); }
+    static __device__ __forceinline__ __nv_bfloat16 put(float v) { return __float2bfloat16_rn(v); }
+};
+
+// A run of W components as it stands in memory.
+template <class T, int W, bool VEC> struct Run {
+    T v[W];
+    __device__ __forceinline__ void load(const uint8_t* p) {
+        if constexpr (VEC) *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(p);
+        else
+#pragma unroll
+            for (int i = 0; i < W; ++i) v[i] = reinterpret_cast<const T*>(p)[i];
+    }
+    __device__ __forceinline__ void store(uint8_t* p) const {
+        if constexpr (VEC) *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(v);
+        else
+#pragma unroll
+            for (int i = 0; i < W; ++i) reinterpret_cast<T*>(p)[i] = v[i];
+    }
+};
+
+// The session of row i: the last one whose range begins at or before it; -1 where it is in none.  A warp calls it.
+__device__ __forceinline__ int session_of_row(const int32_t* begin, int sessions, int i) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, hi = sessions;
+    for (;;) {
+        const int step = (hi - lo + 31) / 32, at = lo + min(lane, (hi - lo - 1) / step) * step;
+        const uint32_t m = __ballot_sync(kFull, begin[at] <= i);
+        if (m == 0) return -1;
+        const int j = min(31 - __clz(m), (hi - lo - 1) / step);
+        lo += j * step;
+        hi = min(hi, lo + step);
+        if (step == 1) break;
+    }
+    return begin[lo] <= i && i < begin[lo + 1] ? lo : -1;
+}
+
+// INTER: pairs are neighbours, else half a turned part away.  VEC: 16 bytes at a time.
+template <class T, bool INTER, bool VEC, bool PAGES>
+__global__ void __launch_bounds__(kTurnThreads) turn_kernel(const __grid_constant__ TurnArgs a, const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
+                                                            uint32_t* status) {
+    constexpr int W = VEC ? 16 / (int)sizeof(T) : INTER ? 2 : 1, REST = VEC ? W : 1;
+    extern __shared__ float2 turn[];              // [rows of the block][pairs] cosine, sine
+    __shared__ int64_t row_to[kMostRows];         // where a row's key goes, from the layer's first key on; -1: nowhere
+    __shared__ int row_pos[kMostRows];            // its position; the row is in some range
+    __shared__ bool row_in[kMostRows];
+    const int tid = threadIdx.x, r0 = blockIdx.x * a.rows_block, rows = min(a.rows_block, a.rows - r0);
+    if (PAGES) {
+        bool bad = false;
+        for (int s = blockIdx.x * kTurnThreads + tid; s < b.rows; s += gridDim.x * kTurnThreads)
+            bad |= a.begin[s] < 0 || a.begin[s + 1] < a.begin[s] || a.begin[s + 1] > a.rows;
+        if (bad) atomicOr(status, kStRange);
+        const int w = tid >> 5;
+        if (w < rows) {
+            const int i = r0 + w, s = session_of_row(a.begin, b.rows, i);
+            if ((tid & 31) == 0) {
+                int64_t to = -1;
+                int stands = 0;
+                if (s >= 0) {
+                    const int len = b.len[s];
+                    const long long t = (long long)len + (i - a.begin[s]);
+                    stands = (int)t;
+                    int page = -1;
+                    if (len >= 0 && t < most_positions(b, p)) page = b.table[(int64_t)s * b.max_pages + t / p.page_pos];
+                    if (page >= 0 && page < p.n_pages && b.ref[page] == 1) to = (int64_t)page * p.spage + (int64_t)(t % p.page_pos) * p.sp;
+                    if (to < 0) { to = -1; atomicOr(status, kStRange); }
+                }
+                row_to[w] = to;
+                row_in[w] = s >= 0;
+                row_pos[w] = a.pos ? a.pos[i] : stands;
+            }
+        }
+    } else if (tid < rows) row_pos[tid] = a.pos[r0 + tid];
+    __syncthreads();
+    for (int i = tid; i < rows * a.pairs; i += kTurnThreads) {
+        const int r = i / a.pairs;
+        const uint64_t angle = (uint64_t)(int64_t)row_pos[r] * a.turns[i - r * a.pairs] + (1ull << 31);
+        float s, c;
+        sincospif((float)(int32_t)(angle >> 32) * 0x1p-31f, &s, &c);
+        turn[i] = make_float2(c * a.scale, a.back ? -s * a.scale : s * a.scale);
+    }
+    __syncthreads();
+    const int units = rows * a.units;
+    constexpr int K = VEC ? 4 : 2;
+    for (int u0 = tid; u0 < units; u0 += K * kTurnThreads) {
+        Run<T, W, VEC> x[K], y[K];
+        uint8_t* to[K];
+        int at[K], pairs_from[K], kind[K];        // kind: 0 nothing, 1 a pair of runs (or one run of neighbours), 2 a run that is copied
+        int half[K];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int u = u0 + k * kTurnThreads;
+            kind[k] = 0;
+            if (u >= units) continue;
+            const int r = a.rows_block == 1 ? 0 : a.units == 1 ? u : (int)__umulhi((uint32_t)u, (uint32_t)a.units_magic), v = u - r * a.units;
+            int t = 0;
+#pragma unroll
+            for (int i = 1; i < kMostSets; ++i) t += i < a.sets && v >= a.set[i].first;
+            const TurnSet& s = a.set[t];
+            const int w = v - s.first, h = s.per_head == 1 ? w : (int)__umulhi((uint32_t)w, (uint32_t)s.per_head_magic), e = w - h * s.per_head;
+            const uint8_t* from = s.x + (int64_t)(r0 + r) * s.xs_row + (int64_t)h * s.xs_head;
+            if (PAGES && t > 0) {
+                if (row_to[r] < 0) continue;
+                to[k] = p.base + (int64_t)a.layer * p.sl + (t == 2 ? p.skv : 0) + row_to[r] + (int64_t)h * p.sh;
+            } else {
+                if (PAGES && !row_in[r]) continue;
+                to[k] = s.out + (int64_t)(r0 + r) * s.os_row + (int64_t)h * s.os_head;
+            }
+            const int turned = INTER ? s.dim / W : s.dim / (2 * W);
+            if (e < turned) {
+                kind[k] = 1;
+                at[k] = e * W * (int)sizeof(T);
+                half[k] = s.dim / 2 * (int)sizeof(T);
+                pairs_from[k] = r * a.pairs + (INTER ? e * W / 2 : e * W);
+                x[k].load(from + at[k]);
+                if (!INTER) y[k].load(from + at[k] + half[k]);
+            } else {
+                kind[k] = 2;
+                at[k] = (s.dim + (e - turned) * REST) * (int)sizeof(T);
+                if constexpr (VEC) x[k].load(from + at[k]);
+                else x[k].v[0] = *reinterpret_cast<const T*>(from + at[k]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (kind[k] == 1) {
+                if (INTER) {
+#pragma unroll
+                    for (int i = 0; i < W; i += 2) {
+                        const float2 cs = turn[pairs_from[k] + i / 2];
+                        const float xa = Wide<T>::get(x[k].v[i]), xb = Wide<T>::get(x[k].v[i + 1 < W ? i + 1 : i]);
+                        x[k].v[i] = Wide<T>::put(xa * cs.x - xb * cs.y);
+                        x[k].v[i + 1 < W ? i + 1 : i] = Wide<T>::put(xb * cs.x + xa * cs.y);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < W; ++i) {
+                        const float2 cs = turn[pairs_from[k] + i];
+                        const float xa = Wide<T>::get(x[k].v[i]), xb = Wide<T>::get(y[k].v[i]);
+                        x[k].v[i] = Wide<T>::put(xa * cs.x - xb * cs.y);
+                        y[k].v[i] = Wide<T>::put(xb * cs.x + xa * cs.y);
+                    }
+                    y[k].store(to[k] + at[k] + half[k]);
+                }
+                x[k].store(to[k] + at[k]);
+            } else if (kind[k] == 2) {
+                if constexpr (VEC) x[k].store(to[k] + at[k]);
+                else *reinterpret_cast<T*>(to[k] + at[k]) = x[k].v[0];
+            }
+        }
+    }
+}
+
+int magic_of(int n) { return n > 1 ? (int)(uint32_t)(((1ull << 32) + n - 1) / n) : 0; }
+
+// Units of the sets, and the launch: rows of a block so that there are several blocks an SM, at most kMostRows.
+template <bool PAGES>
+plc_status launch_turn(TurnArgs& a, const PoolDev& p, const BookDev& b, int dtype, bool inter, bool vec, uint32_t* status, cudaStream_t st) {
+    const int esz = dtype == PLC_OUT_F32 ? 4 : 2, w = 16 / esz;
+    int units = 0;
+    for (int i = 0; i < a.sets; ++i) {
+        TurnSet& s = a.set[i];
+        s.per_head = vec ? (inter ? s.dim / w : s.dim / 2 / w) + (a.d - s.dim) / w : s.dim / 2 + a.d - s.dim;
+        s.per_head_magic = magic_of(s.per_head);
+        s.first = units;
+        units += s.heads * s.per_head;
+    }
+    a.units = units;
+    a.units_magic = magic_of(units);
+    const int per = a.rows / (4 * sm_count());
+    a.rows_block = per < 1 || units > 20000 ? 1 : per > kMostRows ? kMostRows : per;      // (the quotients by a magic number are exact below 2^32 / divisor)
+    const unsigned grid = (unsigned)((a.rows + a.rows_block - 1) / a.rows_block);
+    const size_t smem = (size_t)a.rows_block * a.pairs * sizeof(float2);
+    auto go = [&](auto* kern) -> cudaError_t {
+        cudaError_t e = smem > 49152 ? cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+        return e != cudaSuccess ? e : launch_kernel(kern, grid, kTurnThreads, smem, st, false, 1, a, p, b, status);
+    };
+    cudaError_t e;
+#define PLC_TURN(T) (inter ? (vec ? go(turn_kernel<T, true, true, PAGES>) : go(turn_kernel<T, true, false, PAGES>)) \
+                           : (vec ? go(turn_kernel<T, false, true, PAGES>) : go(turn_kernel<T, false, false, PAGES>)))
+    if (dtype == PLC_OUT_F32) e = PLC_TURN(float);
+    else if (dtype == PLC_OUT_F16) e = PLC_TURN(__half);
+    else e = PLC_TURN(__nv_bfloat16);
+#undef PLC_TURN
+    if (e != cudaSuccess) return PLC_E_CUDA;
+    count_launch(1);
+    return PLC_OK;
+}
+
+plc_status check_rotary(const plc_rotary* r, int head_dim, TurnArgs* a) {
+    if (!r || !r->turns_dev) return PLC_E_INVALID;
+    if (r->dim < 2 || r->dim % 2 || r->dim > head_dim) return PLC_E_SHAPE;
+    if (!isfinite(r->scale)) return PLC_E_INVALID;
+    if (reinterpret_cast<uintptr_t>(r->turns_dev) & 7) return PLC_E_ALIGN;
+    a->turns = r->turns_dev;
+    a->pairs = r->dim / 2;
+    a->scale = r->scale;
+    return PLC_OK;
+}
+// Whether runs of 16 bytes cover the turned part, its halves and the rest.
+bool wide_runs(int dim, int d, bool inter, int esz) { return (inter ? dim : dim / 2) * esz % 16 == 0 && (d - dim) * esz % 16 == 0; }
+bool wide_set(const TurnSet& s) {
+    return ((reinterpret_cast<uintptr_t>(s.x) | reinterpret_cast<uintptr_t>(s.out) | (uintptr_t)s.xs_row | (uintptr_t)s.xs_head | (uintptr_t)s.os_row |
+             (uintptr_t)s.os_head) & 15) == 0;
+}
+
+}  // namespace
+}  // namespace plc
+
+using namespace plc;
+
+extern "C" {
+
+plc_status plc_rotary_turns(const double* radians, int32_t n, uint64_t* turns) {
+    if (!radians || !turns || n < 1) return PLC_E_INVALID;
+    for (int i = 0; i < n; ++i) {
+        const double f = radians[i];
+        if (!(f >= 0.0) || f > 65536.0) return PLC_E_INVALID;
+        // f = m 2^(e - 53); turns = m / (2 pi) 2^(e - 53 + 64).  1 / (2 pi) = 0x28BE60DB9391054A 7F09D5F47D4D3770 2^-128
+        int e;
+        const uint64_t m = (uint64_t)ldexp(frexp(f, &e), 53);
+        const unsigned __int128 lo = (unsigned __int128)m * 0x7F09D5F47D4D3770ull, hi = (unsigned __int128)m * 0x28BE60DB9391054Aull + (uint64_t)(lo >> 64);
+        // m / (2 pi) = (hi 2^64 + (low half of lo)) 2^-128; times 2^(e + 11), rounded
+        const int shift = 53 - e;                 // of hi, to the right: at least 36
+        if (shift > 126) { turns[i] = 0; continue; }
+        turns[i] = (uint64_t)((hi + ((unsigned __int128)1 << (shift - 1))) >> shift);
+    }
+    return PLC_OK;
+}
+
+plc_status plc_rotary_apply(const plc_rotary* rotary, const plc_rotary_set* sets, int32_t n_sets, const int32_t* pos_dev, int32_t n_rows, int32_t head_dim,
+                            int32_t dtype, int32_t back, void* stream) {
+    TurnArgs a{};
+    if (!sets || n_sets < 1 || !pos_dev || n_rows < 0 || head_dim < 2) return PLC_E_INVALID;
+    if (dtype != PLC_OUT_F32 && dtype != PLC_OUT_F16 && dtype != PLC_OUT_BF16) return PLC_E_INVALID;
+    if (n_sets > kMostSets || head_dim > kMostDim) return PLC_E_SHAPE;
+    const plc_status rc = check_rotary(rotary, head_dim, &a);
+    if (rc) return rc;
+    const int esz = dtype == PLC_OUT_F32 ? 4 : 2;
+    bool vec = wide_runs(rotary->dim, head_dim, rotary->interleaved != 0, esz);
+    long long heads = 0;
+    for (int i = 0; i < n_sets; ++i) {
+        const plc_rotary_set& s = sets[i];
+        if (!s.x_dev || !s.out_dev || s.heads < 1) return PLC_E_INVALID;
+        if ((reinterpret_cast<uintptr_t>(s.x_dev) | reinterpret_cast<uintptr_t>(s.out_dev)) & (esz - 1)) return PLC_E_ALIGN;
+        if (s.x_dev == s.out_dev && ((n_rows > 1 && s.x_stride_row != s.out_stride_row) || (s.heads > 1 && s.x_stride_head != s.out_stride_head))) return PLC_E_INVALID;
+        heads += s.heads;
+        if (heads > (1 << 12)) return PLC_E_SHAPE;
+        a.set[i] = TurnSet{static_cast<const uint8_t*>(s.x_dev), static_cast<uint8_t*>(s.out_dev), s.x_stride_row * esz, s.x_stride_head * esz, s.out_stride_row * esz,
+                           s.out_stride_head * esz, s.heads, rotary->dim, 0, 0, 0};
+        vec = vec && wide_set(a.set[i]);
+    }
+    if (n_rows == 0) return PLC_OK;
+    a.sets = n_sets; a.back = back != 0; a.pos = pos_dev; a.rows = n_rows; a.d = head_dim;
+    return launch_turn<false>(a, PoolDev{}, BookDev{}, dtype, rotary->interleaved != 0, vec, nullptr, static_cast<cudaStream_t>(stream));
+}
+
+plc_status plc_pages_append(const plc_page_pool* pool, int32_t layer, const plc_page_book* book, const plc_rotary* rotary, const plc_new_tokens* t,
+                            uint32_t* status_dev, void* stream) {
+    PoolDev p;
+    BookDev b;
+    TurnArgs a{};
+    plc_status rc = check_pool(pool, &p);
+    if (rc || (rc = check_book(book, &b))) return rc;
+    if (!t || !t->k_dev || !t->v_dev || !t->begin_dev || t->n_rows < 0 || t->n_heads < 0 || !status_dev || layer < 0 || layer >= p.L) return PLC_E_INVALID;
+    if (t->n_heads > 0 && (!t->q_dev || !t->out_dev)) return PLC_E_INVALID;
+    if (rotary && (rc = check_rotary(rotary, p.d, &a))) return rc;
+    if ((long long)t->n_heads + 2 * p.H > (1 << 14)) return PLC_E_SHAPE;
+    const int esz = p.esz, dim = rotary ? rotary->dim : 0;
+    const bool inter = rotary && rotary->interleaved;
+    if ((reinterpret_cast<uintptr_t>(t->k_dev) | reinterpret_cast<uintptr_t>(t->v_dev) | reinterpret_cast<uintptr_t>(t->n_heads ? t->q_dev : nullptr) |
+         reinterpret_cast<uintptr_t>(t->n_heads ? t->out_dev : nullptr)) & (esz - 1))
+        return PLC_E_ALIGN;
+    if (t->n_heads > 0 && t->q_dev == t->out_dev &&
+        ((t->n_rows > 1 && t->q_stride_row != t->out_stride_row) || (t->n_heads > 1 && t->q_stride_head != t->out_stride_head)))
+        return PLC_E_INVALID;
+    if (t->n_rows == 0) return PLC_OK;
+    a.set[0] = TurnSet{static_cast<const uint8_t*>(t->q_dev), static_cast<uint8_t*>(t->out_dev), t->q_stride_row * esz, t->q_stride_head * esz, t->out_stride_row * esz,
+                       t->out_stride_head * esz, t->n_heads, dim, 0, 0, 0};
+    a.set[1] = TurnSet{static_cast<const uint8_t*>(t->k_dev), nullptr, t->k_stride_row * esz, t->k_stride_head * esz, 0, 0, p.H, dim, 0, 0, 0};
+    a.set[2] = TurnSet{static_cast<const uint8_t*>(t->v_dev), nullptr, t->v_stride_row * esz, t->v_stride_head * esz, 0, 0, p.H, 0, 0, 0, 0};
+    const bool vec = wide_runs(dim, p.d, inter, esz) && (t->n_heads == 0 || wide_set(a.set[0])) && wide_set(a.set[1]) && wide_set(a.set[2]);
+    a.sets = 3; a.pos = t->pos_dev; a.rows = t->n_rows; a.d = p.d; a.begin = t->begin_dev; a.layer = layer;
+    return launch_turn<true>(a, p, b, pool->dtype, inter, vec, status_dev, static_cast<cudaStream_t>(stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,225 @@
+// Attention weights that cached positions receive (plc_pages_weigh), added up for eviction.
+//
+// weight[s][h][t] = decay weight[s][h][t] + sum over the session's newest rows i that see t, and over the query heads g of KV head h, of
+// exp(scale q_ig . k_t - lse_ig), with the log-sum-exp that the attention has left: no maximum and no sum is carried, every tile of positions stands by itself.
+//
+// A warp takes tiles of 16 positions.  The product S = K Q^T has the positions as rows; the components may come in any order as long as K and Q have the same
+// one, so a lane's 16 bytes of a key, as they come from the page, are its operands of two products: keys go from HBM to registers
+// and never through shared memory, while the queries of a (session, head) stay in registers.  The exponentials of a tile's columns are summed in a fixed
+// order by the lanes that share a position, and one lane adds the sum to the weight: the same call gives the same bits.
+// All (session, head, tile) form one sequence, cut into equal ranges, one a warp.
+#include <cuda_bf16.h>
+#include <math.h>
+
+#include "plc_pages.cuh"
+
+namespace plc {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896f;
+
+struct WeighArgs {
+    const uint16_t* q; int64_t qs_row, qs_head;   // elements
+    const float* lse; const int32_t* rows; const int32_t* begin;
+    int n_list, n_rows, heads, group, layer;
+    float* weight; int64_t ws_row, ws_head; int n_pos;
+    float decay, scale;
+};
+
+// A session as the call gives it, cut to what there is: entries first .. first + n - 1 of the list stand at its last n positions.
+struct Session { int first, n, len; };
+__device__ __forceinline__ Session session_of(const PoolDev& p, const BookDev& b, const WeighArgs& a, int s, bool* bad) {
+    const int b0 = a.begin[s], b1 = a.begin[s + 1], len = b.len[s], most = most_positions(b, p);
+    Session x;
+    x.first = min(max(b0, 0), a.n_list);
+    x.n = min(max(b1, x.first), a.n_list) - x.first;
+    x.len = x.n > 0 ? min(max(len, 0), most) : 0;
+    *bad = b0 < 0 || b1 < b0 || b1 > a.n_list || len < 0 || len > most || x.n > len;
+    return x;
+}
+
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+template <class T> __device__ __forceinline__ void mma16816(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
+template <> __device__ __forceinline__ void mma16816<__half>(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+constexpr int kThreads = 128, kWarps = kThreads / 32, kTile = 16;
+
+// Row tiles of eight columns (a column: an entry's query head).
+template <class T, int D>
+__global__ void __launch_bounds__(kThreads) weigh_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b, const __grid_constant__ WeighArgs a,
+                                                         uint32_t* status) {
+    constexpr int B = D / 32;                     // 32-component blocks of a vector
+    __shared__ long long upto_s[kThreads];
+    __shared__ long long warp_sum_s[kWarps];
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    // tiles of the sessions: a thread sums a run of them, the threads' sums are scanned
+    const int run = (b.rows + kThreads - 1) / kThreads, first_s = min(b.rows, tid * run), last_s = min(b.rows, first_s + run);
+    auto tiles_of = [&](int s, bool* bad) -> long long { return (long long)((session_of(p, b, a, s, bad).len + kTile - 1) / kTile) * p.H; };
+    long long mine = 0;
+    bool any_bad = false;
+    for (int s = first_s; s < last_s; ++s) {
+        bool bad;
+        mine += tiles_of(s, &bad);
+        any_bad |= bad;
+    }
+    if (any_bad && blockIdx.x == 0) atomicOr(status, kStRange);
+    long long upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(kFull, upto, o);
+        if (lane >= o) upto += v;
+    }
+    if (lane == 31) warp_sum_s[wid] = upto;
+    __syncthreads();
+    long long total = 0;
+    for (int w = 0; w < kWarps; ++w) {
+        if (w < wid) upto += warp_sum_s[w];
+        total += warp_sum_s[w];
+    }
+    upto_s[tid] = upto;
+    __syncthreads();
+    const long long workers = min((long long)gridDim.x * kWarps, total), me = (long long)blockIdx.x * kWarps + wid;
+    if (me >= workers) return;
+    const long long t0 = total * me / workers, t1 = total * (me + 1) / workers;
+    int s = 0;
+    long long rest = t0;
+    {
+        int j = 0;
+        while (upto_s[j] <= t0) ++j;
+        rest -= j ? upto_s[j - 1] : 0;
+        s = j * run;
+        bool bad;
+        for (;; ++s) {
+            const long long f = tiles_of(s, &bad);
+            if (rest < f) break;
+            rest -= f;
+        }
+    }
+    long long left = t1 - t0;
+    bool bad;
+    Session x = session_of(p, b, a, s, &bad);
+    int tiles = (x.len + kTile - 1) / kTile, h = (int)(rest / tiles), tile = (int)(rest - (long long)h * tiles);
+    const int quad = lane >> 2, part = lane & 3;
+    const float c2 = a.scale * kLog2e;
+    while (left > 0) {
+        const int todo = (int)min(left, (long long)(tiles - tile));
+        const int cols = x.n * a.group;
+        for (int i = 0; i < todo; ++i) {
+            const int base = (tile + i) * kTile, t_mine = base + (lane & 15);
+            int page = -1;
+            if (t_mine < x.len) {
+                page = b.table[(int64_t)s * b.max_pages + t_mine / p.page_pos];
+                if (page < 0 || page >= p.n_pages) { page = -1; atomicOr(status, kStRange); }
+            }
+            const int64_t off = page < 0 ? -1 : (int64_t)a.layer * p.sl + (int64_t)page * p.spage + (int64_t)(t_mine % p.page_pos) * p.sp + (int64_t)h * p.sh;
+            const int64_t off0 = __shfl_sync(kFull, off, quad), off1 = __shfl_sync(kFull, off, quad + 8);
+            uint4 k0[B], k1[B];
+#pragma unroll
+            for (int e = 0; e < B; ++e) {
+                k0[e] = off0 < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(p.base + off0 + e * 64 + part * 16);
+                k1[e] = off1 < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(p.base + off1 + e * 64 + part * 16);
+            }
+            float sum0 = 0.f, sum1 = 0.f;
+            const int seen0 = base + quad - (x.len - x.n), seen1 = seen0 + 8;             // entries from this one on see the position
+            for (int col0 = 0; col0 < cols; col0 += 8) {
+                float acc[4] = {0.f, 0.f, 0.f, 0.f};
+                const int col = col0 + quad, entry = col / a.group;
+                int row = -1;
+                if (col < cols) row = a.rows ? a.rows[x.first + entry] : x.first + entry;
+                if (row < -1 || row >= a.n_rows) { atomicOr(status, kStRange); row = -1; }
+                const int head = h * a.group + col - entry * a.group;
+                const uint16_t* q = a.q + (int64_t)max(row, 0) * a.qs_row + (int64_t)head * a.qs_head + part * 8;
+                const float l_mine = row < 0 ? INFINITY : a.lse[(int64_t)row * a.heads + head] * kLog2e;
+#pragma unroll
+                for (int e = 0; e < B; ++e) {
+                    const uint4 v = row < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(q + e * 32);
+                    mma16816<T>(acc, k0[e].x, k1[e].x, k0[e].y, k1[e].y, v.x, v.y);
+                    mma16816<T>(acc, k0[e].z, k1[e].z, k0[e].w, k1[e].w, v.z, v.w);
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {     // columns 2 part + j
+                    const float l = __shfl_sync(kFull, l_mine, (2 * part + j) * 4);
+                    const int en = __shfl_sync(kFull, entry, (2 * part + j) * 4);
+                    const bool dead = isinf(l);
+                    sum0 += dead || en < seen0 ? 0.f : exp2_approx(fmaf(acc[j], c2, -l));
+                    sum1 += dead || en < seen1 ? 0.f : exp2_approx(fmaf(acc[2 + j], c2, -l));
+                }
+            }
+            sum0 += __shfl_xor_sync(kFull, sum0, 1);
+            sum1 += __shfl_xor_sync(kFull, sum1, 1);
+            sum0 += __shfl_xor_sync(kFull, sum0, 2);
+            sum1 += __shfl_xor_sync(kFull, sum1, 2);
+            const int t = base + quad + 8 * part;
+            if (part < 2 && t < x.len) {
+                if (t >= a.n_pos) atomicOr(status, kStCapacity);
+                else {
+                    float* w = a.weight + (int64_t)s * a.ws_row + (int64_t)h * a.ws_head + t;
+                    const bool there = (part ? off1 : off0) >= 0;
+                    const float old = t < x.len - x.n && a.decay != 0.f ? *w * a.decay : 0.f;
+                    *w = there ? old + (part ? sum1 : sum0) : old;
+                }
+            }
+        }
+        left -= todo;
+        tile = 0;
+        if (left > 0 && ++h == p.H) {
+            h = 0;
+            do x = session_of(p, b, a, ++s, &bad);
+            while (x.len == 0);
+            tiles = (x.len + kTile - 1) / kTile;
+        }
+    }
+}
+
+template <class T>
+cudaError_t launch_weigh(const PoolDev& p, const BookDev& b, const WeighArgs& a, uint32_t* status, cudaStream_t st) {
+    const unsigned grid = 4u * sm_count();
+    switch (p.d) {
+        case 32: return launch_kernel(weigh_kernel<T, 32>, grid, kThreads, 0, st, false, 1, p, b, a, status);
+        case 64: return launch_kernel(weigh_kernel<T, 64>, grid, kThreads, 0, st, false, 1, p, b, a, status);
+        case 128: return launch_kernel(weigh_kernel<T, 128>, grid, kThreads, 0, st, false, 1, p, b, a, status);
+        default: return launch_kernel(weigh_kernel<T, 256>, grid, kThreads, 0, st, false, 1, p, b, a, status);
+    }
+}
+
+}  // namespace
+}  // namespace plc
+
+using namespace plc;
+
+extern "C" {
+
+plc_status plc_pages_weigh(const plc_page_pool* pool, int32_t layer, const plc_page_book* book, const plc_weigh_queries* t, float scale, float decay,
+                           const plc_weights* weights, uint32_t* status_dev, void* stream) {
+    PoolDev p;
+    BookDev b;
+    plc_status rc = check_pool(pool, &p);
+    if (rc || (rc = check_book(book, &b))) return rc;
+    if (!t || !t->q_dev || !t->lse_dev || !t->begin_dev || t->n_rows < 0 || t->n_list < 0 || !weights || !weights->base_dev || !status_dev) return PLC_E_INVALID;
+    if (layer < 0 || layer >= p.L || pool->dtype == PLC_OUT_F32 || !(scale > 0.f) || isinf(scale) || !isfinite(decay) || decay < 0.f) return PLC_E_INVALID;
+    if (t->n_heads < 1 || weights->n_pos < 1) return PLC_E_INVALID;
+    if (t->n_heads % p.H || t->n_heads > (1 << 16) || (!t->rows_dev && t->n_list > t->n_rows)) return PLC_E_SHAPE;
+    const int group = t->n_heads / p.H;
+    if ((long long)t->n_list * group > (1 << 30)) return PLC_E_SHAPE;
+    if (!plc_aligned16(t->q_dev) || t->q_stride_row % 8 || t->q_stride_head % 8 || (reinterpret_cast<uintptr_t>(weights->base_dev) & 3)) return PLC_E_ALIGN;
+    if (t->n_list == 0) return PLC_OK;
+    const WeighArgs a{static_cast<const uint16_t*>(t->q_dev), t->q_stride_row, t->q_stride_head, t->lse_dev, t->rows_dev, t->begin_dev, t->n_list, t->n_rows, t->n_heads,
+                      group, layer, weights->base_dev + (int64_t)layer * weights->stride_layer, weights->stride_row, weights->stride_head, weights->n_pos, decay, scale};
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if ((pool->dtype == PLC_OUT_F16 ? launch_weigh<__half>(p, b, a, status_dev, st) : launch_weigh<__nv_bfloat16>(p, b, a, status_dev, st)) != cudaSuccess) return PLC_E_CUDA;
+    count_launch(1);
+    return PLC_OK;
+}
+
+}  // extern "C"

@@ -1,11 +1,12 @@
-"""Paged KV cache, attention of drafted tokens over it, and beam search: binding of the plc_pages_*, plc_tree_attention
-and plc_beam_* calls.
+"""Paged KV cache, attention of drafted tokens over it, beam search, rotary positions, eviction and log probabilities: binding of
+the plc_pages_*, plc_tree_attention, plc_beam_*, plc_rotary_* and plc_token_logprobs calls.
 
 As in the rest of the binding nothing is computed here: tensors become pointers, and the work runs on the current stream
 of the tensors' device.  Results and workspaces are allocated by torch on that stream, so that calls on several streams
 and captured graphs do not share any.
 """
 import ctypes as C
+import math
 
 from . import E_ALIGN, E_CAPACITY, E_CUDA, E_INVALID, E_SHAPE, OUT_BF16, OUT_F16, OUT_F32, KVView, PlcError, PoolView, _check, lib
 
@@ -27,6 +28,31 @@ class TreeQueries(C.Structure):
 
 class RowSet(C.Structure):
     _fields_ = [("src_dev", C.c_void_p), ("dst_dev", C.c_void_p), ("src_stride", C.c_int64), ("dst_stride", C.c_int64), ("row_bytes", C.c_int64)]
+
+
+class RotaryC(C.Structure):
+    _fields_ = [("turns_dev", C.c_void_p), ("dim", C.c_int32), ("interleaved", C.c_int32), ("scale", C.c_float)]
+
+
+class RotarySet(C.Structure):
+    _fields_ = [("x_dev", C.c_void_p), ("out_dev", C.c_void_p), ("x_stride_row", C.c_int64), ("x_stride_head", C.c_int64), ("out_stride_row", C.c_int64),
+                ("out_stride_head", C.c_int64), ("heads", C.c_int32)]
+
+
+class NewTokens(C.Structure):
+    _fields_ = [("q_dev", C.c_void_p), ("q_stride_row", C.c_int64), ("q_stride_head", C.c_int64), ("out_dev", C.c_void_p), ("out_stride_row", C.c_int64),
+                ("out_stride_head", C.c_int64), ("k_dev", C.c_void_p), ("k_stride_row", C.c_int64), ("k_stride_head", C.c_int64), ("v_dev", C.c_void_p),
+                ("v_stride_row", C.c_int64), ("v_stride_head", C.c_int64), ("begin_dev", C.c_void_p), ("pos_dev", C.c_void_p), ("n_rows", C.c_int32),
+                ("n_heads", C.c_int32)]
+
+
+class Weights(C.Structure):
+    _fields_ = [("base_dev", C.c_void_p), ("stride_row", C.c_int64), ("stride_layer", C.c_int64), ("stride_head", C.c_int64), ("n_pos", C.c_int32)]
+
+
+class WeighQueries(C.Structure):
+    _fields_ = [("q_dev", C.c_void_p), ("q_stride_row", C.c_int64), ("q_stride_head", C.c_int64), ("lse_dev", C.c_void_p), ("rows_dev", C.c_void_p),
+                ("begin_dev", C.c_void_p), ("n_rows", C.c_int32), ("n_list", C.c_int32), ("n_heads", C.c_int32)]
 
 
 def _need(ok, code, where):
@@ -54,7 +80,10 @@ def _lib():
                             ("plc_pages_compact", [P, P, P, P, P, U, P, P]), ("plc_pages_workspace", [I, I, I, P]), ("plc_take_status", [P, P, P]),
                             ("plc_tree_attention", [P, I, P, P, F, P, U, P, P]), ("plc_tree_attention_workspace", [P, I, I, I, P]),
                             ("plc_beam_select", [P, I, L, I, I, I, P, P, I, I, P, P, P, P, U, P]), ("plc_beam_workspace", [I, I, I, I, P]),
-                            ("plc_beam_reorder", [P, I, P, I, I, P, P])):
+                            ("plc_beam_reorder", [P, I, P, I, I, P, P]), ("plc_rotary_apply", [P, P, I, P, I, I, I, I, P]), ("plc_pages_append", [P, I, P, P, P, P, P]),
+                            ("plc_pages_weigh", [P, I, P, P, F, F, P, P, P]), ("plc_pages_evict", [P, P, P, P, I, I, P, P, P, U, P, P]),
+                            ("plc_pages_evict_workspace", [P, I, I, P]), ("plc_token_logprobs", [P, I, L, I, I, P, I, I, P, P, P, P, P, U, P, P]),
+                            ("plc_token_logprobs_workspace", [I, I, I, P])):
             getattr(api, name).argtypes = types
         _api = api
     return _api
@@ -289,6 +318,114 @@ class PagePool:
         _check(_run(dev, api.plc_tree_attention, self._by, layer, a, C.byref(t), d ** -0.5 if scale is None else scale, ws.data_ptr(), need, self._word), where)
         return out, lse
 
+    def append(self, layer, book, q, k, v, begin, rotary=None, pos=None, out=None):
+        """Writes the new tokens' keys k, turned by `rotary` (None: as they are), and values v [N][kv heads][d] into the layer's pages behind their
+        sessions' lengths, and returns the turned queries q [N][heads][d] (q None: None).  Session s has the rows begin[s] .. begin[s+1]-1.  pos [N] int32: the
+        positions that they turn by (drafted trees: their depths; after evictions), len + i if not given.  out: where the queries go, q itself is allowed.
+        The book stays as it is; keep counts the tokens in."""
+        import torch
+        where, dev, api = "plc_pages_append", self.device, _lib()
+        a = self._book(book, where)
+        H, d = self._c.n_kv_heads, self._c.head_dim
+        N = k.shape[0]
+        for t in (k, v):
+            _need(t.dim() == 3 and t.shape == (N, H, d), E_SHAPE, where)
+            _need(t.device == dev and t.dtype == self.kv.dtype and t.stride(2) == 1, E_INVALID, where)
+        _int32(E_INVALID, where, layer)
+        _int32(E_SHAPE, where, N)
+        _need(_i32(begin, dev, where).numel() == book.rows + 1, E_SHAPE, where)
+        if pos is not None:
+            _need(_i32(pos, dev, where).numel() == N, E_SHAPE, where)
+        heads, queries = 0, (None, 0, 0, None, 0, 0)
+        if q is not None:
+            _need(q.dim() == 3 and q.shape[0] == N and q.shape[2] == d and q.shape[1] > 0, E_SHAPE, where)
+            _need(q.device == dev and q.dtype == self.kv.dtype and q.stride(2) == 1, E_INVALID, where)
+            heads = q.shape[1]
+            _int32(E_SHAPE, where, heads)
+            if out is None:
+                out = torch.empty((N, heads, d), dtype=q.dtype, device=dev)
+            else:
+                _need(out.shape == q.shape and out.dtype == q.dtype and out.device == dev and out.stride(2) == 1, E_INVALID, where)
+            queries = (q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0), out.stride(1))
+        else:
+            _need(out is None, E_INVALID, where)
+        by = None
+        if rotary is not None:
+            _need(rotary.device == dev, E_INVALID, where)
+            by = rotary._by
+        if N == 0:
+            return out
+        t = NewTokens(*queries, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), begin.data_ptr(),
+                      None if pos is None else pos.data_ptr(), N, heads)
+        _check(_run(dev, api.plc_pages_append, self._by, layer, a, by, C.byref(t), self._word), where)
+        return out
+
+    def new_weights(self, rows, n_pos):
+        """Weights of empty rows: [rows][layers][kv heads][n_pos] float32, rows first, so that they follow beams through beam_reorder."""
+        import torch
+        return torch.zeros((rows, self._c.n_layers, self._c.n_kv_heads, n_pos), dtype=torch.float32, device=self.device)
+
+    def _weights(self, weight, book, where):
+        import torch
+        _need(weight.dim() == 4 and weight.shape[:3] == (book.rows, self._c.n_layers, self._c.n_kv_heads), E_SHAPE, where)
+        _need(weight.dtype == torch.float32 and weight.device == self.device and (weight.stride(3) == 1 or weight.shape[3] == 1), E_INVALID, where)
+        _int32(E_SHAPE, where, weight.shape[3])
+        row, layer, head, _ = weight.stride()
+        return Weights(weight.data_ptr(), row, layer, head, weight.shape[3])
+
+    def attention_weights(self, layer, book, q, lse, begin, weight, rows=None, scale=None, decay=1.0):
+        """Adds to weight [rows][layers][kv heads][positions] (in place, and returned) what the layer's positions receive from the sessions' newest tokens:
+        weight = decay * weight + sum of exp(scale q.k - lse).  q [N][heads][d] and lse [N][heads] as tree_attention had and left them.  Session s has the
+        entries begin[s] .. begin[s+1]-1, which stand at its last positions (the book after keep); entry e is row e of q and lse, or row rows[e] (int32; -1: none):
+        the accepted ones of a draft.  decay 0: nothing of the old weights is read."""
+        where, dev, api = "plc_pages_weigh", self.device, _lib()
+        a = self._book(book, where)
+        _need(q.dim() == 3, E_SHAPE, where)
+        (N, heads, d), (row, head, one) = q.shape, q.stride()
+        _need(d == self._c.head_dim and lse.shape == (N, heads), E_SHAPE, where)
+        _int32(E_INVALID, where, layer)
+        _int32(E_SHAPE, where, N, heads)
+        _need(q.device == dev and q.dtype == self.kv.dtype and one == 1, E_INVALID, where)
+        _kind(q.dtype, where, wide=False)
+        _need(lse.dtype.itemsize == 4 and lse.is_floating_point() and lse.device == dev and lse.is_contiguous(), E_INVALID, where)
+        _need(_i32(begin, dev, where).numel() == book.rows + 1, E_SHAPE, where)
+        n_list = N if rows is None else _i32(rows, dev, where).numel()
+        _int32(E_SHAPE, where, n_list)
+        w = self._weights(weight, book, where)
+        if n_list == 0:
+            return weight
+        t = WeighQueries(q.data_ptr(), row, head, lse.data_ptr(), None if rows is None else rows.data_ptr(), begin.data_ptr(), N, n_list, heads)
+        _check(_run(dev, api.plc_pages_weigh, self._by, layer, a, C.byref(t), d ** -0.5 if scale is None else scale, decay, C.byref(w), self._word), where)
+        return weight
+
+    def evict(self, book, weight, budget, recent=0):
+        """(new book, new weights): rows longer than `budget` (an int, or int32 [rows] on the device, negative: the row stays) keep, in every layer and head by
+        itself, their last `recent` positions and those of the largest weights; what is kept moves together.  Tokens appended later turn by
+        positions of their own (append's pos): len no longer counts what was evicted."""
+        import torch
+        where, dev, api = "plc_pages_evict", self.device, _lib()
+        a = self._book(book, where)
+        w = self._weights(weight, book, where)
+        _int32(E_INVALID, where, recent)
+        budgets = None
+        if torch.is_tensor(budget):
+            _need(_i32(budget, dev, where).numel() == book.rows, E_SHAPE, where)
+            budgets, budget = budget.data_ptr(), 0
+        _int32(E_INVALID, where, budget)
+        n_pos = weight.shape[3]
+        need = self._need_bytes.get((book.rows, n_pos))
+        if need is None:
+            b = C.c_uint64()
+            _check(api.plc_pages_evict_workspace(self._by, book.rows, n_pos, C.byref(b)), "plc_pages_evict_workspace")
+            if len(self._need_bytes) >= 4096:
+                self._need_bytes.clear()
+            need = self._need_bytes[(book.rows, n_pos)] = b.value
+        new, _ = PageBook._new(book.rows, book.max_pages, self.n_pages, dev)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        out = torch.empty(weight.shape, dtype=torch.float32, device=dev)
+        _check(_run(dev, api.plc_pages_evict, self._by, a, C.byref(w), budgets, budget, recent, new._by, out.data_ptr(), ws.data_ptr(), need, self._word), where)
+        return new, out
+
     def check(self):
         """Waits for the current stream's work and raises where a call has found something wrong on the device; clears the word.
         What a call that still runs on another stream finds stays there for the next check."""
@@ -352,3 +489,110 @@ def beam_reorder(parent, states, status=None):
         some = sets[i:i + 80]
         _check(_run(dev, api.plc_beam_reorder, (C.c_int64 * len(some))(*some), len(some) // 5, parent.data_ptr(), rows_in, rows, word), where)
     return out
+
+
+class Rotary:
+    """Rotary positions: pair i of `dim` components turns by a frequency f_i a position, pairs being (i, i + dim/2), or neighbours where `interleaved`.
+    f_i = base ** (-2 i / dim), stretched for contexts longer than the trained one by `ramp`:
+
+      "none"   as they are
+      "all"    f / factor
+      "base"   base * factor ** (dim / (dim - 2)) in place of base
+      "turns"  pairs that turn at least `fast` times over `context` positions stay, those that turn at most `slow` times are divided by factor, between them
+               blended linearly in the number of turns
+      "index"  the same, blended linearly in the pair's number, between those (rounded outwards) that turn `fast` and `slow` times
+
+    scale multiplies what turns.  frequencies: dim/2 numbers in radians a position, in place of all of these."""
+
+    def __init__(self, dim, base=10000.0, interleaved=False, ramp="none", factor=1.0, context=None, slow=1.0, fast=32.0, scale=1.0, frequencies=None, device="cuda"):
+        import torch
+        where = "Rotary"
+        _need(dim >= 2 and dim % 2 == 0, E_SHAPE, where)
+        f = rotary_frequencies(dim, base, ramp, factor, context, slow, fast) if frequencies is None else [float(x) for x in frequencies]
+        _need(len(f) == dim // 2, E_SHAPE, where)
+        _need(math.isfinite(scale), E_INVALID, where)
+        turns = (C.c_uint64 * len(f))()
+        _check(_lib().plc_rotary_turns((C.c_double * len(f))(*f), len(f), turns), "plc_rotary_turns")
+        signed = [x - (1 << 64) if x >> 63 else x for x in turns]
+        self.dim, self.interleaved, self.scale, self.frequencies = dim, bool(interleaved), float(scale), f
+        self.turns = torch.tensor(signed, dtype=torch.int64).to(device)
+        self.device = self.turns.device
+        self._c = RotaryC(self.turns.data_ptr(), dim, int(self.interleaved), self.scale)
+        self._by = C.byref(self._c)
+
+    def apply(self, x, pos, back=False, out=None):
+        """x [N][heads][d], or up to four of them (queries and keys, any strides with the components contiguous), turned at positions pos [N] (int32);
+        back: by the opposite angles, the gradient.  out: where the results go, x itself is allowed."""
+        import torch
+        where, dev, api = "plc_rotary_apply", self.device, _lib()
+        xs = (x,) if torch.is_tensor(x) else tuple(x)
+        outs = (None,) * len(xs) if out is None else (out,) if torch.is_tensor(out) else tuple(out)
+        _need(len(xs) >= 1, E_INVALID, where)
+        _need(len(xs) <= 4 and len(outs) == len(xs), E_SHAPE, where)
+        N, d, kind = _i32(pos, dev, where).numel(), xs[0].shape[-1] if xs[0].dim() == 3 else 0, _kind(xs[0].dtype, where)
+        _int32(E_SHAPE, where, N)
+        sets, got = (RotarySet * len(xs))(), []
+        for i, (t, o) in enumerate(zip(xs, outs)):
+            _need(t.dim() == 3 and t.shape[0] == N and t.shape[2] == d, E_SHAPE, where)
+            _need(t.device == dev and t.dtype == xs[0].dtype and t.stride(2) == 1, E_INVALID, where)
+            if o is None:
+                o = torch.empty(t.shape, dtype=t.dtype, device=dev)
+            else:
+                _need(o.shape == t.shape and o.dtype == t.dtype and o.device == dev and o.stride(2) == 1, E_INVALID, where)
+            got.append(o)
+            _int32(E_SHAPE, where, t.shape[1])
+            sets[i] = RotarySet(t.data_ptr(), o.data_ptr(), t.stride(0), t.stride(1), o.stride(0), o.stride(1), t.shape[1])
+        if N:
+            _check(_run(dev, api.plc_rotary_apply, self._by, sets, len(xs), pos.data_ptr(), N, d, kind, int(back)), where)
+        return got[0] if torch.is_tensor(x) else tuple(got)
+
+
+def rotary_frequencies(dim, base=10000.0, ramp="none", factor=1.0, context=None, slow=1.0, fast=32.0):
+    """The dim/2 frequencies of Rotary, in radians a position."""
+    where = "rotary_frequencies"
+    _need(ramp in ("none", "all", "base", "turns", "index") and base > 0 and factor > 0, E_INVALID, where)
+    if ramp == "base":
+        _need(dim > 2, E_SHAPE, where)
+        base *= factor ** (dim / (dim - 2))
+    f = [base ** (-2.0 * i / dim) for i in range(dim // 2)]
+    if ramp == "all":
+        return [x / factor for x in f]
+    if ramp in ("none", "base"):
+        return f
+    _need(context is not None and context > 0 and 0 < slow < fast, E_INVALID, where)
+    if ramp == "turns":
+        keep = [(context * x / (2 * math.pi) - slow) / (fast - slow) for x in f]
+    else:
+        _need(base > 1, E_INVALID, where)
+        lo, hi = (dim * math.log(context / (2 * math.pi * x)) / (2 * math.log(base)) for x in (fast, slow))
+        lo, hi = max(math.floor(lo), 0), min(math.ceil(hi), dim - 1)
+        keep = [1 - (i - lo) / max(hi - lo, 0.001) for i in range(dim // 2)]
+    keep = [min(max(g, 0.0), 1.0) for g in keep]
+    return [g * x + (1 - g) * x / factor for g, x in zip(keep, f)]
+
+
+def token_logprobs(logits, tokens, n_top=0, status=None):
+    """(logp, entropy, top_logp, top_token) of rows of logits [N][vocab]: the log probabilities [N][m] of tokens [N][m] (or [N]; int32, -1: none, 0),
+    the rows' entropies [N] in nats, and the n_top likeliest tokens [N][n_top] with their log probabilities.  status: int32 word that receives 32 for a token
+    out of range."""
+    import torch
+    where, dev, api = "plc_token_logprobs", logits.device, _lib()
+    _need(logits.is_cuda and logits.dim() == 2, E_INVALID, where)
+    (N, V), (row, one) = logits.shape, logits.stride()
+    _need(one == 1 or V == 1, E_INVALID, where)
+    _need(_i32(tokens, dev, where).dim() in (1, 2) and tokens.shape[0] == N, E_SHAPE, where)
+    m = 1 if tokens.dim() == 1 else tokens.shape[1]
+    _int32(E_SHAPE, where, N, V, m, n_top)
+    _need(n_top >= 0, E_INVALID, where)
+    word = None if status is None else _i32(status, dev, where).data_ptr()
+    kind = _kind(logits.dtype, where)
+    logp = torch.empty(tokens.shape, dtype=torch.float32, device=dev)
+    entropy = torch.empty(N, dtype=torch.float32, device=dev)
+    top_logp = torch.empty((N, n_top), dtype=torch.float32, device=dev)
+    top_token = torch.empty((N, n_top), dtype=torch.int32, device=dev)
+    if N:
+        need = _bytes(dev, api.plc_token_logprobs_workspace, N, V, n_top)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        _check(_run(dev, api.plc_token_logprobs, logits.data_ptr(), kind, row, N, V, tokens.data_ptr(), m, n_top, logp.data_ptr(), entropy.data_ptr(), top_logp.data_ptr(),
+                    top_token.data_ptr(), ws.data_ptr(), need, word), where)
+    return logp, entropy, top_logp, top_token

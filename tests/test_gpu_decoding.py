@@ -1,0 +1,744 @@
+"""Rotary positions, the append to pages, attention weights, eviction and log probabilities on the GPU against the oracle's literal definitions (binary64).
+
+Tolerances, with u = half a step of the type (relative).
+  * A turn: the angle is off by half a step of a binary32 number up to 2^31 units of 2^-31 half turns (2^-25 half turns, below 2^-23) and the functions by
+    2^-23, so that cosine and sine are off by at most 2^-22; two products and a sum of binary32: |y - exact| <= 2^-21 scale (|x_a| + |x_b|), and the
+    rounding of the result, u |exact| and half the smallest step.  The oracle's own angle, pos f in binary64, is off by 2^-53 pos f, below 2^-22 for the
+    positions here (|pos| < 2^30).
+  * Weights: a score is a sum of d binary32 products, off by d 2^-23 of the sum of |q k| scale =: B; the exponent c s - l (three roundings of binary32) is off by
+    2^-23 (B + |lse|) more at most, the exponential by 2^-22; the sum over n G terms and the old weight by (n G + 2) 2^-24 of the whole.
+  * Log probabilities, with m1, m2 the mean and mean square of the distance y to the row's largest logit: an exponential is off by 2^-22 + 2^-23 y, a sum of 32 by 2^-20,
+    so the logarithm of the sum by 2^-20 + 2^-23 m1, the mean distance by 2^-20 (1 + m1 + m2) and as much again from the normaliser; the result is rounded.
+What moves or is copied is equal bit for bit; books, counts, tokens are equal.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2604_15356_b200 as plc
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    plc.build()
+    return torch.device("cuda:0")
+
+
+@pytest.fixture(scope="module")
+def ora():
+    from oracle import serving
+    return serving
+
+
+def i32(v, dev):
+    return torch.as_tensor(np.asarray(v), dtype=torch.int32).to(dev)
+
+
+def normal(rng, shape, dtype):
+    return torch.from_numpy(rng.standard_normal(shape).astype(np.float32)).to(TYPES[dtype])
+
+
+def wide(x):
+    return x.double().cpu().numpy()
+
+
+def turn_tolerance(x, exact, dim, inter, scale, dtype):
+    """Of each component: its pair's magnitudes."""
+    m, t = np.abs(x), np.zeros(x.shape)
+    if inter:
+        pair = m[..., 0:dim:2] + m[..., 1:dim:2]
+        t[..., 0:dim:2] = t[..., 1:dim:2] = pair
+    else:
+        pair = m[..., :dim // 2] + m[..., dim // 2:dim]
+        t[..., :dim // 2] = t[..., dim // 2:dim] = pair
+    f = torch.finfo(TYPES[dtype])
+    return 2.0 ** -21 * abs(scale) * t + f.eps / 2 * np.abs(exact) * (t > 0) + f.smallest_normal * f.eps / 2
+
+
+# ---------------------------------------------------------------------------------------------- rotary
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("N, heads, d, dim", [(1, (1,), 64, 64), (3, (5, 1), 128, 128), (37, (8, 2), 96, 48), (2, (3, 2, 1, 1), 80, 20), (5, (2,), 34, 6), (700, (4, 1), 64, 32),
+                                              (1300, (1,), 32, 32), (4, (2, 2), 256, 256), (2, (1,), 2, 2)])
+def test_turns(dev, ora, dtype, inter, N, heads, d, dim):
+    """Several sets in a call, part of the head, vectors that are and are not runs of 16 bytes; forwards, back and onto itself."""
+    rng = np.random.default_rng(N * d + dim)
+    rot = plc.Rotary(dim, base=500.0, interleaved=inter, scale=1.25)
+    xs = [normal(rng, (N, h, d), dtype) for h in heads]
+    pos = rng.integers(-(1 << 30), 1 << 30, N)
+    pos[:2] = (0, 5)[:min(N, 2)]
+    on = tuple(x.to(dev) for x in xs)
+    for back in (False, True):
+        got = rot.apply(on, i32(pos, dev), back=back)
+        for x, g in zip(xs, got):
+            ex = ora.rotary(wide(x), pos, rot.frequencies, inter, 1.25, back)
+            off = np.abs(wide(g) - ex)
+            assert (off <= turn_tolerance(wide(x), ex, dim, inter, 1.25, dtype)).all(), off.max()
+            assert torch.equal(g[..., dim:].cpu(), x[..., dim:])
+    mine = tuple(x.clone() for x in on)
+    again = rot.apply(mine, i32(pos, dev), back=True, out=mine)
+    assert all(a.data_ptr() == m.data_ptr() and torch.equal(a, g) for a, m, g in zip(again, mine, got))
+
+
+@pytest.mark.parametrize("ramp, more", [("none", {}), ("all", dict(factor=4.0)), ("base", dict(factor=8.0)), ("turns", dict(factor=8.0, context=8192, slow=1.0, fast=4.0)),
+                                        ("index", dict(factor=16.0, context=4096))])
+def test_turns_of_long_contexts(dev, ora, ramp, more):
+    rng = np.random.default_rng(5)
+    rot = plc.Rotary(128, base=500000.0, ramp=ramp, **more)
+    x = normal(rng, (6, 2, 128), "f32")
+    pos = np.array([0, 1, 8191, 131071, (1 << 20) + 1, (1 << 30) - 1])
+    ex = ora.rotary(wide(x), pos, rot.frequencies)
+    got = wide(rot.apply(x.to(dev), i32(pos, dev)))
+    assert (np.abs(got - ex) <= turn_tolerance(wide(x), ex, 128, False, 1.0, "f32")).all()
+
+
+def test_turns_at_the_ends_of_the_positions(dev):
+    """int32's lowest and highest positions: exact arithmetic on a frequency that is a fraction of a turn."""
+    f = 2 * math.pi * 0.25                                       # just off a quarter turn a position, as the binary64 number is
+    rot = plc.Rotary(2, frequencies=[f])
+    pos = np.array([-(1 << 31), -(1 << 31) + 1, -1, 0, 1, 2, (1 << 31) - 1])
+    x = torch.tensor([1.0, 0.0], device=dev).expand(len(pos), 1, 2).contiguous()
+    y = rot.apply(x, i32(pos, dev)).cpu()[:, 0]
+    want = np.array([[round(math.cos(math.pi / 2 * (int(p) % 4))), round(math.sin(math.pi / 2 * (int(p) % 4)))] for p in pos])
+    assert np.abs(y.numpy() - want).max() < 2.0 ** -20
+
+
+def test_turns_are_the_gradient_of_each_other(dev):
+    """back is the transpose, scale included: checked against autograd of the formula and by differences."""
+    rng = np.random.default_rng(6)
+    for inter in (False, True):
+        rot = plc.Rotary(32, base=100.0, interleaved=inter, scale=0.75)
+        x, g, pos = normal(rng, (7, 3, 48), "f32").to(dev), normal(rng, (7, 3, 48), "f32").to(dev), i32(np.arange(7) * 3 - 4, dev)
+        xd = x.double().requires_grad_()
+        t = pos.double()[:, None] * torch.tensor(rot.frequencies, dtype=torch.float64, device=dev)
+        a, b = (xd[..., 0:32:2], xd[..., 1:32:2]) if inter else (xd[..., :16], xd[..., 16:32])
+        c, s = 0.75 * t.cos()[:, None], 0.75 * t.sin()[:, None]
+        ya, yb = a * c - b * s, b * c + a * s
+        y = torch.cat((torch.stack((ya, yb), -1).flatten(-2) if inter else torch.cat((ya, yb), -1), xd[..., 32:]), -1)
+        want, = torch.autograd.grad(y, xd, g.double())
+        got = rot.apply(g, pos, back=True)
+        tol = torch.from_numpy(turn_tolerance(wide(g), wide(want), 32, inter, 0.75, "f32")).to(dev)
+        assert bool(((got.double() - want).abs() <= tol).all())
+        step = torch.zeros_like(x)
+        step[3, 1, 5] = 0.5                                      # the turn is linear: a difference is exact but for rounding
+        diff = ((rot.apply(x + step, pos) - rot.apply(x - step, pos)).double() * g.double()).sum()
+        assert abs(float(diff - got[3, 1, 5])) < 2.0 ** -17
+
+
+def test_turns_strided_slices(dev):
+    """Slices of a fused projection as they stand, into slices, rows far apart; a stream other than the default one."""
+    rng = np.random.default_rng(7)
+    rot = plc.Rotary(64)
+    both = normal(rng, (9, 12, 64), "bf16").to(dev)
+    pos = i32(np.arange(9), dev)
+    want = rot.apply(both.contiguous(), pos)
+    q, k = both[:, :7], both[:, 7:9]
+    to = torch.full((9, 20, 72), 3.0, dtype=torch.bfloat16, device=dev)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        rot.apply((q, k), pos, out=(to[:, 2:9, 8:], to[:, 9:11, 8:]))
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(to[:, 2:9, 8:], want[:, :7]) and torch.equal(to[:, 9:11, 8:], want[:, 7:9])
+    assert bool((to[:, :2] == 3).all()) and bool((to[:, 11:] == 3).all()) and bool((to[..., :8] == 3).all())
+    odd = torch.zeros(9, 3, 65, dtype=torch.bfloat16, device=dev)
+    odd[..., 1:] = both[:, :3]
+    assert torch.equal(rot.apply(odd[..., 1:], pos), want[:, :3])          # off 16-byte boundaries
+    assert rot.apply(both[:0], pos[:0]).shape == (0, 12, 64)
+
+
+# ---------------------------------------------------------------------------------------------- append
+
+def pages_for(rng, L, H, d, page, held, spare, dtype, dev, slots_first, cols=None):
+    """A pool with a layer of margin, and a table of scattered pages."""
+    pages = sum(held) + spare
+    shape = (L + 1, 2, pages, page, H, d) if slots_first else (L + 1, 2, pages, H, page, d)
+    base = normal(rng, shape, dtype).to(dev)
+    kv = base.transpose(3, 4) if slots_first else base
+    order = rng.permutation(pages)
+    table = np.full((len(held), cols or max(max(held), 1) + 1), -1, np.int32)
+    at = 0
+    for s, n in enumerate(held):
+        table[s, :n] = order[at:at + n]
+        at += n
+    ref = np.bincount(table[table >= 0], minlength=pages).astype(np.int32)
+    return kv[:L], base, table, ref
+
+
+def book_of(table, length, ref, dev):
+    return plc.PageBook(i32(table, dev), i32(length, dev), i32(ref, dev))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("d, dim, H, G, page, inter, slots_first, given", [(32, 32, 3, 2, 16, False, False, False), (64, 32, 1, 5, 1, True, True, True),
+                                                                         (128, 128, 8, 4, 24, False, True, False), (256, 64, 2, 1, 100, True, False, True),
+                                                                         (128, 12, 2, 2, 16, False, False, True)])
+def test_append(dev, ora, dtype, d, dim, H, G, page, inter, slots_first, given):
+    """Lengths of zero and around page ends, sessions without tokens, rows before, between and behind the ranges, all else in the pool untouched."""
+    rng = np.random.default_rng(d + H + page)
+    lens, n = [0, 1, 47, 48, 49, 100, 7, 0], [3, 1, 20, 0, 1, 2, 0, 1]
+    held = [-(-(a + b) // page) for a, b in zip(lens, n)]
+    kv, base, table, ref = pages_for(rng, 2, H, d, page, held, 3, dtype, dev, slots_first)
+    begin = np.cumsum([2] + n)
+    N = int(begin[-1]) + 3
+    fused = normal(rng, (N, H * (G + 2), d), dtype).to(dev)
+    q, k, v = fused[:, :H * G], fused[:, H * G:H * G + H], fused[:, H * G + H:]
+    rot = plc.Rotary(dim, base=1000.0, interleaved=inter)
+    pos = rng.integers(0, 100000, N) if given else None
+    pool, before = plc.PagePool(kv), base.clone()
+    book = book_of(table, lens, ref, dev)
+    out = torch.full((N, H * G, d), 9.0, dtype=TYPES[dtype], device=dev)
+    got = pool.append(1, book, q, k, v, i32(begin, dev), rotary=rot, pos=None if pos is None else i32(pos, dev), out=out)
+    pool.check()
+    assert got.data_ptr() == out.data_ptr()
+    places, within, bits = ora.append_places(table, lens, ref, begin, page, N)
+    assert bits == 0
+    at = np.array([0 if w is None else w for w in within]) if pos is None else pos
+    turned_q, turned_k = ora.rotary(wide(q), at, rot.frequencies, inter), ora.rotary(wide(k), at, rot.frequencies, inter)
+    tol_q, tol_k = turn_tolerance(wide(q), turned_q, dim, inter, 1.0, dtype), turn_tolerance(wide(k), turned_k, dim, inter, 1.0, dtype)
+    for i in range(N):
+        if within[i] is None:
+            assert bool((out[i] == 9).all())
+            continue
+        assert (np.abs(wide(out[i]) - turned_q[i]) <= tol_q[i]).all()
+        p, s = places[i]
+        assert (np.abs(wide(kv[1, 0, p, :, s]) - turned_k[i]) <= tol_k[i]).all()
+        assert torch.equal(kv[1, 1, p, :, s], v[i])
+        view = before.transpose(3, 4) if slots_first else before
+        view[1, :, p, :, s] = kv[1, :, p, :, s]
+    assert torch.equal(base, before)
+    again = pool.append(1, book, None, k, v, i32(begin, dev))               # no queries, nothing turned
+    assert again is None
+    for i in range(N):
+        if places[i]:
+            assert torch.equal(kv[1, 0, places[i][0], :, places[i][1]], k[i])
+    mine = q.contiguous()
+    assert torch.equal(pool.append(0, book, mine, k, v, i32(begin, dev), rotary=rot, pos=i32(at, dev), out=mine)[2:-3], out[2:-3])
+
+
+def test_append_leaves_out_what_has_no_place(dev, ora):
+    """A shared page, a page out of range, no page, a position behind the table, lengths out of range."""
+    rng = np.random.default_rng(9)
+    kv, base, table, ref = pages_for(rng, 1, 2, 64, 4, [2, 1, 2, 1, 1, 1], 2, "f16", dev, False, cols=2)
+    lens = np.array([4, 2, 3, 3, -2, 1 << 30])
+    ref[table[0, 1]] += 1
+    table[2, 1] = 99
+    begin = np.array([0, 2, 3, 5, 8, 9, 10])
+    N = 10
+    q, k, v = (normal(rng, (N, h, 64), "f16").to(dev) for h in (4, 2, 2))
+    pool, before = plc.PagePool(kv), base.clone()
+    got = pool.append(0, book_of(table, lens, ref, dev), q, k, v, i32(begin, dev), rotary=plc.Rotary(64), pos=i32(np.zeros(N), dev))
+    with pytest.raises(plc.PlcError) as e:
+        pool.check()
+    assert e.value.code == plc.E_INVALID
+    assert torch.equal(got, q)                                              # positions 0: turned by nothing
+    places, _, bits = ora.append_places(table, lens, ref, begin, 4, N)
+    assert bits == ora.RANGE and [p is not None for p in places] == [False, False, True, True, False, True, False, False, False, False]
+    for i, p in enumerate(places):
+        if p:
+            assert torch.equal(kv[0, 0, p[0], :, p[1]], k[i]) and torch.equal(kv[0, 1, p[0], :, p[1]], v[i])
+            before[0, :, p[0], :, p[1]] = kv[0, :, p[0], :, p[1]]
+    assert torch.equal(base, before)
+    for bad in ([0, 2, 1, 5, 8, 9, 10], [-1, 2, 3, 5, 8, 9, 10], [0, 2, 3, 5, 8, 9, 11]):
+        pool.append(0, book_of(table, [0] * 6, ref, dev), q, k, v, i32(bad, dev))
+        with pytest.raises(plc.PlcError):
+            pool.check()
+
+
+# ---------------------------------------------------------------------------------------------- weights
+
+def weigh_case(dev, ora, seed, dtype, d, H, G, page, lens, n, slots_first=False, picked=False, decay=0.5, cap=None, dead=(), bad_pages=(), nan_behind=True, strided=False,
+               lse_off=0.3, L=1, layer=0):
+    """lens: positions of the sessions, their n newest tokens among them."""
+    rng = np.random.default_rng(seed)
+    S = len(lens)
+    kv, base, table, ref = pages_for(rng, L, H, d, page, [-(-x // page) for x in lens], 2, dtype, dev, slots_first)
+    keys = kv[layer, 0].clone()
+    if nan_behind:                                                          # what no session holds is NaN
+        kv[layer, 0] = float("nan")
+        for s in range(S):
+            t = torch.arange(lens[s])
+            if len(t):
+                at = torch.as_tensor(table[s].astype(np.int64))[t // page].to(dev)
+                kv[layer, 0, at, :, (t % page).to(dev)] = keys[at, :, (t % page).to(dev)]
+    for s, j in bad_pages:
+        table[s, j] = 10 ** 6
+    begin = np.cumsum([1 if picked else 0] + list(n))
+    M = int(begin[-1])
+    N = M + 5 if picked else M
+    rows = np.sort(rng.permutation(N)[:M]).astype(np.int32) if picked else None
+    for e in dead if picked else ():
+        rows[e] = -1
+    q = normal(rng, (N, H * G, d), dtype)
+    lse = (rng.standard_normal((N, H * G)) * lse_off + math.log(max(lens) + 1)).astype(np.float32)
+    for e in () if picked else dead:
+        lse[e] = -np.inf
+    cap = cap or max(lens) + 3
+    w = rng.random((S, L + 1, H, cap)).astype(np.float32)
+    on = torch.from_numpy(w).to(dev)
+    pool = plc.PagePool(kv)
+    qd = q.to(dev)
+    if strided:
+        room = torch.zeros(N, H * G + 2, d + 8, dtype=TYPES[dtype], device=dev)
+        room[:, 1:-1, 8:] = qd
+        qd = room[:, 1:-1, 8:]
+    got = pool.attention_weights(layer, book_of(table, lens, ref, dev), qd, torch.from_numpy(lse).to(dev), i32(begin, dev), on[:, :L],
+                                 rows=None if rows is None else torch.from_numpy(rows).to(dev), decay=decay)
+    assert got.data_ptr() == on.data_ptr()
+    k64 = wide(keys)
+
+    def k_of(s, h, t):
+        return None if (s, t // page) in bad_pages else k64[table[s, t // page], h, t % page]
+    ex, reach = ora.weigh(wide(q), lse.astype(np.float64), k_of, lens, begin, rows, d ** -0.5, decay, w[:, layer])
+    after = on.cpu().numpy()
+    off = np.abs(after[:, layer] - ex)
+    tol = 2.0 ** -23 * reach + (2.0 ** -22 + (max(n) * G + 2) * 2.0 ** -24) * np.abs(ex)
+    assert (off <= tol).all(), (off.max(), np.argwhere(~(off <= tol))[:5])
+    after[:, layer] = w[:, layer]
+    assert np.array_equal(after, w)                                         # the other layers' weights
+    for s in range(S):
+        at = lens[s] if n[s] else 0
+        assert np.array_equal(on.cpu().numpy()[s, layer, :, at:], w[s, layer, :, at:])
+    return pool
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d, H, G, page, slots_first", [(32, 3, 1, 16, False), (64, 1, 5, 1, True), (128, 2, 8, 24, False), (128, 4, 1, 64, True), (256, 1, 3, 100, False),
+                                                        (256, 2, 16, 32, True)])
+def test_weights_of_ragged_sessions(dev, ora, dtype, d, H, G, page, slots_first):
+    """Lengths of zero and one, around tile and page ends; sessions without entries, entries that are all there is, one entry and several."""
+    weigh_case(dev, ora, d + H, dtype, d, H, G, page, lens=[0, 1, 15, 16, 17, 130, 33, 64], n=[0, 1, 15, 1, 4, 9, 0, 2], slots_first=slots_first).check()
+
+
+@pytest.mark.parametrize("dtype, d, H, G, n, picked", [("f16", 64, 1, 1, 1, False), ("bf16", 128, 2, 4, 1, True), ("f16", 128, 1, 8, 40, True), ("bf16", 64, 2, 7, 33, False),
+                                                       ("f16", 256, 1, 2, 70, False), ("bf16", 32, 1, 1, 130, True), ("f16", 128, 1, 4, 150, False), ("bf16", 128, 1, 1, 300, False)])
+def test_weights_of_many_entries(dev, ora, dtype, d, H, G, n, picked):
+    weigh_case(dev, ora, n + d, dtype, d, H, G, 16, lens=[200 + n, n, 37, 300 + n], n=[n, n, 1, n // 2], picked=picked, strided=True).check()
+
+
+def test_weights_entries_that_count_for_nothing(dev, ora):
+    """Rows of -1, rows that saw nothing; decay of 0 over NaN, of 1; several layers."""
+    weigh_case(dev, ora, 1, "f16", 64, 2, 2, 16, lens=[40, 9, 70], n=[3, 2, 6], picked=True, dead=(1, 4, 7), L=3, layer=2).check()
+    weigh_case(dev, ora, 2, "bf16", 128, 1, 4, 16, lens=[40, 9, 70], n=[3, 2, 30], dead=(0, 4, 5, 17), decay=1.0).check()
+    weigh_case(dev, ora, 3, "bf16", 128, 1, 4, 16, lens=[4, 2], n=[1, 2], dead=(0, 1, 2), decay=1.0).check()
+    pool = plc.PagePool(torch.ones(1, 2, 2, 1, 16, 64, dtype=torch.float16, device=dev))
+    w = torch.full((1, 1, 1, 20), float("nan"), device=dev)
+    book = book_of(np.array([[1, 0]]), [18], np.array([1, 1]), dev)
+    pool.attention_weights(0, book, torch.zeros(1, 1, 64, dtype=torch.float16, device=dev), torch.zeros(1, 1, device=dev), i32([0, 1], dev), w, decay=0.0)
+    assert bool((w[..., :18] == 1).all()) and bool(w[..., 18:].isnan().all())
+    # NaN in a key shows at its own position alone, and not for rows that count for nothing
+    for n, G in ((1, 1), (1, 8), (40, 4)):
+        kv = torch.zeros(1, 2, 8, 1, 16, 64, dtype=torch.float16, device=dev)
+        kv[0, 0, 1, 0, 3] = float("nan")
+        pool, book = plc.PagePool(kv), book_of(np.array([[0, 1, 2, 3, 4, 5, 6, 7]]), [100], np.array([1] * 8), dev)
+        q = torch.ones(n, G, 64, dtype=torch.float16, device=dev)
+        w = pool.attention_weights(0, book, q, torch.zeros(n, G, device=dev), i32([0, n], dev), pool.new_weights(1, 100))
+        assert w.isnan().nonzero().tolist() == [[0, 0, 0, 19]]
+        w = pool.attention_weights(0, book, q, torch.full((n, G), -math.inf, device=dev), i32([0, n], dev), pool.new_weights(1, 100))
+        assert not w.any()
+
+
+def test_weights_what_is_out_of_range(dev, ora):
+    for n, G in (([3, 2], 2), ([30, 2], 4)):
+        pool = weigh_case(dev, ora, 4, "f16", 64, 1, G, 16, lens=[60, 20], n=n, bad_pages=((0, 1), (1, 0)))
+        with pytest.raises(plc.PlcError) as e:
+            pool.check()
+        assert e.value.code == plc.E_INVALID
+        pool = weigh_case(dev, ora, 5, "f16", 64, 1, G, 16, lens=[60, 20], n=n, cap=33)
+        with pytest.raises(plc.PlcError) as e:
+            pool.check()
+        assert e.value.code == plc.E_CAPACITY
+    pool = plc.PagePool(torch.zeros(1, 2, 4, 1, 16, 64, dtype=torch.float16, device=dev))
+    q, lse = torch.zeros(8, 16, 64, dtype=torch.float16, device=dev), torch.zeros(8, 16, device=dev)
+    for length, begin, rows in (([3], [0, 8], None), ([40], [0, 8], None), ([-1], [0, 8], None), ([20], [0, 9], None), ([20], [3, 1], None), ([20], [0, 2], [0, 8]),
+                                ([20], [0, 2], [-2, 0])):
+        w = pool.attention_weights(0, book_of(np.array([[0, 1]]), length, np.array([1, 1, 0, 0]), dev), q, lse, i32(begin, dev), pool.new_weights(1, 64),
+                                   rows=None if rows is None else i32(rows, dev))
+        assert bool(w.isfinite().all())
+        with pytest.raises(plc.PlcError) as e:
+            pool.check()
+        assert e.value.code == plc.E_INVALID
+
+
+def test_weights_of_an_attention_sum_to_one(dev):
+    """What tree_attention's lse normalises: each head's weights of one entry add up to 1; the same call gives the same bits."""
+    rng = np.random.default_rng(8)
+    for n, G in ((1, 4), (9, 4), (100, 2)):
+        kv, _, table, ref = pages_for(rng, 1, 2, 128, 32, [40, 5], 1, "bf16", dev, False)
+        pool, q = plc.PagePool(kv), normal(rng, (n + 1, 2 * G, 128), "bf16").to(dev)
+        before, after = book_of(table, [1200 - n, 100], ref, dev), book_of(table, [1200, 101], ref, dev)
+        begin = i32([0, n, n + 1], dev)
+        _, lse = pool.tree_attention(0, before, q, begin)
+        w = pool.attention_weights(0, after, q, lse, begin, pool.new_weights(2, 1200))
+        assert torch.allclose(w[0, 0].double().sum(-1), torch.tensor(float(n * G), dtype=torch.float64, device=dev), rtol=2.0 ** -14)
+        assert torch.allclose(w[1, 0].double().sum(-1), torch.tensor(float(G), dtype=torch.float64, device=dev), rtol=2.0 ** -14)
+        for _ in range(3):
+            assert torch.equal(w, pool.attention_weights(0, after, q, lse, begin, pool.new_weights(2, 1200)))
+
+
+def test_weights_offsets_pass_32_bits(dev):
+    """Pages farther apart than 2^31 elements, weights' rows too."""
+    far = (1 << 31) + 64
+    store = torch.empty(2 * far + 4 * 8 * 64, dtype=torch.float16, device=dev)
+    kv = store.as_strided((1, 2, 3, 1, 8, 64), (0, 8 * 64, far, 8 * 64, 64, 1))
+    rng = np.random.default_rng(3)
+    kv[0, 0] = normal(rng, (3, 1, 8, 64), "f16").to(dev)
+    room = torch.empty((1 << 30) + (1 << 29) + 64, device=dev)
+    for n in (1, 30):
+        w = room.as_strided((2, 1, 1, 20), ((1 << 30) + (1 << 29) + 1, 20, 20, 1))
+        w[:] = 0
+        q = normal(rng, (n, 1, 64), "f16").to(dev)
+        book = book_of(np.array([[0, 1, 2], [2, 0, 1]]), [0, max(14, min(n, 20))], np.array([2, 2, 2]), dev)
+        m = min(n, 14)
+        plc.PagePool(kv).attention_weights(0, book, q, torch.zeros(n, 1, device=dev), i32([0, 0, m], dev), w)
+        T = max(14, min(n, 20))
+        K = torch.cat([kv[0, 0, 2, 0], kv[0, 0, 0, 0], kv[0, 0, 1, 0]])[:T].double()
+        z = (q[:m, 0].double() @ K.t() / 8).exp()
+        z = z * (torch.arange(T, device=dev) <= (T - m + torch.arange(m, device=dev))[:, None])
+        assert torch.allclose(w[1, 0, 0, :T].double(), z.sum(0), rtol=1e-4) and not w[0].any()
+
+
+# ---------------------------------------------------------------------------------------------- eviction
+
+def evict_case(dev, ora, seed, dtype, d, H, L, page, lens, budget, recent, slots_first=False, share=(), spare=4, weights=None, cap=None, bad_pages=(), scalar=None):
+    """share: (row, from row, pages) whose first pages are another row's."""
+    rng = np.random.default_rng(seed)
+    S = len(lens)
+    kv, base, table, ref = pages_for(rng, L, H, d, page, [-(-max(x, 0) // page) + 1 for x in lens], spare, dtype, dev, slots_first)
+    for s, o, n in share:
+        table[s, :n] = table[o, :n]
+    for s, j in bad_pages:
+        table[s, j] = 10 ** 6
+    ref = np.bincount(table[(table >= 0) & (table < len(ref))], minlength=len(ref)).astype(np.int32)
+    T = cap or max(max(lens), 1) + 2
+    w = rng.random((S, L, H, T)).astype(np.float32) ** 4 if weights is None else weights(rng, (S, L, H, T)).astype(np.float32)
+    on = torch.from_numpy(w).to(dev)
+    pool, book = plc.PagePool(kv), book_of(table, lens, ref, dev)
+    want_kv = base.clone()
+    view, old = (want_kv.transpose(3, 4) if slots_first else want_kv), (base.clone().transpose(3, 4) if slots_first else base.clone())
+    new, new_w = pool.evict(book, on, i32(budget, dev) if scalar is None else scalar, recent=recent)
+    t, n, r, ww, moves, bits = ora.evict(table, np.asarray(lens), ref, w, budget, recent, page)
+    for s, l, h, a, b in moves:
+        view[l, :, b[0], h, b[1]] = old[l, :, a[0], h, a[1]]
+    assert np.array_equal(new.table.cpu().numpy(), t) and np.array_equal(new.len.cpu().numpy(), n) and np.array_equal(new.ref.cpu().numpy(), r)
+    assert np.array_equal(new_w.cpu().numpy().view(np.int32), ww.view(np.int32))
+    assert torch.equal(base.view(torch.int16 if dtype != "f32" else torch.int32), want_kv.view(torch.int16 if dtype != "f32" else torch.int32))
+    assert np.array_equal(on.cpu().numpy().view(np.int32), w.view(np.int32))
+    return pool, bits
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("d, H, L, page, slots_first", [(32, 3, 2, 16, False), (64, 1, 1, 1, True), (128, 2, 2, 24, False), (256, 2, 1, 100, True)])
+def test_eviction_of_ragged_rows(dev, ora, dtype, d, H, L, page, slots_first):
+    """Budgets of zero, one, the length, more, negative ones; lengths of zero and around page and piece ends."""
+    pool, bits = evict_case(dev, ora, d, dtype, d, H, L, page, lens=[0, 1, 127, 128, 129, 300, 60, 261, 30, 5], budget=[0, 0, 64, 127, 128, 77, 60, -1, 31, 1], recent=5,
+                            slots_first=slots_first)
+    assert bits == 0
+    pool.check()
+
+
+@pytest.mark.parametrize("recent", [0, 3, 40, 1000])
+def test_eviction_keeps_the_recent_ones(dev, ora, recent):
+    evict_case(dev, ora, recent, "f16", 64, 2, 2, 16, lens=[200, 50, 41], budget=[40] * 3, recent=recent, scalar=40)[0].check()
+
+
+@pytest.mark.parametrize("kind", ["equal", "zeros", "few values", "specials", "tiny"])
+def test_eviction_of_weights_that_are_alike(dev, ora, kind):
+    """Ties go to the lower position; -0 is 0; NaN is lightest; infinities and denormals have their places."""
+    def weights(rng, shape):
+        if kind == "equal":
+            return np.ones(shape)
+        if kind == "zeros":
+            return np.where(rng.random(shape) < 0.5, 0.0, -0.0)
+        if kind == "few values":
+            return rng.integers(0, 3, shape)
+        if kind == "tiny":
+            return rng.integers(0, 100, shape) * 2.0 ** -149
+        return rng.choice([np.nan, np.inf, -np.inf, 0.0, 1.0, -1.0], shape)
+    evict_case(dev, ora, 3, "f16", 32, 2, 2, 16, lens=[300, 150, 20], budget=[100, 149, 3], recent=2, weights=weights)[0].check()
+
+
+def test_eviction_from_shared_pages(dev, ora):
+    """Beams over one prompt: shared pages of rows that go are replaced by fresh ones, those of rows that stay are not touched."""
+    share = ((1, 0, 5), (2, 0, 3), (4, 3, 2))
+    pool, bits = evict_case(dev, ora, 4, "bf16", 64, 2, 2, 16, lens=[100, 90, 110, 64, 70], budget=[50, 50, -1, 33, 20], recent=7, share=share, spare=12)
+    assert bits == 0
+    pool.check()
+
+
+def test_eviction_without_free_pages_changes_nothing(dev, ora):
+    share = ((1, 0, 5), (2, 0, 3), (4, 3, 2))               # ten of their own pages are free, twelve are needed
+    pool, bits = evict_case(dev, ora, 4, "bf16", 64, 2, 2, 16, lens=[100, 90, 110, 64, 70], budget=[50, 50, -1, 33, 20], recent=7, share=share, spare=0)
+    assert bits == ora.CAPACITY
+    with pytest.raises(plc.PlcError) as e:
+        pool.check()
+    assert e.value.code == plc.E_CAPACITY
+    kv = torch.randn(1, 2, 5, 1, 4, 32, device=dev)
+    pool, w = plc.PagePool(kv), torch.rand(2, 1, 1, 20, device=dev)
+    before = kv.clone()
+    table = np.array([[0, 1, 2], [0, 1, 3]])
+    for hold, short in ((1, True), (0, False)):                             # one free page where two are needed; page 4 held by the caller or not
+        ref = np.array([2, 2, 1, 1, hold])
+        new, got = pool.evict(book_of(table, [12, 10], ref, dev), w, 4)
+        with pytest.raises(plc.PlcError) as e:
+            pool.check()
+        assert e.value.code == plc.E_CAPACITY
+        assert np.array_equal(new.table.cpu().numpy(), table) and new.len.tolist() == [12, 10] and new.ref.tolist() == ref.tolist()
+        assert torch.equal(kv, before)
+        for s, n in ((0, 12), (1, 10)):
+            assert torch.equal(got[s, ..., :n], w[s, ..., :n]) and not got[s, ..., n:].any()
+
+
+def test_eviction_leaves_rows_that_are_out_of_range(dev, ora):
+    pool, bits = evict_case(dev, ora, 6, "f16", 64, 2, 1, 16, lens=[100, 70, 40, 90], budget=[50, 30, 20, 45], recent=3, cap=95, bad_pages=((1, 2), (3, 6)))
+    assert bits == ora.RANGE
+    with pytest.raises(plc.PlcError) as e:
+        pool.check()
+    assert e.value.code == plc.E_INVALID
+    pool, bits = evict_case(dev, ora, 7, "f16", 64, 2, 1, 16, lens=[-5, 70], budget=[50, 30], recent=3)
+    assert bits == ora.RANGE
+    with pytest.raises(plc.PlcError):
+        pool.check()
+
+
+def test_eviction_of_a_long_row(dev, ora):
+    """Many pieces of one row, which wait for nothing but what they write over; nearly all and nearly nothing kept."""
+    for budget, d, dtype, page in ((5000, 32, "f16", 16), (9990, 64, "f32", 128), (3, 32, "bf16", 100), (9000, 256, "f32", 64)):
+        evict_case(dev, ora, budget, dtype, d, 1, 1, page, lens=[10000], budget=[budget], recent=2)[0].check()
+
+
+def test_eviction_offsets_pass_32_bits(dev):
+    far = (1 << 31) + 64
+    store = torch.empty(2 * far + 4 * 8 * 64, dtype=torch.float16, device=dev)
+    kv = store.as_strided((1, 2, 3, 1, 8, 64), (0, 8 * 64, far, 8 * 64, 64, 1))
+    rng = np.random.default_rng(3)
+    x = normal(rng, (2, 3, 1, 8, 64), "f16").to(dev)
+    kv[0] = x
+    w = torch.tensor([float(t % 2) for t in range(24)], device=dev).view(1, 1, 1, 24)
+    new, _ = plc.PagePool(kv).evict(book_of(np.array([[2, 0, 1]]), [24], np.array([1, 1, 1]), dev), w, 12)
+    flat = torch.cat([x[:, 2, 0], x[:, 0, 0], x[:, 1, 0]], 1)[:, 1::2]
+    got = torch.cat([kv[0, :, 2, 0], kv[0, :, 0, 0]], 1)[:, :12]
+    assert torch.equal(got, flat) and new.table.tolist() == [[2, 0, -1]] and new.len.tolist() == [12]
+
+
+# ---------------------------------------------------------------------------------------------- log probabilities
+
+def logprobs_case(dev, ora, x, tokens, n_top, dtype, exact_rows=None):
+    on = x.to(TYPES[dtype]).to(dev)
+    logp, entropy, top_logp, top_token = plc.token_logprobs(on, i32(tokens, dev), n_top)
+    pl, pe, pt, ptok, m = ora.token_logprobs(wide(on), np.asarray(tokens), n_top)
+    l = 2.0 ** -20 + 2.0 ** -23 * m[:, 0]
+    got = wide(logp)
+    assert np.array_equal(np.isnan(got), np.isnan(pl))
+    fine = ~np.isnan(pl)
+    inf = fine & np.isinf(pl)
+    assert np.array_equal(got[inf], pl[inf])
+    fine &= ~inf
+    assert (np.abs(got - np.where(fine, pl, 0))[fine] <= (l[:, None] + 2.0 ** -23 * np.abs(np.where(fine, pl, 0)))[fine]).all()
+    ge = wide(entropy)
+    assert np.array_equal(np.isnan(ge), np.isnan(pe))
+    ok = ~np.isnan(pe)
+    assert (np.abs(ge - pe)[ok] <= (2.0 ** -19 * (1 + m.sum(1)) + 2.0 ** -23 * pe)[ok]).all(), np.abs(ge - pe)[ok].max()
+    assert np.array_equal(top_token.cpu().numpy(), ptok)
+    gt = wide(top_logp)
+    none = np.isinf(pt)
+    assert np.array_equal(gt[none], pt[none])
+    assert (np.abs(gt - np.where(none, 0, pt))[~none] <= (l[:, None] + 2.0 ** -23 * np.abs(np.where(none, 0, pt)))[~none]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("N, V, m, n_top", [(1, 1, 1, 1), (3, 7, 2, 9), (5, 1000, 1, 0), (2, 32000, 3, 5), (70, 4097, 1, 20), (1, 128256, 1, 128), (9, 50257, 7, 8)])
+def test_logprobs(dev, ora, dtype, N, V, m, n_top):
+    """One row split over the GPU and many; odd vocabularies, whose rows start off 16-byte boundaries; no alternatives, more than there are tokens; padding."""
+    rng = np.random.default_rng(V + m)
+    x = torch.from_numpy(rng.standard_normal((N, V)).astype(np.float32)) * 3
+    tokens = rng.integers(0, V, (N, m))
+    tokens[0, 0] = int(x[0].argmax())
+    if N > 2:
+        tokens[1] = -1
+    logprobs_case(dev, ora, x, tokens, n_top, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+def test_logprobs_of_peaks_masks_and_rows_that_are_none(dev, ora, dtype):
+    V = 9000
+    rng = np.random.default_rng(2)
+    x = torch.from_numpy(rng.standard_normal((12, V)).astype(np.float32))
+    low = torch.finfo(TYPES[dtype]).min
+    x[0] = 1.0                                            # all alike: ties to the lower token, entropy log V
+    x[1] = -200.0
+    x[1, 77] = 40.0                                       # one token has it all
+    x[2, 10:] = -math.inf                                 # ten tokens are left
+    x[3, 3:] = low                                        # masked by the lowest value
+    x[4] = low                                            # all of it
+    x[5] = -math.inf                                      # nothing
+    x[6, 4000] = math.nan
+    x[7, 8999] = math.inf
+    x[8] = -math.inf
+    x[8, 5000] = 2.5                                      # one token
+    x[9, ::2] = 8.0                                       # 4500 equal ones on top
+    x[10, :4500] = -math.inf
+    x[11] = torch.linspace(0, 60, V)
+    tokens = np.array([[5, 0], [77, 3], [9, 11], [1, 8000], [0, 8999], [0, -1], [1, 2], [8999, 0], [5000, 1], [1, 8998], [0, 4500], [0, 8999]])
+    logprobs_case(dev, ora, x, tokens, 16, dtype)
+    logprobs_case(dev, ora, x[:, :33], tokens % 33, 40, dtype)
+
+
+def test_logprobs_strides_and_tokens_out_of_range(dev, ora):
+    rng = np.random.default_rng(4)
+    room = torch.from_numpy(rng.standard_normal((6, 5000)).astype(np.float32)).half().to(dev)
+    word = torch.zeros(1, dtype=torch.int32, device=dev)
+    a = plc.token_logprobs(room[:, 3:4000], i32(rng.integers(0, 3997, (6, 1)), dev), 4, status=word)
+    b = plc.token_logprobs(room[:, 3:4000].contiguous(), i32(np.random.default_rng(0).integers(0, 3997, 6), dev), 4)
+    assert torch.equal(a[1], b[1]) and torch.equal(a[2], b[2]) and torch.equal(a[3], b[3]) and b[0].shape == (6,) and int(word) == 0
+    logp, *_ = plc.token_logprobs(room, i32([[0, 5000], [-2, 1], [-1, 2], [1 << 30, 3], [4, 4], [0, 0]], dev), status=word)
+    assert int(word) == 32 and logp[0, 1] == 0 and logp[1, 0] == 0 and logp[2, 0] == 0 and logp[3, 0] == 0 and bool((logp[:, 1][1:] < 0).all())
+    assert plc.token_logprobs(room[:0], i32(np.zeros((0, 2)), dev), 3)[2].shape == (0, 3)
+
+
+def test_logprobs_agree_with_beam_selection(dev):
+    """The likeliest alternatives of a row are a single beam's best continuations."""
+    x = torch.randn(5, 32000, device=dev, generator=torch.Generator(device=dev).manual_seed(1)) * 3
+    _, _, top, token = plc.token_logprobs(x, torch.zeros(5, 1, dtype=torch.int32, device=dev), 12)
+    score, _, best = plc.beam_select(x[:, None], torch.zeros(5, 1, device=dev), 12)
+    assert torch.equal(token, best) and torch.allclose(top, score, rtol=0, atol=2.0 ** -19)
+
+
+# ---------------------------------------------------------------------------------------------- together
+
+def test_a_decoding_loop(dev, ora):
+    """Prompt, drafted tree, acceptance, weights and eviction, captured into a graph and replayed on fresh pages: each step against the formulas."""
+    rng = np.random.default_rng(11)
+    L, H, G, d, page, S, cap = 2, 2, 2, 64, 16, 3, 96
+    kv = torch.zeros(L, 2, 40, H, page, d, dtype=torch.float16, device=dev)
+    pool, rot = plc.PagePool(kv), plc.Rotary(d, base=1000.0)
+    prompt = [20, 33, 7]
+    begin = i32(np.cumsum([0] + prompt), dev)
+    N = sum(prompt)
+    x = [normal(rng, (N, H * (G + 2), d), "f16").to(dev) for _ in range(L)]
+    room, same = i32([48] * S, dev), i32([0, 1, 2], dev)
+    path = torch.arange(33, dtype=torch.int32, device=dev).expand(S, -1).contiguous()
+    draft = [normal(rng, (4 * S, H * (G + 2), d), "f16").to(dev) for _ in range(L)]
+    dbegin, depth = i32([0, 4, 8, 12], dev), i32([p + t for p in prompt for t in (0, 1, 1, 2)], dev)
+    mask = i32([0b0001, 0b0011, 0b0101, 0b1101] * S, dev).view(-1, 1)      # nodes 1 and 2 under 0, 3 under 2
+    taken, count = i32([[0, 2, 3]] * S, dev), i32([3] * S, dev)
+    accepted, abegin = i32([r + 4 * s for s in range(S) for r in (0, 2, 3)], dev), i32([0, 3, 6, 9], dev)
+    logits, tokens = torch.randn(S, 1000, device=dev, dtype=torch.float32), i32([1, 2, 3], dev)
+
+    def split(t):
+        return t[:, :H * G], t[:, H * G:H * G + H], t[:, H * G + H:]
+
+    def loop():
+        kv.zero_()
+        book, w, outs = pool.new_book(S, 8), pool.new_weights(S, cap), []
+        book = pool.fork(book, same, room)
+        lses = []
+        for l in range(L):
+            q, k, v = split(x[l])
+            q = pool.append(l, book, q, k, v, begin, rotary=rot)
+            out, lse = pool.tree_attention(l, book, q, begin)
+            lses.append((q, lse))
+            outs.append(out)
+        book = pool.keep(book, path, i32c)
+        for l, (q, lse) in enumerate(lses):
+            pool.attention_weights(l, book, q, lse, begin, w)
+        book = pool.fork(book, same, room)
+        lses = []
+        for l in range(L):
+            q, k, v = split(draft[l])
+            q = pool.append(l, book, q, k, v, dbegin, rotary=rot, pos=depth)
+            out, lse = pool.tree_attention(l, book, q, dbegin, mask=mask)
+            lses.append((q, lse))
+            outs.append(out)
+        book = pool.keep(book, taken, count)
+        for l, (q, lse) in enumerate(lses):
+            pool.attention_weights(l, book, q, lse, abegin, w, rows=accepted, decay=0.5)
+        book2, w2 = pool.evict(book, w, 16, recent=4)
+        return outs, book, w, book2, w2, plc.token_logprobs(logits, tokens, 4)
+    i32c = i32(prompt, dev)
+    plain = loop()
+    kv_plain = kv.clone()
+    pool.check()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        loop()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = loop()
+    for _ in range(2):
+        graph.replay()
+    torch.cuda.synchronize()
+    pool.check()
+    assert torch.equal(kv, kv_plain)
+    for a, b in ((got[2], plain[2]), (got[4], plain[4]), (got[1].table, plain[1].table), (got[3].table, plain[3].table), (got[3].ref, plain[3].ref)):
+        assert torch.equal(a, b)
+    for a, b in zip(got[0] + list(got[5]), plain[0] + list(plain[5])):
+        assert torch.equal(a, b)
+    # session 1, layer 1, against the definitions in 64 bits: keys and values of prompt and accepted draft
+    outs, book, w, book2, w2, _ = plain
+    s, l = 1, 1
+    at = prompt[0]
+    qkv, dq = wide(x[l])[at:at + 33], wide(draft[l])[4:8]
+    turn = lambda t, p: ora.rotary(t, p, rot.frequencies)  # noqa: E731
+    Q, K = turn(qkv[:, :H * G], np.arange(33)), turn(qkv[:, H * G:H * G + H], np.arange(33))
+    dp = np.array([33, 34, 34, 35])
+    DQ, DK = turn(dq[:, :H * G], dp), turn(dq[:, H * G:H * G + H], dp)
+    keys = np.concatenate([K, DK[[0, 2, 3]]])
+    want = np.zeros((H, 36))
+    for h in range(H):
+        for g in range(h * G, (h + 1) * G):
+            z = np.where(np.tril(np.ones((33, 33), bool)), Q[:, g] @ K[:, h].T / 8, -np.inf)
+            first = np.exp(z - np.logaddexp.reduce(z, 1, keepdims=True)).sum(0)
+            want[h, :33] += 0.5 * first
+            for j, r in enumerate((0, 2, 3)):
+                z = DQ[r, g] @ keys[:33 + j + 1, h].T / 8
+                want[h, :33 + j + 1] += np.exp(z - np.logaddexp.reduce(z))
+    # f16 keys and queries are off by 2^-11 each after the turn: scores by about 64 * 2^-10 / 8 of unit products at most
+    assert np.abs(wide(w[s, l, :, :36]) - want).max() < 0.02 * want.max()
+    assert book.len.tolist() == [23, 36, 10] and book2.len.tolist() == [16, 16, 10]
+    for h in range(H):
+        ww = w[s, l, h, :32].cpu().numpy()
+        kept = sorted(sorted(range(32), key=lambda t: (-ww[t], t))[:12]) + [32, 33, 34, 35]
+        t2 = book2.table[s].cpu().numpy()
+        now = torch.stack([kv_plain[l, 0, t2[i // page], h, i % page] for i in range(16)])
+        assert np.abs(wide(now) - keys[kept, h]).max() < 2.0 ** -8
+
+
+def test_two_calls_on_two_streams(dev):
+    """Nothing is shared between calls but what the caller passes."""
+    rng = np.random.default_rng(12)
+    pools = []
+    for i in range(2):
+        kv, _, table, ref = pages_for(rng, 2, 4, 64, 16, [40, 30], 2, "f16", dev, False)
+        pools.append((plc.PagePool(kv), book_of(table, [600, 450], ref, dev), torch.rand(2, 2, 4, 640, device=dev), torch.randn(64, 9000, device=dev), kv, kv.clone()))
+    tokens = torch.zeros(64, 1, dtype=torch.int32, device=dev)
+    alone = []
+    for pool, book, w, x, kv, keep in pools:
+        b, nw = pool.evict(book, w, 300, recent=10)
+        alone.append((b.table.clone(), nw, kv.clone(), plc.token_logprobs(x, tokens, 8)))
+        kv.copy_(keep)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = []
+        streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+        for st, (pool, book, w, x, kv, keep) in zip(streams, pools):
+            with torch.cuda.stream(st):
+                b, nw = pool.evict(book, w, 300, recent=10)
+                got.append((b, nw, kv, plc.token_logprobs(x, tokens, 8)))
+        torch.cuda.synchronize()
+        for (b, nw, kv, lp), (t0, w0, k0, l0) in zip(got, alone):
+            assert torch.equal(b.table, t0) and torch.equal(nw, w0) and torch.equal(kv, k0) and all(torch.equal(p, q) for p, q in zip(lp, l0))
+        for pool, book, w, x, kv, keep in pools:
+            kv.copy_(keep)
+        torch.cuda.synchronize()
