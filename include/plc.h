@@ -547,9 +547,12 @@ typedef struct {
  * read).  Sessions without entries are left as they are.  Entries whose lse is infinite (they saw nothing) count for nothing.
  * scale: positive and finite, as for the attention; decay: finite, not negative.  Scores and sums are binary32, sums in an order
  * that does not change from call to call.  Positions from n_pos on are left out (bit 1).  Ranges, lengths, rows and page numbers out of range, and more entries
- * than positions (bit 32): ranges and lengths are cut to what there is, a row counts for nothing, positions without a page receive nothing. */
+ * than positions (bit 32): ranges and lengths are cut to what there is, a row counts for nothing, positions without a page receive nothing.
+ * workspace: plc_pages_weigh_workspace bytes. */
 plc_status plc_pages_weigh(const plc_page_pool* pool, int32_t layer, const plc_page_book* book, const plc_weigh_queries* queries, float scale,
-                           float decay, const plc_weights* weights, uint32_t* status_dev, void* stream);
+                           float decay, const plc_weights* weights, void* workspace_dev, uint64_t workspace_bytes, uint32_t* status_dev,
+                           void* stream);
+plc_status plc_pages_weigh_workspace(const plc_page_pool* pool, int32_t sessions, int32_t n_heads, int32_t n_list, uint64_t* bytes);
 
 /* Rows with more than their budget (budget_dev [rows], negative: the row stays; or NULL: `budget` for all) keep that many positions: in every layer and head by
  * itself the last min(recent, budget) ones, and of the others those with the largest weights, ties to the lower position, NaN last.  What is kept moves together in

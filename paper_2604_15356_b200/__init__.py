@@ -14,7 +14,7 @@ _INC = os.path.join(os.path.dirname(_HERE), "include")
 _SO = os.path.join(_HERE, "libplc.so")
 _SOURCES = ["plc_api.cu", "plc_topk.cu", "plc_prefix.cu", "plc_codec.cu", "plc_coop.cu", "plc_dense.cu", "plc_static.cu", "plc_trie.cu",
             "plc_pages.cu", "plc_attend.cu", "plc_attend_few_f16.cu", "plc_attend_few_bf16.cu",
-            "plc_attend_many_f16.cu", "plc_attend_many_bf16.cu", "plc_beam.cu", "plc_rotary.cu", "plc_weigh.cu", "plc_evict.cu", "plc_logprobs.cu"]
+            "plc_attend_many_f16.cu", "plc_attend_many_bf16.cu", "plc_beam.cu", "plc_rotary.cu", "plc_weigh.cu", "plc_weigh_many.cu", "plc_evict.cu", "plc_logprobs.cu"]
 
 OK, E_INVALID, E_SHAPE, E_ALIGN, E_CAPACITY, E_CORRUPT, E_STATE, E_CUDA = range(8)
 PRED_TOPK, PRED_DENSE, PRED_LINEAR = 0, 1, 2
@@ -28,7 +28,7 @@ EXPORTS = ["plc_create", "plc_destroy", "plc_reserve", "plc_topk_softmax", "plc_
            "plc_trie_stats", "plc_create_linear", "plc_prefix_clusters", "plc_rotq_record_bytes", "plc_encode_rotq",
            "plc_decode_rotq", "plc_poll_status", "plc_last_schedule", "plc_kernel_ms", "plc_take_status", "plc_pages_workspace", "plc_pages_fork",
            "plc_pages_keep", "plc_pages_compact", "plc_tree_attention", "plc_tree_attention_workspace", "plc_beam_workspace",
-           "plc_beam_select", "plc_beam_reorder", "plc_rotary_turns", "plc_rotary_apply", "plc_pages_append", "plc_pages_weigh", "plc_pages_evict",
+           "plc_beam_select", "plc_beam_reorder", "plc_rotary_turns", "plc_rotary_apply", "plc_pages_append", "plc_pages_weigh", "plc_pages_weigh_workspace", "plc_pages_evict",
            "plc_pages_evict_workspace", "plc_token_logprobs", "plc_token_logprobs_workspace"]
 
 
@@ -40,7 +40,7 @@ def build(force=False, verbose=False):
     """Compile libplc.so for sm_100a with nvcc (in-tree)."""
     srcs = sources()
     deps = srcs + [os.path.join(_CSRC, h) for h in ("plc_common.cuh", "plc_coder.cuh", "plc_codec.cuh", "plc_pages.cuh", "plc_attend.cuh", "plc_attend_few.cuh",
-                                                        "plc_attend_many.cuh", "plc_logits.cuh")] + [os.path.join(_INC, "plc.h")]
+                                                        "plc_attend_many.cuh", "plc_logits.cuh", "plc_tensor.cuh", "plc_weigh.cuh")] + [os.path.join(_INC, "plc.h")]
     if not force and os.path.exists(_SO) and all(os.path.getmtime(_SO) >= os.path.getmtime(d) for d in deps):
         return _SO
     cmd = ["nvcc", "-t", "0", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

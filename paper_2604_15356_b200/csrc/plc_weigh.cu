@@ -11,32 +11,12 @@
 #include <cuda_bf16.h>
 #include <math.h>
 
-#include "plc_pages.cuh"
+#include "plc_weigh.cuh"
 
 namespace plc {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896f;
-
-struct WeighArgs {
-    const uint16_t* q; int64_t qs_row, qs_head;   // elements
-    const float* lse; const int32_t* rows; const int32_t* begin;
-    int n_list, n_rows, heads, group, layer;
-    float* weight; int64_t ws_row, ws_head; int n_pos;
-    float decay, scale;
-};
-
-// A session as the call gives it, cut to what there is: entries first .. first + n - 1 of the list stand at its last n positions.
-struct Session { int first, n, len; };
-__device__ __forceinline__ Session session_of(const PoolDev& p, const BookDev& b, const WeighArgs& a, int s, bool* bad) {
-    const int b0 = a.begin[s], b1 = a.begin[s + 1], len = b.len[s], most = most_positions(b, p);
-    Session x;
-    x.first = min(max(b0, 0), a.n_list);
-    x.n = min(max(b1, x.first), a.n_list) - x.first;
-    x.len = x.n > 0 ? min(max(len, 0), most) : 0;
-    *bad = b0 < 0 || b1 < b0 || b1 > a.n_list || len < 0 || len > most || x.n > len;
-    return x;
-}
 
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
@@ -65,7 +45,7 @@ __global__ void __launch_bounds__(kThreads) weigh_kernel(const __grid_constant__
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     // tiles of the sessions: a thread sums a run of them, the threads' sums are scanned
     const int run = (b.rows + kThreads - 1) / kThreads, first_s = min(b.rows, tid * run), last_s = min(b.rows, first_s + run);
-    auto tiles_of = [&](int s, bool* bad) -> long long { return (long long)((session_of(p, b, a, s, bad).len + kTile - 1) / kTile) * p.H; };
+    auto tiles_of = [&](int s, bool* bad) -> long long { return (long long)((newest_of(p, b, a, s, bad).len + kTile - 1) / kTile) * p.H; };
     long long mine = 0;
     bool any_bad = false;
     for (int s = first_s; s < last_s; ++s) {
@@ -108,7 +88,7 @@ __global__ void __launch_bounds__(kThreads) weigh_kernel(const __grid_constant__
     }
     long long left = t1 - t0;
     bool bad;
-    Session x = session_of(p, b, a, s, &bad);
+    Newest x = newest_of(p, b, a, s, &bad);
     int tiles = (x.len + kTile - 1) / kTile, h = (int)(rest / tiles), tile = (int)(rest - (long long)h * tiles);
     const int quad = lane >> 2, part = lane & 3;
     const float c2 = a.scale * kLog2e;
@@ -161,21 +141,13 @@ __global__ void __launch_bounds__(kThreads) weigh_kernel(const __grid_constant__
             sum0 += __shfl_xor_sync(kFull, sum0, 2);
             sum1 += __shfl_xor_sync(kFull, sum1, 2);
             const int t = base + quad + 8 * part;
-            if (part < 2 && t < x.len) {
-                if (t >= a.n_pos) atomicOr(status, kStCapacity);
-                else {
-                    float* w = a.weight + (int64_t)s * a.ws_row + (int64_t)h * a.ws_head + t;
-                    const bool there = (part ? off1 : off0) >= 0;
-                    const float old = t < x.len - x.n && a.decay != 0.f ? *w * a.decay : 0.f;
-                    *w = there ? old + (part ? sum1 : sum0) : old;
-                }
-            }
+            if (part < 2 && t < x.len) put_weight(a, x, s, h, t, part ? sum1 : sum0, (part ? off1 : off0) >= 0, status);
         }
         left -= todo;
         tile = 0;
         if (left > 0 && ++h == p.H) {
             h = 0;
-            do x = session_of(p, b, a, ++s, &bad);
+            do x = newest_of(p, b, a, ++s, &bad);
             while (x.len == 0);
             tiles = (x.len + kTile - 1) / kTile;
         }
@@ -193,6 +165,10 @@ cudaError_t launch_weigh(const PoolDev& p, const BookDev& b, const WeighArgs& a,
     }
 }
 
+// Columns (entries times the query heads of a group) a session from which the tensor cores' kernel takes the call.  By the mean, which is what the host knows.
+constexpr int kFewColumns = 16;
+bool many_columns(const PoolDev& p, int sessions, int heads, int n_list) { return (long long)n_list * (heads / p.H) > (long long)kFewColumns * sessions; }
+
 }  // namespace
 }  // namespace plc
 
@@ -200,23 +176,40 @@ using namespace plc;
 
 extern "C" {
 
+plc_status plc_pages_weigh_workspace(const plc_page_pool* pool, int32_t sessions, int32_t n_heads, int32_t n_list, uint64_t* bytes) {
+    PoolDev p;
+    const plc_status rc = check_pool(pool, &p);
+    if (rc) return rc;
+    if (n_heads < 1 || sessions < 1 || n_list < 0 || !bytes) return PLC_E_INVALID;
+    if (n_heads % p.H || n_heads > (1 << 16)) return PLC_E_SHAPE;
+    *bytes = many_columns(p, sessions, n_heads, n_list) ? weigh_many_bytes() : 16;
+    return PLC_OK;
+}
+
 plc_status plc_pages_weigh(const plc_page_pool* pool, int32_t layer, const plc_page_book* book, const plc_weigh_queries* t, float scale, float decay,
-                           const plc_weights* weights, uint32_t* status_dev, void* stream) {
+                           const plc_weights* weights, void* workspace_dev, uint64_t workspace_bytes, uint32_t* status_dev, void* stream) {
     PoolDev p;
     BookDev b;
     plc_status rc = check_pool(pool, &p);
     if (rc || (rc = check_book(book, &b))) return rc;
-    if (!t || !t->q_dev || !t->lse_dev || !t->begin_dev || t->n_rows < 0 || t->n_list < 0 || !weights || !weights->base_dev || !status_dev) return PLC_E_INVALID;
+    if (!t || !t->q_dev || !t->lse_dev || !t->begin_dev || t->n_rows < 0 || t->n_list < 0 || !weights || !weights->base_dev || !workspace_dev || !status_dev) return PLC_E_INVALID;
     if (layer < 0 || layer >= p.L || pool->dtype == PLC_OUT_F32 || !(scale > 0.f) || isinf(scale) || !isfinite(decay) || decay < 0.f) return PLC_E_INVALID;
     if (t->n_heads < 1 || weights->n_pos < 1) return PLC_E_INVALID;
     if (t->n_heads % p.H || t->n_heads > (1 << 16) || (!t->rows_dev && t->n_list > t->n_rows)) return PLC_E_SHAPE;
     const int group = t->n_heads / p.H;
     if ((long long)t->n_list * group > (1 << 30)) return PLC_E_SHAPE;
-    if (!plc_aligned16(t->q_dev) || t->q_stride_row % 8 || t->q_stride_head % 8 || (reinterpret_cast<uintptr_t>(weights->base_dev) & 3)) return PLC_E_ALIGN;
+    const bool many = many_columns(p, b.rows, t->n_heads, t->n_list);
+    if (!plc_aligned16(workspace_dev) || !plc_aligned16(t->q_dev) || t->q_stride_row % 8 || t->q_stride_head % 8 || (reinterpret_cast<uintptr_t>(weights->base_dev) & 3)) return PLC_E_ALIGN;
+    if (workspace_bytes < (many ? weigh_many_bytes() : 16)) return PLC_E_CAPACITY;
     if (t->n_list == 0) return PLC_OK;
     const WeighArgs a{static_cast<const uint16_t*>(t->q_dev), t->q_stride_row, t->q_stride_head, t->lse_dev, t->rows_dev, t->begin_dev, t->n_list, t->n_rows, t->n_heads,
-                      group, layer, weights->base_dev + (int64_t)layer * weights->stride_layer, weights->stride_row, weights->stride_head, weights->n_pos, decay, scale};
+                      group, layer, weights->base_dev + (int64_t)layer * weights->stride_layer, weights->stride_row, weights->stride_head, weights->n_pos, decay, scale, nullptr, nullptr};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (many) {
+        if (launch_weigh_many(p, b, a, workspace_dev, pool->dtype == PLC_OUT_BF16, status_dev, st) != cudaSuccess) return PLC_E_CUDA;
+        count_launch(2);
+        return PLC_OK;
+    }
     if ((pool->dtype == PLC_OUT_F16 ? launch_weigh<__half>(p, b, a, status_dev, st) : launch_weigh<__nv_bfloat16>(p, b, a, status_dev, st)) != cudaSuccess) return PLC_E_CUDA;
     count_launch(1);
     return PLC_OK;

@@ -81,7 +81,7 @@ def _lib():
                             ("plc_tree_attention", [P, I, P, P, F, P, U, P, P]), ("plc_tree_attention_workspace", [P, I, I, I, P]),
                             ("plc_beam_select", [P, I, L, I, I, I, P, P, I, I, P, P, P, P, U, P]), ("plc_beam_workspace", [I, I, I, I, P]),
                             ("plc_beam_reorder", [P, I, P, I, I, P, P]), ("plc_rotary_apply", [P, P, I, P, I, I, I, I, P]), ("plc_pages_append", [P, I, P, P, P, P, P]),
-                            ("plc_pages_weigh", [P, I, P, P, F, F, P, P, P]), ("plc_pages_evict", [P, P, P, P, I, I, P, P, P, U, P, P]),
+                            ("plc_pages_weigh", [P, I, P, P, F, F, P, P, U, P, P]), ("plc_pages_weigh_workspace", [P, I, I, I, P]), ("plc_pages_evict", [P, P, P, P, I, I, P, P, P, U, P, P]),
                             ("plc_pages_evict_workspace", [P, I, I, P]), ("plc_token_logprobs", [P, I, L, I, I, P, I, I, P, P, P, P, P, U, P, P]),
                             ("plc_token_logprobs_workspace", [I, I, I, P])):
             getattr(api, name).argtypes = types
@@ -378,6 +378,7 @@ class PagePool:
         weight = decay * weight + sum of exp(scale q.k - lse).  q [N][heads][d] and lse [N][heads] as tree_attention had and left them.  Session s has the
         entries begin[s] .. begin[s+1]-1, which stand at its last positions (the book after keep); entry e is row e of q and lse, or row rows[e] (int32; -1: none):
         the accepted ones of a draft.  decay 0: nothing of the old weights is read."""
+        import torch
         where, dev, api = "plc_pages_weigh", self.device, _lib()
         a = self._book(book, where)
         _need(q.dim() == 3, E_SHAPE, where)
@@ -394,8 +395,18 @@ class PagePool:
         w = self._weights(weight, book, where)
         if n_list == 0:
             return weight
+        need = self._need_bytes.get((book.rows, heads, n_list, "weigh"))
+        if need is None:
+            b = C.c_uint64()
+            with torch.cuda.device(dev):
+                _check(api.plc_pages_weigh_workspace(self._by, book.rows, heads, n_list, C.byref(b)), "plc_pages_weigh_workspace")
+            if len(self._need_bytes) >= 4096:
+                self._need_bytes.clear()
+            need = self._need_bytes[(book.rows, heads, n_list, "weigh")] = b.value
+        ws = torch.empty(need, dtype=torch.uint8, device=dev)
         t = WeighQueries(q.data_ptr(), row, head, lse.data_ptr(), None if rows is None else rows.data_ptr(), begin.data_ptr(), N, n_list, heads)
-        _check(_run(dev, api.plc_pages_weigh, self._by, layer, a, C.byref(t), d ** -0.5 if scale is None else scale, decay, C.byref(w), self._word), where)
+        _check(_run(dev, api.plc_pages_weigh, self._by, layer, a, C.byref(t), d ** -0.5 if scale is None else scale, decay, C.byref(w), ws.data_ptr(), need,
+                    self._word), where)
         return weight
 
     def evict(self, book, weight, budget, recent=0):
