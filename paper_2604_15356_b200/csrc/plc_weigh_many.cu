@@ -86,6 +86,29 @@ template <int D> struct Walk {
     __device__ __forceinline__ int cols(const WeighArgs& a) const { return min(M::rows, x.n * a.group - rt * M::rows); }
 };
 
+// Adds the exponentials of 32 columns' scores.  PLAIN: all of them count; else columns before `first_row` do not, nor those whose row counts for nothing, so
+// that a key of infinities or NaN shows in the rows that see it alone.
+template <bool PLAIN>
+__device__ __forceinline__ void add_up(const uint32_t (&r)[32], const float* neg, unsigned long long c2, int first_row, unsigned long long (&acc)[4]) {
+#pragma unroll
+    for (int k = 0; k < 32; k += 4) {
+        const float4 n = *reinterpret_cast<const float4*>(neg + k);
+        float e[4];
+        unpack2(fma2(pack2(__uint_as_float(r[k]), __uint_as_float(r[k + 1])), c2, pack2(n.x, n.y)), e[0], e[1]);
+        unpack2(fma2(pack2(__uint_as_float(r[k + 2]), __uint_as_float(r[k + 3])), c2, pack2(n.z, n.w)), e[2], e[3]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) e[j] = exp2_approx(e[j]);
+        if (!PLAIN) {
+            const float nn[4] = {n.x, n.y, n.z, n.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (k + j < first_row || isinf(nn[j])) e[j] = 0.f;
+        }
+        acc[k >> 1 & 2] = add2(acc[k >> 1 & 2], pack2(e[0], e[1]));
+        acc[(k >> 1 & 2) + 1] = add2(acc[(k >> 1 & 2) + 1], pack2(e[2], e[3]));
+    }
+}
+
 template <class T, int D>
 __global__ void __launch_bounds__(Many<D>::threads, 1) weigh_many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b, const __grid_constant__ WeighArgs a,
                                                                          uint32_t* status) {
@@ -193,42 +216,33 @@ __global__ void __launch_bounds__(Many<D>::threads, 1) weigh_many_kernel(const _
             const uint32_t* odd = none + (int)(i & (kRing - 1)) * 4;
             const int last_t = w.pt * M::pos + M::pos - 1;
             const bool plain = !(odd[0] | odd[1] | odd[2] | odd[3]) && (long long)(last_t - (w.x.len - w.x.n)) * a.group <= row0;
-            const int chunks = (cols + 31) / 32;
-            float part[4] = {0.f, 0.f, 0.f, 0.f};
             unsigned long long acc[4] = {0ull, 0ull, 0ull, 0ull};
-#pragma unroll 1
-            for (int ch = 0; ch < chunks; ++ch) {
-                uint32_t r[32];
-                tmem_ld32(s_at + buf * M::groups * M::rows + ch * 32, r);
-                wait_ld(r);
+            const uint32_t at = s_at + buf * M::groups * M::rows;
+            if (plain && cols == M::rows) {       // the next columns come while these are summed
+                uint32_t r[2][32];
+                tmem_ld32(at, r[0]);
 #pragma unroll
-                for (int k = 0; k < 32; k += 4) {
-                    const float4 n = *reinterpret_cast<const float4*>(l + ch * 32 + k);
-                    float e[4];
-                    unpack2(fma2(pack2(__uint_as_float(r[k]), __uint_as_float(r[k + 1])), c2, pack2(n.x, n.y)), e[0], e[1]);
-                    unpack2(fma2(pack2(__uint_as_float(r[k + 2]), __uint_as_float(r[k + 3])), c2, pack2(n.z, n.w)), e[2], e[3]);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) e[j] = exp2_approx(e[j]);
-                    if (!plain) {                 // a key of infinities or NaN shows in the rows that count and see it alone
-                        const float nn[4] = {n.x, n.y, n.z, n.w};
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            if (ch * 32 + k + j < first_row || isinf(nn[j])) e[j] = 0.f;
-                    }
-                    acc[(k >> 1) & 2] = add2(acc[(k >> 1) & 2], pack2(e[0], e[1]));
-                    acc[(k >> 1 & 2) + 1] = add2(acc[(k >> 1 & 2) + 1], pack2(e[2], e[3]));
+                for (int ch = 0; ch < M::rows / 32; ++ch) {
+                    wait_ld(r[ch & 1]);
+                    if (ch + 1 < M::rows / 32) tmem_ld32(at + ch * 32 + 32, r[(ch + 1) & 1]);
+                    add_up<true>(r[ch & 1], l + ch * 32, c2, 0, acc);
+                }
+            } else {
+                for (int ch = 0; ch < (cols + 31) / 32; ++ch) {
+                    uint32_t r[32];
+                    tmem_ld32(at + ch * 32, r);
+                    wait_ld(r);
+                    add_up<false>(r, l + ch * 32, c2, first_row - ch * 32, acc);
                 }
             }
             fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(s_empty + 8 * buf);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            {
                 float lo, hi;
-                unpack2(acc[j], lo, hi);
-                part[j] = lo + hi;
+                unpack2(add2(add2(acc[0], acc[1]), add2(acc[2], acc[3])), lo, hi);
+                sum += lo + hi;
             }
-            sum += (part[0] + part[1]) + (part[2] + part[3]);
             const Newest x = w.x;
             const int s = w.s, h = w.h, ended = w.rt + 1 == w.row_tiles, words = item & (kRing - 1);
             const bool other = w.next(p, b, a);
