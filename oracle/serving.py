@@ -225,19 +225,19 @@ def weigh(q, lse, k_of, length, begin, rows, scale, decay, weight):
             continue
         start = int(length[s]) - len(entries)
         for h in range(H):
+            rowed = [(j, e if rows is None else int(rows[e])) for j, e in enumerate(entries)]
+            terms = [(j, r, g) for j, r in rowed if 0 <= r < q.shape[0] for g in range(h * G, (h + 1) * G) if not math.isinf(lse[r, g])]
+            stands = np.array([start + j for j, _, _ in terms])
+            z = np.array([q[r, g] for _, r, g in terms]).reshape(len(terms), q.shape[2])
+            l = np.array([float(lse[r, g]) for _, r, g in terms])
             for t in range(min(int(length[s]), T)):
-                total = far = 0.0
                 key = k_of(s, h, t)
-                for j, e in enumerate(entries):
-                    r = e if rows is None else int(rows[e])
-                    if not 0 <= r < q.shape[0] or t > start + j or key is None:
-                        continue
-                    for g in range(h * G, (h + 1) * G):
-                        if math.isinf(lse[r, g]):
-                            continue
-                        w = math.exp(scale * float(q[r, g] @ key) - float(lse[r, g]))
-                        total += w
-                        far += w * (scale * float(np.abs(q[r, g]) @ np.abs(key)) * (len(key) + 2) + 2 * abs(float(lse[r, g])))
+                total = far = 0.0
+                if key is not None and len(terms):
+                    sees = stands >= t
+                    w = np.exp(scale * (z[sees] @ key) - l[sees])
+                    total = float(w.sum())
+                    far = float(w @ (scale * (np.abs(z[sees]) @ np.abs(key)) * (len(key) + 2) + 2 * np.abs(l[sees])))
                 old = decay * float(out[s, h, t]) if t < start and decay else 0.0
                 out[s, h, t] = old + total
                 reach[s, h, t] = far

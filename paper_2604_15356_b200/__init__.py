@@ -40,7 +40,7 @@ def build(force=False, verbose=False):
     """Compile libplc.so for sm_100a with nvcc (in-tree)."""
     srcs = sources()
     deps = srcs + [os.path.join(_CSRC, h) for h in ("plc_common.cuh", "plc_coder.cuh", "plc_codec.cuh", "plc_pages.cuh", "plc_attend.cuh", "plc_attend_few.cuh",
-                                                        "plc_attend_many.cuh", "plc_logits.cuh", "plc_tensor.cuh", "plc_weigh.cuh")] + [os.path.join(_INC, "plc.h")]
+                                                        "plc_attend_many.cuh", "plc_logits.cuh", "plc_tensor.cuh", "plc_weigh.cuh", "plc_boxes.cuh")] + [os.path.join(_INC, "plc.h")]
     if not force and os.path.exists(_SO) and all(os.path.getmtime(_SO) >= os.path.getmtime(d) for d in deps):
         return _SO
     cmd = ["nvcc", "-t", "0", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

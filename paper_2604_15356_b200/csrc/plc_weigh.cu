@@ -203,7 +203,7 @@ plc_status plc_pages_weigh(const plc_page_pool* pool, int32_t layer, const plc_p
     if (workspace_bytes < (many ? weigh_many_bytes() : 16)) return PLC_E_CAPACITY;
     if (t->n_list == 0) return PLC_OK;
     const WeighArgs a{static_cast<const uint16_t*>(t->q_dev), t->q_stride_row, t->q_stride_head, t->lse_dev, t->rows_dev, t->begin_dev, t->n_list, t->n_rows, t->n_heads,
-                      group, layer, weights->base_dev + (int64_t)layer * weights->stride_layer, weights->stride_row, weights->stride_head, weights->n_pos, decay, scale, nullptr, nullptr};
+                      group, layer, weights->base_dev + (int64_t)layer * weights->stride_layer, weights->stride_row, weights->stride_head, weights->n_pos, decay, scale, nullptr, nullptr, 0, {}, 0};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (many) {
         if (launch_weigh_many(p, b, a, workspace_dev, pool->dtype == PLC_OUT_BF16, status_dev, st) != cudaSuccess) return PLC_E_CUDA;

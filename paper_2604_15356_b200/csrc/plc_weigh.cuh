@@ -12,6 +12,8 @@ struct WeighArgs {
     float decay, scale;
     int4* first;                                  // [grid]: session, head, position tile of a CTA's range (-1: none), row tiles of that item before it
     float* part;                                  // [2 * grid][positions of a tile] sums of items that more than one CTA has
+    int box_pos, box_dim[4];                      // keys come in boxes of so many positions (0: in pieces of 16 bytes); what dimensions 1 .. 4 of their map are
+    int q_boxes;                                  // the queries of a row tile are one box
 };
 
 uint64_t weigh_many_bytes();

@@ -7,6 +7,7 @@
 //
 // Work: all (session, head, position tile, row tile) form one sequence, cut into equal ranges, one a CTA.  The first and the last piece of a range may be parts of an
 // item (session, head, position tile); those leave their sums in the workspace, and a second launch adds them in a fixed order.
+#include "plc_boxes.cuh"
 #include "plc_tensor.cuh"
 #include "plc_weigh.cuh"
 
@@ -17,7 +18,9 @@ constexpr float kLog2e = 1.44269504088896f;
 // Row tiles whose normalisers, and items whose positions, are kept: the copies run up to four of them ahead of the exponentials.
 constexpr int kRing = 8;
 
-template <int D> struct Many {
+// DEEP: many row tiles an item, so that the queries' ring is what counts; else keys of the next item arrive while this one's are used.
+template <int D, bool DEEP> struct Many {
+    static constexpr int k_slots = DEEP ? 1 : 2, q_slots = DEEP ? 4 : 2;
     static constexpr int blocks = (D + 63) / 64;                       // 128-byte wide column blocks (32 components: half of one)
     static constexpr int groups = D == 256 ? 1 : 2, pos = 128 * groups;  // positions of a tile; four warps for each 128
     static constexpr int rows = D == 256 ? 64 : 128;                   // of a row tile
@@ -25,13 +28,13 @@ template <int D> struct Many {
     static constexpr int soft = 128 * groups, copy = 128, threads = soft + copy + 32;
     static constexpr int tmem = 2 * groups * rows;                     // S twice
     static constexpr int words = pos / 32;
-    static constexpr size_t used = 2 * (size_t)k_bytes + 2 * q_bytes + 2 * pos * 8 + 2 * rows * 8 + kRing * (rows + words + 4) * 4 + 256 + 1024;
+    static constexpr size_t used = k_slots * (size_t)k_bytes + q_slots * q_bytes + kRing * (rows + words + 4) * 4 + 256 + 1024;
     static constexpr size_t smem = used > 120 * 1024 ? used : 120 * 1024;                    // one CTA an SM: it takes the tensor memory
 };
 
 // Where a CTA's range stands: item (session, head, position tile) and row tile in it.
-template <int D> struct Walk {
-    using M = Many<D>;
+template <int D, bool DEEP> struct Walk {
+    using M = Many<D, DEEP>;
     int s, h, pt, rt, tiles, row_tiles;
     Newest x;
     // the first row tile that sees any of position tile pt
@@ -86,6 +89,12 @@ template <int D> struct Walk {
     __device__ __forceinline__ int cols(const WeighArgs& a) const { return min(M::rows, x.n * a.group - rt * M::rows); }
 };
 
+// Waits, for so long at most, until a barrier's phase is complete.
+__device__ __noinline__ void land(uint32_t bar, uint32_t parity) {
+    for (uint32_t k = 0; k < kSpin; ++k)
+        if (mbar_done(bar, parity)) break;
+}
+
 // Adds the exponentials of 32 columns' scores.  PLAIN: all of them count; else columns before `first_row` do not, nor those whose row counts for nothing, so
 // that a key of infinities or NaN shows in the rows that see it alone.
 template <bool PLAIN>
@@ -109,35 +118,38 @@ __device__ __forceinline__ void add_up(const uint32_t (&r)[32], const float* neg
     }
 }
 
-template <class T, int D>
-__global__ void __launch_bounds__(Many<D>::threads, 1) weigh_many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b, const __grid_constant__ WeighArgs a,
-                                                                         uint32_t* status) {
-    using M = Many<D>;
-    constexpr int pieces = D / 8, copy_warp = M::soft / 32, mma_warp = copy_warp + M::copy / 32;
+template <class T, int D, bool DEEP>
+__global__ void __launch_bounds__(Many<D, DEEP>::threads, 1) weigh_many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b, const __grid_constant__ WeighArgs a,
+                                                                         const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap q_map, uint32_t* status) {
+    using M = Many<D, DEEP>;
+    constexpr int QS = M::q_slots, KS = M::k_slots, pieces = D / 8, copy_warp = M::soft / 32, mma_warp = copy_warp + M::copy / 32;
     extern __shared__ uint8_t smem_raw[];
     __shared__ long long sums[M::threads / 32];
     __shared__ long long range_at[2];
     uint8_t* ks = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint8_t* qs = ks + 2 * M::k_bytes;
-    uint64_t* k_from = reinterpret_cast<uint64_t*>(qs + 2 * M::q_bytes);       // [2][pos] where a position's key stands
-    uint64_t* q_from = k_from + 2 * M::pos;                                    // [2][rows] where a row stands
-    float* neg = reinterpret_cast<float*>(q_from + 2 * M::rows);               // [kRing][rows] - lse log2 e; -inf: no row
+    uint8_t* qs = ks + KS * M::k_bytes;
+    float* neg = reinterpret_cast<float*>(qs + QS * M::q_bytes);                // [kRing][rows] - lse log2 e; -inf: no row
     uint32_t* there = reinterpret_cast<uint32_t*>(neg + kRing * M::rows);          // [kRing][words] positions that have a page
     uint32_t* none = there + kRing * M::words;                                     // [kRing][4] row tiles with rows that count for nothing
     uint64_t* bars = reinterpret_cast<uint64_t*>(none + kRing * 4);
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 12);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 12 + 2 * QS);
     volatile uint32_t* failed = tmem_slot + 1;
     const int tid = threadIdx.x, wid = tid >> 5, lane = tid & 31;
-    const uint32_t k_full = smem_u32(bars), k_empty = k_full + 16, q_full = k_full + 32, q_empty = k_full + 48, s_full = k_full + 64, s_empty = k_full + 80;
+    const uint32_t k_full = smem_u32(bars), k_empty = k_full + 16, s_full = k_full + 32, s_empty = k_full + 64, q_full = k_full + 96,
+                   q_empty = q_full + 8 * QS;
     chain_next();
     if (tid == 0) {
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(k_full + 8 * i, M::copy + M::copy / 32);
-            mbar_init(k_empty + 8 * i, 1);
-            mbar_init(q_full + 8 * i, M::copy + M::copy / 32);
+        for (int i = 0; i < QS; ++i) {
+            mbar_init(q_full + 8 * i, M::copy / 32 + (a.q_boxes ? 1 : M::copy));
             mbar_init(q_empty + 8 * i, 1);
-            mbar_init(s_full + 8 * i, 1);
-            mbar_init(s_empty + 8 * i, M::soft / 32);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(k_full + 8 * i, a.box_pos ? 1 : M::copy + M::copy / 32);
+            mbar_init(k_empty + 8 * i, 1);
+            for (int m = 0; m < M::groups; ++m) {
+                mbar_init(s_full + 8 * (2 * m + i), 1);
+                mbar_init(s_empty + 8 * (2 * m + i), 4);
+            }
         }
         *failed = 0u;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -147,7 +159,7 @@ __global__ void __launch_bounds__(Many<D>::threads, 1) weigh_many_kernel(const _
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     // ---- the range: a thread sums the steps of a run of sessions, the threads' sums are scanned
-    Walk<D> w{};
+    Walk<D, DEEP> w{};
     long long total = 0, mine = 0;
     const int run = (b.rows + M::threads - 1) / M::threads, s0 = min(b.rows, tid * run), s1 = min(b.rows, s0 + run);
     bool any_bad = false;
@@ -204,21 +216,24 @@ __global__ void __launch_bounds__(Many<D>::threads, 1) weigh_many_kernel(const _
         const unsigned long long c2 = pack2(c, c);
         float sum = 0.f;
         bool began = steps > 0 && w.rt == w.begin_of(a, w.pt);                 // the item's first row tile was this CTA's
-        int item = 0;
+        int item = 0, first_row = 0, full_row = 0;                             // the rows that see this thread's position, and all of the tile's
+        auto enter = [&]() {
+            const int start = w.x.len - w.x.n;
+            first_row = max(w.pt * M::pos + pos - start, 0) * a.group;         // (at most the session's rows)
+            full_row = max(w.pt * M::pos + M::pos - 1 - start, 0) * a.group;
+        };
+        if (steps > 0) enter();
+        const uint32_t full = s_full + 16 * group, empty = s_empty + 16 * group;
         for (long long i = 0; i < steps; ++i) {
-            const int buf = (int)(i & 1), cols = w.cols(a), t = w.pt * M::pos + pos;
-            const int row0 = w.rt * M::rows;
-            // columns from this one on see the position
-            const int first_row = (int)min(max((long long)(t - (w.x.len - w.x.n)) * a.group - row0, 0ll), (long long)M::rows);
-            if (!__all_sync(kFull, mbar_wait(s_full + 8 * buf, (uint32_t)(i >> 1) & 1u, failed, status))) break;
+            const int buf = (int)i & 1, ring = (int)i & (kRing - 1), row0 = w.rt * M::rows;
+            if (!__all_sync(kFull, mbar_wait(full + 8 * buf, (uint32_t)(i >> 1) & 1u, failed, status))) break;
             fence_after();
-            const float* l = neg + (int)(i & (kRing - 1)) * M::rows;
-            const uint32_t* odd = none + (int)(i & (kRing - 1)) * 4;
-            const int last_t = w.pt * M::pos + M::pos - 1;
-            const bool plain = !(odd[0] | odd[1] | odd[2] | odd[3]) && (long long)(last_t - (w.x.len - w.x.n)) * a.group <= row0;
+            const float* l = neg + ring * M::rows;
+            const uint4 odd = *reinterpret_cast<const uint4*>(none + ring * 4);
+            const bool plain = (odd.x | odd.y | odd.z | odd.w) == 0 && full_row <= row0;
             unsigned long long acc[4] = {0ull, 0ull, 0ull, 0ull};
             const uint32_t at = s_at + buf * M::groups * M::rows;
-            if (plain && cols == M::rows) {       // the next columns come while these are summed
+            if (plain) {                          // (rows behind the session's last one count for nothing)       // the next columns come while these are summed
                 uint32_t r[2][32];
                 tmem_ld32(at, r[0]);
 #pragma unroll
@@ -228,146 +243,187 @@ __global__ void __launch_bounds__(Many<D>::threads, 1) weigh_many_kernel(const _
                     add_up<true>(r[ch & 1], l + ch * 32, c2, 0, acc);
                 }
             } else {
-                for (int ch = 0; ch < (cols + 31) / 32; ++ch) {
+                for (int ch = 0; ch < (w.cols(a) + 31) / 32; ++ch) {
                     uint32_t r[32];
                     tmem_ld32(at + ch * 32, r);
                     wait_ld(r);
-                    add_up<false>(r, l + ch * 32, c2, first_row - ch * 32, acc);
+                    add_up<false>(r, l + ch * 32, c2, first_row - row0 - ch * 32, acc);
                 }
             }
             fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(s_empty + 8 * buf);
+            if (lane == 0) mbar_arrive(empty + 8 * buf);
             {
                 float lo, hi;
                 unpack2(add2(add2(acc[0], acc[1]), add2(acc[2], acc[3])), lo, hi);
                 sum += lo + hi;
             }
-            const Newest x = w.x;
-            const int s = w.s, h = w.h, ended = w.rt + 1 == w.row_tiles, words = item & (kRing - 1);
-            const bool other = w.next(p, b, a);
+            const bool ended = w.rt + 1 == w.row_tiles;
             if (ended || i + 1 == steps) {
+                const bool have = there[(item & (kRing - 1)) * M::words + (pos >> 5)] >> lane & 1u;
+                const int t = w.pt * M::pos + pos;
                 if (began && ended) {
-                    if (t < x.len) put_weight(a, x, s, h, t, sum, there[words * M::words + (pos >> 5)] >> lane & 1u, status);
-                } else a.part[((int64_t)2 * me + (item ? 1 : 0)) * M::pos + pos] = there[words * M::words + (pos >> 5)] >> lane & 1u ? sum : 0.f;
+                    if (t < w.x.len) put_weight(a, w.x, w.s, w.h, t, sum, have, status);
+                } else a.part[((int64_t)2 * me + (item ? 1 : 0)) * M::pos + pos] = have ? sum : 0.f;
                 sum = 0.f;
                 began = true;
             }
-            item += other;
+            if (w.next(p, b, a)) {
+                ++item;
+                if (i + 1 < steps) enter();
+            }
         }
     } else if (wid < mma_warp) {
-        // ---- copies, four warps: keys at the start of an item, queries for every row tile
-        const int lt = tid - M::soft;
-        constexpr int step = M::copy / pieces > 0 ? M::copy / pieces : 1;      // vectors a round
-        const int cc = lt % pieces, r0 = lt / pieces;
-        const uint32_t to = (cc >> 3) * 128, k_s = smem_u32(ks), q_s = smem_u32(qs);
+        // ---- copies, four warps that do not wait for each other: keys at the start of an item, queries for every row tile.  Boxes are issued by the first
+        // warp; pieces of 16 bytes by all, a warp a quarter of the vectors.
+        const int lt = tid - M::soft, cw = wid - copy_warp;
+        const uint32_t k_s = smem_u32(ks), q_s = smem_u32(qs);
         bool fresh = true, ok = true;
-        int item = 0;
-        // this thread's row of a row tile, looked up a tile ahead
-        uint64_t row_at = 0;
-        float row_neg = 0.f;
-        auto look_up = [&](const Walk<D>& v) {
+        int item = 0, k_last = -1;
+        long long q_last = -1;                    // the last item, and row tile, whose boxes have been issued
+        // this thread's row of a row tile; its log-sum-exp is loaded a tile ahead
+        int row = -1;
+        const uint16_t* row_q = nullptr;
+        float row_lse = 0.f;
+        auto look_up = [&](const Walk<D, DEEP>& v) {
             const int r = v.rt * M::rows + lt;
-            row_at = 0;
-            row_neg = -INFINITY;
+            row = -1;
             if (lt < M::rows && r < v.x.n * a.group) {
                 const int entry = r / a.group, head = v.h * a.group + r - entry * a.group;
-                const int row = a.rows ? a.rows[v.x.first + entry] : v.x.first + entry;
-                if (row >= 0 && row < a.n_rows) {
-                    const float l = a.lse[(int64_t)row * a.heads + head];
-                    if (!isinf(l)) {
-                        row_neg = -l * kLog2e;
-                        row_at = reinterpret_cast<uint64_t>(a.q + (int64_t)row * a.qs_row + (int64_t)head * a.qs_head);
-                    }
-                } else if (row != -1) atomicOr(status, kStRange);
+                row = a.rows ? a.rows[v.x.first + entry] : v.x.first + entry;
+                if (row < -1 || row >= a.n_rows) { atomicOr(status, kStRange); row = -1; }
+                if (row >= 0) {
+                    row_lse = a.lse[(int64_t)row * a.heads + head];
+                    row_q = a.q + (int64_t)row * a.qs_row + (int64_t)head * a.qs_head;
+                }
+            }
+        };
+        auto page_of = [&](int t) -> int {        // of a position of the item; -1: none
+            if (t >= w.x.len) return -1;
+            const int page = b.table[(int64_t)w.s * b.max_pages + t / p.page_pos];
+            if (page >= 0 && page < p.n_pages) return page;
+            atomicOr(status, kStRange);
+            return -1;
+        };
+        // N vectors that the lanes know the addresses of (0: none) into rows v0 ... of a block of `all` vectors
+        auto pieces_of = [&](uint64_t at, int n, uint32_t to, int v0, int all) {
+#pragma unroll 4
+            for (int u = lane; u < n * pieces; u += 32) {
+                const int v = u / pieces, c = u % pieces, r = v0 + v;
+                const uint64_t from = __shfl_sync(kFull, at, v);
+                copy16(to + (c >> 3) * (all * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4), from ? reinterpret_cast<const uint8_t*>(from) + c * 16 : p.base, from != 0);
             }
         };
         if (steps > 0) look_up(w);
         for (long long i = 0; i < steps; ++i) {
-            const int buf = (int)(i & 1), kb = item & 1;
-            if (lt < M::rows) {
-                q_from[buf * M::rows + lt] = row_at;
-                neg[(int)(i & (kRing - 1)) * M::rows + lt] = row_neg;
-            }
+            const int qb = (int)i & (QS - 1), kb = item & (KS - 1), ring = (int)i & (kRing - 1);
+            const uint64_t row_at = row >= 0 && !isinf(row_lse) ? reinterpret_cast<uint64_t>(row_q) : 0ull;
+            if (lt < M::rows) neg[ring * M::rows + lt] = row_at ? -row_lse * kLog2e : -INFINITY;
             const uint32_t odd = __ballot_sync(kFull, lt < M::rows && row_at == 0);
-            if (lane == 0) none[(int)(i & (kRing - 1)) * 4 + (wid - copy_warp)] = odd;
-            if (fresh) {
-#pragma unroll
-                for (int g = 0; g < M::groups; ++g) {
-                    const int k = g * 128 + lt, t = w.pt * M::pos + k;
-                    uint64_t at = 0;
-                    if (t < w.x.len) {
-                        const int page = b.table[(int64_t)w.s * b.max_pages + t / p.page_pos];
-                        if (page >= 0 && page < p.n_pages)
-                            at = reinterpret_cast<uint64_t>(p.base + (int64_t)a.layer * p.sl + (int64_t)w.h * p.sh + (int64_t)page * p.spage + (int64_t)(t % p.page_pos) * p.sp);
-                        else atomicOr(status, kStRange);
+            if (lane == 0) none[ring * 4 + cw] = odd;
+            if (fresh && a.box_pos) {
+                if (cw == 0) {
+                    const int boxes = M::pos / a.box_pos, t = w.pt * M::pos + lane * a.box_pos, page = lane < boxes ? page_of(t) : -1;
+                    const uint32_t have = __ballot_sync(kFull, page >= 0);
+                    if (lane < M::words) {        // 32 positions' words
+                        uint32_t word = 0;
+                        if (a.box_pos >= 32) word = have >> (lane * 32 / a.box_pos) & 1u ? ~0u : 0u;
+                        else
+                            for (int e = 0; e < 32 / a.box_pos; ++e)
+                                if (have >> (lane * (32 / a.box_pos) + e) & 1u) word |= ((1u << a.box_pos) - 1u) << (e * a.box_pos);
+                        there[(item & (kRing - 1)) * M::words + lane] = word;
                     }
-                    k_from[kb * M::pos + k] = at;
-                    const uint32_t have = __ballot_sync(kFull, at != 0);
+                    __syncwarp();
+                    ok = __all_sync(kFull, ok && mbar_wait(k_empty + 8 * kb, ((uint32_t)(item / KS) & 1u) ^ 1u, failed, status));
+                    if (!ok) break;
+                    if (lane == 0)
+                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(k_full + 8 * kb), "r"(__popc(have) * a.box_pos * M::blocks * 128) : "memory");
+                    __syncwarp();
+                    if (page >= 0) {
+                        int c[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) c[k] = a.box_dim[k] == 0 ? t % p.page_pos : a.box_dim[k] == 1 ? w.h : a.box_dim[k] == 2 ? page : 0;
+#pragma unroll
+                        for (int k = 0; k < M::blocks; ++k)
+                            asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(
+                                             k_s + kb * M::k_bytes + k * (M::pos * 128) + lane * a.box_pos * 128),
+                                         "l"(&k_map), "r"(k * 64), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]), "r"(k_full + 8 * kb)
+                                         : "memory");
+                    }
+                    k_last = item;
+                }
+            } else if (fresh) {
+                uint64_t at[M::pos / 128];
+#pragma unroll
+                for (int g = 0; g < M::pos / 128; ++g) {
+                    const int k = cw * (M::pos / 4) + g * 32 + lane, t = w.pt * M::pos + k, page = page_of(t);
+                    at[g] = page < 0 ? 0ull
+                                     : reinterpret_cast<uint64_t>(p.base + (int64_t)a.layer * p.sl + (int64_t)w.h * p.sh + (int64_t)page * p.spage + (int64_t)(t % p.page_pos) * p.sp);
+                    const uint32_t have = __ballot_sync(kFull, page >= 0);
                     if (lane == 0) there[(item & (kRing - 1)) * M::words + (k >> 5)] = have;
                 }
+                ok = __all_sync(kFull, ok && mbar_wait(k_empty + 8 * kb, ((uint32_t)(item / KS) & 1u) ^ 1u, failed, status));
+                if (!ok) break;
+#pragma unroll
+                for (int g = 0; g < M::pos / 128; ++g) pieces_of(at[g], 32, k_s + kb * M::k_bytes, cw * (M::pos / 4) + g * 32, M::pos);
+                mbar_arrive_copies(k_full + 8 * kb);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(k_full + 8 * kb);
             }
-            asm volatile("bar.sync 1, %0;" ::"n"(M::copy) : "memory");
-            if (fresh) {
-                ok = __all_sync(kFull, ok && mbar_wait(k_empty + 8 * kb, ((uint32_t)(item >> 1) & 1u) ^ 1u, failed, status));
-                if (ok) {
-#pragma unroll 8
-                    for (int r = r0; r < M::pos; r += step) {
-                        const uint64_t at = k_from[kb * M::pos + r];
-                        copy16(k_s + kb * M::k_bytes + to * M::pos + r * 128 + (((cc & 7) ^ (r & 7)) << 4), at ? reinterpret_cast<const uint8_t*>(at) + cc * 16 : p.base, at != 0);
-                    }
-                    mbar_arrive_copies(k_full + 8 * kb);
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(k_full + 8 * kb);
-                }
-            }
-            const int cols = w.cols(a);
+            const int cols = w.cols(a), q_row = w.x.first + w.rt * (M::rows / a.group), q_head = w.h * a.group;
             fresh = w.next(p, b, a);
             item += fresh;
             if (i + 1 < steps) look_up(w);
-            ok = __all_sync(kFull, ok && mbar_wait(q_empty + 8 * buf, ((uint32_t)(i >> 1) & 1u) ^ 1u, failed, status));
-            if (ok) {
-                const int upto = min(M::rows, (cols + 15) & ~15);
-#pragma unroll 8
-                for (int r = r0; r < upto; r += step) {
-                    const uint64_t at = q_from[buf * M::rows + r];
-                    copy16(q_s + buf * M::q_bytes + to * M::rows + r * 128 + (((cc & 7) ^ (r & 7)) << 4), at ? reinterpret_cast<const uint8_t*>(at) + cc * 16 : p.base, at != 0);
+            ok = __all_sync(kFull, ok && mbar_wait(q_empty + 8 * qb, ((uint32_t)(i / QS) & 1u) ^ 1u, failed, status));
+            if (!ok) break;
+            if (a.q_boxes) {
+                if (cw == 0 && lane == 0) {
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(q_full + 8 * qb), "r"(M::q_bytes) : "memory");
+#pragma unroll
+                    for (int k = 0; k < M::blocks; ++k)
+                        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+                                         q_s + qb * M::q_bytes + k * (M::rows * 128)),
+                                     "l"(&q_map), "r"(k * 64), "r"(q_head), "r"(q_row), "r"(q_full + 8 * qb)
+                                     : "memory");
                 }
-                mbar_arrive_copies(q_full + 8 * buf);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(q_full + 8 * buf);
+                q_last = i;
+            } else {
+                if (cw * 32 < M::rows && cw * 32 < cols) pieces_of(row_at, 32, q_s + qb * M::q_bytes, cw * 32, M::rows);
+                mbar_arrive_copies(q_full + 8 * qb);
             }
-            // (all four warps go on to the next barrier, so that none waits there alone; each leaves once all see that somebody has given up)
-            uint32_t stop;
-            asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, 2, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-                         : "=r"(stop) : "r"((uint32_t)!ok), "n"(M::copy) : "memory");
-            if (stop) break;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_full + 8 * qb);
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
+        if (!ok && cw == 0) {                     // boxes still in flight (none after a complete run) land before the CTA ends
+            for (int k = max(0, k_last - KS + 1); k <= k_last; ++k) land(k_full + 8 * (k & (KS - 1)), (uint32_t)(k / KS) & 1u);
+            for (long long k = max(0ll, q_last - QS + 1); k <= q_last; ++k) land(q_full + 8 * ((int)k & (QS - 1)), (uint32_t)(k / QS) & 1u);
+        }
     } else if (lane == 0) {
         // ---- products
         int item = 0;
         bool fresh = true, ok = true;
         for (long long i = 0; i < steps; ++i) {
-            const int buf = (int)(i & 1), kb = item & 1;
+            const int buf = (int)i & 1, qb = (int)i & (QS - 1), kb = item & (KS - 1);
             const uint32_t n = (uint32_t)min(M::rows, (w.cols(a) + 15) & ~15);
-            if (fresh) ok = ok && mbar_wait(k_full + 8 * kb, (uint32_t)(item >> 1) & 1u, failed, status);
-            ok = ok && mbar_wait(q_full + 8 * buf, (uint32_t)(i >> 1) & 1u, failed, status);
-            ok = ok && mbar_wait(s_empty + 8 * buf, ((uint32_t)(i >> 1) & 1u) ^ 1u, failed, status);
-            if (!ok) break;
+            if (fresh) ok = ok && mbar_wait(k_full + 8 * kb, (uint32_t)(item / KS) & 1u, failed, status);
+            ok = ok && mbar_wait(q_full + 8 * qb, (uint32_t)(i / QS) & 1u, failed, status);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            fence_after();
             const uint32_t id = (1u << 4) | (Kind<T>::format << 7) | (Kind<T>::format << 10) | (8u << 24) | ((n >> 3) << 17);
-            const uint64_t q_at = desc_k(smem_u32(qs) + buf * M::q_bytes);
+            const uint64_t q_at = desc_k(smem_u32(qs) + qb * M::q_bytes);
 #pragma unroll
             for (int m = 0; m < M::groups; ++m) {
+                ok = ok && mbar_wait(s_empty + 8 * (2 * m + buf), ((uint32_t)(i >> 1) & 1u) ^ 1u, failed, status);
+                if (!ok) break;
+                fence_after();
                 const uint64_t k_at = desc_k(smem_u32(ks) + kb * M::k_bytes + m * 128 * 128);
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k)
                     mma_ss(tmem + (buf * M::groups + m) * M::rows, k_at + (k >> 2) * (M::pos * 128 / 16) + 2 * (k & 3), q_at + (k >> 2) * (M::rows * 128 / 16) + 2 * (k & 3), id, k ? 1u : 0u);
+                mma_commit(s_full + 8 * (2 * m + buf));
             }
-            mma_commit(s_full + 8 * buf);
-            mma_commit(q_empty + 8 * buf);
+            if (!ok) break;
+            mma_commit(q_empty + 8 * qb);
             fresh = w.next(p, b, a);
             if (fresh) {
                 mma_commit(k_empty + 8 * kb);
@@ -386,9 +442,9 @@ __global__ void __launch_bounds__(Many<D>::threads, 1) weigh_many_kernel(const _
 // Adds the pieces of items that more than one CTA had: block c looks at the boundary between CTAs c - 1 and c, and takes the item if that is the first
 // boundary inside it.
 template <int D>
-__global__ void __launch_bounds__(Many<D>::pos) weigh_join_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b, const __grid_constant__ WeighArgs a, int workers,
+__global__ void __launch_bounds__(Many<D, true>::pos) weigh_join_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b, const __grid_constant__ WeighArgs a, int workers,
                                                                   uint32_t* status) {
-    using M = Many<D>;
+    using M = Many<D, true>;
     chain_wait();
     const int c = blockIdx.x + 1, pos = threadIdx.x;
     const int4 f = a.first[c], prev = a.first[c - 1];
@@ -407,22 +463,40 @@ __global__ void __launch_bounds__(Many<D>::pos) weigh_join_kernel(const __grid_c
     if (t < x.len) put_weight(a, x, f.x, f.y, t, sum, true, status);           // (a position without a page has sums of 0)
 }
 
-template <class T, int D>
-cudaError_t launch(const PoolDev& p, const BookDev& b, const WeighArgs& a, uint32_t* status, cudaStream_t st) {
-    using M = Many<D>;
-    cudaError_t e = cudaFuncSetAttribute(weigh_many_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)M::smem);
+// The queries of a row tile as one box: the heads of a group by as many rows as make up the tile.  Where rows are picked, the group does not divide the tile, or strides are not
+// positive, they come in pieces.
+template <int D> bool query_boxes(const WeighArgs& a, bool bf16, CUtensorMap* map) {
+    using M = Many<D, true>;
+    if (a.rows || D < 64 || M::rows % a.group || a.qs_row <= 0 || a.qs_head <= 0 || a.qs_row >= (1ll << 38) || a.qs_head >= (1ll << 38)) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)a.heads, (cuuint64_t)a.n_rows}, strides[2] = {(cuuint64_t)a.qs_head * 2, (cuuint64_t)a.qs_row * 2};
+    const cuuint32_t boxes[3] = {64, (cuuint32_t)a.group, (cuuint32_t)(M::rows / a.group)}, ones[3] = {1, 1, 1};
+    const EncodeTiledFn fn = encode_tiled_fn();
+    return fn && fn(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<uint16_t*>(a.q), dims, strides, boxes, ones,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <class T, int D, bool DEEP>
+cudaError_t launch(const PoolDev& p, const BookDev& b, const WeighArgs& args, uint32_t* status, cudaStream_t st) {
+    using M = Many<D, DEEP>;
+    cudaError_t e = cudaFuncSetAttribute(weigh_many_kernel<T, D, DEEP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)M::smem);
     if (e != cudaSuccess) return e;
+    WeighArgs a = args;
+    CUtensorMap k_map{}, q_map{};
+    const bool bf16 = Kind<T>::format == 1;
+    const int even = p.page_pos & -p.page_pos, box = even > 128 ? 128 : even;     // the largest power of two that divides a page, so that boxes fill a tile
+    a.box_pos = box >= 8 && page_boxes(p, a.layer, bf16, box, &k_map, a.box_dim) ? box : 0;
+    a.q_boxes = query_boxes<D>(a, bf16, &q_map);
     const int grid = sm_count();
-    e = launch_kernel(weigh_many_kernel<T, D>, grid, M::threads, M::smem, st, false, 1, p, b, a, status);
+    e = launch_kernel(weigh_many_kernel<T, D, DEEP>, grid, M::threads, M::smem, st, false, 1, p, b, a, k_map, q_map, status);
     return e != cudaSuccess ? e : launch_kernel(weigh_join_kernel<D>, grid - 1, M::pos, 0, st, true, 1, p, b, a, grid, status);
 }
-template <class T>
+template <class T, bool DEEP>
 cudaError_t launch_by_dim(const PoolDev& p, const BookDev& b, const WeighArgs& a, uint32_t* status, cudaStream_t st) {
     switch (p.d) {
-        case 32: return launch<T, 32>(p, b, a, status, st);
-        case 64: return launch<T, 64>(p, b, a, status, st);
-        case 128: return launch<T, 128>(p, b, a, status, st);
-        default: return launch<T, 256>(p, b, a, status, st);
+        case 32: return launch<T, 32, DEEP>(p, b, a, status, st);
+        case 64: return launch<T, 64, DEEP>(p, b, a, status, st);
+        case 128: return launch<T, 128, DEEP>(p, b, a, status, st);
+        default: return launch<T, 256, DEEP>(p, b, a, status, st);
     }
 }
 
@@ -434,7 +508,9 @@ cudaError_t launch_weigh_many(const PoolDev& p, const BookDev& b, const WeighArg
     WeighArgs a = args;
     a.first = static_cast<int4*>(workspace);
     a.part = reinterpret_cast<float*>(a.first + sm_count());
-    return bf16 ? launch_by_dim<__nv_bfloat16>(p, b, a, status, st) : launch_by_dim<__half>(p, b, a, status, st);
+    const bool deep = (long long)a.n_list * a.group > 512ll * b.rows;          // by the mean: from four row tiles a session on
+    if (deep) return bf16 ? launch_by_dim<__nv_bfloat16, true>(p, b, a, status, st) : launch_by_dim<__half, true>(p, b, a, status, st);
+    return bf16 ? launch_by_dim<__nv_bfloat16, false>(p, b, a, status, st) : launch_by_dim<__half, false>(p, b, a, status, st);
 }
 
 }  // namespace plc

@@ -320,9 +320,13 @@ def test_weights_of_ragged_sessions(dev, ora, dtype, d, H, G, page, slots_first)
 
 
 @pytest.mark.parametrize("dtype, d, H, G, n, picked", [("f16", 64, 1, 1, 1, False), ("bf16", 128, 2, 4, 1, True), ("f16", 128, 1, 8, 40, True), ("bf16", 64, 2, 7, 33, False),
-                                                       ("f16", 256, 1, 2, 70, False), ("bf16", 32, 1, 1, 130, True), ("f16", 128, 1, 4, 150, False), ("bf16", 128, 1, 1, 300, False)])
-def test_weights_of_many_entries(dev, ora, dtype, d, H, G, n, picked):
-    weigh_case(dev, ora, n + d, dtype, d, H, G, 16, lens=[200 + n, n, 37, 300 + n], n=[n, n, 1, n // 2], picked=picked, strided=True).check()
+                                                       ("f16", 256, 1, 2, 70, False), ("bf16", 32, 1, 1, 130, True), ("f16", 128, 1, 4, 150, False), ("bf16", 128, 1, 1, 300, False),
+                                                       ("f16", 64, 2, 4, 330, False), ("bf16", 256, 1, 2, 530, False), ("f16", 128, 1, 8, 260, True), ("bf16", 32, 2, 2, 600, False),
+                                                       ("f16", 256, 1, 3, 400, False), ("bf16", 128, 2, 16, 200, False), ("f16", 128, 1, 128, 9, False), ("f16", 64, 1, 256, 5, False)])
+@pytest.mark.parametrize("page", [16, 24, 256, 100])
+def test_weights_of_many_entries(dev, ora, dtype, d, H, G, n, picked, page):
+    """Drafts and chunks, with keys and queries in boxes and in pieces; ranges that begin inside items."""
+    weigh_case(dev, ora, n + d, dtype, d, H, G, page, lens=[200 + n, n, 37, 300 + n], n=[n, n, 1, n // 2], picked=picked, strided=True).check()
 
 
 def test_weights_entries_that_count_for_nothing(dev, ora):
