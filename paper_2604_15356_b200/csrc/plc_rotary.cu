@@ -3,8 +3,7 @@
 //
 // A pair (x_a, x_b) of components at position pos becomes s (x_a cos t - x_b sin t, x_b cos t + x_a sin t), t = pos f_i.  The frequency is held in turns a
 // position as a fraction of 64 bits, so that the product with the position, cut to its low 64 bits, is the angle modulo a turn to 2^-33 turns at any
-// position that an int holds: no product in 64-bit floating point and no reduction.  Its sine and cosine are formed once a row and pair, in shared memory, for all
-// heads.
+// position that an int holds: no product in 64-bit floating point and no reduction.  Its sine and cosine are formed once a row and pair, for all heads.
 //
 // Bound by HBM where rows are many (each component read and written once, 16 bytes a thread and access), by the launch where they are few.  A block takes a few
 // rows with all their heads.
@@ -23,14 +22,14 @@ struct TurnSet {
     const uint8_t* x; uint8_t* out;
     int64_t xs_row, xs_head, os_row, os_head;     // bytes
     int heads, dim;                               // dim: components that turn
-    int per_head, per_head_magic;                 // units of a head; 2^32 over it, rounded up
+    int per_head;                                 // units of a head: runs, or pairs and components
     int first;                                    // unit of a row that the set begins with
 };
 struct TurnArgs {
     TurnSet set[kMostSets];
-    int sets, units, units_magic;                 // units of a row
+    int sets, units;                              // units of a row
     const uint64_t* turns; int pairs; float scale; bool back;
-    const int32_t* pos; int rows, d, rows_block;
+    const int32_t* pos; int rows, d, rows_block, shares;             // shares: warps that share a row
     const int32_t* begin; int layer;              // pages: ranges of the sessions' rows
 };
 
@@ -48,21 +47,11 @@ template <> struct Wide<__nv_bfloat16> {
     static __device__ __forceinline__ __nv_bfloat16 put(float v) { return __float2bfloat16_rn(v); }
 };
 
-// A run of W components as it stands in memory.
-template <class T, int W, bool VEC> struct Run {
-    T v[W];
-    __device__ __forceinline__ void load(const uint8_t* p) {
-        if constexpr (VEC) *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(p);
-        else
-#pragma unroll
-            for (int i = 0; i < W; ++i) v[i] = reinterpret_cast<const T*>(p)[i];
-    }
-    __device__ __forceinline__ void store(uint8_t* p) const {
-        if constexpr (VEC) *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(v);
-        else
-#pragma unroll
-            for (int i = 0; i < W; ++i) reinterpret_cast<T*>(p)[i] = v[i];
-    }
+// A run of 16 bytes.
+template <class T, int W> struct Run {
+    alignas(16) T v[W];
+    __device__ __forceinline__ void load(const uint8_t* p) { *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ void store(uint8_t* p) const { *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(v); }
 };
 
 // The session of row i: the last one whose range begins at or before it; -1 where it is in none.  A warp calls it.
@@ -81,153 +70,191 @@ __device__ __forceinline__ int session_of_row(const int32_t* begin, int sessions
     return begin[lo] <= i && i < begin[lo + 1] ? lo : -1;
 }
 
-// INTER: pairs are neighbours, else half a turned part away.  VEC: 16 bytes at a time.
-template <class T, bool INTER, bool VEC, bool PAGES>
-__global__ void __launch_bounds__(kTurnThreads) turn_kernel(const __grid_constant__ TurnArgs a, const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
-                                                            uint32_t* status) {
-    constexpr int W = VEC ? 16 / (int)sizeof(T) : INTER ? 2 : 1, REST = VEC ? W : 1;
-    extern __shared__ float2 turn[];              // [rows of the block][pairs] cosine, sine
-    __shared__ int64_t row_to[kMostRows];         // where a row's key goes, from the layer's first key on; -1: nowhere
-    __shared__ int row_pos[kMostRows];            // its position; the row is in some range
-    __shared__ bool row_in[kMostRows];
-    const int tid = threadIdx.x, r0 = blockIdx.x * a.rows_block, rows = min(a.rows_block, a.rows - r0);
+// The angle of a pair at a position: cosine and sine, times the magnitude.
+__device__ __forceinline__ float2 turn_of(const TurnArgs& a, int pos, int pair) {
+    const uint64_t angle = (uint64_t)(int64_t)pos * a.turns[pair] + (1ull << 31);
+    float s, c;
+    sincospif((float)(int32_t)(angle >> 32) * 0x1p-31f, &s, &c);
+    return make_float2(c * a.scale, a.back ? -s * a.scale : s * a.scale);
+}
+
+// Where row i stands: its session's position and the place of its key, in bytes from the layer's first one (-1: nowhere).  A warp calls it; false where
+// the row is in no range.
+__device__ __forceinline__ bool place_of(const TurnArgs& a, const PoolDev& p, const BookDev& b, int i, int* pos, int64_t* to, uint32_t* status) {
+    const int s = session_of_row(a.begin, b.rows, i);
+    if (s < 0) return false;
+    const int len = b.len[s];
+    const long long t = (long long)len + (i - a.begin[s]);
+    int page = -1;
+    if (len >= 0 && t < most_positions(b, p)) page = b.table[(int64_t)s * b.max_pages + t / p.page_pos];
+    *to = page >= 0 && page < p.n_pages && b.ref[page] == 1 ? (int64_t)page * p.spage + (int64_t)(t % p.page_pos) * p.sp : -1;
+    if (*to == -1 && (threadIdx.x & 31) == 0) atomicOr(status, kStRange);
+    *pos = a.pos ? a.pos[i] : (int)t;
+    return true;
+}
+// Ranges that do not rise.
+__device__ __forceinline__ void check_ranges(const TurnArgs& a, const BookDev& b, uint32_t* status) {
+    bool bad = false;
+    for (int s = blockIdx.x * blockDim.x + threadIdx.x; s < b.rows; s += gridDim.x * blockDim.x) bad |= a.begin[s] < 0 || a.begin[s + 1] < a.begin[s] || a.begin[s + 1] > a.rows;
+    if (bad) atomicOr(status, kStRange);
+}
+
+// Runs of 16 bytes.  A warp takes a row's heads, or a share of them: a lane has the same run of every head, whose cosines and sines it keeps in registers, and as
+// many heads at a time as the runs of one leave lanes for.  64 bytes a lane on their way and eight blocks an SM: 16384 rows of 32 + 8 heads of 128 in bf16 63.7 us (5.3 TB/s),
+// with twice as many bytes a lane and four blocks 70; cosines and sines read again for each head 66 to 74.  INTER: pairs are neighbours, else half a turned part away.
+constexpr int kRowThreads = 128;
+template <class T, bool INTER, bool PAGES>
+__global__ void __launch_bounds__(kRowThreads, 8) turn_rows_kernel(const __grid_constant__ TurnArgs a, const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
+                                                                uint32_t* status) {
+    constexpr int W = 16 / (int)sizeof(T), P = INTER ? W / 2 : W, U = INTER ? 4 : 2;        // components and pairs of a run; heads a lane has on their way
+    extern __shared__ float2 turn_s[];                                          // [warps][pairs]
+    if (PAGES) check_ranges(a, b, status);
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    const long long at = (long long)blockIdx.x * (kRowThreads / 32) + wid;
+    const int i = (int)(at / a.shares), share = (int)(at - (long long)i * a.shares);
+    if (i >= a.rows) return;
+    int pos;
+    int64_t row_to = -1;
     if (PAGES) {
-        bool bad = false;
-        for (int s = blockIdx.x * kTurnThreads + tid; s < b.rows; s += gridDim.x * kTurnThreads)
-            bad |= a.begin[s] < 0 || a.begin[s + 1] < a.begin[s] || a.begin[s + 1] > a.rows;
-        if (bad) atomicOr(status, kStRange);
-        const int w = tid >> 5;
-        if (w < rows) {
-            const int i = r0 + w, s = session_of_row(a.begin, b.rows, i);
-            if ((tid & 31) == 0) {
-                int64_t to = -1;
-                int stands = 0;
-                if (s >= 0) {
-                    const int len = b.len[s];
-                    const long long t = (long long)len + (i - a.begin[s]);
-                    stands = (int)t;
-                    int page = -1;
-                    if (len >= 0 && t < most_positions(b, p)) page = b.table[(int64_t)s * b.max_pages + t / p.page_pos];
-                    if (page >= 0 && page < p.n_pages && b.ref[page] == 1) to = (int64_t)page * p.spage + (int64_t)(t % p.page_pos) * p.sp;
-                    if (to < 0) { to = -1; atomicOr(status, kStRange); }
-                }
-                row_to[w] = to;
-                row_in[w] = s >= 0;
-                row_pos[w] = a.pos ? a.pos[i] : stands;
+        if (!place_of(a, p, b, i, &pos, &row_to, status)) return;
+    } else pos = a.pos[i];
+    float2* turn = turn_s + wid * a.pairs;
+    for (int k = lane; k < a.pairs; k += 32) turn[k] = turn_of(a, pos, k);
+    __syncwarp();
+    auto address = [&](int t, int h) -> uint8_t* {                              // of a head of set t where it goes; null: nowhere
+        if (PAGES && t > 0) return row_to < 0 ? nullptr : p.base + (int64_t)a.layer * p.sl + (t == 2 ? p.skv : 0) + row_to + (int64_t)h * p.sh;
+        return a.set[t].out + (int64_t)i * a.set[t].os_row + (int64_t)h * a.set[t].os_head;
+    };
+#pragma unroll 1
+    for (int t = 0; t < a.sets; ++t) {
+        const TurnSet& s = a.set[t];
+        const int lo = s.heads * share / a.shares, hi = s.heads * (share + 1) / a.shares;
+        if (lo == hi || (PAGES && t > 0 && row_to < 0)) continue;
+        const uint8_t* from = s.x + (int64_t)i * s.xs_row;
+        const int turned = s.dim / W / (INTER ? 1 : 2), wide = min(s.per_head, 32), abreast = 32 / wide, h0 = lo + lane / wide;
+        const int64_t half = (int64_t)s.dim / 2 * (int)sizeof(T);
+#pragma unroll 1
+        for (int e0 = 0; e0 < s.per_head; e0 += 32) {
+            const int e = e0 + lane % wide;
+            if (lane >= abreast * wide || e >= s.per_head) continue;
+            const bool turns = e < turned;
+            const int64_t off = turns ? (int64_t)e * 16 : (int64_t)s.dim * (int)sizeof(T) + (int64_t)(e - turned) * 16;
+            float2 cs[P];
+            if (turns) {
+#pragma unroll
+                for (int k = 0; k < P; ++k) cs[k] = turn[e * P + k];
             }
-        }
-    } else if (tid < rows) row_pos[tid] = a.pos[r0 + tid];
-    __syncthreads();
-    for (int i = tid; i < rows * a.pairs; i += kTurnThreads) {
-        const int r = i / a.pairs;
-        const uint64_t angle = (uint64_t)(int64_t)row_pos[r] * a.turns[i - r * a.pairs] + (1ull << 31);
-        float s, c;
-        sincospif((float)(int32_t)(angle >> 32) * 0x1p-31f, &s, &c);
-        turn[i] = make_float2(c * a.scale, a.back ? -s * a.scale : s * a.scale);
-    }
-    __syncthreads();
-    const int units = rows * a.units;
-    constexpr int K = VEC ? 4 : 2;
-    for (int u0 = tid; u0 < units; u0 += K * kTurnThreads) {
-        Run<T, W, VEC> x[K], y[K];
-        uint8_t* to[K];
-        int at[K], pairs_from[K], kind[K];        // kind: 0 nothing, 1 a pair of runs (or one run of neighbours), 2 a run that is copied
-        int half[K];
+#pragma unroll 1
+            for (int h = h0; h < hi; h += U * abreast) {
+                Run<T, W> x[U], y[U];
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const int u = u0 + k * kTurnThreads;
-            kind[k] = 0;
-            if (u >= units) continue;
-            const int r = a.rows_block == 1 ? 0 : a.units == 1 ? u : (int)__umulhi((uint32_t)u, (uint32_t)a.units_magic), v = u - r * a.units;
-            int t = 0;
-#pragma unroll
-            for (int i = 1; i < kMostSets; ++i) t += i < a.sets && v >= a.set[i].first;
-            const TurnSet& s = a.set[t];
-            const int w = v - s.first, h = s.per_head == 1 ? w : (int)__umulhi((uint32_t)w, (uint32_t)s.per_head_magic), e = w - h * s.per_head;
-            const uint8_t* from = s.x + (int64_t)(r0 + r) * s.xs_row + (int64_t)h * s.xs_head;
-            if (PAGES && t > 0) {
-                if (row_to[r] < 0) continue;
-                to[k] = p.base + (int64_t)a.layer * p.sl + (t == 2 ? p.skv : 0) + row_to[r] + (int64_t)h * p.sh;
-            } else {
-                if (PAGES && !row_in[r]) continue;
-                to[k] = s.out + (int64_t)(r0 + r) * s.os_row + (int64_t)h * s.os_head;
-            }
-            const int turned = INTER ? s.dim / W : s.dim / (2 * W);
-            if (e < turned) {
-                kind[k] = 1;
-                at[k] = e * W * (int)sizeof(T);
-                half[k] = s.dim / 2 * (int)sizeof(T);
-                pairs_from[k] = r * a.pairs + (INTER ? e * W / 2 : e * W);
-                x[k].load(from + at[k]);
-                if (!INTER) y[k].load(from + at[k] + half[k]);
-            } else {
-                kind[k] = 2;
-                at[k] = (s.dim + (e - turned) * REST) * (int)sizeof(T);
-                if constexpr (VEC) x[k].load(from + at[k]);
-                else x[k].v[0] = *reinterpret_cast<const T*>(from + at[k]);
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            if (kind[k] == 1) {
-                if (INTER) {
-#pragma unroll
-                    for (int i = 0; i < W; i += 2) {
-                        const float2 cs = turn[pairs_from[k] + i / 2];
-                        const float xa = Wide<T>::get(x[k].v[i]), xb = Wide<T>::get(x[k].v[i + 1 < W ? i + 1 : i]);
-                        x[k].v[i] = Wide<T>::put(xa * cs.x - xb * cs.y);
-                        x[k].v[i + 1 < W ? i + 1 : i] = Wide<T>::put(xb * cs.x + xa * cs.y);
+                for (int u = 0; u < U; ++u)
+                    if (h + u * abreast < hi) {
+                        const uint8_t* src = from + (int64_t)(h + u * abreast) * s.xs_head + off;
+                        x[u].load(src);
+                        if (!INTER && turns) y[u].load(src + half);
                     }
-                } else {
 #pragma unroll
-                    for (int i = 0; i < W; ++i) {
-                        const float2 cs = turn[pairs_from[k] + i];
-                        const float xa = Wide<T>::get(x[k].v[i]), xb = Wide<T>::get(y[k].v[i]);
-                        x[k].v[i] = Wide<T>::put(xa * cs.x - xb * cs.y);
-                        y[k].v[i] = Wide<T>::put(xb * cs.x + xa * cs.y);
+                for (int u = 0; u < U; ++u)
+                    if (h + u * abreast < hi) {
+                        uint8_t* dst = address(t, h + u * abreast) + off;
+                        if (turns) {
+#pragma unroll
+                            for (int k = 0; k < P; ++k) {
+                                T& a0 = x[u].v[INTER ? 2 * k : k];
+                                T& b0 = INTER ? x[u].v[2 * k + 1 < W ? 2 * k + 1 : 0] : y[u].v[k];
+                                const float xa = Wide<T>::get(a0), xb = Wide<T>::get(b0);
+                                a0 = Wide<T>::put(xa * cs[k].x - xb * cs[k].y);
+                                b0 = Wide<T>::put(xb * cs[k].x + xa * cs[k].y);
+                            }
+                            if (!INTER) y[u].store(dst + half);
+                        }
+                        x[u].store(dst);
                     }
-                    y[k].store(to[k] + at[k] + half[k]);
-                }
-                x[k].store(to[k] + at[k]);
-            } else if (kind[k] == 2) {
-                if constexpr (VEC) x[k].store(to[k] + at[k]);
-                else *reinterpret_cast<T*>(to[k] + at[k]) = x[k].v[0];
             }
         }
     }
 }
 
-int magic_of(int n) { return n > 1 ? (int)(uint32_t)(((1ull << 32) + n - 1) / n) : 0; }
+// Component by component, where addresses, strides or parts of a head are not runs of 16 bytes.  A block takes a few rows with all their heads.
+template <class T, bool INTER, bool PAGES>
+__global__ void __launch_bounds__(kTurnThreads) turn_parts_kernel(const __grid_constant__ TurnArgs a, const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
+                                                                  uint32_t* status) {
+    extern __shared__ float2 turn[];              // [rows of the block][pairs] cosine, sine
+    __shared__ int64_t row_to[kMostRows];         // where a row's key goes; -1: nowhere
+    __shared__ int row_pos[kMostRows];            // its position; the row is in some range
+    __shared__ bool row_in[kMostRows];
+    const int tid = threadIdx.x, r0 = blockIdx.x * a.rows_block, rows = min(a.rows_block, a.rows - r0);
+    if (PAGES) {
+        check_ranges(a, b, status);
+        const int w = tid >> 5;
+        if (w < rows) {
+            int pos = 0;
+            int64_t to = -1;
+            const bool in = place_of(a, p, b, r0 + w, &pos, &to, status);
+            if ((tid & 31) == 0) { row_to[w] = to; row_in[w] = in; row_pos[w] = pos; }
+        }
+    } else if (tid < rows) row_pos[tid] = a.pos[r0 + tid];
+    __syncthreads();
+    for (int i = tid; i < rows * a.pairs; i += kTurnThreads) turn[i] = turn_of(a, row_pos[i / a.pairs], i % a.pairs);
+    __syncthreads();
+    const int units = rows * a.units;
+    for (int u = tid; u < units; u += kTurnThreads) {
+        const int r = a.rows_block == 1 ? 0 : u / a.units, v = u - r * a.units;
+        int t = 0;
+#pragma unroll
+        for (int i = 1; i < kMostSets; ++i) t += i < a.sets && v >= a.set[i].first;
+        const TurnSet& s = a.set[t];
+        const int w = v - s.first, h = w / s.per_head, e = w - h * s.per_head;
+        if (PAGES && (t > 0 ? row_to[r] < 0 : !row_in[r])) continue;
+        const T* from = reinterpret_cast<const T*>(s.x + (int64_t)(r0 + r) * s.xs_row + (int64_t)h * s.xs_head);
+        T* to = reinterpret_cast<T*>(PAGES && t > 0 ? p.base + (int64_t)a.layer * p.sl + (t == 2 ? p.skv : 0) + row_to[r] + (int64_t)h * p.sh
+                                                    : s.out + (int64_t)(r0 + r) * s.os_row + (int64_t)h * s.os_head);
+        if (e < s.dim / 2) {
+            const int ia = INTER ? 2 * e : e, ib = INTER ? 2 * e + 1 : e + s.dim / 2;
+            const float2 cs = turn[r * a.pairs + e];
+            const float xa = Wide<T>::get(from[ia]), xb = Wide<T>::get(from[ib]);
+            to[ia] = Wide<T>::put(xa * cs.x - xb * cs.y);
+            to[ib] = Wide<T>::put(xb * cs.x + xa * cs.y);
+        } else to[e + s.dim / 2] = from[e + s.dim / 2];
+    }
+}
 
-// Units of the sets, and the launch: rows of a block so that there are several blocks an SM, at most kMostRows.
+// Units of the sets, and the launch.
 template <bool PAGES>
 plc_status launch_turn(TurnArgs& a, const PoolDev& p, const BookDev& b, int dtype, bool inter, bool vec, uint32_t* status, cudaStream_t st) {
-    const int esz = dtype == PLC_OUT_F32 ? 4 : 2, w = 16 / esz;
-    int units = 0;
+    const int esz = dtype == PLC_OUT_F32 ? 4 : 2, w = 16 / esz, sms = sm_count();
+    int units = 0, heads = 0;
     for (int i = 0; i < a.sets; ++i) {
         TurnSet& s = a.set[i];
         s.per_head = vec ? (inter ? s.dim / w : s.dim / 2 / w) + (a.d - s.dim) / w : s.dim / 2 + a.d - s.dim;
-        s.per_head_magic = magic_of(s.per_head);
         s.first = units;
         units += s.heads * s.per_head;
+        heads = s.heads > heads ? s.heads : heads;
     }
-    a.units = units;
-    a.units_magic = magic_of(units);
-    const int per = a.rows / (4 * sm_count());
-    a.rows_block = per < 1 || units > 20000 ? 1 : per > kMostRows ? kMostRows : per;      // (the quotients by a magic number are exact below 2^32 / divisor)
-    const unsigned grid = (unsigned)((a.rows + a.rows_block - 1) / a.rows_block);
-    const size_t smem = (size_t)a.rows_block * a.pairs * sizeof(float2);
-    auto go = [&](auto* kern) -> cudaError_t {
-        cudaError_t e = smem > 49152 ? cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
-        return e != cudaSuccess ? e : launch_kernel(kern, grid, kTurnThreads, smem, st, false, 1, a, p, b, status);
-    };
+    auto go = [&](auto* kern, unsigned grid, int threads, size_t smem) { return launch_kernel(kern, grid, threads, smem, st, false, 1, a, p, b, status); };
     cudaError_t e;
-#define PLC_TURN(T) (inter ? (vec ? go(turn_kernel<T, true, true, PAGES>) : go(turn_kernel<T, true, false, PAGES>)) \
-                           : (vec ? go(turn_kernel<T, false, true, PAGES>) : go(turn_kernel<T, false, false, PAGES>)))
-    if (dtype == PLC_OUT_F32) e = PLC_TURN(float);
-    else if (dtype == PLC_OUT_F16) e = PLC_TURN(__half);
-    else e = PLC_TURN(__nv_bfloat16);
-#undef PLC_TURN
+    if (vec) {
+        // warps that share a row: so many that there are sixteen an SM, as long as each has the runs of a load for all of its lanes
+        const long long want = (16ll * sms + a.rows - 1) / a.rows, most = (units + 127) / 128;
+        a.shares = (int)(want < most ? want : most);
+        constexpr int warps = kRowThreads / 32;
+        const unsigned grid = (unsigned)(((long long)a.rows * a.shares + warps - 1) / warps);
+        const size_t smem = (size_t)warps * a.pairs * sizeof(float2);
+        if (dtype == PLC_OUT_F32) e = inter ? go(turn_rows_kernel<float, true, PAGES>, grid, kRowThreads, smem) : go(turn_rows_kernel<float, false, PAGES>, grid, kRowThreads, smem);
+        else if (dtype == PLC_OUT_F16) e = inter ? go(turn_rows_kernel<__half, true, PAGES>, grid, kRowThreads, smem) : go(turn_rows_kernel<__half, false, PAGES>, grid, kRowThreads, smem);
+        else e = inter ? go(turn_rows_kernel<__nv_bfloat16, true, PAGES>, grid, kRowThreads, smem) : go(turn_rows_kernel<__nv_bfloat16, false, PAGES>, grid, kRowThreads, smem);
+    } else {
+        // rows of a block so that there are several blocks an SM
+        const int per = a.rows / (4 * sms);
+        a.units = units;
+        a.rows_block = per < 1 ? 1 : per > kMostRows ? kMostRows : per;
+        const unsigned grid = (unsigned)((a.rows + a.rows_block - 1) / a.rows_block);
+        const size_t smem = (size_t)a.rows_block * a.pairs * sizeof(float2);
+        if (dtype == PLC_OUT_F32) e = inter ? go(turn_parts_kernel<float, true, PAGES>, grid, kTurnThreads, smem) : go(turn_parts_kernel<float, false, PAGES>, grid, kTurnThreads, smem);
+        else if (dtype == PLC_OUT_F16) e = inter ? go(turn_parts_kernel<__half, true, PAGES>, grid, kTurnThreads, smem) : go(turn_parts_kernel<__half, false, PAGES>, grid, kTurnThreads, smem);
+        else e = inter ? go(turn_parts_kernel<__nv_bfloat16, true, PAGES>, grid, kTurnThreads, smem) : go(turn_parts_kernel<__nv_bfloat16, false, PAGES>, grid, kTurnThreads, smem);
+    }
     if (e != cudaSuccess) return PLC_E_CUDA;
     count_launch(1);
     return PLC_OK;
@@ -293,7 +320,7 @@ plc_status plc_rotary_apply(const plc_rotary* rotary, const plc_rotary_set* sets
         heads += s.heads;
         if (heads > (1 << 12)) return PLC_E_SHAPE;
         a.set[i] = TurnSet{static_cast<const uint8_t*>(s.x_dev), static_cast<uint8_t*>(s.out_dev), s.x_stride_row * esz, s.x_stride_head * esz, s.out_stride_row * esz,
-                           s.out_stride_head * esz, s.heads, rotary->dim, 0, 0, 0};
+                           s.out_stride_head * esz, s.heads, rotary->dim, 0, 0};
         vec = vec && wide_set(a.set[i]);
     }
     if (n_rows == 0) return PLC_OK;
@@ -322,9 +349,9 @@ plc_status plc_pages_append(const plc_page_pool* pool, int32_t layer, const plc_
         return PLC_E_INVALID;
     if (t->n_rows == 0) return PLC_OK;
     a.set[0] = TurnSet{static_cast<const uint8_t*>(t->q_dev), static_cast<uint8_t*>(t->out_dev), t->q_stride_row * esz, t->q_stride_head * esz, t->out_stride_row * esz,
-                       t->out_stride_head * esz, t->n_heads, dim, 0, 0, 0};
-    a.set[1] = TurnSet{static_cast<const uint8_t*>(t->k_dev), nullptr, t->k_stride_row * esz, t->k_stride_head * esz, 0, 0, p.H, dim, 0, 0, 0};
-    a.set[2] = TurnSet{static_cast<const uint8_t*>(t->v_dev), nullptr, t->v_stride_row * esz, t->v_stride_head * esz, 0, 0, p.H, 0, 0, 0, 0};
+                       t->out_stride_head * esz, t->n_heads, dim, 0, 0};
+    a.set[1] = TurnSet{static_cast<const uint8_t*>(t->k_dev), nullptr, t->k_stride_row * esz, t->k_stride_head * esz, 0, 0, p.H, dim, 0, 0};
+    a.set[2] = TurnSet{static_cast<const uint8_t*>(t->v_dev), nullptr, t->v_stride_row * esz, t->v_stride_head * esz, 0, 0, p.H, 0, 0, 0};
     const bool vec = wide_runs(dim, p.d, inter, esz) && (t->n_heads == 0 || wide_set(a.set[0])) && wide_set(a.set[1]) && wide_set(a.set[2]);
     a.sets = 3; a.pos = t->pos_dev; a.rows = t->n_rows; a.d = p.d; a.begin = t->begin_dev; a.layer = layer;
     return launch_turn<true>(a, p, b, pool->dtype, inter, vec, status_dev, static_cast<cudaStream_t>(stream));

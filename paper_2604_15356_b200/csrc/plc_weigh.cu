@@ -35,9 +35,11 @@ template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float* c, ui
 
 constexpr int kThreads = 128, kWarps = kThreads / 32, kTile = 16;
 
-// Row tiles of eight columns (a column: an entry's query head).
-template <class T, int D>
-__global__ void __launch_bounds__(kThreads) weigh_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b, const __grid_constant__ WeighArgs a,
+// NT: tiles of eight columns (a column: an entry's query head) that a warp has in registers.
+// Blocks an SM: what the registers of the keys on their way, of the queries and of the rest leave.
+template <int D, int NT> constexpr int kPerSm = D == 256 ? (NT == 1 ? 3 : 2) : D == 128 ? (NT == 1 ? 5 : 4) : NT == 1 ? 7 : 5;
+template <class T, int D, int NT>
+__global__ void __launch_bounds__(kThreads, kPerSm<D, NT>) weigh_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b, const __grid_constant__ WeighArgs a,
                                                          uint32_t* status) {
     constexpr int B = D / 32;                     // 32-component blocks of a vector
     __shared__ long long upto_s[kThreads];
@@ -92,56 +94,88 @@ __global__ void __launch_bounds__(kThreads) weigh_kernel(const __grid_constant__
     int tiles = (x.len + kTile - 1) / kTile, h = (int)(rest / tiles), tile = (int)(rest - (long long)h * tiles);
     const int quad = lane >> 2, part = lane & 3;
     const float c2 = a.scale * kLog2e;
-    while (left > 0) {
-        const int todo = (int)min(left, (long long)(tiles - tile));
-        const int cols = x.n * a.group;
-        for (int i = 0; i < todo; ++i) {
-            const int base = (tile + i) * kTile, t_mine = base + (lane & 15);
-            int page = -1;
-            if (t_mine < x.len) {
-                page = b.table[(int64_t)s * b.max_pages + t_mine / p.page_pos];
-                if (page < 0 || page >= p.n_pages) { page = -1; atomicOr(status, kStRange); }
-            }
-            const int64_t off = page < 0 ? -1 : (int64_t)a.layer * p.sl + (int64_t)page * p.spage + (int64_t)(t_mine % p.page_pos) * p.sp + (int64_t)h * p.sh;
-            const int64_t off0 = __shfl_sync(kFull, off, quad), off1 = __shfl_sync(kFull, off, quad + 8);
-            uint4 k0[B], k1[B];
+    // Where the vectors of tile i of the item stand, as far as this lane's position is concerned (-1: it has none).  Looked up two tiles ahead, loaded one ahead.
+    auto look_up = [&](int i) -> int64_t {
+        const int t = i * kTile + (lane & 15);
+        if (t >= x.len) return -1;
+        const int page = b.table[(int64_t)s * b.max_pages + t / p.page_pos];
+        if (page < 0 || page >= p.n_pages) { atomicOr(status, kStRange); return -1; }
+        return (int64_t)a.layer * p.sl + (int64_t)page * p.spage + (int64_t)(t % p.page_pos) * p.sp + (int64_t)h * p.sh;
+    };
+    auto fetch = [&](int64_t off, uint4 (&k0)[B], uint4 (&k1)[B]) {
+        const int64_t off0 = __shfl_sync(kFull, off, quad), off1 = __shfl_sync(kFull, off, quad + 8);
 #pragma unroll
-            for (int e = 0; e < B; ++e) {
-                k0[e] = off0 < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(p.base + off0 + e * 64 + part * 16);
-                k1[e] = off1 < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(p.base + off1 + e * 64 + part * 16);
+        for (int e = 0; e < B; ++e) {
+            k0[e] = off0 < 0 ? make_uint4(0, 0, 0, 0) : __ldcs(reinterpret_cast<const uint4*>(p.base + off0 + e * 64 + part * 16));
+            k1[e] = off1 < 0 ? make_uint4(0, 0, 0, 0) : __ldcs(reinterpret_cast<const uint4*>(p.base + off1 + e * 64 + part * 16));
+        }
+    };
+    while (left > 0) {
+        const int todo = (int)min(left, (long long)(tiles - tile)), cols = x.n * a.group;
+        int64_t off = look_up(tile), next = todo > 1 ? look_up(tile + 1) : -1;
+        uint4 k0[B], k1[B];
+        fetch(off, k0, k1);
+        // the queries, a lane its column's run of components and log-sum-exp
+        uint4 q[NT][B];
+        float l_mine[NT];
+        int entry[NT];
+        auto queries = [&](int col0) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int col = col0 + n * 8 + quad;
+                entry[n] = col / a.group;
+                int row = -1;
+                if (col < cols) row = a.rows ? a.rows[x.first + entry[n]] : x.first + entry[n];
+                if (row < -1 || row >= a.n_rows) { atomicOr(status, kStRange); row = -1; }
+                const int head = h * a.group + col - entry[n] * a.group;
+                l_mine[n] = row < 0 ? INFINITY : a.lse[(int64_t)row * a.heads + head] * kLog2e;
+                const uint16_t* from = a.q + (int64_t)max(row, 0) * a.qs_row + (int64_t)(row < 0 ? 0 : head) * a.qs_head + part * 8;
+#pragma unroll
+                for (int e = 0; e < B; ++e) q[n][e] = row < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(from + e * 32);
             }
+        };
+        queries(0);
+        for (int i = 0; i < todo; ++i) {
+            const int base = (tile + i) * kTile;
+            const bool have0 = __shfl_sync(kFull, off, quad) >= 0, have1 = __shfl_sync(kFull, off, quad + 8) >= 0;
             float sum0 = 0.f, sum1 = 0.f;
             const int seen0 = base + quad - (x.len - x.n), seen1 = seen0 + 8;             // entries from this one on see the position
-            for (int col0 = 0; col0 < cols; col0 += 8) {
-                float acc[4] = {0.f, 0.f, 0.f, 0.f};
-                const int col = col0 + quad, entry = col / a.group;
-                int row = -1;
-                if (col < cols) row = a.rows ? a.rows[x.first + entry] : x.first + entry;
-                if (row < -1 || row >= a.n_rows) { atomicOr(status, kStRange); row = -1; }
-                const int head = h * a.group + col - entry * a.group;
-                const uint16_t* q = a.q + (int64_t)max(row, 0) * a.qs_row + (int64_t)head * a.qs_head + part * 8;
-                const float l_mine = row < 0 ? INFINITY : a.lse[(int64_t)row * a.heads + head] * kLog2e;
+            // sessions of more columns than the call's mean take them in turns
+            for (int col0 = 0; col0 < cols; col0 += 8 * NT) {
+                if (cols > 8 * NT && (i > 0 || col0 > 0)) queries(col0);
+                float acc[NT][4];
 #pragma unroll
-                for (int e = 0; e < B; ++e) {
-                    const uint4 v = row < 0 ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(q + e * 32);
-                    mma16816<T>(acc, k0[e].x, k1[e].x, k0[e].y, k1[e].y, v.x, v.y);
-                    mma16816<T>(acc, k0[e].z, k1[e].z, k0[e].w, k1[e].w, v.z, v.w);
+                for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[n][j] = 0.f;
+#pragma unroll
+                    for (int e = 0; e < B; ++e) {
+                        mma16816<T>(acc[n], k0[e].x, k1[e].x, k0[e].y, k1[e].y, q[n][e].x, q[n][e].y);
+                        mma16816<T>(acc[n], k0[e].z, k1[e].z, k0[e].w, k1[e].w, q[n][e].z, q[n][e].w);
+                    }
+                }
+                if (col0 + 8 * NT >= cols) {      // the keys are not needed any more
+                    off = next;
+                    if (i + 1 < todo) fetch(off, k0, k1);
+                    next = i + 2 < todo ? look_up(tile + i + 2) : -1;
                 }
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {     // columns 2 part + j
-                    const float l = __shfl_sync(kFull, l_mine, (2 * part + j) * 4);
-                    const int en = __shfl_sync(kFull, entry, (2 * part + j) * 4);
-                    const bool dead = isinf(l);
-                    sum0 += dead || en < seen0 ? 0.f : exp2_approx(fmaf(acc[j], c2, -l));
-                    sum1 += dead || en < seen1 ? 0.f : exp2_approx(fmaf(acc[2 + j], c2, -l));
-                }
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) { // columns 2 part + j
+                        const float l = __shfl_sync(kFull, l_mine[n], (2 * part + j) * 4);
+                        const int en = __shfl_sync(kFull, entry[n], (2 * part + j) * 4);
+                        const bool dead = isinf(l);
+                        sum0 += dead || en < seen0 ? 0.f : exp2_approx(fmaf(acc[n][j], c2, -l));
+                        sum1 += dead || en < seen1 ? 0.f : exp2_approx(fmaf(acc[n][2 + j], c2, -l));
+                    }
             }
             sum0 += __shfl_xor_sync(kFull, sum0, 1);
             sum1 += __shfl_xor_sync(kFull, sum1, 1);
             sum0 += __shfl_xor_sync(kFull, sum0, 2);
             sum1 += __shfl_xor_sync(kFull, sum1, 2);
             const int t = base + quad + 8 * part;
-            if (part < 2 && t < x.len) put_weight(a, x, s, h, t, part ? sum1 : sum0, (part ? off1 : off0) >= 0, status);
+            if (part < 2 && t < x.len) put_weight(a, x, s, h, t, part ? sum1 : sum0, part ? have1 : have0, status);
         }
         left -= todo;
         tile = 0;
@@ -154,14 +188,19 @@ __global__ void __launch_bounds__(kThreads) weigh_kernel(const __grid_constant__
     }
 }
 
+template <class T, int D>
+cudaError_t launch(const PoolDev& p, const BookDev& b, const WeighArgs& a, uint32_t* status, cudaStream_t st) {
+    const unsigned sms = sm_count();
+    return (long long)a.n_list * a.group <= 8ll * b.rows ? launch_kernel(weigh_kernel<T, D, 1>, kPerSm<D, 1> * sms, kThreads, 0, st, false, 1, p, b, a, status)
+                                                         : launch_kernel(weigh_kernel<T, D, 2>, kPerSm<D, 2> * sms, kThreads, 0, st, false, 1, p, b, a, status);
+}
 template <class T>
 cudaError_t launch_weigh(const PoolDev& p, const BookDev& b, const WeighArgs& a, uint32_t* status, cudaStream_t st) {
-    const unsigned grid = 4u * sm_count();
     switch (p.d) {
-        case 32: return launch_kernel(weigh_kernel<T, 32>, grid, kThreads, 0, st, false, 1, p, b, a, status);
-        case 64: return launch_kernel(weigh_kernel<T, 64>, grid, kThreads, 0, st, false, 1, p, b, a, status);
-        case 128: return launch_kernel(weigh_kernel<T, 128>, grid, kThreads, 0, st, false, 1, p, b, a, status);
-        default: return launch_kernel(weigh_kernel<T, 256>, grid, kThreads, 0, st, false, 1, p, b, a, status);
+        case 32: return launch<T, 32>(p, b, a, status, st);
+        case 64: return launch<T, 64>(p, b, a, status, st);
+        case 128: return launch<T, 128>(p, b, a, status, st);
+        default: return launch<T, 256>(p, b, a, status, st);
     }
 }
 
@@ -182,7 +221,7 @@ plc_status plc_pages_weigh_workspace(const plc_page_pool* pool, int32_t sessions
     if (rc) return rc;
     if (n_heads < 1 || sessions < 1 || n_list < 0 || !bytes) return PLC_E_INVALID;
     if (n_heads % p.H || n_heads > (1 << 16)) return PLC_E_SHAPE;
-    *bytes = many_columns(p, sessions, n_heads, n_list) ? weigh_many_bytes() : 16;
+    *bytes = many_columns(p, sessions, n_heads, n_list) ? weigh_many_bytes() : 0;
     return PLC_OK;
 }
 
@@ -192,15 +231,16 @@ plc_status plc_pages_weigh(const plc_page_pool* pool, int32_t layer, const plc_p
     BookDev b;
     plc_status rc = check_pool(pool, &p);
     if (rc || (rc = check_book(book, &b))) return rc;
-    if (!t || !t->q_dev || !t->lse_dev || !t->begin_dev || t->n_rows < 0 || t->n_list < 0 || !weights || !weights->base_dev || !workspace_dev || !status_dev) return PLC_E_INVALID;
+    if (!t || !t->q_dev || !t->lse_dev || !t->begin_dev || t->n_rows < 0 || t->n_list < 0 || !weights || !weights->base_dev || !status_dev) return PLC_E_INVALID;
     if (layer < 0 || layer >= p.L || pool->dtype == PLC_OUT_F32 || !(scale > 0.f) || isinf(scale) || !isfinite(decay) || decay < 0.f) return PLC_E_INVALID;
     if (t->n_heads < 1 || weights->n_pos < 1) return PLC_E_INVALID;
     if (t->n_heads % p.H || t->n_heads > (1 << 16) || (!t->rows_dev && t->n_list > t->n_rows)) return PLC_E_SHAPE;
     const int group = t->n_heads / p.H;
     if ((long long)t->n_list * group > (1 << 30)) return PLC_E_SHAPE;
     const bool many = many_columns(p, b.rows, t->n_heads, t->n_list);
+    if (many && !workspace_dev) return PLC_E_INVALID;
     if (!plc_aligned16(workspace_dev) || !plc_aligned16(t->q_dev) || t->q_stride_row % 8 || t->q_stride_head % 8 || (reinterpret_cast<uintptr_t>(weights->base_dev) & 3)) return PLC_E_ALIGN;
-    if (workspace_bytes < (many ? weigh_many_bytes() : 16)) return PLC_E_CAPACITY;
+    if (workspace_bytes < (many ? weigh_many_bytes() : 0)) return PLC_E_CAPACITY;
     if (t->n_list == 0) return PLC_OK;
     const WeighArgs a{static_cast<const uint16_t*>(t->q_dev), t->q_stride_row, t->q_stride_head, t->lse_dev, t->rows_dev, t->begin_dev, t->n_list, t->n_rows, t->n_heads,
                       group, layer, weights->base_dev + (int64_t)layer * weights->stride_layer, weights->stride_row, weights->stride_head, weights->n_pos, decay, scale, nullptr, nullptr, 0, {}, 0};

@@ -403,9 +403,9 @@ class PagePool:
             if len(self._need_bytes) >= 4096:
                 self._need_bytes.clear()
             need = self._need_bytes[(book.rows, heads, n_list, "weigh")] = b.value
-        ws = torch.empty(need, dtype=torch.uint8, device=dev)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev).data_ptr() if need else None
         t = WeighQueries(q.data_ptr(), row, head, lse.data_ptr(), None if rows is None else rows.data_ptr(), begin.data_ptr(), N, n_list, heads)
-        _check(_run(dev, api.plc_pages_weigh, self._by, layer, a, C.byref(t), d ** -0.5 if scale is None else scale, decay, C.byref(w), ws.data_ptr(), need,
+        _check(_run(dev, api.plc_pages_weigh, self._by, layer, a, C.byref(t), d ** -0.5 if scale is None else scale, decay, C.byref(w), ws, need,
                     self._word), where)
         return weight
 

@@ -130,7 +130,7 @@ def test_weights_that_are_refused(lib):
         q, w = serving.WeighQueries(**t), serving.Weights(base, 800, 400, 100, n_pos)
         return lib.plc_pages_weigh(C.byref(p or pool()), layer, C.byref(b or book()), C.byref(q), C.c_float(scale), C.c_float(decay), C.byref(w), C.c_void_p(ws),
                                    C.c_uint64(ws_bytes), C.c_void_p(status), None)
-    for kw in (dict(layer=2), dict(layer=-1), dict(ws=0), dict(scale=0.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(decay=-1.0), dict(decay=float("inf")), dict(base=0),
+    for kw in (dict(layer=2), dict(layer=-1), dict(ws=0, n_rows=700, n_list=700), dict(scale=0.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(decay=-1.0), dict(decay=float("inf")), dict(base=0),
                dict(n_pos=0), dict(status=0), dict(q_dev=None), dict(lse_dev=None), dict(begin_dev=None), dict(n_rows=-1), dict(n_list=-1), dict(n_heads=0),
                dict(p=pool(dtype=plc.OUT_F32)), dict(b=book(rows=0))):
         assert call(**kw) == plc.E_INVALID, kw
@@ -139,9 +139,9 @@ def test_weights_that_are_refused(lib):
     for kw in (dict(q_dev=A + 2), dict(q_stride_row=516), dict(q_stride_head=68), dict(base=B + 2), dict(ws=WS + 8)):
         assert call(**kw) == plc.E_ALIGN, kw
     n = C.c_uint64()
-    for rows in (7, 700):
-        assert lib.plc_pages_weigh_workspace(C.byref(pool()), 3, 8, rows, C.byref(n)) == plc.OK and n.value >= 16
-        assert call(n_rows=rows, n_list=rows, ws_bytes=n.value - 1) == plc.E_CAPACITY
+    assert lib.plc_pages_weigh_workspace(C.byref(pool()), 3, 8, 7, C.byref(n)) == plc.OK and n.value == 0
+    assert lib.plc_pages_weigh_workspace(C.byref(pool()), 3, 8, 700, C.byref(n)) == plc.OK and n.value > 0
+    assert call(n_rows=700, n_list=700, ws_bytes=n.value - 1) == plc.E_CAPACITY
     assert lib.plc_pages_weigh_workspace(C.byref(pool()), 0, 8, 7, C.byref(n)) == plc.E_INVALID and lib.plc_pages_weigh_workspace(C.byref(pool()), 3, 8, 7, None) == plc.E_INVALID
     assert lib.plc_pages_weigh_workspace(C.byref(pool()), 3, 6, 7, C.byref(n)) == plc.E_SHAPE
     assert call(n_list=0) == plc.OK
