@@ -4,30 +4,41 @@
 // together in order, keys, values and weights alike, and the pages behind the new length are released.
 //
 // Two launches.  The first selects: a block a (row, layer, head) finds the weight of the last position that is kept by its bits, eight at a time from the
-// top, writes a bit for each position that is kept, and the kept weights; one block more decides, like the plan of a fork, which pages are fresh ones.  The
-// second moves the vectors and writes the new book.  A position never moves up, and a block that takes a (row, layer, head, keys or values) reads each
-// piece of it before it writes, so it can stay in its pages.
-#include <math.h>
-
+// top, and writes a bit for each position that is kept, and the kept weights; one block more decides, like the plan of a fork, which pages are fresh ones.  The
+// second moves the vectors in pieces and writes the new book.  A position never moves up, so that a row can stay in its pages: a piece's places hold one or two
+// earlier pieces of the same row, and it is written once those have been read.
 #include "plc_pages.cuh"
 
 namespace plc {
 namespace {
 
-constexpr int kSelectThreads = 256, kMoveThreads = 256;
-constexpr int kPiecePos = 128;                    // positions of a piece, four words of kept bits
+constexpr int kSelectThreads = 256, kSelectWarps = kSelectThreads / 32;
+constexpr int kCopyThreads = 256, kMoveThreads = kCopyThreads + 64;      // that copy; and two warps that find out what comes next
+constexpr int kHeld = 4096;                       // positions of a row whose weights stay in shared memory while they are selected
+constexpr uint32_t kSpin = 1u << 22;
 
+// Positions of a piece: as many vectors as 32 KB of shared memory hold, at most 128.
+constexpr int piece_log2(int vector_bytes) { return vector_bytes <= 256 ? 7 : vector_bytes <= 512 ? 6 : 5; }
+
+struct EvictHead {
+    int32_t short_of;                             // the free pages do not suffice
+    int32_t pad;
+    unsigned long long ticket;                    // pieces that blocks have taken
+};
 struct EvictArgs {
     const float* weight; int64_t ws_row, ws_layer, ws_head; int n_pos;
     float* out;                                   // [rows][L][H][n_pos]
     const int32_t* budgets; int budget, recent;
+    int piece_log2, pieces;                       // positions of a piece; pieces that n_pos has
     // workspace
-    int32_t* head;                                // [4]: 1 where the free pages do not suffice
+    EvictHead* head;
+    long long* first;                             // [rows + 1] pieces of the rows before
     int32_t* base;                                // [rows] index of the row's first fresh page in `list`; -1: the row stays as it is
+    int32_t* count;                               // [rows] its fresh pages
     int32_t* list;                                // [n_pages]
-    uint32_t* kept;                               // [rows][L][H][pieces][4] a bit a position
+    uint32_t* kept;                               // [rows][L][H][pieces][positions of a piece / 32] a bit a position
     int32_t* ahead;                               // [rows][L][H][pieces] positions kept before the piece
-    int pieces;
+    uint32_t* read;                               // [rows][L][H][pieces][2] a piece's keys, values have been read
 };
 
 // What becomes of a row.
@@ -42,6 +53,7 @@ __device__ __forceinline__ EvictRow evict_row(const PoolDev& p, const BookDev& i
     return r;
 }
 __device__ __forceinline__ bool page_ok(const PoolDev& p, int page) { return page >= 0 && page < p.n_pages; }
+__device__ __forceinline__ int pages_for(const PoolDev& p, int n) { return (int)(((long long)n + p.page_pos - 1) / p.page_pos); }
 
 // Order of the weights as unsigned numbers; NaN is lightest, -0 is +0.
 __device__ __forceinline__ uint32_t weight_order(float w) {
@@ -50,164 +62,209 @@ __device__ __forceinline__ uint32_t weight_order(float w) {
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 
-// One block: which rows go, how many fresh pages they need and which.
+// Sum over the block's threads before this one; *total: over all.
+__device__ __forceinline__ long long sum_before(long long v, long long* total) {
+    __shared__ long long part[kSelectWarps];
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    long long x = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long y = __shfl_up_sync(kFull, x, o);
+        if (lane >= o) x += y;
+    }
+    __syncthreads();                              // the sums before have been read
+    if (lane == 31) part[wid] = x;
+    __syncthreads();
+    long long before = x - v, all = 0;
+#pragma unroll
+    for (int w = 0; w < kSelectWarps; ++w) {
+        if (w < wid) before += part[w];
+        all += part[w];
+    }
+    *total = all;
+    return before;
+}
+
+// One block: which rows go, how many fresh pages each needs and which, and how many pieces there are to move.
+constexpr int kOutOfRange = 1 << 30;
 __device__ __forceinline__ void evict_plan(const PoolDev& p, const BookDev& in, const EvictArgs& a, uint32_t* status) {
-    __shared__ long long sums[kSelectThreads / 32];
-    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-    long long need = 0;
+    const int tid = threadIdx.x;
     uint32_t bits = 0;
-    for (int s0 = 0; s0 < in.rows; s0 += kSelectThreads / 32) {       // a warp a row
-        const int s = s0 + wid;
-        int mine = 0;
-        bool ok = false;
-        if (s < in.rows) {
-            const EvictRow r = evict_row(p, in, a, s);
-            if (r.bad) bits |= kStRange;
-            ok = r.goes;
-            if (ok) {
-                const int held = (r.len + p.page_pos - 1) / p.page_pos, keep = (r.now + p.page_pos - 1) / p.page_pos;
-                bool good = true;
-                for (int j = lane; j < held; j += 32) {
-                    const int page = in.table[(int64_t)s * in.max_pages + j];
-                    if (!page_ok(p, page)) good = false;
-                    else if (j < keep && in.ref[page] != 1) ++mine;
-                }
-                ok = __all_sync(kFull, good);
-                if (!ok) bits |= kStRange;
-                mine = ok ? __reduce_add_sync(kFull, mine) : 0;
-            }
-        }
-        __syncthreads();
-        if (lane == 0) sums[wid] = mine;
-        __syncthreads();
-        long long at = need;
-        for (int w = 0; w < kSelectThreads / 32; ++w) {
-            if (w < wid) at += sums[w];
-            need += sums[w];
-        }
-        if (s < in.rows && lane == 0) a.base[s] = ok ? (int)min(at, 0x7fffffffll) : -1;
+    for (int s = tid; s < in.rows; s += kSelectThreads) {
+        const EvictRow r = evict_row(p, in, a, s);
+        if (r.bad) bits |= kStRange;
+        a.base[s] = r.goes ? pages_for(p, r.len) : -1;                   // pages that the row holds, for now
+        a.count[s] = r.goes ? 0 : -1;
     }
     __syncthreads();
+    const long long entries = (long long)in.rows * in.max_pages;
+#pragma unroll 2
+    for (long long e = tid; e < entries; e += kSelectThreads) {
+        const int row = entries <= 0x7fffffffll ? (int)e / in.max_pages : (int)(e / in.max_pages), at = (int)(e - (long long)row * in.max_pages);
+        const int page = in.table[e], holds = a.base[row];
+        if (at >= holds) continue;
+        if (!page_ok(p, page)) atomicOr(&a.count[row], kOutOfRange);
+        else if (in.ref[page] != 1 && at < pages_for(p, evict_row(p, in, a, row).now)) atomicAdd(&a.count[row], 1);
+    }
+    __syncthreads();
+    long long need = 0, moves = 0;
+    for (int s0 = 0; s0 < in.rows; s0 += kSelectThreads) {
+        const int s = s0 + tid;
+        int count = s < in.rows ? __ldcg(&a.count[s]) : -1;
+        if (count >= kOutOfRange) { bits |= kStRange; count = -1; }
+        const EvictRow r = count >= 0 ? evict_row(p, in, a, s) : EvictRow{};
+        const long long pieces = count >= 0 ? (long long)((r.len + (1 << a.piece_log2) - 1) >> a.piece_log2) * p.L * p.H * 2 : 0;
+        long long total;
+        const long long at = need + sum_before(count >= 0 ? count : 0, &total);
+        need += total;
+        const long long first = moves + sum_before(pieces, &total);
+        moves += total;
+        if (s < in.rows) {
+            a.base[s] = count >= 0 ? (int)min(at, 0x7fffffffll) : -1;
+            a.count[s] = count;
+            a.first[s] = first;
+        }
+    }
     long long found = 0;
     for (long long i0 = 0; i0 < p.n_pages && found < need; i0 += kSelectThreads) {
         const long long i = i0 + tid;
         const bool free = i < p.n_pages && in.ref[i] == 0;
-        const uint32_t m = __ballot_sync(kFull, free);
-        __syncthreads();
-        if (lane == 0) sums[wid] = __popc(m);
-        __syncthreads();
-        long long at = found + __popc(m & lanemask_lt());
-        for (int w = 0; w < kSelectThreads / 32; ++w) {
-            if (w < wid) at += sums[w];
-            found += sums[w];
-        }
+        long long total;
+        const long long at = found + sum_before(free, &total);
         if (free && at < need) a.list[at] = (int)i;
+        found += total;
     }
-    if (found < need) bits |= kStCapacity;
+    const bool short_of = found < need;
+    if (short_of) bits |= kStCapacity;
     if (bits) atomicOr(status, bits);
-    if (tid == 0) a.head[0] = found < need;
+    if (tid == 0) {
+        a.head->short_of = short_of;
+        a.head->ticket = 0;
+        a.first[in.rows] = short_of ? 0 : moves;
+    }
 }
 
 __device__ __forceinline__ void copy_weights(const float* w, float* out, int n, int n_pos) {
     for (int t = threadIdx.x; t < n_pos; t += blockDim.x) out[t] = t < n ? w[t] : 0.f;
 }
 
+struct SelectShared {
+    uint32_t key[kHeld];                          // of a short row's weights
+    int bins[256];
+    int above[kSelectWarps], equal[kSelectWarps];
+    uint32_t prefix;
+    int want;
+};
+
+// The loops are kept small: a block goes through each of them few times, and code that comes from memory for the first time costs more than it does.
 __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev in, const __grid_constant__ BookDev out,
                                                                       const __grid_constant__ EvictArgs a, uint32_t* status) {
+    __shared__ SelectShared sh;
     chain_next();
     if (blockIdx.x == 0) { evict_plan(p, in, a, status); return; }
-    __shared__ int bins[256];
-    __shared__ int warp_above[8], warp_equal[8], warp_recent[8];
-    __shared__ uint32_t prefix_s;
-    __shared__ int want_s;
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-    const long long lane_at = blockIdx.x - 1;
-    for (long long i = lane_at * kSelectThreads + tid; i < p.n_pages; i += (long long)(gridDim.x - 1) * kSelectThreads) out.ref[i] = in.ref[i];
-    const int h = (int)(lane_at % p.H), l = (int)(lane_at / p.H % p.L), s = (int)(lane_at / p.H / p.L);
-    const EvictRow r = evict_row(p, in, a, s);
+    const int lane_at = blockIdx.x - 1, h = lane_at % p.H, l = lane_at / p.H % p.L, s = lane_at / p.H / p.L;
     const float* w = a.weight + (int64_t)s * a.ws_row + (int64_t)l * a.ws_layer + (int64_t)h * a.ws_head;
-    float* to = a.out + lane_at * a.n_pos;
+    float* to = a.out + (int64_t)lane_at * a.n_pos;
+    // the weights are on their way before the row's length is known
+#pragma unroll 4
+    for (int t = tid; t < min(a.n_pos, kHeld); t += kSelectThreads) sh.key[t] = weight_order(w[t]);
+    for (int i = lane_at * kSelectThreads + tid; i < p.n_pages; i += (gridDim.x - 1) * kSelectThreads) out.ref[i] = in.ref[i];
+    const EvictRow r = evict_row(p, in, a, s);
     bool good = r.goes;
     if (good)
-        for (int j = tid; j < (r.len + p.page_pos - 1) / p.page_pos; j += kSelectThreads) good = good && page_ok(p, in.table[(int64_t)s * in.max_pages + j]);
+        for (int j = tid; j < pages_for(p, r.len); j += kSelectThreads) good = good && page_ok(p, in.table[(int64_t)s * in.max_pages + j]);
     if (!__syncthreads_and(good)) {
         copy_weights(w, to, min(max(r.len, 0), a.n_pos), a.n_pos);
         return;
     }
     const int n = r.len - min(a.recent, r.now);                          // candidates; what stands behind them is kept
-    int want = r.now - (r.len - n);
-    // the want-th largest key among the candidates, eight bits at a time
-    uint32_t prefix = 0;
-    bool all = want == 0;                                                // nothing of them is kept
-    for (int shift = 24; shift >= 0 && !all; shift -= 8) {
-        bins[tid] = 0;
+    int want = r.now - (r.len - n);                                      // of the candidates
+    const bool held = r.len <= kHeld;
+    const int pieces = (r.len + (1 << a.piece_log2) - 1) >> a.piece_log2;
+    uint32_t* read = a.read + (int64_t)lane_at * a.pieces * 2;
+    for (int c = tid; c < 2 * pieces; c += kSelectThreads) read[c] = 0;
+    auto key = [&](int t) { return held ? sh.key[t] : weight_order(w[t]); };
+    // the want-th largest key among the candidates, eight bits at a time from the top
+    uint32_t last = 0;
+#pragma unroll 1
+    for (int shift = 24; shift >= 0 && want > 0; shift -= 8) {
+        sh.bins[tid] = 0;
         __syncthreads();
+        const uint32_t above = shift == 24 ? 0u : ~0u << (shift + 8);
+#pragma unroll 2
         for (int t = tid; t < n; t += kSelectThreads) {
-            const uint32_t k = weight_order(w[t]);
-            if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&bins[k >> shift & 255], 1);
+            const uint32_t k = key(t);
+            if ((k & above) == last) atomicAdd(&sh.bins[k >> shift & 255], 1);
         }
         __syncthreads();
-        if (wid == 0) {                                                  // from the top: the bin that the want-th falls into
-            int mine = 0;
-            for (int i = 0; i < 8; ++i) mine += bins[255 - (lane * 8 + i)];
-            int upto = mine;
+        if (wid == 0) {                                                  // the bin that the want-th falls into
+            const int4 b0 = *reinterpret_cast<const int4*>(sh.bins + 8 * (31 - lane)), b1 = *reinterpret_cast<const int4*>(sh.bins + 8 * (31 - lane) + 4);
+            const int sum = b0.x + b0.y + b0.z + b0.w + b1.x + b1.y + b1.z + b1.w;
+            int upto = sum;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const int v = __shfl_up_sync(kFull, upto, o);
                 if (lane >= o) upto += v;
             }
-            if (upto >= want && upto - mine < want) {
-                int left = want - (upto - mine), i = 0;
-                while (left > bins[255 - (lane * 8 + i)]) left -= bins[255 - (lane * 8 + i++)];
-                prefix_s = prefix | (uint32_t)(255 - (lane * 8 + i)) << shift;
-                want_s = left;
+            if (upto >= want && upto - sum < want) {
+                int left = want - (upto - sum), i = 8 * (31 - lane) + 7;
+                while (left > sh.bins[i]) left -= sh.bins[i--];
+                sh.prefix = last | (uint32_t)i << shift;
+                sh.want = left;
             }
         }
         __syncthreads();
-        prefix = prefix_s;
-        want = want_s;
-        __syncthreads();
+        last = sh.prefix;
+        want = sh.want;
     }
-    const uint32_t last = all ? ~0u : prefix;                            // kept: above it, and the first `want` that equal it
-    // a warp takes a run of pieces; first what it keeps, then where that goes
-    const int pieces = (r.len + kPiecePos - 1) / kPiecePos, each = (pieces + 7) / 8, p0 = min(pieces, wid * each), p1 = min(pieces, p0 + each);
-    int above = 0, equal = 0, recent = 0;
-    for (int t0 = p0 * kPiecePos; t0 < min(p1 * kPiecePos, r.len); t0 += 32) {
-        const int t = t0 + lane;
-        const uint32_t k = t < n ? weight_order(w[t]) : 0u;
-        above += __popc(__ballot_sync(kFull, t < n && k > last && !all));
-        equal += __popc(__ballot_sync(kFull, t < n && k == last && !all));
-        recent += __popc(__ballot_sync(kFull, t >= n && t < r.len));
+    const bool nothing = want == 0;
+    // kept: what is above `last`, the first `want` that equal it, and what stands behind the candidates.  A warp takes a run of groups of 32 positions; first
+    // how many it keeps, then where they go.
+    auto is_above = [&](uint32_t k, int t) { return __ballot_sync(kFull, t < n ? !nothing && k > last : t < r.len); };
+    auto is_equal = [&](uint32_t k, int t) { return __ballot_sync(kFull, t < n && !nothing && k == last); };
+    const int groups = (r.len + 31) / 32, each = (groups + kSelectWarps - 1) / kSelectWarps, g0 = wid * each, g1 = min(g0 + each, groups);
+    int above = 0, equal = 0;
+#pragma unroll 2
+    for (int g = g0; g < g1; ++g) {
+        const int t = g * 32 + lane;
+        const uint32_t k = t < n ? key(t) : 0u;
+        above += __popc(is_above(k, t));
+        equal += __popc(is_equal(k, t));
     }
-    if (lane == 0) { warp_above[wid] = above; warp_equal[wid] = equal; warp_recent[wid] = recent; }
+    if (lane == 0) { sh.above[wid] = above; sh.equal[wid] = equal; }
     __syncthreads();
-    int at = 0, ties = 0;                                                // kept, and equal ones seen, before this warp's run
-    for (int v = 0; v < wid; ++v) {
-        at += warp_above[v] + warp_recent[v] + max(0, min(warp_equal[v], want - ties));
-        ties += warp_equal[v];
-    }
+    int at = 0, ties = 0;
+    for (int v = 0; v < wid; ++v) { at += sh.above[v]; ties += sh.equal[v]; }
+    const int words_log2 = a.piece_log2 - 5, words = 1 << words_log2;
+    uint32_t* kept = a.kept + ((int64_t)lane_at * a.pieces << words_log2);
+    int32_t* ahead = a.ahead + (int64_t)lane_at * a.pieces;
     const uint32_t lt = lanemask_lt();
-    for (int t0 = p0 * kPiecePos; t0 < p1 * kPiecePos; t0 += 32) {
-        if (t0 % kPiecePos == 0 && lane == 0) a.ahead[lane_at * a.pieces + t0 / kPiecePos] = at;
-        const int t = t0 + lane;
+#pragma unroll 2
+    for (int g = g0; g < g1; ++g) {
+        const int t = g * 32 + lane;
         const float x = t < r.len ? w[t] : 0.f;
-        const uint32_t k = weight_order(x);
-        const uint32_t eq = __ballot_sync(kFull, t < n && k == last && !all);
-        const bool take = t < n ? !all && (k > last || (k == last && ties + __popc(eq & lt) < want)) : t < r.len;
-        const uint32_t m = __ballot_sync(kFull, take);
-        if (take) to[at + __popc(m & lt)] = x;
-        if (lane == 0) a.kept[(lane_at * a.pieces + t0 / kPiecePos) * 4 + t0 % kPiecePos / 32] = m;
-        at += __popc(m);
+        const uint32_t k = t < n ? key(t) : 0u, up = is_above(k, t), eq = is_equal(k, t);
+        const uint32_t m = up | __ballot_sync(kFull, (eq >> lane & 1u) && ties + __popc(eq & lt) < want);
+        const int here = at + min(ties, want);
+        if (m >> lane & 1u) to[here + __popc(m & lt)] = x;
+        if (lane == 0) {
+            kept[g] = m;
+            if ((g & (words - 1)) == 0) ahead[g >> words_log2] = here;
+        }
+        at += __popc(up);
         ties += __popc(eq);
     }
+    // words of the last piece that no position reaches
+    for (int c = groups + tid; c < pieces << words_log2; c += kSelectThreads) kept[c] = 0;
     for (int t = r.now + tid; t < a.n_pos; t += kSelectThreads) to[t] = 0.f;
 }
 
-// Page j of row s's new positions: its own where nobody else holds it, else a fresh one.  `fresh` of them come before.
+// The row's new pages: its own where nobody else holds them, else fresh ones.
 __device__ __forceinline__ void evict_book(const PoolDev& p, const BookDev& in, const BookDev& out, const EvictArgs& a, int s, uint32_t* status) {
     const int lane = threadIdx.x & 31;                                   // a warp calls it
-    const bool goes = a.base[s] >= 0 && !a.head[0];
-    const int len = in.len[s], now = goes ? evict_row(p, in, a, s).now : len, keep = goes ? (now + p.page_pos - 1) / p.page_pos : in.max_pages;
+    const bool goes = a.base[s] >= 0 && !a.head->short_of;
+    const int len = in.len[s], now = goes ? evict_row(p, in, a, s).now : len, keep = goes ? pages_for(p, now) : in.max_pages;
     int at = a.base[s];
     uint32_t bits = 0;
     for (int j0 = 0; j0 < in.max_pages; j0 += 32) {
@@ -215,7 +272,7 @@ __device__ __forceinline__ void evict_book(const PoolDev& p, const BookDev& in, 
         const int64_t i = (int64_t)s * in.max_pages + j;
         int page = j < in.max_pages ? in.table[i] : -1;
         if (page != -1 && !page_ok(p, page)) bits |= kStRange;
-        const bool fresh = goes && j < keep && j < in.max_pages && in.ref[page] != 1;
+        const bool fresh = goes && j < keep && in.ref[page] != 1;
         const uint32_t m = __ballot_sync(kFull, fresh);
         if (goes && page_ok(p, page) && (fresh || j >= keep)) atomicAdd(&out.ref[page], -1);
         if (fresh) {
@@ -229,77 +286,166 @@ __device__ __forceinline__ void evict_book(const PoolDev& p, const BookDev& in, 
     if (bits) atomicOr(status, bits);
 }
 
-__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev in, const __grid_constant__ BookDev out,
+// The row that a piece belongs to: the last one that begins at or before it.  A warp calls it.
+__device__ __forceinline__ int row_of(const long long* first, int rows, long long item) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, hi = rows;
+    for (;;) {
+        const int step = (hi - lo + 31) / 32, most = (hi - lo - 1) / step, at = lo + min(lane, most) * step;
+        const int j = min(31 - __clz(__ballot_sync(kFull, first[at] <= item)), most);
+        lo += j * step;
+        hi = min(hi, lo + step);
+        if (step == 1) return lo;
+    }
+}
+
+// A piece that a block has taken: its row (-1: there are no more) and its number in it.
+struct Taken { long long rest; int s; };
+// A piece of a row's keys or values of one head, with which of its positions are kept.
+struct Piece {
+    uint8_t* plane;
+    uint32_t* read;                               // its row's first piece's word
+    int s, c, first, n;                           // row (-1: there are no more), piece; where the first that is kept goes; how many are
+    uint32_t kept[4];
+    int before[4];
+};
+
+// Moves the pieces.  A block takes them in order, a row's piece of all layers and heads before its next: it reads what is kept of a piece into shared memory, says so, and writes
+// once the one or two pieces whose places it writes over have been read; those are earlier ones, taken by blocks that run.
+__global__ void __launch_bounds__(kMoveThreads, 6) evict_move_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev in, const __grid_constant__ BookDev out,
                                                                   const __grid_constant__ EvictArgs a, int lanes_log2, uint32_t* status) {
-    __shared__ int64_t src_s[kPiecePos], dst_s[kPiecePos];
-    __shared__ int n_s;
-    chain_wait();
+    extern __shared__ uint4 held[];
+    __shared__ int64_t src_s[2][128], dst_s[2][128];
+    __shared__ Piece piece_s[2];
+    __shared__ Taken taken_s[2];
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-    const bool short_of = a.head[0] != 0;
+    chain_wait();
     for (int s = blockIdx.x * (kMoveThreads / 32) + wid; s < in.rows; s += gridDim.x * (kMoveThreads / 32)) evict_book(p, in, out, a, s, status);
-    const long long items = 2ll * in.rows * p.L * p.H;
-    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-        const long long at_lane = item >> 1;
-        const int kv = (int)(item & 1), h = (int)(at_lane % p.H), l = (int)(at_lane / p.H % p.L), s = (int)(at_lane / p.H / p.L);
-        if (a.base[s] < 0) continue;
-        const EvictRow r = evict_row(p, in, a, s);
-        if (short_of) {                                                  // the weights stay as they are, too
-            if (kv == 0) copy_weights(a.weight + (int64_t)s * a.ws_row + (int64_t)l * a.ws_layer + (int64_t)h * a.ws_head, a.out + at_lane * a.n_pos, min(r.len, a.n_pos), a.n_pos);
-            continue;
+    const long long total = a.first[in.rows], lanes = (long long)p.L * p.H;
+    if (a.head->short_of)                                                // the weights stay as they are, too
+        for (long long at = blockIdx.x; at < lanes * in.rows; at += gridDim.x) {
+            const int h = (int)(at % p.H), l = (int)(at / p.H % p.L), s = (int)(at / p.H / p.L);
+            if (a.base[s] >= 0)
+                copy_weights(a.weight + (int64_t)s * a.ws_row + (int64_t)l * a.ws_layer + (int64_t)h * a.ws_head, a.out + at * a.n_pos, in.len[s], a.n_pos);
         }
-        uint8_t* plane = p.base + (int64_t)l * p.sl + (int64_t)kv * p.skv + (int64_t)h * p.sh;
-        const int32_t* table = in.table + (int64_t)s * in.max_pages;
-        const int pieces = (r.len + kPiecePos - 1) / kPiecePos;
-        for (int c = 0; c < pieces; ++c) {
-            __syncthreads();
-            const int first = a.ahead[at_lane * a.pieces + c];
-            if (tid < kPiecePos) {
-                const uint32_t m = a.kept[(at_lane * a.pieces + c) * 4 + wid];
-                int before = 0, n = 0;
-                for (int v = 0; v < 4; ++v) {
-                    const int cnt = __popc(a.kept[(at_lane * a.pieces + c) * 4 + v]);
-                    if (v < wid) before += cnt;
-                    n += cnt;
-                }
-                if (tid == 0) n_s = n;
-                if (m >> lane & 1u) {
-                    const int i = before + __popc(m & lanemask_lt()), t = c * kPiecePos + tid, to = first + i, j = to / p.page_pos;
-                    const int page = table[t / p.page_pos];
-                    int mine = table[j];
-                    if (in.ref[mine] != 1) {                             // the row's how-manieth fresh page it is
-                        int k = 0;
-                        for (int e = 0; e < j; ++e) k += in.ref[table[e]] != 1;
-                        mine = a.list[a.base[s] + k];
-                    }
-                    src_s[i] = (int64_t)page * p.spage + (int64_t)(t % p.page_pos) * p.sp;
-                    dst_s[i] = (int64_t)mine * p.spage + (int64_t)(to % p.page_pos) * p.sp;
-                }
-            }
-            __syncthreads();
-            const int n = n_s, units = n << lanes_log2;
-            for (int u0 = 0; u0 < units; u0 += 8 * kMoveThreads) {
-                uint4 x[8];
+    const uint32_t held_at = (uint32_t)__cvta_generic_to_shared(held);
+    const int mask = (1 << lanes_log2) - 1, words = 1 << (a.piece_log2 - 5);
+    // What comes next is found in two steps, each by a warp of its own and a piece ahead of the other: its number and row, then what is kept of it.
+    auto take = [&](Taken& x) {
+        const long long item = (long long)__shfl_sync(kFull, lane == 0 ? atomicAdd(&a.head->ticket, 1ull) : 0ull, 0);
+        const int s = item < total ? row_of(a.first, in.rows, item) : -1;
+        if (lane == 0) { x.s = s; x.rest = s < 0 ? 0 : item - a.first[s]; }
+    };
+    auto enter = [&](const Taken& t, Piece& x) {
+        if (t.s < 0) {
+            if (lane == 0) x.s = -1;
+            return;
+        }
+        long long c;
+        int of_row;                               // layer and head
+        if (t.rest <= 0x7fffffffll && lanes <= 0x3fffffffll) {
+            c = (int)t.rest / (int)(2 * lanes);
+            of_row = ((int)t.rest - (int)(2 * lanes) * (int)c) >> 1;
+        } else {
+            c = t.rest / (2 * lanes);
+            of_row = (int)((t.rest - 2 * lanes * c) / 2);
+        }
+        const long long at = (long long)t.s * lanes + of_row;
+        const uint32_t kept = lane < words ? a.kept[(at * a.pieces + c) * words + lane] : 0u;
+        const int first = a.ahead[at * a.pieces + c], l = of_row / p.H, h = of_row - l * p.H, kv = (int)(t.rest & 1), mine = __popc(kept);
+        int before = 0, n = 0;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const int u = u0 + k * kMoveThreads + tid;
-                    if (u < units) x[k] = *reinterpret_cast<const uint4*>(plane + src_s[u >> lanes_log2] + (u & ((1 << lanes_log2) - 1)) * 16);
+        for (int v = 0; v < 4; ++v) {
+            const int m = __shfl_sync(kFull, mine, v);
+            before += v < lane ? m : 0;
+            n += m;
+        }
+        if (lane < 4) { x.kept[lane] = kept; x.before[lane] = before; }
+        if (lane == 0) {
+            x.s = t.s;
+            x.c = (int)c;
+            x.first = first;
+            x.n = n;
+            x.plane = p.base + (int64_t)l * p.sl + (int64_t)kv * p.skv + (int64_t)h * p.sh;
+            x.read = a.read + at * a.pieces * 2 + kv;
+        }
+    };
+    constexpr int taker = kCopyThreads / 32, enterer = taker + 1;
+    if (wid == taker) { take(taken_s[0]); take(taken_s[1]); }
+    __syncthreads();
+    if (wid == enterer) enter(taken_s[0], piece_s[0]);
+    __syncthreads();
+    for (int turn = 0; piece_s[turn].s >= 0; turn ^= 1) {
+        const Piece& x = piece_s[turn];
+        const int32_t* table = in.table + (int64_t)x.s * in.max_pages;
+        int64_t *src = src_s[turn], *dst = dst_s[turn];
+        // fresh pages among those before the first that is written
+        const bool fresh = a.count[x.s] > 0;
+        const int j0 = x.first / p.page_pos;
+        int skipped = 0;
+        if (fresh)
+            for (int e = 0; e < j0; e += kMoveThreads) skipped += __syncthreads_count(e + tid < j0 && in.ref[table[min(e + tid, j0 - 1)]] != 1);
+        if (wid < words) {
+            const uint32_t m = x.kept[wid];
+            if (m >> lane & 1u) {
+                const int i = x.before[wid] + __popc(m & lanemask_lt()), t = (x.c << a.piece_log2) + tid, to = x.first + i, from_page = t / p.page_pos, j = to / p.page_pos;
+                int mine = table[j];
+                if (fresh && in.ref[mine] != 1) {
+                    int k = skipped;
+                    for (int e = j0; e < j; ++e) k += in.ref[table[e]] != 1;
+                    mine = a.list[a.base[x.s] + k];
                 }
-                __syncthreads();                                         // all of the piece has been read that lies before what is written
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const int u = u0 + k * kMoveThreads + tid;
-                    if (u < units && src_s[u >> lanes_log2] != dst_s[u >> lanes_log2])
-                        *reinterpret_cast<uint4*>(plane + dst_s[u >> lanes_log2] + (u & ((1 << lanes_log2) - 1)) * 16) = x[k];
-                }
+                src[i] = (int64_t)table[from_page] * p.spage + (int64_t)(t - from_page * p.page_pos) * p.sp;
+                dst[i] = (int64_t)mine * p.spage + (int64_t)(to - j * p.page_pos) * p.sp;
             }
+        }
+        __syncthreads();
+        const int units = wid < taker ? x.n << lanes_log2 : 0;
+        uint8_t* plane = x.plane;
+#pragma unroll 2
+        for (int u = tid; u < units; u += kCopyThreads) {
+            const int64_t from = src[u >> lanes_log2];
+            if (from != dst[u >> lanes_log2])
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(held_at + u * 16), "l"(plane + from + (u & mask) * 16) : "memory");
+        }
+        if (wid == taker) take(taken_s[turn]);
+        if (wid == enterer) enter(taken_s[turn ^ 1], piece_s[turn ^ 1]);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();
+        if (tid == enterer * 32) asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(x.read + 2 * x.c), "r"(1u) : "memory");
+        // have the pieces been read that this one is written over?
+        bool ok = true;
+        if (wid < 2 && lane == 0 && x.n > 0) {
+            const int other = (wid == 0 ? x.first : x.first + x.n - 1) >> a.piece_log2;
+            if (other < x.c) {
+                uint32_t done = 0;
+                for (uint32_t k = 0; k < kSpin && !done; ++k) asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(done) : "l"(x.read + 2 * other) : "memory");
+                ok = done != 0;
+                if (!ok) atomicOr(status, kStTimeout);
+            }
+        }
+        if (!__syncthreads_and(ok)) continue;
+#pragma unroll 2
+        for (int u = tid; u < units; u += kCopyThreads) {
+            const int64_t to = dst[u >> lanes_log2];
+            if (src[u >> lanes_log2] != to) *reinterpret_cast<uint4*>(plane + to + (u & mask) * 16) = held[u];
         }
     }
 }
 
-int pieces_of(int n_pos) { return (n_pos + kPiecePos - 1) / kPiecePos; }
-uint64_t evict_bytes(const PoolDev& p, long long rows, int n_pos) {
-    const uint64_t words = 4 + (((uint64_t)rows + p.n_pages + 3) & ~3ull), lanes = (uint64_t)rows * p.L * p.H;
-    return 4 * (words + lanes * pieces_of(n_pos) * 5);
+struct EvictLayout { uint64_t first, base, count, list, kept, ahead, read, bytes; };
+EvictLayout layout_of(const PoolDev& p, long long rows, int n_pos) {
+    const uint64_t piece = 1u << piece_log2(p.d * p.esz), pieces = ((uint64_t)n_pos + piece - 1) / piece, lanes = (uint64_t)rows * p.L * p.H;
+    EvictLayout x;
+    x.first = sizeof(EvictHead);
+    x.base = x.first + 8 * (rows + 1);
+    x.count = x.base + 4 * rows;
+    x.list = x.count + 4 * rows;
+    x.kept = x.list + 4ull * p.n_pages;
+    x.ahead = x.kept + lanes * pieces * (piece / 32) * 4;
+    x.read = x.ahead + lanes * pieces * 4;
+    x.bytes = x.read + lanes * pieces * 8;
+    return x;
 }
 plc_status check_lanes(const PoolDev& p, long long rows, int n_pos) {
     if (n_pos < 1) return PLC_E_INVALID;
@@ -324,7 +470,7 @@ plc_status plc_pages_evict_workspace(const plc_page_pool* pool, int32_t rows, in
     if (rows < 1 || !bytes) return PLC_E_INVALID;
     if (rows > (1 << 20)) return PLC_E_SHAPE;
     if ((rc = check_lanes(p, rows, n_pos))) return rc;
-    *bytes = evict_bytes(p, rows, n_pos);
+    *bytes = layout_of(p, rows, n_pos).bytes;
     return PLC_OK;
 }
 
@@ -341,21 +487,22 @@ plc_status plc_pages_evict(const plc_page_pool* pool, const plc_page_book* in, c
     const uint64_t t = 4ull * i.rows * i.max_pages, n = 4ull * p.n_pages;
     if (overlap(i.table, t, o.table, t) || overlap(i.len, 4ull * i.rows, o.len, 4ull * i.rows) || overlap(i.ref, n, o.ref, n)) return PLC_E_INVALID;
     if (weights->base_dev == out_weights_dev) return PLC_E_INVALID;
-    if (workspace_bytes < evict_bytes(p, i.rows, weights->n_pos)) return PLC_E_CAPACITY;
+    const EvictLayout x = layout_of(p, i.rows, weights->n_pos);
+    if (workspace_bytes < x.bytes) return PLC_E_CAPACITY;
     const long long lanes = (long long)i.rows * p.L * p.H;
-    EvictArgs a{weights->base_dev, weights->stride_row, weights->stride_layer, weights->stride_head, weights->n_pos, out_weights_dev, budget_dev, budget, recent,
-                nullptr, nullptr, nullptr, nullptr, nullptr, pieces_of(weights->n_pos)};
-    a.head = static_cast<int32_t*>(workspace_dev);
-    a.base = a.head + 4;
-    a.list = a.base + i.rows;
-    a.kept = reinterpret_cast<uint32_t*>(a.head + 4 + (((uint64_t)i.rows + p.n_pages + 3) & ~3ull));
-    a.ahead = reinterpret_cast<int32_t*>(a.kept + (uint64_t)lanes * a.pieces * 4);
+    uint8_t* ws = static_cast<uint8_t*>(workspace_dev);
+    const int log2 = piece_log2(p.d * p.esz), piece = 1 << log2;
+    const EvictArgs a{weights->base_dev, weights->stride_row, weights->stride_layer, weights->stride_head, weights->n_pos, out_weights_dev, budget_dev, budget, recent,
+                      log2, (int)(((long long)weights->n_pos + piece - 1) / piece), reinterpret_cast<EvictHead*>(ws), reinterpret_cast<long long*>(ws + x.first),
+                      reinterpret_cast<int32_t*>(ws + x.base), reinterpret_cast<int32_t*>(ws + x.count), reinterpret_cast<int32_t*>(ws + x.list),
+                      reinterpret_cast<uint32_t*>(ws + x.kept), reinterpret_cast<int32_t*>(ws + x.ahead), reinterpret_cast<uint32_t*>(ws + x.read)};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     int lanes_log2 = 0;
     while ((16 << lanes_log2) < p.d * p.esz) ++lanes_log2;
     if (launch_kernel(evict_select_kernel, (unsigned)(1 + lanes), kSelectThreads, 0, st, false, 1, p, i, o, a, status_dev) != cudaSuccess) return PLC_E_CUDA;
-    const long long most = 8ll * sm_count();
-    if (launch_kernel(evict_move_kernel, (unsigned)(2 * lanes < most ? 2 * lanes : most), kMoveThreads, 0, st, true, 1, p, i, o, a, lanes_log2, status_dev) != cudaSuccess)
+    // as many blocks as run at once (six of 32 KB an SM), or as the pieces that full rows would have
+    const long long most = 6ll * sm_count(), want = 2 * lanes * a.pieces;
+    if (launch_kernel(evict_move_kernel, (unsigned)(want < most ? want : most), kMoveThreads, (size_t)piece * p.d * p.esz, st, true, 1, p, i, o, a, lanes_log2, status_dev) != cudaSuccess)
         return PLC_E_CUDA;
     count_launch(2);
     return PLC_OK;
