@@ -36,6 +36,8 @@ struct EvictArgs {
     int32_t* base;                                // [rows] index of the row's first fresh page in `list`; -1: the row stays as it is
     int32_t* count;                               // [rows] its fresh pages
     int32_t* list;                                // [n_pages]
+    int32_t* rank;                                // [rows][row_pages] the how-manieth fresh page of its row a new page is, -1: the row's own
+    int row_pages;                                // pages that n_pos positions fill
     uint32_t* kept;                               // [rows][L][H][pieces][positions of a piece / 32] a bit a position
     int32_t* ahead;                               // [rows][L][H][pieces] positions kept before the piece
     uint32_t* read;                               // [rows][L][H][pieces][2] a piece's keys, values have been read
@@ -178,6 +180,17 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const __gr
         copy_weights(w, to, min(max(r.len, 0), a.n_pos), a.n_pos);
         return;
     }
+    if (l == 0 && h == 0) {                       // a block of the row: which of its new pages are fresh ones
+        const int keep = pages_for(p, r.now);
+        long long before = 0, some;
+        for (int j0 = 0; j0 < keep; j0 += kSelectThreads) {
+            const int j = j0 + tid;
+            const bool shared = j < keep && in.ref[in.table[(int64_t)s * in.max_pages + j]] != 1;
+            const long long at = before + sum_before(shared, &some);
+            if (j < keep) a.rank[(int64_t)s * a.row_pages + j] = shared ? (int)at : -1;
+            before += some;
+        }
+    }
     const int n = r.len - min(a.recent, r.now);                          // candidates; what stands behind them is kept
     int want = r.now - (r.len - n);                                      // of the candidates
     const bool held = r.len <= kHeld;
@@ -265,22 +278,15 @@ __device__ __forceinline__ void evict_book(const PoolDev& p, const BookDev& in, 
     const int lane = threadIdx.x & 31;                                   // a warp calls it
     const bool goes = a.base[s] >= 0 && !a.head->short_of;
     const int len = in.len[s], now = goes ? evict_row(p, in, a, s).now : len, keep = goes ? pages_for(p, now) : in.max_pages;
-    int at = a.base[s];
     uint32_t bits = 0;
-    for (int j0 = 0; j0 < in.max_pages; j0 += 32) {
-        const int j = j0 + lane;
+    for (int j = lane; j < in.max_pages; j += 32) {
         const int64_t i = (int64_t)s * in.max_pages + j;
-        int page = j < in.max_pages ? in.table[i] : -1;
+        const int page = in.table[i], rank = goes && j < keep ? a.rank[(int64_t)s * a.row_pages + j] : -1;
         if (page != -1 && !page_ok(p, page)) bits |= kStRange;
-        const bool fresh = goes && j < keep && in.ref[page] != 1;
-        const uint32_t m = __ballot_sync(kFull, fresh);
-        if (goes && page_ok(p, page) && (fresh || j >= keep)) atomicAdd(&out.ref[page], -1);
-        if (fresh) {
-            page = a.list[at + __popc(m & lanemask_lt())];
-            out.ref[page] = 1;                                           // it was free, and this row alone has it
-        }
-        at += __popc(m);
-        if (j < in.max_pages) out.table[i] = j < keep ? page : -1;
+        if (goes && page_ok(p, page) && (rank >= 0 || j >= keep)) atomicAdd(&out.ref[page], -1);
+        const int now_at = rank >= 0 ? a.list[a.base[s] + rank] : page;
+        if (rank >= 0) out.ref[now_at] = 1;                              // it was free, and this row alone has it
+        out.table[i] = j < keep ? now_at : -1;
     }
     if (lane == 0) out.len[s] = now;
     if (bits) atomicOr(status, bits);
@@ -379,22 +385,12 @@ __global__ void __launch_bounds__(kMoveThreads, 6) evict_move_kernel(const __gri
         const Piece& x = piece_s[turn];
         const int32_t* table = in.table + (int64_t)x.s * in.max_pages;
         int64_t *src = src_s[turn], *dst = dst_s[turn];
-        // fresh pages among those before the first that is written
         const bool fresh = a.count[x.s] > 0;
-        const int j0 = x.first / p.page_pos;
-        int skipped = 0;
-        if (fresh)
-            for (int e = 0; e < j0; e += kMoveThreads) skipped += __syncthreads_count(e + tid < j0 && in.ref[table[min(e + tid, j0 - 1)]] != 1);
         if (wid < words) {
             const uint32_t m = x.kept[wid];
             if (m >> lane & 1u) {
                 const int i = x.before[wid] + __popc(m & lanemask_lt()), t = (x.c << a.piece_log2) + tid, to = x.first + i, from_page = t / p.page_pos, j = to / p.page_pos;
-                int mine = table[j];
-                if (fresh && in.ref[mine] != 1) {
-                    int k = skipped;
-                    for (int e = j0; e < j; ++e) k += in.ref[table[e]] != 1;
-                    mine = a.list[a.base[x.s] + k];
-                }
+                const int rank = fresh ? a.rank[(int64_t)x.s * a.row_pages + j] : -1, mine = rank >= 0 ? a.list[a.base[x.s] + rank] : table[j];
                 src[i] = (int64_t)table[from_page] * p.spage + (int64_t)(t - from_page * p.page_pos) * p.sp;
                 dst[i] = (int64_t)mine * p.spage + (int64_t)(to - j * p.page_pos) * p.sp;
             }
@@ -412,14 +408,16 @@ __global__ void __launch_bounds__(kMoveThreads, 6) evict_move_kernel(const __gri
         if (wid == enterer) enter(taken_s[turn ^ 1], piece_s[turn ^ 1]);
         asm volatile("cp.async.wait_all;" ::: "memory");
         __syncthreads();
-        if (tid == enterer * 32) asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(x.read + 2 * x.c), "r"(1u) : "memory");
+        // The copies have arrived, so that nothing can change what they brought: the word needs no fence before it (which, behind the block's writes, took 4500
+        // clocks), and who sees it writes behind a barrier.
+        if (tid == enterer * 32) asm volatile("st.relaxed.gpu.global.u32 [%0], %1;" ::"l"(x.read + 2 * x.c), "r"(1u) : "memory");
         // have the pieces been read that this one is written over?
         bool ok = true;
         if (wid < 2 && lane == 0 && x.n > 0) {
             const int other = (wid == 0 ? x.first : x.first + x.n - 1) >> a.piece_log2;
             if (other < x.c) {
                 uint32_t done = 0;
-                for (uint32_t k = 0; k < kSpin && !done; ++k) asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(done) : "l"(x.read + 2 * other) : "memory");
+                for (uint32_t k = 0; k < kSpin && !done; ++k) asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(done) : "l"(x.read + 2 * other) : "memory");
                 ok = done != 0;
                 if (!ok) atomicOr(status, kStTimeout);
             }
@@ -433,7 +431,8 @@ __global__ void __launch_bounds__(kMoveThreads, 6) evict_move_kernel(const __gri
     }
 }
 
-struct EvictLayout { uint64_t first, base, count, list, kept, ahead, read, bytes; };
+struct EvictLayout { uint64_t first, base, count, list, rank, kept, ahead, read, bytes; };
+uint64_t row_pages(const PoolDev& p, int n_pos) { return ((uint64_t)n_pos + p.page_pos - 1) / p.page_pos; }
 EvictLayout layout_of(const PoolDev& p, long long rows, int n_pos) {
     const uint64_t piece = 1u << piece_log2(p.d * p.esz), pieces = ((uint64_t)n_pos + piece - 1) / piece, lanes = (uint64_t)rows * p.L * p.H;
     EvictLayout x;
@@ -441,7 +440,8 @@ EvictLayout layout_of(const PoolDev& p, long long rows, int n_pos) {
     x.base = x.first + 8 * (rows + 1);
     x.count = x.base + 4 * rows;
     x.list = x.count + 4 * rows;
-    x.kept = x.list + 4ull * p.n_pages;
+    x.rank = x.list + 4ull * p.n_pages;
+    x.kept = x.rank + 4 * rows * row_pages(p, n_pos);
     x.ahead = x.kept + lanes * pieces * (piece / 32) * 4;
     x.read = x.ahead + lanes * pieces * 4;
     x.bytes = x.read + lanes * pieces * 8;
@@ -495,6 +495,7 @@ plc_status plc_pages_evict(const plc_page_pool* pool, const plc_page_book* in, c
     const EvictArgs a{weights->base_dev, weights->stride_row, weights->stride_layer, weights->stride_head, weights->n_pos, out_weights_dev, budget_dev, budget, recent,
                       log2, (int)(((long long)weights->n_pos + piece - 1) / piece), reinterpret_cast<EvictHead*>(ws), reinterpret_cast<long long*>(ws + x.first),
                       reinterpret_cast<int32_t*>(ws + x.base), reinterpret_cast<int32_t*>(ws + x.count), reinterpret_cast<int32_t*>(ws + x.list),
+                      reinterpret_cast<int32_t*>(ws + x.rank), (int)row_pages(p, weights->n_pos),
                       reinterpret_cast<uint32_t*>(ws + x.kept), reinterpret_cast<int32_t*>(ws + x.ahead), reinterpret_cast<uint32_t*>(ws + x.read)};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     int lanes_log2 = 0;

@@ -403,9 +403,10 @@ class PagePool:
             if len(self._need_bytes) >= 4096:
                 self._need_bytes.clear()
             need = self._need_bytes[(book.rows, heads, n_list, "weigh")] = b.value
-        ws = torch.empty(need, dtype=torch.uint8, device=dev).data_ptr() if need else None
+        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
         t = WeighQueries(q.data_ptr(), row, head, lse.data_ptr(), None if rows is None else rows.data_ptr(), begin.data_ptr(), N, n_list, heads)
-        _check(_run(dev, api.plc_pages_weigh, self._by, layer, a, C.byref(t), d ** -0.5 if scale is None else scale, decay, C.byref(w), ws, need,
+        _check(_run(dev, api.plc_pages_weigh, self._by, layer, a, C.byref(t), d ** -0.5 if scale is None else scale, decay, C.byref(w),
+                    None if ws is None else ws.data_ptr(), need,
                     self._word), where)
         return weight
 
@@ -418,11 +419,11 @@ class PagePool:
         a = self._book(book, where)
         w = self._weights(weight, book, where)
         _int32(E_INVALID, where, recent)
-        budgets = None
-        if torch.is_tensor(budget):
+        budgets, scalar = None, budget
+        if torch.is_tensor(budget):                          # (held on to by its own name: what is allocated below must not take its place)
             _need(_i32(budget, dev, where).numel() == book.rows, E_SHAPE, where)
-            budgets, budget = budget.data_ptr(), 0
-        _int32(E_INVALID, where, budget)
+            budgets, scalar = budget.data_ptr(), 0
+        _int32(E_INVALID, where, scalar)
         n_pos = weight.shape[3]
         need = self._need_bytes.get((book.rows, n_pos))
         if need is None:
@@ -434,7 +435,7 @@ class PagePool:
         new, _ = PageBook._new(book.rows, book.max_pages, self.n_pages, dev)
         ws = torch.empty(need, dtype=torch.uint8, device=dev)
         out = torch.empty(weight.shape, dtype=torch.float32, device=dev)
-        _check(_run(dev, api.plc_pages_evict, self._by, a, C.byref(w), budgets, budget, recent, new._by, out.data_ptr(), ws.data_ptr(), need, self._word), where)
+        _check(_run(dev, api.plc_pages_evict, self._by, a, C.byref(w), budgets, scalar, recent, new._by, out.data_ptr(), ws.data_ptr(), need, self._word), where)
         return new, out
 
     def check(self):
