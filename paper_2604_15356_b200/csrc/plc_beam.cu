@@ -27,6 +27,14 @@ struct SelectArgs : RowArgs {
     float* out_score; int32_t* out_parent; int32_t* out_token;
 };
 
+template <class T>
+__global__ void __launch_bounds__(kRowThreads, kResident) beam_rows_kernel(RowArgs a) {
+    chain_next();
+    const int row = blockIdx.x / a.parts;
+    if (a.done && a.done[row]) return;            // one continuation, at the beam's own score: the logits are not needed
+    row_part<T, false>(a, row, blockIdx.x - row * a.parts);
+}
+
 // A continuation: its score's order-preserving bits (0: none), and its place (row in the session, column) as one number.
 struct Cont { unsigned long long score; uint32_t place; };
 __device__ __forceinline__ bool better(const Cont& a, const Cont& b) { return a.score > b.score || (a.score == b.score && a.place < b.place); }
@@ -240,7 +248,7 @@ plc_status plc_beam_select(const void* logits_dev, int32_t dtype, int64_t row_st
     a.top = reinterpret_cast<float*>(a.sum + rows * a.parts);
     a.out_score = out_score_dev; a.out_parent = out_parent_dev; a.out_token = out_token_dev;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    auto kern = dtype == PLC_OUT_F32 ? rows_kernel<float, false> : dtype == PLC_OUT_F16 ? rows_kernel<__half, false> : rows_kernel<__nv_bfloat16, false>;
+    auto kern = dtype == PLC_OUT_F32 ? beam_rows_kernel<float> : dtype == PLC_OUT_F16 ? beam_rows_kernel<__half> : beam_rows_kernel<__nv_bfloat16>;
     if (launch_kernel(kern, (unsigned)(rows * a.parts), kRowThreads, 0, st, false, 1, static_cast<RowArgs>(a)) != cudaSuccess) return PLC_E_CUDA;
     const size_t smem = (size_t)beams * a.parts * a.k * 8;
     if (cudaFuncSetAttribute(beam_merge_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostListed * 8) != cudaSuccess) return PLC_E_CUDA;

@@ -171,14 +171,28 @@ __device__ __noinline__ uint32_t cut(unsigned long long* buf, int n, int k, int 
     return least;
 }
 
+template <class T> struct Step { static constexpr int groups = 4; };                  // 64 bytes a lane
+template <> struct Step<float> { static constexpr int groups = 2; };
+
+// What a lane adds to the spread in a step that holds a logit of -inf: that has the exponential 0 and adds nothing, not 0 times infinity.  `left`: logits from x on.
+template <class T>
+__device__ __noinline__ float careful_spread(const T* x, int left, float m) {
+    float sum = 0.f;
+    for (int g = 0; g < Step<T>::groups; ++g)
+        for (int k = 0; k < 8; ++k) {
+            if (g * 256 + k >= left) continue;
+            const float d = fmaxf((widen(x[g * 256 + k]) - m) * kLog2e, -1e4f);
+            sum = fmaf(exp2_approx(d), d, sum);
+        }
+    return sum;
+}
+
 // A block takes a part of a row in two passes.  The first streams: a warp takes 32 lanes times kGroups times eight logits a step, the next step's loads on
 // their way, forms the sum and keeps the maximum of each lane's chunks of steps.  The k-th largest of the lanes' maxima is a bound that k logits reach and
 // few others do, so the second pass looks at the chunks that reach it alone: about k of them, from L2.
-template <class T> struct Step { static constexpr int groups = 4; };                  // 64 bytes a lane
-template <> struct Step<float> { static constexpr int groups = 2; };
 // SPREAD: also the sum that the entropy is made of.
 template <class T, bool SPREAD>
-__global__ void __launch_bounds__(kRowThreads, kResident) rows_kernel(RowArgs a) {
+__device__ __forceinline__ void row_part(const RowArgs& a, int row, int part) {
     constexpr int groups = Step<T>::groups, step = 256 * groups;
     __shared__ float tops[kChunks][kRowThreads];
     __shared__ unsigned long long found[kRoom];
@@ -187,9 +201,6 @@ __global__ void __launch_bounds__(kRowThreads, kResident) rows_kernel(RowArgs a)
     __shared__ __align__(16) uint32_t order[kRowThreads];
     __shared__ float bound;
     __shared__ int count;
-    chain_next();
-    const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
-    if (a.done && a.done[row]) return;            // one continuation, at the beam's own score: the logits are not needed
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const T* x0 = static_cast<const T*>(a.logits) + (int64_t)row * a.row_stride;
     const bool vec = (reinterpret_cast<uintptr_t>(x0) & 15) == 0;
@@ -228,32 +239,49 @@ __global__ void __launch_bounds__(kRowThreads, kResident) rows_kernel(RowArgs a)
             s *= f;
             m = t;
         }
-        float part_sum = 0.f, part_spread = 0.f;
+        float part_sum = 0.f;
         const unsigned long long neg = pack2(-m, -m), scale = pack2(kLog2e, kLog2e);
+        if constexpr (SPREAD) {
+            unsigned long long sums[2] = {0ull, 0ull}, far[2] = {0ull, 0ull};
 #pragma unroll
-        for (int g = 0; g < groups; ++g) {
-            float x[8];
-            now[g].widen(x);
-            unsigned long long e[4];
+            for (int g = 0; g < groups; ++g) {
+                float x[8];
+                now[g].widen(x);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                float lo, hi;
-                unpack2(fma2(add2(pack2(x[2 * k], x[2 * k + 1]), neg), scale, 0ull), lo, hi);
-                e[k] = pack2(exp2_approx(lo), exp2_approx(hi));
-                if (SPREAD) {                     // a logit of -inf has the exponential 0, not 0 times infinity
-                    const float d0 = fmaxf(lo, -1e4f), d1 = fmaxf(hi, -1e4f);
-                    float e0, e1;
-                    unpack2(e[k], e0, e1);
-                    part_spread = fmaf(e0, -d0, part_spread);
-                    part_spread = fmaf(e1, -d1, part_spread);
+                for (int k = 0; k < 4; ++k) {
+                    const unsigned long long d = fma2(add2(pack2(x[2 * k], x[2 * k + 1]), neg), scale, 0ull);
+                    float lo, hi;
+                    unpack2(d, lo, hi);
+                    const unsigned long long e = pack2(exp2_approx(lo), exp2_approx(hi));
+                    sums[k & 1] = add2(sums[k & 1], e);
+                    far[k & 1] = fma2(e, d, far[k & 1]);
                 }
             }
             float lo, hi;
-            unpack2(add2(add2(e[0], e[1]), add2(e[2], e[3])), lo, hi);
-            part_sum += lo + hi;
+            unpack2(add2(sums[0], sums[1]), lo, hi);
+            part_sum = lo + hi;
+            unpack2(add2(far[0], far[1]), lo, hi);
+            float part_spread = lo + hi;
+            if (part_spread != part_spread) part_spread = careful_spread(x0 + column(wid, i) + lane * 8, c1 - column(wid, i) - lane * 8, m);
+            spread -= (double)part_spread;
+        } else {
+#pragma unroll
+            for (int g = 0; g < groups; ++g) {
+                float x[8];
+                now[g].widen(x);
+                unsigned long long e[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    float lo, hi;
+                    unpack2(fma2(add2(pack2(x[2 * k], x[2 * k + 1]), neg), scale, 0ull), lo, hi);
+                    e[k] = pack2(exp2_approx(lo), exp2_approx(hi));
+                }
+                float lo, hi;
+                unpack2(add2(add2(e[0], e[1]), add2(e[2], e[3])), lo, hi);
+                part_sum += lo + hi;
+            }
         }
         s += (double)part_sum;
-        if (SPREAD) spread += (double)part_spread;
         if (--left == 0 || i + 1 == steps) {
             tops[chunk++][tid] = chunk_top;
             top = fmaxf(top, chunk_top);

@@ -13,7 +13,6 @@ namespace {
 
 constexpr int kMostTop = 128, kMostTokens = 1 << 20;
 constexpr int kMostListed = 1024;                 // entries of a row's lists
-constexpr int kJoinThreads = 128;
 
 struct LogprobArgs : RowArgs {
     const int32_t* tokens; int n_tokens, n_top, esz_log2, bf16;
@@ -21,27 +20,27 @@ struct LogprobArgs : RowArgs {
     uint32_t* status;
 };
 
-// A block a row.
-__global__ void __launch_bounds__(kJoinThreads) logprob_join_kernel(LogprobArgs a) {
-    __shared__ unsigned long long keys[kMostListed];
+// A row's results from its parts: a block, of the same threads as a part.  LISTED: entries of its lists at most.
+template <int LISTED>
+__device__ __forceinline__ void finish_row(const LogprobArgs& a, int row) {
+    __shared__ unsigned long long keys[LISTED];
     __shared__ double log_sum;
     __shared__ float row_top;
-    chain_wait();
-    const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
+    const int tid = threadIdx.x, lane = tid & 31;
     const long long slot = (long long)row * a.parts;
     const int entries = a.parts * a.k;
-    for (int i = tid; i < entries; i += kJoinThreads) keys[i] = a.list[slot * a.k + i];
+    for (int i = tid; i < entries; i += kRowThreads) keys[i] = __ldcg(a.list + slot * a.k + i);
     if (tid < 32) {                               // at most 64 parts, two a lane
         float top = -FLT_MAX;
-        for (int q = lane; q < a.parts; q += 32) top = fmaxf(top, a.top[slot + q]);
+        for (int q = lane; q < a.parts; q += 32) top = fmaxf(top, __ldcg(a.top + slot + q));
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
         double sum = 0.0, spread = 0.0;
         for (int q = lane; q < a.parts; q += 32) {
-            const float t = a.top[slot + q];
-            const double f = (double)exp2_approx((t - top) * kLog2e), s = a.sum[slot + q];
+            const float t = __ldcg(a.top + slot + q);
+            const double f = (double)exp2_approx((t - top) * kLog2e), s = __ldcg(a.sum + slot + q);
             sum += f * s;
-            if (s != 0.0) spread += f * (a.spread[slot + q] + s * ((double)top - (double)t));
+            if (s != 0.0) spread += f * (__ldcg(a.spread + slot + q) + s * ((double)top - (double)t));
         }
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
@@ -59,7 +58,7 @@ __global__ void __launch_bounds__(kJoinThreads) logprob_join_kernel(LogprobArgs 
     __syncthreads();
     const double l = log_sum;
     const float top = row_top;
-    for (int i = tid; i < a.n_tokens; i += kJoinThreads) {
+    for (int i = tid; i < a.n_tokens; i += kRowThreads) {
         const long long at = (long long)row * a.n_tokens + i;
         const int v = a.tokens[at];
         float y = 0.f;
@@ -72,7 +71,7 @@ __global__ void __launch_bounds__(kJoinThreads) logprob_join_kernel(LogprobArgs 
         a.logp[at] = y;
     }
     // an entry's place is the number of better ones: those before it in its own list, and in each other list as many as a bisection finds
-    for (int i = tid; i < entries; i += kJoinThreads) {
+    for (int i = tid; i < entries; i += kRowThreads) {
         const unsigned long long key = keys[i];
         const int mine = i / a.k;
         int place = i - mine * a.k;
@@ -94,27 +93,55 @@ __global__ void __launch_bounds__(kJoinThreads) logprob_join_kernel(LogprobArgs 
             a.top_token[(long long)row * a.n_top + place] = some ? (int)~(uint32_t)key : -1;
         }
     }
-    for (int i = min(a.n_top, a.V) + tid; i < a.n_top; i += kJoinThreads) {
+    for (int i = min(a.n_top, a.V) + tid; i < a.n_top; i += kRowThreads) {
         a.top_logp[(long long)row * a.n_top + i] = -INFINITY;
         a.top_token[(long long)row * a.n_top + i] = -1;
     }
 }
 
-// Parts of a row, as for beams: the least rounds of blocks times (a warp's logits plus what is done once).
-constexpr int kSetUp = 1500;
-int row_parts(long long rows, int V, int k) {
-    const long long most = (V + 4095) / 4096, fit = k ? kMostListed / k : 64, slots = (long long)kResident * sm_count();
+// How the parts of a row come together: a block has a row; a cluster has it, whose first block finishes it behind the cluster's barrier; or a second launch does.
+enum Way { kBlock, kCluster, kJoin };
+template <class T, int WAY>
+__global__ void __launch_bounds__(kRowThreads, kResident) logprob_rows_kernel(const __grid_constant__ LogprobArgs a) {
+    if (WAY == kJoin) chain_next();
+    const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
+    row_part<T, true>(a, row, part);
+    if (WAY == kJoin) return;
+    if (WAY == kBlock) __syncthreads();
+    else {
+        asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+        if (part > 0) return;
+    }
+    finish_row<WAY == kBlock ? kMostTop : kMostListed>(a, row);
+}
+__global__ void __launch_bounds__(kRowThreads) logprob_join_kernel(const __grid_constant__ LogprobArgs a) {
+    chain_wait();
+    finish_row<kMostListed>(a, blockIdx.x);
+}
+
+// Rows that are few enough for a cluster each take one launch; with vocabularies beyond kMostClustered
+// more blocks a row are worth the second one.  Else as many parts as for beams: the least rounds of blocks times (a warp's logits plus what is done once).
+constexpr int kSetUp = 1500, kMostClustered = 1 << 18;
+struct RowPlan { Way way; int parts; };
+RowPlan row_plan(long long rows, int V, int k) {
+    const long long slots = (long long)kResident * sm_count();
+    if (rows * 8 <= slots && V <= kMostClustered) {
+        int parts = 1;
+        while (parts < 8 && V > 4096 * parts) parts *= 2;
+        return RowPlan{parts == 1 ? kBlock : kCluster, parts};
+    }
+    const long long most = (V + 4095) / 4096, fit = k ? kMostListed / k : 64;
     long long best = 1, least = 0;
     for (long long q = 1; q <= most && q <= fit && q <= 64; ++q) {
         const long long cost = (rows * q + slots - 1) / slots * ((V + q - 1) / q / kRowWarps + kSetUp);
         if (q == 1 || cost < least) { best = q; least = cost; }
     }
-    return (int)best;
+    return RowPlan{best == 1 ? kBlock : kJoin, (int)best};
 }
-uint64_t logprob_bytes(long long rows, int V, int n_top, int* parts, int* k) {
+uint64_t logprob_bytes(long long rows, int V, int n_top, RowPlan* plan, int* k) {
     *k = n_top < V ? n_top : V;
-    *parts = row_parts(rows, V, *k);
-    return (uint64_t)rows * *parts * (8ull * *k + 20);
+    *plan = row_plan(rows, V, *k);
+    return (uint64_t)rows * plan->parts * (8ull * *k + 20);
 }
 plc_status check_rows(int32_t rows, int32_t vocab, int32_t n_tokens, int32_t n_top) {
     if (rows < 1 || vocab < 1 || n_tokens < 0 || n_top < 0) return PLC_E_INVALID;
@@ -132,8 +159,9 @@ plc_status plc_token_logprobs_workspace(int32_t rows, int32_t vocab, int32_t n_t
     const plc_status rc = check_rows(rows, vocab, 0, n_top);
     if (rc) return rc;
     if (!bytes) return PLC_E_INVALID;
-    int parts, k;
-    *bytes = logprob_bytes(rows, vocab, n_top, &parts, &k);
+    RowPlan plan;
+    int k;
+    *bytes = logprob_bytes(rows, vocab, n_top, &plan, &k);
     return PLC_OK;
 }
 
@@ -147,7 +175,9 @@ plc_status plc_token_logprobs(const void* logits_dev, int32_t dtype, int64_t row
     const int esz = dtype == PLC_OUT_F32 ? 4 : 2;
     if ((reinterpret_cast<uintptr_t>(logits_dev) & (esz - 1)) || (reinterpret_cast<uintptr_t>(workspace_dev) & 15)) return PLC_E_ALIGN;
     LogprobArgs a{};
-    const uint64_t need = logprob_bytes(rows, vocab, n_top, &a.parts, &a.k);
+    RowPlan plan;
+    const uint64_t need = logprob_bytes(rows, vocab, n_top, &plan, &a.k);
+    a.parts = plan.parts;
     if (workspace_bytes < need) return PLC_E_CAPACITY;
     if ((long long)rows * a.parts > 0x7fffffffll) return PLC_E_SHAPE;
     a.logits = logits_dev; a.row_stride = row_stride; a.rows = rows; a.V = vocab;
@@ -159,10 +189,15 @@ plc_status plc_token_logprobs(const void* logits_dev, int32_t dtype, int64_t row
     a.tokens = tokens_dev; a.n_tokens = n_tokens; a.n_top = n_top; a.esz_log2 = esz == 4 ? 2 : 1; a.bf16 = dtype == PLC_OUT_BF16;
     a.logp = logp_dev; a.entropy = entropy_dev; a.top_logp = top_logp_dev; a.top_token = top_token_dev; a.status = status_dev;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    auto kern = dtype == PLC_OUT_F32 ? rows_kernel<float, true> : dtype == PLC_OUT_F16 ? rows_kernel<__half, true> : rows_kernel<__nv_bfloat16, true>;
-    if (launch_kernel(kern, (unsigned)(rows * a.parts), kRowThreads, 0, st, false, 1, static_cast<RowArgs>(a)) != cudaSuccess) return PLC_E_CUDA;
-    if (launch_kernel(logprob_join_kernel, (unsigned)rows, kJoinThreads, 0, st, true, 1, a) != cudaSuccess) return PLC_E_CUDA;
-    count_launch(2);
+    auto go = [&](auto* block, auto* cluster, auto* join) {
+        return launch_kernel(plan.way == kBlock ? block : plan.way == kCluster ? cluster : join, (unsigned)(rows * a.parts), kRowThreads, 0, st, false,
+                             plan.way == kCluster ? (unsigned)a.parts : 1u, a);
+    };
+#define PLC_ROWS(T) go(logprob_rows_kernel<T, kBlock>, logprob_rows_kernel<T, kCluster>, logprob_rows_kernel<T, kJoin>)
+    if ((dtype == PLC_OUT_F32 ? PLC_ROWS(float) : dtype == PLC_OUT_F16 ? PLC_ROWS(__half) : PLC_ROWS(__nv_bfloat16)) != cudaSuccess) return PLC_E_CUDA;
+#undef PLC_ROWS
+    if (plan.way == kJoin && launch_kernel(logprob_join_kernel, (unsigned)rows, kRowThreads, 0, st, true, 1, a) != cudaSuccess) return PLC_E_CUDA;
+    count_launch(plan.way == kJoin ? 2 : 1);
     return PLC_OK;
 }
 
