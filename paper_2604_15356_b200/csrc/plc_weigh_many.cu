@@ -25,7 +25,7 @@ template <int D, bool DEEP> struct Many {
     static constexpr int groups = D == 256 ? 1 : 2, pos = 128 * groups;  // positions of a tile; four warps for each 128
     static constexpr int rows = D == 256 ? 64 : 128;                   // of a row tile
     static constexpr int k_bytes = blocks * pos * 128, q_bytes = blocks * rows * 128;
-    static constexpr int soft = 128 * groups, copy = 128, threads = soft + copy + 32;
+    static constexpr int soft = 128 * groups, copy = 128, threads = soft + copy + 64;           // exponentials; copies; boxes of keys, products
     static constexpr int tmem = 2 * groups * rows;                     // S twice
     static constexpr int words = pos / 32;
     static constexpr size_t used = k_slots * (size_t)k_bytes + q_slots * q_bytes + kRing * (rows + words + 4) * 4 + 256 + 1024;
@@ -122,7 +122,7 @@ template <class T, int D, bool DEEP>
 __global__ void __launch_bounds__(Many<D, DEEP>::threads, 1) weigh_many_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b, const __grid_constant__ WeighArgs a,
                                                                          const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap q_map, uint32_t* status) {
     using M = Many<D, DEEP>;
-    constexpr int QS = M::q_slots, KS = M::k_slots, pieces = D / 8, copy_warp = M::soft / 32, mma_warp = copy_warp + M::copy / 32;
+    constexpr int QS = M::q_slots, KS = M::k_slots, pieces = D / 8, copy_warp = M::soft / 32, box_warp = copy_warp + M::copy / 32, mma_warp = box_warp + 1;
     extern __shared__ uint8_t smem_raw[];
     __shared__ long long sums[M::threads / 32];
     __shared__ long long range_at[2];
@@ -273,14 +273,14 @@ __global__ void __launch_bounds__(Many<D, DEEP>::threads, 1) weigh_many_kernel(c
                 if (i + 1 < steps) enter();
             }
         }
-    } else if (wid < mma_warp) {
-        // ---- copies, four warps that do not wait for each other: keys at the start of an item, queries for every row tile.  Boxes are issued by the first
-        // warp; pieces of 16 bytes by all, a warp a quarter of the vectors.
+    } else if (wid < box_warp) {
+        // ---- copies, four warps that do not wait for each other: queries for every row tile (as a box: by the first warp), and where keys do not come in boxes those
+        // at the start of an item.  Pieces of 16 bytes are shared by all, a warp a quarter of the vectors.
         const int lt = tid - M::soft, cw = wid - copy_warp;
         const uint32_t k_s = smem_u32(ks), q_s = smem_u32(qs);
         bool fresh = true, ok = true;
-        int item = 0, k_last = -1;
-        long long q_last = -1;                    // the last item, and row tile, whose boxes have been issued
+        int item = 0;
+        long long q_last = -1;                    // the last row tile whose box has been issued
         // this thread's row of a row tile; its log-sum-exp is loaded a tile ahead
         int row = -1;
         const uint16_t* row_q = nullptr;
@@ -321,38 +321,7 @@ __global__ void __launch_bounds__(Many<D, DEEP>::threads, 1) weigh_many_kernel(c
             if (lt < M::rows) neg[ring * M::rows + lt] = row_at ? -row_lse * kLog2e : -INFINITY;
             const uint32_t odd = __ballot_sync(kFull, lt < M::rows && row_at == 0);
             if (lane == 0) none[ring * 4 + cw] = odd;
-            if (fresh && a.box_pos) {
-                if (cw == 0) {
-                    const int boxes = M::pos / a.box_pos, t = w.pt * M::pos + lane * a.box_pos, page = lane < boxes ? page_of(t) : -1;
-                    const uint32_t have = __ballot_sync(kFull, page >= 0);
-                    if (lane < M::words) {        // 32 positions' words
-                        uint32_t word = 0;
-                        if (a.box_pos >= 32) word = have >> (lane * 32 / a.box_pos) & 1u ? ~0u : 0u;
-                        else
-                            for (int e = 0; e < 32 / a.box_pos; ++e)
-                                if (have >> (lane * (32 / a.box_pos) + e) & 1u) word |= ((1u << a.box_pos) - 1u) << (e * a.box_pos);
-                        there[(item & (kRing - 1)) * M::words + lane] = word;
-                    }
-                    __syncwarp();
-                    ok = __all_sync(kFull, ok && mbar_wait(k_empty + 8 * kb, ((uint32_t)(item / KS) & 1u) ^ 1u, failed, status));
-                    if (!ok) break;
-                    if (lane == 0)
-                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(k_full + 8 * kb), "r"(__popc(have) * a.box_pos * M::blocks * 128) : "memory");
-                    __syncwarp();
-                    if (page >= 0) {
-                        int c[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) c[k] = a.box_dim[k] == 0 ? t % p.page_pos : a.box_dim[k] == 1 ? w.h : a.box_dim[k] == 2 ? page : 0;
-#pragma unroll
-                        for (int k = 0; k < M::blocks; ++k)
-                            asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(
-                                             k_s + kb * M::k_bytes + k * (M::pos * 128) + lane * a.box_pos * 128),
-                                         "l"(&k_map), "r"(k * 64), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]), "r"(k_full + 8 * kb)
-                                         : "memory");
-                    }
-                    k_last = item;
-                }
-            } else if (fresh) {
+            if (fresh && !a.box_pos) {
                 uint64_t at[M::pos / 128];
 #pragma unroll
                 for (int g = 0; g < M::pos / 128; ++g) {
@@ -395,10 +364,58 @@ __global__ void __launch_bounds__(Many<D, DEEP>::threads, 1) weigh_many_kernel(c
             if (lane == 0) mbar_arrive(q_full + 8 * qb);
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
-        if (!ok && cw == 0) {                     // boxes still in flight (none after a complete run) land before the CTA ends
-            for (int k = max(0, k_last - KS + 1); k <= k_last; ++k) land(k_full + 8 * (k & (KS - 1)), (uint32_t)(k / KS) & 1u);
+        if (!ok && cw == 0)                       // boxes still in flight (none after a complete run) land before the CTA ends
             for (long long k = max(0ll, q_last - QS + 1); k <= q_last; ++k) land(q_full + 8 * ((int)k & (QS - 1)), (uint32_t)(k / QS) & 1u);
+    } else if (wid == box_warp) {
+        // ---- boxes of keys: a lane looks a box's page up, an item ahead
+        const uint32_t k_s = smem_u32(ks);
+        const int boxes = a.box_pos ? M::pos / a.box_pos : 0;
+        int t = 0, page = -1, last = -1;
+        bool ok = true;
+        auto look_up = [&]() {                    // -1: behind the last position, -2: no page
+            t = w.pt * M::pos + lane * a.box_pos;
+            page = lane < boxes && t < w.x.len ? b.table[(int64_t)w.s * b.max_pages + t / p.page_pos] : -1;
+            if (page == -1 && lane < boxes && t < w.x.len) page = -2;
+        };
+        long long left = boxes ? steps : 0;
+        if (left > 0) look_up();
+        for (int item = 0; left > 0; ++item) {
+            const int kb = item & (KS - 1), at = t, h = w.h;
+            const bool there_is = page >= 0 && page < p.n_pages;
+            if (page < -1 || page >= p.n_pages) atomicOr(status, kStRange);
+            const int here = page;
+            const uint32_t have = __ballot_sync(kFull, there_is);
+            left -= w.row_tiles - w.rt;
+            w.rt = w.row_tiles - 1;
+            if (left > 0) { w.next(p, b, a); look_up(); }
+            ok = __all_sync(kFull, mbar_wait(k_empty + 8 * kb, ((uint32_t)(item / KS) & 1u) ^ 1u, failed, status));
+            if (!ok) break;
+            if (lane < M::words) {                // 32 positions' words
+                uint32_t word = 0;
+                if (a.box_pos >= 32) word = have >> (lane * 32 / a.box_pos) & 1u ? ~0u : 0u;
+                else
+                    for (int e = 0; e < 32 / a.box_pos; ++e)
+                        if (have >> (lane * (32 / a.box_pos) + e) & 1u) word |= ((1u << a.box_pos) - 1u) << (e * a.box_pos);
+                there[(item & (kRing - 1)) * M::words + lane] = word;
+            }
+            __syncwarp();                         // the words, which lane 0's arrival tells of
+            if (lane == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(k_full + 8 * kb), "r"(__popc(have) * a.box_pos * M::blocks * 128) : "memory");
+            __syncwarp();
+            if (there_is) {
+                int c[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) c[k] = a.box_dim[k] == 0 ? at % p.page_pos : a.box_dim[k] == 1 ? h : a.box_dim[k] == 2 ? here : 0;
+#pragma unroll
+                for (int k = 0; k < M::blocks; ++k)
+                    asm volatile("cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];" ::"r"(
+                                     k_s + kb * M::k_bytes + k * (M::pos * 128) + lane * a.box_pos * 128),
+                                 "l"(&k_map), "r"(k * 64), "r"(c[0]), "r"(c[1]), "r"(c[2]), "r"(c[3]), "r"(k_full + 8 * kb)
+                                 : "memory");
+            }
+            last = item;
         }
+        if (!ok)
+            for (int k = max(0, last - KS + 1); k <= last; ++k) land(k_full + 8 * (k & (KS - 1)), (uint32_t)(k / KS) & 1u);
     } else if (lane == 0) {
         // ---- products
         int item = 0;

@@ -432,7 +432,7 @@ class PagePool:
             if len(self._need_bytes) >= 4096:
                 self._need_bytes.clear()
             need = self._need_bytes[(book.rows, n_pos)] = b.value
-        new, _ = PageBook._new(book.rows, book.max_pages, self.n_pages, dev)
+        new, _ = PageBook._new(book.rows, book.max_pages, self.n_pages, dev)     # (the workspace is not the book's to hold: it goes by n_pos)
         ws = torch.empty(need, dtype=torch.uint8, device=dev)
         out = torch.empty(weight.shape, dtype=torch.float32, device=dev)
         _check(_run(dev, api.plc_pages_evict, self._by, a, C.byref(w), budgets, scalar, recent, new._by, out.data_ptr(), ws.data_ptr(), need, self._word), where)
@@ -536,27 +536,41 @@ class Rotary:
         """x [N][heads][d], or up to four of them (queries and keys, any strides with the components contiguous), turned at positions pos [N] (int32);
         back: by the opposite angles, the gradient.  out: where the results go, x itself is allowed."""
         import torch
-        where, dev, api = "plc_rotary_apply", self.device, _lib()
-        xs = (x,) if torch.is_tensor(x) else tuple(x)
-        outs = (None,) * len(xs) if out is None else (out,) if torch.is_tensor(out) else tuple(out)
-        _need(len(xs) >= 1, E_INVALID, where)
-        _need(len(xs) <= 4 and len(outs) == len(xs), E_SHAPE, where)
-        N, d, kind = _i32(pos, dev, where).numel(), xs[0].shape[-1] if xs[0].dim() == 3 else 0, _kind(xs[0].dtype, where)
-        _int32(E_SHAPE, where, N)
-        sets, got = (RotarySet * len(xs))(), []
-        for i, (t, o) in enumerate(zip(xs, outs)):
-            _need(t.dim() == 3 and t.shape[0] == N and t.shape[2] == d, E_SHAPE, where)
-            _need(t.device == dev and t.dtype == xs[0].dtype and t.stride(2) == 1, E_INVALID, where)
-            if o is None:
-                o = torch.empty(t.shape, dtype=t.dtype, device=dev)
+        where, dev = "plc_rotary_apply", self.device
+        single = isinstance(x, torch.Tensor)
+        xs = (x,) if single else tuple(x)
+        n_sets = len(xs)
+        _need(n_sets >= 1, E_INVALID, where)
+        outs = None if out is None else (out,) if isinstance(out, torch.Tensor) else tuple(out)
+        _need(n_sets <= 4 and (outs is None or len(outs) == n_sets), E_SHAPE, where)
+        N, dtype = _i32(pos, dev, where).numel(), xs[0].dtype
+        kind, sets, got, d = _kind(dtype, where), [], [], None
+        for i, t in enumerate(xs):
+            shape = t.shape
+            if len(shape) != 3 or shape[0] != N or (d is not None and shape[2] != d):
+                raise PlcError(E_SHAPE, where)
+            (_, heads, d), (row, head, one) = shape, t.stride()
+            if one != 1 or t.dtype != dtype or t.device != dev:
+                raise PlcError(E_INVALID, where)
+            if outs is None:
+                o = torch.empty(shape, dtype=dtype, device=dev)
+                out_row, out_head = heads * d, d
             else:
-                _need(o.shape == t.shape and o.dtype == t.dtype and o.device == dev and o.stride(2) == 1, E_INVALID, where)
+                o = outs[i]
+                _need(o.shape == shape and o.dtype == dtype and o.device == dev and o.stride(2) == 1, E_INVALID, where)
+                out_row, out_head, _ = o.stride()
             got.append(o)
-            _int32(E_SHAPE, where, t.shape[1])
-            sets[i] = RotarySet(t.data_ptr(), o.data_ptr(), t.stride(0), t.stride(1), o.stride(0), o.stride(1), t.shape[1])
+            if N > 0x7fffffff or heads > 0x7fffffff:
+                raise PlcError(E_SHAPE, where)
+            sets += (t.data_ptr(), o.data_ptr(), row, head, out_row, out_head, heads)     # a plc_rotary_set, seven 64-bit words
         if N:
-            _check(_run(dev, api.plc_rotary_apply, self._by, sets, len(xs), pos.data_ptr(), N, d, kind, int(back)), where)
-        return got[0] if torch.is_tensor(x) else tuple(got)
+            rc = _run(dev, _lib().plc_rotary_apply, self._by, _SETS[n_sets](*sets), n_sets, pos.data_ptr(), N, d, kind, 1 if back else 0)
+            if rc:
+                raise PlcError(rc, where)
+        return got[0] if single else tuple(got)
+
+
+_SETS = [C.c_int64 * (7 * n) for n in range(5)]
 
 
 def rotary_frequencies(dim, base=10000.0, ramp="none", factor=1.0, context=None, slow=1.0, fast=32.0):
@@ -586,7 +600,7 @@ def rotary_frequencies(dim, base=10000.0, ramp="none", factor=1.0, context=None,
 def token_logprobs(logits, tokens, n_top=0, status=None):
     """(logp, entropy, top_logp, top_token) of rows of logits [N][vocab]: the log probabilities [N][m] of tokens [N][m] (or [N]; int32, -1: none, 0),
     the rows' entropies [N] in nats, and the n_top likeliest tokens [N][n_top] with their log probabilities.  status: int32 word that receives 32 for a token
-    out of range."""
+    out of range.  The four are views of one allocation, with the call's workspace behind them for as long as one of them lives."""
     import torch
     where, dev, api = "plc_token_logprobs", logits.device, _lib()
     _need(logits.is_cuda and logits.dim() == 2, E_INVALID, where)
@@ -598,13 +612,17 @@ def token_logprobs(logits, tokens, n_top=0, status=None):
     _need(n_top >= 0, E_INVALID, where)
     word = None if status is None else _i32(status, dev, where).data_ptr()
     kind = _kind(logits.dtype, where)
-    logp = torch.empty(tokens.shape, dtype=torch.float32, device=dev)
-    entropy = torch.empty(N, dtype=torch.float32, device=dev)
-    top_logp = torch.empty((N, n_top), dtype=torch.float32, device=dev)
-    top_token = torch.empty((N, n_top), dtype=torch.int32, device=dev)
+    # one allocation: log probabilities, entropies, the alternatives' and their tokens, and the workspace behind them
+    need = _bytes(dev, api.plc_token_logprobs_workspace, N, V, n_top) if N else 0
+    tops = N * n_top
+    a, b, c = N * m, N * m + N, N * m + N + tops
+    d = c + tops + 3 & ~3
+    store = torch.empty(d + (need + 3) // 4, dtype=torch.float32, device=dev)
+    logp, entropy = store.as_strided(tokens.shape, tokens.stride(), 0), store.as_strided((N,), (1,), a)
+    top_logp = store.as_strided((N, n_top), (n_top, 1), b)
+    top_token = store.view(torch.int32).as_strided((N, n_top), (n_top, 1), c)
     if N:
-        need = _bytes(dev, api.plc_token_logprobs_workspace, N, V, n_top)
-        ws = torch.empty(need, dtype=torch.uint8, device=dev)
-        _check(_run(dev, api.plc_token_logprobs, logits.data_ptr(), kind, row, N, V, tokens.data_ptr(), m, n_top, logp.data_ptr(), entropy.data_ptr(), top_logp.data_ptr(),
-                    top_token.data_ptr(), ws.data_ptr(), need, word), where)
+        at = store.data_ptr()
+        _check(_run(dev, api.plc_token_logprobs, logits.data_ptr(), kind, row, N, V, tokens.data_ptr(), m, n_top, at, at + 4 * a, at + 4 * b, at + 4 * c,
+                    at + 4 * d, need, word), where)
     return logp, entropy, top_logp, top_token
