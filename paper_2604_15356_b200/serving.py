@@ -432,10 +432,12 @@ class PagePool:
             if len(self._need_bytes) >= 4096:
                 self._need_bytes.clear()
             need = self._need_bytes[(book.rows, n_pos)] = b.value
-        new, _ = PageBook._new(book.rows, book.max_pages, self.n_pages, dev)     # (the workspace is not the book's to hold: it goes by n_pos)
-        ws = torch.empty(need, dtype=torch.uint8, device=dev)
-        out = torch.empty(weight.shape, dtype=torch.float32, device=dev)
-        _check(_run(dev, api.plc_pages_evict, self._by, a, C.byref(w), budgets, scalar, recent, new._by, out.data_ptr(), ws.data_ptr(), need, self._word), where)
+        new, _ = PageBook._new(book.rows, book.max_pages, self.n_pages, dev)
+        (rows, layers, heads, _), n = weight.shape, weight.numel() + 3 & ~3
+        store = torch.empty(n + (need + 3) // 4, dtype=torch.float32, device=dev)     # the workspace, a seventeenth of the weights, behind them
+        out = store.as_strided((rows, layers, heads, n_pos), (layers * heads * n_pos, heads * n_pos, n_pos, 1), 0)
+        at = store.data_ptr()
+        _check(_run(dev, api.plc_pages_evict, self._by, a, C.byref(w), budgets, scalar, recent, new._by, at, at + 4 * n, need, self._word), where)
         return new, out
 
     def check(self):
