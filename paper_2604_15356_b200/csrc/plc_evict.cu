@@ -171,7 +171,7 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const __gr
     // the weights are on their way before the row's length is known
 #pragma unroll 4
     for (int t = tid; t < min(a.n_pos, kHeld); t += kSelectThreads) sh.key[t] = weight_order(w[t]);
-    for (int i = lane_at * kSelectThreads + tid; i < p.n_pages; i += (gridDim.x - 1) * kSelectThreads) out.ref[i] = in.ref[i];
+    for (long long i = (long long)lane_at * kSelectThreads + tid; i < p.n_pages; i += (long long)(gridDim.x - 1) * kSelectThreads) out.ref[i] = in.ref[i];
     const EvictRow r = evict_row(p, in, a, s);
     bool good = r.goes;
     if (good)
