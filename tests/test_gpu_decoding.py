@@ -389,6 +389,20 @@ def test_weights_of_an_attention_sum_to_one(dev):
             assert torch.equal(w, pool.attention_weights(0, after, q, lse, begin, pool.new_weights(2, 1200)))
 
 
+@pytest.mark.parametrize("G, n", [(2, [1]), (4, [0, 9, 3]), (1, [700])])
+def test_weights_of_many_sessions(dev, ora, G, n):
+    """More sessions than a block has threads, many of them without entries or positions, few and many columns on the average; one long one among them."""
+    S = 1100
+    lens = [(37 * i) % 45 if i % 3 else 0 for i in range(S)]
+    news = [min(lens[i], n[i % len(n)]) if i % 5 else 0 for i in range(S)]
+    if len(n) == 1 and n[0] > 100:
+        lens, news = [3] * S, [1 if i % 7 == 0 else 0 for i in range(S)]
+        lens[500], news[500] = 900, 700
+    weigh_case(dev, ora, S + G, "f16", 64, 1, G, 16, lens=lens, n=news).check()
+    if G == 4:
+        weigh_case(dev, ora, S + G, "bf16", 64, 1, 16, 16, lens=lens, n=news).check()
+
+
 def test_weights_offsets_pass_32_bits(dev):
     """Pages farther apart than 2^31 elements, weights' rows too."""
     far = (1 << 31) + 64
@@ -518,6 +532,21 @@ def test_eviction_of_a_long_row(dev, ora):
     """Many pieces of one row, which wait for nothing but what they write over; nearly all and nearly nothing kept."""
     for budget, d, dtype, page in ((5000, 32, "f16", 16), (9990, 64, "f32", 128), (3, 32, "bf16", 100), (9000, 256, "f32", 64)):
         evict_case(dev, ora, budget, dtype, d, 1, 1, page, lens=[10000], budget=[budget], recent=2)[0].check()
+
+
+@pytest.mark.parametrize("page", [1, 16, 256])
+def test_eviction_of_many_rows(dev, ora, page):
+    """More rows than a block has threads, with nothing to do for most; pages of one position and pages that are longer than the rows."""
+    S = 700
+    lens = [(91 * i) % 70 for i in range(S)]
+    budget = [(-1, 5, 40, 60, 0)[i % 5] for i in range(S)]
+    share = tuple((i + 1, i, max(1, lens[i + 1] // page)) for i in range(0, S - 1, 9) if lens[i] >= page and lens[i + 1] >= page)
+    pool, bits = evict_case(dev, ora, page, "f16", 32, 1, 1, page, lens=lens, budget=budget, recent=2, share=share if page < 256 else (), spare=S * 6 if page == 1 else S)
+    if bits == 0:
+        return pool.check()
+    with pytest.raises(plc.PlcError) as e:                                  # rows that share more pages than the other has are out of range, as the oracle says
+        pool.check()
+    assert bits == ora.RANGE and e.value.code == plc.E_INVALID
 
 
 def test_eviction_offsets_pass_32_bits(dev):
@@ -746,3 +775,41 @@ def test_two_calls_on_two_streams(dev):
         for pool, book, w, x, kv, keep in pools:
             kv.copy_(keep)
         torch.cuda.synchronize()
+
+
+def test_captured_graphs_share_nothing(dev):
+    """Two graphs with the same calls, replayed at the same time on two streams, each give what the calls give by themselves."""
+    rng = np.random.default_rng(13)
+    sides = []
+    for i in range(2):
+        kv, _, table, ref = pages_for(rng, 1, 2, 64, 16, [40, 30], 2, "f16", dev, False)
+        pool, book, after = plc.PagePool(kv), book_of(table, [600, 400], ref, dev), book_of(table, [620, 420], ref, dev)
+        q, begin, x = normal(rng, (40, 8, 64), "f16").to(dev), i32([0, 20, 40], dev), torch.randn(9, 40000, device=dev)
+        k, v, tokens = normal(rng, (40, 2, 64), "f16").to(dev), normal(rng, (40, 2, 64), "f16").to(dev), torch.zeros(9, 2, dtype=torch.int32, device=dev)
+        rot, keep = plc.Rotary(64), kv.clone()
+
+        def calls(pool=pool, book=book, after=after, q=q, begin=begin, x=x, k=k, v=v, tokens=tokens, rot=rot, keep=keep, kv=kv):
+            kv.copy_(keep)
+            turned = pool.append(0, book, q, k, v, begin, rotary=rot)
+            out, lse = pool.tree_attention(0, book, turned, begin)
+            w = pool.attention_weights(0, after, turned, lse, begin, pool.new_weights(2, 640))
+            new, nw = pool.evict(after, w, 300, recent=10)
+            return (turned, out, lse, w, new.table, new.len, new.ref, nw, kv) + plc.token_logprobs(x, tokens, 8)
+        alone = [t.clone() for t in calls()]
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            calls()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            got = calls()
+        sides.append((g, got, alone, s, pool, calls))                       # a replay reads the calls' inputs, which `calls` holds
+    for _ in range(5):
+        for g, _, _, s, _, _ in sides:
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    for _, got, alone, _, pool, _ in sides:
+        pool.check()
+        assert all(torch.equal(a, b) for a, b in zip(got, alone))
