@@ -174,19 +174,6 @@ __device__ __noinline__ uint32_t cut(unsigned long long* buf, int n, int k, int 
 template <class T> struct Step { static constexpr int groups = 4; };                  // 64 bytes a lane
 template <> struct Step<float> { static constexpr int groups = 2; };
 
-// What a lane adds to the spread in a step that holds a logit of -inf: that has the exponential 0 and adds nothing, not 0 times infinity.  `left`: logits from x on.
-template <class T>
-__device__ __noinline__ float careful_spread(const T* x, int left, float m) {
-    float sum = 0.f;
-    for (int g = 0; g < Step<T>::groups; ++g)
-        for (int k = 0; k < 8; ++k) {
-            if (g * 256 + k >= left) continue;
-            const float d = fmaxf((widen(x[g * 256 + k]) - m) * kLog2e, -1e4f);
-            sum = fmaf(exp2_approx(d), d, sum);
-        }
-    return sum;
-}
-
 // A block takes a part of a row in two passes.  The first streams: a warp takes 32 lanes times kGroups times eight logits a step, the next step's loads on
 // their way, forms the sum and keeps the maximum of each lane's chunks of steps.  The k-th largest of the lanes' maxima is a bound that k logits reach and
 // few others do, so the second pass looks at the chunks that reach it alone: about k of them, from L2.
@@ -200,6 +187,7 @@ __device__ __forceinline__ void row_part(const RowArgs& a, int row, int part) {
     __shared__ double wsum[kRowWarps], wspread[SPREAD ? kRowWarps : 1];
     __shared__ __align__(16) uint32_t order[kRowThreads];
     __shared__ float bound;
+    __shared__ int reach[2][kRowWarps];
     __shared__ int count;
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const T* x0 = static_cast<const T*>(a.logits) + (int64_t)row * a.row_stride;
@@ -249,10 +237,11 @@ __device__ __forceinline__ void row_part(const RowArgs& a, int row, int part) {
                 now[g].widen(x);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const unsigned long long d = fma2(add2(pack2(x[2 * k], x[2 * k + 1]), neg), scale, 0ull);
                     float lo, hi;
-                    unpack2(d, lo, hi);
+                    unpack2(fma2(add2(pack2(x[2 * k], x[2 * k + 1]), neg), scale, 0ull), lo, hi);
                     const unsigned long long e = pack2(exp2_approx(lo), exp2_approx(hi));
+                    // a logit of -inf has the exponential 0, and adds nothing, not 0 times infinity
+                    const unsigned long long d = pack2(fmaxf(lo, -1e4f), fmaxf(hi, -1e4f));
                     sums[k & 1] = add2(sums[k & 1], e);
                     far[k & 1] = fma2(e, d, far[k & 1]);
                 }
@@ -261,9 +250,7 @@ __device__ __forceinline__ void row_part(const RowArgs& a, int row, int part) {
             unpack2(add2(sums[0], sums[1]), lo, hi);
             part_sum = lo + hi;
             unpack2(add2(far[0], far[1]), lo, hi);
-            float part_spread = lo + hi;
-            if (part_spread != part_spread) part_spread = careful_spread(x0 + column(wid, i) + lane * 8, c1 - column(wid, i) - lane * 8, m);
-            spread -= (double)part_spread;
+            spread -= (double)(lo + hi);
         } else {
 #pragma unroll
             for (int g = 0; g < groups; ++g) {
@@ -341,23 +328,63 @@ __device__ __forceinline__ void row_part(const RowArgs& a, int row, int part) {
         const int at = column(w, i) + (lane >> 3) * 256 + l * 8 + (lane & 7);
         return lane < 8 * groups && at < c1 ? ((unsigned long long)order_bits(widen(x0[at])) << 32) | (uint32_t)~at : 0ull;
     };
+    if (a.k > kRowThreads / 2) {
+        // With as many places as lanes the least of the lanes' maxima is the bound, and five times as many logits reach it as are wanted, now and then more than there is room
+        // for (1024 rows of 128256, 128 of each: 555 us).  One that goes by the lanes' chunks is nearer to the k-th largest (122 us; for 64 of each it would be 100 instead of 89).
+        float* list = reinterpret_cast<float*>(found);
+        const float limit = bound;
+        for (int c = 0; c < chunk; ++c) {
+            const bool take = tops[c][tid] >= limit;
+            const uint32_t b = __ballot_sync(kFull, take);
+            int at = 0;
+            if (lane == 0 && b) at = atomicAdd(&count, __popc(b));
+            at = __shfl_sync(kFull, at, 0) + __popc(b & lt);
+            if (take && at < 2 * kRoom) list[at] = tops[c][tid];
+        }
+        __syncthreads();
+        const int listed = count;
+        if (listed <= 2 * kRoom) {
+            uint32_t least = 0;
+            for (int bit = 31; bit >= 0; --bit) {
+                const uint32_t t = least | (1u << bit);
+                int c = 0;
+                for (int i = tid; i < listed; i += kRowThreads) c += order_bits(list[i]) >= t;
+                c = __reduce_add_sync(kFull, c);
+                if (lane == 0) reach[bit & 1][wid] = c;
+                __syncthreads();
+                if (reach[bit & 1][0] + reach[bit & 1][1] + reach[bit & 1][2] + reach[bit & 1][3] >= a.k) least = t;
+            }
+            if (tid == 0) bound = value_of(least);
+        }
+        if (tid == 0) count = 0;
+        __syncthreads();
+    }
     {
         const float limit = bound;
         const uint32_t least = order_bits(limit);
         for (int c = 0; c < chunk; ++c) {
             uint32_t who = __ballot_sync(kFull, tops[c][tid] >= limit);
-            while (who) {
-                const int l = __ffs(who) - 1;
-                who &= who - 1;
+            while (who) {                         // four lanes' chunks at a time, so that their loads are on their way together
+                int l[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    l[k] = __ffs(who) - 1;
+                    who &= who - 1;
+                }
                 for (int i = c * per_chunk; i < min(steps, (c + 1) * per_chunk); ++i) {
-                    const unsigned long long key = look(wid, l, i);
-                    const bool take = (uint32_t)(key >> 32) >= least && key != 0;
-                    const uint32_t b = __ballot_sync(kFull, take);
-                    if (!b) continue;
-                    int at = 0;
-                    if (lane == 0) at = atomicAdd(&count, __popc(b));
-                    at = __shfl_sync(kFull, at, 0) + __popc(b & lt);
-                    if (take && at < kRoom) found[at] = key;
+                    unsigned long long key[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) key[k] = l[k] >= 0 ? look(wid, l[k], i) : 0ull;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const bool take = (uint32_t)(key[k] >> 32) >= least && key[k] != 0;
+                        const uint32_t b = __ballot_sync(kFull, take);
+                        if (!b) continue;
+                        int at = 0;
+                        if (lane == 0) at = atomicAdd(&count, __popc(b));
+                        at = __shfl_sync(kFull, at, 0) + __popc(b & lt);
+                        if (take && at < kRoom) found[at] = key[k];
+                    }
                 }
             }
         }

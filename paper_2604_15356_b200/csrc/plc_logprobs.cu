@@ -29,6 +29,16 @@ __device__ __forceinline__ void finish_row(const LogprobArgs& a, int row) {
     const int tid = threadIdx.x, lane = tid & 31;
     const long long slot = (long long)row * a.parts;
     const int entries = a.parts * a.k;
+    auto logit_of = [&](int i, int* v) -> float { // of the i-th given token, and which it is
+        *v = a.tokens[(long long)row * a.n_tokens + i];
+        if (*v < 0 || *v >= a.V) return 0.f;
+        const uint8_t* x = static_cast<const uint8_t*>(a.logits) + (((int64_t)row * a.row_stride + *v) << a.esz_log2);
+        return a.esz_log2 == 2 ? *reinterpret_cast<const float*>(x)
+               : a.bf16 ? widen(*reinterpret_cast<const __nv_bfloat16*>(x)) : widen(*reinterpret_cast<const __half*>(x));
+    };
+    int first_token = -1;
+    float first_logit = 0.f;
+    if (tid < a.n_tokens) first_logit = logit_of(tid, &first_token);           // on its way while the parts come together
     for (int i = tid; i < entries; i += kRowThreads) keys[i] = __ldcg(a.list + slot * a.k + i);
     if (tid < 32) {                               // at most 64 parts, two a lane
         float top = -FLT_MAX;
@@ -59,16 +69,11 @@ __device__ __forceinline__ void finish_row(const LogprobArgs& a, int row) {
     const double l = log_sum;
     const float top = row_top;
     for (int i = tid; i < a.n_tokens; i += kRowThreads) {
-        const long long at = (long long)row * a.n_tokens + i;
-        const int v = a.tokens[at];
-        float y = 0.f;
-        if (v >= 0 && v < a.V) {
-            const uint8_t* x = static_cast<const uint8_t*>(a.logits) + (((int64_t)row * a.row_stride + v) << a.esz_log2);
-            const float z = a.esz_log2 == 2 ? *reinterpret_cast<const float*>(x)
-                            : a.bf16 ? widen(*reinterpret_cast<const __nv_bfloat16*>(x)) : widen(*reinterpret_cast<const __half*>(x));
-            y = (float)(((double)z - (double)top) - l);
-        } else if (v != -1 && a.status) atomicOr(a.status, kStRange);
-        a.logp[at] = y;
+        int v = first_token;
+        const float z = i == tid ? first_logit : logit_of(i, &v);
+        const bool inside = v >= 0 && v < a.V;
+        if (!inside && v != -1 && a.status) atomicOr(a.status, kStRange);
+        a.logp[(long long)row * a.n_tokens + i] = inside ? (float)(((double)z - (double)top) - l) : 0.f;
     }
     // an entry's place is the number of better ones: those before it in its own list, and in each other list as many as a bisection finds
     for (int i = tid; i < entries; i += kRowThreads) {

@@ -47,12 +47,23 @@ template <> struct Wide<__nv_bfloat16> {
     static __device__ __forceinline__ __nv_bfloat16 put(float v) { return __float2bfloat16_rn(v); }
 };
 
-// A run of 16 bytes.
+// A run of W components: 16, 8 or 4 bytes.
 template <class T, int W> struct Run {
-    alignas(16) T v[W];
-    __device__ __forceinline__ void load(const uint8_t* p) { *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(p); }
-    __device__ __forceinline__ void store(uint8_t* p) const { *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(v); }
+    static constexpr int bytes = W * (int)sizeof(T);
+    alignas(bytes) T v[W];
+    __device__ __forceinline__ void load(const uint8_t* p) {
+        if constexpr (bytes == 16) *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(p);
+        else if constexpr (bytes == 8) *reinterpret_cast<uint2*>(v) = *reinterpret_cast<const uint2*>(p);
+        else *reinterpret_cast<uint32_t*>(v) = *reinterpret_cast<const uint32_t*>(p);
+    }
+    __device__ __forceinline__ void store(uint8_t* p) const {
+        if constexpr (bytes == 16) *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(v);
+        else if constexpr (bytes == 8) *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(v);
+        else *reinterpret_cast<uint32_t*>(p) = *reinterpret_cast<const uint32_t*>(v);
+    }
 };
+// Bytes of a run: 16 where strides, addresses, the turned part, its halves and the rest allow it, else 4 (two neighbours of binary32: 8).
+constexpr int run_bytes(bool wide, int esz, bool inter) { return wide ? 16 : esz == 4 && inter ? 8 : 4; }
 
 // The session of row i: the last one whose range begins at or before it; -1 where it is in none.  A warp calls it.
 __device__ __forceinline__ int session_of_row(const int32_t* begin, int sessions, int i) {
@@ -99,14 +110,14 @@ __device__ __forceinline__ void check_ranges(const TurnArgs& a, const BookDev& b
     if (bad) atomicOr(status, kStRange);
 }
 
-// Runs of 16 bytes.  A warp takes a row's heads, or a share of them: a lane has the same run of every head, whose cosines and sines it keeps in registers, and as
+// A warp takes a row's heads, or a share of them: a lane has the same run of every head, whose cosines and sines it keeps in registers, and as
 // many heads at a time as the runs of one leave lanes for.  64 bytes a lane on their way and eight blocks an SM: 16384 rows of 32 + 8 heads of 128 in bf16 63.7 us (5.3 TB/s),
 // with twice as many bytes a lane and four blocks 70; cosines and sines read again for each head 66 to 74.  INTER: pairs are neighbours, else half a turned part away.
 constexpr int kRowThreads = 128;
-template <class T, bool INTER, bool PAGES>
+template <class T, bool INTER, bool PAGES, bool WIDE>
 __global__ void __launch_bounds__(kRowThreads, 8) turn_rows_kernel(const __grid_constant__ TurnArgs a, const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
                                                                 uint32_t* status) {
-    constexpr int W = 16 / (int)sizeof(T), P = INTER ? W / 2 : W, U = INTER ? 4 : 2;        // components and pairs of a run; heads a lane has on their way
+    constexpr int bytes = run_bytes(WIDE, sizeof(T), INTER), W = bytes / (int)sizeof(T), P = INTER ? W / 2 : W, U = WIDE && !INTER ? 2 : 4;        // components and pairs of a run; heads a lane has on their way
     extern __shared__ float2 turn_s[];                                          // [warps][pairs]
     if (PAGES) check_ranges(a, b, status);
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
@@ -138,7 +149,7 @@ __global__ void __launch_bounds__(kRowThreads, 8) turn_rows_kernel(const __grid_
             const int e = e0 + lane % wide;
             if (lane >= abreast * wide || e >= s.per_head) continue;
             const bool turns = e < turned;
-            const int64_t off = turns ? (int64_t)e * 16 : (int64_t)s.dim * (int)sizeof(T) + (int64_t)(e - turned) * 16;
+            const int64_t off = turns ? (int64_t)e * bytes : (int64_t)s.dim * (int)sizeof(T) + (int64_t)(e - turned) * bytes;
             float2 cs[P];
             if (turns) {
 #pragma unroll
@@ -176,7 +187,7 @@ __global__ void __launch_bounds__(kRowThreads, 8) turn_rows_kernel(const __grid_
     }
 }
 
-// Component by component, where addresses, strides or parts of a head are not runs of 16 bytes.  A block takes a few rows with all their heads.
+// Component by component, where addresses, strides or parts of a head allow no runs.  A block takes a few rows with all their heads.
 template <class T, bool INTER, bool PAGES>
 __global__ void __launch_bounds__(kTurnThreads) turn_parts_kernel(const __grid_constant__ TurnArgs a, const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
                                                                   uint32_t* status) {
@@ -220,30 +231,44 @@ __global__ void __launch_bounds__(kTurnThreads) turn_parts_kernel(const __grid_c
     }
 }
 
+// Whether runs of so many bytes cover the turned part, its halves and the rest of every set, and start on their boundaries.
+bool in_runs(const TurnArgs& a, bool inter, int esz, int bytes) {
+    for (int i = 0; i < a.sets; ++i) {
+        const TurnSet& s = a.set[i];
+        if (s.heads == 0) continue;
+        const uintptr_t bits = reinterpret_cast<uintptr_t>(s.x) | reinterpret_cast<uintptr_t>(s.out) | (uintptr_t)s.xs_row | (uintptr_t)s.xs_head | (uintptr_t)s.os_row |
+                               (uintptr_t)s.os_head | (uintptr_t)((inter ? s.dim : s.dim / 2) * esz) | (uintptr_t)((a.d - s.dim) * esz);
+        if (bits & (bytes - 1)) return false;
+    }
+    return true;
+}
+
 // Units of the sets, and the launch.
 template <bool PAGES>
-plc_status launch_turn(TurnArgs& a, const PoolDev& p, const BookDev& b, int dtype, bool inter, bool vec, uint32_t* status, cudaStream_t st) {
-    const int esz = dtype == PLC_OUT_F32 ? 4 : 2, w = 16 / esz, sms = sm_count();
-    int units = 0, heads = 0;
+plc_status launch_turn(TurnArgs& a, const PoolDev& p, const BookDev& b, int dtype, bool inter, uint32_t* status, cudaStream_t st) {
+    const int esz = dtype == PLC_OUT_F32 ? 4 : 2, sms = sm_count();
+    const bool wide = in_runs(a, inter, esz, 16), runs = wide || in_runs(a, inter, esz, run_bytes(false, esz, inter));
+    const int w = run_bytes(wide, esz, inter) / esz;
+    int units = 0;
     for (int i = 0; i < a.sets; ++i) {
         TurnSet& s = a.set[i];
-        s.per_head = vec ? (inter ? s.dim / w : s.dim / 2 / w) + (a.d - s.dim) / w : s.dim / 2 + a.d - s.dim;
+        s.per_head = runs ? (inter ? s.dim / w : s.dim / 2 / w) + (a.d - s.dim) / w : s.dim / 2 + a.d - s.dim;
         s.first = units;
         units += s.heads * s.per_head;
-        heads = s.heads > heads ? s.heads : heads;
     }
     auto go = [&](auto* kern, unsigned grid, int threads, size_t smem) { return launch_kernel(kern, grid, threads, smem, st, false, 1, a, p, b, status); };
     cudaError_t e;
-    if (vec) {
+    if (runs) {
         // warps that share a row: so many that there are sixteen an SM, as long as each has the runs of a load for all of its lanes
         const long long want = (16ll * sms + a.rows - 1) / a.rows, most = (units + 127) / 128;
         a.shares = (int)(want < most ? want : most);
         constexpr int warps = kRowThreads / 32;
         const unsigned grid = (unsigned)(((long long)a.rows * a.shares + warps - 1) / warps);
         const size_t smem = (size_t)warps * a.pairs * sizeof(float2);
-        if (dtype == PLC_OUT_F32) e = inter ? go(turn_rows_kernel<float, true, PAGES>, grid, kRowThreads, smem) : go(turn_rows_kernel<float, false, PAGES>, grid, kRowThreads, smem);
-        else if (dtype == PLC_OUT_F16) e = inter ? go(turn_rows_kernel<__half, true, PAGES>, grid, kRowThreads, smem) : go(turn_rows_kernel<__half, false, PAGES>, grid, kRowThreads, smem);
-        else e = inter ? go(turn_rows_kernel<__nv_bfloat16, true, PAGES>, grid, kRowThreads, smem) : go(turn_rows_kernel<__nv_bfloat16, false, PAGES>, grid, kRowThreads, smem);
+        auto rows = [&](auto* wide_inter, auto* wide_half, auto* inter_kern, auto* half) { return go(wide ? (inter ? wide_inter : wide_half) : inter ? inter_kern : half, grid, kRowThreads, smem); };
+#define PLC_TURN(T) rows(turn_rows_kernel<T, true, PAGES, true>, turn_rows_kernel<T, false, PAGES, true>, turn_rows_kernel<T, true, PAGES, false>, turn_rows_kernel<T, false, PAGES, false>)
+        e = dtype == PLC_OUT_F32 ? PLC_TURN(float) : dtype == PLC_OUT_F16 ? PLC_TURN(__half) : PLC_TURN(__nv_bfloat16);
+#undef PLC_TURN
     } else {
         // rows of a block so that there are several blocks an SM
         const int per = a.rows / (4 * sms);
@@ -251,9 +276,10 @@ plc_status launch_turn(TurnArgs& a, const PoolDev& p, const BookDev& b, int dtyp
         a.rows_block = per < 1 ? 1 : per > kMostRows ? kMostRows : per;
         const unsigned grid = (unsigned)((a.rows + a.rows_block - 1) / a.rows_block);
         const size_t smem = (size_t)a.rows_block * a.pairs * sizeof(float2);
-        if (dtype == PLC_OUT_F32) e = inter ? go(turn_parts_kernel<float, true, PAGES>, grid, kTurnThreads, smem) : go(turn_parts_kernel<float, false, PAGES>, grid, kTurnThreads, smem);
-        else if (dtype == PLC_OUT_F16) e = inter ? go(turn_parts_kernel<__half, true, PAGES>, grid, kTurnThreads, smem) : go(turn_parts_kernel<__half, false, PAGES>, grid, kTurnThreads, smem);
-        else e = inter ? go(turn_parts_kernel<__nv_bfloat16, true, PAGES>, grid, kTurnThreads, smem) : go(turn_parts_kernel<__nv_bfloat16, false, PAGES>, grid, kTurnThreads, smem);
+        auto parts = [&](auto* inter_kern, auto* half) { return go(inter ? inter_kern : half, grid, kTurnThreads, smem); };
+#define PLC_TURN(T) parts(turn_parts_kernel<T, true, PAGES>, turn_parts_kernel<T, false, PAGES>)
+        e = dtype == PLC_OUT_F32 ? PLC_TURN(float) : dtype == PLC_OUT_F16 ? PLC_TURN(__half) : PLC_TURN(__nv_bfloat16);
+#undef PLC_TURN
     }
     if (e != cudaSuccess) return PLC_E_CUDA;
     count_launch(1);
@@ -270,13 +296,6 @@ plc_status check_rotary(const plc_rotary* r, int head_dim, TurnArgs* a) {
     a->scale = r->scale;
     return PLC_OK;
 }
-// Whether runs of 16 bytes cover the turned part, its halves and the rest.
-bool wide_runs(int dim, int d, bool inter, int esz) { return (inter ? dim : dim / 2) * esz % 16 == 0 && (d - dim) * esz % 16 == 0; }
-bool wide_set(const TurnSet& s) {
-    return ((reinterpret_cast<uintptr_t>(s.x) | reinterpret_cast<uintptr_t>(s.out) | (uintptr_t)s.xs_row | (uintptr_t)s.xs_head | (uintptr_t)s.os_row |
-             (uintptr_t)s.os_head) & 15) == 0;
-}
-
 }  // namespace
 }  // namespace plc
 
@@ -310,7 +329,6 @@ plc_status plc_rotary_apply(const plc_rotary* rotary, const plc_rotary_set* sets
     const plc_status rc = check_rotary(rotary, head_dim, &a);
     if (rc) return rc;
     const int esz = dtype == PLC_OUT_F32 ? 4 : 2;
-    bool vec = wide_runs(rotary->dim, head_dim, rotary->interleaved != 0, esz);
     long long heads = 0;
     for (int i = 0; i < n_sets; ++i) {
         const plc_rotary_set& s = sets[i];
@@ -321,11 +339,10 @@ plc_status plc_rotary_apply(const plc_rotary* rotary, const plc_rotary_set* sets
         if (heads > (1 << 12)) return PLC_E_SHAPE;
         a.set[i] = TurnSet{static_cast<const uint8_t*>(s.x_dev), static_cast<uint8_t*>(s.out_dev), s.x_stride_row * esz, s.x_stride_head * esz, s.out_stride_row * esz,
                            s.out_stride_head * esz, s.heads, rotary->dim, 0, 0};
-        vec = vec && wide_set(a.set[i]);
     }
     if (n_rows == 0) return PLC_OK;
     a.sets = n_sets; a.back = back != 0; a.pos = pos_dev; a.rows = n_rows; a.d = head_dim;
-    return launch_turn<false>(a, PoolDev{}, BookDev{}, dtype, rotary->interleaved != 0, vec, nullptr, static_cast<cudaStream_t>(stream));
+    return launch_turn<false>(a, PoolDev{}, BookDev{}, dtype, rotary->interleaved != 0, nullptr, static_cast<cudaStream_t>(stream));
 }
 
 plc_status plc_pages_append(const plc_page_pool* pool, int32_t layer, const plc_page_book* book, const plc_rotary* rotary, const plc_new_tokens* t,
@@ -352,9 +369,8 @@ plc_status plc_pages_append(const plc_page_pool* pool, int32_t layer, const plc_
                        t->out_stride_head * esz, t->n_heads, dim, 0, 0};
     a.set[1] = TurnSet{static_cast<const uint8_t*>(t->k_dev), nullptr, t->k_stride_row * esz, t->k_stride_head * esz, 0, 0, p.H, dim, 0, 0};
     a.set[2] = TurnSet{static_cast<const uint8_t*>(t->v_dev), nullptr, t->v_stride_row * esz, t->v_stride_head * esz, 0, 0, p.H, 0, 0, 0};
-    const bool vec = wide_runs(dim, p.d, inter, esz) && (t->n_heads == 0 || wide_set(a.set[0])) && wide_set(a.set[1]) && wide_set(a.set[2]);
     a.sets = 3; a.pos = t->pos_dev; a.rows = t->n_rows; a.d = p.d; a.begin = t->begin_dev; a.layer = layer;
-    return launch_turn<true>(a, p, b, pool->dtype, inter, vec, status_dev, static_cast<cudaStream_t>(stream));
+    return launch_turn<true>(a, p, b, pool->dtype, inter, status_dev, static_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"
