@@ -326,7 +326,6 @@ __global__ void __launch_bounds__(kMoveThreads, 6) evict_move_kernel(const __gri
     __shared__ Taken taken_s[2];
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     chain_wait();
-    for (int s = blockIdx.x * (kMoveThreads / 32) + wid; s < in.rows; s += gridDim.x * (kMoveThreads / 32)) evict_book(p, in, out, a, s, status);
     const long long total = a.first[in.rows], lanes = (long long)p.L * p.H;
     if (a.head->short_of)                                                // the weights stay as they are, too
         for (long long at = blockIdx.x; at < lanes * in.rows; at += gridDim.x) {
@@ -337,8 +336,8 @@ __global__ void __launch_bounds__(kMoveThreads, 6) evict_move_kernel(const __gri
     const uint32_t held_at = (uint32_t)__cvta_generic_to_shared(held);
     const int mask = (1 << lanes_log2) - 1, words = 1 << (a.piece_log2 - 5);
     // What comes next is found in two steps, each by a warp of its own and a piece ahead of the other: its number and row, then what is kept of it.
-    auto take = [&](Taken& x) {
-        const long long item = (long long)__shfl_sync(kFull, lane == 0 ? atomicAdd(&a.head->ticket, 1ull) : 0ull, 0);
+    auto tickets = [&](int n) { return (long long)__shfl_sync(kFull, lane == 0 ? atomicAdd(&a.head->ticket, (unsigned long long)n) : 0ull, 0); };
+    auto take = [&](Taken& x, long long item) {
         const int s = item < total ? row_of(a.first, in.rows, item) : -1;
         if (lane == 0) { x.s = s; x.rest = s < 0 ? 0 : item - a.first[s]; }
     };
@@ -377,7 +376,12 @@ __global__ void __launch_bounds__(kMoveThreads, 6) evict_move_kernel(const __gri
         }
     };
     constexpr int taker = kCopyThreads / 32, enterer = taker + 1;
-    if (wid == taker) { take(taken_s[0]); take(taken_s[1]); }
+    if (wid == taker) {
+        const long long item = tickets(2);
+        take(taken_s[0], item);
+        take(taken_s[1], item + 1);
+    } else                                        // the others write the book meanwhile
+        for (int s = blockIdx.x * (kCopyThreads / 32) + wid; s < in.rows && wid < taker; s += gridDim.x * (kCopyThreads / 32)) evict_book(p, in, out, a, s, status);
     __syncthreads();
     if (wid == enterer) enter(taken_s[0], piece_s[0]);
     __syncthreads();
@@ -404,7 +408,7 @@ __global__ void __launch_bounds__(kMoveThreads, 6) evict_move_kernel(const __gri
             if (from != dst[u >> lanes_log2])
                 asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(held_at + u * 16), "l"(plane + from + (u & mask) * 16) : "memory");
         }
-        if (wid == taker) take(taken_s[turn]);
+        if (wid == taker) take(taken_s[turn], tickets(1));
         if (wid == enterer) enter(taken_s[turn ^ 1], piece_s[turn ^ 1]);
         asm volatile("cp.async.wait_all;" ::: "memory");
         __syncthreads();
