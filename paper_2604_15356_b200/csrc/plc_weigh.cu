@@ -7,7 +7,10 @@
 // one, so a lane's 16 bytes of a key, as they come from the page, are its operands of two products: keys go from HBM to registers
 // and never through shared memory, while the queries of a (session, head) stay in registers.  The exponentials of a tile's columns are summed in a fixed
 // order by the lanes that share a position, and one lane adds the sum to the weight: the same call gives the same bits.
-// All (session, head, tile) form one sequence, cut into equal ranges, one a warp.
+// All (session, head, tile) form one sequence, cut into equal ranges, one a warp.  A tile's keys are loaded while the one before is multiplied, its page is
+// looked up a tile earlier still.  HBM bound: 64 sessions of up to 4096 positions, 8 x 4 heads of 128, one token each: 61 us on the device (355 MB, 5.8 TB/s); without the
+// loads ahead 80 us.
+// Products of this size are on the tensor cores' warp instructions, since nothing is to be gained by more: the tensor pipe is busy 8 % of the time.
 #include <cuda_bf16.h>
 #include <math.h>
 
@@ -204,7 +207,9 @@ cudaError_t launch_weigh(const PoolDev& p, const BookDev& b, const WeighArgs& a,
     }
 }
 
-// Columns (entries times the query heads of a group) a session from which the tensor cores' kernel takes the call.  By the mean, which is what the host knows.
+// Columns (entries times the query heads of a group) a session beyond which the other kernel takes the call, by the mean, which is what the host knows.  Half as many sessions as
+// above, us a call, here and there: 16 columns 37 and 54 (before its boxes had a warp of their own; now 44), 32 columns 65 and 44; with queries in shared memory 32 columns took 64 here, 64
+// columns 137.
 constexpr int kFewColumns = 16;
 bool many_columns(const PoolDev& p, int sessions, int heads, int n_list) { return (long long)n_list * (heads / p.H) > (long long)kFewColumns * sessions; }
 

@@ -2,8 +2,15 @@
 //
 // As in the other kernel positions are the rows of S = K Q^T, here the 128 lanes of tensor memory: a thread has a position, and the exponentials of the
 // tile's columns are summed in its register, from row tile to row tile.  A CTA holds a tile of positions in shared memory (two of them, so that the next one arrives meanwhile)
-// and goes through the row tiles that see any of it; Q and S have two buffers each.  Bound by the exponentials (16 a clock and SM; the products need half as long)
-// or, where there is one row tile, by HBM.
+// and goes through the row tiles that see any of it; Q and S have two buffers each, Q four where there are many row tiles.  Boxes of pages and of queries where their layouts allow it,
+// else pieces of 16 bytes.
+//
+// Bound by the exponentials (16 a clock and SM; the products need half as long): 2048 tokens of 8 x 4 heads of 128 behind 8192 positions 243 us on the device (156 GFLOP, 640 TFLOP/s;
+// the exponentials' unit is busy 0.67 of the time, the tensor pipe 0.33, at the clock that the power leaves: 950 W).  A step, 128 rows by 256 positions, takes 2950 clocks: 2050 of the
+// unit, 250 around them in the sums, 300 waiting, 230 between steps.  Two threads a position were slower (297 us against 263 then), a quarter of the exponentials by a
+// polynomial hardly faster (241 against 249).
+// Or, where there is one row tile, by HBM: 32 sessions of up to 4096 positions, 5 tokens of 8 x 4 heads of 128: 44 us (177 MB, 4.1 TB/s).  Tiles of 128 positions with four
+// buffers of keys took 76 with one warp for all copies against 54.
 //
 // Work: all (session, head, position tile, row tile) form one sequence, cut into equal ranges, one a CTA.  The first and the last piece of a range may be parts of an
 // item (session, head, position tile); those leave their sums in the workspace, and a second launch adds them in a fixed order.
@@ -15,7 +22,7 @@ namespace plc {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896f;
-// Row tiles whose normalisers, and items whose positions, are kept: the copies run up to four of them ahead of the exponentials.
+// Row tiles whose normalisers, and items whose positions, are kept: the copies run up to six of them ahead of the exponentials.
 constexpr int kRing = 8;
 
 // DEEP: many row tiles an item, so that the queries' ring is what counts; else keys of the next item arrive while this one's are used.
