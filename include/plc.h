@@ -483,7 +483,8 @@ typedef struct {
 /* turns[i] = radians[i] / (2 pi) 2^64 modulo 2^64, rounded to nearest (exact arithmetic; host side, no GPU work); 0 <= radians <= 65536. */
 plc_status plc_rotary_turns(const double* radians, int32_t n, uint64_t* turns);
 
-/* x, out [n_rows][heads][head_dim], strides in elements; out is x itself with x's strides, or does not overlap it. */
+/* x, out [n_rows][heads][head_dim], strides in elements; out is x itself with x's strides, or does not
+ * overlap it, nor itself. */
 typedef struct {
     const void* x_dev;
     void* out_dev;
@@ -548,6 +549,7 @@ typedef struct {
  * scale: positive and finite, as for the attention; decay: finite, not negative.  Scores and sums are binary32, sums in an order
  * that does not change from call to call.  Positions from n_pos on are left out (bit 1).  Ranges, lengths, rows and page numbers out of range, and more entries
  * than positions (bit 32): ranges and lengths are cut to what there is, a row counts for nothing, positions without a page receive nothing.
+ * What a call does goes by the mean number of entries: sessions of very different numbers belong in calls of their own.
  * workspace: plc_pages_weigh_workspace bytes (0 where the sessions have few entries: NULL then). */
 plc_status plc_pages_weigh(const plc_page_pool* pool, int32_t layer, const plc_page_book* book, const plc_weigh_queries* queries, float scale,
                            float decay, const plc_weights* weights, void* workspace_dev, uint64_t workspace_bytes, uint32_t* status_dev,

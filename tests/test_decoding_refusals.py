@@ -94,7 +94,8 @@ def apply(lib, r=None, sets=None, n_sets=1, pos=A, rows=3, d=64, dtype=plc.OUT_F
 
 def test_turns_that_are_refused(lib):
     for kw in (dict(x_dev=None), dict(out_dev=None), dict(heads=0), dict(n_sets=0), dict(pos=0), dict(rows=-1), dict(d=1), dict(dtype=3), dict(r=rotary(turns=0)),
-               dict(r=rotary(scale=float("inf"))), dict(out_dev=A, out_stride_row=512), dict(out_dev=A, out_stride_head=128)):
+               dict(r=rotary(scale=float("inf"))), dict(out_dev=A, out_stride_row=512), dict(out_dev=A, out_stride_head=128),
+               dict(out_stride_row=0), dict(out_stride_head=0)):
         assert apply(lib, **kw) == plc.E_INVALID, kw
     for kw in (dict(n_sets=5), dict(d=2048), dict(r=rotary(dim=66)), dict(r=rotary(dim=7)), dict(r=rotary(dim=0)), dict(heads=4097), dict(heads=2049, n_sets=2)):
         assert apply(lib, **kw) == plc.E_SHAPE, kw
@@ -114,7 +115,7 @@ def test_appends_that_are_refused(lib):
     def call(layer=0, p=None, b=None, r=rotary(), status=A, **change):
         return lib.plc_pages_append(C.byref(p or pool()), layer, C.byref(b or book()), C.byref(r) if r else None, C.byref(tokens(**change)), C.c_void_p(status), None)
     for kw in (dict(layer=-1), dict(layer=2), dict(status=0), dict(q_dev=None), dict(out_dev=None), dict(k_dev=None), dict(v_dev=None), dict(begin_dev=None), dict(n_rows=-1),
-               dict(n_heads=-1), dict(r=rotary(turns=0)), dict(b=book(rows=0)), dict(p=pool(base=0)), dict(out_dev=A, out_stride_row=1024)):
+               dict(n_heads=-1), dict(r=rotary(turns=0)), dict(b=book(rows=0)), dict(p=pool(base=0)), dict(out_dev=A, out_stride_row=1024), dict(out_stride_row=0), dict(out_stride_head=0)):
         assert call(**kw) == plc.E_INVALID, kw
     for kw in (dict(r=rotary(dim=128)), dict(r=rotary(dim=5)), dict(p=pool(d=48)), dict(n_heads=1 << 14), dict(b=book(rows=1 << 21))):
         assert call(**kw) == plc.E_SHAPE, kw
@@ -124,15 +125,15 @@ def test_appends_that_are_refused(lib):
 
 
 def test_weights_that_are_refused(lib):
-    def call(layer=0, p=None, b=None, scale=0.125, decay=1.0, base=B, n_pos=100, status=A, ws=WS, ws_bytes=1 << 20, **change):
+    def call(layer=0, p=None, b=None, scale=0.125, decay=1.0, base=B, n_pos=100, status=A, ws=WS, ws_bytes=1 << 20, strides=(800, 400, 100), **change):
         t = dict(q_dev=A, q_stride_row=512, q_stride_head=64, lse_dev=A, rows_dev=None, begin_dev=A, n_rows=7, n_list=7, n_heads=8)
         t.update(change)
-        q, w = serving.WeighQueries(**t), serving.Weights(base, 800, 400, 100, n_pos)
+        q, w = serving.WeighQueries(**t), serving.Weights(base, *strides, n_pos)
         return lib.plc_pages_weigh(C.byref(p or pool()), layer, C.byref(b or book()), C.byref(q), C.c_float(scale), C.c_float(decay), C.byref(w), C.c_void_p(ws),
                                    C.c_uint64(ws_bytes), C.c_void_p(status), None)
     for kw in (dict(layer=2), dict(layer=-1), dict(ws=0, n_rows=700, n_list=700), dict(scale=0.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(decay=-1.0), dict(decay=float("inf")), dict(base=0),
                dict(n_pos=0), dict(status=0), dict(q_dev=None), dict(lse_dev=None), dict(begin_dev=None), dict(n_rows=-1), dict(n_list=-1), dict(n_heads=0),
-               dict(p=pool(dtype=plc.OUT_F32)), dict(b=book(rows=0))):
+               dict(p=pool(dtype=plc.OUT_F32)), dict(b=book(rows=0)), dict(strides=(0, 400, 100)), dict(strides=(800, 0, 100)), dict(strides=(800, 400, 0))):
         assert call(**kw) == plc.E_INVALID, kw
     for kw in (dict(n_heads=6), dict(n_list=8), dict(n_rows=1 << 29, n_list=1 << 29, n_heads=16), dict(p=pool(d=48))):
         assert call(**kw) == plc.E_SHAPE, kw

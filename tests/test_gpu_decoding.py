@@ -221,6 +221,7 @@ def test_append(dev, ora, dtype, d, dim, H, G, page, inter, slots_first, given):
     for i in range(N):
         if places[i]:
             assert torch.equal(kv[1, 0, places[i][0], :, places[i][1]], k[i])
+    assert torch.equal(pool.append(0, book, q, k, v, i32(begin, dev))[2:-3], q[2:-3])      # queries as they are
     mine = q.contiguous()
     assert torch.equal(pool.append(0, book, mine, k, v, i32(begin, dev), rotary=rot, pos=i32(at, dev), out=mine)[2:-3], out[2:-3])
 
