@@ -296,29 +296,32 @@ __device__ __forceinline__ void row_part(const RowArgs& a, int row, int part) {
     }
     __syncthreads();
     const long long slot = (long long)row * a.parts + part;
-    {
-        int rank = 0;                             // of the lane's maximum among all
-        const uint32_t mine = order[tid];
-#pragma unroll 4
-        for (int i = 0; i < kRowThreads; i += 4) {
-            const uint4 v = *reinterpret_cast<const uint4*>(order + i);
-            rank += (v.x > mine || (v.x == mine && i < tid)) + (v.y > mine || (v.y == mine && i + 1 < tid)) + (v.z > mine || (v.z == mine && i + 2 < tid)) +
-                    (v.w > mine || (v.w == mine && i + 3 < tid));
+    if (wid == 0 && a.k > 0) {
+        // the k-th largest of the lanes' maxima, by the upper half of their bits: what is just below it will do as a bound
+        uint32_t v[kRowWarps], least = 0;
+#pragma unroll
+        for (int i = 0; i < kRowWarps; ++i) v[i] = order[i * 32 + lane];
+#pragma unroll 1
+        for (int bit = 31; bit >= 16; --bit) {
+            const uint32_t t = least | (1u << bit);
+            int c = 0;
+#pragma unroll
+            for (int i = 0; i < kRowWarps; ++i) c += v[i] >= t;
+            if (__reduce_add_sync(kFull, c) >= a.k) least = t;
         }
-        if (rank == a.k - 1) bound = top;
-        if (tid == 0) {
-            float all = wtop[0];
-            for (int w = 1; w < kRowWarps; ++w) all = fmaxf(all, wtop[w]);
-            double sum = 0.0, far = 0.0;
-            for (int w = 0; w < kRowWarps; ++w) {
-                const double f = (double)exp2_approx((wtop[w] - all) * kLog2e);
-                sum += wsum[w] * f;
-                if (SPREAD && wsum[w] != 0.0) far += f * (wspread[w] + wsum[w] * ((double)all - (double)wtop[w]) * (double)kLog2e);
-            }
-            a.sum[slot] = sum;
-            if (SPREAD) a.spread[slot] = far * 0.693147180559945309;
-            a.top[slot] = all;
+        if (lane == 0) bound = value_of(max(least, order_bits(-INFINITY)));
+    } else if (tid == 32) {
+        float all = wtop[0];
+        for (int w = 1; w < kRowWarps; ++w) all = fmaxf(all, wtop[w]);
+        double sum = 0.0, far = 0.0;
+        for (int w = 0; w < kRowWarps; ++w) {
+            const double f = (double)exp2_approx((wtop[w] - all) * kLog2e);
+            sum += wsum[w] * f;
+            if (SPREAD && wsum[w] != 0.0) far += f * (wspread[w] + wsum[w] * ((double)all - (double)wtop[w]) * (double)kLog2e);
         }
+        a.sum[slot] = sum;
+        if (SPREAD) a.spread[slot] = far * 0.693147180559945309;
+        a.top[slot] = all;
     }
     if (a.k == 0) return;
     __syncthreads();
