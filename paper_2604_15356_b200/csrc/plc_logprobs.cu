@@ -22,6 +22,16 @@ struct LogprobArgs : RowArgs {
     uint32_t* status;
 };
 
+// ln of a row's sum of exponentials, not less than 1: e ln 2 in binary64 and, of what is left between 3/4 and 3/2, log1p in binary32, which is off by 2^-24 of at most 0.41 (and
+// of the whole where the sum is near 1).  The sum of a row that is no distribution (NaN, or nothing but -inf) has none.
+__device__ __forceinline__ double log_of(double sum) {
+    if (!(sum > 0.0) || isinf(sum)) return (double)NAN;
+    const long long bits = __double_as_longlong(sum);
+    const int e = (int)((bits + (1ll << 51)) >> 52) - 1023;
+    const double m = __longlong_as_double(bits - ((long long)e << 52));
+    return (double)e * 0.693147180559945309 + (double)log1pf((float)(m - 1.0));
+}
+
 // A row's results from its parts: a block, of the same threads as a part.  LISTED: entries of its lists at most.
 template <int LISTED>
 __device__ __forceinline__ void finish_row(const LogprobArgs& a, int row) {
@@ -38,41 +48,51 @@ __device__ __forceinline__ void finish_row(const LogprobArgs& a, int row) {
         return a.esz_log2 == 2 ? *reinterpret_cast<const float*>(x)
                : a.bf16 ? widen(*reinterpret_cast<const __nv_bfloat16*>(x)) : widen(*reinterpret_cast<const __half*>(x));
     };
+    // The first warp joins the sums; meanwhile the others have the lists and the first tokens' logits come.
+    const int seat = (tid + kRowThreads - 32) % kRowThreads;
     int first_token = -1;
     float first_logit = 0.f;
-    if (tid < a.n_tokens) first_logit = logit_of(tid, &first_token);           // on its way while the parts come together
-    for (int i = tid; i < entries; i += kRowThreads) keys[i] = __ldcg(a.list + slot * a.k + i);
-    if (tid < 32) {                               // at most 64 parts, two a lane
-        float top = -FLT_MAX;
-        for (int q = lane; q < a.parts; q += 32) top = fmaxf(top, __ldcg(a.top + slot + q));
+    double spread = 0.0, sum = 0.0;
+    if (tid < 32) {
+        const int upto = min(a.parts, 32);        // at most 64 parts, two a lane
+        float t[2];
+        double s[2], w[2];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
-        double sum = 0.0, spread = 0.0;
-        for (int q = lane; q < a.parts; q += 32) {
-            const float t = __ldcg(a.top + slot + q);
-            const double f = (double)exp2_approx((t - top) * kLog2e), s = __ldcg(a.sum + slot + q);
-            sum += f * s;
-            if (s != 0.0) spread += f * (__ldcg(a.spread + slot + q) + s * ((double)top - (double)t));
+        for (int e = 0; e < 2; ++e) {
+            const int q = lane + 32 * e;
+            const bool some = q < a.parts;
+            t[e] = some ? __ldcg(a.top + slot + q) : -FLT_MAX;
+            s[e] = some ? __ldcg(a.sum + slot + q) : 0.0;
+            w[e] = some ? __ldcg(a.spread + slot + q) : 0.0;
         }
+        float top = fmaxf(t[0], t[1]);
+        for (int o = 1; o < upto; o <<= 1) top = fmaxf(top, __shfl_xor_sync(kFull, top, o));
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
+        for (int e = 0; e < 2; ++e) {
+            if (s[e] == 0.0) continue;
+            const double f = (double)exp2_approx((t[e] - top) * kLog2e);
+            sum += f * s[e];
+            spread += f * (w[e] + s[e] * ((double)top - (double)t[e]));
+        }
+        for (int o = 1; o < upto; o <<= 1) {
             sum += __shfl_xor_sync(kFull, sum, o);
             spread += __shfl_xor_sync(kFull, spread, o);
         }
         if (lane == 0) {
-            const bool some = sum > 0.0;          // NaN, and nothing but -inf: not a distribution
-            const double l = some ? log(sum) : (double)NAN;
-            log_sum = l;
+            log_sum = log_of(sum);
             row_top = top;
-            if (a.entropy) a.entropy[row] = (float)(l + spread / sum);
         }
+    } else {
+        for (int i = tid - 32; i < entries; i += kRowThreads - 32) keys[i] = __ldcg(a.list + slot * a.k + i);
+        if (seat < a.n_tokens) first_logit = logit_of(seat, &first_token);
     }
     __syncthreads();
     const double l = log_sum;
     const float top = row_top;
-    for (int i = tid; i < a.n_tokens; i += kRowThreads) {
+    if (tid == 0 && a.entropy) a.entropy[row] = (float)(l + spread / sum);
+    for (int i = seat; i < a.n_tokens; i += kRowThreads) {
         int v = first_token;
-        const float z = i == tid ? first_logit : logit_of(i, &v);
+        const float z = i == seat && tid >= 32 ? first_logit : logit_of(i, &v);
         const bool inside = v >= 0 && v < a.V;
         if (!inside && v != -1 && a.status) atomicOr(a.status, kStRange);
         a.logp[(long long)row * a.n_tokens + i] = inside ? (float)(((double)z - (double)top) - l) : 0.f;
