@@ -310,18 +310,24 @@ __device__ __forceinline__ void row_part(const RowArgs& a, int row, int part) {
             if (__reduce_add_sync(kFull, c) >= a.k) least = t;
         }
         if (lane == 0) bound = value_of(max(least, order_bits(-INFINITY)));
-    } else if (tid == 32) {
-        float all = wtop[0];
-        for (int w = 1; w < kRowWarps; ++w) all = fmaxf(all, wtop[w]);
-        double sum = 0.0, far = 0.0;
-        for (int w = 0; w < kRowWarps; ++w) {
-            const double f = (double)exp2_approx((wtop[w] - all) * kLog2e);
-            sum += wsum[w] * f;
-            if (SPREAD && wsum[w] != 0.0) far += f * (wspread[w] + wsum[w] * ((double)all - (double)wtop[w]) * (double)kLog2e);
+    } else if (wid == 1) {                        // a lane a warp's sums, added in the warps' order
+        const int w = min(lane, kRowWarps - 1);
+        float all = wtop[w];
+#pragma unroll
+        for (int o = kRowWarps / 2; o > 0; o >>= 1) all = fmaxf(all, __shfl_xor_sync(kFull, all, o));
+        const double f = (double)exp2_approx((wtop[w] - all) * kLog2e), s_here = wsum[w] * f;
+        double far_here = 0.0, sum = 0.0, far = 0.0;
+        if (SPREAD && wsum[w] != 0.0) far_here = f * (wspread[w] + wsum[w] * ((double)all - (double)wtop[w]) * (double)kLog2e);
+#pragma unroll
+        for (int v = 0; v < kRowWarps; ++v) {
+            sum += __shfl_sync(kFull, s_here, v);
+            if (SPREAD) far += __shfl_sync(kFull, far_here, v);
         }
-        a.sum[slot] = sum;
-        if (SPREAD) a.spread[slot] = far * 0.693147180559945309;
-        a.top[slot] = all;
+        if (lane == 0) {
+            a.sum[slot] = sum;
+            if (SPREAD) a.spread[slot] = far * 0.693147180559945309;
+            a.top[slot] = all;
+        }
     }
     if (a.k == 0) return;
     __syncthreads();
