@@ -7,6 +7,7 @@ and captured graphs do not share any.
 """
 import ctypes as C
 import math
+import struct
 
 from . import E_ALIGN, E_CAPACITY, E_CUDA, E_INVALID, E_SHAPE, OUT_BF16, OUT_F16, OUT_F32, KVView, PlcError, PoolView, _check, lib
 
@@ -343,7 +344,7 @@ class PagePool:
             heads = q.shape[1]
             _int32(E_SHAPE, where, heads)
             if out is None:
-                out = torch.empty((N, heads, d), dtype=q.dtype, device=dev)
+                out = torch.empty_strided((N, heads, d), (heads * d, d, 1), dtype=q.dtype, device=dev)
             else:
                 _need(out.shape == q.shape and out.dtype == q.dtype and out.device == dev and out.stride(2) == 1, E_INVALID, where)
             queries = (q.data_ptr(), q.stride(0), q.stride(1), out.data_ptr(), out.stride(0), out.stride(1))
@@ -434,7 +435,7 @@ class PagePool:
             need = self._need_bytes[(book.rows, n_pos)] = b.value
         new, _ = PageBook._new(book.rows, book.max_pages, self.n_pages, dev)
         (rows, layers, heads, _), n = weight.shape, weight.numel() + 3 & ~3
-        store = torch.empty(n + (need + 3) // 4, dtype=torch.float32, device=dev)     # the workspace, a seventeenth of the weights, behind them
+        store = torch.empty_strided((n + (need + 3) // 4,), (1,), dtype=torch.float32, device=dev)     # the workspace, a seventeenth of the weights, behind them
         out = store.as_strided((rows, layers, heads, n_pos), (layers * heads * n_pos, heads * n_pos, n_pos, 1), 0)
         at = store.data_ptr()
         _check(_run(dev, api.plc_pages_evict, self._by, a, C.byref(w), budgets, scalar, recent, new._by, at, at + 4 * n, need, self._word), where)
@@ -540,39 +541,37 @@ class Rotary:
         import torch
         where, dev = "plc_rotary_apply", self.device
         single = isinstance(x, torch.Tensor)
-        xs = (x,) if single else tuple(x)
-        n_sets = len(xs)
-        _need(n_sets >= 1, E_INVALID, where)
-        outs = None if out is None else (out,) if isinstance(out, torch.Tensor) else tuple(out)
-        _need(n_sets <= 4 and (outs is None or len(outs) == n_sets), E_SHAPE, where)
-        N, dtype = _i32(pos, dev, where).numel(), xs[0].dtype
-        kind, sets, got, d = _kind(dtype, where), [], [], None
-        for i, t in enumerate(xs):
+        xs = (x,) if single else x
+        outs = (None,) * len(xs) if out is None else (out,) if isinstance(out, torch.Tensor) else out
+        _need(len(xs) >= 1, E_INVALID, where)
+        _need(len(xs) <= 4 and len(outs) == len(xs), E_SHAPE, where)
+        if xs[0].dim() != 3:
+            raise PlcError(E_SHAPE, where)
+        N, dtype, d = _i32(pos, dev, where).numel(), xs[0].dtype, xs[0].shape[2]
+        kind, sets, got = _kind(dtype, where), [], []
+        for t, o in zip(xs, outs):
             shape = t.shape
-            if len(shape) != 3 or shape[0] != N or (d is not None and shape[2] != d):
+            if len(shape) != 3 or shape[0] != N or shape[2] != d or N > 0x7fffffff or shape[1] > 0x7fffffff:
                 raise PlcError(E_SHAPE, where)
-            (_, heads, d), (row, head, one) = shape, t.stride()
+            heads, (row, head, one) = shape[1], t.stride()
             if one != 1 or t.dtype != dtype or t.device != dev:
                 raise PlcError(E_INVALID, where)
-            if outs is None:
-                o = torch.empty(shape, dtype=dtype, device=dev)
+            if o is None:
                 out_row, out_head = heads * d, d
+                o = torch.empty_strided(shape, (out_row, d, 1), dtype=dtype, device=dev)
             else:
-                o = outs[i]
                 _need(o.shape == shape and o.dtype == dtype and o.device == dev and o.stride(2) == 1, E_INVALID, where)
                 out_row, out_head, _ = o.stride()
             got.append(o)
-            if N > 0x7fffffff or heads > 0x7fffffff:
-                raise PlcError(E_SHAPE, where)
             sets += (t.data_ptr(), o.data_ptr(), row, head, out_row, out_head, heads)     # a plc_rotary_set, seven 64-bit words
         if N:
-            rc = _run(dev, _lib().plc_rotary_apply, self._by, _SETS[n_sets](*sets), n_sets, pos.data_ptr(), N, d, kind, 1 if back else 0)
+            rc = _run(dev, _lib().plc_rotary_apply, self._by, _SETS[len(xs)].pack(*sets), len(xs), pos.data_ptr(), N, d, kind, 1 if back else 0)
             if rc:
                 raise PlcError(rc, where)
         return got[0] if single else tuple(got)
 
 
-_SETS = [C.c_int64 * (7 * n) for n in range(5)]
+_SETS = [struct.Struct("%dq" % (7 * n)) for n in range(5)]
 
 
 def rotary_frequencies(dim, base=10000.0, ramp="none", factor=1.0, context=None, slow=1.0, fast=32.0):
@@ -619,7 +618,7 @@ def token_logprobs(logits, tokens, n_top=0, status=None):
     tops = N * n_top
     a, b, c = N * m, N * m + N, N * m + N + tops
     d = c + tops + 3 & ~3
-    store = torch.empty(d + (need + 3) // 4, dtype=torch.float32, device=dev)
+    store = torch.empty_strided((d + (need + 3) // 4,), (1,), dtype=torch.float32, device=dev)
     logp, entropy = store.as_strided(tokens.shape, tokens.stride(), 0), store.as_strided((N,), (1,), a)
     top_logp = store.as_strided((N, n_top), (n_top, 1), b)
     top_token = store.view(torch.int32).as_strided((N, n_top), (n_top, 1), c)
