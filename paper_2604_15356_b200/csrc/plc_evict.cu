@@ -19,7 +19,7 @@ namespace {
 
 constexpr int kSelectThreads = 256, kSelectWarps = kSelectThreads / 32;
 constexpr int kCopyThreads = 256, kMoveThreads = kCopyThreads + 64;      // that copy; and two warps that find out what comes next
-constexpr int kHeld = 4096;                       // positions of a row whose weights stay in shared memory while they are selected
+constexpr int kPlanThreads = 1024;                // of a plan in a launch of its own
 constexpr uint32_t kSpin = 1u << 22;
 
 // Positions of a piece: as many vectors as 32 KB of shared memory hold, at most 128.
@@ -35,6 +35,8 @@ struct EvictArgs {
     float* out;                                   // [rows][L][H][n_pos]
     const int32_t* budgets; int budget, recent;
     int piece_log2, pieces;                       // positions of a piece; pieces that n_pos has
+    int held;                                     // positions of a row whose weights stay in shared memory while they are selected
+    int planned;                                  // 1: a block of the selection makes the plan
     // workspace
     EvictHead* head;
     long long* first;                             // [rows + 1] pieces of the rows before
@@ -70,8 +72,8 @@ __device__ __forceinline__ uint32_t weight_order(float w) {
 }
 
 // Sum over the block's threads before this one; *total: over all.
-__device__ __forceinline__ long long sum_before(long long v, long long* total) {
-    __shared__ long long part[kSelectWarps];
+template <int THREADS> __device__ __forceinline__ long long sum_before(long long v, long long* total) {
+    __shared__ long long part[THREADS / 32];
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
     long long x = v;
 #pragma unroll
@@ -84,7 +86,7 @@ __device__ __forceinline__ long long sum_before(long long v, long long* total) {
     __syncthreads();
     long long before = x - v, all = 0;
 #pragma unroll
-    for (int w = 0; w < kSelectWarps; ++w) {
+    for (int w = 0; w < THREADS / 32; ++w) {
         if (w < wid) before += part[w];
         all += part[w];
     }
@@ -92,39 +94,55 @@ __device__ __forceinline__ long long sum_before(long long v, long long* total) {
     return before;
 }
 
-// One block: which rows go, how many fresh pages each needs and which, and how many pieces there are to move.
+// How many of row s's new pages others hold, which makes them fresh ones: -1 where the row stays, kOutOfRange where a page of its does not exist.  A block calls it, which also
+// writes down which they are.
 constexpr int kOutOfRange = 1 << 30;
+__device__ __forceinline__ void count_fresh(const PoolDev& p, const BookDev& in, const EvictArgs& a, int s, const EvictRow& r, bool good) {
+    const int keep = good ? pages_for(p, r.now) : 0;
+    long long before = 0, some;
+    for (int j0 = 0; j0 < keep; j0 += kSelectThreads) {
+        const int j = j0 + threadIdx.x;
+        const bool shared = j < keep && in.ref[in.table[(int64_t)s * in.max_pages + j]] != 1;
+        const long long at = before + sum_before<kSelectThreads>(shared, &some);
+        if (j < keep) a.rank[(int64_t)s * a.row_pages + j] = shared ? (int)at : -1;
+        before += some;
+    }
+    if (!a.planned && threadIdx.x == 0) a.count[s] = !r.goes ? -1 : good ? (int)before : kOutOfRange;
+}
+
+// One block: how many fresh pages each row needs (where the rows' own blocks have not counted them) and which, and how many pieces there are to move.
+template <int THREADS>
 __device__ __forceinline__ void evict_plan(const PoolDev& p, const BookDev& in, const EvictArgs& a, uint32_t* status) {
     const int tid = threadIdx.x;
     uint32_t bits = 0;
-    for (int s = tid; s < in.rows; s += kSelectThreads) {
-        const EvictRow r = evict_row(p, in, a, s);
-        if (r.bad) bits |= kStRange;
-        a.base[s] = r.goes ? pages_for(p, r.len) : -1;                   // pages that the row holds, for now
-        a.count[s] = r.goes ? 0 : -1;
-    }
-    __syncthreads();
-    const long long entries = (long long)in.rows * in.max_pages;
+    if (a.planned) {
+        for (int s = tid; s < in.rows; s += THREADS) {
+            const EvictRow r = evict_row(p, in, a, s);
+            a.base[s] = r.goes ? pages_for(p, r.len) : -1;               // pages that the row holds, for now
+            a.count[s] = r.goes ? 0 : -1;
+        }
+        __syncthreads();
+        const int entries = in.rows * in.max_pages;
 #pragma unroll 2
-    for (long long e = tid; e < entries; e += kSelectThreads) {
-        const int row = entries <= 0x7fffffffll ? (int)e / in.max_pages : (int)(e / in.max_pages), at = (int)(e - (long long)row * in.max_pages);
-        const int page = in.table[e], holds = a.base[row];
-        if (at >= holds) continue;
-        if (!page_ok(p, page)) atomicOr(&a.count[row], kOutOfRange);
-        else if (in.ref[page] != 1 && at < pages_for(p, evict_row(p, in, a, row).now)) atomicAdd(&a.count[row], 1);
+        for (int e = tid; e < entries; e += THREADS) {
+            const int row = e / in.max_pages, at = e - row * in.max_pages, page = in.table[e], holds = a.base[row];
+            if (at >= holds) continue;
+            if (!page_ok(p, page)) atomicOr(&a.count[row], kOutOfRange);
+            else if (in.ref[page] != 1 && at < pages_for(p, evict_row(p, in, a, row).now)) atomicAdd(&a.count[row], 1);
+        }
+        __syncthreads();
     }
-    __syncthreads();
     long long need = 0, moves = 0;
-    for (int s0 = 0; s0 < in.rows; s0 += kSelectThreads) {
+    for (int s0 = 0; s0 < in.rows; s0 += THREADS) {
         const int s = s0 + tid;
         int count = s < in.rows ? __ldcg(&a.count[s]) : -1;
-        if (count >= kOutOfRange) { bits |= kStRange; count = -1; }
-        const EvictRow r = count >= 0 ? evict_row(p, in, a, s) : EvictRow{};
+        const EvictRow r = s < in.rows ? evict_row(p, in, a, s) : EvictRow{};
+        if (r.bad || count >= kOutOfRange) { bits |= kStRange; count = -1; }
         const long long pieces = count >= 0 ? (long long)((r.len + (1 << a.piece_log2) - 1) >> a.piece_log2) * p.L * p.H * 2 : 0;
         long long total;
-        const long long at = need + sum_before(count >= 0 ? count : 0, &total);
+        const long long at = need + sum_before<THREADS>(count >= 0 ? count : 0, &total);
         need += total;
-        const long long first = moves + sum_before(pieces, &total);
+        const long long first = moves + sum_before<THREADS>(pieces, &total);
         moves += total;
         if (s < in.rows) {
             a.base[s] = count >= 0 ? (int)min(at, 0x7fffffffll) : -1;
@@ -132,13 +150,17 @@ __device__ __forceinline__ void evict_plan(const PoolDev& p, const BookDev& in, 
             a.first[s] = first;
         }
     }
+    constexpr int EACH = 8;                       // pages of a thread at a time
     long long found = 0;
-    for (long long i0 = 0; i0 < p.n_pages && found < need; i0 += kSelectThreads) {
-        const long long i = i0 + tid;
-        const bool free = i < p.n_pages && in.ref[i] == 0;
+    for (long long i0 = 0; i0 < p.n_pages && found < need; i0 += EACH * THREADS) {
+        const long long i = i0 + EACH * tid;
+        uint32_t free = 0;
+#pragma unroll
+        for (int k = 0; k < EACH; ++k)
+            if (i + k < p.n_pages && in.ref[i + k] == 0) free |= 1u << k;
         long long total;
-        const long long at = found + sum_before(free, &total);
-        if (free && at < need) a.list[at] = (int)i;
+        long long at = found + sum_before<THREADS>(__popc(free), &total);
+        for (; free && at < need; free &= free - 1) a.list[at++] = (int)i + __ffs(free) - 1;
         found += total;
     }
     const bool short_of = found < need;
@@ -150,13 +172,18 @@ __device__ __forceinline__ void evict_plan(const PoolDev& p, const BookDev& in, 
         a.first[in.rows] = short_of ? 0 : moves;
     }
 }
+__global__ void __launch_bounds__(kPlanThreads) evict_plan_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev in, const __grid_constant__ EvictArgs a,
+                                                                  uint32_t* status) {
+    chain_next();
+    chain_wait();
+    evict_plan<kPlanThreads>(p, in, a, status);
+}
 
 __device__ __forceinline__ void copy_weights(const float* w, float* out, int n, int n_pos) {
     for (int t = threadIdx.x; t < n_pos; t += blockDim.x) out[t] = t < n ? w[t] : 0.f;
 }
 
 struct SelectShared {
-    uint32_t key[kHeld];                          // of a short row's weights
     int bins[256];
     int above[kSelectWarps], equal[kSelectWarps];
     uint32_t prefix;
@@ -166,43 +193,35 @@ struct SelectShared {
 // The loops are kept small: a block goes through each of them few times, and code that comes from memory for the first time costs more than it does.
 __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(const __grid_constant__ PoolDev p, const __grid_constant__ BookDev in, const __grid_constant__ BookDev out,
                                                                       const __grid_constant__ EvictArgs a, uint32_t* status) {
+    extern __shared__ uint32_t key_s[];           // of a short row's weights
     __shared__ SelectShared sh;
     chain_next();
-    if (blockIdx.x == 0) { evict_plan(p, in, a, status); return; }
+    if ((int)blockIdx.x < a.planned) { evict_plan<kSelectThreads>(p, in, a, status); return; }
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-    const int lane_at = blockIdx.x - 1, h = lane_at % p.H, l = lane_at / p.H % p.L, s = lane_at / p.H / p.L;
+    const int lane_at = blockIdx.x - a.planned, h = lane_at % p.H, l = lane_at / p.H % p.L, s = lane_at / p.H / p.L;
     const float* w = a.weight + (int64_t)s * a.ws_row + (int64_t)l * a.ws_layer + (int64_t)h * a.ws_head;
     float* to = a.out + (int64_t)lane_at * a.n_pos;
     // the weights are on their way before the row's length is known
 #pragma unroll 4
-    for (int t = tid; t < min(a.n_pos, kHeld); t += kSelectThreads) sh.key[t] = weight_order(w[t]);
-    for (long long i = (long long)lane_at * kSelectThreads + tid; i < p.n_pages; i += (long long)(gridDim.x - 1) * kSelectThreads) out.ref[i] = in.ref[i];
+    for (int t = tid; t < a.held; t += kSelectThreads) key_s[t] = weight_order(w[t]);
+    for (long long i = (long long)lane_at * kSelectThreads + tid; i < p.n_pages; i += (long long)(gridDim.x - a.planned) * kSelectThreads) out.ref[i] = in.ref[i];
     const EvictRow r = evict_row(p, in, a, s);
     bool good = r.goes;
     if (good)
         for (int j = tid; j < pages_for(p, r.len); j += kSelectThreads) good = good && page_ok(p, in.table[(int64_t)s * in.max_pages + j]);
-    if (!__syncthreads_and(good)) {
+    good = __syncthreads_and(good);
+    if (l == 0 && h == 0) count_fresh(p, in, a, s, r, good);              // a block of the row
+    if (!good) {
         copy_weights(w, to, min(max(r.len, 0), a.n_pos), a.n_pos);
         return;
     }
-    if (l == 0 && h == 0) {                       // a block of the row: which of its new pages are fresh ones
-        const int keep = pages_for(p, r.now);
-        long long before = 0, some;
-        for (int j0 = 0; j0 < keep; j0 += kSelectThreads) {
-            const int j = j0 + tid;
-            const bool shared = j < keep && in.ref[in.table[(int64_t)s * in.max_pages + j]] != 1;
-            const long long at = before + sum_before(shared, &some);
-            if (j < keep) a.rank[(int64_t)s * a.row_pages + j] = shared ? (int)at : -1;
-            before += some;
-        }
-    }
     const int n = r.len - min(a.recent, r.now);                          // candidates; what stands behind them is kept
     int want = r.now - (r.len - n);                                      // of the candidates
-    const bool held = r.len <= kHeld;
+    const bool held = r.len <= a.held;
     const int pieces = (r.len + (1 << a.piece_log2) - 1) >> a.piece_log2;
     uint32_t* read = a.read + (int64_t)lane_at * a.pieces * 2;
     for (int c = tid; c < 2 * pieces; c += kSelectThreads) read[c] = 0;
-    auto key = [&](int t) { return held ? sh.key[t] : weight_order(w[t]); };
+    auto key = [&](int t) { return held ? key_s[t] : weight_order(w[t]); };
     // the want-th largest key among the candidates, eight bits at a time from the top
     uint32_t last = 0;
 #pragma unroll 1
@@ -501,20 +520,27 @@ plc_status plc_pages_evict(const plc_page_pool* pool, const plc_page_book* in, c
     const long long lanes = (long long)i.rows * p.L * p.H;
     uint8_t* ws = static_cast<uint8_t*>(workspace_dev);
     const int log2 = piece_log2(p.d * p.esz), piece = 1 << log2;
+    // Weights in shared memory: all of a row of 4096, as many as there is room for where few blocks run anyway (one row of 13000 positions in 4 heads: 68 us without, 34 with).
+    const int most_held = lanes <= 4 * sm_count() ? 49152 : 8192, held = weights->n_pos < most_held ? weights->n_pos : most_held;
+    // The plan is a block of the selection where it has little to look at, else a launch of its own, and the rows' blocks count their pages (31 rows of 4176 pages of one
+    // position: 307 us before, 96 so; where 16 rows have 65 pages each a launch more costs 2 us).
+    const bool apart = (long long)i.rows * i.max_pages > 16384;
     const EvictArgs a{weights->base_dev, weights->stride_row, weights->stride_layer, weights->stride_head, weights->n_pos, out_weights_dev, budget_dev, budget, recent,
-                      log2, (int)(((long long)weights->n_pos + piece - 1) / piece), reinterpret_cast<EvictHead*>(ws), reinterpret_cast<long long*>(ws + x.first),
-                      reinterpret_cast<int32_t*>(ws + x.base), reinterpret_cast<int32_t*>(ws + x.count), reinterpret_cast<int32_t*>(ws + x.list),
-                      reinterpret_cast<int32_t*>(ws + x.rank), (int)row_pages(p, weights->n_pos),
+                      log2, (int)(((long long)weights->n_pos + piece - 1) / piece), held, apart ? 0 : 1, reinterpret_cast<EvictHead*>(ws),
+                      reinterpret_cast<long long*>(ws + x.first), reinterpret_cast<int32_t*>(ws + x.base), reinterpret_cast<int32_t*>(ws + x.count),
+                      reinterpret_cast<int32_t*>(ws + x.list), reinterpret_cast<int32_t*>(ws + x.rank), (int)row_pages(p, weights->n_pos),
                       reinterpret_cast<uint32_t*>(ws + x.kept), reinterpret_cast<int32_t*>(ws + x.ahead), reinterpret_cast<uint32_t*>(ws + x.read)};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     int lanes_log2 = 0;
     while ((16 << lanes_log2) < p.d * p.esz) ++lanes_log2;
-    if (launch_kernel(evict_select_kernel, (unsigned)(1 + lanes), kSelectThreads, 0, st, false, 1, p, i, o, a, status_dev) != cudaSuccess) return PLC_E_CUDA;
+    if (held * 4 > 40 * 1024 && cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 49152 * 4) != cudaSuccess) return PLC_E_CUDA;
+    if (launch_kernel(evict_select_kernel, (unsigned)(a.planned + lanes), kSelectThreads, (size_t)held * 4, st, false, 1, p, i, o, a, status_dev) != cudaSuccess) return PLC_E_CUDA;
+    if (apart && launch_kernel(evict_plan_kernel, 1, kPlanThreads, 0, st, true, 1, p, i, a, status_dev) != cudaSuccess) return PLC_E_CUDA;
     // as many blocks as run at once (six of 32 KB an SM), or as the pieces that full rows would have
     const long long most = 6ll * sm_count(), want = 2 * lanes * a.pieces;
     if (launch_kernel(evict_move_kernel, (unsigned)(want < most ? want : most), kMoveThreads, (size_t)piece * p.d * p.esz, st, true, 1, p, i, o, a, lanes_log2, status_dev) != cudaSuccess)
         return PLC_E_CUDA;
-    count_launch(2);
+    count_launch(apart ? 3 : 2);
     return PLC_OK;
 }
 

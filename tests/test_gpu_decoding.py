@@ -535,6 +535,21 @@ def test_eviction_of_a_long_row(dev, ora):
         evict_case(dev, ora, budget, dtype, d, 1, 1, page, lens=[10000], budget=[budget], recent=2)[0].check()
 
 
+def test_eviction_of_rows_that_shared_memory_does_not_hold(dev, ora):
+    evict_case(dev, ora, 21, "f16", 32, 1, 1, 64, lens=[50001, 49152, 49153], budget=[20000, 49151, 5], recent=100, weights=lambda r, s: r.integers(0, 2000, s))[0].check()
+
+
+def test_eviction_of_many_pages(dev, ora):
+    """Pages of one position, which are counted by the rows' blocks; shared ones, a page out of range, a length out of range among them."""
+    lens, budget = [3000, 2900, 10, 3100, 2800, -1, 3100], [1500, 100, 50, 3000, 2799, 7, 900]
+    pool, bits = evict_case(dev, ora, 22, "bf16", 32, 2, 1, 1, lens=lens, budget=budget, recent=9, share=((1, 0, 2500), (4, 3, 1000)), spare=9000, bad_pages=((6, 3000),))
+    assert bits == ora.RANGE
+    with pytest.raises(plc.PlcError):
+        pool.check()
+    pool, bits = evict_case(dev, ora, 23, "bf16", 32, 2, 1, 1, lens=lens[:5], budget=budget[:5], recent=9, share=((1, 0, 2500), (4, 3, 1000)), spare=0)
+    assert bits == ora.CAPACITY                            # 3500 of their own pages are free, 1500 + 100 + 1000 + 1000 are needed
+
+
 @pytest.mark.parametrize("page", [1, 16, 256])
 def test_eviction_of_many_rows(dev, ora, page):
     """More rows than a block has threads, with nothing to do for most; pages of one position and pages that are longer than the rows."""
