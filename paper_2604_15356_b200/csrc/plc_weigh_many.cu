@@ -27,10 +27,10 @@ constexpr int kRing = 8;
 
 // DEEP: many row tiles an item, so that the queries' ring is what counts; else keys of the next item arrive while this one's are used.
 template <int D, bool DEEP> struct Many {
-    static constexpr int k_slots = DEEP ? 1 : 2, q_slots = DEEP ? 4 : 2;
+    static constexpr int k_slots = DEEP ? 1 : 2, q_slots = DEEP && D != 256 ? 4 : 2;
     static constexpr int blocks = (D + 63) / 64;                       // 128-byte wide column blocks (32 components: half of one)
     static constexpr int groups = D == 256 ? 1 : 2, pos = 128 * groups;  // positions of a tile; four warps for each 128
-    static constexpr int rows = D == 256 ? 64 : 128;                   // of a row tile
+    static constexpr int rows = D == 256 && !DEEP ? 64 : 128;          // of a row tile
     static constexpr int k_bytes = blocks * pos * 128, q_bytes = blocks * rows * 128;
     static constexpr int soft = 128 * groups, copy = 128, threads = soft + copy + 64;           // exponentials; copies; boxes of keys, products
     static constexpr int tmem = 2 * groups * rows;                     // S twice
@@ -489,8 +489,8 @@ __global__ void __launch_bounds__(Many<D, true>::pos) weigh_join_kernel(const __
 
 // The queries of a row tile as one box: the heads of a group by as many rows as make up the tile.  Where rows are picked, the group does not divide the tile, or strides are not
 // positive, they come in pieces.
-template <int D> bool query_boxes(const WeighArgs& a, bool bf16, CUtensorMap* map) {
-    using M = Many<D, true>;
+template <int D, bool DEEP> bool query_boxes(const WeighArgs& a, bool bf16, CUtensorMap* map) {
+    using M = Many<D, DEEP>;
     if (a.rows || D < 64 || M::rows % a.group || a.qs_row <= 0 || a.qs_head <= 0 || a.qs_row >= (1ll << 38) || a.qs_head >= (1ll << 38)) return false;
     const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)a.heads, (cuuint64_t)a.n_rows}, strides[2] = {(cuuint64_t)a.qs_head * 2, (cuuint64_t)a.qs_row * 2};
     const cuuint32_t boxes[3] = {64, (cuuint32_t)a.group, (cuuint32_t)(M::rows / a.group)}, ones[3] = {1, 1, 1};
@@ -509,7 +509,7 @@ cudaError_t launch(const PoolDev& p, const BookDev& b, const WeighArgs& args, ui
     const bool bf16 = Kind<T>::format == 1;
     const int even = p.page_pos & -p.page_pos, box = even > 128 ? 128 : even;     // the largest power of two that divides a page, so that boxes fill a tile
     a.box_pos = box >= 8 && page_boxes(p, a.layer, bf16, box, &k_map, a.box_dim) ? box : 0;
-    a.q_boxes = query_boxes<D>(a, bf16, &q_map);
+    a.q_boxes = query_boxes<D, DEEP>(a, bf16, &q_map);
     const int grid = sm_count();
     e = launch_kernel(weigh_many_kernel<T, D, DEEP>, grid, M::threads, M::smem, st, false, 1, p, b, a, k_map, q_map, status);
     return e != cudaSuccess ? e : launch_kernel(weigh_join_kernel<D>, grid - 1, M::pos, 0, st, true, 1, p, b, a, grid, status);
@@ -532,7 +532,9 @@ cudaError_t launch_weigh_many(const PoolDev& p, const BookDev& b, const WeighArg
     WeighArgs a = args;
     a.first = static_cast<int4*>(workspace);
     a.part = reinterpret_cast<float*>(a.first + sm_count());
-    const bool deep = (long long)a.n_list * a.group > 512ll * b.rows;          // by the mean: from four row tiles a session on
+    // By the mean of the columns a session.  16 sessions of up to 4000 positions, 8 KV heads, us with keys ahead and with queries ahead: 120 columns of 64 / 128 / 256 components
+    // 29.1 / 30.2 / 48.1 and 28.8 / 30.4 / 52.3, 240 columns 43.4 / 45.1 / 76.2 and 43.3 / 43.5 / 67.8, 800 columns 111 / 116 / 218 and 110 / 114 / 169.
+    const bool deep = (long long)a.n_list * a.group > 192ll * b.rows;
     if (deep) return bf16 ? launch_by_dim<__nv_bfloat16, true>(p, b, a, status, st) : launch_by_dim<__half, true>(p, b, a, status, st);
     return bf16 ? launch_by_dim<__nv_bfloat16, false>(p, b, a, status, st) : launch_by_dim<__half, false>(p, b, a, status, st);
 }
