@@ -28,7 +28,7 @@ struct TurnSet {
 struct TurnArgs {
     TurnSet set[kMostSets];
     int sets, units;                              // units of a row
-    const uint64_t* turns; int pairs; float scale; bool back;
+    const uint64_t* turns; int pairs; float scale; bool back; int lanes;             // lanes: of a row, where rows share a warp
     const int32_t* pos; int rows, d, rows_block, shares;             // shares: warps that share a row
     const int32_t* begin; int layer;              // pages: ranges of the sessions' rows
 };
@@ -187,6 +187,79 @@ __global__ void __launch_bounds__(kRowThreads, 8) turn_rows_kernel(const __grid_
     }
 }
 
+// The same for rows of few runs, several of which share a warp (a.lanes lanes each): the heads of all sets are taken as if they were one set's.  The blocks stay,
+// and the next row's position is on its way while one is turned.
+// A warp a row leaves most lanes without a load there.  Measured, rows of heads: 67732 of 2 + 2 of 32 in bf16 58 -> 12.5 us, 73352 of 2 + 2 of 128 (64 turned) in fp16
+// 70 -> 43, 47345 of 2 + 2 of 80 in binary32 46 -> 27.
+template <class T, bool INTER, bool WIDE>
+__global__ void __launch_bounds__(kRowThreads, 8) turn_small_kernel(const __grid_constant__ TurnArgs a) {
+    constexpr int bytes = run_bytes(WIDE, sizeof(T), INTER), W = bytes / (int)sizeof(T), P = INTER ? W / 2 : W, U = WIDE && !INTER ? 2 : 4;
+    extern __shared__ float2 turn_s[];                                          // [rows of the block][pairs]
+    const int lanes = a.lanes, log2 = __ffs(lanes) - 1, sub = (threadIdx.x & 31) >> log2, lane = threadIdx.x & (lanes - 1);
+    const int rows_warp = 32 >> log2, wid = threadIdx.x >> 5, step = gridDim.x * (kRowThreads / 32);
+    float2* turn = turn_s + (wid * rows_warp + sub) * a.pairs;
+    const int dim = a.set[0].dim, per_head = a.set[0].per_head, turned = dim / W / (INTER ? 1 : 2), half = dim / 2 * (int)sizeof(T);
+    const int wide = min(per_head, lanes), abreast = lanes / wide, heads = a.units / per_head;
+    const int last = (a.rows - 1) / rows_warp;
+    int at = blockIdx.x * (kRowThreads / 32) + wid, i = at * rows_warp + sub, next_pos = at <= last && i < a.rows ? a.pos[i] : 0;
+    for (; at <= last; at += step) {
+        i = at * rows_warp + sub;
+        const int pos = next_pos;
+        if (at + step <= last && i + step * rows_warp < a.rows) next_pos = a.pos[i + step * rows_warp];
+        __syncwarp();                             // the row before has been turned
+        for (int k = lane; k < a.pairs; k += lanes) turn[k] = turn_of(a, pos, k);
+        __syncwarp();
+        if (i >= a.rows) continue;
+#pragma unroll 1
+        for (int e0 = 0; e0 < per_head; e0 += lanes) {
+            const int e = e0 + lane % wide;
+            if (lane >= abreast * wide || e >= per_head) continue;
+            const bool turns = e < turned;
+            const int off = turns ? e * bytes : dim * (int)sizeof(T) + (e - turned) * bytes;
+            float2 cs[P];
+            if (turns) {
+#pragma unroll
+                for (int k = 0; k < P; ++k) cs[k] = turn[e * P + k];
+            }
+#pragma unroll 1
+            for (int h0 = lane / wide; h0 < heads; h0 += U * abreast) {
+                Run<T, W> x[U], y[U];
+                uint8_t* to[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    int h = h0 + u * abreast, t = 0;
+                    to[u] = nullptr;
+                    if (h >= heads) continue;
+#pragma unroll
+                    for (int k = 0; k + 1 < kMostSets; ++k)
+                        if (h >= a.set[t].heads) h -= a.set[t++].heads;
+                    const TurnSet& s = a.set[t];
+                    const uint8_t* from = s.x + (int64_t)i * s.xs_row + (int64_t)h * s.xs_head + off;
+                    to[u] = s.out + (int64_t)i * s.os_row + (int64_t)h * s.os_head + off;
+                    x[u].load(from);
+                    if (!INTER && turns) y[u].load(from + half);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (to[u]) {
+                        if (turns) {
+#pragma unroll
+                            for (int k = 0; k < P; ++k) {
+                                T& a0 = x[u].v[INTER ? 2 * k : k];
+                                T& b0 = INTER ? x[u].v[2 * k + 1 < W ? 2 * k + 1 : 0] : y[u].v[k];
+                                const float xa = Wide<T>::get(a0), xb = Wide<T>::get(b0);
+                                a0 = Wide<T>::put(xa * cs[k].x - xb * cs[k].y);
+                                b0 = Wide<T>::put(xb * cs[k].x + xa * cs[k].y);
+                            }
+                            if (!INTER) y[u].store(to[u] + half);
+                        }
+                        x[u].store(to[u]);
+                    }
+            }
+        }
+    }
+}
+
 // Component by component, where addresses, strides or parts of a head allow no runs.  A block takes a few rows with all their heads.
 template <class T, bool INTER, bool PAGES>
 __global__ void __launch_bounds__(kTurnThreads) turn_parts_kernel(const __grid_constant__ TurnArgs a, const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
@@ -262,12 +335,24 @@ plc_status launch_turn(TurnArgs& a, const PoolDev& p, const BookDev& b, int dtyp
         // warps that share a row: so many that there are sixteen an SM, as long as each has the runs of a load for all of its lanes
         const long long want = (16ll * sms + a.rows - 1) / a.rows, most = (units + 127) / 128;
         a.shares = (int)(want < most ? want : most);
+        a.units = units;
+        // or, where rows are many and small, rows that share a warp: as few lanes as leave each two rounds of loads.  40000 rows of 4 + 4 heads of 128 in bf16: halves
+        // 36.5 us (twice the loads a lane 41), neighbours 39 (half the loads 47)
+        a.lanes = 32;
+        const int loads = wide && !inter ? 4 : 8;
+        if (!PAGES && a.shares == 1)
+            while (a.lanes > 4 && units <= loads * a.lanes / 2) a.lanes /= 2;
         constexpr int warps = kRowThreads / 32;
-        const unsigned grid = (unsigned)(((long long)a.rows * a.shares + warps - 1) / warps);
-        const size_t smem = (size_t)warps * a.pairs * sizeof(float2);
-        auto rows = [&](auto* wide_inter, auto* wide_half, auto* inter_kern, auto* half) { return go(wide ? (inter ? wide_inter : wide_half) : inter ? inter_kern : half, grid, kRowThreads, smem); };
-#define PLC_TURN(T) rows(turn_rows_kernel<T, true, PAGES, true>, turn_rows_kernel<T, false, PAGES, true>, turn_rows_kernel<T, true, PAGES, false>, turn_rows_kernel<T, false, PAGES, false>)
-        e = dtype == PLC_OUT_F32 ? PLC_TURN(float) : dtype == PLC_OUT_F16 ? PLC_TURN(__half) : PLC_TURN(__nv_bfloat16);
+        const bool small = a.lanes < 32;
+        const long long full = ((long long)a.rows * a.shares * a.lanes / 32 + warps) / warps, stay = 8ll * sms;
+        const unsigned grid = (unsigned)(small ? (full < stay ? full : stay) : ((long long)a.rows * a.shares + warps - 1) / warps);
+        const size_t smem = (size_t)warps * (32 / a.lanes) * a.pairs * sizeof(float2);
+        auto rows = [&](auto* wide_inter, auto* wide_half, auto* inter_kern, auto* half) { return wide ? (inter ? wide_inter : wide_half) : inter ? inter_kern : half; };
+#define PLC_TURN(T) go(rows(turn_rows_kernel<T, true, PAGES, true>, turn_rows_kernel<T, false, PAGES, true>, turn_rows_kernel<T, true, PAGES, false>, turn_rows_kernel<T, false, PAGES, false>), grid, kRowThreads, smem)
+#define PLC_TURN_SMALL(T) launch_kernel(rows(turn_small_kernel<T, true, true>, turn_small_kernel<T, false, true>, turn_small_kernel<T, true, false>, turn_small_kernel<T, false, false>), grid, kRowThreads, smem, st, false, 1, a)
+        if (small) e = dtype == PLC_OUT_F32 ? PLC_TURN_SMALL(float) : dtype == PLC_OUT_F16 ? PLC_TURN_SMALL(__half) : PLC_TURN_SMALL(__nv_bfloat16);
+        else e = dtype == PLC_OUT_F32 ? PLC_TURN(float) : dtype == PLC_OUT_F16 ? PLC_TURN(__half) : PLC_TURN(__nv_bfloat16);
+#undef PLC_TURN_SMALL
 #undef PLC_TURN
     } else {
         // rows of a block so that there are several blocks an SM
