@@ -3,9 +3,9 @@
 // A row that holds more than its budget keeps, in every layer and head by itself, the positions of the largest weights and its last ones; what is kept moves
 // together in order, keys, values and weights alike, and the pages behind the new length are released.
 //
-// Two launches.  The first selects: a block a (row, layer, head) finds the weight of the last position that is kept by its bits, eight at a time from the
-// top, and writes a bit for each position that is kept, and the kept weights; one block more decides, like the plan of a fork, which pages are fresh ones.  The
-// second moves the vectors in pieces and writes the new book.  A position never moves up, so that a row can stay in its pages: a piece's places hold one or two
+// Two launches, three where books are large.  The first selects: a block a (row, layer, head) finds the weight of the last position that is kept by its bits, eight at a time from the
+// top, and writes a bit for each position that is kept, and the kept weights; one block more decides, like the plan of a fork, which pages are fresh ones
+// (a launch of its own where books are large).  The last moves the vectors in pieces and writes the new book.  A position never moves up, so that a row can stay in its pages: a piece's places hold one or two
 // earlier pieces of the same row, and it is written once those have been read.
 //
 // HBM bound where much moves: 16 rows of up to 2048 positions, 8 layers of 8 heads of 128 in bf16, 1024 kept: 129 us on the device, 18 of them the selection (0.5 GB moved, 4.5 TB/s).

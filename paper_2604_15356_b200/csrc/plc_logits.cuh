@@ -339,7 +339,7 @@ __device__ __forceinline__ void row_part(const RowArgs& a, int row, int part) {
     };
     if (a.k > kRowThreads / 2) {
         // With as many places as lanes the least of the lanes' maxima is the bound, and five times as many logits reach it as are wanted, now and then more than there is room
-        // for (1024 rows of 128256, 128 of each: 555 us).  One that goes by the lanes' chunks is nearer to the k-th largest (122 us; for 64 of each it would be 100 instead of 89).
+        // for (1024 rows of 128256, 128 of each: 555 us).  One that goes by the lanes' chunks is nearer to the k-th largest (119 us; for 64 of each it was 100 instead of 89, 85 by now).
         float* list = reinterpret_cast<float*>(found);
         const float limit = bound;
         for (int c = 0; c < chunk; ++c) {

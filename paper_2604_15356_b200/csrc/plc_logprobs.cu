@@ -3,8 +3,8 @@
 // With y = x - max x and Z = sum exp y:  log p_v = y_v - ln Z,  H = ln Z + (sum exp(y) (-y)) / Z.  One pass over the logits (the rows of beam selection, with the
 // second sum beside the first) leaves maximum, sums and the n largest of each part of a row; a second, small launch joins the parts and
 // looks the given tokens up, where not a block or a cluster has the whole row and does so itself.  HBM bound: each logit is read once.
-// Measured on the device: 1024 rows of 128256 in bf16, 8 alternatives 65 us (263 MB, 4.0 TB/s; issue slots 0.63, the exponentials' unit 0.57 busy; without exponentials 57, without
-// the maxima 60); 64 alternatives 89, 128 126; one row of 32000 9 us.
+// Measured on the device: 1024 rows of 128256 in bf16, 8 alternatives 61 us (263 MB, 4.3 TB/s; issue slots 0.63, the exponentials' unit 0.57 busy; of 65 us then
+// without exponentials 57, without the maxima 60); 64 alternatives 85, 128 119; one row of 32000 8 us.
 //
 // Exponentials and the sums of 32 of them are binary32, what is added up beyond binary64.  The largest term of Z is exactly 1 and -y >= 0, so that neither a
 // log probability near 0 nor a small entropy is the difference of larger numbers (terms below 2^-24 of their group are rounded to it).

@@ -2,7 +2,7 @@
 //
 // As in the other kernel positions are the rows of S = K Q^T, here the 128 lanes of tensor memory: a thread has a position, and the exponentials of the
 // tile's columns are summed in its register, from row tile to row tile.  A CTA holds a tile of positions in shared memory (two of them, so that the next one arrives meanwhile)
-// and goes through the row tiles that see any of it; Q and S have two buffers each, Q four where there are many row tiles.  Boxes of pages and of queries where their layouts allow it,
+// and goes through the row tiles that see any of it; Q and S have two buffers each, Q four where there are many row tiles of up to 128 components.  Boxes of pages and of queries where their layouts allow it,
 // else pieces of 16 bytes.
 //
 // Bound by the exponentials (16 a clock and SM; the products need half as long): 2048 tokens of 8 x 4 heads of 128 behind 8192 positions 243 us on the device (156 GFLOP, 640 TFLOP/s;
