@@ -352,6 +352,7 @@ __device__ __forceinline__ void row_part(const RowArgs& a, int row, int part) {
         }
         __syncthreads();
         const int listed = count;
+        __syncthreads();                          // all have read it: the branch, which has barriers, is taken by all or none, and the counter begins anew behind it
         if (listed <= 2 * kRoom) {
             uint32_t least = 0;
             for (int bit = 31; bit >= 0; --bit) {
