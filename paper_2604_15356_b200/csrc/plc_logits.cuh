@@ -27,7 +27,7 @@ struct RowArgs {
 
 // A key orders by (value, lower column first): the value's order-preserving bits above the complement of the column.
 __device__ __forceinline__ uint32_t order_bits(float x) {
-    const uint32_t b = __float_as_uint(x + 0.0f);                       // -0 becomes +0
+    const uint32_t b = __float_as_uint(x + 0.0f);                       // -0 becomes +0, NaN of either sign the positive one, which stands above all: its row has its places filled
     return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o); }

@@ -114,3 +114,30 @@ def test_many_beams_where_many_reach_the_bound(dev, dtype):
         assert parent[s].tolist() == [s * W + w for _, w, _ in c] and token[s].tolist() == [v for _, _, v in c], s
         want = np.array([-f for f, _, _ in c])
         assert (np.abs(out[s] - want) <= slack + 2.0 ** -24 * np.abs(want)).all(), s
+
+
+@pytest.mark.parametrize("dtype, bits", [("f16", 0xfe00), ("bf16", 0xffc0), ("f32", 0xffc00000), ("f16", 0x7e00), ("bf16", 0x7fc0), ("f32", 0x7fc00000)])
+def test_rows_of_nan_have_every_place_written(dev, dtype, bits):
+    """NaN of both signs: a row that is no distribution has alternatives -inf and -1 at every place, whatever was in the memory, also where few or no other logits are
+    there to stand in it.  One part a row, a cluster a row, parts that a second launch joins."""
+    from paper_2604_15356_b200 import serving
+    api, word = serving._lib(), torch.int32 if dtype == "f32" else torch.int16
+    wrapped = bits - (1 << 8 * TYPES[dtype].itemsize) if bits >> (8 * TYPES[dtype].itemsize - 1) else bits
+    for N, width, n_top, some in ((3, 5, 5, 1), (3, 5, 9, 1), (2, 128, 128, 1), (3, 3, 3, 3), (3, 9000, 16, 9000), (2, 128256, 128, 128200), (200, 20000, 7, 19997), (200, 20000, 7, 20000)):
+        x = torch.randn(N, width, generator=torch.Generator().manual_seed(width)).to(TYPES[dtype])
+        x[1].view(word)[torch.randperm(width, generator=torch.Generator().manual_seed(1))[:some]] = wrapped
+        assert int(x[1].isnan().sum()) == some
+        on, tokens = x.to(dev), torch.zeros(N, 1, dtype=torch.int32, device=dev)
+        need = serving._bytes(dev, api.plc_token_logprobs_workspace, N, width, n_top)
+        logp, entropy = torch.full((N, 1), 7.0, device=dev), torch.full((N,), 7.0, device=dev)
+        top, token = torch.full((N, n_top), 7.0, device=dev), torch.full((N, n_top), 7, dtype=torch.int32, device=dev)
+        ws = torch.full((need,), 7, dtype=torch.uint8, device=dev)
+        assert api.plc_token_logprobs(on.data_ptr(), serving._kind(on.dtype, ""), width, N, width, tokens.data_ptr(), 1, n_top, logp.data_ptr(), entropy.data_ptr(), top.data_ptr(),
+                                      token.data_ptr(), ws.data_ptr(), need, None, torch.cuda.current_stream().cuda_stream) == plc.OK
+        assert bool((token[1] == -1).all()) and bool((top[1] == -math.inf).all()), (N, width, n_top, some)
+        assert bool(logp[1].isnan().all()) and bool(entropy[1].isnan())
+        other = torch.log_softmax(x[0].double(), 0).sort(descending=True, stable=True)
+        k = min(n_top, width)
+        assert token[0, :k].tolist() == other.indices[:k].tolist() and bool((token[0, k:] == -1).all()) and bool((top[0, k:] == -math.inf).all())
+        # standard normal logits: mean distance to the largest below 8, so 2^-20 + 2^-23 8 and the rounding
+        assert bool(((top[0, :k].double().cpu() - other.values[:k]).abs() <= 2.0 ** -19 + 2.0 ** -24 * other.values[:k].abs()).all())
