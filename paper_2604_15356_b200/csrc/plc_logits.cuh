@@ -171,8 +171,11 @@ __device__ __noinline__ uint32_t cut(unsigned long long* buf, int n, int k, int 
     return least;
 }
 
-template <class T> struct Step { static constexpr int groups = 4; };                  // 64 bytes a lane
-template <> struct Step<float> { static constexpr int groups = 2; };
+// groups: 64 bytes a lane.  last_bit: the bits of order_bits below it are alike in all values of the type of one sign.
+template <class T> struct Step;
+template <> struct Step<__nv_bfloat16> { static constexpr int groups = 4, last_bit = 16; };
+template <> struct Step<__half> { static constexpr int groups = 4, last_bit = 13; };
+template <> struct Step<float> { static constexpr int groups = 2, last_bit = 0; };
 
 // A block takes a part of a row in two passes.  The first streams: a warp takes 32 lanes times kGroups times eight logits a step, the next step's loads on
 // their way, forms the sum and keeps the maximum of each lane's chunks of steps.  The k-th largest of the lanes' maxima is a bound that k logits reach and
@@ -297,12 +300,13 @@ __device__ __forceinline__ void row_part(const RowArgs& a, int row, int part) {
     __syncthreads();
     const long long slot = (long long)row * a.parts + part;
     if (wid == 0 && a.k > 0) {
-        // the k-th largest of the lanes' maxima, by the upper half of their bits: what is just below it will do as a bound
+        // the k-th largest of the lanes' maxima, by all the bits that differ: logits far from 0 lie closer together than half of their bits tell (512 rows of 128256 in binary32
+        // around 1000, beams: 893 us by the upper 16 bits, 59 by all)
         uint32_t v[kRowWarps], least = 0;
 #pragma unroll
         for (int i = 0; i < kRowWarps; ++i) v[i] = order[i * 32 + lane];
 #pragma unroll 1
-        for (int bit = 31; bit >= 16; --bit) {
+        for (int bit = 31; bit >= Step<T>::last_bit; --bit) {
             const uint32_t t = least | (1u << bit);
             int c = 0;
 #pragma unroll

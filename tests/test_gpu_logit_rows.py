@@ -141,3 +141,22 @@ def test_rows_of_nan_have_every_place_written(dev, dtype, bits):
         assert token[0, :k].tolist() == other.indices[:k].tolist() and bool((token[0, k:] == -1).all()) and bool((top[0, k:] == -math.inf).all())
         # standard normal logits: mean distance to the largest below 8, so 2^-20 + 2^-23 8 and the rounding
         assert bool(((top[0, :k].double().cpu() - other.values[:k]).abs() <= 2.0 ** -19 + 2.0 ** -24 * other.values[:k].abs()).all())
+
+
+@pytest.mark.parametrize("dtype, mean, spread", [("f32", 1000.0, 1.0), ("f32", -1000.0, 1.0), ("f16", 50.0, 0.1), ("f16", -900.0, 4.0), ("bf16", -50.0, 1.0), ("f32", 0.0, 1e-4)])
+@pytest.mark.parametrize("places", [1, 8, 64])
+def test_places_of_logits_far_from_zero(dev, dtype, mean, spread, places):
+    """Logits whose upper bits are alike, of both signs: the bound that the places go by is the k-th largest maximum itself."""
+    N = 1024
+    x = (torch.from_numpy(np.random.default_rng(places).standard_normal((4, V)).astype(np.float32)) * spread + mean).to(TYPES[dtype])
+    on = x.to(dev).repeat(N // 4, 1)
+    logp, entropy, top, token = plc.token_logprobs(on, torch.zeros(N, 1, dtype=torch.int32, device=dev), places)
+    score, parent, best = plc.beam_select(on.view(N, 1, V), torch.zeros(N, 1, device=dev), places)
+    assert torch.equal(token, best) and bool((parent == torch.arange(N, device=dev)[:, None]).all())
+    for r in range(4):
+        order, most, l, m, y = best_of(x[r])
+        want = (y[order[:places]] - most) - l
+        for t in (top, score):
+            assert torch.equal(t.view(N // 4, 4, places)[:, r], t[r].expand(N // 4, -1))
+            assert (np.abs(t[r].double().cpu().numpy() - want) <= 2.0 ** -20 + 2.0 ** -23 * m + 2.0 ** -24 * np.abs(want)).all()
+        assert token[r].tolist() == order[:places].tolist() and bool((token.view(N // 4, 4, places)[:, r] == token[r]).all())
