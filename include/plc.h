@@ -558,7 +558,7 @@ plc_status plc_pages_weigh_workspace(const plc_page_pool* pool, int32_t sessions
 
 /* Rows with more than their budget (budget_dev [rows], negative: the row stays; or NULL: `budget` for all) keep that many positions: in every layer and head by
  * itself the last min(recent, budget) ones, and of the others those with the largest weights, ties to the lower position, NaN last.  What is kept moves together in
- * order, in the pages and in out_weights_dev [rows][n_layers][n_kv_heads][n_pos] (contiguous; must not overlap weights; 0 from the new length on).
+ * order, in the pages and in out_weights_dev [rows][n_layers][n_kv_heads][n_pos] (contiguous, outside of what lies between the first and the last element of weights; 0 from the new length on).
  * The new length is the budget, pages behind it are released; of the pages that the row still has, those with other holders are replaced by fresh ones, the
  * lowest-numbered free ones of `in`, in order.  Other rows stay as they are, what they hold behind their length too, and their weights are copied.
  * Keys that were turned stay turned: later tokens are given their positions by plc_new_tokens.pos_dev, since len + i no longer counts what was evicted.

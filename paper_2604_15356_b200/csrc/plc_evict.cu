@@ -483,6 +483,14 @@ bool overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return x < y + nb && y < x + na;
 }
+// Whether the kept weights lie between the first and the last of the old ones, or across either end: other blocks still read those while they are written.
+bool among(const PoolDev& p, int rows, const plc_weights& w, const float* out) {
+    __int128 lo = 0, hi = w.n_pos;                // elements from the base
+    const __int128 reach[3] = {(__int128)(rows - 1) * w.stride_row, (__int128)(p.L - 1) * w.stride_layer, (__int128)(p.H - 1) * w.stride_head};
+    for (const __int128 r : reach) (r < 0 ? lo : hi) += r;
+    const __int128 base = (__int128)reinterpret_cast<uintptr_t>(w.base_dev), to = (__int128)reinterpret_cast<uintptr_t>(out);
+    return to < base + 4 * hi && base + 4 * lo < to + (__int128)4 * rows * p.L * p.H * w.n_pos;
+}
 
 }  // namespace
 }  // namespace plc
@@ -514,7 +522,7 @@ plc_status plc_pages_evict(const plc_page_pool* pool, const plc_page_book* in, c
     if (!plc_aligned16(workspace_dev) || ((reinterpret_cast<uintptr_t>(weights->base_dev) | reinterpret_cast<uintptr_t>(out_weights_dev)) & 3)) return PLC_E_ALIGN;
     const uint64_t t = 4ull * i.rows * i.max_pages, n = 4ull * p.n_pages;
     if (overlap(i.table, t, o.table, t) || overlap(i.len, 4ull * i.rows, o.len, 4ull * i.rows) || overlap(i.ref, n, o.ref, n)) return PLC_E_INVALID;
-    if (weights->base_dev == out_weights_dev) return PLC_E_INVALID;
+    if (among(p, i.rows, *weights, out_weights_dev)) return PLC_E_INVALID;
     const EvictLayout x = layout_of(p, i.rows, weights->n_pos);
     if (workspace_bytes < x.bytes) return PLC_E_CAPACITY;
     const long long lanes = (long long)i.rows * p.L * p.H;

@@ -216,3 +216,27 @@ def test_the_oracle_by_hand():
     assert t.tolist() == [[3, 2, -1]] and r.tolist() == [0, 1, 1, 1] and ww.tolist() == [[[[5, 9, 2, 0, 0, 0]]]]
     lp, h, tl, tt, _ = o.token_logprobs(np.log(np.array([[.5, .25, .25]])), np.array([[1, -1]]), 4)
     assert np.allclose(np.exp(lp), [[.25, 1]]) and np.allclose(h, 1.5 * math.log(2)) and tt.tolist() == [[0, 1, 2, -1]] and np.isinf(tl[0, 3])
+
+
+def test_evictions_onto_the_weights_are_refused(lib):
+    """Kept weights that lie among the old ones, shifted or between rows that are far apart: 3 rows, 2 layers, 4 heads, 100 positions, 9600 bytes where they are contiguous."""
+    def call(base, out, strides=(800, 400, 100)):
+        w = serving.Weights(base, *strides, 100)
+        n = C.c_uint64()
+        assert lib.plc_pages_evict_workspace(C.byref(pool()), 3, 100, C.byref(n)) == plc.OK
+        return lib.plc_pages_evict(C.byref(pool()), C.byref(book()), C.byref(w), None, 5, 1, C.byref(book(B + (1 << 20))), C.c_void_p(out), C.c_void_p(WS), C.c_uint64(n.value - 1),
+                                   C.c_void_p(A), None)
+    at = 1 << 26
+    for out in (at, at + 4, at + 9596, at - 4, at - 9596):
+        assert call(at, out) == plc.E_INVALID, out
+    for out in (at + 9600, at - 9600):
+        assert call(at, out) == plc.E_CAPACITY, out             # past the check, to the workspace that is a byte short
+    wide = (10000, 400, 100)                                     # rows 40000 bytes apart, the last one ends at 83200
+    for out in (at + 83196, at + 4000, at - 9596):
+        assert call(at, out, wide) == plc.E_INVALID, out
+    assert call(at, at + 83200, wide) == plc.E_CAPACITY
+    down = (-800, 400, 100)                                      # rows that go down
+    assert call(at, at - 6400, down) == plc.E_INVALID and call(at, at - 6400 - 9600, down) == plc.E_CAPACITY and call(at, at + 3200, down) == plc.E_CAPACITY
+    assert call(at, at + 3196, down) == plc.E_INVALID
+    huge = (1 << 62, 1 << 62, 1 << 62)                           # no sum of these wraps
+    assert call(at, at + 4096, huge) == plc.E_INVALID and call(at, at - 9600, huge) == plc.E_CAPACITY
