@@ -550,6 +550,7 @@ typedef struct {
  * that does not change from call to call.  Positions from n_pos on are left out (bit 1).  Ranges, lengths, rows and page numbers out of range, and more entries
  * than positions (bit 32): ranges and lengths are cut to what there is, a row counts for nothing, positions without a page receive nothing.
  * What a call does goes by the mean number of entries: sessions of very different numbers belong in calls of their own.
+ * Weights of which one element belongs to two rows or heads are refused.
  * workspace: plc_pages_weigh_workspace bytes (0 where the sessions have few entries: NULL then). */
 plc_status plc_pages_weigh(const plc_page_pool* pool, int32_t layer, const plc_page_book* book, const plc_weigh_queries* queries, float scale,
                            float decay, const plc_weights* weights, void* workspace_dev, uint64_t workspace_bytes, uint32_t* status_dev,

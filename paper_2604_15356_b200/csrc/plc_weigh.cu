@@ -239,7 +239,7 @@ plc_status plc_pages_weigh(const plc_page_pool* pool, int32_t layer, const plc_p
     if (!t || !t->q_dev || !t->lse_dev || !t->begin_dev || t->n_rows < 0 || t->n_list < 0 || !weights || !weights->base_dev || !status_dev) return PLC_E_INVALID;
     if (layer < 0 || layer >= p.L || pool->dtype == PLC_OUT_F32 || !(scale > 0.f) || isinf(scale) || !isfinite(decay) || decay < 0.f) return PLC_E_INVALID;
     if (t->n_heads < 1 || weights->n_pos < 1) return PLC_E_INVALID;
-    if ((b.rows > 1 && weights->stride_row == 0) || (p.L > 1 && weights->stride_layer == 0) || (p.H > 1 && weights->stride_head == 0)) return PLC_E_INVALID;
+    if (!runs_apart(weights->stride_row, b.rows, weights->stride_head, p.H, weights->n_pos) || (p.L > 1 && weights->stride_layer == 0)) return PLC_E_INVALID;
     if (t->n_heads % p.H || t->n_heads > (1 << 16) || (!t->rows_dev && t->n_list > t->n_rows)) return PLC_E_SHAPE;
     const int group = t->n_heads / p.H;
     if ((long long)t->n_list * group > (1 << 30)) return PLC_E_SHAPE;

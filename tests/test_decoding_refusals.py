@@ -240,3 +240,25 @@ def test_evictions_onto_the_weights_are_refused(lib):
     assert call(at, at + 3196, down) == plc.E_INVALID
     huge = (1 << 62, 1 << 62, 1 << 62)                           # no sum of these wraps
     assert call(at, at + 4096, huge) == plc.E_INVALID and call(at, at - 9600, huge) == plc.E_CAPACITY
+
+
+def test_weights_on_top_of_each_other_are_refused(lib):
+    """Against every pair of runs: strides of either sign, nested and not, from 0 on; one row or one head needs no stride."""
+    rng = np.random.default_rng(1)
+    seen = set()
+    for i in range(4000):
+        rows, H, n = int(rng.integers(1, 6)), int(rng.integers(1, 6)), int(rng.integers(1, 9))
+        row, head = (int(x) for x in rng.integers(-6 * n, 6 * n + 1, 2))
+        starts = sorted(r * row + h * head for r in range(rows) for h in range(H))
+        apart = all(b - a >= n for a, b in zip(starts, starts[1:]))
+        q = serving.WeighQueries(A, 64 * H, 64, A, None, A, 7, 0, H)
+        rc = lib.plc_pages_weigh(C.byref(pool(L=1, H=H)), 0, C.byref(book(rows=rows)), C.byref(q), C.c_float(1.0), C.c_float(1.0),
+                                 C.byref(serving.Weights(B, row, 0, head, n)), C.c_void_p(WS), C.c_uint64(1 << 20), C.c_void_p(A), None)
+        assert rc == (plc.OK if apart else plc.E_INVALID), (rows, H, n, row, head)
+        seen.add((apart, row < 0, head < 0, abs(row) > abs(head), rows > 1 and H > 1))
+    assert len(seen) >= 28
+    q = serving.WeighQueries(A, 256, 64, A, None, A, 7, 0, 4)
+    for row, head, rc in ((1 << 62, 1 << 62, plc.E_INVALID), (-(1 << 63), 1 << 61, plc.OK), (1 << 62, 100, plc.OK), (400, 100, plc.OK), (399, 100, plc.E_INVALID), (100, 300, plc.OK),
+                          (100, 299, plc.E_INVALID)):
+        assert lib.plc_pages_weigh(C.byref(pool(L=1)), 0, C.byref(book()), C.byref(q), C.c_float(1.0), C.c_float(1.0), C.byref(serving.Weights(B, row, 0, head, 100)), C.c_void_p(WS),
+                                   C.c_uint64(1 << 20), C.c_void_p(A), None) == rc, (row, head)
