@@ -41,19 +41,16 @@ inline plc_status check_book(const plc_page_book* b, BookDev* out) {
     return PLC_OK;
 }
 
-// Whether runs of n elements at i*a + j*b (i < na, j < nb) are apart from each other.  Strides that nest, as those of nearly all tensors do, are seen at once; others
-// are looked at one j at a time, where two runs are nearest.
+// Whether runs of n elements at i*a + j*b (i < na, j < nb) are apart from each other.  Strides that nest, as those of nearly all tensors do, are seen at once; for others
+// each step along the shorter of the two is held against the nearest along the other.
 inline bool runs_apart(int64_t a, int64_t na, int64_t b, int64_t nb, int64_t n) {
     __int128 x = a < 0 ? -(__int128)a : a, y = b < 0 ? -(__int128)b : b;         // a run's mirror image counts as it does
-    if (na < 2) x = 0;
-    if (nb < 2) y = 0;
     if ((na > 1 && x < n) || (nb > 1 && y < n)) return false;
-    if (na < 2 || nb < 2) return true;
-    if (y > x) { const __int128 t = x; x = y; y = t; const int64_t m = na; na = nb; nb = m; }
-    if (x >= (nb - 1) * y + n) return true;
-    for (int64_t j = 1; j < nb; ++j) {            // some i x within n of j y?
-        const __int128 i = j * y / x, off = j * y - i * x;
-        if ((i < na && off < n) || (i + 1 < na && x - off < n)) return false;
+    if (na < 2 || nb < 2 || x >= (nb - 1) * y + n || y >= (na - 1) * x + n) return true;
+    if (na > nb) { const __int128 t = x; x = y; y = t; const int64_t m = na; na = nb; nb = m; }
+    for (int64_t i = 1; i < na; ++i) {
+        const __int128 j = i * x / y, off = i * x - j * y;
+        if ((j < nb && off < n) || (j + 1 < nb && y - off < n)) return false;
     }
     return true;
 }

@@ -416,13 +416,16 @@ plc_status plc_rotary_apply(const plc_rotary* rotary, const plc_rotary_set* sets
     const int esz = dtype == PLC_OUT_F32 ? 4 : 2;
     long long heads = 0;
     for (int i = 0; i < n_sets; ++i) {
+        if (sets[i].heads < 1) return PLC_E_INVALID;
+        heads += sets[i].heads;
+    }
+    if (heads > (1 << 12)) return PLC_E_SHAPE;
+    for (int i = 0; i < n_sets; ++i) {
         const plc_rotary_set& s = sets[i];
-        if (!s.x_dev || !s.out_dev || s.heads < 1) return PLC_E_INVALID;
+        if (!s.x_dev || !s.out_dev) return PLC_E_INVALID;
         if ((reinterpret_cast<uintptr_t>(s.x_dev) | reinterpret_cast<uintptr_t>(s.out_dev)) & (esz - 1)) return PLC_E_ALIGN;
         if (s.x_dev == s.out_dev && ((n_rows > 1 && s.x_stride_row != s.out_stride_row) || (s.heads > 1 && s.x_stride_head != s.out_stride_head))) return PLC_E_INVALID;
-        if ((n_rows > 1 && s.out_stride_row == 0) || (s.heads > 1 && s.out_stride_head == 0)) return PLC_E_INVALID;     // results on top of each other
-        heads += s.heads;
-        if (heads > (1 << 12)) return PLC_E_SHAPE;
+        if (n_rows > 0 && !runs_apart(s.out_stride_row, n_rows, s.out_stride_head, s.heads, head_dim)) return PLC_E_INVALID;     // results on top of each other
         a.set[i] = TurnSet{static_cast<const uint8_t*>(s.x_dev), static_cast<uint8_t*>(s.out_dev), s.x_stride_row * esz, s.x_stride_head * esz, s.out_stride_row * esz,
                            s.out_stride_head * esz, s.heads, rotary->dim, 0, 0};
     }
@@ -450,7 +453,7 @@ plc_status plc_pages_append(const plc_page_pool* pool, int32_t layer, const plc_
     if (t->n_heads > 0 && t->q_dev == t->out_dev &&
         ((t->n_rows > 1 && t->q_stride_row != t->out_stride_row) || (t->n_heads > 1 && t->q_stride_head != t->out_stride_head)))
         return PLC_E_INVALID;
-    if ((t->n_heads > 0 && t->n_rows > 1 && t->out_stride_row == 0) || (t->n_heads > 1 && t->out_stride_head == 0)) return PLC_E_INVALID;
+    if (t->n_heads > 0 && t->n_rows > 0 && !runs_apart(t->out_stride_row, t->n_rows, t->out_stride_head, t->n_heads, p.d)) return PLC_E_INVALID;
     if (t->n_rows == 0) return PLC_OK;
     a.set[0] = TurnSet{static_cast<const uint8_t*>(t->q_dev), static_cast<uint8_t*>(t->out_dev), t->q_stride_row * esz, t->q_stride_head * esz, t->out_stride_row * esz,
                        t->out_stride_head * esz, t->n_heads, dim, 0, 0};

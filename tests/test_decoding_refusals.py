@@ -262,3 +262,28 @@ def test_weights_on_top_of_each_other_are_refused(lib):
                           (100, 299, plc.E_INVALID)):
         assert lib.plc_pages_weigh(C.byref(pool(L=1)), 0, C.byref(book()), C.byref(q), C.c_float(1.0), C.c_float(1.0), C.byref(serving.Weights(B, row, 0, head, 100)), C.c_void_p(WS),
                                    C.c_uint64(1 << 20), C.c_void_p(A), None) == rc, (row, head)
+
+
+def test_results_on_top_of_each_other_are_refused(lib):
+    """Turned rows and heads, against every pair of runs; so many rows that only the heads can be gone through."""
+    rng = np.random.default_rng(2)
+    answers = set()
+    for i in range(3000):
+        rows, heads, d = int(rng.integers(1, 6)), int(rng.integers(1, 6)), 2 * int(rng.integers(1, 5))
+        row, head = (int(x) for x in rng.integers(-6 * d, 6 * d + 1, 2))
+        starts = sorted(r * row + h * head for r in range(rows) for h in range(heads))
+        apart = all(b - a >= d for a, b in zip(starts, starts[1:]))
+        # the second set is looked at behind the first and is off its boundary, so that nothing is launched
+        t = dict(x_dev=A, x_stride_row=4096, x_stride_head=256, heads=heads)
+        s = (serving.RotarySet * 2)(serving.RotarySet(out_dev=B, out_stride_row=row, out_stride_head=head, **t),
+                                    serving.RotarySet(out_dev=WS + 1, out_stride_row=1 << 20, out_stride_head=64, **t))
+        rc = lib.plc_rotary_apply(C.byref(rotary(dim=2)), s, 2, C.c_void_p(A), rows, d, plc.OUT_F16, 0, None)
+        assert rc == (plc.E_ALIGN if apart else plc.E_INVALID), (rows, heads, d, row, head)
+        answers.add((apart, abs(row) > abs(head), row < 0, head < 0))
+    assert len(answers) == 16
+    s = (serving.RotarySet * 2)(serving.RotarySet(A, B, 64, 64, 128, (1 << 36) + 64, 2), serving.RotarySet(A, WS + 1, 64, 64, 1 << 20, 64, 1))
+    assert lib.plc_rotary_apply(C.byref(rotary()), s, 2, C.c_void_p(A), 0x7fffffff, 64, plc.OUT_F16, 0, None) == plc.E_ALIGN     # between the rows
+    s[0].out_stride_head += 64
+    assert lib.plc_rotary_apply(C.byref(rotary()), s, 2, C.c_void_p(A), 0x7fffffff, 64, plc.OUT_F16, 0, None) == plc.E_INVALID
+    for kw in (dict(out_stride_head=63), dict(out_stride_row=511), dict(out_stride_row=64)):
+        assert lib.plc_pages_append(C.byref(pool()), 0, C.byref(book()), None, C.byref(tokens(**kw)), C.c_void_p(A), None) == plc.E_INVALID, kw
