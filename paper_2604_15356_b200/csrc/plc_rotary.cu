@@ -89,8 +89,9 @@ __device__ __forceinline__ float2 turn_of(const TurnArgs& a, int pos, int pair) 
     return make_float2(c * a.scale, a.back ? -s * a.scale : s * a.scale);
 }
 
-// Where row i stands: its session's position and the place of its key, in bytes from the layer's first one (-1: nowhere).  A warp calls it; false where
-// the row is in no range.
+// Where row i stands: its session's position and the place of its key, in bytes from the layer's first one (kNowhere: it has none; offsets are
+// multiples of 16, of either sign).  A warp calls it; false where the row is in no range.
+constexpr int64_t kNowhere = -1;
 __device__ __forceinline__ bool place_of(const TurnArgs& a, const PoolDev& p, const BookDev& b, int i, int* pos, int64_t* to, uint32_t* status) {
     const int s = session_of_row(a.begin, b.rows, i);
     if (s < 0) return false;
@@ -98,8 +99,8 @@ __device__ __forceinline__ bool place_of(const TurnArgs& a, const PoolDev& p, co
     const long long t = (long long)len + (i - a.begin[s]);
     int page = -1;
     if (len >= 0 && t < most_positions(b, p)) page = b.table[(int64_t)s * b.max_pages + t / p.page_pos];
-    *to = page >= 0 && page < p.n_pages && b.ref[page] == 1 ? (int64_t)page * p.spage + (int64_t)(t % p.page_pos) * p.sp : -1;
-    if (*to == -1 && (threadIdx.x & 31) == 0) atomicOr(status, kStRange);
+    *to = page >= 0 && page < p.n_pages && b.ref[page] == 1 ? (int64_t)page * p.spage + (int64_t)(t % p.page_pos) * p.sp : kNowhere;
+    if (*to == kNowhere && (threadIdx.x & 31) == 0) atomicOr(status, kStRange);
     *pos = a.pos ? a.pos[i] : (int)t;
     return true;
 }
@@ -125,7 +126,7 @@ __global__ void __launch_bounds__(kRowThreads, 8) turn_rows_kernel(const __grid_
     const int i = (int)(at / a.shares), share = (int)(at - (long long)i * a.shares);
     if (i >= a.rows) return;
     int pos;
-    int64_t row_to = -1;
+    int64_t row_to = kNowhere;
     if (PAGES) {
         if (!place_of(a, p, b, i, &pos, &row_to, status)) return;
     } else pos = a.pos[i];
@@ -133,14 +134,14 @@ __global__ void __launch_bounds__(kRowThreads, 8) turn_rows_kernel(const __grid_
     for (int k = lane; k < a.pairs; k += 32) turn[k] = turn_of(a, pos, k);
     __syncwarp();
     auto address = [&](int t, int h) -> uint8_t* {                              // of a head of set t where it goes; null: nowhere
-        if (PAGES && t > 0) return row_to < 0 ? nullptr : p.base + (int64_t)a.layer * p.sl + (t == 2 ? p.skv : 0) + row_to + (int64_t)h * p.sh;
+        if (PAGES && t > 0) return row_to == kNowhere ? nullptr : p.base + (int64_t)a.layer * p.sl + (t == 2 ? p.skv : 0) + row_to + (int64_t)h * p.sh;
         return a.set[t].out + (int64_t)i * a.set[t].os_row + (int64_t)h * a.set[t].os_head;
     };
 #pragma unroll 1
     for (int t = 0; t < a.sets; ++t) {
         const TurnSet& s = a.set[t];
         const int lo = s.heads * share / a.shares, hi = s.heads * (share + 1) / a.shares;
-        if (lo == hi || (PAGES && t > 0 && row_to < 0)) continue;
+        if (lo == hi || (PAGES && t > 0 && row_to == kNowhere)) continue;
         const uint8_t* from = s.x + (int64_t)i * s.xs_row;
         const int turned = s.dim / W / (INTER ? 1 : 2), wide = min(s.per_head, 32), abreast = 32 / wide, h0 = lo + lane / wide;
         const int64_t half = (int64_t)s.dim / 2 * (int)sizeof(T);
@@ -265,7 +266,7 @@ template <class T, bool INTER, bool PAGES>
 __global__ void __launch_bounds__(kTurnThreads) turn_parts_kernel(const __grid_constant__ TurnArgs a, const __grid_constant__ PoolDev p, const __grid_constant__ BookDev b,
                                                                   uint32_t* status) {
     extern __shared__ float2 turn[];              // [rows of the block][pairs] cosine, sine
-    __shared__ int64_t row_to[kMostRows];         // where a row's key goes; -1: nowhere
+    __shared__ int64_t row_to[kMostRows];         // where a row's key goes, or kNowhere
     __shared__ int row_pos[kMostRows];            // its position; the row is in some range
     __shared__ bool row_in[kMostRows];
     const int tid = threadIdx.x, r0 = blockIdx.x * a.rows_block, rows = min(a.rows_block, a.rows - r0);
@@ -274,7 +275,7 @@ __global__ void __launch_bounds__(kTurnThreads) turn_parts_kernel(const __grid_c
         const int w = tid >> 5;
         if (w < rows) {
             int pos = 0;
-            int64_t to = -1;
+            int64_t to = kNowhere;
             const bool in = place_of(a, p, b, r0 + w, &pos, &to, status);
             if ((tid & 31) == 0) { row_to[w] = to; row_in[w] = in; row_pos[w] = pos; }
         }
@@ -290,7 +291,7 @@ __global__ void __launch_bounds__(kTurnThreads) turn_parts_kernel(const __grid_c
         for (int i = 1; i < kMostSets; ++i) t += i < a.sets && v >= a.set[i].first;
         const TurnSet& s = a.set[t];
         const int w = v - s.first, h = w / s.per_head, e = w - h * s.per_head;
-        if (PAGES && (t > 0 ? row_to[r] < 0 : !row_in[r])) continue;
+        if (PAGES && (t > 0 ? row_to[r] == kNowhere : !row_in[r])) continue;
         const T* from = reinterpret_cast<const T*>(s.x + (int64_t)(r0 + r) * s.xs_row + (int64_t)h * s.xs_head);
         T* to = reinterpret_cast<T*>(PAGES && t > 0 ? p.base + (int64_t)a.layer * p.sl + (t == 2 ? p.skv : 0) + row_to[r] + (int64_t)h * p.sh
                                                     : s.out + (int64_t)(r0 + r) * s.os_row + (int64_t)h * s.os_head);

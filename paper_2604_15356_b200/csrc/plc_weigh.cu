@@ -37,6 +37,7 @@ template <> __device__ __forceinline__ void mma16816<__nv_bfloat16>(float* c, ui
 }
 
 constexpr int kThreads = 128, kWarps = kThreads / 32, kTile = 16;
+constexpr int64_t kNoKey = -1;                    // no offset: those are multiples of 16 bytes, of either sign
 
 // NT: tiles of eight columns (a column: an entry's query head) that a warp has in registers.
 // Blocks an SM: what the registers of the keys on their way, of the queries and of the rest leave.
@@ -97,25 +98,25 @@ __global__ void __launch_bounds__(kThreads, kPerSm<D, NT>) weigh_kernel(const __
     int tiles = (x.len + kTile - 1) / kTile, h = (int)(rest / tiles), tile = (int)(rest - (long long)h * tiles);
     const int quad = lane >> 2, part = lane & 3;
     const float c2 = a.scale * kLog2e;
-    // Where the vectors of tile i of the item stand, as far as this lane's position is concerned (-1: it has none).  Looked up two tiles ahead, loaded one ahead.
+    // Where the vectors of tile i of the item stand, as far as this lane's position is concerned (kNoKey: it has none).  Looked up two tiles ahead, loaded one ahead.
     auto look_up = [&](int i) -> int64_t {
         const int t = i * kTile + (lane & 15);
-        if (t >= x.len) return -1;
+        if (t >= x.len) return kNoKey;
         const int page = b.table[(int64_t)s * b.max_pages + t / p.page_pos];
-        if (page < 0 || page >= p.n_pages) { atomicOr(status, kStRange); return -1; }
+        if (page < 0 || page >= p.n_pages) { atomicOr(status, kStRange); return kNoKey; }
         return (int64_t)a.layer * p.sl + (int64_t)page * p.spage + (int64_t)(t % p.page_pos) * p.sp + (int64_t)h * p.sh;
     };
     auto fetch = [&](int64_t off, uint4 (&k0)[B], uint4 (&k1)[B]) {
         const int64_t off0 = __shfl_sync(kFull, off, quad), off1 = __shfl_sync(kFull, off, quad + 8);
 #pragma unroll
         for (int e = 0; e < B; ++e) {
-            k0[e] = off0 < 0 ? make_uint4(0, 0, 0, 0) : __ldcs(reinterpret_cast<const uint4*>(p.base + off0 + e * 64 + part * 16));
-            k1[e] = off1 < 0 ? make_uint4(0, 0, 0, 0) : __ldcs(reinterpret_cast<const uint4*>(p.base + off1 + e * 64 + part * 16));
+            k0[e] = off0 == kNoKey ? make_uint4(0, 0, 0, 0) : __ldcs(reinterpret_cast<const uint4*>(p.base + off0 + e * 64 + part * 16));
+            k1[e] = off1 == kNoKey ? make_uint4(0, 0, 0, 0) : __ldcs(reinterpret_cast<const uint4*>(p.base + off1 + e * 64 + part * 16));
         }
     };
     while (left > 0) {
         const int todo = (int)min(left, (long long)(tiles - tile)), cols = x.n * a.group;
-        int64_t off = look_up(tile), next = todo > 1 ? look_up(tile + 1) : -1;
+        int64_t off = look_up(tile), next = todo > 1 ? look_up(tile + 1) : kNoKey;
         uint4 k0[B], k1[B];
         fetch(off, k0, k1);
         // the queries, a lane its column's run of components and log-sum-exp
@@ -140,7 +141,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm<D, NT>) weigh_kernel(const __
         queries(0);
         for (int i = 0; i < todo; ++i) {
             const int base = (tile + i) * kTile;
-            const bool have0 = __shfl_sync(kFull, off, quad) >= 0, have1 = __shfl_sync(kFull, off, quad + 8) >= 0;
+            const bool have0 = __shfl_sync(kFull, off, quad) != kNoKey, have1 = __shfl_sync(kFull, off, quad + 8) != kNoKey;
             float sum0 = 0.f, sum1 = 0.f;
             const int seen0 = base + quad - (x.len - x.n), seen1 = seen0 + 8;             // entries from this one on see the position
             // sessions of more columns than the call's mean take them in turns
@@ -160,7 +161,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm<D, NT>) weigh_kernel(const __
                 if (col0 + 8 * NT >= cols) {      // the keys are not needed any more
                     off = next;
                     if (i + 1 < todo) fetch(off, k0, k1);
-                    next = i + 2 < todo ? look_up(tile + i + 2) : -1;
+                    next = i + 2 < todo ? look_up(tile + i + 2) : kNoKey;
                 }
 #pragma unroll
                 for (int n = 0; n < NT; ++n)

@@ -829,3 +829,43 @@ def test_captured_graphs_share_nothing(dev):
     for _, got, alone, _, pool, _ in sides:
         pool.check()
         assert all(torch.equal(a, b) for a, b in zip(got, alone))
+
+
+# ---------------------------------------------------------------------------------------------- layouts that go down
+
+def downwards(kv, dims):
+    """(pool, its memory): the same elements with these dimensions going down in memory, as the library's own structures can say it and torch's strides cannot."""
+    store = kv.flip(dims).contiguous()
+    pool, s, base = plc.PagePool(store), list(store.stride()), store.data_ptr()
+    for i in dims:
+        base += (store.shape[i] - 1) * s[i] * store.element_size()
+        s[i] = -s[i]
+    pool._c.view = plc.KVView(base, *s[:5])
+    return pool, store
+
+
+@pytest.mark.parametrize("dims", [(2,), (4,), (0, 1, 2, 3, 4)])
+@pytest.mark.parametrize("d, dim, dtype", [(64, 64, "f16"), (128, 12, "bf16"), (128, 30, "f16")])
+def test_pools_that_go_down_in_memory(dev, d, dim, dtype, dims):
+    """Offsets of either sign: rows of runs of 16 and 4 bytes and component by component, few and many columns, eviction."""
+    rng = np.random.default_rng(d + dim)
+    H, G, L = 2, 2, 2
+    kv, _, table, ref = pages_for(rng, L, H, d, 16, [9, 6], 2, dtype, dev, False)
+    kv = kv.clone()
+    up, (down, store) = plc.PagePool(kv), downwards(kv, dims)
+    rot, book, weight = plc.Rotary(dim, base=100.0), book_of(table, [120, 60], ref, dev), torch.rand(2, L, H, 144, device=dev)
+    for n in (1, 20):
+        q, k, v = (normal(rng, (2 * n, h, d + (dim == 30)), dtype).to(dev) for h in (H * G, H, H))
+        at = slice(-d, None)                                            # (component by component: off 4-byte boundaries)
+        begin, after = i32([0, n, 2 * n], dev), book_of(table, [120 + n, 60 + n], ref, dev)
+        for layer in range(L):
+            a, b = (p.append(layer, book, q[..., at], k[..., at], v[..., at], begin, rotary=rot) for p in (up, down))
+            assert torch.equal(a, b)
+            lse = torch.full((2 * n, H * G), 5.0, device=dev)
+            wa, wb = (p.attention_weights(layer, after, a, lse, begin, weight.clone()) for p in (up, down))
+            assert torch.allclose(wa, wb, rtol=2.0 ** -20, atol=0) and not torch.equal(wa, weight)
+        assert torch.equal(store.flip(dims), kv)
+    a, b = (p.evict(after, weight, 70, recent=5) for p in (up, down))
+    assert torch.equal(a[1], b[1]) and torch.equal(a[0].table, b[0].table) and torch.equal(store.flip(dims), kv) and a[0].len.tolist() == [70, 70]
+    up.check()
+    down.check()
