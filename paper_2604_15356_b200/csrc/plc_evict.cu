@@ -184,7 +184,7 @@ __device__ __forceinline__ void copy_weights(const float* w, float* out, int n, 
 }
 
 struct SelectShared {
-    int bins[256];
+    alignas(16) int bins[256];                    // counted by ints, read by int4
     int above[kSelectWarps], equal[kSelectWarps];
     uint32_t prefix;
     int want;

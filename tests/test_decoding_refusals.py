@@ -287,3 +287,13 @@ def test_results_on_top_of_each_other_are_refused(lib):
     assert lib.plc_rotary_apply(C.byref(rotary()), s, 2, C.c_void_p(A), 0x7fffffff, 64, plc.OUT_F16, 0, None) == plc.E_INVALID
     for kw in (dict(out_stride_head=63), dict(out_stride_row=511), dict(out_stride_row=64)):
         assert lib.plc_pages_append(C.byref(pool()), 0, C.byref(book()), None, C.byref(tokens(**kw)), C.c_void_p(A), None) == plc.E_INVALID, kw
+
+
+def test_shared_memory_that_is_read_in_wide_words_is_aligned():
+    """Arrays of ints that kernels read as int4 or uint4 say so: where the compiler puts the next variable is no promise."""
+    import os
+    import re
+    src = os.path.join(os.path.dirname(plc.__file__), "csrc")
+    for name, array in (("plc_evict.cu", "bins"), ("plc_logits.cuh", "order")):
+        text = open(os.path.join(src, name)).read()
+        assert re.search(r"(alignas\(16\)|__align__\(16\)) (int|uint32_t) %s\[" % array, text), (name, array)
