@@ -869,3 +869,31 @@ def test_pools_that_go_down_in_memory(dev, d, dim, dtype, dims):
     assert torch.equal(a[1], b[1]) and torch.equal(a[0].table, b[0].table) and torch.equal(store.flip(dims), kv) and a[0].len.tolist() == [70, 70]
     up.check()
     down.check()
+
+
+# ---------------------------------------------------------------------------------------------- many small rows
+
+@pytest.mark.parametrize("dtype, inter, heads, d, dim", [("f16", False, (1,), 32, 32), ("bf16", True, (2, 2), 32, 32), ("f32", True, (2, 2), 80, 20), ("f16", False, (1, 1), 34, 8),
+                                                         ("bf16", False, (1, 2), 64, 48)])
+def test_turns_of_more_small_rows_than_blocks_stay(dev, dtype, inter, heads, d, dim):
+    """Rows that share a warp, so many that each block goes on to rows behind its first ones several times; a last round that is not full; forwards, back, onto itself."""
+    N = 100003
+    gen = torch.Generator(device=dev).manual_seed(d + dim)
+    rot = plc.Rotary(dim, base=300.0, interleaved=inter, scale=1.5)
+    pos = torch.randint(-(1 << 20), 1 << 20, (N,), generator=gen, device=dev, dtype=torch.int32)
+    xs = tuple(torch.randn(N, h, d, generator=gen, device=dev).to(TYPES[dtype]) for h in heads)
+    t = pos.double()[:, None] * torch.tensor(rot.frequencies, dtype=torch.float64, device=dev)
+    c, s, f = 1.5 * t.cos()[:, None], 1.5 * t.sin()[:, None], torch.finfo(TYPES[dtype])
+    for back in (False, True):
+        got = rot.apply(xs, pos, back=back)
+        for x, g in zip(xs, got):
+            y = x.double()
+            a, b = (y[..., 0:dim:2], y[..., 1:dim:2]) if inter else (y[..., :dim // 2], y[..., dim // 2:dim])
+            ga, gb = (g[..., 0:dim:2], g[..., 1:dim:2]) if inter else (g[..., :dim // 2], g[..., dim // 2:dim])
+            sign = -1.0 if back else 1.0
+            for have, want in ((ga, a * c - sign * b * s), (gb, b * c + sign * a * s)):
+                tol = 2.0 ** -21 * 1.5 * (a.abs() + b.abs()) + f.eps / 2 * want.abs() + f.smallest_normal * f.eps / 2
+                assert bool(((have.double() - want).abs() <= tol).all())
+            assert torch.equal(g[..., dim:], x[..., dim:])
+    mine = tuple(x.clone() for x in xs)
+    assert all(torch.equal(a, b) for a, b in zip(rot.apply(mine, pos, back=True, out=mine), got))
