@@ -3,7 +3,7 @@ the plc_pages_*, plc_tree_attention, plc_beam_*, plc_rotary_* and plc_token_logp
 
 As in the rest of the binding nothing is computed here: tensors become pointers, and the work runs on the current stream
 of the tensors' device.  Results and workspaces are allocated by torch on that stream, so that calls on several streams
-and captured graphs do not share any.
+and captured graphs do not share any.  No call is recorded for autograd.
 """
 import ctypes as C
 import math
@@ -537,7 +537,8 @@ class Rotary:
 
     def apply(self, x, pos, back=False, out=None):
         """x [N][heads][d], or up to four of them (queries and keys, any strides with the components contiguous), turned at positions pos [N] (int32);
-        back: by the opposite angles, the gradient.  out: where the results go, x itself is allowed."""
+        back: by the opposite angles, which turns a gradient of the results into x's.  Nothing is recorded for autograd, also where x requires a gradient:
+        a function of the caller's joins the two.  out: where the results go, x itself is allowed."""
         import torch
         where, dev = "plc_rotary_apply", self.device
         single = isinstance(x, torch.Tensor)
@@ -565,6 +566,8 @@ class Rotary:
             got.append(o)
             sets += (t.data_ptr(), o.data_ptr(), row, head, out_row, out_head, heads)     # a plc_rotary_set, seven 64-bit words
         if N:
+            if dev.type != "cuda":
+                raise PlcError(E_INVALID, where)
             rc = _run(dev, _lib().plc_rotary_apply, self._by, _SETS[len(xs)].pack(*sets), len(xs), pos.data_ptr(), N, d, kind, 1 if back else 0)
             if rc:
                 raise PlcError(rc, where)

@@ -297,3 +297,11 @@ def test_shared_memory_that_is_read_in_wide_words_is_aligned():
     for name, array in (("plc_evict.cu", "bins"), ("plc_logits.cuh", "order")):
         text = open(os.path.join(src, name)).read()
         assert re.search(r"(alignas\(16\)|__align__\(16\)) (int|uint32_t) %s\[" % array, text), (name, array)
+
+
+def test_turns_of_tensors_on_the_host_are_refused():
+    import torch
+    r = plc.Rotary(8, device="cpu")
+    with pytest.raises(plc.PlcError) as e:
+        r.apply(torch.zeros(3, 2, 16), torch.zeros(3, dtype=torch.int32))
+    assert e.value.code == plc.E_INVALID
