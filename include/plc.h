@@ -493,8 +493,8 @@ typedef struct {
 } plc_rotary_set;
 
 /* Turns the rows of up to four sets (queries and keys, say) at positions pos_dev [n_rows]; back: by the opposite angles, which is the gradient
- * of the turn.  dtype as plc_page_pool; head_dim <= 1024, all sets together at most 4096 heads.  Arithmetic is binary32, the angle is exact to
- * 2^-33 turns and its sine and cosine are binary32, the result is rounded once.  16 bytes at a time where strides, addresses and dim allow
+ * of the turn.  dtype as plc_page_pool; head_dim <= 1024, all sets together at most 4096 heads.  Arithmetic is binary32: the angle is off by at most
+ * 2^-25 turns at any position (2^-26 by its rounding to binary32, below 2^-32 before), its sine and cosine are binary32, the result is rounded once.  16 bytes at a time where strides, addresses and dim allow
  * it, else 4, else component by component. */
 plc_status plc_rotary_apply(const plc_rotary* rotary, const plc_rotary_set* sets, int32_t n_sets, const int32_t* pos_dev, int32_t n_rows,
                             int32_t head_dim, int32_t dtype, int32_t back, void* stream);

@@ -2,8 +2,9 @@
 // beside them (plc_pages_append).
 //
 // A pair (x_a, x_b) of components at position pos becomes s (x_a cos t - x_b sin t, x_b cos t + x_a sin t), t = pos f_i.  The frequency is held in turns a
-// position as a fraction of 64 bits, so that the product with the position, cut to its low 64 bits, is the angle modulo a turn to 2^-33 turns at any
-// position that an int holds: no product in 64-bit floating point and no reduction.  Its sine and cosine are formed once a row and pair, for all heads.
+// position as a fraction of 64 bits, so that the product with the position, cut to its low 64 bits, is the angle modulo a turn to 2^-32 turns at any
+// position that an int holds: no product in 64-bit floating point and no reduction.  The functions take it in binary32, which is off by up to 2^-26 turns (half a step just
+// below half a turn, 9e-8 rad), about as much as sines of binary32 are off anyway.  They are formed once a row and pair, for all heads.
 //
 // Bound by HBM where rows are many (each component read and written once, 16 bytes a thread and access), by the launch where they are few.  A block takes a few
 // rows with all their heads.
