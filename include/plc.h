@@ -563,8 +563,10 @@ plc_status plc_pages_weigh_workspace(const plc_page_pool* pool, int32_t sessions
  * The new length is the budget, pages behind it are released; of the pages that the row still has, those with other holders are replaced by fresh ones, the
  * lowest-numbered free ones of `in`, in order.  Other rows stay as they are, what they hold behind their length too, and their weights are copied.
  * Keys that were turned stay turned: later tokens are given their positions by plc_new_tokens.pos_dev, since len + i no longer counts what was evicted.
- * If the free pages do not suffice, bit 1 is set and out is what in was, weights and pool as before.  A length out of range or above n_pos, and a page number
- * out of range, leave the row as it is (bit 32).  n_layers*n_kv_heads*rows < 2^30.  workspace: plc_pages_evict_workspace bytes. */
+ * If the free pages do not suffice, bit 1 is set and out is what in was, weights and pool as before.  A length out of range leaves the row as it is (bit 32), and so do,
+ * of a row with more than its budget, a length above n_pos and a page number out of range among those of its positions;
+ * elsewhere a page number out of range stays and sets bit 32, and of a length above n_pos the first n_pos weights are copied.  n_layers*n_kv_heads*rows < 2^30.
+ * workspace: plc_pages_evict_workspace bytes. */
 plc_status plc_pages_evict(const plc_page_pool* pool, const plc_page_book* in, const plc_weights* weights, const int32_t* budget_dev, int32_t budget,
                            int32_t recent, const plc_page_book* out, float* out_weights_dev, void* workspace_dev, uint64_t workspace_bytes,
                            uint32_t* status_dev, void* stream);

@@ -528,7 +528,7 @@ plc_status plc_pages_evict(const plc_page_pool* pool, const plc_page_book* in, c
     const long long lanes = (long long)i.rows * p.L * p.H;
     uint8_t* ws = static_cast<uint8_t*>(workspace_dev);
     const int log2 = piece_log2(p.d * p.esz), piece = 1 << log2;
-    // Weights in shared memory: all of a row of 4096, as many as there is room for where few blocks run anyway (five rows of up to 13423 positions in 4 heads: 68 us without, 59 with).
+    // Weights in shared memory: rows of up to 8192, as long as there is room for (49152) where few blocks run anyway (five rows of up to 13423 positions in 4 heads: 68 us without, 59 with).
     const int most_held = lanes <= 4 * sm_count() ? 49152 : 8192, held = weights->n_pos < most_held ? weights->n_pos : most_held;
     // The plan is a block of the selection where it has little to look at, else a launch of its own, and the rows' blocks count their pages (31 rows of 4176 pages of one
     // position: 308 us in the selection, 116 so; where 16 rows have 65 pages each a launch more costs 2 us).

@@ -435,7 +435,7 @@ class PagePool:
             need = self._need_bytes[(book.rows, n_pos)] = b.value
         new, _ = PageBook._new(book.rows, book.max_pages, self.n_pages, dev)
         (rows, layers, heads, _), n = weight.shape, weight.numel() + 3 & ~3
-        store = torch.empty_strided((n + (need + 3) // 4,), (1,), dtype=torch.float32, device=dev)     # the workspace, a seventeenth of the weights, behind them
+        store = torch.empty_strided((n + (need + 3) // 4,), (1,), dtype=torch.float32, device=dev)     # the workspace behind them: 18, 13 or 8 times smaller (pieces of 128, 64, 32 positions), and 4 bytes for each page of the pool and of the rows
         out = store.as_strided((rows, layers, heads, n_pos), (layers * heads * n_pos, heads * n_pos, n_pos, 1), 0)
         at = store.data_ptr()
         _check(_run(dev, api.plc_pages_evict, self._by, a, C.byref(w), budgets, scalar, recent, new._by, at, at + 4 * n, need, self._word), where)
