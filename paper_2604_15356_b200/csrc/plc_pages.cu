@@ -297,6 +297,7 @@ __device__ __forceinline__ void copy_counts(const PoolDev& p, const BookDev& in,
 template <int THREADS>
 __device__ __forceinline__ void keep_move(const PoolDev& p, int lanes_log2, const BookDev& in, const int32_t* paths, const int32_t* n_path, int stride, int s, int share,
                                           int shares) {
+    constexpr int64_t kStays = -1;                // no offset: those are multiples of 16, of either sign
     __shared__ int64_t from[kKeepBatch], to[kKeepBatch];
     const int n = n_path[s], len = in.len[s];
     const int32_t* path = paths + (long long)s * stride;
@@ -308,7 +309,7 @@ __device__ __forceinline__ void keep_move(const PoolDev& p, int lanes_log2, cons
         __syncthreads();
         for (int i = threadIdx.x; i < m; i += THREADS) {
             const int a = len + path[i0 + i], b = len + i0 + i;
-            from[i] = a == b ? -1 : (int64_t)row[a / p.page_pos] * p.spage + (int64_t)(a % p.page_pos) * p.sp;
+            from[i] = a == b ? kStays : (int64_t)row[a / p.page_pos] * p.spage + (int64_t)(a % p.page_pos) * p.sp;
             to[i] = (int64_t)row[b / p.page_pos] * p.spage + (int64_t)(b % p.page_pos) * p.sp;
         }
         __syncthreads();
@@ -320,10 +321,10 @@ __device__ __forceinline__ void keep_move(const PoolDev& p, int lanes_log2, cons
                 uint4 x[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
-                    if (i + k < m && from[i + k] >= 0) x[k] = *reinterpret_cast<const uint4*>(base + from[i + k]);
+                    if (i + k < m && from[i + k] != kStays) x[k] = *reinterpret_cast<const uint4*>(base + from[i + k]);
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
-                    if (i + k < m && from[i + k] >= 0) *reinterpret_cast<uint4*>(base + to[i + k]) = x[k];
+                    if (i + k < m && from[i + k] != kStays) *reinterpret_cast<uint4*>(base + to[i + k]) = x[k];
             }
         }
     }

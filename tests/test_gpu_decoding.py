@@ -897,3 +897,32 @@ def test_turns_of_more_small_rows_than_blocks_stay(dev, dtype, inter, heads, d, 
             assert torch.equal(g[..., dim:], x[..., dim:])
     mine = tuple(x.clone() for x in xs)
     assert all(torch.equal(a, b) for a, b in zip(rot.apply(mine, pos, back=True, out=mine), got))
+
+
+@pytest.mark.parametrize("dims", [(2,), (4,), (0, 1, 2, 3, 4)])
+def test_books_of_pools_that_go_down_in_memory(dev, dims):
+    """Attention of few and of many rows, accepted drafts that move, forks that copy a page, and pages that move together."""
+    rng = np.random.default_rng(5)
+    kv, _, table, ref = pages_for(rng, 2, 2, 64, 16, [9, 6], 6, "f16", dev, False, cols=9)
+    kv = kv.clone()
+    up, (down, store) = plc.PagePool(kv), downwards(kv, dims)
+    book = book_of(table, [100, 50], ref, dev)
+    for n in (1, 40):
+        q, begin = normal(rng, (2 * n, 8, 64), "f16").to(dev), i32([0, n, 2 * n], dev)
+        (a, la), (b, lb) = (p.tree_attention(1, book, q, begin) for p in (up, down))
+        # two roundings of values below 4, sums of up to 140 products in another order
+        assert torch.allclose(a.float(), b.float(), rtol=0, atol=2.0 ** -8) and torch.allclose(la, lb, rtol=2.0 ** -16)
+    path, count = i32([[0, 3, 7, 20], [2, 5, 0, 0]], dev), i32([4, 2], dev)
+    a, b = (p.keep(book, path, count) for p in (up, down))
+    assert a.len.tolist() == b.len.tolist() == [104, 52] and torch.equal(store.flip(dims), kv)
+    parent, room = i32([0, 0, 1], dev), i32([10, 3, 7], dev)
+    a, b = (p.fork(x, parent, room) for p, x in ((up, a), (down, b)))
+    assert torch.equal(a.table, b.table) and torch.equal(a.ref, b.ref)
+    (a, ma), (b, mb) = (p.compact(x) for p, x in ((up, a), (down, b)))
+    assert torch.equal(a.table, b.table) and torch.equal(ma, mb)
+    for s in range(3):                                                      # what the rows hold (pages that nobody holds may have been left differently)
+        t = torch.arange(int(a.len[s]), device=dev)
+        at = a.table[s].long()[t // 16]
+        assert torch.equal(kv[:, :, at, :, t % 16], store.flip(dims)[:, :, at, :, t % 16])
+    up.check()
+    down.check()
