@@ -532,6 +532,7 @@ class Rotary:
         self.dim, self.interleaved, self.scale, self.frequencies = dim, bool(interleaved), float(scale), f
         self.turns = torch.tensor(signed, dtype=torch.int64).to(device)
         self.device = self.turns.device
+        self._on_gpu = self.turns.is_cuda
         self._c = RotaryC(self.turns.data_ptr(), dim, int(self.interleaved), self.scale)
         self._by = C.byref(self._c)
 
@@ -566,7 +567,7 @@ class Rotary:
             got.append(o)
             sets += (t.data_ptr(), o.data_ptr(), row, head, out_row, out_head, heads)     # a plc_rotary_set, seven 64-bit words
         if N:
-            if dev.type != "cuda":
+            if not self._on_gpu:
                 raise PlcError(E_INVALID, where)
             rc = _run(dev, _lib().plc_rotary_apply, self._by, _SETS[len(xs)].pack(*sets), len(xs), pos.data_ptr(), N, d, kind, 1 if back else 0)
             if rc:
