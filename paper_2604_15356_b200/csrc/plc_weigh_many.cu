@@ -5,10 +5,11 @@
 // and goes through the row tiles that see any of it; Q and S have two buffers each, Q four where there are many row tiles of up to 128 components.  Boxes of pages and of queries where their layouts allow it,
 // else pieces of 16 bytes.
 //
-// Bound by the exponentials (16 a clock and SM; the products need half as long): 2048 tokens of 8 x 4 heads of 128 behind 8192 positions 243 us on the device (156 GFLOP, 640 TFLOP/s;
-// the exponentials' unit is busy 0.67 of the time, the tensor pipe 0.33, at the clock that the power leaves: 950 W).  A step, 128 rows by 256 positions, takes 2950 clocks: 2050 of the
-// unit, 250 around them in the sums, 300 waiting, 230 between steps.  Two threads a position were slower (297 us against 263 then), a quarter of the exponentials by a
-// polynomial hardly faster (241 against 249).
+// Bound by the exponentials (16 a clock and SM; the products need half as long) and by what is serial with them: 2048 tokens of 8 x 4 heads of 128 behind 8192 positions 243 us on the
+// device (156 GFLOP, 640 TFLOP/s; the exponentials' unit is busy 0.67 of the time, the tensor pipe 0.33).  A step, 128 rows by 256 positions, takes 3160 clocks: 2300 to 2700 in the sums, of
+// which the unit needs 2048, 170 to 580 waiting, 150 to 200 between steps; 8000 clocks pass before the first.  The power is not what bounds it: by the SMs' own counters calls in a row run at
+// 1.83 GHz, where the unit alone would need 141 us (one call after a second's pause at 1.64 GHz).  Two threads a position were slower (297 us against 263 then), a quarter of the exponentials
+// by a polynomial hardly faster (241 against 249).
 // Or, where there is one row tile, by HBM: 32 sessions of up to 4096 positions, 5 tokens of 8 x 4 heads of 128: 44 us (177 MB, 4.1 TB/s).  Tiles of 128 positions with four
 // buffers of keys took 76 with one warp for all copies against 54.
 //
