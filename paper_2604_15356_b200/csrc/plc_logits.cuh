@@ -344,7 +344,7 @@ __device__ __forceinline__ void row_part(const RowArgs& a, int row, int part) {
         const int at = column(w, i) + (lane >> 3) * 256 + l * 8 + (lane & 7);
         return lane < 8 * groups && at < c1 ? ((unsigned long long)order_bits(widen(x0[at])) << 32) | (uint32_t)~at : 0ull;
     };
-    if (a.k > kRowThreads / 2) {
+    if (a.k > kRowThreads / 2 && chunk > 1) {     // (with one chunk a lane it is the same bound)
         // With as many places as lanes the least of the lanes' maxima is the bound, and five times as many logits reach it as are wanted, now and then more than there is room
         // for (1024 rows of 128256, 128 of each: 555 us).  One that goes by the lanes' chunks is nearer to the k-th largest (119 us; for 64 of each it was 100 instead of 89, 85 by now).
         float* list = reinterpret_cast<float*>(found);
