@@ -926,3 +926,64 @@ def test_books_of_pools_that_go_down_in_memory(dev, dims):
         assert torch.equal(kv[:, :, at, :, t % 16], store.flip(dims)[:, :, at, :, t % 16])
     up.check()
     down.check()
+
+
+# ---------------------------------------------------------------------------------------------- more than 2^31 elements
+
+def test_turns_of_more_than_32_bits_of_elements(dev):
+    """Rows by a warp, rows that share one, and component by component: the last rows of a large tensor are those of a small one."""
+    for heads, d, dtype in ((40, 128, "bf16"), (1, 32, "f16"), (3, 31, "f16")):
+        N = (1 << 31) // (heads * d) + 1000
+        rot = plc.Rotary(30 if d == 31 else d, base=100.0)
+        x = torch.empty(N, heads, d, dtype=TYPES[dtype], device=dev)
+        x[-2000:].normal_()
+        x[:100].normal_()
+        pos = torch.arange(N, dtype=torch.int32, device=dev) % 5000
+        y = rot.apply(x, pos)
+        for part in (slice(0, 100), slice(N - 2000, N)):
+            assert torch.equal(y[part], rot.apply(x[part].clone(), pos[part].clone())), (heads, d)
+        del x, y
+
+
+def test_append_to_pages_and_from_rows_that_are_far_apart(dev):
+    far = (1 << 31) + 64
+    store = torch.zeros(2 * far + 4 * 8 * 64, dtype=torch.float16, device=dev)
+    kv = store.as_strided((1, 2, 3, 1, 8, 64), (0, 8 * 64, far, 8 * 64, 64, 1))
+    rows = torch.empty((1 << 31) + 4 * 64, dtype=torch.float16, device=dev)
+    k = rows.as_strided((3, 1, 64), ((1 << 30) + 64, 64, 1))
+    k.normal_()
+    pool, book = plc.PagePool(kv), book_of(np.array([[2, 0, 1]]), [15], np.array([1, 1, 1]), dev)
+    pool.append(0, book, None, k, k, i32([0, 3], dev))
+    pool.check()
+    for i, (page, slot) in enumerate(((0, 7), (1, 0), (1, 1))):              # positions 15, 16, 17 of pages 2, 0, 1
+        assert torch.equal(kv[0, 0, page, 0, slot], k[i, 0]) and torch.equal(kv[0, 1, page, 0, slot], k[i, 0])
+    assert not kv[0, :, 2].any()
+
+
+def test_rows_of_logits_of_more_than_32_bits_of_elements(dev):
+    V = 128256
+    N = (1 << 31) // V + 100
+    x = torch.empty(N, V, dtype=torch.float16, device=dev)
+    x[:10].normal_()
+    x[10:-30] = 0
+    x[-30:].normal_()
+    tokens = torch.arange(N, dtype=torch.int32, device=dev)[:, None] % V
+    got = plc.token_logprobs(x, tokens, 8)
+    score, parent, token = plc.beam_select(x.view(N, 1, V), torch.zeros(N, 1, device=dev), 8)
+    for part in (slice(0, 10), slice(N - 30, N)):
+        want = plc.token_logprobs(x[part].clone(), tokens[part].clone(), 8)
+        # (another number of parts a row: another order of sums)
+        assert torch.equal(got[3][part], want[3]) and torch.equal(token[part], want[3])
+        assert all(torch.allclose(a[part], b, rtol=0, atol=2.0 ** -18) for a, b in zip(got[:3], want[:3])) and torch.allclose(score[part], want[2], rtol=0, atol=2.0 ** -18)
+
+
+def test_eviction_by_weights_that_are_slices(dev):
+    """Rows, layers and heads of a larger tensor, in another order, and one row's weights for all: as if they were copied out."""
+    rng = np.random.default_rng(8)
+    kv, _, table, ref = pages_for(rng, 2, 3, 64, 16, [9, 6], 2, "f16", dev, False)
+    kv, book = kv.clone(), book_of(table, [130, 90], ref, dev)
+    room = torch.rand(4, 3, 5, 200, device=dev)
+    for w in (room[1:3, :2, 1:4, 7:150], room.transpose(0, 1)[:2, 1:3, 2:, :131], room[:1, :2, :3].expand(2, -1, -1, -1), room[:2, :2, :1].expand(-1, -1, 3, -1)):
+        a, b = kv.clone(), kv.clone()
+        (na, wa), (nb, wb) = plc.PagePool(a).evict(book, w, 89, recent=3), plc.PagePool(b).evict(book, w.contiguous(), 89, recent=3)
+        assert torch.equal(wa, wb) and torch.equal(na.table, nb.table) and torch.equal(a, b) and na.len.tolist() == [89, 89] and not torch.equal(a, kv)
